@@ -327,6 +327,112 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
                                  const float *d_min_scale, void *d_out, daf_stream stream);
 
 /*
+ * Operators of a transformer's training step that keep little for the backward pass by construction (the codec above
+ * serves what they do keep).  The same conventions: caller-owned buffers and workspaces, work enqueued on `stream`,
+ * arguments checked on the host before anything is launched.  Results do not depend on the order in which CTAs run:
+ * the same inputs give the same bits.
+ */
+
+/*
+ * Attention, and its backward pass, which recomputes the probabilities instead of keeping them: what a step keeps of
+ * it are q, k, v, the output and one float per row.
+ *   S[i][j] = scale * q_i . k_j,   out_i = sum over visible j of softmax(S[i])[j] v_j,   lse_i = log sum exp S[i][j]
+ * Query i of sequence b sees key j if j < key_lengths[b] (all keys when d_key_lengths is NULL; values are clamped to
+ * [0, keys]) and, when causal, j <= i + keys - queries.  A row that sees no key has out = 0, lse = -inf and takes and
+ * gives no gradient; what lies in k and v beyond a sequence's length is never used, whatever it holds.  Query head h
+ * reads key head h / (heads / kv_heads); the gradients of shared heads are summed over their readers.
+ *   d_q, d_out, d_grad_out, d_grad_q : [batch, queries, heads, head_dim]
+ *   d_k, d_v, d_grad_k, d_grad_v     : [batch, keys, kv_heads, head_dim]
+ * all of dtype, head_dim elements contiguous, the other dimensions by the strides below ({batch, sequence, head}, in
+ * elements; the slices of one packed projection are fine): pointers 16-byte aligned, strides of extents above one multiples of
+ * 16 bytes, at least head_dim and below 2^36.  d_lse: [batch, heads, queries] floats, contiguous.  d_key_lengths: batch
+ * int32.  Softmax statistics and sums are kept in binary32.  16-bit inputs: probabilities and score gradients are rounded
+ * to dtype where they enter the second products; binary32 inputs: binary32 products throughout.
+ * heads a multiple of kv_heads, head_dim a multiple of 8 (DAF_ERR_SHAPE), head_dim <= 128, queries and keys <= 2^24,
+ * batch * heads <= 65535, batch * heads * queries <= 2^32 (DAF_ERR_UNSUPPORTED).  batch, queries or keys == 0 are valid.
+ * daf_attention_grad takes the forward pass's inputs, out and lse; d_workspace: daf_attention_grad_workspace(params)
+ * bytes (0 for bad params), 16-byte aligned.  The gradient buffers must not overlap the inputs.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
+ */
+typedef struct daf_attention_params {
+    uint32_t struct_size;     /* sizeof(daf_attention_params)                  */
+    uint32_t dtype;           /* daf_dtype of every tensor                     */
+    uint32_t batch, queries, keys, heads, kv_heads, head_dim;
+    uint32_t causal;          /* 0 or 1                                        */
+    float    scale;           /* finite; usually 1 / sqrt(head_dim)            */
+    uint32_t reserved[2];     /* 0                                             */
+    uint64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];             /* {batch, sequence, head}  */
+    uint64_t grad_out_stride[3], grad_q_stride[3], grad_k_stride[3], grad_v_stride[3];  /* daf_attention_grad only */
+} daf_attention_params;
+daf_status daf_attention(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
+                         const int32_t *d_key_lengths, void *d_out, float *d_lse, daf_stream stream);
+uint64_t   daf_attention_grad_workspace(const daf_attention_params *params);
+daf_status daf_attention_grad(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
+                              const int32_t *d_key_lengths, const void *d_out, const float *d_lse, const void *d_grad_out,
+                              void *d_grad_q, void *d_grad_k, void *d_grad_v, void *d_workspace, uint64_t workspace_bytes,
+                              daf_stream stream);
+
+/*
+ * The join between two blocks: gate, residual scale and the norms on both sides of it, row by row.
+ *   u = norm(y) * post_weight + post_bias where d_post_weight is given, else u = y
+ *   z = x + residual_scale * gate * u                  (no factor gate where d_gate is NULL)
+ *   h = norm(z) * weight + bias
+ * norm(t) = (t - mean(t)) / sqrt(mean((t - mean(t))^2) + eps) over the row's `width` elements, with mean(t) taken as 0
+ * for DAF_NORM_RMS.  Arithmetic in binary32, one rounding per output; h is taken from z before that rounding.
+ *   d_x, d_y, d_z, d_h : rows * width elements of dtype, row-major; d_z may be d_x, d_h may be d_y.  32-byte aligned for
+ *                        DAF_F32, 16 otherwise.
+ *   d_weight, d_bias, d_post_weight, d_post_bias : width elements of param_dtype (DAF_F32 or dtype), 16-byte aligned;
+ *                        all but d_weight may be NULL (d_post_bias needs d_post_weight).
+ *   d_gate             : gates * width elements of param_dtype: gates == 1 one gate for all rows, gates == G row r uses
+ *                        gate r / (rows / G) (rows a multiple of G); NULL exactly when gates == 0.
+ * width: a positive multiple of 8 (DAF_ERR_SHAPE), at most 8192 (DAF_ERR_UNSUPPORTED).  rows == 0 is a valid call.
+ *
+ * daf_residual_norm_grad: from z and y (the only activations it needs: the row statistics are recomputed) and the
+ * gradients of z (NULL: zero) and h, the gradients of x, y and the parameters.  d_grad_x, d_grad_y: like d_z (d_grad_x
+ * may be d_grad_z or d_grad_h, d_grad_y may be d_y).  Each parameter gradient may be NULL (not wanted) and has the
+ * layout and type of its parameter; sums are kept in binary32.  d_workspace: daf_residual_norm_grad_workspace(params)
+ * bytes (0 for bad params), 16-byte aligned.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
+ */
+typedef enum daf_norm_kind { DAF_NORM_LAYER = 0, DAF_NORM_RMS = 1 } daf_norm_kind;
+typedef struct daf_norm_params {
+    uint32_t struct_size;     /* sizeof(daf_norm_params)                                       */
+    uint32_t dtype;           /* daf_dtype of the activations                                  */
+    uint32_t param_dtype;     /* daf_dtype of weights, biases and gates: DAF_F32 or dtype      */
+    uint32_t kind;            /* daf_norm_kind of both norms                                   */
+    uint64_t rows;
+    uint32_t width;
+    uint32_t gates;           /* 0: no gate, 1: one for all rows, G: one for each rows / G rows */
+    float    residual_scale;
+    float    eps;
+    uint32_t reserved;        /* 0                                                             */
+} daf_norm_params;
+daf_status daf_residual_norm(const daf_norm_params *params, const void *d_x, const void *d_y, const void *d_weight,
+                             const void *d_bias, const void *d_gate, const void *d_post_weight, const void *d_post_bias,
+                             void *d_z, void *d_h, daf_stream stream);
+uint64_t   daf_residual_norm_grad_workspace(const daf_norm_params *params);
+daf_status daf_residual_norm_grad(const daf_norm_params *params, const void *d_z, const void *d_y, const void *d_weight,
+                                  const void *d_gate, const void *d_post_weight, const void *d_post_bias,
+                                  const void *d_grad_z, const void *d_grad_h, void *d_grad_x, void *d_grad_y,
+                                  void *d_grad_weight, void *d_grad_bias, void *d_grad_gate, void *d_grad_post_weight,
+                                  void *d_grad_post_bias, void *d_workspace, uint64_t workspace_bytes, daf_stream stream);
+
+/*
+ * Clipping by the global gradient norm: norm = sqrt(sum of squares over all n tensors), every tensor times
+ * min(1, max_norm / (norm + eps)), rounded to its type.  HOST arrays of n entries: dtypes (daf_dtype of each tensor;
+ * they may differ), d_in, d_out, numel (0 is fine).  d_out[i] may be d_in[i] (in place), otherwise the tensors must
+ * not overlap; d_out == NULL computes the norm alone.  Pointers need the alignment of their element type.  d_norm
+ * (device, one float) receives the norm before clipping; an infinite or NaN norm shows there (the factor is then 0 or
+ * NaN).  Squares are summed in binary32 within a CTA's share and in binary64 across CTAs.  n has no limit (one pair of
+ * launches per 512 tensors).  max_norm, eps >= 0.  d_workspace: daf_clip_norm_workspace(n) bytes, 16-byte aligned.
+ * Errors: INVALID_ARG, CAPACITY (workspace too small), SHAPE (a tensor of more than 2^45 elements), CUDA.
+ */
+uint64_t   daf_clip_norm_workspace(uint32_t n);
+daf_status daf_clip_norm_batch(uint32_t n, const uint32_t *dtypes, const void *const *d_in, void *const *d_out,
+                               const uint64_t *numel, float max_norm, float eps, float *d_norm, void *d_workspace,
+                               uint64_t workspace_bytes, daf_stream stream);
+
+/*
  * Host-side page pool for packed buffers (Sec. 3.4.2: one preallocated contiguous arena,
  * page-granular first-fit allocation; Sec. 3.4.3: every allocation carries an importance,
  * and the least important one is evicted first).  The pool does bookkeeping only: it never

@@ -61,6 +61,23 @@ class daf_store_stats(ctypes.Structure):
                 + [(n, ctypes.c_uint64) for n in ("entries", "kept", "evictions", "resizes", "grows", "shrinks", "moves")])
 
 
+_u64x3 = ctypes.c_uint64 * 3
+
+
+class daf_attention_params(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_uint32) for n in ("struct_size", "dtype", "batch", "queries", "keys", "heads", "kv_heads", "head_dim",
+                                                "causal")]
+                + [("scale", ctypes.c_float), ("reserved", ctypes.c_uint32 * 2)]
+                + [(n, _u64x3) for n in ("q_stride", "k_stride", "v_stride", "out_stride", "grad_out_stride", "grad_q_stride",
+                                         "grad_k_stride", "grad_v_stride")])
+
+
+class daf_norm_params(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_uint32), ("param_dtype", ctypes.c_uint32),
+                ("kind", ctypes.c_uint32), ("rows", ctypes.c_uint64), ("width", ctypes.c_uint32), ("gates", ctypes.c_uint32),
+                ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float), ("reserved", ctypes.c_uint32)]
+
+
 class DafError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -100,6 +117,15 @@ SIGNATURES = {
     "daf_tensor_compress": (ctypes.c_int, [ctypes.c_uint32, _vp, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint32,
                                            ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
     "daf_tensor_decompress": (ctypes.c_int, [ctypes.c_uint32, _vp, ctypes.c_uint64, ctypes.c_uint32, _vp, _vp, _vp]),
+    "daf_attention": (ctypes.c_int, [ctypes.POINTER(daf_attention_params), _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "daf_attention_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_attention_params)]),
+    "daf_attention_grad": (ctypes.c_int, [ctypes.POINTER(daf_attention_params)] + [_vp] * 11 + [ctypes.c_uint64, _vp]),
+    "daf_residual_norm": (ctypes.c_int, [ctypes.POINTER(daf_norm_params)] + [_vp] * 10),
+    "daf_residual_norm_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_norm_params)]),
+    "daf_residual_norm_grad": (ctypes.c_int, [ctypes.POINTER(daf_norm_params)] + [_vp] * 16 + [ctypes.c_uint64, _vp]),
+    "daf_clip_norm_workspace": (ctypes.c_uint64, [ctypes.c_uint32]),
+    "daf_clip_norm_batch": (ctypes.c_int, [ctypes.c_uint32, _vp, _vp, _vp, _vp, ctypes.c_float, ctypes.c_float, _vp, _vp,
+                                           ctypes.c_uint64, _vp]),
     "daf_pool_create": (_vp, [ctypes.c_uint64, ctypes.c_uint64]),
     "daf_pool_destroy": (None, [_vp]),
     "daf_pool_alloc": (ctypes.c_uint64, [_vp, ctypes.c_uint64, ctypes.c_double, _u64p]),
@@ -460,6 +486,226 @@ def tensor_decompress(packed, width: int, min_scale, shape, dtype, stream=None):
     out = _torch().empty(shape, dtype=dtype, device=packed.device)
     daf_tensor_decompress(packed, width, min_scale, out, stream)
     return out
+
+
+# ------------------------------------------------------------------------------------ operators of a transformer's step
+NORM_LAYER, NORM_RMS = 0, 1
+
+
+def daf_attention(params, d_q, d_k, d_v, d_key_lengths, d_out, d_lse, stream=None):
+    status = _call(lib().daf_attention, d_q, stream, ctypes.byref(params), _ptr(d_q), _ptr(d_k), _ptr(d_v), _ptr(d_key_lengths),
+                   _ptr(d_out), _ptr(d_lse))
+    _check(status, "daf_attention")
+
+
+def daf_attention_grad_workspace(params) -> int:
+    return int(lib().daf_attention_grad_workspace(ctypes.byref(params)))
+
+
+def daf_attention_grad(params, d_q, d_k, d_v, d_key_lengths, d_out, d_lse, d_grad_out, d_grad_q, d_grad_k, d_grad_v, d_workspace,
+                       workspace_bytes, stream=None):
+    status = _call(lib().daf_attention_grad, d_q, stream, ctypes.byref(params), _ptr(d_q), _ptr(d_k), _ptr(d_v),
+                   _ptr(d_key_lengths), _ptr(d_out), _ptr(d_lse), _ptr(d_grad_out), _ptr(d_grad_q), _ptr(d_grad_k),
+                   _ptr(d_grad_v), _ptr(d_workspace), workspace_bytes)
+    _check(status, "daf_attention_grad")
+
+
+def daf_residual_norm(params, d_x, d_y, d_weight, d_bias, d_gate, d_post_weight, d_post_bias, d_z, d_h, stream=None):
+    status = _call(lib().daf_residual_norm, d_x, stream, ctypes.byref(params), _ptr(d_x), _ptr(d_y), _ptr(d_weight), _ptr(d_bias),
+                   _ptr(d_gate), _ptr(d_post_weight), _ptr(d_post_bias), _ptr(d_z), _ptr(d_h))
+    _check(status, "daf_residual_norm")
+
+
+def daf_residual_norm_grad_workspace(params) -> int:
+    return int(lib().daf_residual_norm_grad_workspace(ctypes.byref(params)))
+
+
+def daf_residual_norm_grad(params, d_z, d_y, d_weight, d_gate, d_post_weight, d_post_bias, d_grad_z, d_grad_h, d_grad_x, d_grad_y,
+                           d_grad_weight, d_grad_bias, d_grad_gate, d_grad_post_weight, d_grad_post_bias, d_workspace,
+                           workspace_bytes, stream=None):
+    status = _call(lib().daf_residual_norm_grad, d_z, stream, ctypes.byref(params), _ptr(d_z), _ptr(d_y), _ptr(d_weight),
+                   _ptr(d_gate), _ptr(d_post_weight), _ptr(d_post_bias), _ptr(d_grad_z), _ptr(d_grad_h), _ptr(d_grad_x),
+                   _ptr(d_grad_y), _ptr(d_grad_weight), _ptr(d_grad_bias), _ptr(d_grad_gate), _ptr(d_grad_post_weight),
+                   _ptr(d_grad_post_bias), _ptr(d_workspace), workspace_bytes)
+    _check(status, "daf_residual_norm_grad")
+
+
+def daf_clip_norm_workspace(n: int) -> int:
+    return int(lib().daf_clip_norm_workspace(n))
+
+
+def daf_clip_norm_batch(d_in, d_out, max_norm, eps, d_norm, d_workspace, workspace_bytes, stream=None):
+    """d_in, d_out: lists of tensors (d_out None: the norm alone)."""
+    n = len(d_in)
+    status = _call(lib().daf_clip_norm_batch, d_norm, stream, n, (ctypes.c_uint32 * n)(*[dtype_code(t) for t in d_in]),
+                   _ptr_array(d_in), None if d_out is None else _ptr_array(d_out), (ctypes.c_uint64 * n)(*[t.numel() for t in d_in]),
+                   max_norm, eps, _ptr(d_norm), _ptr(d_workspace), workspace_bytes)
+    _check(status, "daf_clip_norm_batch")
+
+
+def _same_kind(where: str, ref, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and (t.device != ref.device or t.dtype != ref.dtype):
+            raise ValueError(f"{where}: {name} is {t.dtype} on {t.device}, expected {ref.dtype} on {ref.device}")
+
+
+def _strided(t):
+    """t itself when the attention kernels can address it (rows contiguous and on 16-byte boundaries, nothing broadcast), else
+    a contiguous copy."""
+    unit = 16 // t.element_size()
+    s = t.stride()
+    if s[3] == 1 and t.data_ptr() % 16 == 0 and all(t.shape[i] <= 1 or (s[i] % unit == 0 and s[i] >= t.shape[3]) for i in (0, 1, 2)):
+        return t
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+def _stride3(t):
+    s = t.stride()
+    return _u64x3(s[0], s[1], s[2])
+
+
+def _attention_params(where: str, q, k, v, causal, scale, key_lengths) -> daf_attention_params:
+    if not q.is_cuda or q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+        raise ValueError(f"{where} expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
+    (b, sq, h, d), (bk, sk, hkv, dk) = q.shape, k.shape
+    if b != bk or d != dk or hkv == 0 or h % hkv:
+        raise ValueError(f"{where}: q {tuple(q.shape)} and k {tuple(k.shape)} do not belong together")
+    _same_kind(where, q, k=k, v=v)
+    if key_lengths is not None and (key_lengths.dtype != _torch().int32 or key_lengths.device != q.device
+                                    or tuple(key_lengths.shape) != (b,) or not key_lengths.is_contiguous()):
+        raise ValueError(f"{where}: key_lengths is an int32 tensor of {b} lengths on {q.device}")
+    p = daf_attention_params(ctypes.sizeof(daf_attention_params), dtype_code(q), b, sq, sk, h, hkv, d, 1 if causal else 0,
+                             d ** -0.5 if scale is None else scale)
+    p.q_stride, p.k_stride, p.v_stride = _stride3(q), _stride3(k), _stride3(v)
+    return p
+
+
+def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None, out=None, lse=None, stream=None):
+    """(out, lse): softmax attention of q [B, Sq, H, D] over k, v [B, Sk, Hkv, D] and the logarithm of each row's sum of
+    exponentials [B, H, Sq] that the backward pass needs (daf_attention).  Slices of a packed projection are read in place;
+    tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
+    first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq."""
+    torch = _torch()
+    q, k, v = _strided(q), _strided(k), _strided(v)
+    p = _attention_params("attention", q, k, v, causal, scale, key_lengths)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    _same_kind("attention", q, out=out)
+    if out.shape != q.shape or tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 \
+            or lse.device != q.device or not lse.is_contiguous():
+        raise ValueError("attention: out has the shape of q, lse is a contiguous float32 tensor [B, H, Sq]")
+    p.out_stride = _stride3(out)
+    if out.stride(3) != 1:
+        raise ValueError("attention: the last dimension of out must be contiguous")
+    daf_attention(p, q, k, v, key_lengths, out, lse, stream)
+    return out, lse
+
+
+def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: float | None = None, key_lengths=None, grads=None,
+                   stream=None):
+    """(grad_q, grad_k, grad_v) of ``attention`` from its inputs, its two results and grad_out (daf_attention_grad).  grads:
+    three tensors to write into (they may be slices of one packed gradient), fresh contiguous ones by default."""
+    torch = _torch()
+    q, k, v, out, grad_out = _strided(q), _strided(k), _strided(v), _strided(out), _strided(grad_out)
+    p = _attention_params("attention_grad", q, k, v, causal, scale, key_lengths)
+    if grads is None:
+        grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
+    gq, gk, gv = grads
+    _same_kind("attention_grad", q, out=out, grad_out=grad_out, grad_q=gq, grad_k=gk, grad_v=gv)
+    if out.shape != q.shape or grad_out.shape != q.shape or gq.shape != q.shape or gk.shape != k.shape or gv.shape != v.shape:
+        raise ValueError("attention_grad: out, grad_out and grad_q have the shape of q, grad_k and grad_v that of k")
+    if tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 or lse.device != q.device \
+            or not lse.is_contiguous() or any(t.stride(3) != 1 for t in grads):
+        raise ValueError("attention_grad: lse is a contiguous float32 tensor [B, H, Sq], the gradients' last dimension is contiguous")
+    p.out_stride, p.grad_out_stride = _stride3(out), _stride3(grad_out)
+    p.grad_q_stride, p.grad_k_stride, p.grad_v_stride = _stride3(gq), _stride3(gk), _stride3(gv)
+    n = daf_attention_grad_workspace(p)
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    daf_attention_grad(p, q, k, v, key_lengths, out, lse, grad_out, gq, gk, gv, ws, n, stream)
+    return gq, gk, gv
+
+
+def _norm_params(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps) -> daf_norm_params:
+    if not x.is_cuda or x.dim() < 1 or not x.is_contiguous() or not y.is_contiguous() or x.shape != y.shape:
+        raise ValueError(f"{where} expects contiguous CUDA tensors of one shape")
+    if kind not in ("layer", "rms"):
+        raise ValueError(f"{where}: kind is 'layer' or 'rms'")
+    width = x.shape[-1]
+    rows = x.numel() // width if width else 0
+    _same_kind(where, x, y=y)
+    _same_kind(where, weight, bias=bias, gate=gate, post_weight=post_weight, post_bias=post_bias)
+    for name, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias)):
+        if t is not None and (tuple(t.shape) != (width,) or not t.is_contiguous()):
+            raise ValueError(f"{where}: {name} must be a contiguous vector of {width}")
+    gates = 0
+    if gate is not None:
+        gates = 1 if gate.dim() == 1 else int(gate.shape[0])
+        if tuple(gate.shape) not in ((width,), (gates, width)) or not gate.is_contiguous() or gates == 0:
+            raise ValueError(f"{where}: gate must be contiguous, [{width}] or [G, {width}]")
+    if weight.device != x.device:
+        raise ValueError(f"{where}: parameters and activations are on different devices")
+    return daf_norm_params(ctypes.sizeof(daf_norm_params), dtype_code(x), dtype_code(weight), NORM_LAYER if kind == "layer" else NORM_RMS,
+                           rows, width, gates, residual_scale, eps, 0)
+
+
+def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_bias=None, residual_scale: float = 1.0,
+                  kind: str = "layer", eps: float = 1e-6, out=None, stream=None):
+    """(z, h): z = x + residual_scale * gate * post_norm(y), h = norm(z) * weight + bias over the last dimension, in one pass
+    (daf_residual_norm).  post_norm only with post_weight; gate [C], or [G, C] for G equal runs of rows; parameters in the
+    activations' type or float32.  out: (z, h) to write into, z may be x and h may be y."""
+    p = _norm_params("residual_norm", x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps)
+    z, h = out if out is not None else (_torch().empty_like(x), _torch().empty_like(x))
+    _same_kind("residual_norm", x, z=z, h=h)
+    if z.shape != x.shape or h.shape != x.shape or not z.is_contiguous() or not h.is_contiguous():
+        raise ValueError("residual_norm: z and h are contiguous and have the shape of x")
+    daf_residual_norm(p, x, y, weight, bias, gate, post_weight, post_bias, z, h, stream)
+    return z, h
+
+
+def residual_norm_grad(z, y, weight, bias, grad_z, grad_h, *, gate=None, post_weight=None, post_bias=None,
+                       residual_scale: float = 1.0, kind: str = "layer", eps: float = 1e-6, stream=None) -> dict:
+    """Gradients of ``residual_norm`` from z, y and those of z (None: zero) and h (daf_residual_norm_grad): a dict with "x", "y",
+    "weight", "bias", "gate", "post_weight" and "post_bias", None where there is no such parameter."""
+    torch = _torch()
+    p = _norm_params("residual_norm_grad", z, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps)
+    _same_kind("residual_norm_grad", z, grad_z=grad_z, grad_h=grad_h)
+    for t in (grad_z, grad_h):
+        if t is not None and (t.shape != z.shape or not t.is_contiguous()):
+            raise ValueError("residual_norm_grad: the gradients are contiguous and have the shape of z")
+    g = {"x": torch.empty_like(z), "y": torch.empty_like(z)}
+    for name, t in (("weight", weight), ("bias", bias), ("gate", gate), ("post_weight", post_weight), ("post_bias", post_bias)):
+        g[name] = None if t is None else torch.empty_like(t)
+    n = daf_residual_norm_grad_workspace(p)
+    ws = torch.empty(n, dtype=torch.uint8, device=z.device) if n else None
+    daf_residual_norm_grad(p, z, y, weight, gate, post_weight, post_bias, grad_z, grad_h, g["x"], g["y"], g["weight"], g["bias"],
+                           g["gate"], g["post_weight"], g["post_bias"], ws, n, stream)
+    return g
+
+
+def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, stream=None):
+    """Scales the tensors of ``grads`` in place (or into ``out``) by min(1, max_norm / (norm + eps)), norm being the 2-norm over
+    all of them; returns the norm as a float32 scalar tensor on their device (daf_clip_norm_batch).  Nothing is read back."""
+    torch = _torch()
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if not grads:
+        return torch.zeros((), dtype=torch.float32)
+    dev = grads[0].device
+    if len(out) != len(grads):
+        raise ValueError("clip_grad_norm: out holds one tensor for each gradient")
+    for g, o in zip(grads, out):
+        if not g.is_cuda or g.device != dev or not g.is_contiguous():
+            raise ValueError("clip_grad_norm expects contiguous CUDA tensors on one device")
+        if o is not g and (o.device != dev or not o.is_contiguous() or o.dtype != g.dtype or o.shape != g.shape):
+            raise ValueError("clip_grad_norm: an output differs from its gradient in shape, type or device")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    n = daf_clip_norm_workspace(len(grads))
+    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    daf_clip_norm_batch(grads, out, max_norm, eps, norm, ws, n, stream)
+    return norm
 
 
 class Pool:

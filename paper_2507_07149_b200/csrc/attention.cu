@@ -1,0 +1,124 @@
+// Entry points of attention: argument checks and the choice of the kernels.
+#include "attention.cuh"
+
+namespace daf {
+
+constexpr uint32_t kAttnRowPad = 128;            // rows of the backward workspace are padded to whole tiles
+
+static bool tensor_ok(const void *p, const uint64_t (&st)[3], uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t bytes)
+{
+    if (!p || (reinterpret_cast<uintptr_t>(p) & 15u)) return false;
+    const uint32_t unit = 16u / bytes;           // a row starts on a 16-byte boundary
+    const uint32_t extent[3] = {B, S, H};
+    for (int i = 0; i < 3; i++)
+        // an extent of one has no stride; otherwise elements of two rows must not share memory
+        if (extent[i] > 1u && (st[i] < D || st[i] % unit || st[i] >= (1ull << 36))) return false;
+    return true;
+}
+
+static daf_status check_attention(const daf_attention_params *p)
+{
+    if (!p || p->struct_size != sizeof(daf_attention_params) || p->dtype > DAF_BF16 || p->reserved[0] || p->reserved[1]) return DAF_ERR_INVALID_ARG;
+    if (p->causal > 1u || !(p->scale > -INFINITY && p->scale < INFINITY)) return DAF_ERR_INVALID_ARG;
+    if (p->heads == 0 || p->kv_heads == 0 || p->heads % p->kv_heads || p->head_dim == 0 || p->head_dim % 8u) return DAF_ERR_SHAPE;
+    if (p->head_dim > 128u || p->queries > (1u << 24) || p->keys > (1u << 24)) return DAF_ERR_UNSUPPORTED;
+    if ((uint64_t)p->batch * p->heads > 65535u || (uint64_t)p->batch * p->heads * p->queries > (1ull << 32)) return DAF_ERR_UNSUPPORTED;
+    return DAF_OK;
+}
+
+static AttnTensor tensor_of(const void *p, const uint64_t (&st)[3])
+{
+    return {const_cast<void *>(p), st[0], st[1], st[2]};
+}
+
+static uint32_t padded_rows(uint32_t rows) { return (rows + kAttnRowPad - 1u) / kAttnRowPad * kAttnRowPad; }
+
+static AttnArgs args_of(const daf_attention_params *p)
+{
+    AttnArgs a = {};
+    a.B = p->batch;
+    a.Sq = p->queries;
+    a.Sk = p->keys;
+    a.H = p->heads;
+    a.Hkv = p->kv_heads;
+    a.D = p->head_dim;
+    a.group = p->heads / p->kv_heads;
+    a.causal = p->causal;
+    a.rows_padded = padded_rows(p->queries);
+    a.scale = p->scale;
+    a.scale_log2 = p->scale * 1.4426950408889634f;
+    return a;
+}
+
+}  // namespace daf
+
+using namespace daf;
+
+extern "C" daf_status daf_attention(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
+                                    const int32_t *d_key_lengths, void *d_out, float *d_lse, daf_stream stream)
+{
+    const daf_status st = check_attention(params);
+    if (st != DAF_OK) return st;
+    const daf_attention_params &p = *params;
+    const uint32_t eb = p.dtype == DAF_F32 ? 4u : 2u;
+    if (reinterpret_cast<uintptr_t>(d_key_lengths) & 3u) return DAF_ERR_INVALID_ARG;
+    if (p.batch == 0 || p.queries == 0) return DAF_OK;
+    if (!tensor_ok(d_q, p.q_stride, p.batch, p.queries, p.heads, p.head_dim, eb) || !d_lse || (reinterpret_cast<uintptr_t>(d_lse) & 3u) ||
+        !tensor_ok(d_out, p.out_stride, p.batch, p.queries, p.heads, p.head_dim, eb) ||
+        (p.keys && (!tensor_ok(d_k, p.k_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb) ||
+                    !tensor_ok(d_v, p.v_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb))))
+        return DAF_ERR_INVALID_ARG;
+    AttnArgs a = args_of(params);
+    a.q = tensor_of(d_q, p.q_stride);
+    a.k = tensor_of(d_k, p.k_stride);
+    a.v = tensor_of(d_v, p.v_stride);
+    a.out = tensor_of(d_out, p.out_stride);
+    a.lse = d_lse;
+    a.lengths = d_key_lengths;
+    return attn_forward_general(p.dtype, a, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" uint64_t daf_attention_grad_workspace(const daf_attention_params *params)
+{
+    if (check_attention(params) != DAF_OK) return 0;
+    return 2ull * params->batch * params->heads * padded_rows(params->queries) * sizeof(float) + 16u;
+}
+
+extern "C" daf_status daf_attention_grad(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
+                                         const int32_t *d_key_lengths, const void *d_out, const float *d_lse,
+                                         const void *d_grad_out, void *d_grad_q, void *d_grad_k, void *d_grad_v,
+                                         void *d_workspace, uint64_t workspace_bytes, daf_stream stream)
+{
+    const daf_status st = check_attention(params);
+    if (st != DAF_OK) return st;
+    const daf_attention_params &p = *params;
+    const uint32_t eb = p.dtype == DAF_F32 ? 4u : 2u;
+    if (reinterpret_cast<uintptr_t>(d_key_lengths) & 3u) return DAF_ERR_INVALID_ARG;
+    if (p.batch == 0 || (p.queries == 0 && p.keys == 0)) return DAF_OK;
+    if (p.queries && (!tensor_ok(d_q, p.q_stride, p.batch, p.queries, p.heads, p.head_dim, eb) || !d_lse || (reinterpret_cast<uintptr_t>(d_lse) & 3u) ||
+                      !tensor_ok(d_out, p.out_stride, p.batch, p.queries, p.heads, p.head_dim, eb) ||
+                      !tensor_ok(d_grad_out, p.grad_out_stride, p.batch, p.queries, p.heads, p.head_dim, eb) ||
+                      !tensor_ok(d_grad_q, p.grad_q_stride, p.batch, p.queries, p.heads, p.head_dim, eb)))
+        return DAF_ERR_INVALID_ARG;
+    if (p.keys && (!tensor_ok(d_k, p.k_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb) ||
+                   !tensor_ok(d_v, p.v_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb) ||
+                   !tensor_ok(d_grad_k, p.grad_k_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb) ||
+                   !tensor_ok(d_grad_v, p.grad_v_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb)))
+        return DAF_ERR_INVALID_ARG;
+    if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 15u)) return DAF_ERR_INVALID_ARG;
+    if (workspace_bytes < daf_attention_grad_workspace(params)) return DAF_ERR_CAPACITY;
+    AttnArgs a = args_of(params);
+    a.q = tensor_of(d_q, p.q_stride);
+    a.k = tensor_of(d_k, p.k_stride);
+    a.v = tensor_of(d_v, p.v_stride);
+    a.out = tensor_of(d_out, p.out_stride);
+    a.grad_out = tensor_of(d_grad_out, p.grad_out_stride);
+    a.dq = tensor_of(d_grad_q, p.grad_q_stride);
+    a.dk = tensor_of(d_grad_k, p.grad_k_stride);
+    a.dv = tensor_of(d_grad_v, p.grad_v_stride);
+    a.lse = const_cast<float *>(d_lse);
+    a.lengths = d_key_lengths;
+    a.row_lse2 = reinterpret_cast<float *>(d_workspace);
+    a.row_delta = a.row_lse2 + (uint64_t)a.B * a.H * a.rows_padded;
+    return attn_backward_general(p.dtype, a, reinterpret_cast<cudaStream_t>(stream));
+}

@@ -1,0 +1,40 @@
+// What the attention kernels and their entry points share.
+#pragma once
+#include "common.cuh"
+
+namespace daf {
+
+// [batch, sequence, head, element] with the last one contiguous; strides in elements.
+struct AttnTensor {
+    void *p;
+    uint64_t sb, ss, sh;
+};
+
+struct AttnArgs {
+    AttnTensor q, k, v, out, grad_out, dq, dk, dv;
+    float *lse;                  // [B, H, Sq]: natural logarithm of each row's sum of exponentials, -inf for a row that sees no key
+    const int32_t *lengths;      // keys of each sequence, or null
+    float *row_lse2, *row_delta; // backward workspace, [B, H, rows_padded]: see attention_rows_kernel
+    uint32_t B, Sq, Sk, H, Hkv, D, group, causal, rows_padded;
+    float scale, scale_log2;     // scale_log2 = scale * log2(e)
+};
+
+// Keys of sequence b.
+__device__ __forceinline__ uint32_t attn_length(const AttnArgs &a, uint32_t b)
+{
+    if (!a.lengths) return a.Sk;
+    const int n = __ldg(a.lengths + b);
+    return n < 0 ? 0u : (uint32_t)n < a.Sk ? (uint32_t)n : a.Sk;
+}
+// Keys [0, limit) are visible to query i of a sequence with n keys.
+__device__ __forceinline__ int attn_limit(const AttnArgs &a, uint32_t n, int i)
+{
+    if (!a.causal) return (int)n;
+    const int c = i + 1 + (int)a.Sk - (int)a.Sq;
+    return c < (int)n ? c : (int)n;
+}
+
+daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);
+daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);
+
+}  // namespace daf

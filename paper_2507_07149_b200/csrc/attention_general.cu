@@ -1,0 +1,342 @@
+// Attention in binary32 arithmetic: forward, and the backward pass that recomputes the probabilities.
+//
+//   S = scale q k^T over the visible keys,  P = exp(S - L) with L = log sum exp S,  out = P v
+//   delta = sum(grad_out * out),  dS = P (grad_out v^T - delta) scale
+//   dq = dS k,  dk = dS^T q,  dv = P^T grad_out   (dk, dv summed over the query heads of a key head)
+//
+// One CTA per 64 rows of the tensor it produces: the forward and dq kernels hold 64 queries and walk the keys, the dk / dv
+// kernel holds 64 keys of a key head and walks the queries of every head that reads it, so no sum crosses CTAs.  Tiles are
+// widened to binary32 in shared memory; a thread owns 4 x 4 scores and 4 x (D / 16) outputs.
+#include "attention.cuh"
+
+namespace daf {
+
+constexpr int kGenThreads = 256;
+constexpr int kTile = 64;
+constexpr int kScorePitch = kTile + 4;
+
+// rows [first, first + 64) of one head into dst[row][DP + 4], zero beyond `limit` rows and D columns
+template <typename T, int DP>
+__device__ __forceinline__ void load_tile(float *dst, const AttnTensor &t, uint32_t b, uint32_t h, uint32_t first, uint32_t limit, uint32_t D)
+{
+    const char *base = reinterpret_cast<const char *>(t.p) + (t.sb * b + t.sh * h) * Elem<T>::kBytes;
+    for (int i = threadIdx.x; i < kTile * (DP / 8); i += kGenThreads) {
+        const uint32_t r = i / (DP / 8), c = (i % (DP / 8)) * 8;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (first + r < limit && c < D) {
+            const char *p = base + (t.ss * (first + r) + c) * Elem<T>::kBytes;
+            if (Elem<T>::kBytes == 2) {
+                Elem<T>::widen8(__ldg(reinterpret_cast<const uint4 *>(p)), x);
+            } else {
+                const float4 u = __ldg(reinterpret_cast<const float4 *>(p)), w = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+                x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+                x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+            }
+        }
+        float4 *d = reinterpret_cast<float4 *>(dst + r * (DP + 4) + c);
+        d[0] = make_float4(x[0], x[1], x[2], x[3]);
+        d[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+
+__device__ __forceinline__ float dot4(const float4 &a, const float4 &b, float c)
+{
+    return __fmaf_rn(a.w, b.w, __fmaf_rn(a.z, b.z, __fmaf_rn(a.y, b.y, __fmaf_rn(a.x, b.x, c))));
+}
+
+// acc[i][j] = A[4 ty + i] . B[tx + 16 j]
+template <int DP> __device__ __forceinline__ void product_nt(const float *A, const float *B, int ty, int tx, float (&acc)[4][4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = 0.0f;
+#pragma unroll 4
+    for (int d = 0; d < DP; d += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            a[i] = *reinterpret_cast<const float4 *>(A + (4 * ty + i) * (DP + 4) + d);
+            b[i] = *reinterpret_cast<const float4 *>(B + (tx + 16 * i) * (DP + 4) + d);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[i][j] = dot4(a[i], b[j], acc[i][j]);
+    }
+}
+
+// acc[i][4 jj + e] += sum over k of W[4 ty + i][k] * B[k][64 jj + 4 tx + e]
+template <int DP> __device__ __forceinline__ void product_nn(const float *W, const float *B, int ty, int tx, float (&acc)[4][DP / 16])
+{
+#pragma unroll 2
+    for (int k = 0; k < kTile; k += 4) {
+        float4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = *reinterpret_cast<const float4 *>(W + (4 * ty + i) * kScorePitch + k);
+#pragma unroll
+        for (int kk = 0; kk < 4; kk++) {
+#pragma unroll
+            for (int jj = 0; jj < DP / 64; jj++) {
+                const float4 b = *reinterpret_cast<const float4 *>(B + (k + kk) * (DP + 4) + 64 * jj + 4 * tx);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float x = kk == 0 ? w[i].x : kk == 1 ? w[i].y : kk == 2 ? w[i].z : w[i].w;
+                    acc[i][4 * jj] = __fmaf_rn(x, b.x, acc[i][4 * jj]);
+                    acc[i][4 * jj + 1] = __fmaf_rn(x, b.y, acc[i][4 * jj + 1]);
+                    acc[i][4 * jj + 2] = __fmaf_rn(x, b.z, acc[i][4 * jj + 2]);
+                    acc[i][4 * jj + 3] = __fmaf_rn(x, b.w, acc[i][4 * jj + 3]);
+                }
+            }
+        }
+    }
+}
+
+template <typename T> __device__ __forceinline__ void store4(void *p, uint64_t at, float a, float b, float c, float d);
+template <> __device__ __forceinline__ void store4<float>(void *p, uint64_t at, float a, float b, float c, float d)
+{
+    *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p) + at) = make_float4(a, b, c, d);
+}
+template <> __device__ __forceinline__ void store4<__half>(void *p, uint64_t at, float a, float b, float c, float d)
+{
+    __half2 *q = reinterpret_cast<__half2 *>(reinterpret_cast<__half *>(p) + at);
+    q[0] = __floats2half2_rn(a, b);
+    q[1] = __floats2half2_rn(c, d);
+}
+template <> __device__ __forceinline__ void store4<__nv_bfloat16>(void *p, uint64_t at, float a, float b, float c, float d)
+{
+    __nv_bfloat162 *q = reinterpret_cast<__nv_bfloat162 *>(reinterpret_cast<__nv_bfloat16 *>(p) + at);
+    q[0] = __floats2bfloat162_rn(a, b);
+    q[1] = __floats2bfloat162_rn(c, d);
+}
+
+// 64 rows of a thread block's result, times by[i]
+template <typename T, int DP>
+__device__ __forceinline__ void store_tile(const AttnTensor &t, uint32_t b, uint32_t h, uint32_t first, uint32_t limit, uint32_t D, int ty, int tx,
+                                           const float (&acc)[4][DP / 16], const float (&by)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t r = first + 4 * ty + i;
+        if (r >= limit) continue;
+        const uint64_t at = t.sb * b + t.sh * h + t.ss * r;
+#pragma unroll
+        for (int jj = 0; jj < DP / 64; jj++) {
+            const uint32_t c = 64 * jj + 4 * tx;
+            if (c < D)
+                store4<T>(t.p, at + c, acc[i][4 * jj] * by[i], acc[i][4 * jj + 1] * by[i], acc[i][4 * jj + 2] * by[i], acc[i][4 * jj + 3] * by[i]);
+        }
+    }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kGenThreads) attention_general_kernel(const __grid_constant__ AttnArgs a)
+{
+    extern __shared__ __align__(16) float smem[];
+    float *const Q = smem, *const K = Q + kTile * (DP + 4), *const V = K + kTile * (DP + 4), *const P = V + kTile * (DP + 4);
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    const uint32_t m0 = blockIdx.x * kTile, h = blockIdx.y % a.H, b = blockIdx.y / a.H;
+    const uint32_t n = attn_length(a, b);
+    load_tile<T, DP>(Q, a.q, b, h, m0, a.Sq, a.D);
+    float m[4], l[4], o[4][DP / 16] = {};
+    int limit[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        m[i] = -INFINITY;
+        l[i] = 0.0f;
+        limit[i] = attn_limit(a, n, (int)m0 + 4 * ty + i);
+    }
+    const int end = attn_limit(a, n, (int)(m0 + kTile < a.Sq ? m0 + kTile : a.Sq) - 1);
+    for (int n0 = 0; n0 < end; n0 += kTile) {
+        __syncthreads();
+        load_tile<T, DP>(K, a.k, b, h / a.group, n0, n, a.D);
+        load_tile<T, DP>(V, a.v, b, h / a.group, n0, n, a.D);
+        __syncthreads();
+        float s[4][4];
+        product_nt<DP>(Q, K, ty, tx, s);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                s[i][j] = n0 + tx + 16 * j < limit[i] ? s[i][j] * a.scale_log2 : -INFINITY;
+                top = fmaxf(top, s[i][j]);
+            }
+#pragma unroll
+            for (int d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float next = fmaxf(m[i], top), base = next == -INFINITY ? 0.0f : next;
+            const float fade = exp2f(m[i] - base);
+            m[i] = next;
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float p = exp2f(s[i][j] - base);
+                sum += p;
+                P[(4 * ty + i) * kScorePitch + tx + 16 * j] = p;
+            }
+            l[i] = __fmaf_rn(l[i], fade, sum);
+#pragma unroll
+            for (int c = 0; c < DP / 16; c++) o[i][c] *= fade;
+        }
+        __syncwarp();                                              // a warp's rows of P are read by that warp alone
+        product_nn<DP>(P, V, ty, tx, o);
+    }
+    float by[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+#pragma unroll
+        for (int d = 8; d; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+        by[i] = l[i] > 0.0f ? __fdiv_rn(1.0f, l[i]) : 0.0f;
+        const uint32_t r = m0 + 4 * ty + i;
+        if (tx == 0 && r < a.Sq)
+            a.lse[((uint64_t)b * a.H + h) * a.Sq + r] = l[i] > 0.0f ? (m[i] + log2f(l[i])) * 0.69314718055994531f : -INFINITY;
+    }
+    store_tile<T, DP>(a.out, b, h, m0, a.Sq, a.D, ty, tx, o, by);
+}
+
+// What the backward kernels need of each row, a warp per row: lse in units of log2, +inf for rows that see nothing and
+// for the padding (their probabilities then come out as exp2(-inf) = 0), and delta = sum(grad_out * out).
+template <typename T> __global__ void __launch_bounds__(kGenThreads) attention_rows_kernel(const __grid_constant__ AttnArgs a)
+{
+    const uint64_t w = (uint64_t)blockIdx.x * (kGenThreads / 32) + (threadIdx.x >> 5);
+    const uint32_t lane = threadIdx.x & 31u;
+    if (w >= (uint64_t)a.B * a.H * a.rows_padded) return;
+    const uint32_t i = (uint32_t)(w % a.rows_padded), bh = (uint32_t)(w / a.rows_padded), h = bh % a.H, b = bh / a.H;
+    float lse2 = INFINITY, delta = 0.0f;
+    if (i < a.Sq) {
+        const float l = a.lse[(uint64_t)bh * a.Sq + i];
+        if (l != -INFINITY) lse2 = l * 1.4426950408889634f;
+        const T *o = reinterpret_cast<const T *>(a.out.p) + a.out.sb * b + a.out.ss * i + a.out.sh * h;
+        const T *g = reinterpret_cast<const T *>(a.grad_out.p) + a.grad_out.sb * b + a.grad_out.ss * i + a.grad_out.sh * h;
+        for (uint32_t d = lane; d < a.D; d += 32u) delta = __fmaf_rn((float)o[d], (float)g[d], delta);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
+    if (lane == 0) {
+        a.row_lse2[w] = lse2;
+        a.row_delta[w] = delta;
+    }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kGenThreads) attention_dq_general_kernel(const __grid_constant__ AttnArgs a)
+{
+    extern __shared__ __align__(16) float smem[];
+    constexpr int TW = kTile * (DP + 4);
+    float *const Q = smem, *const G = Q + TW, *const K = G + TW, *const V = K + TW, *const S = V + TW;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    const uint32_t m0 = blockIdx.x * kTile, h = blockIdx.y % a.H, b = blockIdx.y / a.H;
+    const uint32_t n = attn_length(a, b);
+    load_tile<T, DP>(Q, a.q, b, h, m0, a.Sq, a.D);
+    load_tile<T, DP>(G, a.grad_out, b, h, m0, a.Sq, a.D);
+    float lse2[4], delta[4], o[4][DP / 16] = {};
+    int limit[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint64_t w = ((uint64_t)b * a.H + h) * a.rows_padded + m0 + 4 * ty + i;
+        lse2[i] = a.row_lse2[w];
+        delta[i] = a.row_delta[w];
+        limit[i] = attn_limit(a, n, (int)m0 + 4 * ty + i);
+    }
+    const int end = attn_limit(a, n, (int)(m0 + kTile < a.Sq ? m0 + kTile : a.Sq) - 1);
+    for (int n0 = 0; n0 < end; n0 += kTile) {
+        __syncthreads();
+        load_tile<T, DP>(K, a.k, b, h / a.group, n0, n, a.D);
+        load_tile<T, DP>(V, a.v, b, h / a.group, n0, n, a.D);
+        __syncthreads();
+        float s[4][4], e[4][4];
+        product_nt<DP>(Q, K, ty, tx, s);
+        product_nt<DP>(G, V, ty, tx, e);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float p = exp2f(__fmaf_rn(s[i][j], a.scale_log2, -lse2[i]));
+                S[(4 * ty + i) * kScorePitch + tx + 16 * j] = n0 + tx + 16 * j < limit[i] ? p * (e[i][j] - delta[i]) : 0.0f;
+            }
+        __syncwarp();
+        product_nn<DP>(S, K, ty, tx, o);
+    }
+    const float by[4] = {a.scale, a.scale, a.scale, a.scale};
+    store_tile<T, DP>(a.dq, b, h, m0, a.Sq, a.D, ty, tx, o, by);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kGenThreads) attention_dkv_general_kernel(const __grid_constant__ AttnArgs a)
+{
+    extern __shared__ __align__(16) float smem[];
+    constexpr int TW = kTile * (DP + 4), SW = kTile * kScorePitch;
+    float *const K = smem, *const V = K + TW, *const Q = V + TW, *const G = Q + TW, *const P = G + TW, *const S = P + SW;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    const uint32_t n0 = blockIdx.x * kTile, kh = blockIdx.y % a.Hkv, b = blockIdx.y / a.Hkv;
+    const uint32_t n = attn_length(a, b);
+    load_tile<T, DP>(K, a.k, b, kh, n0, n, a.D);
+    load_tile<T, DP>(V, a.v, b, kh, n0, n, a.D);
+    float dk[4][DP / 16] = {}, dv[4][DP / 16] = {};
+    // the first query that sees key n0
+    const int64_t from = a.causal ? (int64_t)n0 + (int64_t)a.Sq - (int64_t)a.Sk : 0;
+    const uint32_t start = from > 0 ? (uint32_t)(from / kTile * kTile) : 0u;
+    for (uint32_t h = kh * a.group; n0 < n && h < (kh + 1) * a.group; h++)
+        for (uint32_t m0 = start; m0 < a.Sq; m0 += kTile) {
+            __syncthreads();
+            load_tile<T, DP>(Q, a.q, b, h, m0, a.Sq, a.D);
+            load_tile<T, DP>(G, a.grad_out, b, h, m0, a.Sq, a.D);
+            __syncthreads();
+            float s[4][4], e[4][4];
+            product_nt<DP>(K, Q, ty, tx, s);
+            product_nt<DP>(V, G, ty, tx, e);
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const uint64_t w = ((uint64_t)b * a.H + h) * a.rows_padded + m0 + tx + 16 * j;
+                const float lse2 = a.row_lse2[w], delta = a.row_delta[w];
+                const int limit = attn_limit(a, n, (int)m0 + tx + 16 * j);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const bool see = (int)n0 + 4 * ty + i < limit;
+                    const float p = see ? exp2f(__fmaf_rn(s[i][j], a.scale_log2, -lse2)) : 0.0f;
+                    P[(4 * ty + i) * kScorePitch + tx + 16 * j] = p;
+                    S[(4 * ty + i) * kScorePitch + tx + 16 * j] = p * (e[i][j] - delta);
+                }
+            }
+            __syncwarp();
+            product_nn<DP>(P, G, ty, tx, dv);
+            product_nn<DP>(S, Q, ty, tx, dk);
+        }
+    const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f}, by[4] = {a.scale, a.scale, a.scale, a.scale};
+    store_tile<T, DP>(a.dv, b, kh, n0, a.Sk, a.D, ty, tx, dv, one);
+    store_tile<T, DP>(a.dk, b, kh, n0, a.Sk, a.D, ty, tx, dk, by);
+}
+
+template <typename K> static daf_status launch_general(K kernel, uint32_t rows, uint32_t heads, uint32_t B, int smem, const AttnArgs &a, cudaStream_t s)
+{
+    int ctas = 0;                                                  // asked for the shared-memory limit it raises
+    if (persistent_ctas(reinterpret_cast<const void *>(kernel), kGenThreads, smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    kernel<<<dim3((rows + kTile - 1) / kTile, heads * B), kGenThreads, smem, s>>>(a);
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
+
+template <typename T, int DP> static daf_status forward(const AttnArgs &a, cudaStream_t s)
+{
+    return launch_general(&attention_general_kernel<T, DP>, a.Sq, a.H, a.B, (3 * kTile * (DP + 4) + kTile * kScorePitch) * 4, a, s);
+}
+template <typename T, int DP> static daf_status backward(const AttnArgs &a, cudaStream_t s)
+{
+    if (a.Sq) {
+        const uint64_t rows = (uint64_t)a.B * a.H * a.rows_padded;
+        attention_rows_kernel<T><<<(uint32_t)((rows + 7u) / 8u), kGenThreads, 0, s>>>(a);
+        const daf_status st = launch_general(&attention_dq_general_kernel<T, DP>, a.Sq, a.H, a.B, (4 * kTile * (DP + 4) + kTile * kScorePitch) * 4, a, s);
+        if (st != DAF_OK) return st;
+    }
+    if (!a.Sk) return DAF_OK;
+    return launch_general(&attention_dkv_general_kernel<T, DP>, a.Sk, a.Hkv, a.B, (4 * kTile * (DP + 4) + 2 * kTile * kScorePitch) * 4, a, s);
+}
+
+#define DAF_ATTN_BY_TYPE(CALL)                                                                          \
+    dtype == DAF_F32 ? (a.D <= 64 ? CALL<float, 64>(a, s) : CALL<float, 128>(a, s))                      \
+    : dtype == DAF_F16 ? (a.D <= 64 ? CALL<__half, 64>(a, s) : CALL<__half, 128>(a, s))                  \
+                       : (a.D <= 64 ? CALL<__nv_bfloat16, 64>(a, s) : CALL<__nv_bfloat16, 128>(a, s))
+
+daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s) { return DAF_ATTN_BY_TYPE(forward); }
+daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s) { return DAF_ATTN_BY_TYPE(backward); }
+
+}  // namespace daf
