@@ -350,8 +350,10 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
  * to dtype where they enter the second products; binary32 inputs: binary32 products throughout.
  * heads a multiple of kv_heads, head_dim a multiple of 8 (DAF_ERR_SHAPE), head_dim <= 128, queries and keys <= 2^24,
  * batch * heads <= 65535, batch * heads * queries <= 2^32 (DAF_ERR_UNSUPPORTED).  batch, queries or keys == 0 are valid.
- * daf_attention_grad takes the forward pass's inputs, out and lse; d_workspace: daf_attention_grad_workspace(params)
- * bytes (0 for bad params), 16-byte aligned.  The gradient buffers must not overlap the inputs.
+ * daf_attention_grad takes the forward pass's inputs, out and lse.  d_workspace: daf_attention_workspace(params) or
+ * daf_attention_grad_workspace(params) bytes (0 for bad params), 16-byte aligned, contents irrelevant; it holds the device
+ * status word afterwards (daf_poll_status: DAF_OK, or DAF_ERR_TIMEOUT when a wait inside a kernel ran out).  No output
+ * may overlap an input.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
  */
 typedef struct daf_attention_params {
@@ -365,7 +367,9 @@ typedef struct daf_attention_params {
     uint64_t grad_out_stride[3], grad_q_stride[3], grad_k_stride[3], grad_v_stride[3];  /* daf_attention_grad only */
 } daf_attention_params;
 daf_status daf_attention(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
-                         const int32_t *d_key_lengths, void *d_out, float *d_lse, daf_stream stream);
+                         const int32_t *d_key_lengths, void *d_out, float *d_lse, void *d_workspace,
+                         uint64_t workspace_bytes, daf_stream stream);
+uint64_t   daf_attention_workspace(const daf_attention_params *params);
 uint64_t   daf_attention_grad_workspace(const daf_attention_params *params);
 daf_status daf_attention_grad(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
                               const int32_t *d_key_lengths, const void *d_out, const float *d_lse, const void *d_grad_out,

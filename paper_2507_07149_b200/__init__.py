@@ -117,7 +117,8 @@ SIGNATURES = {
     "daf_tensor_compress": (ctypes.c_int, [ctypes.c_uint32, _vp, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint32,
                                            ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
     "daf_tensor_decompress": (ctypes.c_int, [ctypes.c_uint32, _vp, ctypes.c_uint64, ctypes.c_uint32, _vp, _vp, _vp]),
-    "daf_attention": (ctypes.c_int, [ctypes.POINTER(daf_attention_params), _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "daf_attention": (ctypes.c_int, [ctypes.POINTER(daf_attention_params)] + [_vp] * 7 + [ctypes.c_uint64, _vp]),
+    "daf_attention_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_attention_params)]),
     "daf_attention_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_attention_params)]),
     "daf_attention_grad": (ctypes.c_int, [ctypes.POINTER(daf_attention_params)] + [_vp] * 11 + [ctypes.c_uint64, _vp]),
     "daf_residual_norm": (ctypes.c_int, [ctypes.POINTER(daf_norm_params)] + [_vp] * 10),
@@ -492,10 +493,14 @@ def tensor_decompress(packed, width: int, min_scale, shape, dtype, stream=None):
 NORM_LAYER, NORM_RMS = 0, 1
 
 
-def daf_attention(params, d_q, d_k, d_v, d_key_lengths, d_out, d_lse, stream=None):
+def daf_attention(params, d_q, d_k, d_v, d_key_lengths, d_out, d_lse, d_workspace, workspace_bytes, stream=None):
     status = _call(lib().daf_attention, d_q, stream, ctypes.byref(params), _ptr(d_q), _ptr(d_k), _ptr(d_v), _ptr(d_key_lengths),
-                   _ptr(d_out), _ptr(d_lse))
+                   _ptr(d_out), _ptr(d_lse), _ptr(d_workspace), workspace_bytes)
     _check(status, "daf_attention")
+
+
+def daf_attention_workspace(params) -> int:
+    return int(lib().daf_attention_workspace(ctypes.byref(params)))
 
 
 def daf_attention_grad_workspace(params) -> int:
@@ -581,7 +586,8 @@ def _attention_params(where: str, q, k, v, causal, scale, key_lengths) -> daf_at
     return p
 
 
-def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None, out=None, lse=None, stream=None):
+def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None, out=None, lse=None,
+              check: bool = False, stream=None):
     """(out, lse): softmax attention of q [B, Sq, H, D] over k, v [B, Sk, Hkv, D] and the logarithm of each row's sum of
     exponentials [B, H, Sq] that the backward pass needs (daf_attention).  Slices of a packed projection are read in place;
     tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
@@ -600,12 +606,16 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     p.out_stride = _stride3(out)
     if out.stride(3) != 1:
         raise ValueError("attention: the last dimension of out must be contiguous")
-    daf_attention(p, q, k, v, key_lengths, out, lse, stream)
+    n = daf_attention_workspace(p)
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    daf_attention(p, q, k, v, key_lengths, out, lse, ws, n, stream)
+    if check:
+        _check(daf_poll_status(ws, stream), "daf_attention (device status)")
     return out, lse
 
 
 def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: float | None = None, key_lengths=None, grads=None,
-                   stream=None):
+                   check: bool = False, stream=None):
     """(grad_q, grad_k, grad_v) of ``attention`` from its inputs, its two results and grad_out (daf_attention_grad).  grads:
     three tensors to write into (they may be slices of one packed gradient), fresh contiguous ones by default."""
     torch = _torch()
@@ -625,6 +635,8 @@ def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: 
     n = daf_attention_grad_workspace(p)
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     daf_attention_grad(p, q, k, v, key_lengths, out, lse, grad_out, gq, gk, gv, ws, n, stream)
+    if check:
+        _check(daf_poll_status(ws, stream), "daf_attention_grad (device status)")
     return gq, gk, gv
 
 

@@ -31,6 +31,25 @@ static AttnTensor tensor_of(const void *p, const uint64_t (&st)[3])
     return {const_cast<void *>(p), st[0], st[1], st[2]};
 }
 
+bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows)
+{
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+        return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(fn) : nullptr;
+    }();
+    if (!encode) return false;
+    const cuuint64_t extent[4] = {D, H, S, B}, none = (2ull * D + 15u) & ~15ull;     // an extent of one has no stride of its own
+    const cuuint64_t stride[3] = {H > 1u ? 2ull * t.sh : none, S > 1u ? 2ull * t.ss : none, B > 1u ? 2ull * t.sb : none};
+    const cuuint32_t box[4] = {64, 1, rows, 1}, step[4] = {1, 1, 1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride, box, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static uint32_t padded_rows(uint32_t rows) { return (rows + kAttnRowPad - 1u) / kAttnRowPad * kAttnRowPad; }
 
 static AttnArgs args_of(const daf_attention_params *p)
@@ -54,8 +73,14 @@ static AttnArgs args_of(const daf_attention_params *p)
 
 using namespace daf;
 
+extern "C" uint64_t daf_attention_workspace(const daf_attention_params *params)
+{
+    return check_attention(params) == DAF_OK ? sizeof(WorkspaceHeader) : 0u;
+}
+
 extern "C" daf_status daf_attention(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
-                                    const int32_t *d_key_lengths, void *d_out, float *d_lse, daf_stream stream)
+                                    const int32_t *d_key_lengths, void *d_out, float *d_lse, void *d_workspace,
+                                    uint64_t workspace_bytes, daf_stream stream)
 {
     const daf_status st = check_attention(params);
     if (st != DAF_OK) return st;
@@ -68,6 +93,8 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
         (p.keys && (!tensor_ok(d_k, p.k_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb) ||
                     !tensor_ok(d_v, p.v_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb))))
         return DAF_ERR_INVALID_ARG;
+    if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 15u)) return DAF_ERR_INVALID_ARG;
+    if (workspace_bytes < daf_attention_workspace(params)) return DAF_ERR_CAPACITY;
     AttnArgs a = args_of(params);
     a.q = tensor_of(d_q, p.q_stride);
     a.k = tensor_of(d_k, p.k_stride);
@@ -75,13 +102,16 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
     a.out = tensor_of(d_out, p.out_stride);
     a.lse = d_lse;
     a.lengths = d_key_lengths;
-    return attn_forward_general(p.dtype, a, reinterpret_cast<cudaStream_t>(stream));
+    WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    return p.dtype == DAF_F32 ? attn_forward_general(p.dtype, a, header, s)
+           : p.dtype == DAF_F16 ? attn_forward_tc<__half>(a, header, s) : attn_forward_tc<__nv_bfloat16>(a, header, s);
 }
 
 extern "C" uint64_t daf_attention_grad_workspace(const daf_attention_params *params)
 {
     if (check_attention(params) != DAF_OK) return 0;
-    return 2ull * params->batch * params->heads * padded_rows(params->queries) * sizeof(float) + 16u;
+    return 2ull * params->batch * params->heads * padded_rows(params->queries) * sizeof(float) + sizeof(WorkspaceHeader);
 }
 
 extern "C" daf_status daf_attention_grad(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
@@ -118,7 +148,7 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     a.dv = tensor_of(d_grad_v, p.grad_v_stride);
     a.lse = const_cast<float *>(d_lse);
     a.lengths = d_key_lengths;
-    a.row_lse2 = reinterpret_cast<float *>(d_workspace);
+    a.row_lse2 = reinterpret_cast<float *>(reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader));
     a.row_delta = a.row_lse2 + (uint64_t)a.B * a.H * a.rows_padded;
     return attn_backward_general(p.dtype, a, reinterpret_cast<cudaStream_t>(stream));
 }

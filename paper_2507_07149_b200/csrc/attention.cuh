@@ -1,5 +1,7 @@
 // What the attention kernels and their entry points share.
 #pragma once
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace daf {
@@ -34,7 +36,12 @@ __device__ __forceinline__ int attn_limit(const AttnArgs &a, uint32_t n, int i)
     return c < (int)n ? c : (int)n;
 }
 
-daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);
+daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
+template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
+
+// Map of a tensor for copies of `rows` rows times 64 elements of one head; false if the driver refuses it.
+bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows);
+
 daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);
 
 }  // namespace daf

@@ -130,8 +130,9 @@ __device__ __forceinline__ void store_tile(const AttnTensor &t, uint32_t b, uint
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kGenThreads) attention_general_kernel(const __grid_constant__ AttnArgs a)
+__global__ void __launch_bounds__(kGenThreads) attention_general_kernel(const __grid_constant__ AttnArgs a, WorkspaceHeader *header)
 {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) header->status = 0u;
     extern __shared__ __align__(16) float smem[];
     float *const Q = smem, *const K = Q + kTile * (DP + 4), *const V = K + kTile * (DP + 4), *const P = V + kTile * (DP + 4);
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
@@ -307,17 +308,18 @@ __global__ void __launch_bounds__(kGenThreads) attention_dkv_general_kernel(cons
     store_tile<T, DP>(a.dk, b, kh, n0, a.Sk, a.D, ty, tx, dk, by);
 }
 
-template <typename K> static daf_status launch_general(K kernel, uint32_t rows, uint32_t heads, uint32_t B, int smem, const AttnArgs &a, cudaStream_t s)
+template <typename K, typename... More>
+static daf_status launch_general(K kernel, uint32_t rows, uint32_t heads, uint32_t B, int smem, const AttnArgs &a, cudaStream_t s, More... more)
 {
     int ctas = 0;                                                  // asked for the shared-memory limit it raises
     if (persistent_ctas(reinterpret_cast<const void *>(kernel), kGenThreads, smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
-    kernel<<<dim3((rows + kTile - 1) / kTile, heads * B), kGenThreads, smem, s>>>(a);
+    kernel<<<dim3((rows + kTile - 1) / kTile, heads * B), kGenThreads, smem, s>>>(a, more...);
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 
-template <typename T, int DP> static daf_status forward(const AttnArgs &a, cudaStream_t s)
+template <typename T, int DP> static daf_status forward(const AttnArgs &a, cudaStream_t s, WorkspaceHeader *header)
 {
-    return launch_general(&attention_general_kernel<T, DP>, a.Sq, a.H, a.B, (3 * kTile * (DP + 4) + kTile * kScorePitch) * 4, a, s);
+    return launch_general(&attention_general_kernel<T, DP>, a.Sq, a.H, a.B, (3 * kTile * (DP + 4) + kTile * kScorePitch) * 4, a, s, header);
 }
 template <typename T, int DP> static daf_status backward(const AttnArgs &a, cudaStream_t s)
 {
@@ -331,12 +333,12 @@ template <typename T, int DP> static daf_status backward(const AttnArgs &a, cuda
     return launch_general(&attention_dkv_general_kernel<T, DP>, a.Sk, a.Hkv, a.B, (4 * kTile * (DP + 4) + 2 * kTile * kScorePitch) * 4, a, s);
 }
 
-#define DAF_ATTN_BY_TYPE(CALL)                                                                          \
-    dtype == DAF_F32 ? (a.D <= 64 ? CALL<float, 64>(a, s) : CALL<float, 128>(a, s))                      \
-    : dtype == DAF_F16 ? (a.D <= 64 ? CALL<__half, 64>(a, s) : CALL<__half, 128>(a, s))                  \
-                       : (a.D <= 64 ? CALL<__nv_bfloat16, 64>(a, s) : CALL<__nv_bfloat16, 128>(a, s))
+#define DAF_ATTN_BY_TYPE(CALL, ...)                                                                                      \
+    dtype == DAF_F32 ? (a.D <= 64 ? CALL<float, 64>(a, s, ##__VA_ARGS__) : CALL<float, 128>(a, s, ##__VA_ARGS__))         \
+    : dtype == DAF_F16 ? (a.D <= 64 ? CALL<__half, 64>(a, s, ##__VA_ARGS__) : CALL<__half, 128>(a, s, ##__VA_ARGS__))     \
+                       : (a.D <= 64 ? CALL<__nv_bfloat16, 64>(a, s, ##__VA_ARGS__) : CALL<__nv_bfloat16, 128>(a, s, ##__VA_ARGS__))
 
-daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s) { return DAF_ATTN_BY_TYPE(forward); }
+daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s) { return DAF_ATTN_BY_TYPE(forward, header); }
 daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s) { return DAF_ATTN_BY_TYPE(backward); }
 
 }  // namespace daf

@@ -46,10 +46,10 @@ A = 1 << 20                                      # an aligned address that is ne
     (dict(v_stride=(896, 132, 64)), daf.ERR_INVALID_ARG), (dict(out_stride=(1 << 40, 256, 64)), daf.ERR_INVALID_ARG)])
 def test_attention_parameters(change, status):
     p = ctypes.byref(attention_params(**change))
-    assert daf.lib().daf_attention(p, A, A, A, None, A, A, None) == status
+    assert daf.lib().daf_attention(p, A, A, A, None, A, A, A, 1 << 30, None) == status
     assert daf.lib().daf_attention_grad(p, A, A, A, None, A, A, A, A, A, A, A, 1 << 30, None) == status
     if not any(k.endswith("stride") for k in change):
-        assert daf.lib().daf_attention_grad_workspace(p) == 0
+        assert daf.lib().daf_attention_grad_workspace(p) == 0 and daf.lib().daf_attention_workspace(p) == 0
 
 
 def test_attention_pointers_and_workspace():
@@ -57,11 +57,12 @@ def test_attention_pointers_and_workspace():
     ref = ctypes.byref(p)
     need = daf.daf_attention_grad_workspace(p)
     assert need >= 2 * 2 * 4 * 128 * 4
-    ok = [A, A, A, None, A, A]
-    for i, bad in ((0, None), (1, None), (2, A + 8), (3, A + 2), (4, None), (4, A + 4), (5, None), (5, A + 2)):
+    ok = [A, A, A, None, A, A, A]
+    for i, bad in ((0, None), (1, None), (2, A + 8), (3, A + 2), (4, None), (4, A + 4), (5, None), (5, A + 2), (6, None), (6, A + 8)):
         args = list(ok)
         args[i] = bad
-        assert daf.lib().daf_attention(ref, *args, None) == daf.ERR_INVALID_ARG, i
+        assert daf.lib().daf_attention(ref, *args, 1 << 20, None) == daf.ERR_INVALID_ARG, i
+    assert daf.lib().daf_attention(ref, *ok, daf.daf_attention_workspace(p) - 1, None) == daf.ERR_CAPACITY
     ok = [A, A, A, None, A, A, A, A, A, A, A]
     for i, bad in ((0, A + 2), (4, None), (5, None), (6, None), (7, A + 8), (8, None), (9, None), (10, None), (10, A + 4)):
         args = list(ok)
@@ -71,8 +72,8 @@ def test_attention_pointers_and_workspace():
     for n in ("grad_out_stride", "grad_q_stride", "grad_k_stride", "grad_v_stride"):
         assert daf.lib().daf_attention_grad(ctypes.byref(attention_params(**{n: (896, 130, 64)})), *ok, need, None) == daf.ERR_INVALID_ARG
     # nothing to do is no error, whatever the pointers
-    assert daf.lib().daf_attention(ctypes.byref(attention_params(batch=0)), None, None, None, None, None, None, None) == daf.OK
-    assert daf.lib().daf_attention(ctypes.byref(attention_params(queries=0)), None, None, None, None, None, None, None) == daf.OK
+    assert daf.lib().daf_attention(ctypes.byref(attention_params(batch=0)), None, None, None, None, None, None, None, 0, None) == daf.OK
+    assert daf.lib().daf_attention(ctypes.byref(attention_params(queries=0)), None, None, None, None, None, None, None, 0, None) == daf.OK
 
 
 @pytest.mark.parametrize("change,status", [
