@@ -148,7 +148,16 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     a.dv = tensor_of(d_grad_v, p.grad_v_stride);
     a.lse = const_cast<float *>(d_lse);
     a.lengths = d_key_lengths;
-    a.row_lse2 = reinterpret_cast<float *>(reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader));
-    a.row_delta = a.row_lse2 + (uint64_t)a.B * a.H * a.rows_padded;
-    return attn_backward_general(p.dtype, a, reinterpret_cast<cudaStream_t>(stream));
+    a.row_nl2 = reinterpret_cast<float *>(reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader));
+    a.row_ndelta = a.row_nl2 + (uint64_t)a.B * a.H * a.rows_padded;
+    WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (p.queries) {
+        const daf_status rows = attn_rows(p.dtype, a, header, s);
+        if (rows != DAF_OK) return rows;
+    } else if (cudaMemsetAsync(header, 0, sizeof(uint32_t), s) != cudaSuccess) {
+        return DAF_ERR_CUDA;
+    }
+    if (p.dtype == DAF_F32 || p.queries == 0 || p.keys == 0) return attn_backward_general(p.dtype, a, s);
+    return p.dtype == DAF_F16 ? attn_backward_tc<__half>(a, header, s) : attn_backward_tc<__nv_bfloat16>(a, header, s);
 }

@@ -16,7 +16,7 @@ struct AttnArgs {
     AttnTensor q, k, v, out, grad_out, dq, dk, dv;
     float *lse;                  // [B, H, Sq]: natural logarithm of each row's sum of exponentials, -inf for a row that sees no key
     const int32_t *lengths;      // keys of each sequence, or null
-    float *row_lse2, *row_delta; // backward workspace, [B, H, rows_padded]: see attention_rows_kernel
+    float *row_nl2, *row_ndelta; // backward workspace, [B, H, rows_padded]: see attention_rows_kernel
     uint32_t B, Sq, Sk, H, Hkv, D, group, causal, rows_padded;
     float scale, scale_log2;     // scale_log2 = scale * log2(e)
 };
@@ -42,6 +42,8 @@ template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHea
 // Map of a tensor for copies of `rows` rows times 64 elements of one head; false if the driver refuses it.
 bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows);
 
+daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);
+template <typename T> daf_status attn_backward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 
 }  // namespace daf

@@ -15,6 +15,17 @@ constexpr int kGenThreads = 256;
 constexpr int kTile = 64;
 constexpr int kScorePitch = kTile + 4;
 
+// eight elements from a 16-byte boundary
+template <typename T> __device__ __forceinline__ void load8_any(const void *p, float (&x)[8])
+{
+    const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
+    Elem<T>::widen8(u, x);
+    if (Elem<T>::kBytes == 4) {
+        const float4 w = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+        x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+    }
+}
+
 // rows [first, first + 64) of one head into dst[row][DP + 4], zero beyond `limit` rows and D columns
 template <typename T, int DP>
 __device__ __forceinline__ void load_tile(float *dst, const AttnTensor &t, uint32_t b, uint32_t h, uint32_t first, uint32_t limit, uint32_t D)
@@ -24,14 +35,7 @@ __device__ __forceinline__ void load_tile(float *dst, const AttnTensor &t, uint3
         const uint32_t r = i / (DP / 8), c = (i % (DP / 8)) * 8;
         float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (first + r < limit && c < D) {
-            const char *p = base + (t.ss * (first + r) + c) * Elem<T>::kBytes;
-            if (Elem<T>::kBytes == 2) {
-                Elem<T>::widen8(__ldg(reinterpret_cast<const uint4 *>(p)), x);
-            } else {
-                const float4 u = __ldg(reinterpret_cast<const float4 *>(p)), w = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-                x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-                x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
-            }
+            load8_any<T>(base + (t.ss * (first + r) + c) * Elem<T>::kBytes, x);
         }
         float4 *d = reinterpret_cast<float4 *>(dst + r * (DP + 4) + c);
         d[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -195,27 +199,34 @@ __global__ void __launch_bounds__(kGenThreads) attention_general_kernel(const __
     store_tile<T, DP>(a.out, b, h, m0, a.Sq, a.D, ty, tx, o, by);
 }
 
-// What the backward kernels need of each row, a warp per row: lse in units of log2, +inf for rows that see nothing and
-// for the padding (their probabilities then come out as exp2(-inf) = 0), and delta = sum(grad_out * out).
-template <typename T> __global__ void __launch_bounds__(kGenThreads) attention_rows_kernel(const __grid_constant__ AttnArgs a)
+// What the backward kernels need of each row, D / 8 lanes (rounded up to a power of two) per row: -lse in units of log2,
+// -inf for rows that see nothing and for the padding (their probabilities then come out as exp2(-inf) = 0), and
+// -delta = -sum(grad_out * out).
+template <typename T> __global__ void __launch_bounds__(kGenThreads) attention_rows_kernel(const __grid_constant__ AttnArgs a, uint32_t lanes, WorkspaceHeader *header)
 {
-    const uint64_t w = (uint64_t)blockIdx.x * (kGenThreads / 32) + (threadIdx.x >> 5);
-    const uint32_t lane = threadIdx.x & 31u;
-    if (w >= (uint64_t)a.B * a.H * a.rows_padded) return;
+    if (blockIdx.x == 0 && threadIdx.x == 0) header->status = 0u;
+    const uint32_t lane = threadIdx.x % lanes;
+    const uint64_t w = (uint64_t)blockIdx.x * (kGenThreads / lanes) + threadIdx.x / lanes;
+    const bool exists = w < (uint64_t)a.B * a.H * a.rows_padded;
     const uint32_t i = (uint32_t)(w % a.rows_padded), bh = (uint32_t)(w / a.rows_padded), h = bh % a.H, b = bh / a.H;
-    float lse2 = INFINITY, delta = 0.0f;
-    if (i < a.Sq) {
+    float nl2 = -INFINITY, delta = 0.0f;
+    if (exists && i < a.Sq) {
         const float l = a.lse[(uint64_t)bh * a.Sq + i];
-        if (l != -INFINITY) lse2 = l * 1.4426950408889634f;
-        const T *o = reinterpret_cast<const T *>(a.out.p) + a.out.sb * b + a.out.ss * i + a.out.sh * h;
-        const T *g = reinterpret_cast<const T *>(a.grad_out.p) + a.grad_out.sb * b + a.grad_out.ss * i + a.grad_out.sh * h;
-        for (uint32_t d = lane; d < a.D; d += 32u) delta = __fmaf_rn((float)o[d], (float)g[d], delta);
-    }
+        if (l != -INFINITY) nl2 = -l * 1.4426950408889634f;
+        if (lane * 8u < a.D) {
+            const T *o = reinterpret_cast<const T *>(a.out.p) + a.out.sb * b + a.out.ss * i + a.out.sh * h + lane * 8u;
+            const T *g = reinterpret_cast<const T *>(a.grad_out.p) + a.grad_out.sb * b + a.grad_out.ss * i + a.grad_out.sh * h + lane * 8u;
+            float x[8], y[8];
+            load8_any<T>(o, x);
+            load8_any<T>(g, y);
 #pragma unroll
-    for (int d = 16; d; d >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
-    if (lane == 0) {
-        a.row_lse2[w] = lse2;
-        a.row_delta[w] = delta;
+            for (int e = 0; e < 8; e++) delta = __fmaf_rn(x[e], y[e], delta);
+        }
+    }
+    for (uint32_t d = lanes >> 1; d; d >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
+    if (exists && lane == 0) {
+        a.row_nl2[w] = nl2;
+        a.row_ndelta[w] = -delta;
     }
 }
 
@@ -230,13 +241,13 @@ __global__ void __launch_bounds__(kGenThreads) attention_dq_general_kernel(const
     const uint32_t n = attn_length(a, b);
     load_tile<T, DP>(Q, a.q, b, h, m0, a.Sq, a.D);
     load_tile<T, DP>(G, a.grad_out, b, h, m0, a.Sq, a.D);
-    float lse2[4], delta[4], o[4][DP / 16] = {};
+    float nl2[4], nd[4], o[4][DP / 16] = {};
     int limit[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const uint64_t w = ((uint64_t)b * a.H + h) * a.rows_padded + m0 + 4 * ty + i;
-        lse2[i] = a.row_lse2[w];
-        delta[i] = a.row_delta[w];
+        nl2[i] = a.row_nl2[w];
+        nd[i] = a.row_ndelta[w];
         limit[i] = attn_limit(a, n, (int)m0 + 4 * ty + i);
     }
     const int end = attn_limit(a, n, (int)(m0 + kTile < a.Sq ? m0 + kTile : a.Sq) - 1);
@@ -252,8 +263,8 @@ __global__ void __launch_bounds__(kGenThreads) attention_dq_general_kernel(const
         for (int i = 0; i < 4; i++)
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                const float p = exp2f(__fmaf_rn(s[i][j], a.scale_log2, -lse2[i]));
-                S[(4 * ty + i) * kScorePitch + tx + 16 * j] = n0 + tx + 16 * j < limit[i] ? p * (e[i][j] - delta[i]) : 0.0f;
+                const float p = exp2f(__fmaf_rn(s[i][j], a.scale_log2, nl2[i]));
+                S[(4 * ty + i) * kScorePitch + tx + 16 * j] = n0 + tx + 16 * j < limit[i] ? p * (e[i][j] + nd[i]) : 0.0f;
             }
         __syncwarp();
         product_nn<DP>(S, K, ty, tx, o);
@@ -289,14 +300,14 @@ __global__ void __launch_bounds__(kGenThreads) attention_dkv_general_kernel(cons
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const uint64_t w = ((uint64_t)b * a.H + h) * a.rows_padded + m0 + tx + 16 * j;
-                const float lse2 = a.row_lse2[w], delta = a.row_delta[w];
+                const float nl2 = a.row_nl2[w], nd = a.row_ndelta[w];
                 const int limit = attn_limit(a, n, (int)m0 + tx + 16 * j);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const bool see = (int)n0 + 4 * ty + i < limit;
-                    const float p = see ? exp2f(__fmaf_rn(s[i][j], a.scale_log2, -lse2)) : 0.0f;
+                    const float p = see ? exp2f(__fmaf_rn(s[i][j], a.scale_log2, nl2)) : 0.0f;
                     P[(4 * ty + i) * kScorePitch + tx + 16 * j] = p;
-                    S[(4 * ty + i) * kScorePitch + tx + 16 * j] = p * (e[i][j] - delta);
+                    S[(4 * ty + i) * kScorePitch + tx + 16 * j] = p * (e[i][j] + nd);
                 }
             }
             __syncwarp();
@@ -324,13 +335,23 @@ template <typename T, int DP> static daf_status forward(const AttnArgs &a, cudaS
 template <typename T, int DP> static daf_status backward(const AttnArgs &a, cudaStream_t s)
 {
     if (a.Sq) {
-        const uint64_t rows = (uint64_t)a.B * a.H * a.rows_padded;
-        attention_rows_kernel<T><<<(uint32_t)((rows + 7u) / 8u), kGenThreads, 0, s>>>(a);
         const daf_status st = launch_general(&attention_dq_general_kernel<T, DP>, a.Sq, a.H, a.B, (4 * kTile * (DP + 4) + kTile * kScorePitch) * 4, a, s);
         if (st != DAF_OK) return st;
     }
     if (!a.Sk) return DAF_OK;
     return launch_general(&attention_dkv_general_kernel<T, DP>, a.Sk, a.Hkv, a.B, (4 * kTile * (DP + 4) + 2 * kTile * kScorePitch) * 4, a, s);
+}
+
+daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s)
+{
+    uint32_t lanes = 1;
+    while (lanes * 8u < a.D) lanes *= 2u;
+    const uint64_t per = kGenThreads / lanes, rows = (uint64_t)a.B * a.H * a.rows_padded;
+    const uint32_t grid = (uint32_t)((rows + per - 1u) / per);
+    if (dtype == DAF_F32) attention_rows_kernel<float><<<grid, kGenThreads, 0, s>>>(a, lanes, header);
+    else if (dtype == DAF_F16) attention_rows_kernel<__half><<<grid, kGenThreads, 0, s>>>(a, lanes, header);
+    else attention_rows_kernel<__nv_bfloat16><<<grid, kGenThreads, 0, s>>>(a, lanes, header);
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 
 #define DAF_ATTN_BY_TYPE(CALL, ...)                                                                                      \

@@ -1,0 +1,472 @@
+// Attention backward for 16-bit inputs on the tensor cores: one kernel body, two instances.
+//
+//   dk / dv (DKV)  holds 128 keys,    walks the queries of every head that reads them:  T1 = k q^T,  T2 = v grad_out^T
+//   dq             holds 128 queries, walks the keys:                                   T1 = q k^T,  T2 = grad_out v^T
+//   P = exp2(c T1 - L),  dS = P (T2 - delta)      (L = lse log2(e); both operands of T1 and T2 come from shared memory)
+//   dv += P grad_out,  dk += dS q                 /  dq += dS k        (P and dS, 16 bits, from tensor memory)
+//
+// No sum crosses CTAs: no atomics, the same bits every time, and no binary32 copies of the gradients.  The price is that
+// S and dP are computed twice (7 products instead of 5); against it stands that every A operand of a second product is
+// where softmax leaves it -- in tensor memory, row by row -- so that P and dS never pass through shared memory.
+//
+// A persistent CTA (one per SM): warps 0-3 and 4-7 take the walk's blocks of 64 in turn (a thread owns one of the 128
+// rows), warp 8 issues the products, two blocks of T ahead of the sums, warp 9 the copies.  Tensor memory: the sums
+// (up to 256 columns) and two blocks of T1, T2 (2 x 128 columns), P over T1 and dS over T2.  Blocks of 64 rather than 128
+// because two blocks in flight matter more than the wider product.
+// P and dS are rounded to the input type, which the second products need; everything else is binary32.
+#pragma once
+#include "attention.cuh"
+#include "tensor_core.cuh"
+
+namespace daf {
+
+constexpr int kGradThreads = 384;
+constexpr uint32_t kHeld = 128, kWalk = 64;
+
+struct AttnGradArgs {
+    CUtensorMap x1, x2, y1, y2;                  // held: k, v or q, grad_out; walked: q, grad_out or k, v
+    AttnArgs a;
+    uint32_t items, tiles;
+    WorkspaceHeader *header;
+};
+
+template <int DP> struct GradSmem {
+    static constexpr int kHeldBuffers = DP == 128 ? 1 : 2, kStages = DP == 128 ? 4 : 6;
+    static constexpr uint32_t kX = kHeld * DP * 2u, kY = kWalk * DP * 2u;
+    static constexpr uint32_t kStats = 2u * kWalk * 4u;           // -L and -delta of a block's queries
+    static constexpr uint32_t kBytes = kHeldBuffers * 2u * kX + kStages * (2u * kY + kStats) + 1024u;
+};
+
+// The i-th item of a CTA: there and back over the list, which starts with the longest items, so that who got a long
+// one gets a short one next.
+__device__ __forceinline__ uint32_t grad_item(uint32_t i)
+{
+    return i * gridDim.x + (i & 1u ? gridDim.x - 1u - blockIdx.x : blockIdx.x);
+}
+
+template <bool DKV> struct GradItem {
+    uint32_t b, h, first, n;                     // h: key head (DKV) or query head
+    uint32_t start, per_head, blocks;            // the walk: `per_head` blocks from `start` on, for each head
+    __device__ __forceinline__ void set(const AttnGradArgs &p, uint32_t item)
+    {
+        const AttnArgs &a = p.a;
+        const uint32_t heads = DKV ? a.Hkv : a.H, all = a.B * heads;
+        uint32_t tile, bh;
+        if (a.causal) {
+            tile = item / all;
+            bh = item - tile * all;
+            if (!DKV) tile = p.tiles - 1u - tile;
+        } else {
+            bh = item / p.tiles;
+            tile = item - bh * p.tiles;
+        }
+        b = bh / heads;
+        h = bh - b * heads;
+        first = tile * kHeld;
+        n = attn_length(a, b);
+        start = 0;
+        per_head = 0;
+        if (DKV) {
+            const int from = a.causal ? (int)(first + a.Sq) - (int)a.Sk : 0;   // the first query that sees a key of the tile
+            if (from > 0) start = (uint32_t)from / kWalk * kWalk;
+            if (first < n && start < a.Sq) per_head = (a.Sq - start + kWalk - 1u) / kWalk;
+            blocks = per_head * a.group;
+        } else {
+            const uint32_t last = (first + kHeld < a.Sq ? first + kHeld : a.Sq) - 1u;
+            const int end = attn_limit(a, n, (int)last);
+            per_head = blocks = end > 0 ? ((uint32_t)end + kWalk - 1u) / kWalk : 0u;
+        }
+    }
+};
+
+// Walks the blocks of a CTA's items one after another: block `i` of the item, at row `row` of head `head`.
+template <bool DKV> struct GradCursor {
+    GradItem<DKV> it;
+    uint32_t turn, i, row, head, count;          // count: blocks passed, over all items
+    bool more;
+    __device__ __forceinline__ void open(const AttnGradArgs &p)
+    {
+        turn = count = 0;
+        enter(p);
+    }
+    // to the first block of item number `turn`, or of the next one that has blocks
+    __device__ __forceinline__ void enter(const AttnGradArgs &p)
+    {
+        for (;; turn++) {
+            const uint32_t item = grad_item(turn);
+            more = item < p.items;
+            // the way back may pass the list's end before the way there of the same pair does
+            if (!more && turn * gridDim.x >= p.items) return;
+            if (!more) continue;
+            it.set(p, item);
+            if (it.blocks) break;
+        }
+        i = 0;
+        row = it.start;
+        head = DKV ? it.h * p.a.group : it.h / p.a.group;
+    }
+    __device__ __forceinline__ bool last() const { return i + 1u == it.blocks; }
+    __device__ __forceinline__ uint32_t cols(const AttnGradArgs &p) const
+    {
+        const uint32_t left = (DKV ? p.a.Sq : it.n) - row;
+        return left < kWalk ? left : kWalk;
+    }
+    __device__ __forceinline__ void step(const AttnGradArgs &p)
+    {
+        count++;
+        if (++i == it.blocks) {
+            turn++;
+            enter(p);
+            return;
+        }
+        row += kWalk;
+        if (DKV && i % it.per_head == 0) {
+            row = it.start;
+            head++;
+        }
+    }
+};
+
+template <typename T, int DP, bool DKV>
+__global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const __grid_constant__ AttnGradArgs p)
+{
+    using Smem = GradSmem<DP>;
+    constexpr bool BF16 = __is_same(T, __nv_bfloat16);
+    constexpr int STAGES = Smem::kStages, HELD = Smem::kHeldBuffers;
+    constexpr uint32_t XBOX = kHeld * 128u, YBOX = kWalk * 128u;  // bytes of a 64-element box
+    extern __shared__ unsigned char s_raw[];
+    __shared__ __align__(8) uint64_t x_full[HELD], x_empty[HELD], y_full[STAGES], y_empty[STAGES], t_full[2], ps_ready[2], acc_full,
+        acc_empty, tail, drain;
+    __shared__ uint32_t s_tmem, s_abort;
+    unsigned char *const smem = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
+    unsigned char *const s_y = smem + HELD * 2u * Smem::kX;
+    float *const s_stats = reinterpret_cast<float *>(s_y + STAGES * 2u * Smem::kY);
+    const AttnArgs &a = p.a;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    if (threadIdx.x == 0) {
+        s_abort = 0u;
+        for (int i = 0; i < HELD; i++) {
+            bar_init(&x_full[i], 1);
+            bar_init(&x_empty[i], 1);
+        }
+        for (int i = 0; i < STAGES; i++) {
+            bar_init(&y_full[i], 1);
+            bar_init(&y_empty[i], 1);
+        }
+        for (int w = 0; w < 2; w++) {
+            bar_init(&t_full[w], 1);
+            bar_init(&ps_ready[w], 4);
+        }
+        bar_init(&acc_full, 1);
+        bar_init(&acc_empty, 8);
+        bar_init(&tail, 1);
+        bar_init(&drain, 1);
+        fence_async();
+    }
+    if (warp == 0) tmem_alloc(&s_tmem, 512);
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = s_tmem;
+    volatile uint32_t *const stop = &s_abort;
+
+    if (warp < 8) {                                                // ---- probabilities, score gradients, results
+        take_registers<208>();
+        const uint32_t w = warp >> 2, quarter = (warp & 3u) << 21, lane_row = (warp & 3u) * 32u + lane;
+        const uint32_t t1 = tmem + 256u + w * 128u + quarter, t2 = t1 + 64u;
+        uint32_t count = 0, t_ph = 0, acc_ph = 0, stage = 0, y_ph = 0;   // count: blocks passed, over all items and both warpgroups
+        const int off = (int)a.Sk - (int)a.Sq;
+        const uint64_t c2 = pair(a.scale_log2, a.scale_log2);
+        for (uint32_t turn = 0; turn * gridDim.x < p.items; turn++) {
+            const uint32_t item = grad_item(turn);
+            if (item >= p.items) continue;
+            GradItem<DKV> it;
+            it.set(p, item);
+            const uint32_t row = it.first + lane_row, rows = DKV ? a.Sk : a.Sq, live = DKV ? it.n : a.Sq;
+            const bool idle = it.first + (warp & 3u) * 32u >= live; // no row of the warp takes part
+            float nl = 0.0f, nd = 0.0f;
+            int limit = 0;                                          // dq: keys the row sees
+            if (!DKV && it.blocks) {
+                const uint64_t at = ((uint64_t)it.b * a.H + it.h) * a.rows_padded + row;
+                nl = a.row_nl2[at];
+                nd = a.row_ndelta[at];
+                limit = row < a.Sq ? attn_limit(a, it.n, (int)row) : (int)it.n;
+            }
+            uint32_t at = it.start, in_head = 0;
+            bool ok = true;
+            for (uint32_t i = 0; i < it.blocks; i++) {
+                if ((count & 1u) == w) {
+                    if (!(ok = bar_wait(&t_full[w], t_ph, stop))) break;
+                    t_ph ^= 1u;
+                    if (DKV && !(ok = bar_wait(&y_full[stage], y_ph, stop))) break;   // the statistics came by copy
+                    if (!idle) {
+                        tmem_after_sync();
+                        const int cols = (int)((DKV ? a.Sq : it.n) - at);
+                        // the row's visible columns are [lo, hi)
+                        int lo = 0, hi = kWalk;
+                        if (DKV) lo = row >= it.n ? (int)kWalk : a.causal ? (int)row - off - (int)at : 0;
+                        else hi = limit - (int)at;
+                        const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < (int)kWalk);
+                        const float *const st = s_stats + stage * 2u * kWalk;
+#pragma unroll
+                        for (int ch = 0; ch < 2; ch++) {
+                            if (32 * ch < cols) {
+                                float s[32], e[32];
+                                tmem_load32(t1 + 32 * ch, s);
+                                tmem_load32(t2 + 32 * ch, e);
+                                tmem_wait_loads();
+                                uint32_t r1[16], r2[16];
+#pragma unroll
+                                for (int k = 0; k < 8; k++) {      // four columns
+                                    uint64_t l2[2], d2[2];
+                                    if (DKV) {
+                                        const float4 u = *reinterpret_cast<const float4 *>(st + 32 * ch + 4 * k);
+                                        const float4 v = *reinterpret_cast<const float4 *>(st + kWalk + 32 * ch + 4 * k);
+                                        l2[0] = pair(u.x, u.y); l2[1] = pair(u.z, u.w);
+                                        d2[0] = pair(v.x, v.y); d2[1] = pair(v.z, v.w);
+                                    } else {
+                                        l2[0] = l2[1] = pair(nl, nl);
+                                        d2[0] = d2[1] = pair(nd, nd);
+                                    }
+#pragma unroll
+                                    for (int q = 0; q < 2; q++) {
+                                        const int c = 4 * k + 2 * q;
+                                        float u, v, x, y;
+                                        unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
+                                        u = exp2_fast(u);
+                                        v = exp2_fast(v);
+                                        unpair(mul2(pair(u, v), add2(pair(e[c], e[c + 1]), d2[q])), x, y);
+                                        if (masked) {              // selected, not multiplied: what is masked may be NaN
+                                            const int g = 32 * ch + c;
+                                            if (g < lo || g >= hi) u = x = 0.0f;
+                                            if (g + 1 < lo || g + 1 >= hi) v = y = 0.0f;
+                                        }
+                                        r1[2 * k + q] = round2<T>(u, v);
+                                        r2[2 * k + q] = round2<T>(x, y);
+                                    }
+                                }
+                                if (DKV) tmem_store16(t1 + 16 * ch, r1);
+                                tmem_store16(t2 + 16 * ch, r2);
+                            }
+                        }
+                        tmem_wait_stores();
+                        tmem_before_sync();
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&ps_ready[w]);
+                }
+                count++;
+                if (++stage == STAGES) {
+                    stage = 0;
+                    y_ph ^= 1u;
+                }
+                at += kWalk;
+                if (DKV && ++in_head == it.per_head) {
+                    in_head = 0;
+                    at = it.start;
+                }
+            }
+            if (!ok) break;
+            if (it.blocks) {
+                if (!bar_wait(&acc_full, acc_ph, stop)) break;
+                acc_ph ^= 1u;
+                tmem_after_sync();
+            }
+            // DKV: the first warpgroup stores dv, the second dk; dq: half of the columns each
+            const AttnTensor &to = !DKV ? a.dq : w == 0 ? a.dv : a.dk;
+            const float by = DKV && w == 0 ? 1.0f : a.scale;
+            constexpr uint32_t WIDTH = DKV ? DP : DP / 2;
+            const uint32_t from = DKV ? 0u : w * (DP / 2);
+            const uint32_t acc = tmem + w * WIDTH + quarter;
+            const bool any = it.blocks && !idle, keep = any && row < live;
+            char *const dst = reinterpret_cast<char *>(to.p) + 2u * (to.sb * it.b + to.sh * it.h + to.ss * row);
+#pragma unroll
+            for (uint32_t ch = 0; ch < WIDTH / 32; ch++) {
+                float o[32];
+                if (any) {
+                    tmem_load32(acc + 32 * ch, o);
+                    tmem_wait_loads();
+                }
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const uint32_t d = from + 32u * ch + 8u * k;
+                    if (row < rows && d < a.D) {
+                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                        if (keep) {
+                            v.x = round2<T>(o[8 * k] * by, o[8 * k + 1] * by);
+                            v.y = round2<T>(o[8 * k + 2] * by, o[8 * k + 3] * by);
+                            v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
+                            v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
+                        }
+                        *reinterpret_cast<uint4 *>(dst + 2u * d) = v;
+                    }
+                }
+            }
+            if (it.blocks) {
+                tmem_before_sync();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&acc_empty);
+            }
+        }
+    } else {
+        leave_registers<88>();
+        if (warp == 9) {                                           // ---- copies
+            GradCursor<DKV> cur;
+            uint32_t st = 0, ph = 1, x = 0, x_ph = 1, tail_ph = 0;
+            for (cur.open(p); cur.more; cur.step(p)) {
+                const bool one = lane == 0;
+                if (cur.i == 0) {
+                    if (!bar_wait(&x_empty[x], x_ph, stop)) break;
+                    if (one) {
+                        const uint32_t dst = smem_u32(smem) + x * 2u * Smem::kX;
+                        bar_expect(&x_full[x], 2u * Smem::kX);
+                        for (int e = 0; e < DP / 64; e++) {
+                            tma_load(dst + e * XBOX, &p.x1, &x_full[x], 64 * e, cur.it.h, cur.it.first, cur.it.b);
+                            tma_load(dst + Smem::kX + e * XBOX, &p.x2, &x_full[x], 64 * e, cur.it.h, cur.it.first, cur.it.b);
+                        }
+                    }
+                    if (++x == HELD) {
+                        x = 0;
+                        x_ph ^= 1u;
+                    }
+                }
+                if (!bar_wait(&y_empty[st], ph, stop)) break;
+                const uint32_t cols = cur.cols(p), end = (cols + 15u) & ~15u;
+                // dS is zero in a masked column, but 0 * NaN is not: rows of k behind the sequence's end that the last
+                // product's steps of 16 keys still touch are cleared
+                const bool clear = !DKV && cur.it.n < a.Sk && cols != end;
+                uint64_t *const bar = clear ? &tail : &y_full[st];
+                unsigned char *const dst = s_y + st * 2u * Smem::kY;
+                if (one) {
+                    bar_expect(bar, 2u * Smem::kY + (DKV ? Smem::kStats : 0u));
+                    for (int e = 0; e < DP / 64; e++) {
+                        tma_load(smem_u32(dst) + e * YBOX, &p.y1, bar, 64 * e, cur.head, cur.row, cur.it.b);
+                        tma_load(smem_u32(dst) + Smem::kY + e * YBOX, &p.y2, bar, 64 * e, cur.head, cur.row, cur.it.b);
+                    }
+                    if (DKV) {
+                        const uint64_t at = ((uint64_t)cur.it.b * a.H + cur.head) * a.rows_padded + cur.row;
+                        bulk_load(smem_u32(s_stats + st * 2u * kWalk), a.row_nl2 + at, kWalk * 4u, bar);
+                        bulk_load(smem_u32(s_stats + st * 2u * kWalk + kWalk), a.row_ndelta + at, kWalk * 4u, bar);
+                    }
+                }
+                if (clear) {
+                    if (!bar_wait(&tail, tail_ph, stop)) break;
+                    tail_ph ^= 1u;
+                    for (uint32_t i = lane; i < (end - cols) * 8u * (DP / 64); i += 32u)
+                        *reinterpret_cast<uint4 *>(dst + i / (8u * (end - cols)) * YBOX + (cols * 8u + i % (8u * (end - cols))) * 16u) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                    fence_async();
+                    __syncwarp();
+                    if (one) bar_arrive(&y_full[st]);
+                }
+                if (++st == STAGES) {
+                    st = 0;
+                    ph ^= 1u;
+                }
+            }
+            if (*stop) {                                           // giving up: let the copies in flight land first
+                const uint64_t until = now_ns() + 1000000000ull;
+                while (now_ns() < until) __nanosleep(1000);
+            }
+        } else if (warp == 8 && lane == 0) {                       // ---- products
+            const uint32_t steps = (a.D + 15u) / 16u;
+            const uint32_t acc_desc = product_desc(BF16, steps * 16u, true);
+            const uint32_t xs = smem_u32(smem), ys = smem_u32(s_y);
+            GradCursor<DKV> ahead, cur;
+            ahead.open(p);
+            cur.open(p);
+            uint32_t t_st = 0, t_phase = 0, x = 0, x_ph = 0, c_st = 0, acc_ph = 1, ps_ph[2] = {0, 0};
+            bool ok = true;
+            // T1 and T2 of the block `ahead` stands at
+            auto scores = [&]() {
+                if (!ahead.more) return;
+                if (ahead.i == 0 && !(ok = bar_wait(&x_full[x], x_ph, stop))) return;
+                if (!(ok = bar_wait(&y_full[t_st], t_phase, stop))) return;
+                tmem_after_sync();
+                const uint32_t w = ahead.count & 1u, t = tmem + 256u + w * 128u;
+                const uint32_t desc = product_desc(BF16, (ahead.cols(p) + 15u) & ~15u, false);
+                for (uint32_t k = 0; k < 2; k++) {
+                    const uint64_t A = operand_desc(xs + x * 2u * Smem::kX + k * Smem::kX, 16), B = operand_desc(ys + t_st * 2u * Smem::kY + k * Smem::kY, 16);
+                    for (uint32_t s = 0; s < steps; s++)
+                        product_ss(t + k * 64u, A + (s & 3u) * 2u + (s >> 2) * (XBOX / 16u), B + (s & 3u) * 2u + (s >> 2) * (YBOX / 16u), desc, s > 0);
+                }
+                products_done(&t_full[w]);
+                if (ahead.last()) {
+                    products_done(&x_empty[x]);
+                    if (++x == HELD) {
+                        x = 0;
+                        x_ph ^= 1u;
+                    }
+                }
+                if (++t_st == STAGES) {
+                    t_st = 0;
+                    t_phase ^= 1u;
+                }
+                ahead.step(p);
+            };
+            scores();
+            if (ok) scores();
+            for (; ok && cur.more; cur.step(p)) {
+                const uint32_t w = cur.count & 1u, t = tmem + 256u + w * 128u, n16 = (cur.cols(p) + 15u) / 16u;
+                if (!bar_wait(&ps_ready[w], ps_ph[w], stop)) break;
+                ps_ph[w] ^= 1u;
+                if (cur.i == 0) {
+                    if (!bar_wait(&acc_empty, acc_ph, stop)) break;
+                    acc_ph ^= 1u;
+                }
+                tmem_after_sync();
+                const uint64_t y1 = operand_desc(ys + c_st * 2u * Smem::kY, YBOX), y2 = operand_desc(ys + c_st * 2u * Smem::kY + Smem::kY, YBOX);
+                if (DKV) {
+                    for (uint32_t s = 0; s < n16; s++) product_ts(tmem, t + s * 8u, y2 + s * 128u, acc_desc, cur.i > 0 || s > 0);
+                    for (uint32_t s = 0; s < n16; s++) product_ts(tmem + DP, t + 64u + s * 8u, y1 + s * 128u, acc_desc, cur.i > 0 || s > 0);
+                } else {
+                    for (uint32_t s = 0; s < n16; s++) product_ts(tmem, t + 64u + s * 8u, y1 + s * 128u, acc_desc, cur.i > 0 || s > 0);
+                }
+                products_done(&y_empty[c_st]);
+                if (cur.last()) products_done(&acc_full);
+                if (++c_st == STAGES) c_st = 0;
+                scores();
+            }
+            products_done(&drain);
+            bar_wait(&drain, 0, stop);
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s_abort) p.header->status = DAF_ERR_TIMEOUT;
+    if (warp == 0) tmem_free(tmem, 512);
+}
+
+template <typename T, int DP, bool DKV> static daf_status launch_grad(const AttnGradArgs &p, cudaStream_t s)
+{
+    int ctas = 0;
+    const auto kernel = &attention_grad_kernel<T, DP, DKV>;
+    if (persistent_ctas(reinterpret_cast<const void *>(kernel), kGradThreads, (int)GradSmem<DP>::kBytes, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    kernel<<<p.items < (uint32_t)ctas ? p.items : (uint32_t)ctas, kGradThreads, GradSmem<DP>::kBytes, s>>>(p);
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
+
+// Keys and queries both exist (the entry point writes the gradients of the other cases).
+template <typename T> daf_status attn_backward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s)
+{
+    const bool bf16 = __is_same(T, __nv_bfloat16);
+    AttnGradArgs p;
+    p.a = a;
+    p.header = header;
+    const auto maps = [&](const AttnTensor &x1, const AttnTensor &x2, uint32_t Sx, uint32_t Hx, const AttnTensor &y1, const AttnTensor &y2, uint32_t Sy, uint32_t Hy) {
+        return attn_tensor_map(&p.x1, bf16, x1, a.B, Sx, Hx, a.D, kHeld) && attn_tensor_map(&p.x2, bf16, x2, a.B, Sx, Hx, a.D, kHeld) &&
+               attn_tensor_map(&p.y1, bf16, y1, a.B, Sy, Hy, a.D, kWalk) && attn_tensor_map(&p.y2, bf16, y2, a.B, Sy, Hy, a.D, kWalk);
+    };
+    if (!maps(a.k, a.v, a.Sk, a.Hkv, a.q, a.grad_out, a.Sq, a.H)) return DAF_ERR_CUDA;
+    p.tiles = (a.Sk + kHeld - 1u) / kHeld;
+    p.items = p.tiles * a.B * a.Hkv;
+    daf_status st = a.D <= 64u ? launch_grad<T, 64, true>(p, s) : launch_grad<T, 128, true>(p, s);
+    if (st != DAF_OK) return st;
+    if (!maps(a.q, a.grad_out, a.Sq, a.H, a.k, a.v, a.Sk, a.Hkv)) return DAF_ERR_CUDA;
+    p.tiles = (a.Sq + kHeld - 1u) / kHeld;
+    p.items = p.tiles * a.B * a.H;
+    st = a.D <= 64u ? launch_grad<T, 64, false>(p, s) : launch_grad<T, 128, false>(p, s);
+    return st;
+}
+
+}  // namespace daf
