@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     __shared__ uint32_t s_tmem, s_abort;
     unsigned char *const smem = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
     const AttnArgs &a = p.a;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
     if (threadIdx.x == 0) {
         s_abort = 0u;
         bar_init(&q_full, 1);
@@ -291,71 +291,74 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 while (now_ns() < until) __nanosleep(1000);
             }
         } else if (warp == 8) {                                        // ---- products
-            if (lane == 0) {
-                uint32_t st = 0, ph = 0, q_ph = 0, p_ph[2] = {0, 0};
-                const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2u * Smem::kTile;
-                const uint32_t steps = (a.D + 15u) / 16u;              // of the first product
-                const uint32_t pv_desc = product_desc(BF16, steps * 16u, true);
-                for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
-                    const FwdItem it(p, item);
-                    if (it.both == 0) continue;
-                    if (!bar_wait(&q_full, q_ph, stop)) break;
-                    q_ph ^= 1u;
-                    // S of half w for the key block in stage `at`
-                    auto scores = [&](int w, int j, uint32_t at) {
-                        const uint32_t valid = it.n - (uint32_t)j * kBlock, cols = valid < (uint32_t)kBlock ? (valid + 15u) & ~15u : kBlock;
-                        const uint32_t desc = product_desc(BF16, cols, false);
-                        const uint64_t q = operand_desc(q_smem + w * Smem::kTile, 16), k = operand_desc(kv_smem + at * Smem::kTile, 16);
-                        for (uint32_t s = 0; s < steps; s++) {
-                            const uint32_t by = (s & 3u) * 2u + (s >> 2) * 1024u;         // 32 bytes along the row, 16 KiB per 64 elements
-                            product_ss(tmem + w * 128u, q + by, k + by, desc, s > 0);
-                        }
-                        products_done(&s_full[w]);
-                    };
-                    auto next = [&]() {
-                        if (++st == STAGES) {
-                            st = 0;
-                            ph ^= 1u;
-                        }
-                    };
-                    if (!bar_wait(&kv_full[st], ph, stop)) break;
-                    tmem_after_sync();
-                    for (int w = 0; w < 2; w++)
-                        if (it.blocks[w] > 0) scores(w, 0, st);
-                    products_done(&kv_empty[st]);
-                    if (it.both == 1) products_done(&q_empty);
-                    next();
-                    for (int j = 0; j < it.both; j++) {
-                        const uint32_t v_st = st;
-                        if (!bar_wait(&kv_full[st], ph, stop)) break;
-                        next();
-                        const bool more = j + 1 < it.both;
-                        if (more && !bar_wait(&kv_full[st], ph, stop)) break;
-                        const uint32_t valid = it.n - (uint32_t)j * kBlock;
-                        const uint32_t pv_steps = valid < (uint32_t)kBlock ? (valid + 15u) / 16u : kBlock / 16;
-                        for (int w = 0; w < 2; w++) {
-                            if (j >= it.blocks[w]) continue;
-                            if (!bar_wait(&p_ready[w], p_ph[w], stop)) break;
-                            p_ph[w] ^= 1u;
-                            tmem_after_sync();
-                            const uint64_t v = operand_desc(kv_smem + v_st * Smem::kTile, 16384);
-                            for (uint32_t s = 0; s < pv_steps; s++)                      // 16 keys: 2 KiB of v, 8 columns of P
-                                product_ts(tmem + 256u + w * DP, tmem + w * 128u + s * 8u, v + s * 128u, pv_desc, j > 0 || s > 0);
-                            products_done(&o_done[w]);
-                            if (j + 1 < it.blocks[w]) scores(w, j + 1, st);
-                        }
-                        products_done(&kv_empty[v_st]);
-                        if (more) {
-                            products_done(&kv_empty[st]);
-                            if (j + 2 == it.both) products_done(&q_empty);
-                            next();
-                        }
+            const uint32_t one = elect_lane();
+            uint32_t st = 0, ph = 0, q_ph = 0, p_ph[2] = {0, 0};
+            const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2u * Smem::kTile;
+            const uint32_t steps = (a.D + 15u) / 16u;              // of the first product
+            const uint32_t pv_desc = product_desc(BF16, steps * 16u, true);
+            for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
+                const FwdItem it(p, item);
+                if (it.both == 0) continue;
+                if (!bar_wait(&q_full, q_ph, stop)) break;
+                q_ph ^= 1u;
+                // S of half w for the key block in stage `at`
+                auto scores = [&](int w, int j, uint32_t at) {
+                    const uint32_t valid = it.n - (uint32_t)j * kBlock, cols = valid < (uint32_t)kBlock ? (valid + 15u) & ~15u : kBlock;
+                    const uint32_t desc = product_desc(BF16, cols, false);
+                    const uint64_t q = operand_desc(q_smem + w * Smem::kTile, 16), k = operand_desc(kv_smem + at * Smem::kTile, 16);
+#pragma unroll
+                    for (uint32_t s = 0; s < DP / 16; s++) {
+                        const uint32_t by = (s & 3u) * 2u + (s >> 2) * 1024u;         // 32 bytes along the row, 16 KiB per 64 elements
+                        if (s < steps) product_ss(one, tmem + w * 128u, q + by, k + by, desc, s > 0);
                     }
-                    if (*stop) break;
+                    products_done(one, &s_full[w]);
+                };
+                auto next = [&]() {
+                    if (++st == STAGES) {
+                        st = 0;
+                        ph ^= 1u;
+                    }
+                };
+                if (!bar_wait(&kv_full[st], ph, stop)) break;
+                tmem_after_sync();
+#pragma unroll
+                for (int w = 0; w < 2; w++)
+                    if (it.blocks[w] > 0) scores(w, 0, st);
+                products_done(one, &kv_empty[st]);
+                if (it.both == 1) products_done(one, &q_empty);
+                next();
+                for (int j = 0; j < it.both; j++) {
+                    const uint32_t v_st = st;
+                    if (!bar_wait(&kv_full[st], ph, stop)) break;
+                    next();
+                    const bool more = j + 1 < it.both;
+                    if (more && !bar_wait(&kv_full[st], ph, stop)) break;
+                    const uint32_t valid = it.n - (uint32_t)j * kBlock;
+                    const uint32_t pv_steps = valid < (uint32_t)kBlock ? (valid + 15u) / 16u : kBlock / 16;
+#pragma unroll
+                    for (int w = 0; w < 2; w++) {
+                        if (j >= it.blocks[w]) continue;
+                        if (!bar_wait(&p_ready[w], p_ph[w], stop)) break;
+                        p_ph[w] ^= 1u;
+                        tmem_after_sync();
+                        const uint64_t v = operand_desc(kv_smem + v_st * Smem::kTile, 16384);
+#pragma unroll
+                        for (uint32_t s = 0; s < kBlock / 16; s++)                   // 16 keys: 2 KiB of v, 8 columns of P
+                            if (s < pv_steps) product_ts(one, tmem + 256u + w * DP, tmem + w * 128u + s * 8u, v + s * 128u, pv_desc, j > 0 || s > 0);
+                        products_done(one, &o_done[w]);
+                        if (j + 1 < it.blocks[w]) scores(w, j + 1, st);
+                    }
+                    products_done(one, &kv_empty[v_st]);
+                    if (more) {
+                        products_done(one, &kv_empty[st]);
+                        if (j + 2 == it.both) products_done(one, &q_empty);
+                        next();
+                    }
                 }
-                products_done(&drain);
-                bar_wait(&drain, 0, stop);
+                if (*stop) break;
             }
+            products_done(one, &drain);
+            bar_wait(&drain, 0, stop);
         }
     }
     tmem_before_sync();

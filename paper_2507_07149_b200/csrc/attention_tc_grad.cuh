@@ -82,7 +82,7 @@ template <bool DKV> struct GradItem {
 // Walks the blocks of a CTA's items one after another: block `i` of the item, at row `row` of head `head`.
 template <bool DKV> struct GradCursor {
     GradItem<DKV> it;
-    uint32_t turn, i, row, head, count;          // count: blocks passed, over all items
+    uint32_t turn, i, in_head, row, head, count; // count: blocks passed, over all items
     bool more;
     __device__ __forceinline__ void open(const AttnGradArgs &p)
     {
@@ -101,7 +101,7 @@ template <bool DKV> struct GradCursor {
             it.set(p, item);
             if (it.blocks) break;
         }
-        i = 0;
+        i = in_head = 0;
         row = it.start;
         head = DKV ? it.h * p.a.group : it.h / p.a.group;
     }
@@ -120,7 +120,8 @@ template <bool DKV> struct GradCursor {
             return;
         }
         row += kWalk;
-        if (DKV && i % it.per_head == 0) {
+        if (DKV && ++in_head == it.per_head) {
+            in_head = 0;
             row = it.start;
             head++;
         }
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
     unsigned char *const s_y = smem + HELD * 2u * Smem::kX;
     float *const s_stats = reinterpret_cast<float *>(s_y + STAGES * 2u * Smem::kY);
     const AttnArgs &a = p.a;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
     if (threadIdx.x == 0) {
         s_abort = 0u;
         for (int i = 0; i < HELD; i++) {
@@ -208,13 +209,17 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                         else hi = limit - (int)at;
                         const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < (int)kWalk);
                         const float *const st = s_stats + stage * 2u * kWalk;
+                        float s[64], e[64];
+#pragma unroll
+                        for (int ch = 0; ch < 2; ch++)
+                            if (32 * ch < cols) {
+                                tmem_load32(t1 + 32 * ch, s + 32 * ch);
+                                tmem_load32(t2 + 32 * ch, e + 32 * ch);
+                            }
+                        tmem_wait_loads();
 #pragma unroll
                         for (int ch = 0; ch < 2; ch++) {
                             if (32 * ch < cols) {
-                                float s[32], e[32];
-                                tmem_load32(t1 + 32 * ch, s);
-                                tmem_load32(t2 + 32 * ch, e);
-                                tmem_wait_loads();
                                 uint32_t r1[16], r2[16];
 #pragma unroll
                                 for (int k = 0; k < 8; k++) {      // four columns
@@ -230,19 +235,23 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                                     }
 #pragma unroll
                                     for (int q = 0; q < 2; q++) {
-                                        const int c = 4 * k + 2 * q;
+                                        const int c = 32 * ch + 4 * k + 2 * q;
                                         float u, v, x, y;
                                         unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
                                         u = exp2_fast(u);
                                         v = exp2_fast(v);
                                         unpair(mul2(pair(u, v), add2(pair(e[c], e[c + 1]), d2[q])), x, y);
-                                        if (masked) {              // selected, not multiplied: what is masked may be NaN
-                                            const int g = 32 * ch + c;
-                                            if (g < lo || g >= hi) u = x = 0.0f;
-                                            if (g + 1 < lo || g + 1 >= hi) v = y = 0.0f;
-                                        }
                                         r1[2 * k + q] = round2<T>(u, v);
                                         r2[2 * k + q] = round2<T>(x, y);
+                                    }
+                                }
+                                if (masked) {                      // cleared, not multiplied: what is masked may be NaN
+#pragma unroll
+                                    for (int k = 0; k < 16; k++) {
+                                        const int g = 32 * ch + 2 * k;
+                                        const uint32_t m = (g >= lo && g < hi ? 0xFFFFu : 0u) | (g + 1 >= lo && g + 1 < hi ? 0xFFFF0000u : 0u);
+                                        r1[k] &= m;
+                                        r2[k] &= m;
                                     }
                                 }
                                 if (DKV) tmem_store16(t1 + 16 * ch, r1);
@@ -368,7 +377,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 const uint64_t until = now_ns() + 1000000000ull;
                 while (now_ns() < until) __nanosleep(1000);
             }
-        } else if (warp == 8 && lane == 0) {                       // ---- products
+        } else if (warp == 8) {                                    // ---- products
+            const uint32_t one = elect_lane();
             const uint32_t steps = (a.D + 15u) / 16u;
             const uint32_t acc_desc = product_desc(BF16, steps * 16u, true);
             const uint32_t xs = smem_u32(smem), ys = smem_u32(s_y);
@@ -385,14 +395,17 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 tmem_after_sync();
                 const uint32_t w = ahead.count & 1u, t = tmem + 256u + w * 128u;
                 const uint32_t desc = product_desc(BF16, (ahead.cols(p) + 15u) & ~15u, false);
+#pragma unroll
                 for (uint32_t k = 0; k < 2; k++) {
                     const uint64_t A = operand_desc(xs + x * 2u * Smem::kX + k * Smem::kX, 16), B = operand_desc(ys + t_st * 2u * Smem::kY + k * Smem::kY, 16);
-                    for (uint32_t s = 0; s < steps; s++)
-                        product_ss(t + k * 64u, A + (s & 3u) * 2u + (s >> 2) * (XBOX / 16u), B + (s & 3u) * 2u + (s >> 2) * (YBOX / 16u), desc, s > 0);
+#pragma unroll
+                    for (uint32_t s = 0; s < DP / 16; s++)
+                        if (s < steps)
+                            product_ss(one, t + k * 64u, A + ((s & 3u) * 2u + (s >> 2) * (XBOX / 16u)), B + ((s & 3u) * 2u + (s >> 2) * (YBOX / 16u)), desc, s > 0);
                 }
-                products_done(&t_full[w]);
+                products_done(one, &t_full[w]);
                 if (ahead.last()) {
-                    products_done(&x_empty[x]);
+                    products_done(one, &x_empty[x]);
                     if (++x == HELD) {
                         x = 0;
                         x_ph ^= 1u;
@@ -416,18 +429,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 }
                 tmem_after_sync();
                 const uint64_t y1 = operand_desc(ys + c_st * 2u * Smem::kY, YBOX), y2 = operand_desc(ys + c_st * 2u * Smem::kY + Smem::kY, YBOX);
-                if (DKV) {
-                    for (uint32_t s = 0; s < n16; s++) product_ts(tmem, t + s * 8u, y2 + s * 128u, acc_desc, cur.i > 0 || s > 0);
-                    for (uint32_t s = 0; s < n16; s++) product_ts(tmem + DP, t + 64u + s * 8u, y1 + s * 128u, acc_desc, cur.i > 0 || s > 0);
-                } else {
-                    for (uint32_t s = 0; s < n16; s++) product_ts(tmem, t + 64u + s * 8u, y1 + s * 128u, acc_desc, cur.i > 0 || s > 0);
-                }
-                products_done(&y_empty[c_st]);
-                if (cur.last()) products_done(&acc_full);
+                const bool add = cur.i > 0;
+#pragma unroll
+                for (uint32_t s = 0; s < kWalk / 16; s++)
+                    if (DKV && s < n16) product_ts(one, tmem, t + s * 8u, y2 + s * 128u, acc_desc, add || s > 0);
+#pragma unroll
+                for (uint32_t s = 0; s < kWalk / 16; s++)
+                    if (s < n16) product_ts(one, tmem + (DKV ? DP : 0), t + 64u + s * 8u, y1 + s * 128u, acc_desc, add || s > 0);
+                products_done(one, &y_empty[c_st]);
+                if (cur.last()) products_done(one, &acc_full);
                 if (++c_st == STAGES) c_st = 0;
                 scores();
             }
-            products_done(&drain);
+            products_done(one, &drain);
             bar_wait(&drain, 0, stop);
         }
     }

@@ -133,22 +133,32 @@ __device__ __forceinline__ uint32_t product_desc(bool bf16, uint32_t n, bool acr
     const uint32_t t = bf16 ? 1u : 0u;
     return 1u << 4 | t << 7 | t << 10 | (across ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
 }
-__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+// One lane of the (whole, converged) warp.  The products are issued by that lane under a predicate while the warp computes
+// their operands together: those then stay in uniform registers, which the instructions take; inside a branch of one lane
+// every operand would be moved there for each product.
+__device__ __forceinline__ uint32_t elect_lane()
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
 }
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+__device__ __forceinline__ void product_ss(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(one) : "memory");
 }
-// The barrier is arrived at when every product issued so far by this thread is done.
-__device__ __forceinline__ void products_done(uint64_t *bar)
+__device__ __forceinline__ void product_ts(uint32_t one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(one) : "memory");
+}
+// The barrier is arrived at when every product issued so far by this lane is done.
+__device__ __forceinline__ void products_done(uint32_t one, uint64_t *bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(one) : "memory");
 }
 
 // A warpgroup's share of the registers the CTA was launched with (its shares must not add up to more).
