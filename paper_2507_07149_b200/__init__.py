@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -214,22 +215,31 @@ def _torch():
     return torch
 
 
+_codes = {}
+
+
+def _dtype_codes() -> dict:
+    """torch dtype -> daf_dtype."""
+    if not _codes:
+        torch = _torch()
+        _codes.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    return _codes
+
+
 def dtype_code(t) -> int:
-    torch = _torch()
-    return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}[t.dtype]
+    return _dtype_codes()[t.dtype]
 
 
 def _call(fn, ref, stream, *args) -> int:
     """Calls fn(*args, stream) with the device of tensor `ref` current in this thread (the library launches on the
     current device) and, unless a stream is given, on torch's current stream OF THAT DEVICE.  Returns the status."""
-    torch = _torch()
-    dev = ref.device
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    if dev.index == torch.cuda.current_device():
-        return int(fn(*args, int(stream.cuda_stream)))
-    with torch.cuda.device(dev):
-        return int(fn(*args, int(stream.cuda_stream)))
+    cuda = _torch().cuda
+    index = ref.get_device()
+    raw = cuda.current_stream(index).cuda_stream if stream is None else stream.cuda_stream
+    if index == cuda.current_device():
+        return int(fn(*args, raw))
+    with cuda.device(index):
+        return int(fn(*args, raw))
 
 
 def _ptr(t) -> int:
@@ -548,42 +558,86 @@ def daf_clip_norm_batch(d_in, d_out, max_norm, eps, d_norm, d_workspace, workspa
     _check(status, "daf_clip_norm_batch")
 
 
-def _same_kind(where: str, ref, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and (t.device != ref.device or t.dtype != ref.dtype):
-            raise ValueError(f"{where}: {name} is {t.dtype} on {t.device}, expected {ref.dtype} on {ref.device}")
+_MAX_REMEMBERED = 4096                                              # shapes whose parameter blocks are kept
 
 
-def _strided(t):
-    """t itself when the attention kernels can address it (rows contiguous and on 16-byte boundaries, nothing broadcast), else
-    a contiguous copy."""
-    unit = 16 // t.element_size()
-    s = t.stride()
-    if s[3] == 1 and t.data_ptr() % 16 == 0 and all(t.shape[i] <= 1 or (s[i] % unit == 0 and s[i] >= t.shape[3]) for i in (0, 1, 2)):
-        return t
-    t = t.contiguous()
-    return t if t.data_ptr() % 16 == 0 else t.clone()
+def _remember(cache: dict, key, value):
+    if len(cache) >= _MAX_REMEMBERED:
+        cache.clear()
+    cache[key] = value
+    return value
 
 
-def _stride3(t):
-    s = t.stride()
-    return _u64x3(s[0], s[1], s[2])
+def _one_device(where: str, index: int, tensors) -> None:
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"{where}: all tensors belong on one CUDA device")
 
 
-def _attention_params(where: str, q, k, v, causal, scale, key_lengths) -> daf_attention_params:
-    if not q.is_cuda or q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+_attention_plans = {}
+
+
+class _AttentionPlan:
+    """What a call of attention / attention_grad derives from types, shapes and strides alone: remembered per shape, since a
+    model repeats the same ones every step.  `direct`: which of the tensors the kernels can address in place."""
+    __slots__ = ("params", "ref", "ws", "lse_shape", "direct")
+
+
+def _attention_plan(where: str, causal, scale, tensors) -> _AttentionPlan:
+    """tensors: q, k, v, out or None, and for the backward pass grad_out, grad_q, grad_k, grad_v (None: to be allocated)."""
+    torch = _torch()
+    q, k, v = tensors[:3]
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
         raise ValueError(f"{where} expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
     (b, sq, h, d), (bk, sk, hkv, dk) = q.shape, k.shape
     if b != bk or d != dk or hkv == 0 or h % hkv:
         raise ValueError(f"{where}: q {tuple(q.shape)} and k {tuple(k.shape)} do not belong together")
-    _same_kind(where, q, k=k, v=v)
-    if key_lengths is not None and (key_lengths.dtype != _torch().int32 or key_lengths.device != q.device
-                                    or tuple(key_lengths.shape) != (b,) or not key_lengths.is_contiguous()):
-        raise ValueError(f"{where}: key_lengths is an int32 tensor of {b} lengths on {q.device}")
+    if q.dtype not in _dtype_codes():
+        raise ValueError(f"{where}: {q.dtype} is not supported")
+    like_q = (q, k, v, q, q, q, k, v)
+    names = ("q", "k", "v", "out", "grad_out", "grad_q", "grad_k", "grad_v")
+    for name, t, l in zip(names, tensors, like_q):
+        if t is not None and (t.dtype != q.dtype or t.shape != l.shape):
+            raise ValueError(f"{where}: {name} is {t.dtype} {tuple(t.shape)}, expected {q.dtype} {tuple(l.shape)}")
+    plan = _AttentionPlan()
     p = daf_attention_params(ctypes.sizeof(daf_attention_params), dtype_code(q), b, sq, sk, h, hkv, d, 1 if causal else 0,
                              d ** -0.5 if scale is None else scale)
-    p.q_stride, p.k_stride, p.v_stride = _stride3(q), _stride3(k), _stride3(v)
-    return p
+    unit, direct = 16 // q.element_size(), []
+    for i, (name, t, l) in enumerate(zip(names, tensors, like_q)):
+        dense = (l.shape[1] * l.shape[2] * d, l.shape[2] * d, d)
+        s = dense + (1,) if t is None else t.stride()
+        fine = s[3] == 1 and all(l.shape[j] <= 1 or (s[j] % unit == 0 and s[j] >= d) for j in range(3))
+        if not fine and t is not None and (i >= 5 or (i == 3 and len(tensors) == 4)):
+            raise ValueError(f"{where}: {name} needs a contiguous last dimension and rows on 16-byte boundaries")
+        getattr(p, name + "_stride")[:] = s[:3] if fine else dense
+        direct.append(fine)
+    plan.params, plan.ref, plan.direct = p, ctypes.byref(p), direct
+    plan.ws = daf_attention_workspace(p) if len(tensors) == 4 else daf_attention_grad_workspace(p)
+    plan.lse_shape = (b, h, sq)
+    return plan
+
+
+def _addressable(t, direct: bool):
+    """(tensor, address) of t, or of a contiguous copy where the kernels cannot address it."""
+    if direct:
+        at = t.data_ptr()
+        if not at & 15:
+            return t, at
+    t = t.contiguous()
+    if t.data_ptr() & 15:
+        t = t.clone()
+    return t, t.data_ptr()
+
+
+def _check_lengths(where, lengths, q):
+    if lengths is not None and (lengths.dtype != _torch().int32 or lengths.get_device() != q.get_device()
+                                or tuple(lengths.shape) != (q.shape[0],) or not lengths.is_contiguous()):
+        raise ValueError(f"{where}: key_lengths is an int32 tensor of {q.shape[0]} lengths on {q.device}")
+
+
+def _check_lse(where, lse, shape, q):
+    if tuple(lse.shape) != shape or lse.dtype != _torch().float32 or lse.get_device() != q.get_device() or not lse.is_contiguous():
+        raise ValueError(f"{where}: lse is a contiguous float32 tensor [B, H, Sq] on {q.device}")
 
 
 def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None, out=None, lse=None,
@@ -593,22 +647,33 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
     first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq."""
     torch = _torch()
-    q, k, v = _strided(q), _strided(k), _strided(v)
-    p = _attention_params("attention", q, k, v, causal, scale, key_lengths)
+    index = q.get_device()
+    if index < 0:
+        raise ValueError("attention expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
+    if k.get_device() != index or v.get_device() != index:
+        _one_device("attention", index, (k, v))
+    key = (q.dtype, k.dtype, v.dtype, q.shape, k.shape, v.shape, q.stride(), k.stride(), v.stride(), causal, scale,
+           None if out is None else (out.dtype, out.shape, out.stride()))
+    plan = _attention_plans.get(key)
+    if plan is None:
+        plan = _remember(_attention_plans, key, _attention_plan("attention", causal, scale, (q, k, v, out)))
+    if key_lengths is not None:
+        _check_lengths("attention", key_lengths, q)
+    direct = plan.direct
+    (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
+    dev = q.device
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    else:
+        _one_device("attention", index, (out,))
     if lse is None:
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-    _same_kind("attention", q, out=out)
-    if out.shape != q.shape or tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 \
-            or lse.device != q.device or not lse.is_contiguous():
-        raise ValueError("attention: out has the shape of q, lse is a contiguous float32 tensor [B, H, Sq]")
-    p.out_stride = _stride3(out)
-    if out.stride(3) != 1:
-        raise ValueError("attention: the last dimension of out must be contiguous")
-    n = daf_attention_workspace(p)
-    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    daf_attention(p, q, k, v, key_lengths, out, lse, ws, n, stream)
+        lse = torch.empty(plan.lse_shape, dtype=torch.float32, device=dev)
+    else:
+        _check_lse("attention", lse, plan.lse_shape, q)
+    ws = torch.empty(plan.ws, dtype=torch.uint8, device=dev)
+    status = _call(lib().daf_attention, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), out.data_ptr(), lse.data_ptr(),
+                   ws.data_ptr(), plan.ws)
+    _check(status, "daf_attention")
     if check:
         _check(daf_poll_status(ws, stream), "daf_attention (device status)")
     return out, lse
@@ -619,48 +684,90 @@ def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: 
     """(grad_q, grad_k, grad_v) of ``attention`` from its inputs, its two results and grad_out (daf_attention_grad).  grads:
     three tensors to write into (they may be slices of one packed gradient), fresh contiguous ones by default."""
     torch = _torch()
-    q, k, v, out, grad_out = _strided(q), _strided(k), _strided(v), _strided(out), _strided(grad_out)
-    p = _attention_params("attention_grad", q, k, v, causal, scale, key_lengths)
+    index = q.get_device()
+    if index < 0:
+        raise ValueError("attention_grad expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
+    _one_device("attention_grad", index, (k, v, out, grad_out))
+    key = (q.dtype, k.dtype, v.dtype, out.dtype, grad_out.dtype, q.shape, k.shape, v.shape, out.shape, grad_out.shape, q.stride(),
+           k.stride(), v.stride(), out.stride(), grad_out.stride(), causal, scale,
+           None if grads is None else tuple((t.dtype, t.shape, t.stride()) for t in grads))
+    plan = _attention_plans.get(key)
+    if plan is None:
+        plan = _remember(_attention_plans, key, _attention_plan("attention_grad", causal, scale,
+                                                                (q, k, v, out, grad_out) + tuple(grads or (None, None, None))))
+    if key_lengths is not None:
+        _check_lengths("attention_grad", key_lengths, q)
+    _check_lse("attention_grad", lse, plan.lse_shape, q)
+    direct = plan.direct
+    (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
+    (out, oa), (grad_out, ga) = _addressable(out, direct[3]), _addressable(grad_out, direct[4])
+    dev = q.device
     if grads is None:
-        grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
-    gq, gk, gv = grads
-    _same_kind("attention_grad", q, out=out, grad_out=grad_out, grad_q=gq, grad_k=gk, grad_v=gv)
-    if out.shape != q.shape or grad_out.shape != q.shape or gq.shape != q.shape or gk.shape != k.shape or gv.shape != v.shape:
-        raise ValueError("attention_grad: out, grad_out and grad_q have the shape of q, grad_k and grad_v that of k")
-    if tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 or lse.device != q.device \
-            or not lse.is_contiguous() or any(t.stride(3) != 1 for t in grads):
-        raise ValueError("attention_grad: lse is a contiguous float32 tensor [B, H, Sq], the gradients' last dimension is contiguous")
-    p.out_stride, p.grad_out_stride = _stride3(out), _stride3(grad_out)
-    p.grad_q_stride, p.grad_k_stride, p.grad_v_stride = _stride3(gq), _stride3(gk), _stride3(gv)
-    n = daf_attention_grad_workspace(p)
-    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    daf_attention_grad(p, q, k, v, key_lengths, out, lse, grad_out, gq, gk, gv, ws, n, stream)
+        gq, gk, gv = (torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=q.dtype, device=dev),
+                      torch.empty(k.shape, dtype=q.dtype, device=dev))
+    else:
+        gq, gk, gv = grads
+        _one_device("attention_grad", index, grads)
+    ws = torch.empty(plan.ws, dtype=torch.uint8, device=dev)
+    status = _call(lib().daf_attention_grad, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), oa, lse.data_ptr(), ga,
+                   gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), ws.data_ptr(), plan.ws)
+    _check(status, "daf_attention_grad")
     if check:
         _check(daf_poll_status(ws, stream), "daf_attention_grad (device status)")
     return gq, gk, gv
 
 
-def _norm_params(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps) -> daf_norm_params:
-    if not x.is_cuda or x.dim() < 1 or not x.is_contiguous() or not y.is_contiguous() or x.shape != y.shape:
-        raise ValueError(f"{where} expects contiguous CUDA tensors of one shape")
+_norm_plans = {}
+
+
+class _NormPlan:
+    """Parameter block and workspace size of residual_norm / residual_norm_grad for one set of types and shapes."""
+    __slots__ = ("params", "ref", "ws")
+
+
+def _norm_plan(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps) -> _NormPlan:
+    if x.dim() < 1 or x.shape != y.shape or x.dtype != y.dtype or x.dtype not in _dtype_codes():
+        raise ValueError(f"{where} expects tensors of one shape and one of the supported types")
     if kind not in ("layer", "rms"):
         raise ValueError(f"{where}: kind is 'layer' or 'rms'")
     width = x.shape[-1]
     rows = x.numel() // width if width else 0
-    _same_kind(where, x, y=y)
-    _same_kind(where, weight, bias=bias, gate=gate, post_weight=post_weight, post_bias=post_bias)
     for name, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias)):
-        if t is not None and (tuple(t.shape) != (width,) or not t.is_contiguous()):
-            raise ValueError(f"{where}: {name} must be a contiguous vector of {width}")
+        if t is not None and (tuple(t.shape) != (width,) or t.dtype != weight.dtype):
+            raise ValueError(f"{where}: {name} is {t.dtype} {tuple(t.shape)}, expected {weight.dtype} ({width},)")
+    if weight.dtype not in _dtype_codes():
+        raise ValueError(f"{where}: parameters of {weight.dtype} are not supported")
     gates = 0
     if gate is not None:
         gates = 1 if gate.dim() == 1 else int(gate.shape[0])
-        if tuple(gate.shape) not in ((width,), (gates, width)) or not gate.is_contiguous() or gates == 0:
-            raise ValueError(f"{where}: gate must be contiguous, [{width}] or [G, {width}]")
-    if weight.device != x.device:
-        raise ValueError(f"{where}: parameters and activations are on different devices")
-    return daf_norm_params(ctypes.sizeof(daf_norm_params), dtype_code(x), dtype_code(weight), NORM_LAYER if kind == "layer" else NORM_RMS,
-                           rows, width, gates, residual_scale, eps, 0)
+        if tuple(gate.shape) not in ((width,), (gates, width)) or gates == 0 or gate.dtype != weight.dtype:
+            raise ValueError(f"{where}: gate must be [{width}] or [G, {width}] in the other parameters' type")
+    plan = _NormPlan()
+    plan.params = daf_norm_params(ctypes.sizeof(daf_norm_params), dtype_code(x), dtype_code(weight),
+                                  NORM_LAYER if kind == "layer" else NORM_RMS, rows, width, gates, residual_scale, eps, 0)
+    plan.ref = ctypes.byref(plan.params)
+    plan.ws = daf_residual_norm_grad_workspace(plan.params)
+    return plan
+
+
+def _norm_call(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps, *more) -> _NormPlan:
+    """The plan for these tensors; `more` are activations of x's shape and type.  Every tensor is checked for its device and for
+    being contiguous."""
+    vectors = (weight, bias, gate, post_weight, post_bias)
+    key = (x.dtype, y.dtype, x.shape, y.shape, residual_scale, kind, eps, *[None if t is None else (t.dtype, t.shape) for t in vectors])
+    plan = _norm_plans.get(key)
+    if plan is None:
+        plan = _remember(_norm_plans, key, _norm_plan(where, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps))
+    index = x.get_device()
+    if index < 0:
+        raise ValueError(f"{where} expects CUDA tensors")
+    for t in (x, y, *vectors, *more):
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            raise ValueError(f"{where} expects contiguous tensors on one CUDA device")
+    for t in more:
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            raise ValueError(f"{where}: a tensor differs from the activations in shape or type")
+    return plan
 
 
 def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_bias=None, residual_scale: float = 1.0,
@@ -668,12 +775,14 @@ def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_
     """(z, h): z = x + residual_scale * gate * post_norm(y), h = norm(z) * weight + bias over the last dimension, in one pass
     (daf_residual_norm).  post_norm only with post_weight; gate [C], or [G, C] for G equal runs of rows; parameters in the
     activations' type or float32.  out: (z, h) to write into, z may be x and h may be y."""
-    p = _norm_params("residual_norm", x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps)
-    z, h = out if out is not None else (_torch().empty_like(x), _torch().empty_like(x))
-    _same_kind("residual_norm", x, z=z, h=h)
-    if z.shape != x.shape or h.shape != x.shape or not z.is_contiguous() or not h.is_contiguous():
-        raise ValueError("residual_norm: z and h are contiguous and have the shape of x")
-    daf_residual_norm(p, x, y, weight, bias, gate, post_weight, post_bias, z, h, stream)
+    plan = _norm_call("residual_norm", x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps, *(out or ()))
+    if out is None:
+        empty = _torch().empty_like
+        out = empty(x), empty(x)
+    z, h = out
+    status = _call(lib().daf_residual_norm, x, stream, plan.ref, x.data_ptr(), y.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(gate),
+                   _ptr(post_weight), _ptr(post_bias), z.data_ptr(), h.data_ptr())
+    _check(status, "daf_residual_norm")
     return z, h
 
 
@@ -682,41 +791,53 @@ def residual_norm_grad(z, y, weight, bias, grad_z, grad_h, *, gate=None, post_we
     """Gradients of ``residual_norm`` from z, y and those of z (None: zero) and h (daf_residual_norm_grad): a dict with "x", "y",
     "weight", "bias", "gate", "post_weight" and "post_bias", None where there is no such parameter."""
     torch = _torch()
-    p = _norm_params("residual_norm_grad", z, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps)
-    _same_kind("residual_norm_grad", z, grad_z=grad_z, grad_h=grad_h)
-    for t in (grad_z, grad_h):
-        if t is not None and (t.shape != z.shape or not t.is_contiguous()):
-            raise ValueError("residual_norm_grad: the gradients are contiguous and have the shape of z")
-    g = {"x": torch.empty_like(z), "y": torch.empty_like(z)}
-    for name, t in (("weight", weight), ("bias", bias), ("gate", gate), ("post_weight", post_weight), ("post_bias", post_bias)):
-        g[name] = None if t is None else torch.empty_like(t)
-    n = daf_residual_norm_grad_workspace(p)
-    ws = torch.empty(n, dtype=torch.uint8, device=z.device) if n else None
-    daf_residual_norm_grad(p, z, y, weight, gate, post_weight, post_bias, grad_z, grad_h, g["x"], g["y"], g["weight"], g["bias"],
-                           g["gate"], g["post_weight"], g["post_bias"], ws, n, stream)
-    return g
+    plan = _norm_call("residual_norm_grad", z, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps, grad_z, grad_h)
+    empty = torch.empty_like
+    gx, gy, gw = empty(z), empty(z), empty(weight)
+    gb, gg, gpw, gpb = (None if t is None else empty(t) for t in (bias, gate, post_weight, post_bias))
+    ws = torch.empty(plan.ws, dtype=torch.uint8, device=z.device)
+    status = _call(lib().daf_residual_norm_grad, z, stream, plan.ref, z.data_ptr(), y.data_ptr(), weight.data_ptr(), _ptr(gate),
+                   _ptr(post_weight), _ptr(post_bias), _ptr(grad_z), grad_h.data_ptr(), gx.data_ptr(), gy.data_ptr(), gw.data_ptr(),
+                   _ptr(gb), _ptr(gg), _ptr(gpw), _ptr(gpb), ws.data_ptr(), plan.ws)
+    _check(status, "daf_residual_norm_grad")
+    return {"x": gx, "y": gy, "weight": gw, "bias": gb, "gate": gg, "post_weight": gpw, "post_bias": gpb}
 
 
 def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, stream=None):
-    """Scales the tensors of ``grads`` in place (or into ``out``) by min(1, max_norm / (norm + eps)), norm being the 2-norm over
-    all of them; returns the norm as a float32 scalar tensor on their device (daf_clip_norm_batch).  Nothing is read back."""
+    """Scales the tensors of ``grads`` in place (or into ``out``, tensors of the same types and sizes) by
+    min(1, max_norm / (norm + eps)), norm being the 2-norm over all of them; returns the norm as a float32 scalar tensor on
+    their device (daf_clip_norm_batch).  Nothing is read back."""
     torch = _torch()
     grads = list(grads)
-    out = grads if out is None else list(out)
-    if not grads:
+    n = len(grads)
+    if n == 0:
         return torch.zeros((), dtype=torch.float32)
+    tensor, codes = torch.Tensor, _dtype_codes()
+    numel = array("Q", map(tensor.numel, grads))
+    dtypes = [g.dtype for g in grads]
+    try:
+        code = array("I", [codes[t] for t in dtypes])
+    except KeyError as e:
+        raise ValueError(f"clip_grad_norm: {e.args[0]} is not supported") from None
+    index = grads[0].get_device()
+    if index < 0 or any(i != index for i in map(tensor.get_device, grads)) or not all(map(tensor.is_contiguous, grads)):
+        raise ValueError("clip_grad_norm expects contiguous CUDA tensors on one device")
+    src = array("Q", map(tensor.data_ptr, grads))
+    dst = src
+    if out is not None:
+        out = list(out)
+        if len(out) != n or array("Q", map(tensor.numel, out)) != numel or [o.dtype for o in out] != dtypes \
+                or any(i != index for i in map(tensor.get_device, out)) or not all(map(tensor.is_contiguous, out)):
+            raise ValueError("clip_grad_norm: an output differs from its gradient in size, type or device, or is not contiguous")
+        dst = array("Q", map(tensor.data_ptr, out))
     dev = grads[0].device
-    if len(out) != len(grads):
-        raise ValueError("clip_grad_norm: out holds one tensor for each gradient")
-    for g, o in zip(grads, out):
-        if not g.is_cuda or g.device != dev or not g.is_contiguous():
-            raise ValueError("clip_grad_norm expects contiguous CUDA tensors on one device")
-        if o is not g and (o.device != dev or not o.is_contiguous() or o.dtype != g.dtype or o.shape != g.shape):
-            raise ValueError("clip_grad_norm: an output differs from its gradient in shape, type or device")
     norm = torch.empty((), dtype=torch.float32, device=dev)
-    n = daf_clip_norm_workspace(len(grads))
-    ws = torch.empty(n, dtype=torch.uint8, device=dev)
-    daf_clip_norm_batch(grads, out, max_norm, eps, norm, ws, n, stream)
+    ws_bytes = daf_clip_norm_workspace(n)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    at = [a.buffer_info()[0] for a in (code, src, dst, numel)]
+    status = _call(lib().daf_clip_norm_batch, norm, stream, n, at[0], at[1], at[2], at[3], max_norm, eps, norm.data_ptr(),
+                   ws.data_ptr(), ws_bytes)
+    _check(status, "daf_clip_norm_batch")
     return norm
 
 
