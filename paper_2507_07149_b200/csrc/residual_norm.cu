@@ -18,6 +18,7 @@
 // atomics: the same inputs give the same bits).  The next row's loads are issued before the current row's arithmetic.
 // Bound: HBM, four tensors of the stream's size forward, six backward.
 #include "common.cuh"
+#include "pairs.cuh"
 
 namespace daf {
 
@@ -39,45 +40,97 @@ struct JoinArgs {
     uint32_t layer, param_f32;
 };
 
-// Eight elements as they lie in memory (widened only when they are used: half the registers for 16-bit types).
-template <typename T> struct Raw8 {
-    uint4 v;
-    __device__ __forceinline__ void load(const void *p)
-    {
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    }
-    __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
-    __device__ __forceinline__ void get(float (&x)[8]) const { Elem<T>::widen8(v, x); }
-};
-template <> struct Raw8<float> {
-    float v[8];
-    __device__ __forceinline__ void load(const void *p) { Elem<float>::load8(p, v); }
-    __device__ __forceinline__ void zero()
-    {
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = 0.0f;
-    }
-    __device__ __forceinline__ void get(float (&x)[8]) const
-    {
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = v[i];
-    }
-};
-
-// Eight parameters of a vector (binary32 or the activations' type); `fill` where the vector is absent.
-template <typename T> __device__ __forceinline__ void param8(const void *p, uint64_t at, uint32_t f32, float fill, float (&x)[8])
+__device__ __forceinline__ void to_pairs(const float (&f)[8], uint64_t (&x)[4])
 {
-    if (!p) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = fill;
-    } else if (f32) {
-        const float4 *q = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(p) + at);
-        const float4 u = __ldg(q), w = __ldg(q + 1);
-        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-        x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
-    } else {
-        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + at * Elem<T>::kBytes));
-        if (Elem<T>::kBytes == 2) Elem<T>::widen8(u, x);
+    for (int i = 0; i < 4; i++) x[i] = pair(f[2 * i], f[2 * i + 1]);
+}
+template <typename T> __device__ __forceinline__ void store_pairs(void *p, const uint64_t (&x)[4])
+{
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; i++) unpair(x[i], f[2 * i], f[2 * i + 1]);
+    Elem<T>::store8(p, f);
+}
+
+// The next rows of a thread's eight columns of N tensors, DEPTH rows deep: each thread copies its own pieces into its own
+// places of shared memory and reads them back itself, so no thread waits for another.  One row ahead in registers left
+// the kernels waiting for memory (backward, 12608 x 768 bfloat16: 36 us; four rows ahead: see the kernel).
+template <typename T, int N, int DEPTH, int THREADS> struct RowPipe {
+    static constexpr int kDepth = DEPTH;
+    static constexpr int kParts = Elem<T>::kBytes / 2;            // 16-byte pieces of eight elements
+    static constexpr uint32_t kBytes = DEPTH * N * kParts * THREADS * 16u;
+    uint4 *at;
+    uint32_t stage;
+    __device__ __forceinline__ void init(void *smem)
+    {
+        at = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
+        stage = 0;
+    }
+    __device__ __forceinline__ uint4 *place(int t, int part) const { return at + ((stage * N + t) * kParts + part) * THREADS; }
+    // the pieces of the row that will be read DEPTH turns from now (nothing for a row that is not there)
+    __device__ __forceinline__ void fetch(const char *const (&src)[N], uint64_t offset, bool there)
+    {
+        if (there) {
+#pragma unroll
+            for (int t = 0; t < N; t++)
+                if (src[t]) {
+#pragma unroll
+                    for (int k = 0; k < kParts; k++)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(place(t, k))),
+                                     "l"(src[t] + offset + 16 * k) : "memory");
+                }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        stage = stage + 1 == DEPTH ? 0 : stage + 1;
+    }
+    __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory"); }
+    __device__ __forceinline__ void get(int t, const char *const (&)[N], uint64_t, bool there, uint64_t (&x)[4]) const
+    {
+        x[0] = x[1] = x[2] = x[3] = 0ull;
+        if (!there) return;
+        float f[8];
+        const uint4 u = *place(t, 0);
+        Elem<T>::widen8(u, f);
+        if (kParts == 2) {
+            const uint4 v = *place(t, kParts - 1);
+            f[4] = __uint_as_float(v.x); f[5] = __uint_as_float(v.y); f[6] = __uint_as_float(v.z); f[7] = __uint_as_float(v.w);
+        }
+        to_pairs(f, x);
+    }
+};
+// No depth: rows are loaded when they are needed.
+template <typename T, int N, int THREADS> struct RowPipe<T, N, 0, THREADS> {
+    static constexpr int kDepth = 0;
+    static constexpr uint32_t kBytes = 0;
+    __device__ __forceinline__ void init(void *) {}
+    __device__ __forceinline__ void fetch(const char *const (&)[N], uint64_t, bool) {}
+    __device__ __forceinline__ void wait() const {}
+    __device__ __forceinline__ void get(int t, const char *const (&src)[N], uint64_t offset, bool there, uint64_t (&x)[4]) const
+    {
+        x[0] = x[1] = x[2] = x[3] = 0ull;
+        if (!there) return;
+        float f[8];
+        Elem<T>::load8(src[t] + offset, f);
+        to_pairs(f, x);
+    }
+};
+// Depths that fit shared memory: two CTAs per SM forward; one CTA backward, beside the wide kernel's 160 KiB of column sums
+// (which leave no room for binary32 rows).
+template <typename T, int THREADS> using ForwardPipe = RowPipe<T, 2, THREADS == kJoinThreads ? (Elem<T>::kBytes == 2 ? 4 : 3) : 2, THREADS>;
+template <typename T, int THREADS> using BackwardPipe = RowPipe<T, 4, THREADS == kJoinThreads ? (Elem<T>::kBytes == 2 ? 4 : 3) : Elem<T>::kBytes == 2, THREADS>;
+
+// Eight parameters of a vector (binary32 or the activations' type).
+template <typename T> __device__ __forceinline__ void param8(const void *p, uint64_t at, uint32_t f32, uint64_t (&x)[4])
+{
+    if (f32) {
+        const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(reinterpret_cast<const float *>(p) + at);
+        const ulonglong2 u = __ldg(q), w = __ldg(q + 1);
+        x[0] = u.x; x[1] = u.y; x[2] = w.x; x[3] = w.y;
+    } else if (Elem<T>::kBytes == 2) {
+        float f[8];
+        Elem<T>::widen8(__ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + at * Elem<T>::kBytes)), f);
+        to_pairs(f, x);
     }
 }
 
@@ -88,139 +141,165 @@ __device__ __forceinline__ void store_param(void *p, uint64_t at, uint32_t f32, 
     else reinterpret_cast<__half *>(p)[at] = __float2half_rn(v);
 }
 
-// Sums of two values over the threads of a slot.  Two buffers in turn: a warp that writes for sum k + 2 has met, at sum
-// k + 1, every warp that still read sum k.
+// Sums of two or four values over the threads of a slot.  Within a warp the first exchanges leave one of the sums in each
+// half (quarter) of the warp, so that the remaining steps serve all; a slot of several warps meets once, and every warp
+// adds up the warps' sums the same way.  Two buffers in turn: a warp that writes for sum k + 2 has met, at sum k + 1,
+// every warp that still read sum k.
 struct RowSums {
-    float2 (*buf)[32];
+    float *buf;                                   // [2][4][32]
     uint32_t tpr, slot, parity;
+    // v: sum number lane / span of the warp, complete within each span of lanes; afterwards that of the slot
+    template <int SPAN> __device__ __forceinline__ void meet(float &v)
+    {
+        const uint32_t n = tpr >> 5, lane = threadIdx.x & 31u, i = lane % SPAN;
+        float *const b = buf + parity * 128u + lane / SPAN * 32u + slot * n;
+        if (i == 0) b[(threadIdx.x >> 5) - slot * n] = v;
+        asm volatile("bar.sync %0, %1;" ::"r"(slot + 1u), "r"(tpr) : "memory");
+        v = i < n ? b[i] : 0.0f;
+#pragma unroll
+        for (uint32_t k = SPAN; k < 32u; k += SPAN)
+            if (n > k && i + k < n) v += b[i + k];
+#pragma unroll
+        for (int d = SPAN / 2; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        parity ^= 1u;
+    }
     __device__ __forceinline__ void operator()(float &p, float &q)
     {
-        for (uint32_t d = (tpr < 32u ? tpr : 32u) >> 1; d; d >>= 1) {
-            p += __shfl_xor_sync(0xffffffffu, p, d);
-            q += __shfl_xor_sync(0xffffffffu, q, d);
-        }
-        if (tpr > 32u) {
-            const uint32_t n = tpr >> 5, first = slot * n;
-            if ((threadIdx.x & 31u) == 0) buf[parity][threadIdx.x >> 5] = make_float2(p, q);
-            asm volatile("bar.sync %0, %1;" ::"r"(slot + 1u), "r"(tpr) : "memory");
-            p = q = 0.0f;
-            for (uint32_t w = 0; w < n; w++) {
-                const float2 v = buf[parity][first + w];
-                p += v.x;
-                q += v.y;
+        if (tpr < 32u) {
+            for (uint32_t d = tpr >> 1; d; d >>= 1) {
+                p += __shfl_xor_sync(0xffffffffu, p, d);
+                q += __shfl_xor_sync(0xffffffffu, q, d);
             }
-            parity ^= 1u;
+            return;
         }
+        const bool upper = threadIdx.x & 16u;
+        float v = (upper ? q : p) + __shfl_xor_sync(0xffffffffu, upper ? p : q, 16);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (tpr > 32u) meet<16>(v);
+        p = __shfl_sync(0xffffffffu, v, 0);
+        q = __shfl_sync(0xffffffffu, v, 16);
+    }
+    __device__ __forceinline__ void operator()(float &p, float &q, float &r, float &s)
+    {
+        if (tpr < 32u) {
+            (*this)(p, q);
+            (*this)(r, s);
+            return;
+        }
+        const bool upper = threadIdx.x & 16u, odd = threadIdx.x & 8u;
+        const float v0 = (upper ? r : p) + __shfl_xor_sync(0xffffffffu, upper ? p : r, 16);
+        const float v1 = (upper ? s : q) + __shfl_xor_sync(0xffffffffu, upper ? q : s, 16);
+        float v = (odd ? v1 : v0) + __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 8);
+#pragma unroll
+        for (int d = 4; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (tpr > 32u) meet<8>(v);
+        p = __shfl_sync(0xffffffffu, v, 0);
+        q = __shfl_sync(0xffffffffu, v, 8);
+        r = __shfl_sync(0xffffffffu, v, 16);
+        s = __shfl_sync(0xffffffffu, v, 24);
     }
 };
 
-__device__ __forceinline__ float sum8(const float (&x)[8])
+__device__ __forceinline__ float sum8(const uint64_t (&x)[4])
 {
-    return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    const uint64_t s = add2(add2(x[0], x[1]), add2(x[2], x[3]));
+    return low(s) + high(s);
 }
-__device__ __forceinline__ float dot8(const float (&x)[8], const float (&y)[8])
+__device__ __forceinline__ float dot8(const uint64_t (&x)[4], const uint64_t (&y)[4])
 {
-    float a = x[0] * y[0], b = x[1] * y[1];
+    const uint64_t s = add2(fma2(x[1], y[1], mul2(x[0], y[0])), fma2(x[3], y[3], mul2(x[2], y[2])));
+    return low(s) + high(s);
+}
+__device__ __forceinline__ void times(uint64_t (&x)[4], uint64_t by)
+{
 #pragma unroll
-    for (int i = 2; i < 8; i += 2) {
-        a = __fmaf_rn(x[i], y[i], a);
-        b = __fmaf_rn(x[i + 1], y[i + 1], b);
-    }
-    return a + b;
+    for (int i = 0; i < 4; i++) x[i] = mul2(x[i], by);
+}
+__device__ __forceinline__ void times(uint64_t (&x)[4], const uint64_t (&by)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] = mul2(x[i], by[i]);
 }
 
-// 1 / sqrt(mean of squares + eps), correctly rounded steps (the row's 8192 elements share this one value).
-__device__ __forceinline__ float inv_std(float sum_sq, float inv_c, float eps)
+// x <- x - mean (zero for kind "rms"), for two rows at once (the second only if TWO).
+template <bool TWO> __device__ __forceinline__ void centre(RowSums &sums, const JoinArgs &p, uint64_t (&x)[4], uint64_t (&y)[4])
 {
-    return __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum_sq, inv_c, eps)));
+    if (!p.layer) return;
+    float mx = sum8(x), my = TWO ? sum8(y) : 0.0f;
+    sums(mx, my);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        x[i] = add2(x[i], both(-mx * p.inv_c));
+        if (TWO) y[i] = add2(y[i], both(-my * p.inv_c));
+    }
 }
-
-// x <- (x - mean) r for two rows' worth at once (the second may be unused); mine: the thread owns columns of the row.
-template <bool TWO>
-__device__ __forceinline__ void normalize(RowSums &sums, const JoinArgs &p, bool mine, float (&x)[8], float (&y)[8], float &rx, float &ry)
+// x <- (x - mean) r; mine: the thread owns columns of the row.
+__device__ __forceinline__ void normalize(RowSums &sums, const JoinArgs &p, bool mine, uint64_t (&x)[4])
 {
-    float mx = 0.0f, my = 0.0f;
-    if (p.layer) {
-        mx = sum8(x);
-        my = TWO ? sum8(y) : 0.0f;
-        sums(mx, my);
-        mx *= p.inv_c;
-        my *= p.inv_c;
-    }
-    float vx = 0.0f, vy = 0.0f;
-    if (mine) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            x[i] -= mx;
-            if (TWO) y[i] -= my;
-        }
-        vx = dot8(x, x);
-        if (TWO) vy = dot8(y, y);
-    }
-    sums(vx, vy);
-    rx = inv_std(vx, p.inv_c, p.eps);
-    ry = TWO ? inv_std(vy, p.inv_c, p.eps) : 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        x[i] *= rx;
-        if (TWO) y[i] *= ry;
-    }
+    centre<false>(sums, p, x, x);
+    float v = mine ? dot8(x, x) : 0.0f, none = 0.0f;
+    sums(v, none);
+    times(x, both(rsqrtf(__fmaf_rn(v, p.inv_c, p.eps))));
 }
 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == kJoinThreads ? 2 : 1) join_kernel(const __grid_constant__ JoinArgs p)
 {
-    __shared__ float2 s_buf[2][32];
+    __shared__ float s_buf[256];
     const uint32_t slot = threadIdx.x / p.tpr, t = threadIdx.x - slot * p.tpr, col = t * 8u;
     RowSums sums{s_buf, p.tpr, slot, 0u};
     const bool owns = col < p.C;
     const uint64_t step = (uint64_t)gridDim.x * p.slots, n_turns = (p.rows + step - 1u) / step;
     uint64_t row = (uint64_t)blockIdx.x * p.slots + slot;
-    const char *const xs = reinterpret_cast<const char *>(p.x), *const ys = reinterpret_cast<const char *>(p.y);
-    Raw8<T> rx, ry;
-    rx.zero();
-    ry.zero();
-    if (owns && row < p.rows) {
-        rx.load(xs + (row * p.C + col) * Elem<T>::kBytes);
-        ry.load(ys + (row * p.C + col) * Elem<T>::kBytes);
+    extern __shared__ __align__(16) unsigned char s_pipe[];
+    using Pipe = ForwardPipe<T, THREADS>;
+    Pipe pipe;
+    pipe.init(s_pipe);
+    const char *const src[2] = {reinterpret_cast<const char *>(p.x), reinterpret_cast<const char *>(p.y)};
+    const uint64_t ahead = Pipe::kDepth * step;
+#pragma unroll
+    for (int d = 0; d < Pipe::kDepth; d++) {
+        const uint64_t r = row + d * step;
+        pipe.fetch(src, (r * p.C + col) * Elem<T>::kBytes, owns && r < p.rows);
     }
     for (uint64_t turn = 0; turn < n_turns; turn++, row += step) {
         const bool mine = owns && row < p.rows;
         const uint64_t at = row * p.C + col;
-        float x[8], u[8], v[8], r, unused;
-        rx.get(x);
-        ry.get(u);
-        if (owns && row + step < p.rows) {
-            rx.load(xs + (at + step * p.C) * Elem<T>::kBytes);
-            ry.load(ys + (at + step * p.C) * Elem<T>::kBytes);
-        }
+        uint64_t x[4], u[4], v[4], w[4];
+        pipe.wait();
+        pipe.get(0, src, at * Elem<T>::kBytes, mine, x);
+        pipe.get(1, src, at * Elem<T>::kBytes, mine, u);
         if (p.post_weight) {
-            normalize<false>(sums, p, mine, u, u, r, unused);
+            normalize(sums, p, mine, u);
             if (mine) {
-                float b[8];
-                param8<T>(p.post_weight, col, p.param_f32, 1.0f, v);
-                param8<T>(p.post_bias, col, p.param_f32, 0.0f, b);
+                param8<T>(p.post_weight, col, p.param_f32, v);
+                times(u, v);
+                if (p.post_bias) {
+                    param8<T>(p.post_bias, col, p.param_f32, w);
 #pragma unroll
-                for (int i = 0; i < 8; i++) u[i] = __fmaf_rn(u[i], v[i], b[i]);
+                    for (int i = 0; i < 4; i++) u[i] = add2(u[i], w[i]);
+                }
             }
         }
         if (mine) {
             if (p.gate) {
-                param8<T>(p.gate, p.gates > 1u ? row / p.rows_per_gate * p.C + col : col, p.param_f32, 1.0f, v);
-#pragma unroll
-                for (int i = 0; i < 8; i++) u[i] *= v[i];
+                param8<T>(p.gate, p.gates > 1u ? row / p.rows_per_gate * p.C + col : col, p.param_f32, v);
+                times(u, v);
             }
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = __fmaf_rn(p.a, u[i], x[i]);
-            Elem<T>::store8(reinterpret_cast<char *>(p.out_a) + at * Elem<T>::kBytes, x);
+            for (int i = 0; i < 4; i++) x[i] = fma2(both(p.a), u[i], x[i]);
+            store_pairs<T>(reinterpret_cast<char *>(p.out_a) + at * Elem<T>::kBytes, x);
         }
-        normalize<false>(sums, p, mine, x, x, r, unused);
+        pipe.fetch(src, (at + ahead * p.C) * Elem<T>::kBytes, owns && row + ahead < p.rows);   // into the place just read
+        normalize(sums, p, mine, x);
         if (mine) {
-            param8<T>(p.weight, col, p.param_f32, 1.0f, v);
-            param8<T>(p.bias, col, p.param_f32, 0.0f, u);
+            param8<T>(p.weight, col, p.param_f32, v);
+            w[0] = w[1] = w[2] = w[3] = 0ull;
+            if (p.bias) param8<T>(p.bias, col, p.param_f32, w);
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = __fmaf_rn(x[i], v[i], u[i]);
-            Elem<T>::store8(reinterpret_cast<char *>(p.out_b) + at * Elem<T>::kBytes, x);
+            for (int i = 0; i < 4; i++) x[i] = fma2(x[i], v[i], w[i]);
+            store_pairs<T>(reinterpret_cast<char *>(p.out_b) + at * Elem<T>::kBytes, x);
         }
     }
 }
@@ -228,71 +307,73 @@ __global__ void __launch_bounds__(THREADS, THREADS == kJoinThreads ? 2 : 1) join
 // The column sums of one thread's eight columns: in registers, or for rows above 4096 columns (1024 threads, 64
 // registers each) in shared memory, where a thread only ever touches its own columns.
 template <bool SMEM> struct Columns {
-    float v[kSums][8];
+    uint64_t v[kSums][4];
     __device__ __forceinline__ void init(float *, uint32_t, uint32_t)
     {
 #pragma unroll
         for (int q = 0; q < kSums; q++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[q][i] = 0.0f;
+            for (int i = 0; i < 4; i++) v[q][i] = 0ull;
     }
-    __device__ __forceinline__ void add(int q, const float (&x)[8], const float (&y)[8])
+    __device__ __forceinline__ void add(int q, const uint64_t (&x)[4], const uint64_t (&y)[4])
     {
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[q][i] = __fmaf_rn(x[i], y[i], v[q][i]);
+        for (int i = 0; i < 4; i++) v[q][i] = fma2(x[i], y[i], v[q][i]);
     }
-    __device__ __forceinline__ void add(int q, const float (&x)[8])
+    __device__ __forceinline__ void add(int q, const uint64_t (&x)[4])
     {
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[q][i] += x[i];
+        for (int i = 0; i < 4; i++) v[q][i] = add2(x[i], v[q][i]);
     }
-    __device__ __forceinline__ void take(int q, float (&x)[8])
+    __device__ __forceinline__ void take(int q, uint64_t (&x)[4])
     {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
+        for (int i = 0; i < 4; i++) {
             x[i] = v[q][i];
-            v[q][i] = 0.0f;
+            v[q][i] = 0ull;
         }
     }
 };
 template <> struct Columns<true> {
-    float4 *base;
-    uint32_t stride;                               // float4 per sum
+    ulonglong2 *base;
+    uint32_t stride;                               // 16-byte units per sum
     __device__ __forceinline__ void init(float *smem, uint32_t C, uint32_t col)
     {
-        base = reinterpret_cast<float4 *>(smem + col);
+        base = reinterpret_cast<ulonglong2 *>(smem + col);
         stride = C >> 2;
         if (col < C)
-            for (int q = 0; q < kSums; q++) base[q * stride] = base[q * stride + 1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int q = 0; q < kSums; q++) base[q * stride] = base[q * stride + 1] = make_ulonglong2(0ull, 0ull);
     }
-    __device__ __forceinline__ void add(int q, const float (&x)[8])
+    __device__ __forceinline__ void add(int q, const uint64_t (&x)[4])
     {
-        float4 *b = base + q * stride;
-        const float4 u = b[0], w = b[1];
-        b[0] = make_float4(u.x + x[0], u.y + x[1], u.z + x[2], u.w + x[3]);
-        b[1] = make_float4(w.x + x[4], w.y + x[5], w.z + x[6], w.w + x[7]);
+        ulonglong2 *b = base + q * stride;
+        const ulonglong2 u = b[0], w = b[1];
+        b[0] = make_ulonglong2(add2(u.x, x[0]), add2(u.y, x[1]));
+        b[1] = make_ulonglong2(add2(w.x, x[2]), add2(w.y, x[3]));
     }
-    __device__ __forceinline__ void add(int q, const float (&x)[8], const float (&y)[8])
+    __device__ __forceinline__ void add(int q, const uint64_t (&x)[4], const uint64_t (&y)[4])
     {
-        float t[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) t[i] = x[i] * y[i];
-        add(q, t);
+        ulonglong2 *b = base + q * stride;
+        const ulonglong2 u = b[0], w = b[1];
+        b[0] = make_ulonglong2(fma2(x[0], y[0], u.x), fma2(x[1], y[1], u.y));
+        b[1] = make_ulonglong2(fma2(x[2], y[2], w.x), fma2(x[3], y[3], w.y));
     }
-    __device__ __forceinline__ void take(int q, float (&x)[8])
+    __device__ __forceinline__ void take(int q, uint64_t (&x)[4])
     {
-        float4 *b = base + q * stride;
-        const float4 u = b[0], w = b[1];
-        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-        x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
-        b[0] = b[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        ulonglong2 *b = base + q * stride;
+        const ulonglong2 u = b[0], w = b[1];
+        x[0] = u.x; x[1] = u.y; x[2] = w.x; x[3] = w.y;
+        b[0] = b[1] = make_ulonglong2(0ull, 0ull);
     }
 };
 
 // Adds one column sum over the CTA's slots (in slot order) and hands column c's total to out(c, total).
 template <bool WIDE, typename Out>
-__device__ __forceinline__ void over_slots(const JoinArgs &p, uint32_t slot, uint32_t col, const float (&x)[8], float *s_cols, Out out)
+__device__ __forceinline__ void over_slots(const JoinArgs &p, uint32_t slot, uint32_t col, const uint64_t (&pairs)[4], float *s_cols, Out out)
 {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; i++) unpair(pairs[i], x[2 * i], x[2 * i + 1]);
     if (WIDE || p.slots == 1u) {
         if (col < p.C)
             for (int i = 0; i < 8; i++) out(col + i, x[i]);
@@ -316,7 +397,7 @@ template <typename T, bool POST, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) join_grad_kernel(const __grid_constant__ JoinArgs p)
 {
     constexpr bool WIDE = THREADS == kJoinWide;
-    __shared__ float2 s_buf[2][32];
+    __shared__ float s_buf[256];
     __shared__ __align__(16) float s_cols[WIDE ? 4 : kJoinThreads * 8];
     extern __shared__ __align__(16) float s_dyn[];
     const uint32_t slot = threadIdx.x / p.tpr, t = threadIdx.x - slot * p.tpr, col = t * 8u;
@@ -324,75 +405,70 @@ __global__ void __launch_bounds__(THREADS, 1) join_grad_kernel(const __grid_cons
     const bool owns = col < p.C;
     Columns<WIDE> cols;
     cols.init(s_dyn, p.C, col);
-    const char *const zs = reinterpret_cast<const char *>(p.x), *const ys = reinterpret_cast<const char *>(p.y);
-    const char *const gzs = reinterpret_cast<const char *>(p.grad_z), *const ghs = reinterpret_cast<const char *>(p.grad_h);
+    using Pipe = BackwardPipe<T, THREADS>;
+    Pipe pipe;
+    pipe.init(s_dyn + (WIDE ? kSums * p.C : 0u));
+    const char *const src[4] = {reinterpret_cast<const char *>(p.x), reinterpret_cast<const char *>(p.y),
+                                reinterpret_cast<const char *>(p.grad_z), reinterpret_cast<const char *>(p.grad_h)};
+    const uint64_t ahead = (uint64_t)Pipe::kDepth * p.slots;
     const uint32_t n_groups = p.gates > 1u ? p.gates : 1u;
     // CTA j of group g takes an equal run of the group's rows; with more groups than CTAs a CTA takes whole groups in turn
     for (uint32_t g = blockIdx.x / p.per_group, j = blockIdx.x % p.per_group; g < n_groups; g += gridDim.x / p.per_group) {
         const uint64_t lo = g * p.rows_per_gate + p.rows_per_gate * j / p.per_group;
         const uint64_t hi = g * p.rows_per_gate + p.rows_per_gate * (j + 1u) / p.per_group;
-        Raw8<T> rz, ry, rgz, rgh;
-        rz.zero();
-        ry.zero();
-        rgz.zero();
-        rgh.zero();
         uint64_t row = lo + slot;
-        if (owns && row < hi) {
-            const uint64_t b = (row * p.C + col) * Elem<T>::kBytes;
-            rz.load(zs + b);
-            ry.load(ys + b);
-            rgh.load(ghs + b);
-            if (gzs) rgz.load(gzs + b);
+#pragma unroll
+        for (int d = 0; d < Pipe::kDepth; d++) {
+            const uint64_t r = row + (uint64_t)d * p.slots;
+            pipe.fetch(src, (r * p.C + col) * Elem<T>::kBytes, owns && r < hi);
         }
         for (uint64_t first = lo; first < hi; first += p.slots, row += p.slots) {
             const bool mine = owns && row < hi;
             const uint64_t at = row * p.C + col;
-            float z[8], y[8], gz[8], gh[8], w[8], rz_, ry_;
-            rz.get(z);
-            ry.get(y);
-            rgz.get(gz);
-            rgh.get(gh);
-            if (owns && row + p.slots < hi) {
-                const uint64_t b = (at + (uint64_t)p.slots * p.C) * Elem<T>::kBytes;
-                rz.load(zs + b);
-                ry.load(ys + b);
-                rgh.load(ghs + b);
-                if (gzs) rgz.load(gzs + b);
-            }
-            normalize<POST>(sums, p, mine, z, y, rz_, ry_);      // z, and with a post norm y, are the normalized rows now
-            float st = 0.0f, sth = 0.0f;
+            uint64_t z[4], y[4], gz[4], gh[4], w[4];
+            pipe.wait();
+            pipe.get(0, src, at * Elem<T>::kBytes, mine, z);
+            pipe.get(1, src, at * Elem<T>::kBytes, mine, y);
+            pipe.get(2, src, at * Elem<T>::kBytes, mine && p.grad_z, gz);
+            pipe.get(3, src, at * Elem<T>::kBytes, mine, gh);
+            // all sums of the row at once: those of gh w and gh w (z - mean) need no r
+            centre<POST>(sums, p, z, y);
+            float vz = 0.0f, vy = 0.0f, st = 0.0f, sth = 0.0f;
+            uint64_t t[4];
             if (mine) {
+                vz = dot8(z, z);
+                if (POST) vy = dot8(y, y);
+                param8<T>(p.weight, col, p.param_f32, t);
+                times(t, gh);
+                st = p.layer ? sum8(t) : 0.0f;
+                sth = dot8(t, z);
+            }
+            pipe.fetch(src, (at + ahead * p.C) * Elem<T>::kBytes, owns && row + ahead < hi);   // into the place just read
+            sums(vz, sth, st, vy);
+            const float rz = rsqrtf(__fmaf_rn(vz, p.inv_c, p.eps)), ry = POST ? rsqrtf(__fmaf_rn(vy, p.inv_c, p.eps)) : 0.0f;
+            if (POST) times(y, both(ry));                          // the normalized y
+            if (mine) {
+                times(z, both(rz));                                // the normalized z
                 cols.add(0, gh, z);
                 cols.add(1, gh);
-                param8<T>(p.weight, col, p.param_f32, 1.0f, w);
+                const uint64_t m1 = both(-st * p.inv_c), m2 = both(-sth * rz * p.inv_c);
 #pragma unroll
-                for (int i = 0; i < 8; i++) gh[i] *= w[i];
-                st = p.layer ? sum8(gh) : 0.0f;
-                sth = dot8(gh, z);
-            }
-            sums(st, sth);
-            st *= p.inv_c;
-            sth *= p.inv_c;
-            if (mine) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) gz[i] = __fmaf_rn(rz_, __fmaf_rn(-z[i], sth, gh[i] - st), gz[i]);
-                Elem<T>::store8(reinterpret_cast<char *>(p.out_a) + at * Elem<T>::kBytes, gz);
-#pragma unroll
-                for (int i = 0; i < 8; i++) gz[i] *= p.a;         // du
+                for (int i = 0; i < 4; i++) gz[i] = fma2(both(rz), fma2(z[i], m2, add2(t[i], m1)), gz[i]);
+                store_pairs<T>(reinterpret_cast<char *>(p.out_a) + at * Elem<T>::kBytes, gz);
+                times(gz, both(p.a));                              // du
                 if (p.gate) {
                     if (POST) {
-                        float b1[8];
-                        param8<T>(p.post_weight, col, p.param_f32, 1.0f, w);
-                        param8<T>(p.post_bias, col, p.param_f32, 0.0f, b1);
+                        param8<T>(p.post_weight, col, p.param_f32, gh);
+                        w[0] = w[1] = w[2] = w[3] = 0ull;
+                        if (p.post_bias) param8<T>(p.post_bias, col, p.param_f32, w);
 #pragma unroll
-                        for (int i = 0; i < 8; i++) w[i] = __fmaf_rn(y[i], w[i], b1[i]);
+                        for (int i = 0; i < 4; i++) w[i] = fma2(y[i], gh[i], w[i]);
                         cols.add(4, gz, w);
                     } else {
                         cols.add(4, gz, y);
                     }
-                    param8<T>(p.gate, p.gates > 1u ? (uint64_t)g * p.C + col : col, p.param_f32, 1.0f, w);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) gz[i] *= w[i];
+                    param8<T>(p.gate, p.gates > 1u ? (uint64_t)g * p.C + col : col, p.param_f32, w);
+                    times(gz, w);
                 }
             }
             if (POST) {
@@ -400,22 +476,20 @@ __global__ void __launch_bounds__(THREADS, 1) join_grad_kernel(const __grid_cons
                 if (mine) {
                     cols.add(2, gz, y);
                     cols.add(3, gz);
-                    param8<T>(p.post_weight, col, p.param_f32, 1.0f, w);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) gz[i] *= w[i];
+                    param8<T>(p.post_weight, col, p.param_f32, w);
+                    times(gz, w);
                     st = p.layer ? sum8(gz) : 0.0f;
                     sth = dot8(gz, y);
                 }
                 sums(st, sth);
-                st *= p.inv_c;
-                sth *= p.inv_c;
+                const uint64_t m1 = both(-st * p.inv_c), m2 = both(-sth * p.inv_c);
 #pragma unroll
-                for (int i = 0; i < 8; i++) gz[i] = ry_ * __fmaf_rn(-y[i], sth, gz[i] - st);
+                for (int i = 0; i < 4; i++) gz[i] = mul2(both(ry), fma2(y[i], m2, add2(gz[i], m1)));
             }
-            if (mine) Elem<T>::store8(reinterpret_cast<char *>(p.out_b) + at * Elem<T>::kBytes, gz);
+            if (mine) store_pairs<T>(reinterpret_cast<char *>(p.out_b) + at * Elem<T>::kBytes, gz);
         }
         if (p.gate && p.gates > 1u) {
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            uint64_t x[4] = {0ull, 0ull, 0ull, 0ull};
             if (owns) cols.take(4, x);
             const uint64_t at = (uint64_t)(g * p.per_group + j) * p.C;
             over_slots<WIDE>(p, slot, col, x, s_cols, [&](uint32_t c, float v) {
@@ -428,7 +502,7 @@ __global__ void __launch_bounds__(THREADS, 1) join_grad_kernel(const __grid_cons
     for (int q = 0; q < kSums; q++) {
         if ((q == 2 || q == 3) && !POST) continue;
         if (q == 4 && p.gates != 1u) continue;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        uint64_t x[4] = {0ull, 0ull, 0ull, 0ull};
         if (owns) cols.take(q, x);
         float *const to = q == 4 ? p.gate_partial + (uint64_t)blockIdx.x * p.C : p.partial + ((uint64_t)blockIdx.x * 4u + q) * p.C;
         over_slots<WIDE>(p, slot, col, x, s_cols, [&](uint32_t c, float v) { to[c] = v; });
@@ -462,7 +536,8 @@ __global__ void __launch_bounds__(256) join_sums_kernel(const __grid_constant__ 
         float r[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) r[i] = s_part[i][threadIdx.x & 31u];
-        store_param(out, (q < 4u ? 0ull : (uint64_t)(q - 4u) * p.C) + c, p.param_f32, p.bf16, sum8(r));
+        store_param(out, (q < 4u ? 0ull : (uint64_t)(q - 4u) * p.C) + c, p.param_f32, p.bf16,
+                    ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7])));
     }
 }
 
@@ -508,33 +583,34 @@ static void join_grid(const JoinArgs &a, uint32_t most, uint32_t *grid, uint32_t
     *grid = groups < most ? groups * (uint32_t)k : most;
 }
 
-template <typename T> static daf_status run_join(const JoinArgs &a, cudaStream_t s)
+template <typename T, int THREADS> static daf_status launch_join(const JoinArgs &a, cudaStream_t s)
 {
     int ctas = 0;
     const uint64_t turns = (a.rows + a.slots - 1u) / a.slots;
-    if (a.tpr > (uint32_t)kJoinThreads) {
-        if (persistent_ctas(reinterpret_cast<const void *>(&join_kernel<T, kJoinWide>), (int)a.tpr, 0, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
-        join_kernel<T, kJoinWide><<<(uint32_t)(turns < (uint64_t)ctas ? turns : ctas), a.tpr, 0, s>>>(a);
-    } else {
-        if (persistent_ctas(reinterpret_cast<const void *>(&join_kernel<T, kJoinThreads>), kJoinThreads, 0, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
-        join_kernel<T, kJoinThreads><<<(uint32_t)(turns < (uint64_t)ctas ? turns : ctas), a.tpr * a.slots, 0, s>>>(a);
-    }
+    const uint32_t smem = ForwardPipe<T, THREADS>::kBytes;
+    if (persistent_ctas(reinterpret_cast<const void *>(&join_kernel<T, THREADS>), THREADS, (int)smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    join_kernel<T, THREADS><<<(uint32_t)(turns < (uint64_t)ctas ? turns : ctas), a.tpr * a.slots, smem, s>>>(a);
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
+template <typename T> static daf_status run_join(const JoinArgs &a, cudaStream_t s)
+{
+    return a.tpr > (uint32_t)kJoinThreads ? launch_join<T, kJoinWide>(a, s) : launch_join<T, kJoinThreads>(a, s);
+}
 
-template <typename T, bool POST> static daf_status run_join_grad(JoinArgs &a, uint32_t *grid, cudaStream_t s)
+template <typename T, bool POST, int THREADS> static daf_status launch_join_grad(JoinArgs &a, uint32_t *grid, cudaStream_t s)
 {
     int ctas = 0;
-    const bool wide = a.tpr > (uint32_t)kJoinThreads;
-    const uint32_t smem = wide ? kSums * a.C * 4u : 0u;
-    const void *k = wide ? reinterpret_cast<const void *>(&join_grad_kernel<T, POST, kJoinWide>)
-                         : reinterpret_cast<const void *>(&join_grad_kernel<T, POST, kJoinThreads>);
-    if (persistent_ctas(k, wide ? (int)a.tpr : kJoinThreads, (int)smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    const auto kernel = &join_grad_kernel<T, POST, THREADS>;
+    const uint32_t smem = (THREADS == kJoinWide ? kSums * a.C * 4u : 0u) + BackwardPipe<T, THREADS>::kBytes;
+    if (persistent_ctas(reinterpret_cast<const void *>(kernel), THREADS, (int)smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
     join_grid(a, ctas < (int)kJoinCtas ? (uint32_t)ctas : kJoinCtas, grid, &a.per_group);
     a.gate_partial = a.partial + (uint64_t)*grid * 4u * a.C;
-    if (wide) join_grad_kernel<T, POST, kJoinWide><<<*grid, a.tpr, smem, s>>>(a);
-    else join_grad_kernel<T, POST, kJoinThreads><<<*grid, a.tpr * a.slots, 0, s>>>(a);
+    kernel<<<*grid, a.tpr * a.slots, smem, s>>>(a);
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
+template <typename T, bool POST> static daf_status run_join_grad(JoinArgs &a, uint32_t *grid, cudaStream_t s)
+{
+    return a.tpr > (uint32_t)kJoinThreads ? launch_join_grad<T, POST, kJoinWide>(a, grid, s) : launch_join_grad<T, POST, kJoinThreads>(a, grid, s);
 }
 
 }  // namespace daf
