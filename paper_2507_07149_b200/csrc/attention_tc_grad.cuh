@@ -9,10 +9,12 @@
 // S and dP are computed twice (7 products instead of 5); against it stands that every A operand of a second product is
 // where softmax leaves it -- in tensor memory, row by row -- so that P and dS never pass through shared memory.
 //
-// A persistent CTA (one per SM): warps 0-3 and 4-7 take the walk's blocks of 64 in turn (a thread owns one of the 128
-// rows), warp 8 issues the products, two blocks of T ahead of the sums, warp 9 the copies.  Tensor memory: the sums
-// (up to 256 columns) and two blocks of T1, T2 (2 x 128 columns), P over T1 and dS over T2.  Blocks of 64 rather than 128
-// because two blocks in flight matter more than the wider product.
+// A persistent CTA (one per SM): warps 0-7 and 8-15 take the walk's blocks of 64 in turn (a thread owns 32 columns of one
+// of the 128 rows), warp 16 issues the products, up to three blocks of T ahead of the sums, warp 17 the copies.  Tensor
+// memory: the sums (64 to 256 columns) and three blocks of T1, T2 (128 columns each; two where the sums take 256), P over
+// T1 and dS over T2.  What bounds it is the way of a block -- product, tensor memory to registers, exponentials, back,
+// second product, about 2500 cycles of latency --, so blocks in flight matter more than the wider products that blocks
+// of 128 would give, and eight warps per block more than long rows in few threads.
 // P and dS are rounded to the input type, which the second products need; everything else is binary32.
 #pragma once
 #include "attention.cuh"
@@ -20,7 +22,7 @@
 
 namespace daf {
 
-constexpr int kGradThreads = 384;
+constexpr int kGradThreads = 640;                // 16 warps x 104 registers, 4 (two of them idle) x 64: what 640 x 96 gives
 constexpr uint32_t kHeld = 128, kWalk = 64;
 
 struct AttnGradArgs {
@@ -30,10 +32,12 @@ struct AttnGradArgs {
     WorkspaceHeader *header;
 };
 
-template <int DP> struct GradSmem {
+template <int DP, bool DKV> struct GradSmem {
     static constexpr int kHeldBuffers = DP == 128 ? 1 : 2, kStages = DP == 128 ? 4 : 6;
     static constexpr uint32_t kX = kHeld * DP * 2u, kY = kWalk * DP * 2u;
     static constexpr uint32_t kStats = 2u * kWalk * 4u;           // -L and -delta of a block's queries
+    // blocks of T in tensor memory, behind the sums
+    static constexpr uint32_t kAhead = (512u - (DKV ? 2u : 1u) * DP) / 128u < 3u ? 2u : 3u, kT = 512u - kAhead * 128u;
     static constexpr uint32_t kBytes = kHeldBuffers * 2u * kX + kStages * (2u * kY + kStats) + 1024u;
 };
 
@@ -82,11 +86,11 @@ template <bool DKV> struct GradItem {
 // Walks the blocks of a CTA's items one after another: block `i` of the item, at row `row` of head `head`.
 template <bool DKV> struct GradCursor {
     GradItem<DKV> it;
-    uint32_t turn, i, in_head, row, head, count; // count: blocks passed, over all items
+    uint32_t turn, i, in_head, row, head;
     bool more;
     __device__ __forceinline__ void open(const AttnGradArgs &p)
     {
-        turn = count = 0;
+        turn = 0;
         enter(p);
     }
     // to the first block of item number `turn`, or of the next one that has blocks
@@ -113,7 +117,6 @@ template <bool DKV> struct GradCursor {
     }
     __device__ __forceinline__ void step(const AttnGradArgs &p)
     {
-        count++;
         if (++i == it.blocks) {
             turn++;
             enter(p);
@@ -131,12 +134,13 @@ template <bool DKV> struct GradCursor {
 template <typename T, int DP, bool DKV>
 __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const __grid_constant__ AttnGradArgs p)
 {
-    using Smem = GradSmem<DP>;
+    using Smem = GradSmem<DP, DKV>;
     constexpr bool BF16 = __is_same(T, __nv_bfloat16);
     constexpr int STAGES = Smem::kStages, HELD = Smem::kHeldBuffers;
+    constexpr uint32_t AHEAD = Smem::kAhead;
     constexpr uint32_t XBOX = kHeld * 128u, YBOX = kWalk * 128u;  // bytes of a 64-element box
     extern __shared__ unsigned char s_raw[];
-    __shared__ __align__(8) uint64_t x_full[HELD], x_empty[HELD], y_full[STAGES], y_empty[STAGES], t_full[2], ps_ready[2], acc_full,
+    __shared__ __align__(8) uint64_t x_full[HELD], x_empty[HELD], y_full[STAGES], y_empty[STAGES], t_full[3], ps_ready[3], acc_full,
         acc_empty, tail, drain;
     __shared__ uint32_t s_tmem, s_abort;
     unsigned char *const smem = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
@@ -154,12 +158,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             bar_init(&y_full[i], 1);
             bar_init(&y_empty[i], 1);
         }
-        for (int w = 0; w < 2; w++) {
+        for (uint32_t w = 0; w < AHEAD; w++) {
             bar_init(&t_full[w], 1);
-            bar_init(&ps_ready[w], 4);
+            bar_init(&ps_ready[w], 8);
         }
         bar_init(&acc_full, 1);
-        bar_init(&acc_empty, 8);
+        bar_init(&acc_empty, 16);
         bar_init(&tail, 1);
         bar_init(&drain, 1);
         fence_async();
@@ -171,100 +175,102 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
     const uint32_t tmem = s_tmem;
     volatile uint32_t *const stop = &s_abort;
 
-    if (warp < 8) {                                                // ---- probabilities, score gradients, results
-        take_registers<208>();
-        const uint32_t w = warp >> 2, quarter = (warp & 3u) << 21, lane_row = (warp & 3u) * 32u + lane;
-        const uint32_t t1 = tmem + 256u + w * 128u + quarter, t2 = t1 + 64u;
-        uint32_t count = 0, t_ph = 0, acc_ph = 0, stage = 0, y_ph = 0;   // count: blocks passed, over all items and both warpgroups
+    if (warp < 16) {                                               // ---- probabilities, score gradients, results
+        take_registers<104>();
+        const uint32_t turn_of = warp >> 3, part = (warp >> 2) & 1u, quarter = (warp & 3u) << 21, lane_row = (warp & 3u) * 32u + lane;
+        uint32_t count = 0, buf = 0, t_ph = 0, acc_ph = 0, stage = 0, y_ph = 0;   // count: blocks passed, over all items
         const int off = (int)a.Sk - (int)a.Sq;
         const uint64_t c2 = pair(a.scale_log2, a.scale_log2);
-        for (uint32_t turn = 0; turn * gridDim.x < p.items; turn++) {
-            const uint32_t item = grad_item(turn);
-            if (item >= p.items) continue;
-            GradItem<DKV> it;
-            it.set(p, item);
+        GradItem<DKV> it;
+        float nl = 0.0f, nd = 0.0f;
+        // item number `turn`, and for dq what its row brings along; false behind the last one
+        auto enter = [&](uint32_t &turn) {
+            for (; turn * gridDim.x < p.items; turn++) {
+                const uint32_t item = grad_item(turn);
+                if (item >= p.items) continue;
+                it.set(p, item);
+                if (!DKV && it.blocks) {
+                    const uint64_t at = ((uint64_t)it.b * a.H + it.h) * a.rows_padded + it.first + lane_row;
+                    nl = a.row_nl2[at];
+                    nd = a.row_ndelta[at];
+                }
+                return true;
+            }
+            return false;
+        };
+        uint32_t turn = 0;
+        bool ok = enter(turn);
+        while (ok) {
             const uint32_t row = it.first + lane_row, rows = DKV ? a.Sk : a.Sq, live = DKV ? it.n : a.Sq;
             const bool idle = it.first + (warp & 3u) * 32u >= live; // no row of the warp takes part
-            float nl = 0.0f, nd = 0.0f;
-            int limit = 0;                                          // dq: keys the row sees
-            if (!DKV && it.blocks) {
-                const uint64_t at = ((uint64_t)it.b * a.H + it.h) * a.rows_padded + row;
-                nl = a.row_nl2[at];
-                nd = a.row_ndelta[at];
-                limit = row < a.Sq ? attn_limit(a, it.n, (int)row) : (int)it.n;
-            }
+            const int limit = DKV ? 0 : row < a.Sq ? attn_limit(a, it.n, (int)row) : (int)it.n;   // dq: keys the row sees
             uint32_t at = it.start, in_head = 0;
-            bool ok = true;
             for (uint32_t i = 0; i < it.blocks; i++) {
-                if ((count & 1u) == w) {
-                    if (!(ok = bar_wait(&t_full[w], t_ph, stop))) break;
-                    t_ph ^= 1u;
+                if ((count & 1u) == turn_of) {
+                    if (!(ok = bar_wait(&t_full[buf], t_ph, stop))) break;
                     if (DKV && !(ok = bar_wait(&y_full[stage], y_ph, stop))) break;   // the statistics came by copy
-                    if (!idle) {
+                    const int cols = (int)((DKV ? a.Sq : it.n) - at);
+                    if (!idle && 32 * (int)part < cols) {
                         tmem_after_sync();
-                        const int cols = (int)((DKV ? a.Sq : it.n) - at);
-                        // the row's visible columns are [lo, hi)
-                        int lo = 0, hi = kWalk;
-                        if (DKV) lo = row >= it.n ? (int)kWalk : a.causal ? (int)row - off - (int)at : 0;
-                        else hi = limit - (int)at;
-                        const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < (int)kWalk);
-                        const float *const st = s_stats + stage * 2u * kWalk;
-                        float s[64], e[64];
-#pragma unroll
-                        for (int ch = 0; ch < 2; ch++)
-                            if (32 * ch < cols) {
-                                tmem_load32(t1 + 32 * ch, s + 32 * ch);
-                                tmem_load32(t2 + 32 * ch, e + 32 * ch);
-                            }
+                        const uint32_t t = tmem + Smem::kT + buf * 128u + quarter;
+                        float s[32], e[32];
+                        tmem_load32(t + 32u * part, s);
+                        tmem_load32(t + 64u + 32u * part, e);
+                        // of these columns the row sees [lo, hi)
+                        int lo = 0, hi = 32;
+                        if (DKV) lo = row >= it.n ? 32 : a.causal ? (int)row - off - (int)at - 32 * (int)part : 0;
+                        else hi = limit - (int)at - 32 * (int)part;
+                        const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < 32);
+                        const float *const st = s_stats + stage * 2u * kWalk + 32u * part;
                         tmem_wait_loads();
+                        uint32_t r1[16], r2[16];
 #pragma unroll
-                        for (int ch = 0; ch < 2; ch++) {
-                            if (32 * ch < cols) {
-                                uint32_t r1[16], r2[16];
+                        for (int k = 0; k < 8; k++) {              // four columns
+                            uint64_t l2[2], d2[2];
+                            if (DKV) {
+                                const float4 u = *reinterpret_cast<const float4 *>(st + 4 * k);
+                                const float4 v = *reinterpret_cast<const float4 *>(st + kWalk + 4 * k);
+                                l2[0] = pair(u.x, u.y); l2[1] = pair(u.z, u.w);
+                                d2[0] = pair(v.x, v.y); d2[1] = pair(v.z, v.w);
+                            } else {
+                                l2[0] = l2[1] = pair(nl, nl);
+                                d2[0] = d2[1] = pair(nd, nd);
+                            }
 #pragma unroll
-                                for (int k = 0; k < 8; k++) {      // four columns
-                                    uint64_t l2[2], d2[2];
-                                    if (DKV) {
-                                        const float4 u = *reinterpret_cast<const float4 *>(st + 32 * ch + 4 * k);
-                                        const float4 v = *reinterpret_cast<const float4 *>(st + kWalk + 32 * ch + 4 * k);
-                                        l2[0] = pair(u.x, u.y); l2[1] = pair(u.z, u.w);
-                                        d2[0] = pair(v.x, v.y); d2[1] = pair(v.z, v.w);
-                                    } else {
-                                        l2[0] = l2[1] = pair(nl, nl);
-                                        d2[0] = d2[1] = pair(nd, nd);
-                                    }
-#pragma unroll
-                                    for (int q = 0; q < 2; q++) {
-                                        const int c = 32 * ch + 4 * k + 2 * q;
-                                        float u, v, x, y;
-                                        unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
-                                        u = exp2_fast(u);
-                                        v = exp2_fast(v);
-                                        unpair(mul2(pair(u, v), add2(pair(e[c], e[c + 1]), d2[q])), x, y);
-                                        r1[2 * k + q] = round2<T>(u, v);
-                                        r2[2 * k + q] = round2<T>(x, y);
-                                    }
-                                }
-                                if (masked) {                      // cleared, not multiplied: what is masked may be NaN
-#pragma unroll
-                                    for (int k = 0; k < 16; k++) {
-                                        const int g = 32 * ch + 2 * k;
-                                        const uint32_t m = (g >= lo && g < hi ? 0xFFFFu : 0u) | (g + 1 >= lo && g + 1 < hi ? 0xFFFF0000u : 0u);
-                                        r1[k] &= m;
-                                        r2[k] &= m;
-                                    }
-                                }
-                                if (DKV) tmem_store16(t1 + 16 * ch, r1);
-                                tmem_store16(t2 + 16 * ch, r2);
+                            for (int q = 0; q < 2; q++) {
+                                const int c = 4 * k + 2 * q;
+                                float u, v, x, y;
+                                unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
+                                u = exp2_fast(u);
+                                v = exp2_fast(v);
+                                unpair(mul2(pair(u, v), add2(pair(e[c], e[c + 1]), d2[q])), x, y);
+                                r1[2 * k + q] = round2<T>(u, v);
+                                r2[2 * k + q] = round2<T>(x, y);
                             }
                         }
+                        if (masked) {                              // cleared, not multiplied: what is masked may be NaN
+#pragma unroll
+                            for (int k = 0; k < 16; k++) {
+                                const uint32_t m = (2 * k >= lo && 2 * k < hi ? 0xFFFFu : 0u) | (2 * k + 1 >= lo && 2 * k + 1 < hi ? 0xFFFF0000u : 0u);
+                                r1[k] &= m;
+                                r2[k] &= m;
+                            }
+                        }
+                        __syncwarp();
+                        // P and dS go over the columns that this warp has read
+                        if (DKV) tmem_store16(t + 32u * part, r1);
+                        tmem_store16(t + 64u + 32u * part, r2);
                         tmem_wait_stores();
                         tmem_before_sync();
                     }
                     __syncwarp();
-                    if (lane == 0) bar_arrive(&ps_ready[w]);
+                    if (lane == 0) bar_arrive(&ps_ready[buf]);
                 }
                 count++;
+                if (++buf == AHEAD) {
+                    buf = 0;
+                    t_ph ^= 1u;
+                }
                 if (++stage == STAGES) {
                     stage = 0;
                     y_ph ^= 1u;
@@ -276,30 +282,32 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 }
             }
             if (!ok) break;
-            if (it.blocks) {
-                if (!bar_wait(&acc_full, acc_ph, stop)) break;
+            // DKV: warpgroups 0 and 2 store dv, 1 and 3 dk, half of the columns each; dq: a quarter each
+            const uint32_t group = warp >> 2;
+            const AttnTensor &to = !DKV ? a.dq : group & 1u ? a.dk : a.dv;
+            const float by = DKV && !(group & 1u) ? 1.0f : a.scale;
+            constexpr uint32_t WIDTH = DKV ? DP / 2 : DP / 4;
+            const uint32_t from = (DKV ? group >> 1 : group) * WIDTH;
+            const uint32_t acc = tmem + (DKV ? (group & 1u) * DP : 0u) + from + quarter;
+            const bool some = it.blocks > 0, any = some && !idle, keep = any && row < live, exists = row < rows;
+            char *const dst = reinterpret_cast<char *>(to.p) + 2u * (to.sb * it.b + to.sh * it.h + to.ss * row + from);
+            turn++;
+            const bool more = enter(turn);                          // its loads come back while this item's last products run
+            if (some) {
+                if (!(ok = bar_wait(&acc_full, acc_ph, stop))) break;
                 acc_ph ^= 1u;
                 tmem_after_sync();
             }
-            // DKV: the first warpgroup stores dv, the second dk; dq: half of the columns each
-            const AttnTensor &to = !DKV ? a.dq : w == 0 ? a.dv : a.dk;
-            const float by = DKV && w == 0 ? 1.0f : a.scale;
-            constexpr uint32_t WIDTH = DKV ? DP : DP / 2;
-            const uint32_t from = DKV ? 0u : w * (DP / 2);
-            const uint32_t acc = tmem + w * WIDTH + quarter;
-            const bool any = it.blocks && !idle, keep = any && row < live;
-            char *const dst = reinterpret_cast<char *>(to.p) + 2u * (to.sb * it.b + to.sh * it.h + to.ss * row);
 #pragma unroll
-            for (uint32_t ch = 0; ch < WIDTH / 32; ch++) {
-                float o[32];
+            for (uint32_t ch = 0; ch < WIDTH / 16; ch++) {
+                float o[16];
                 if (any) {
-                    tmem_load32(acc + 32 * ch, o);
+                    tmem_load16(acc + 16 * ch, o);
                     tmem_wait_loads();
                 }
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const uint32_t d = from + 32u * ch + 8u * k;
-                    if (row < rows && d < a.D) {
+                for (int k = 0; k < 2; k++) {
+                    if (exists && from + 16u * ch + 8u * k < a.D) {
                         uint4 v = make_uint4(0u, 0u, 0u, 0u);
                         if (keep) {
                             v.x = round2<T>(o[8 * k] * by, o[8 * k + 1] * by);
@@ -307,19 +315,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                             v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
                             v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
                         }
-                        *reinterpret_cast<uint4 *>(dst + 2u * d) = v;
+                        *reinterpret_cast<uint4 *>(dst + 2u * (16u * ch + 8u * k)) = v;
                     }
                 }
             }
-            if (it.blocks) {
+            if (some) {
                 tmem_before_sync();
                 __syncwarp();
                 if (lane == 0) bar_arrive(&acc_empty);
             }
+            ok = more;
         }
     } else {
-        leave_registers<88>();
-        if (warp == 9) {                                           // ---- copies
+        leave_registers<64>();
+        if (warp == 17) {                                          // ---- copies
             GradCursor<DKV> cur;
             uint32_t st = 0, ph = 1, x = 0, x_ph = 1, tail_ph = 0;
             for (cur.open(p); cur.more; cur.step(p)) {
@@ -377,7 +386,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 const uint64_t until = now_ns() + 1000000000ull;
                 while (now_ns() < until) __nanosleep(1000);
             }
-        } else if (warp == 8) {                                    // ---- products
+        } else if (warp == 16) {                                   // ---- products
             const uint32_t one = elect_lane();
             const uint32_t steps = (a.D + 15u) / 16u;
             const uint32_t acc_desc = product_desc(BF16, steps * 16u, true);
@@ -385,7 +394,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             GradCursor<DKV> ahead, cur;
             ahead.open(p);
             cur.open(p);
-            uint32_t t_st = 0, t_phase = 0, x = 0, x_ph = 0, c_st = 0, acc_ph = 1, ps_ph[2] = {0, 0};
+            uint32_t t_st = 0, t_phase = 0, t_buf = 0, x = 0, x_ph = 0, c_st = 0, c_buf = 0, acc_ph = 1, ps_ph = 0;
             bool ok = true;
             // T1 and T2 of the block `ahead` stands at
             auto scores = [&]() {
@@ -393,7 +402,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 if (ahead.i == 0 && !(ok = bar_wait(&x_full[x], x_ph, stop))) return;
                 if (!(ok = bar_wait(&y_full[t_st], t_phase, stop))) return;
                 tmem_after_sync();
-                const uint32_t w = ahead.count & 1u, t = tmem + 256u + w * 128u;
+                const uint32_t t = tmem + Smem::kT + t_buf * 128u;
                 const uint32_t desc = product_desc(BF16, (ahead.cols(p) + 15u) & ~15u, false);
 #pragma unroll
                 for (uint32_t k = 0; k < 2; k++) {
@@ -403,7 +412,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                         if (s < steps)
                             product_ss(one, t + k * 64u, A + ((s & 3u) * 2u + (s >> 2) * (XBOX / 16u)), B + ((s & 3u) * 2u + (s >> 2) * (YBOX / 16u)), desc, s > 0);
                 }
-                products_done(one, &t_full[w]);
+                products_done(one, &t_full[t_buf]);
+                if (++t_buf == AHEAD) t_buf = 0;
                 if (ahead.last()) {
                     products_done(one, &x_empty[x]);
                     if (++x == HELD) {
@@ -417,12 +427,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 }
                 ahead.step(p);
             };
-            scores();
-            if (ok) scores();
+            for (uint32_t i = 0; i < AHEAD && ok; i++) scores();
             for (; ok && cur.more; cur.step(p)) {
-                const uint32_t w = cur.count & 1u, t = tmem + 256u + w * 128u, n16 = (cur.cols(p) + 15u) / 16u;
-                if (!bar_wait(&ps_ready[w], ps_ph[w], stop)) break;
-                ps_ph[w] ^= 1u;
+                const uint32_t t = tmem + Smem::kT + c_buf * 128u, n16 = (cur.cols(p) + 15u) / 16u;
+                if (!bar_wait(&ps_ready[c_buf], ps_ph, stop)) break;
+                if (++c_buf == AHEAD) {
+                    c_buf = 0;
+                    ps_ph ^= 1u;
+                }
                 if (cur.i == 0) {
                     if (!bar_wait(&acc_empty, acc_ph, stop)) break;
                     acc_ph ^= 1u;
@@ -432,10 +444,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 const bool add = cur.i > 0;
 #pragma unroll
                 for (uint32_t s = 0; s < kWalk / 16; s++)
-                    if (DKV && s < n16) product_ts(one, tmem, t + s * 8u, y2 + s * 128u, acc_desc, add || s > 0);
+                    if (DKV && s < n16) product_ts(one, tmem, t + (s >> 1) * 32u + (s & 1u) * 8u, y2 + s * 128u, acc_desc, add || s > 0);
 #pragma unroll
                 for (uint32_t s = 0; s < kWalk / 16; s++)
-                    if (s < n16) product_ts(one, tmem + (DKV ? DP : 0), t + 64u + s * 8u, y1 + s * 128u, acc_desc, add || s > 0);
+                    if (s < n16) product_ts(one, tmem + (DKV ? DP : 0), t + 64u + (s >> 1) * 32u + (s & 1u) * 8u, y1 + s * 128u, acc_desc, add || s > 0);
                 products_done(one, &y_empty[c_st]);
                 if (cur.last()) products_done(one, &acc_full);
                 if (++c_st == STAGES) c_st = 0;
@@ -455,8 +467,8 @@ template <typename T, int DP, bool DKV> static daf_status launch_grad(const Attn
 {
     int ctas = 0;
     const auto kernel = &attention_grad_kernel<T, DP, DKV>;
-    if (persistent_ctas(reinterpret_cast<const void *>(kernel), kGradThreads, (int)GradSmem<DP>::kBytes, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
-    kernel<<<p.items < (uint32_t)ctas ? p.items : (uint32_t)ctas, kGradThreads, GradSmem<DP>::kBytes, s>>>(p);
+    if (persistent_ctas(reinterpret_cast<const void *>(kernel), kGradThreads, (int)GradSmem<DP, DKV>::kBytes, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    kernel<<<p.items < (uint32_t)ctas ? p.items : (uint32_t)ctas, kGradThreads, GradSmem<DP, DKV>::kBytes, s>>>(p);
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 
