@@ -349,7 +349,8 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
  * int32.  Softmax statistics and sums are kept in binary32.  16-bit inputs: probabilities and score gradients are rounded
  * to dtype where they enter the second products; binary32 inputs: binary32 products throughout.
  * heads a multiple of kv_heads, head_dim a multiple of 8 (DAF_ERR_SHAPE), head_dim <= 128, queries and keys <= 2^24,
- * batch * heads <= 65535, batch * heads * queries <= 2^32 (DAF_ERR_UNSUPPORTED).  batch, queries or keys == 0 are valid.
+ * batch * heads <= 65535, batch * heads * queries and batch * kv_heads * keys <= 2^32 (DAF_ERR_UNSUPPORTED).
+ * batch, queries or keys == 0 are valid.
  * daf_attention_grad takes the forward pass's inputs, out and lse.  d_workspace: daf_attention_workspace(params) or
  * daf_attention_grad_workspace(params) bytes (0 for bad params), 16-byte aligned, contents irrelevant; it holds the device
  * status word afterwards (daf_poll_status: DAF_OK, or DAF_ERR_TIMEOUT when a wait inside a kernel ran out).  No output

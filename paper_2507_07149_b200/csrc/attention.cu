@@ -22,7 +22,8 @@ static daf_status check_attention(const daf_attention_params *p)
     if (p->causal > 1u || !(p->scale > -INFINITY && p->scale < INFINITY)) return DAF_ERR_INVALID_ARG;
     if (p->heads == 0 || p->kv_heads == 0 || p->heads % p->kv_heads || p->head_dim == 0 || p->head_dim % 8u) return DAF_ERR_SHAPE;
     if (p->head_dim > 128u || p->queries > (1u << 24) || p->keys > (1u << 24)) return DAF_ERR_UNSUPPORTED;
-    if ((uint64_t)p->batch * p->heads > 65535u || (uint64_t)p->batch * p->heads * p->queries > (1ull << 32)) return DAF_ERR_UNSUPPORTED;
+    const uint64_t heads = (uint64_t)p->batch * p->heads, kv_heads = (uint64_t)p->batch * p->kv_heads;
+    if (heads > 65535u || heads * p->queries > (1ull << 32) || kv_heads * p->keys > (1ull << 32)) return DAF_ERR_UNSUPPORTED;
     return DAF_OK;
 }
 
@@ -31,7 +32,8 @@ static AttnTensor tensor_of(const void *p, const uint64_t (&st)[3])
     return {const_cast<void *>(p), st[0], st[1], st[2]};
 }
 
-bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows)
+static bool encode_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows, uint32_t elems,
+                       CUtensorMapSwizzle swizzle)
 {
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -44,10 +46,19 @@ bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t 
     if (!encode) return false;
     const cuuint64_t extent[4] = {D, H, S, B}, none = (2ull * D + 15u) & ~15ull;     // an extent of one has no stride of its own
     const cuuint64_t stride[3] = {H > 1u ? 2ull * t.sh : none, S > 1u ? 2ull * t.ss : none, B > 1u ? 2ull * t.sb : none};
-    const cuuint32_t box[4] = {64, 1, rows, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {elems, 1, rows, 1}, step[4] = {1, 1, 1, 1};
     return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride, box, step,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows)
+{
+    return encode_map(map, bf16, t, B, S, H, D, rows, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+bool attn_store_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D)
+{
+    return encode_map(map, bf16, t, B, S, H, D, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 static uint32_t padded_rows(uint32_t rows) { return (rows + kAttnRowPad - 1u) / kAttnRowPad * kAttnRowPad; }

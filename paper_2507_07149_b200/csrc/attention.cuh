@@ -12,6 +12,19 @@ struct AttnTensor {
     uint64_t sb, ss, sh;
 };
 
+// Division by a number known on the host, by a product and a shift (Granlund and Montgomery, PLDI'94): n < 2^31.
+struct FastDiv {
+    uint32_t d, mul, shift;
+    __host__ void set(uint32_t by)
+    {
+        d = by;
+        shift = 0;
+        while ((1ull << shift) < by) shift++;
+        mul = (uint32_t)((((1ull << shift) - by) << 32) / by) + 1u;
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
+
 struct AttnArgs {
     AttnTensor q, k, v, out, grad_out, dq, dk, dv;
     float *lse;                  // [B, H, Sq]: natural logarithm of each row's sum of exponentials, -inf for a row that sees no key
@@ -41,6 +54,8 @@ template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHea
 
 // Map of a tensor for copies of `rows` rows times 64 elements of one head; false if the driver refuses it.
 bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows);
+// The same for storing 32 rows times 32 elements.
+bool attn_store_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D);
 
 daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);

@@ -28,8 +28,9 @@ constexpr float kLag = 8.0f;
 constexpr float kNoMax = -1e30f;                 // reference of a row that has seen no key yet
 
 struct AttnForwardArgs {
-    CUtensorMap q, k, v;
+    CUtensorMap q, k, v, out;
     AttnArgs a;
+    FastDiv heads, all_heads, tiles;             // H, B H, q_tiles
     uint32_t items, q_tiles;
     WorkspaceHeader *header;
 };
@@ -37,7 +38,8 @@ struct AttnForwardArgs {
 template <int DP> struct FwdSmem {
     static constexpr int kStages = DP == 128 ? 4 : 8;
     static constexpr uint32_t kTile = 128u * DP * 2u;            // one tile of 128 rows
-    static constexpr uint32_t kBytes = (2u + kStages) * kTile + 1024u;
+    static constexpr uint32_t kOut = 4096u;                       // two pieces of 32 x 32 outputs for each softmax warp
+    static constexpr uint32_t kBytes = (2u + kStages) * kTile + 8u * kOut + 1024u;
 };
 
 // The item's head, batch entry and first query, and its number of key blocks per half.
@@ -47,16 +49,16 @@ struct FwdItem {
     __device__ __forceinline__ FwdItem(const AttnForwardArgs &p, uint32_t item)
     {
         const AttnArgs &a = p.a;
-        const uint32_t heads = a.B * a.H;
         uint32_t bh, qt;
         if (a.causal) {                                            // longest rows first
-            qt = p.q_tiles - 1u - item / heads;
-            bh = item % heads;
+            qt = p.all_heads.div(item);
+            bh = item - qt * p.all_heads.d;
+            qt = p.q_tiles - 1u - qt;
         } else {                                                   // neighbours share keys and values
-            qt = item % p.q_tiles;
-            bh = item / p.q_tiles;
+            bh = p.tiles.div(item);
+            qt = item - bh * p.q_tiles;
         }
-        b = bh / a.H;
+        b = p.heads.div(bh);
         h = bh - b * a.H;
         m0 = qt * kFwdRows;
         n = attn_length(a, b);
@@ -122,7 +124,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
         take_registers<232>();
         const uint32_t w = warp >> 2, quarter = (warp & 3u) << 21;  // lane 32 (warp % 4) in the address's upper half
         const uint32_t ts = tmem + w * 128u + quarter, to = tmem + 256u + w * DP + quarter;
-        uint32_t s_ph = 0, pv = 0;                                  // pv: products into O that were handed over, ever
+        unsigned char *const s_out = smem + (2 + STAGES) * Smem::kTile + warp * Smem::kOut;
+        uint32_t pieces = 0, s_ph = 0, pv = 0;                                  // pv: products into O that were handed over, ever
         const float c = a.scale_log2;
         for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
             const FwdItem it(p, item);
@@ -215,31 +218,35 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
             }
             if (idle) continue;
             if (row < a.Sq) a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
-            char *const dst = reinterpret_cast<char *>(a.out.p) + 2u * (a.out.sb * it.b + a.out.sh * it.h + a.out.ss * row);
 #pragma unroll
             for (int i = 0; i < DP / 32; i++) {
+                if (32u * i >= a.D) continue;
                 float o[32];
                 if (it.blocks[w] > 0) {
                     tmem_load32(to + 32 * i, o);
                     tmem_wait_loads();
                 }
+                unsigned char *const piece = s_out + (pieces++ & 1u) * 2048;
+                if (lane == 0) stores_read<1>();                   // the store before last is out of this half
+                __syncwarp();
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    const uint32_t d = 32u * i + 8u * k;
-                    if (row < a.Sq && d < a.D) {
-                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                        if (l > 0.0f) {
-                            v.x = round2<T>(o[8 * k] * by, o[8 * k + 1] * by);
-                            v.y = round2<T>(o[8 * k + 2] * by, o[8 * k + 3] * by);
-                            v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
-                            v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
-                        }
-                        *reinterpret_cast<uint4 *>(dst + 2u * d) = v;
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (l > 0.0f) {
+                        v.x = round2<T>(o[8 * k] * by, o[8 * k + 1] * by);
+                        v.y = round2<T>(o[8 * k + 2] * by, o[8 * k + 3] * by);
+                        v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
+                        v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
                     }
+                    stage_piece(piece, lane, k, v);
                 }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) tma_store(&p.out, piece, 32 * i, it.h, first + (warp & 3u) * 32u, it.b);
             }
             tmem_before_sync();
         }
+        if (lane == 0) stores_done();
     } else {
         leave_registers<40>();
         if (warp == 9) {                                               // ---- copies
@@ -385,7 +392,10 @@ template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHea
     p.items = p.q_tiles * a.B * a.H;
     p.header = header;
     const bool bf16 = __is_same(T, __nv_bfloat16);
-    if (!attn_tensor_map(&p.q, bf16, a.q, a.B, a.Sq, a.H, a.D, 128)) return DAF_ERR_CUDA;
+    p.heads.set(a.H);
+    p.all_heads.set(a.B * a.H);
+    p.tiles.set(p.q_tiles);
+    if (!attn_tensor_map(&p.q, bf16, a.q, a.B, a.Sq, a.H, a.D, 128) || !attn_store_map(&p.out, bf16, a.out, a.B, a.Sq, a.H, a.D)) return DAF_ERR_CUDA;
     if (a.Sk == 0) p.k = p.v = p.q;                                // never read
     else if (!attn_tensor_map(&p.k, bf16, a.k, a.B, a.Sk, a.Hkv, a.D, 128) || !attn_tensor_map(&p.v, bf16, a.v, a.B, a.Sk, a.Hkv, a.D, 128))
         return DAF_ERR_CUDA;

@@ -27,7 +27,9 @@ constexpr uint32_t kHeld = 128, kWalk = 64;
 
 struct AttnGradArgs {
     CUtensorMap x1, x2, y1, y2;                  // held: k, v or q, grad_out; walked: q, grad_out or k, v
+    CUtensorMap out[2];                          // dv, dk or dq
     AttnArgs a;
+    FastDiv heads, all_heads, tile_div;          // heads of the items, times B, tiles
     uint32_t items, tiles;
     WorkspaceHeader *header;
 };
@@ -38,7 +40,9 @@ template <int DP, bool DKV> struct GradSmem {
     static constexpr uint32_t kStats = 2u * kWalk * 4u;           // -L and -delta of a block's queries
     // blocks of T in tensor memory, behind the sums
     static constexpr uint32_t kAhead = (512u - (DKV ? 2u : 1u) * DP) / 128u < 3u ? 2u : 3u, kT = 512u - kAhead * 128u;
-    static constexpr uint32_t kBytes = kHeldBuffers * 2u * kX + kStages * (2u * kY + kStats) + 1024u;
+    static constexpr uint32_t kOut = 2048u;                       // a piece of 32 x 32 results for each of the 16 warps
+    static constexpr uint32_t kBars = 1024u;                      // barriers and such, ahead of everything
+    static constexpr uint32_t kBytes = kBars + kHeldBuffers * 2u * kX + kStages * (2u * kY + kStats) + 16u * kOut;
 };
 
 // The i-th item of a CTA: there and back over the list, which starts with the longest items, so that who got a long
@@ -54,18 +58,17 @@ template <bool DKV> struct GradItem {
     __device__ __forceinline__ void set(const AttnGradArgs &p, uint32_t item)
     {
         const AttnArgs &a = p.a;
-        const uint32_t heads = DKV ? a.Hkv : a.H, all = a.B * heads;
         uint32_t tile, bh;
         if (a.causal) {
-            tile = item / all;
-            bh = item - tile * all;
+            tile = p.all_heads.div(item);
+            bh = item - tile * p.all_heads.d;
             if (!DKV) tile = p.tiles - 1u - tile;
         } else {
-            bh = item / p.tiles;
+            bh = p.tile_div.div(item);
             tile = item - bh * p.tiles;
         }
-        b = bh / heads;
-        h = bh - b * heads;
+        b = p.heads.div(bh);
+        h = bh - b * p.heads.d;
         first = tile * kHeld;
         n = attn_length(a, b);
         start = 0;
@@ -139,13 +142,26 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
     constexpr int STAGES = Smem::kStages, HELD = Smem::kHeldBuffers;
     constexpr uint32_t AHEAD = Smem::kAhead;
     constexpr uint32_t XBOX = kHeld * 128u, YBOX = kWalk * 128u;  // bytes of a 64-element box
-    extern __shared__ unsigned char s_raw[];
-    __shared__ __align__(8) uint64_t x_full[HELD], x_empty[HELD], y_full[STAGES], y_empty[STAGES], t_full[3], ps_ready[3], acc_full,
-        acc_empty, tail, drain;
-    __shared__ uint32_t s_tmem, s_abort;
-    unsigned char *const smem = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
+    // tiles need 1024-byte boundaries; with nothing declared statically the dynamic part starts on one
+    extern __shared__ __align__(1024) unsigned char s_raw[];
+    struct Bars {
+        uint64_t x_full[2], x_empty[2], y_full[6], y_empty[6], t_full[3], ps_ready[3], acc_full, acc_empty, tail, drain;
+        uint32_t tmem, abort;
+    };
+    static_assert(sizeof(Bars) <= Smem::kBars && HELD <= 2 && STAGES <= 6 && AHEAD <= 3, "barriers fit their places");
+    Bars &bars = *reinterpret_cast<Bars *>(s_raw);
+    uint64_t *const x_full = bars.x_full, *const x_empty = bars.x_empty, *const y_full = bars.y_full, *const y_empty = bars.y_empty,
+             *const t_full = bars.t_full, *const ps_ready = bars.ps_ready;
+    uint64_t &acc_full = bars.acc_full, &acc_empty = bars.acc_empty, &tail = bars.tail, &drain = bars.drain;
+    uint32_t &s_tmem = bars.tmem, &s_abort = bars.abort;
+    if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
+        if (threadIdx.x == 0) p.header->status = DAF_ERR_UNSUPPORTED;
+        return;
+    }
+    unsigned char *const smem = s_raw + Smem::kBars;
     unsigned char *const s_y = smem + HELD * 2u * Smem::kX;
-    float *const s_stats = reinterpret_cast<float *>(s_y + STAGES * 2u * Smem::kY);
+    unsigned char *const s_out = s_y + STAGES * 2u * Smem::kY;
+    float *const s_stats = reinterpret_cast<float *>(s_out + 16u * Smem::kOut);
     const AttnArgs &a = p.a;
     const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
     if (threadIdx.x == 0) {
@@ -282,15 +298,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 }
             }
             if (!ok) break;
-            // DKV: warpgroups 0 and 2 store dv, 1 and 3 dk, half of the columns each; dq: a quarter each
+            // DKV: warpgroups 0 and 2 store dv, 1 and 3 dk, half of the columns each; dq: 32 columns each, as far as they go
             const uint32_t group = warp >> 2;
-            const AttnTensor &to = !DKV ? a.dq : group & 1u ? a.dk : a.dv;
+            const CUtensorMap *const to = &p.out[DKV ? group & 1u : 0u];
             const float by = DKV && !(group & 1u) ? 1.0f : a.scale;
-            constexpr uint32_t WIDTH = DKV ? DP / 2 : DP / 4;
+            constexpr uint32_t WIDTH = DKV ? DP / 2 : 32;
             const uint32_t from = (DKV ? group >> 1 : group) * WIDTH;
             const uint32_t acc = tmem + (DKV ? (group & 1u) * DP : 0u) + from + quarter;
-            const bool some = it.blocks > 0, any = some && !idle, keep = any && row < live, exists = row < rows;
-            char *const dst = reinterpret_cast<char *>(to.p) + 2u * (to.sb * it.b + to.sh * it.h + to.ss * row + from);
+            const bool some = it.blocks > 0, any = some && !idle, keep = any && row < live;
+            const uint32_t out_h = it.h, out_b = it.b, out_row = it.first + (warp & 3u) * 32u;
+            const bool exists = out_row < rows && from < a.D;
             turn++;
             const bool more = enter(turn);                          // its loads come back while this item's last products run
             if (some) {
@@ -298,26 +315,31 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 acc_ph ^= 1u;
                 tmem_after_sync();
             }
+            unsigned char *const piece = s_out + warp * Smem::kOut;
 #pragma unroll
-            for (uint32_t ch = 0; ch < WIDTH / 16; ch++) {
-                float o[16];
+            for (uint32_t ch = 0; ch < WIDTH / 32; ch++) {
+                if (!exists || from + 32u * ch >= a.D) continue;
+                float o[32];
                 if (any) {
-                    tmem_load16(acc + 16 * ch, o);
+                    tmem_load32(acc + 32 * ch, o);
                     tmem_wait_loads();
                 }
+                if (lane == 0) stores_read<0>();
+                __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    if (exists && from + 16u * ch + 8u * k < a.D) {
-                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                        if (keep) {
-                            v.x = round2<T>(o[8 * k] * by, o[8 * k + 1] * by);
-                            v.y = round2<T>(o[8 * k + 2] * by, o[8 * k + 3] * by);
-                            v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
-                            v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
-                        }
-                        *reinterpret_cast<uint4 *>(dst + 2u * (16u * ch + 8u * k)) = v;
+                for (int k = 0; k < 4; k++) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (keep) {
+                        v.x = round2<T>(o[8 * k] * by, o[8 * k + 1] * by);
+                        v.y = round2<T>(o[8 * k + 2] * by, o[8 * k + 3] * by);
+                        v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
+                        v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
                     }
+                    stage_piece(piece, lane, k, v);
                 }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) tma_store(to, piece, from + 32u * ch, out_h, out_row, out_b);
             }
             if (some) {
                 tmem_before_sync();
@@ -326,6 +348,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             }
             ok = more;
         }
+        if (lane == 0) stores_done();
     } else {
         leave_registers<64>();
         if (warp == 17) {                                          // ---- copies
@@ -483,14 +506,21 @@ template <typename T> daf_status attn_backward_tc(const AttnArgs &a, WorkspaceHe
         return attn_tensor_map(&p.x1, bf16, x1, a.B, Sx, Hx, a.D, kHeld) && attn_tensor_map(&p.x2, bf16, x2, a.B, Sx, Hx, a.D, kHeld) &&
                attn_tensor_map(&p.y1, bf16, y1, a.B, Sy, Hy, a.D, kWalk) && attn_tensor_map(&p.y2, bf16, y2, a.B, Sy, Hy, a.D, kWalk);
     };
-    if (!maps(a.k, a.v, a.Sk, a.Hkv, a.q, a.grad_out, a.Sq, a.H)) return DAF_ERR_CUDA;
-    p.tiles = (a.Sk + kHeld - 1u) / kHeld;
-    p.items = p.tiles * a.B * a.Hkv;
+    const auto items = [&](uint32_t S, uint32_t H) {
+        p.tiles = (S + kHeld - 1u) / kHeld;
+        p.items = p.tiles * a.B * H;
+        p.heads.set(H);
+        p.all_heads.set(a.B * H);
+        p.tile_div.set(p.tiles);
+    };
+    if (!maps(a.k, a.v, a.Sk, a.Hkv, a.q, a.grad_out, a.Sq, a.H) || !attn_store_map(&p.out[0], bf16, a.dv, a.B, a.Sk, a.Hkv, a.D) ||
+        !attn_store_map(&p.out[1], bf16, a.dk, a.B, a.Sk, a.Hkv, a.D))
+        return DAF_ERR_CUDA;
+    items(a.Sk, a.Hkv);
     daf_status st = a.D <= 64u ? launch_grad<T, 64, true>(p, s) : launch_grad<T, 128, true>(p, s);
     if (st != DAF_OK) return st;
-    if (!maps(a.q, a.grad_out, a.Sq, a.H, a.k, a.v, a.Sk, a.Hkv)) return DAF_ERR_CUDA;
-    p.tiles = (a.Sq + kHeld - 1u) / kHeld;
-    p.items = p.tiles * a.B * a.H;
+    if (!maps(a.q, a.grad_out, a.Sq, a.H, a.k, a.v, a.Sk, a.Hkv) || !attn_store_map(&p.out[0], bf16, a.dq, a.B, a.Sq, a.H, a.D)) return DAF_ERR_CUDA;
+    items(a.Sq, a.H);
     st = a.D <= 64u ? launch_grad<T, 64, false>(p, s) : launch_grad<T, 128, false>(p, s);
     return st;
 }

@@ -70,6 +70,22 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
+// The way out for a warp's 32 rows: 32 columns at a time through 2 KiB of shared memory and a tiled store, which clips rows
+// and columns behind the tensor's ends.  (Stored by the threads, each its own row, a warp's store touches 32 lines for 512
+// bytes: a third of the time of short sequences.)  The pieces of a row lie where a 64-byte swizzle wants them.
+__device__ __forceinline__ void stage_piece(unsigned char *stage, uint32_t row, uint32_t piece, uint4 v)
+{
+    *reinterpret_cast<uint4 *>(stage + row * 64u + ((piece ^ (row >> 1 & 3u)) * 16u)) = v;
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, const unsigned char *stage, int elem, int head, int row, int batch)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(map), "r"(smem_u32(stage)), "r"(elem), "r"(head), "r"(row), "r"(batch) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// At most N of this thread's stores still read shared memory.
+template <int N> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // Orders this thread's writes to shared memory ahead of later reads by copies and products.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
