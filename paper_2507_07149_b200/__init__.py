@@ -230,12 +230,21 @@ def dtype_code(t) -> int:
     return _dtype_codes()[t.dtype]
 
 
+def _raw_stream(index: int, stream) -> int:
+    """The cudaStream_t of `stream`, or of torch's current stream of device `index`."""
+    if stream is not None:
+        return stream.cuda_stream
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)       # the same without a Stream object
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 def _call(fn, ref, stream, *args) -> int:
     """Calls fn(*args, stream) with the device of tensor `ref` current in this thread (the library launches on the
     current device) and, unless a stream is given, on torch's current stream OF THAT DEVICE.  Returns the status."""
     cuda = _torch().cuda
     index = ref.get_device()
-    raw = cuda.current_stream(index).cuda_stream if stream is None else stream.cuda_stream
+    raw = _raw_stream(index, stream)
     if index == cuda.current_device():
         return int(fn(*args, raw))
     with cuda.device(index):
@@ -574,13 +583,35 @@ def _one_device(where: str, index: int, tensors) -> None:
             raise ValueError(f"{where}: all tensors belong on one CUDA device")
 
 
+def _template(shape, dtype, device):
+    """A tensor of that shape that owns one element: empty_like of it is the cheapest way to allocate the shape again."""
+    return _torch().empty((1,) * len(shape), dtype=dtype, device=device).expand(shape)
+
+
+def _fresh(template):
+    torch = _torch()
+    return torch.empty_like(template, memory_format=torch.contiguous_format)
+
+
+_headers = {}                                                         # (device, stream) -> status workspace
+
+
+def _header(index: int, raw: int):
+    """The workspace of calls that only keep a status word there: one for each stream, whose calls do not overlap."""
+    ws = _headers.get((index, raw))
+    if ws is None:
+        torch = _torch()
+        ws = _remember(_headers, (index, raw), torch.empty(256, dtype=torch.uint8, device=f"cuda:{index}"))
+    return ws
+
+
 _attention_plans = {}
 
 
 class _AttentionPlan:
     """What a call of attention / attention_grad derives from types, shapes and strides alone: remembered per shape, since a
     model repeats the same ones every step.  `direct`: which of the tensors the kernels can address in place."""
-    __slots__ = ("params", "ref", "ws", "lse_shape", "direct")
+    __slots__ = ("params", "ref", "ws", "lse_shape", "direct", "like_q", "like_k", "like_lse", "like_ws")
 
 
 def _attention_plan(where: str, causal, scale, tensors) -> _AttentionPlan:
@@ -614,6 +645,8 @@ def _attention_plan(where: str, causal, scale, tensors) -> _AttentionPlan:
     plan.params, plan.ref, plan.direct = p, ctypes.byref(p), direct
     plan.ws = daf_attention_workspace(p) if len(tensors) == 4 else daf_attention_grad_workspace(p)
     plan.lse_shape = (b, h, sq)
+    plan.like_q, plan.like_k = _template(q.shape, q.dtype, q.device), _template(k.shape, q.dtype, q.device)
+    plan.like_lse, plan.like_ws = _template(plan.lse_shape, torch.float32, q.device), _template((plan.ws,), torch.uint8, q.device)
     return plan
 
 
@@ -646,13 +679,12 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     exponentials [B, H, Sq] that the backward pass needs (daf_attention).  Slices of a packed projection are read in place;
     tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
     first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq."""
-    torch = _torch()
     index = q.get_device()
     if index < 0:
         raise ValueError("attention expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
     if k.get_device() != index or v.get_device() != index:
         _one_device("attention", index, (k, v))
-    key = (q.dtype, k.dtype, v.dtype, q.shape, k.shape, v.shape, q.stride(), k.stride(), v.stride(), causal, scale,
+    key = (index, q.dtype, k.dtype, v.dtype, q.shape, k.shape, v.shape, q.stride(), k.stride(), v.stride(), causal, scale,
            None if out is None else (out.dtype, out.shape, out.stride()))
     plan = _attention_plans.get(key)
     if plan is None:
@@ -661,16 +693,15 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
         _check_lengths("attention", key_lengths, q)
     direct = plan.direct
     (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
-    dev = q.device
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = _fresh(plan.like_q)
     else:
         _one_device("attention", index, (out,))
     if lse is None:
-        lse = torch.empty(plan.lse_shape, dtype=torch.float32, device=dev)
+        lse = _fresh(plan.like_lse)
     else:
         _check_lse("attention", lse, plan.lse_shape, q)
-    ws = torch.empty(plan.ws, dtype=torch.uint8, device=dev)
+    ws = _header(index, _raw_stream(index, stream))
     status = _call(lib().daf_attention, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), out.data_ptr(), lse.data_ptr(),
                    ws.data_ptr(), plan.ws)
     _check(status, "daf_attention")
@@ -683,12 +714,11 @@ def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: 
                    check: bool = False, stream=None):
     """(grad_q, grad_k, grad_v) of ``attention`` from its inputs, its two results and grad_out (daf_attention_grad).  grads:
     three tensors to write into (they may be slices of one packed gradient), fresh contiguous ones by default."""
-    torch = _torch()
     index = q.get_device()
     if index < 0:
         raise ValueError("attention_grad expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
     _one_device("attention_grad", index, (k, v, out, grad_out))
-    key = (q.dtype, k.dtype, v.dtype, out.dtype, grad_out.dtype, q.shape, k.shape, v.shape, out.shape, grad_out.shape, q.stride(),
+    key = (index, q.dtype, k.dtype, v.dtype, out.dtype, grad_out.dtype, q.shape, k.shape, v.shape, out.shape, grad_out.shape, q.stride(),
            k.stride(), v.stride(), out.stride(), grad_out.stride(), causal, scale,
            None if grads is None else tuple((t.dtype, t.shape, t.stride()) for t in grads))
     plan = _attention_plans.get(key)
@@ -701,14 +731,12 @@ def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: 
     direct = plan.direct
     (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
     (out, oa), (grad_out, ga) = _addressable(out, direct[3]), _addressable(grad_out, direct[4])
-    dev = q.device
     if grads is None:
-        gq, gk, gv = (torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=q.dtype, device=dev),
-                      torch.empty(k.shape, dtype=q.dtype, device=dev))
+        gq, gk, gv = _fresh(plan.like_q), _fresh(plan.like_k), _fresh(plan.like_k)
     else:
         gq, gk, gv = grads
         _one_device("attention_grad", index, grads)
-    ws = torch.empty(plan.ws, dtype=torch.uint8, device=dev)
+    ws = _fresh(plan.like_ws)
     status = _call(lib().daf_attention_grad, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), oa, lse.data_ptr(), ga,
                    gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), ws.data_ptr(), plan.ws)
     _check(status, "daf_attention_grad")
@@ -722,7 +750,7 @@ _norm_plans = {}
 
 class _NormPlan:
     """Parameter block and workspace size of residual_norm / residual_norm_grad for one set of types and shapes."""
-    __slots__ = ("params", "ref", "ws")
+    __slots__ = ("params", "ref", "ws", "like_ws")
 
 
 def _norm_plan(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps) -> _NormPlan:
@@ -747,6 +775,7 @@ def _norm_plan(where: str, x, y, weight, bias, gate, post_weight, post_bias, res
                                   NORM_LAYER if kind == "layer" else NORM_RMS, rows, width, gates, residual_scale, eps, 0)
     plan.ref = ctypes.byref(plan.params)
     plan.ws = daf_residual_norm_grad_workspace(plan.params)
+    plan.like_ws = _template((plan.ws,), _torch().uint8, x.device)
     return plan
 
 
@@ -754,13 +783,13 @@ def _norm_call(where: str, x, y, weight, bias, gate, post_weight, post_bias, res
     """The plan for these tensors; `more` are activations of x's shape and type.  Every tensor is checked for its device and for
     being contiguous."""
     vectors = (weight, bias, gate, post_weight, post_bias)
-    key = (x.dtype, y.dtype, x.shape, y.shape, residual_scale, kind, eps, *[None if t is None else (t.dtype, t.shape) for t in vectors])
-    plan = _norm_plans.get(key)
-    if plan is None:
-        plan = _remember(_norm_plans, key, _norm_plan(where, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps))
     index = x.get_device()
     if index < 0:
         raise ValueError(f"{where} expects CUDA tensors")
+    key = (index, x.dtype, y.dtype, x.shape, y.shape, residual_scale, kind, eps, *[None if t is None else (t.dtype, t.shape) for t in vectors])
+    plan = _norm_plans.get(key)
+    if plan is None:
+        plan = _remember(_norm_plans, key, _norm_plan(where, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps))
     for t in (x, y, *vectors, *more):
         if t is not None and (t.get_device() != index or not t.is_contiguous()):
             raise ValueError(f"{where} expects contiguous tensors on one CUDA device")
@@ -795,7 +824,7 @@ def residual_norm_grad(z, y, weight, bias, grad_z, grad_h, *, gate=None, post_we
     empty = torch.empty_like
     gx, gy, gw = empty(z), empty(z), empty(weight)
     gb, gg, gpw, gpb = (None if t is None else empty(t) for t in (bias, gate, post_weight, post_bias))
-    ws = torch.empty(plan.ws, dtype=torch.uint8, device=z.device)
+    ws = _fresh(plan.like_ws)
     status = _call(lib().daf_residual_norm_grad, z, stream, plan.ref, z.data_ptr(), y.data_ptr(), weight.data_ptr(), _ptr(gate),
                    _ptr(post_weight), _ptr(post_bias), _ptr(grad_z), grad_h.data_ptr(), gx.data_ptr(), gy.data_ptr(), gw.data_ptr(),
                    _ptr(gb), _ptr(gg), _ptr(gpw), _ptr(gpb), ws.data_ptr(), plan.ws)
