@@ -115,7 +115,7 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
     a.lengths = d_key_lengths;
     WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    return p.dtype == DAF_F32 ? attn_forward_general(p.dtype, a, header, s)
+    return p.dtype == DAF_F32 ? attn_forward_f32(a, header, s)
            : p.dtype == DAF_F16 ? attn_forward_tc<__half>(a, header, s) : attn_forward_tc<__nv_bfloat16>(a, header, s);
 }
 
@@ -169,6 +169,11 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     } else if (cudaMemsetAsync(header, 0, sizeof(uint32_t), s) != cudaSuccess) {
         return DAF_ERR_CUDA;
     }
-    if (p.dtype == DAF_F32 || p.queries == 0 || p.keys == 0) return attn_backward_general(p.dtype, a, s);
-    return p.dtype == DAF_F16 ? attn_backward_tc<__half>(a, header, s) : attn_backward_tc<__nv_bfloat16>(a, header, s);
+    if (p.queries == 0) {
+        const daf_status st = attn_zero(p.dtype, a.dk, a.B, a.Sk, a.Hkv, a.D, s);
+        return st != DAF_OK ? st : attn_zero(p.dtype, a.dv, a.B, a.Sk, a.Hkv, a.D, s);
+    }
+    if (p.keys == 0) return attn_zero(p.dtype, a.dq, a.B, a.Sq, a.H, a.D, s);
+    return p.dtype == DAF_F32 ? attn_backward_f32(a, s)
+           : p.dtype == DAF_F16 ? attn_backward_tc<__half>(a, header, s) : attn_backward_tc<__nv_bfloat16>(a, header, s);
 }

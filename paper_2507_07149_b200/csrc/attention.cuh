@@ -49,7 +49,10 @@ __device__ __forceinline__ int attn_limit(const AttnArgs &a, uint32_t n, int i)
     return c < (int)n ? c : (int)n;
 }
 
-daf_status attn_forward_general(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
+daf_status attn_forward_f32(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
+daf_status attn_backward_f32(const AttnArgs &a, cudaStream_t s);
+daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
+daf_status attn_zero(uint32_t dtype, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, cudaStream_t s);
 template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 
 // Map of a tensor for copies of `rows` rows times 64 elements of one head; false if the driver refuses it.
@@ -57,8 +60,6 @@ bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t 
 // The same for storing 32 rows times 32 elements.
 bool attn_store_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D);
 
-daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
-daf_status attn_backward_general(uint32_t dtype, const AttnArgs &a, cudaStream_t s);
 template <typename T> daf_status attn_backward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 
 }  // namespace daf
