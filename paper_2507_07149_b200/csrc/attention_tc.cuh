@@ -312,11 +312,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 auto scores = [&](int w, int j, uint32_t at) {
                     const uint32_t valid = it.n - (uint32_t)j * kBlock, cols = valid < (uint32_t)kBlock ? (valid + 15u) & ~15u : kBlock;
                     const uint32_t desc = product_desc(BF16, cols, false);
-                    const uint64_t q = operand_desc(q_smem + w * Smem::kTile, 16), k = operand_desc(kv_smem + at * Smem::kTile, 16);
+                    const uint32_t q = operand_low(q_smem + w * Smem::kTile, 16), k = operand_low(kv_smem + at * Smem::kTile, 16);
+                    product_ss(one, tmem + w * 128u, q, k, desc, false);
 #pragma unroll
-                    for (uint32_t s = 0; s < DP / 16; s++) {
+                    for (uint32_t s = 1; s < DP / 16; s++) {
                         const uint32_t by = (s & 3u) * 2u + (s >> 2) * 1024u;         // 32 bytes along the row, 16 KiB per 64 elements
-                        if (s < steps) product_ss(one, tmem + w * 128u, q + by, k + by, desc, s > 0);
+                        if (s < steps) product_ss<true>(one, tmem + w * 128u, q + by, k + by, desc);
                     }
                     products_done(one, &s_full[w]);
                 };
@@ -348,10 +349,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                         if (!bar_wait(&p_ready[w], p_ph[w], stop)) break;
                         p_ph[w] ^= 1u;
                         tmem_after_sync();
-                        const uint64_t v = operand_desc(kv_smem + v_st * Smem::kTile, 16384);
+                        const uint32_t v = operand_low(kv_smem + v_st * Smem::kTile, 16384);
+                        product_ts(one, tmem + 256u + w * DP, tmem + w * 128u, v, pv_desc, j > 0);
 #pragma unroll
-                        for (uint32_t s = 0; s < kBlock / 16; s++)                   // 16 keys: 2 KiB of v, 8 columns of P
-                            if (s < pv_steps) product_ts(one, tmem + 256u + w * DP, tmem + w * 128u + s * 8u, v + s * 128u, pv_desc, j > 0 || s > 0);
+                        for (uint32_t s = 1; s < kBlock / 16; s++)                   // 16 keys: 2 KiB of v, 8 columns of P
+                            if (s < pv_steps) product_ts<true>(one, tmem + 256u + w * DP, tmem + w * 128u + s * 8u, v + s * 128u, pv_desc);
                         products_done(one, &o_done[w]);
                         if (j + 1 < it.blocks[w]) scores(w, j + 1, st);
                     }

@@ -429,11 +429,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 const uint32_t desc = product_desc(BF16, (ahead.cols(p) + 15u) & ~15u, false);
 #pragma unroll
                 for (uint32_t k = 0; k < 2; k++) {
-                    const uint64_t A = operand_desc(xs + x * 2u * Smem::kX + k * Smem::kX, 16), B = operand_desc(ys + t_st * 2u * Smem::kY + k * Smem::kY, 16);
+                    const uint32_t A = operand_low(xs + x * 2u * Smem::kX + k * Smem::kX, 16), B = operand_low(ys + t_st * 2u * Smem::kY + k * Smem::kY, 16);
+                    product_ss(one, t + k * 64u, A, B, desc, false);
 #pragma unroll
-                    for (uint32_t s = 0; s < DP / 16; s++)
+                    for (uint32_t s = 1; s < DP / 16; s++)
                         if (s < steps)
-                            product_ss(one, t + k * 64u, A + ((s & 3u) * 2u + (s >> 2) * (XBOX / 16u)), B + ((s & 3u) * 2u + (s >> 2) * (YBOX / 16u)), desc, s > 0);
+                            product_ss<true>(one, t + k * 64u, A + ((s & 3u) * 2u + (s >> 2) * (XBOX / 16u)), B + ((s & 3u) * 2u + (s >> 2) * (YBOX / 16u)), desc);
                 }
                 products_done(one, &t_full[t_buf]);
                 if (++t_buf == AHEAD) t_buf = 0;
@@ -463,14 +464,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                     acc_ph ^= 1u;
                 }
                 tmem_after_sync();
-                const uint64_t y1 = operand_desc(ys + c_st * 2u * Smem::kY, YBOX), y2 = operand_desc(ys + c_st * 2u * Smem::kY + Smem::kY, YBOX);
+                const uint32_t y1 = operand_low(ys + c_st * 2u * Smem::kY, YBOX), y2 = operand_low(ys + c_st * 2u * Smem::kY + Smem::kY, YBOX);
                 const bool add = cur.i > 0;
+                // 16 rows of the walk a step: 2 KiB of the tile, 8 columns of P or dS
+                if (DKV) {
+                    product_ts(one, tmem, t, y2, acc_desc, add);
 #pragma unroll
-                for (uint32_t s = 0; s < kWalk / 16; s++)
-                    if (DKV && s < n16) product_ts(one, tmem, t + (s >> 1) * 32u + (s & 1u) * 8u, y2 + s * 128u, acc_desc, add || s > 0);
+                    for (uint32_t s = 1; s < kWalk / 16; s++)
+                        if (s < n16) product_ts<true>(one, tmem, t + (s >> 1) * 32u + (s & 1u) * 8u, y2 + s * 128u, acc_desc);
+                }
+                product_ts(one, tmem + (DKV ? DP : 0), t + 64u, y1, acc_desc, add);
 #pragma unroll
-                for (uint32_t s = 0; s < kWalk / 16; s++)
-                    if (s < n16) product_ts(one, tmem + (DKV ? DP : 0), t + 64u + (s >> 1) * 32u + (s & 1u) * 8u, y1 + s * 128u, acc_desc, add || s > 0);
+                for (uint32_t s = 1; s < kWalk / 16; s++)
+                    if (s < n16) product_ts<true>(one, tmem + (DKV ? DP : 0), t + 64u + (s >> 1) * 32u + (s & 1u) * 8u, y1 + s * 128u, acc_desc);
                 products_done(one, &y_empty[c_st]);
                 if (cur.last()) products_done(one, &acc_full);
                 if (++c_st == STAGES) c_st = 0;

@@ -136,13 +136,11 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t *r)
                  "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
 }
 
-// Operand descriptor of a tile in shared memory with 128-byte swizzle: address, the distance `lead` between 64-element
-// spans of the contiguous dimension (used where that dimension is not the summed one) and 1024 bytes between groups of
-// eight rows.  Steps along a tile are added to the descriptor's address field (units of 16 bytes).
-__device__ __forceinline__ uint64_t operand_desc(uint32_t smem, uint32_t lead)
-{
-    return (uint64_t)((smem >> 4) & 0x3FFFu) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// Operand descriptor of a tile in shared memory with 128-byte swizzle.  Low word: the address and the distance `lead`
+// between 64-element spans of the contiguous dimension (used where that dimension is not the summed one); high word, the
+// same for all: 1024 bytes between groups of eight rows.  Steps along a tile are added to the low word (16-byte units).
+constexpr uint32_t kOperandHigh = 1024u >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t operand_low(uint32_t smem, uint32_t lead) { return (smem >> 4 & 0x3FFFu) | lead >> 4 << 16; }
 // Instruction descriptor: 16-bit operands (both of one type), binary32 accumulator, M = 128.  across: operand B's contiguous
 // dimension is N and not the summed one.
 __device__ __forceinline__ uint32_t product_desc(bool bf16, uint32_t n, bool across)
@@ -159,17 +157,29 @@ __device__ __forceinline__ uint32_t elect_lane()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void product_ss(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+template <bool ADD_ALWAYS = false>
+__device__ __forceinline__ void product_ss(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add = true)
 {
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(one) : "memory");
+    if (ADD_ALWAYS)
+        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 q, %4, 0;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                     "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 1;\n\t}"
+                     ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(one), "n"(kOperandHigh) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 q, %4, 0;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 da, {%1, %5};\n\t"
+                     "mov.b64 db, {%2, %5};\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(one), "n"(kOperandHigh), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void product_ts(uint32_t one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+template <bool ADD_ALWAYS = false>
+__device__ __forceinline__ void product_ts(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add = true)
 {
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(one) : "memory");
+    if (ADD_ALWAYS)
+        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 db;\n\tsetp.ne.b32 q, %4, 0;\n\tmov.b64 db, {%2, %5};\n\t"
+                     "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, 1;\n\t}"
+                     ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(one), "n"(kOperandHigh) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\tsetp.ne.b32 q, %4, 0;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 db, {%2, %5};\n\t"
+                     "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(one), "n"(kOperandHigh), "r"((uint32_t)add) : "memory");
 }
 // The barrier is arrived at when every product issued so far by this lane is done.
 __device__ __forceinline__ void products_done(uint32_t one, uint64_t *bar)
