@@ -4,10 +4,11 @@
 // with c = scale log2(e), l = sum of P and m a reference of the row that follows its running maximum.
 //
 // A persistent CTA (one per SM) takes items of 256 queries of one head and walks the keys in blocks of 128:
-//   warps 0-3, 4-7   softmax of the item's first / second 128 queries; a thread owns one row
-//   warp 8           issues the products; warp 9 issues the copies (10 and 11 only complete their warpgroup)
-// The warpgroups share out the CTA's 384 x 168 registers: 232 for a softmax thread, which holds a row of 128 scores, 40
-// for the others.
+//   warps 0-7, 8-15  softmax of the item's first / second 128 queries; a thread owns 64 of the 128 columns of a row, and the
+//                    two warps of a row exchange its maximum.  (A row to a thread, with half the warps, left the
+//                    exponentials waiting for one another: 197 tokens took 39 us, see below for now.)
+//   warp 16          issues the products; warp 17 issues the copies (18 and 19 only complete their warpgroup)
+// The warpgroups share out the CTA's 640 x 96 registers: 104 for a softmax thread, 64 for the others.
 // Tensor memory holds S and O of both halves (S: 2 x 128 columns, O: 2 x DP); P overwrites its S as 16-bit operands of
 // P v, so scores and probabilities never leave the SM.  The halves alternate: while one is in softmax, the tensor cores
 // work for the other.  Products of one thread execute in the order they are issued, which is what makes
@@ -22,9 +23,10 @@
 
 namespace daf {
 
-constexpr int kFwdThreads = 384;
+constexpr int kFwdThreads = 640;
 constexpr int kFwdRows = 256, kBlock = 128;
 constexpr float kLag = 8.0f;
+constexpr int kTurnPolls = 64;                   // about 2000 cycles
 constexpr float kNoMax = -1e30f;                 // reference of a row that has seen no key yet
 
 struct AttnForwardArgs {
@@ -36,17 +38,19 @@ struct AttnForwardArgs {
 };
 
 template <int DP> struct FwdSmem {
-    static constexpr int kStages = DP == 128 ? 4 : 8;
+    static constexpr int kStages = DP == 128 ? 4 : 6, kQueries = DP == 128 ? 1 : 2;   // key / value tiles, items' queries
     static constexpr uint32_t kTile = 128u * DP * 2u;            // one tile of 128 rows
-    static constexpr uint32_t kOut = 4096u;                       // two pieces of 32 x 32 outputs for each softmax warp
-    static constexpr uint32_t kBytes = (2u + kStages) * kTile + 8u * kOut + 1024u;
+    static constexpr uint32_t kOut = 2048u;                       // a piece of 32 x 32 outputs for each softmax warp
+    static constexpr uint32_t kBars = 1024u;                      // barriers and such, ahead of everything
+    static constexpr uint32_t kKeys = 2u * kQueries * kTile;          // where they begin
+    static constexpr uint32_t kBytes = kBars + kKeys + kStages * kTile + 16u * kOut + 16u * 32u * 4u;
 };
 
 // The item's head, batch entry and first query, and its number of key blocks per half.
 struct FwdItem {
     uint32_t b, h, m0, n;
     int blocks[2], both;
-    __device__ __forceinline__ FwdItem(const AttnForwardArgs &p, uint32_t item)
+    __device__ __forceinline__ void set(const AttnForwardArgs &p, uint32_t item)
     {
         const AttnArgs &a = p.a;
         uint32_t bh, qt;
@@ -74,6 +78,16 @@ struct FwdItem {
     }
 };
 
+// The first item from `item` on (in this CTA's steps) that has key blocks.
+__device__ __forceinline__ bool next_item(const AttnForwardArgs &p, uint32_t &item, FwdItem &it)
+{
+    for (; item < p.items; item += gridDim.x) {
+        it.set(p, item);
+        if (it.both) return true;
+    }
+    return false;
+}
+
 // Zeroes rows [from, to) of a tile in shared memory (128-byte rows of each 64-element box, `box` bytes apart).
 template <int DP> __device__ __forceinline__ void zero_rows(unsigned char *tile, uint32_t box, uint32_t from, uint32_t to, uint32_t lane)
 {
@@ -89,16 +103,30 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     using Smem = FwdSmem<DP>;
     constexpr bool BF16 = __is_same(T, __nv_bfloat16);
     constexpr int STAGES = Smem::kStages;
-    extern __shared__ unsigned char s_raw[];
-    __shared__ __align__(8) uint64_t q_full, q_empty, tail, drain, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2], o_done[2];
-    __shared__ uint32_t s_tmem, s_abort;
-    unsigned char *const smem = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
+    // tiles need 1024-byte boundaries; with nothing declared statically the dynamic part starts on one
+    extern __shared__ __align__(1024) unsigned char s_raw[];
+    struct Bars {
+        uint64_t kv_full[8], kv_empty[8], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], tail, drain;
+        uint32_t tmem, abort, busy[16];
+    };
+    static_assert(sizeof(Bars) <= Smem::kBars && STAGES <= 8, "barriers fit their places");
+    Bars &bars = *reinterpret_cast<Bars *>(s_raw);
+    uint64_t *const kv_full = bars.kv_full, *const kv_empty = bars.kv_empty, *const s_full = bars.s_full, *const p_ready = bars.p_ready,
+             *const o_done = bars.o_done, *const q_full = bars.q_full, *const q_empty = bars.q_empty;
+    uint64_t &tail = bars.tail, &drain = bars.drain;
+    uint32_t &s_tmem = bars.tmem, &s_abort = bars.abort;
+    if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
+        if (threadIdx.x == 0) p.header->status = DAF_ERR_UNSUPPORTED;
+        return;
+    }
+    unsigned char *const smem = s_raw + Smem::kBars;
+    // [warp][lane]: what the two warps of a row tell each other
+    float (*const s_told)[32] = reinterpret_cast<float (*)[32]>(smem + Smem::kKeys + STAGES * Smem::kTile + 16u * Smem::kOut);
     const AttnArgs &a = p.a;
     const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+    if (threadIdx.x < 16) bars.busy[threadIdx.x] = 0u;
     if (threadIdx.x == 0) {
         s_abort = 0u;
-        bar_init(&q_full, 1);
-        bar_init(&q_empty, 1);
         bar_init(&tail, 1);
         bar_init(&drain, 1);
         for (int i = 0; i < STAGES; i++) {
@@ -106,8 +134,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
             bar_init(&kv_empty[i], 1);
         }
         for (int w = 0; w < 2; w++) {
+            bar_init(&q_full[w], 1);
+            bar_init(&q_empty[w], 1);
             bar_init(&s_full[w], 1);
-            bar_init(&p_ready[w], 4);
+            bar_init(&p_ready[w], 8);
             bar_init(&o_done[w], 1);
         }
         fence_async();
@@ -120,59 +150,79 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     const uint32_t tmem = s_tmem;
     volatile uint32_t *const stop = &s_abort;
 
-    if (warp < 8) {                                                // ---- softmax
-        take_registers<232>();
-        const uint32_t w = warp >> 2, quarter = (warp & 3u) << 21;  // lane 32 (warp % 4) in the address's upper half
-        const uint32_t ts = tmem + w * 128u + quarter, to = tmem + 256u + w * DP + quarter;
-        unsigned char *const s_out = smem + (2 + STAGES) * Smem::kTile + warp * Smem::kOut;
-        uint32_t pieces = 0, s_ph = 0, pv = 0;                                  // pv: products into O that were handed over, ever
+    if (warp < 16) {                                               // ---- softmax
+        take_registers<104>();
+        const uint32_t w = warp >> 3, part = warp >> 2 & 1u, quarter = (warp & 3u) << 21;   // lane 32 (warp % 4) in the address's upper half
+        const uint32_t ts = tmem + w * 128u + part * 64u + quarter, to = tmem + 256u + w * DP + part * (DP / 2) + quarter;
+        volatile uint32_t *const busy = bars.busy;
+        const uint32_t meeting = 1u + w * 4u + (warp & 3u);         // barrier of the two warps that share 32 rows
+        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(meeting) : "memory"); };
+        unsigned char *const s_out = smem + Smem::kKeys + STAGES * Smem::kTile + warp * Smem::kOut;
+        uint32_t s_ph = 0, pv = 0;                                  // pv: products into O that were handed over, ever
         const float c = a.scale_log2;
         for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
-            const FwdItem it(p, item);
+            FwdItem it;
+            it.set(p, item);
             const uint32_t first = it.m0 + 128u * w, row = first + (warp & 3u) * 32u + lane;
             if (first >= a.Sq) continue;
+            const int blocks = w ? it.blocks[1] : it.blocks[0];
             const int limit = row < a.Sq ? attn_limit(a, it.n, (int)row) : (int)it.n;
             const bool idle = first + (warp & 3u) * 32u >= a.Sq;   // none of the warp's rows exist
             float m = kNoMax, l = 0.0f;
             bool ok = true;
-            for (int j = 0; j < it.blocks[w]; j++) {
+            for (int j = 0; j < blocks; j++) {
                 if (!(ok = bar_wait(&s_full[w], s_ph, stop))) break;
                 s_ph ^= 1u;
                 if (!idle) {
                     tmem_after_sync();
-                    const int valid = (int)it.n - j * kBlock;       // columns that hold scores, at least
-                    float x[128];
+                    const int valid = (int)it.n - j * kBlock - 64 * (int)part;   // columns that hold scores, at least
+                    const int left = limit - j * kBlock - 64 * (int)part;
+                    const bool masked = __any_sync(0xffffffffu, left < 64);
+                    // 32 scores at a time, once for the maximum and once more for the exponentials: reading tensor memory
+                    // twice costs less than 64 registers
+                    const auto scores = [&](int i, float (&x)[32]) {
+                        tmem_load32(ts + 32 * i, x);
+                        tmem_wait_loads();
+                        if (a.scale < 0.0f) {                       // c is its absolute value
 #pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (32 * i < valid) tmem_load32(ts + 32 * i, x + 32 * i);
-                    tmem_wait_loads();
-                    if (a.scale < 0.0f) {                           // c is its absolute value
+                            for (int k = 0; k < 32; k++) x[k] = -x[k];
+                        }
+                        if (masked) {
 #pragma unroll
-                        for (int i = 0; i < 128; i++) x[i] = -x[i];
+                            for (int k = 0; k < 32; k++)
+                                if (32 * i + k >= left) x[k] = -INFINITY;
+                        }
+                    };
+                    float row_max = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        if (32 * i >= valid) continue;
+                        float x[32];
+                        scores(i, x);
+                        float top[4] = {row_max, x[1], x[2], x[3]};
+                        top[0] = fmaxf(top[0], x[0]);
+#pragma unroll
+                        for (int k = 4; k < 28; k += 8)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) top[e] = fmax3(top[e], x[k + e], x[k + 4 + e]);
+#pragma unroll
+                        for (int e = 0; e < 4; e++) top[e] = fmaxf(top[e], x[28 + e]);
+                        row_max = fmaxf(fmax3(top[0], top[1], top[2]), top[3]);
                     }
-                    const int left = limit - j * kBlock;
-                    if (__any_sync(0xffffffffu, left < kBlock)) {
-#pragma unroll
-                        for (int i = 0; i < 128; i++)
-                            if (i >= left) x[i] = -INFINITY;
-                    }
-                    float top[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                    for (int i = 4; i < 128; i += 8)
-#pragma unroll
-                        for (int k = 0; k < 4; k++)
-                            top[k] = i + 4 + k < 128 ? fmax3(top[k], x[i + k], x[i + 4 + k]) : fmaxf(top[k], x[i + k]);
-                    const float block_max = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    s_told[warp][lane] = row_max;
+                    meet();
+                    row_max = fmaxf(row_max, s_told[warp ^ 4u][lane]);
+                    const float block_max = c * row_max;
                     if (j == 0) {
                         m = fmaxf(block_max, kNoMax);
-                    } else if (__any_sync(0xffffffffu, block_max > m + kLag)) {
+                    } else if (__any_sync(0xffffffffu, block_max > m + kLag)) {   // the same in both warps
                         const float next = fmaxf(m, block_max), fade = exp2_fast(m - next);
                         m = next;
                         l *= fade;
                         if (!(ok = bar_wait(&o_done[w], (pv - 1u) & 1u, stop))) break;
                         tmem_after_sync();
 #pragma unroll
-                        for (int i = 0; i < DP / 16; i++) {
+                        for (int i = 0; i < DP / 32; i++) {
                             float o[16];
                             tmem_load16(to + 16 * i, o);
                             tmem_wait_loads();
@@ -181,16 +231,25 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                             tmem_store16(to + 16 * i, reinterpret_cast<const uint32_t *>(o));
                         }
                     }
+                    // The halves' exponentials take turns: side by side they would both end late and leave the tensor cores
+                    // idle meanwhile.  Only an order that pays, so the wait for the other half's two warps on this
+                    // scheduler is short and nothing depends on it.  Heads of up to 64 alone (4 x 4096 x 16 heads of 64:
+                    // 441 -> 399 us): the products of wider ones take as long as the exponentials (8192 x 16 heads of
+                    // 128: 514 us without, 524 with turns).
+                    for (int i = 0; DP == 64 && i < kTurnPolls && (busy[warp ^ 8u] | busy[warp ^ 12u]); i++) {}
+                    if (DP == 64 && lane == 0) busy[warp] = 1u;
                     const uint64_t c2 = pair(c, c), m2 = pair(-m, -m);
                     uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
+                    for (int i = 0; i < 2; i++) {
                         if (32 * i < valid) {
+                            float x[32];
+                            scores(i, x);
                             uint32_t r[16];
 #pragma unroll
                             for (int k = 0; k < 16; k++) {
                                 float u, v;
-                                unpair(fma2(pair(x[32 * i + 2 * k], x[32 * i + 2 * k + 1]), c2, m2), u, v);
+                                unpair(fma2(pair(x[2 * k], x[2 * k + 1]), c2, m2), u, v);
                                 u = exp2_fast(u);
                                 v = exp2_fast(v);
                                 sum[k & 1] = add2(sum[k & 1], pair(u, v));
@@ -199,6 +258,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                             tmem_store16(ts + 16 * i, r);
                         }
                     }
+                    if (DP == 64 && lane == 0) busy[warp] = 0u;
                     float u, v;
                     unpair(add2(sum[0], sum[1]), u, v);
                     l += u + v;
@@ -210,24 +270,30 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 pv++;
             }
             if (!ok) break;
-            float by = 0.0f;
-            if (it.blocks[w] > 0) {
+            if (!idle) {
+                meet();                                             // both have read the last maximum
+                s_told[warp][lane] = l;
+                meet();
+                l += s_told[warp ^ 4u][lane];
+                meet();                                             // and the sum, before the next item's maximum
+            }
+            const float by = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
+            if (blocks > 0) {
                 if (!bar_wait(&o_done[w], (pv - 1u) & 1u, stop)) break;
                 tmem_after_sync();
-                by = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
             }
             if (idle) continue;
-            if (row < a.Sq) a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+            if (part == 0 && row < a.Sq) a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 #pragma unroll
-            for (int i = 0; i < DP / 32; i++) {
-                if (32u * i >= a.D) continue;
+            for (int i = 0; i < DP / 64; i++) {
+                const uint32_t from = part * (DP / 2) + 32u * i;
+                if (from >= a.D) continue;
                 float o[32];
-                if (it.blocks[w] > 0) {
+                if (blocks > 0) {
                     tmem_load32(to + 32 * i, o);
                     tmem_wait_loads();
                 }
-                unsigned char *const piece = s_out + (pieces++ & 1u) * 2048;
-                if (lane == 0) stores_read<1>();                   // the store before last is out of this half
+                if (lane == 0) stores_read<0>();
                 __syncwarp();
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
@@ -238,36 +304,39 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                         v.z = round2<T>(o[8 * k + 4] * by, o[8 * k + 5] * by);
                         v.w = round2<T>(o[8 * k + 6] * by, o[8 * k + 7] * by);
                     }
-                    stage_piece(piece, lane, k, v);
+                    stage_piece(s_out, lane, k, v);
                 }
                 fence_async();
                 __syncwarp();
-                if (lane == 0) tma_store(&p.out, piece, 32 * i, it.h, first + (warp & 3u) * 32u, it.b);
+                if (lane == 0) tma_store(&p.out, s_out, from, it.h, first + (warp & 3u) * 32u, it.b);
             }
             tmem_before_sync();
         }
         if (lane == 0) stores_done();
     } else {
-        leave_registers<40>();
-        if (warp == 9) {                                               // ---- copies
-            uint32_t st = 0, ph = 1, q_ph = 1, tail_ph = 0;            // a fresh barrier's "previous" phase counts as complete
-            for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
-                const FwdItem it(p, item);
-                if (it.both == 0) continue;
-                if (!bar_wait(&q_empty, q_ph, stop)) break;
-                q_ph ^= 1u;
+        leave_registers<64>();
+        if (warp == 17) {                                               // ---- copies
+            uint32_t st = 0, ph = 1, q = 0, q_ph = 1, tail_ph = 0;   // a fresh barrier's "previous" phase counts as complete
+            FwdItem it;
+            for (uint32_t item = blockIdx.x; next_item(p, item, it); item += gridDim.x) {
+                if (!bar_wait(&q_empty[q], q_ph, stop)) break;
                 if (lane == 0) {
-                    bar_expect(&q_full, ((it.blocks[0] > 0) + (it.blocks[1] > 0)) * Smem::kTile);
+                    bar_expect(&q_full[q], ((it.blocks[0] > 0) + (it.blocks[1] > 0)) * Smem::kTile);
+#pragma unroll
                     for (int w = 0; w < 2; w++)
                         if (it.blocks[w] > 0)
                             for (int x = 0; x < DP / 64; x++)
-                                tma_load(smem_u32(smem) + w * Smem::kTile + x * 16384, &p.q, &q_full, 64 * x, it.h, it.m0 + 128 * w, it.b);
+                                tma_load(smem_u32(smem) + (2u * q + w) * Smem::kTile + x * 16384, &p.q, &q_full[q], 64 * x, it.h, it.m0 + 128 * w, it.b);
+                }
+                if (++q == Smem::kQueries) {
+                    q = 0;
+                    q_ph ^= 1u;
                 }
                 for (int i = 0; i < 2 * it.both; i++) {                // K0 V0 K1 V1 ...
                     const int j = i >> 1;
                     const bool is_v = i & 1;
                     if (!bar_wait(&kv_empty[st], ph, stop)) break;
-                    unsigned char *const dst = smem + (2 + st) * Smem::kTile;
+                    unsigned char *const dst = smem + Smem::kKeys + st * Smem::kTile;
                     // P is zero in a masked column, but 0 * NaN is not: rows of v behind the sequence's end that the
                     // last product's steps of 16 keys still touch are cleared
                     const uint32_t valid = it.n - (uint32_t)j * kBlock, end = (valid + 15u) & ~15u;
@@ -297,22 +366,27 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 const uint64_t until = now_ns() + 1000000000ull;
                 while (now_ns() < until) __nanosleep(1000);
             }
-        } else if (warp == 8) {                                        // ---- products
+        } else if (warp == 16) {                                        // ---- products
             const uint32_t one = elect_lane();
-            uint32_t st = 0, ph = 0, q_ph = 0, p_ph[2] = {0, 0};
-            const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + 2u * Smem::kTile;
+            uint32_t st = 0, ph = 0, q_at = 0, q_ph = 0, p_ph[2] = {0, 0};
+            const uint32_t q_smem = smem_u32(smem), kv_smem = q_smem + Smem::kKeys;
             const uint32_t steps = (a.D + 15u) / 16u;              // of the first product
             const uint32_t pv_desc = product_desc(BF16, steps * 16u, true);
-            for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
-                const FwdItem it(p, item);
-                if (it.both == 0) continue;
-                if (!bar_wait(&q_full, q_ph, stop)) break;
-                q_ph ^= 1u;
+            uint32_t item = blockIdx.x;
+            FwdItem it, after;
+            bool more_items = next_item(p, item, it);
+            while (more_items) {
+                const uint32_t qb = q_at;
+                if (!bar_wait(&q_full[qb], q_ph, stop)) break;
+                if (++q_at == Smem::kQueries) {
+                    q_at = 0;
+                    q_ph ^= 1u;
+                }
                 // S of half w for the key block in stage `at`
                 auto scores = [&](int w, int j, uint32_t at) {
                     const uint32_t valid = it.n - (uint32_t)j * kBlock, cols = valid < (uint32_t)kBlock ? (valid + 15u) & ~15u : kBlock;
                     const uint32_t desc = product_desc(BF16, cols, false);
-                    const uint32_t q = operand_low(q_smem + w * Smem::kTile, 16), k = operand_low(kv_smem + at * Smem::kTile, 16);
+                    const uint32_t q = operand_low(q_smem + (2u * qb + w) * Smem::kTile, 16), k = operand_low(kv_smem + at * Smem::kTile, 16);
                     product_ss(one, tmem + w * 128u, q, k, desc, false);
 #pragma unroll
                     for (uint32_t s = 1; s < DP / 16; s++) {
@@ -333,8 +407,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 for (int w = 0; w < 2; w++)
                     if (it.blocks[w] > 0) scores(w, 0, st);
                 products_done(one, &kv_empty[st]);
-                if (it.both == 1) products_done(one, &q_empty);
+                if (it.both == 1) products_done(one, &q_empty[qb]);
                 next();
+                item += gridDim.x;                                 // decoded while softmax has the first block
+                more_items = next_item(p, item, after);
                 for (int j = 0; j < it.both; j++) {
                     const uint32_t v_st = st;
                     if (!bar_wait(&kv_full[st], ph, stop)) break;
@@ -353,18 +429,19 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                         product_ts(one, tmem + 256u + w * DP, tmem + w * 128u, v, pv_desc, j > 0);
 #pragma unroll
                         for (uint32_t s = 1; s < kBlock / 16; s++)                   // 16 keys: 2 KiB of v, 8 columns of P
-                            if (s < pv_steps) product_ts<true>(one, tmem + 256u + w * DP, tmem + w * 128u + s * 8u, v + s * 128u, pv_desc);
+                            if (s < pv_steps) product_ts<true>(one, tmem + 256u + w * DP, tmem + w * 128u + (s >> 2) * 64u + (s & 3u) * 8u, v + s * 128u, pv_desc);
                         products_done(one, &o_done[w]);
                         if (j + 1 < it.blocks[w]) scores(w, j + 1, st);
                     }
                     products_done(one, &kv_empty[v_st]);
                     if (more) {
                         products_done(one, &kv_empty[st]);
-                        if (j + 2 == it.both) products_done(one, &q_empty);
+                        if (j + 2 == it.both) products_done(one, &q_empty[qb]);
                         next();
                     }
                 }
                 if (*stop) break;
+                it = after;
             }
             products_done(one, &drain);
             bar_wait(&drain, 0, stop);
