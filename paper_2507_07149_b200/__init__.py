@@ -701,7 +701,7 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
         lse = _fresh(plan.like_lse)
     else:
         _check_lse("attention", lse, plan.lse_shape, q)
-    ws = _header(index, _raw_stream(index, stream))
+    ws = _header(index, _raw_stream(index, stream)) if plan.ws <= 256 else _fresh(plan.like_ws)
     status = _call(lib().daf_attention, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), out.data_ptr(), lse.data_ptr(),
                    ws.data_ptr(), plan.ws)
     _check(status, "daf_attention")

@@ -63,6 +63,9 @@ bool attn_store_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B
 
 static uint32_t padded_rows(uint32_t rows) { return (rows + kAttnRowPad - 1u) / kAttnRowPad * kAttnRowPad; }
 
+// -lse and -delta of every row
+static uint64_t rows_bytes(const daf_attention_params *p) { return 2ull * p->batch * p->heads * padded_rows(p->queries) * sizeof(float); }
+
 static AttnArgs args_of(const daf_attention_params *p)
 {
     AttnArgs a = {};
@@ -86,7 +89,8 @@ using namespace daf;
 
 extern "C" uint64_t daf_attention_workspace(const daf_attention_params *params)
 {
-    return check_attention(params) == DAF_OK ? sizeof(WorkspaceHeader) : 0u;
+    if (check_attention(params) != DAF_OK) return 0;
+    return sizeof(WorkspaceHeader) + (params->dtype == DAF_F32 ? attn_planes_workspace(args_of(params), false) : 0u);
 }
 
 extern "C" daf_status daf_attention(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
@@ -115,14 +119,14 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
     a.lengths = d_key_lengths;
     WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    return p.dtype == DAF_F32 ? attn_forward_f32(a, header, s)
+    return p.dtype == DAF_F32 ? attn_forward_planes(a, reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader), header, s)
            : p.dtype == DAF_F16 ? attn_forward_tc<__half>(a, header, s) : attn_forward_tc<__nv_bfloat16>(a, header, s);
 }
 
 extern "C" uint64_t daf_attention_grad_workspace(const daf_attention_params *params)
 {
     if (check_attention(params) != DAF_OK) return 0;
-    return 2ull * params->batch * params->heads * padded_rows(params->queries) * sizeof(float) + sizeof(WorkspaceHeader);
+    return sizeof(WorkspaceHeader) + rows_bytes(params) + (params->dtype == DAF_F32 ? attn_planes_workspace(args_of(params), true) : 0u);
 }
 
 extern "C" daf_status daf_attention_grad(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
@@ -174,6 +178,7 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
         return st != DAF_OK ? st : attn_zero(p.dtype, a.dv, a.B, a.Sk, a.Hkv, a.D, s);
     }
     if (p.keys == 0) return attn_zero(p.dtype, a.dq, a.B, a.Sq, a.H, a.D, s);
-    return p.dtype == DAF_F32 ? attn_backward_f32(a, s)
+    char *const planes = reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader) + rows_bytes(params);
+    return p.dtype == DAF_F32 ? (p.head_dim <= 64u ? attn_backward_planes(a, planes, header, s) : attn_backward_f32(a, s))
            : p.dtype == DAF_F16 ? attn_backward_tc<__half>(a, header, s) : attn_backward_tc<__nv_bfloat16>(a, header, s);
 }

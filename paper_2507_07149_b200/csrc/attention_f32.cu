@@ -119,72 +119,6 @@ __device__ __forceinline__ void store_tile(const AttnTensor &t, uint32_t b, uint
     }
 }
 
-template <int DP>
-__global__ void __launch_bounds__(kGenThreads) attention_f32_kernel(const __grid_constant__ AttnArgs a, WorkspaceHeader *header)
-{
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) header->status = 0u;
-    extern __shared__ __align__(16) float smem[];
-    float *const Q = smem, *const K = Q + kTile * (DP + 4), *const V = K + kTile * (DP + 4), *const P = V + kTile * (DP + 4);
-    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    const uint32_t m0 = blockIdx.x * kTile, h = blockIdx.y % a.H, b = blockIdx.y / a.H;
-    const uint32_t n = attn_length(a, b);
-    load_tile<DP>(Q, a.q, b, h, m0, a.Sq, a.D);
-    float m[4], l[4], o[4][DP / 16] = {};
-    int limit[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        m[i] = -INFINITY;
-        l[i] = 0.0f;
-        limit[i] = attn_limit(a, n, (int)m0 + 4 * ty + i);
-    }
-    const int end = attn_limit(a, n, (int)(m0 + kTile < a.Sq ? m0 + kTile : a.Sq) - 1);
-    for (int n0 = 0; n0 < end; n0 += kTile) {
-        __syncthreads();
-        load_tile<DP>(K, a.k, b, h / a.group, n0, n, a.D);
-        load_tile<DP>(V, a.v, b, h / a.group, n0, n, a.D);
-        __syncthreads();
-        float s[4][4];
-        product_nt<DP>(Q, K, ty, tx, s);
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                s[i][j] = n0 + tx + 16 * j < limit[i] ? s[i][j] * a.scale_log2 : -INFINITY;
-                top = fmaxf(top, s[i][j]);
-            }
-#pragma unroll
-            for (int d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            const float next = fmaxf(m[i], top), base = next == -INFINITY ? 0.0f : next;
-            const float fade = exp2f(m[i] - base);
-            m[i] = next;
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float p = exp2f(s[i][j] - base);
-                sum += p;
-                P[(4 * ty + i) * kScorePitch + tx + 16 * j] = p;
-            }
-            l[i] = __fmaf_rn(l[i], fade, sum);
-#pragma unroll
-            for (int c = 0; c < DP / 16; c++) o[i][c] *= fade;
-        }
-        __syncwarp();                                              // a warp's rows of P are read by that warp alone
-        product_nn<DP>(P, V, ty, tx, o);
-    }
-    float by[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-#pragma unroll
-        for (int d = 8; d; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
-        by[i] = l[i] > 0.0f ? __fdiv_rn(1.0f, l[i]) : 0.0f;
-        const uint32_t r = m0 + 4 * ty + i;
-        if (tx == 0 && r < a.Sq)
-            a.lse[((uint64_t)b * a.H + h) * a.Sq + r] = l[i] > 0.0f ? (m[i] + log2f(l[i])) * 0.69314718055994531f : -INFINITY;
-    }
-    store_tile<DP>(a.out, b, h, m0, a.Sq, a.D, ty, tx, o, by);
-}
-
 // What the backward kernels need of each row, D / 8 lanes (rounded up to a power of two) per row, 128 rows of a head per
 // CTA: -lse in units of log2, -inf for rows that see nothing and for the padding (their probabilities then come out as
 // exp2(-inf) = 0), and -delta = -sum(grad_out * out).
@@ -325,12 +259,7 @@ template <int DP> static daf_status backward(const AttnArgs &a, cudaStream_t s)
     return st != DAF_OK ? st : launch_f32(&attention_dkv_f32_kernel<DP>, a.Sk, a.Hkv, a.B, tile_bytes(DP, 4, 2), a, s);
 }
 
-daf_status attn_forward_f32(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s)
-{
-    return a.D <= 64u ? launch_f32(&attention_f32_kernel<64>, a.Sq, a.H, a.B, tile_bytes(64, 3, 1), a, s, header)
-                      : launch_f32(&attention_f32_kernel<128>, a.Sq, a.H, a.B, tile_bytes(128, 3, 1), a, s, header);
-}
-daf_status attn_backward_f32(const AttnArgs &a, cudaStream_t s) { return a.D <= 64u ? backward<64>(a, s) : backward<128>(a, s); }
+daf_status attn_backward_f32(const AttnArgs &a, cudaStream_t s) { return backward<128>(a, s); }
 
 daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s)
 {

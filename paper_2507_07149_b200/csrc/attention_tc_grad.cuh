@@ -52,7 +52,7 @@ __device__ __forceinline__ uint32_t grad_item(uint32_t i)
     return i * gridDim.x + (i & 1u ? gridDim.x - 1u - blockIdx.x : blockIdx.x);
 }
 
-template <bool DKV> struct GradItem {
+template <bool DKV, uint32_t WALK = kWalk> struct GradItem {
     uint32_t b, h, first, n;                     // h: key head (DKV) or query head
     uint32_t start, per_head, blocks;            // the walk: `per_head` blocks from `start` on, for each head
     __device__ __forceinline__ void set(const AttnGradArgs &p, uint32_t item)
@@ -75,20 +75,20 @@ template <bool DKV> struct GradItem {
         per_head = 0;
         if (DKV) {
             const int from = a.causal ? (int)(first + a.Sq) - (int)a.Sk : 0;   // the first query that sees a key of the tile
-            if (from > 0) start = (uint32_t)from / kWalk * kWalk;
-            if (first < n && start < a.Sq) per_head = (a.Sq - start + kWalk - 1u) / kWalk;
+            if (from > 0) start = (uint32_t)from / WALK * WALK;
+            if (first < n && start < a.Sq) per_head = (a.Sq - start + WALK - 1u) / WALK;
             blocks = per_head * a.group;
         } else {
             const uint32_t last = (first + kHeld < a.Sq ? first + kHeld : a.Sq) - 1u;
             const int end = attn_limit(a, n, (int)last);
-            per_head = blocks = end > 0 ? ((uint32_t)end + kWalk - 1u) / kWalk : 0u;
+            per_head = blocks = end > 0 ? ((uint32_t)end + WALK - 1u) / WALK : 0u;
         }
     }
 };
 
 // Walks the blocks of a CTA's items one after another: block `i` of the item, at row `row` of head `head`.
-template <bool DKV> struct GradCursor {
-    GradItem<DKV> it;
+template <bool DKV, uint32_t WALK = kWalk> struct GradCursor {
+    GradItem<DKV, WALK> it;
     uint32_t turn, i, in_head, row, head;
     bool more;
     __device__ __forceinline__ void open(const AttnGradArgs &p)
@@ -116,7 +116,7 @@ template <bool DKV> struct GradCursor {
     __device__ __forceinline__ uint32_t cols(const AttnGradArgs &p) const
     {
         const uint32_t left = (DKV ? p.a.Sq : it.n) - row;
-        return left < kWalk ? left : kWalk;
+        return left < WALK ? left : WALK;
     }
     __device__ __forceinline__ void step(const AttnGradArgs &p)
     {
@@ -125,7 +125,7 @@ template <bool DKV> struct GradCursor {
             enter(p);
             return;
         }
-        row += kWalk;
+        row += WALK;
         if (DKV && ++in_head == it.per_head) {
             in_head = 0;
             row = it.start;

@@ -148,6 +148,12 @@ __device__ __forceinline__ uint32_t product_desc(bool bf16, uint32_t n, bool acr
     const uint32_t t = bf16 ? 1u : 0u;
     return 1u << 4 | t << 7 | t << 10 | (across ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
 }
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(at) : "memory");
+}
+
 // One lane of the (whole, converged) warp.  The products are issued by that lane under a predicate while the warp computes
 // their operands together: those then stay in uniform registers, which the instructions take; inside a branch of one lane
 // every operand would be moved there for each product.
