@@ -179,6 +179,6 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     }
     if (p.keys == 0) return attn_zero(p.dtype, a.dq, a.B, a.Sq, a.H, a.D, s);
     char *const planes = reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader) + rows_bytes(params);
-    return p.dtype == DAF_F32 ? (p.head_dim <= 64u ? attn_backward_planes(a, planes, header, s) : attn_backward_f32(a, s))
+    return p.dtype == DAF_F32 ? attn_backward_planes(a, planes, header, s)
            : p.dtype == DAF_F16 ? attn_backward_tc<__half>(a, header, s) : attn_backward_tc<__nv_bfloat16>(a, header, s);
 }

@@ -49,11 +49,10 @@ __device__ __forceinline__ int attn_limit(const AttnArgs &a, uint32_t n, int i)
     return c < (int)n ? c : (int)n;
 }
 
-// binary32 inputs in three bfloat16 planes (at `planes_at`, attn_planes_workspace bytes; 0: not for this call)
+// binary32 inputs in three bfloat16 planes (at `planes_at`, attn_planes_workspace bytes)
 uint64_t attn_planes_workspace(const AttnArgs &a, bool backward);
 daf_status attn_forward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_backward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s);
-daf_status attn_backward_f32(const AttnArgs &a, cudaStream_t s);
 daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_zero(uint32_t dtype, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, cudaStream_t s);
 template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);

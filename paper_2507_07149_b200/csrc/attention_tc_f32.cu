@@ -1,4 +1,4 @@
-// Attention for binary32 inputs on the tensor cores: forward, and the backward pass for heads of up to 64.
+// Attention for binary32 inputs on the tensor cores, forward and backward.
 //
 // A binary32 number is the sum of three bfloat16 numbers, x = h + m + l (8 bits each, rounded to nearest one after the
 // other: exact), and a product of two is h h' + (h m' + m h') + (m m' + h l' + l h') up to 2^-24: six bfloat16 products,
@@ -6,13 +6,13 @@
 // are split in registers on their way into tensor memory.  The accumulator of the tensor cores truncates, so it only ever
 // holds one block of the walk: the running sums stay in registers, added there to nearest.
 //
-// Six products at the rate of bfloat16 leave a sixth of 1.6 PFLOP/s, ten times what binary32 multiply-adds reach
-// (attention_f32.cu).  The backward pass holds two tiles in three planes, which for heads above 64 is more than shared
-// memory has: those stay with the multiply-adds.
+// Six products at the rate of bfloat16 leave a sixth of 1.6 PFLOP/s; a loop of binary32 multiply-adds, four by four scores
+// to a thread, reached 25 TFLOP/s, and three TF32 products by mma.sync 30, with 22 bits of each factor.
 //
 //   FWD   holds 128 queries, walks 64 keys a block:     T1 = q k^T;                 sum += P v
 //   DQ    holds 128 queries, walks 64 keys a block:     T1 = q k^T, T2 = g v^T;     sum += dS k
 //   DKV   holds 128 keys, walks 32 queries a block:     T1 = k q^T, T2 = v g^T;     dv += P g, dk += dS q
+// Backward, heads above 64 leave room for blocks of 16 only: the planes of the two held tiles take 192 KiB.
 //
 // A persistent CTA (one per SM): warps 0-7 softmax (two threads to a row), warp 8 the products, warp 9 the copies.  Tensor
 // memory: two blocks of T, the planes of P and dS, one block's sums.
@@ -24,15 +24,15 @@ constexpr int kPlaneThreads = 384;               // 8 warps x 232 registers, 4 (
 enum { kFwd = 0, kDq = 1, kDkv = 2 };
 
 template <int MODE, int DP> struct PlaneShape {
-    static constexpr uint32_t WALK = MODE == kDkv ? 32 : 64;
+    static constexpr uint32_t WALK = MODE != kFwd && DP == 128 ? 16 : MODE == kDkv ? 32 : 64;
     static constexpr uint32_t kHeldTiles = MODE == kFwd ? 1 : 2;
     static constexpr uint32_t kX = 3u * kHeld * DP * 2u, kY = 3u * WALK * DP * 2u;   // a tensor's tile, three planes
-    static constexpr uint32_t kSlots = MODE == kFwd ? (DP == 128 ? 2 : 6) : MODE == kDq ? 4 : 8;
+    static constexpr uint32_t kSlots = DP == 128 ? 2 : MODE == kFwd ? 6 : MODE == kDq ? 4 : 8;
     static constexpr uint32_t kStats = MODE == kDkv ? 2u * WALK * 4u : 0u;           // for each pair of slots
     static constexpr uint32_t kT = WALK * kHeldTiles;              // tensor memory: columns of a block of T,
     static constexpr uint32_t kW = 3u * WALK / 2u * (MODE == kDkv ? 2 : 1);          // of the planes,
     static constexpr uint32_t kSum = MODE == kDkv ? 2u * DP : DP;                    // of the sums
-    static constexpr uint32_t kAtW = 2u * kT, kAtSum = kAtW + kW;
+    static constexpr uint32_t kAtW = 2u * kT, kAtSum = (kAtW + kW + 31u) & ~31u;
     static constexpr uint32_t kBars = 1024u;
     static constexpr uint32_t kBytes = kBars + kHeldTiles * kX + kSlots * kY + kSlots / 2u * kStats + 8u * 32u * 4u;
     static_assert(kAtSum + kSum <= 512u && kBytes <= 232448u, "fits the SM");
@@ -94,7 +94,9 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
 {
     using Shape = PlaneShape<MODE, DP>;
     constexpr bool DKV = MODE == kDkv, FWD = MODE == kFwd;
-    constexpr uint32_t WALK = Shape::WALK, SLOTS = Shape::kSlots, HALF = WALK / 2u, PLANE = WALK / 2u;   // columns: a thread's, a plane's
+    constexpr uint32_t WALK = Shape::WALK, SLOTS = Shape::kSlots, PLANE = WALK / 2u;   // columns of a plane
+    constexpr uint32_t HALF = WALK == 16 ? 16 : WALK / 2u;         // columns of a thread (of 16, the first of a row's two has all)
+    constexpr bool EARLY = FWD && SLOTS == 2u;
     constexpr uint32_t XBOX = kHeld * 128u, YBOX = WALK * 128u, XP = Shape::kX / 3u, YP = Shape::kY / 3u;
     extern __shared__ __align__(1024) unsigned char s_raw[];
     struct Bars {
@@ -168,8 +170,9 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
 #pragma unroll
                 for (int c = 0; c < N / 32; c++) {
                     float x[32];
-                    // DKV: dv in the first DP columns, dk in the next; half of each
-                    tmem_load32(tmem + Shape::kAtSum + quarter + (DKV ? c * DP + part * 32u : part * (DP / 2) + 32u * c), x);
+                    // dv in the first DP columns, dk in the next; half of each
+                    constexpr int PER = DP / 64;                   // pieces of 32 of a tensor's half row
+                    tmem_load32(tmem + Shape::kAtSum + quarter + (uint32_t)(c / PER) * DP + part * (DP / 2) + 32u * (c % PER), x);
                     tmem_wait_loads();
 #pragma unroll
                     for (int k = 0; k < 32; k++) sum[32 * c + k] = FWD ? (sum[32 * c + k] + x[k]) * fade : sum[32 * c + k] + x[k];
@@ -180,7 +183,8 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
             for (uint32_t i = 0; i < it.blocks; i++) {
                 if (!(ok = bar_wait(&bars.t_full[buf], t_ph, stop))) break;
                 if (DKV && !(ok = bar_wait(&bars.y_full[slot + 1u], y_ph, stop))) break;   // the statistics came by copy
-                const int cols = (int)((DKV ? a.Sq : it.n) - at) - (int)(HALF * part);     // columns with values, at least
+                // columns with values, at least
+                const int cols = WALK == 16 && part ? 0 : (int)((DKV ? a.Sq : it.n) - at) - (int)(HALF * part);
                 float s[HALF], e[HALF];
                 float fade = 1.0f;
                 if (!idle) {
@@ -289,9 +293,10 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
             const float by = FWD ? __fdiv_rn(1.0f, l) : a.scale;
 #pragma unroll
             for (int c = 0; c < N / 32; c++) {
-                const AttnTensor &to = FWD ? a.out : !DKV ? a.dq : c ? a.dk : a.dv;
-                const float times = DKV && c == 0 ? 1.0f : by;
-                const uint32_t d0 = DKV ? part * 32u : part * (DP / 2) + 32u * c;
+                constexpr int PER = DP / 64;
+                const AttnTensor &to = FWD ? a.out : !DKV ? a.dq : c / PER ? a.dk : a.dv;
+                const float times = DKV && c / PER == 0 ? 1.0f : by;
+                const uint32_t d0 = part * (DP / 2) + 32u * (c % PER);
                 float *const dst = reinterpret_cast<float *>(to.p) + to.sb * it.b + to.sh * it.h + to.ss * row + d0;
 #pragma unroll
                 for (int k = 0; k < 8; k++)
@@ -398,11 +403,11 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
             };
             uint32_t c_phase = 0;
             scores();
-            // the second block's T goes ahead only where that cannot wait for copies that wait for the first block
+            // with one pair of slots the next block's copies wait for this block's products: all of them, or, forward, T's
             if (ok && SLOTS > 2u) scores();
             for (; ok && cur.more; cur.step(p)) {
                 const uint32_t n16 = (cur.cols(p) + 15u) / 16u, y1 = ys + c_slot * Shape::kY, y2 = y1 + Shape::kY, w = tmem + Shape::kAtW, to = tmem + Shape::kAtSum;
-                if (SLOTS == 2u) scores();
+                if (EARLY) scores();
                 if (!ok || !bar_wait(&bars.w_ready, w_ph, stop)) break;
                 w_ph ^= 1u;
                 if (FWD && !bar_wait(&bars.y_full[c_slot + 1u], c_phase, stop)) break;
@@ -416,7 +421,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
                     c_slot = 0;
                     c_phase ^= 1u;
                 }
-                if (SLOTS > 2u) scores();
+                if (!EARLY) scores();
             }
             products_done(one, &bars.drain);
             bar_wait(&bars.drain, 0, stop);
@@ -477,7 +482,6 @@ static bool set_items(AttnGradArgs &p, const AttnTensor &x1, const AttnTensor &x
 
 uint64_t attn_planes_workspace(const AttnArgs &a, bool backward)
 {
-    if (backward && a.D > 64u) return 0;
     return (backward ? 2u : 1u) * planes_bytes(a.B, a.Sq, a.H, a.D) + 2u * planes_bytes(a.B, a.Sk, a.Hkv, a.D);
 }
 
@@ -495,20 +499,26 @@ daf_status attn_forward_planes(const AttnArgs &a, char *planes_at, WorkspaceHead
     return a.D <= 64u ? launch_planes<kFwd, 64>(p, s) : launch_planes<kFwd, 128>(p, s);
 }
 
-// Queries and keys exist, D <= 64.
+template <int DP> static daf_status backward(AttnGradArgs &p, const AttnTensor (&t)[4], cudaStream_t s)
+{
+    const AttnArgs &a = p.a;
+    if (!set_items(p, t[1], t[2], a.Sk, a.Hkv, t[0], t[3], a.Sq, a.H, PlaneShape<kDkv, DP>::WALK)) return DAF_ERR_CUDA;
+    const daf_status st = launch_planes<kDkv, DP>(p, s);
+    if (st != DAF_OK) return st;
+    if (!set_items(p, t[0], t[3], a.Sq, a.H, t[1], t[2], a.Sk, a.Hkv, PlaneShape<kDq, DP>::WALK)) return DAF_ERR_CUDA;
+    return launch_planes<kDq, DP>(p, s);
+}
+
+// Queries and keys exist.
 daf_status attn_backward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s)
 {
     AttnTensor t[4];
-    daf_status st = split_all(a, planes_at, true, nullptr, t, s);
+    const daf_status st = split_all(a, planes_at, true, nullptr, t, s);
     if (st != DAF_OK) return st;
     AttnGradArgs p = {};
     p.a = a;
     p.header = header;
-    if (!set_items(p, t[1], t[2], a.Sk, a.Hkv, t[0], t[3], a.Sq, a.H, 32)) return DAF_ERR_CUDA;
-    st = launch_planes<kDkv, 64>(p, s);
-    if (st != DAF_OK) return st;
-    if (!set_items(p, t[0], t[3], a.Sq, a.H, t[1], t[2], a.Sk, a.Hkv, 64)) return DAF_ERR_CUDA;
-    return launch_planes<kDq, 64>(p, s);
+    return a.D <= 64u ? backward<64>(p, t, s) : backward<128>(p, t, s);
 }
 
 }  // namespace daf
