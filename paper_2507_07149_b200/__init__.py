@@ -242,12 +242,12 @@ def _raw_stream(index: int, stream) -> int:
 def _call(fn, ref, stream, *args) -> int:
     """Calls fn(*args, stream) with the device of tensor `ref` current in this thread (the library launches on the
     current device) and, unless a stream is given, on torch's current stream OF THAT DEVICE.  Returns the status."""
-    cuda = _torch().cuda
+    torch = _torch()
     index = ref.get_device()
     raw = _raw_stream(index, stream)
-    if index == cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         return int(fn(*args, raw))
-    with cuda.device(index):
+    with torch.cuda.device(index):
         return int(fn(*args, raw))
 
 
@@ -593,6 +593,11 @@ def _fresh(template):
     return torch.empty_like(template, memory_format=torch.contiguous_format)
 
 
+def _like(t, template):
+    """A contiguous tensor of t's shape and type; template: one of that shape from _template."""
+    return _torch().empty_like(t) if t.is_contiguous() else _fresh(template)
+
+
 _headers = {}                                                         # (device, stream) -> status workspace
 
 
@@ -694,7 +699,7 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     direct = plan.direct
     (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
     if out is None:
-        out = _fresh(plan.like_q)
+        out = _like(q, plan.like_q)
     else:
         _one_device("attention", index, (out,))
     if lse is None:
@@ -732,7 +737,7 @@ def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: 
     (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
     (out, oa), (grad_out, ga) = _addressable(out, direct[3]), _addressable(grad_out, direct[4])
     if grads is None:
-        gq, gk, gv = _fresh(plan.like_q), _fresh(plan.like_k), _fresh(plan.like_k)
+        gq, gk, gv = _like(q, plan.like_q), _like(k, plan.like_k), _like(v, plan.like_k)
     else:
         gq, gk, gv = grads
         _one_device("attention_grad", index, grads)

@@ -26,7 +26,7 @@ constexpr int kGradThreads = 640;                // 16 warps x 104 registers, 4 
 constexpr uint32_t kHeld = 128, kWalk = 64;
 
 struct AttnGradArgs {
-    CUtensorMap x1, x2, y1, y2;                  // held: k, v or q, grad_out; walked: q, grad_out or k, v
+    CUtensorMap x1, x2, y1, y2;                  // held: k, v or q, grad_out; walked: q, grad_out or k, v; boxes of a walked tile's rows
     CUtensorMap out[2];                          // dv, dk or dq
     AttnArgs a;
     FastDiv heads, all_heads, tile_div;          // heads of the items, times B, tiles
@@ -361,10 +361,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                     if (one) {
                         const uint32_t dst = smem_u32(smem) + x * 2u * Smem::kX;
                         bar_expect(&x_full[x], 2u * Smem::kX);
-                        for (int e = 0; e < DP / 64; e++) {
-                            tma_load(dst + e * XBOX, &p.x1, &x_full[x], 64 * e, cur.it.h, cur.it.first, cur.it.b);
-                            tma_load(dst + Smem::kX + e * XBOX, &p.x2, &x_full[x], 64 * e, cur.it.h, cur.it.first, cur.it.b);
-                        }
+                        for (int e = 0; e < DP / 64; e++)
+                            for (int r = 0; r < 2; r++) {          // a box has half of a held tile's rows
+                                const int row = cur.it.first + kWalk * r;
+                                tma_load(dst + e * XBOX + r * YBOX, &p.x1, &x_full[x], 64 * e, cur.it.h, row, cur.it.b);
+                                tma_load(dst + Smem::kX + e * XBOX + r * YBOX, &p.x2, &x_full[x], 64 * e, cur.it.h, row, cur.it.b);
+                            }
                     }
                     if (++x == HELD) {
                         x = 0;
@@ -508,10 +510,11 @@ template <typename T> daf_status attn_backward_tc(const AttnArgs &a, WorkspaceHe
     AttnGradArgs p;
     p.a = a;
     p.header = header;
-    const auto maps = [&](const AttnTensor &x1, const AttnTensor &x2, uint32_t Sx, uint32_t Hx, const AttnTensor &y1, const AttnTensor &y2, uint32_t Sy, uint32_t Hy) {
-        return attn_tensor_map(&p.x1, bf16, x1, a.B, Sx, Hx, a.D, kHeld) && attn_tensor_map(&p.x2, bf16, x2, a.B, Sx, Hx, a.D, kHeld) &&
-               attn_tensor_map(&p.y1, bf16, y1, a.B, Sy, Hy, a.D, kWalk) && attn_tensor_map(&p.y2, bf16, y2, a.B, Sy, Hy, a.D, kWalk);
-    };
+    CUtensorMap q, k, v, g;
+    if (!attn_tensor_map(&q, bf16, a.q, a.B, a.Sq, a.H, a.D, kWalk) || !attn_tensor_map(&g, bf16, a.grad_out, a.B, a.Sq, a.H, a.D, kWalk) ||
+        !attn_tensor_map(&k, bf16, a.k, a.B, a.Sk, a.Hkv, a.D, kWalk) || !attn_tensor_map(&v, bf16, a.v, a.B, a.Sk, a.Hkv, a.D, kWalk) ||
+        !attn_store_map(&p.out[0], bf16, a.dv, a.B, a.Sk, a.Hkv, a.D) || !attn_store_map(&p.out[1], bf16, a.dk, a.B, a.Sk, a.Hkv, a.D))
+        return DAF_ERR_CUDA;
     const auto items = [&](uint32_t S, uint32_t H) {
         p.tiles = (S + kHeld - 1u) / kHeld;
         p.items = p.tiles * a.B * H;
@@ -519,13 +522,12 @@ template <typename T> daf_status attn_backward_tc(const AttnArgs &a, WorkspaceHe
         p.all_heads.set(a.B * H);
         p.tile_div.set(p.tiles);
     };
-    if (!maps(a.k, a.v, a.Sk, a.Hkv, a.q, a.grad_out, a.Sq, a.H) || !attn_store_map(&p.out[0], bf16, a.dv, a.B, a.Sk, a.Hkv, a.D) ||
-        !attn_store_map(&p.out[1], bf16, a.dk, a.B, a.Sk, a.Hkv, a.D))
-        return DAF_ERR_CUDA;
+    p.x1 = k; p.x2 = v; p.y1 = q; p.y2 = g;
     items(a.Sk, a.Hkv);
     daf_status st = a.D <= 64u ? launch_grad<T, 64, true>(p, s) : launch_grad<T, 128, true>(p, s);
     if (st != DAF_OK) return st;
-    if (!maps(a.q, a.grad_out, a.Sq, a.H, a.k, a.v, a.Sk, a.Hkv) || !attn_store_map(&p.out[0], bf16, a.dq, a.B, a.Sq, a.H, a.D)) return DAF_ERR_CUDA;
+    p.x1 = q; p.x2 = g; p.y1 = k; p.y2 = v;
+    if (!attn_store_map(&p.out[0], bf16, a.dq, a.B, a.Sq, a.H, a.D)) return DAF_ERR_CUDA;
     items(a.Sq, a.H);
     st = a.D <= 64u ? launch_grad<T, 64, false>(p, s) : launch_grad<T, 128, false>(p, s);
     return st;
