@@ -65,6 +65,10 @@ static uint32_t padded_rows(uint32_t rows) { return (rows + kAttnRowPad - 1u) / 
 
 // -lse and -delta of every row
 static uint64_t rows_bytes(const daf_attention_params *p) { return 2ull * p->batch * p->heads * padded_rows(p->queries) * sizeof(float); }
+static uint64_t maxima_bytes(const daf_attention_params *p)
+{
+    return p->dtype == DAF_F16 ? ((uint64_t)p->batch * p->kv_heads * sizeof(float) + 255u) & ~255ull : 0u;
+}
 
 static AttnArgs args_of(const daf_attention_params *p)
 {
@@ -126,7 +130,7 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
 extern "C" uint64_t daf_attention_grad_workspace(const daf_attention_params *params)
 {
     if (check_attention(params) != DAF_OK) return 0;
-    return sizeof(WorkspaceHeader) + rows_bytes(params) + (params->dtype == DAF_F32 ? attn_planes_workspace(args_of(params), true) : 0u);
+    return sizeof(WorkspaceHeader) + rows_bytes(params) + maxima_bytes(params) + (params->dtype == DAF_F32 ? attn_planes_workspace(args_of(params), true) : 0u);
 }
 
 extern "C" daf_status daf_attention_grad(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,
@@ -167,6 +171,8 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     a.row_ndelta = a.row_nl2 + (uint64_t)a.B * a.H * a.rows_padded;
     WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    a.grad_max = a.row_ndelta + (uint64_t)a.B * a.H * a.rows_padded;
+    if (maxima_bytes(params) && cudaMemsetAsync(a.grad_max, 0, maxima_bytes(params), s) != cudaSuccess) return DAF_ERR_CUDA;
     if (p.queries) {
         const daf_status rows = attn_rows(p.dtype, a, header, s);
         if (rows != DAF_OK) return rows;

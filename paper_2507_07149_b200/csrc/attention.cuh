@@ -30,6 +30,7 @@ struct AttnArgs {
     float *lse;                  // [B, H, Sq]: natural logarithm of each row's sum of exponentials, -inf for a row that sees no key
     const int32_t *lengths;      // keys of each sequence, or null
     float *row_nl2, *row_ndelta; // backward workspace, [B, H, rows_padded]: see attention_rows_kernel
+    float *grad_max;             // float16 backward: [B, Hkv], the largest squared norm of the grad_out rows that meet a key head
     uint32_t B, Sq, Sk, H, Hkv, D, group, causal, rows_padded;
     float scale, scale_log2;     // scale_log2 = scale * log2(e)
 };

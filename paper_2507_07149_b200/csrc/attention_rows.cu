@@ -19,19 +19,22 @@ template <typename T> __device__ __forceinline__ void load8_any(const void *p, f
 
 // What the backward kernels need of each row, D / 8 lanes (rounded up to a power of two) per row, 128 rows of a head per
 // CTA: -lse in units of log2, -inf for rows that see nothing and for the padding (their probabilities then come out as
-// exp2(-inf) = 0), and -delta = -sum(grad_out * out).
+// exp2(-inf) = 0), and -delta = -sum(grad_out * out).  float16 also notes the largest |grad_out|^2 of a key head's readers
+// (a maximum of non-negative floats by their bits: the order of the atomics changes nothing).
 template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_rows_kernel(const __grid_constant__ AttnArgs a, uint32_t lanes, WorkspaceHeader *header)
 {
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) header->status = 0u;
     const uint32_t lane = threadIdx.x % lanes, per = kRowThreads / lanes, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H;
     const uint32_t first = blockIdx.x * kRowsPerCta;
     const bool reads = lane * 8u < a.D;
+    constexpr bool F16 = __is_same(T, __half);
+    float most = 0.0f;
     const T *const o = reinterpret_cast<const T *>(a.out.p) + a.out.sb * b + a.out.sh * h + lane * 8u;
     const T *const g = reinterpret_cast<const T *>(a.grad_out.p) + a.grad_out.sb * b + a.grad_out.sh * h + lane * 8u;
 #pragma unroll 4
     for (uint32_t r = threadIdx.x / lanes; r < kRowsPerCta; r += per) {        // whole warps leave together
         const uint32_t i = first + r;
-        float nl2 = -INFINITY, delta = 0.0f;
+        float nl2 = -INFINITY, delta = 0.0f, norm = 0.0f;
         if (i < a.Sq) {
             const float l = a.lse[(uint64_t)bh * a.Sq + i];
             if (l != -INFINITY) nl2 = -l * 1.4426950408889634f;
@@ -40,14 +43,25 @@ template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_r
                 load8_any<T>(o + a.out.ss * i, x);
                 load8_any<T>(g + a.grad_out.ss * i, y);
 #pragma unroll
-                for (int e = 0; e < 8; e++) delta = __fmaf_rn(x[e], y[e], delta);
+                for (int e = 0; e < 8; e++) {
+                    delta = __fmaf_rn(x[e], y[e], delta);
+                    if (F16) norm = __fmaf_rn(y[e], y[e], norm);
+                }
             }
         }
-        for (uint32_t d = lanes >> 1; d; d >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
+        for (uint32_t d = lanes >> 1; d; d >>= 1) {
+            delta += __shfl_xor_sync(0xffffffffu, delta, d);
+            if (F16) norm += __shfl_xor_sync(0xffffffffu, norm, d);
+        }
+        most = fmaxf(most, norm);
         if (lane == 0) {
             a.row_nl2[(uint64_t)bh * a.rows_padded + i] = nl2;
             a.row_ndelta[(uint64_t)bh * a.rows_padded + i] = -delta;
         }
+    }
+    if (F16) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+        if ((threadIdx.x & 31u) == 0) atomicMax(reinterpret_cast<uint32_t *>(a.grad_max) + b * a.Hkv + h / a.group, top);
     }
 }
 

@@ -15,7 +15,10 @@
 // T1 and dS over T2.  What bounds it is the way of a block -- product, tensor memory to registers, exponentials, back,
 // second product, about 2500 cycles of latency --, so blocks in flight matter more than the wider products that blocks
 // of 128 would give, and eight warps per block more than long rows in few threads.
-// P and dS are rounded to the input type, which the second products need; everything else is binary32.
+// P and dS are rounded to the input type, which the second products need; everything else is binary32.  float16 reaches
+// from 6e-5 (6e-8 with fewer bits) to 65504, and dS may lie anywhere -- a mean over many tokens or a loss scale moves all
+// of grad_out --, so there dS is multiplied by the power of two that brings the largest |grad_out| row of the head to
+// [1, 2), and the sums by its inverse.
 #pragma once
 #include "attention.cuh"
 #include "tensor_core.cuh"
@@ -44,6 +47,13 @@ template <int DP, bool DKV> struct GradSmem {
     static constexpr uint32_t kBars = 1024u;                      // barriers and such, ahead of everything
     static constexpr uint32_t kBytes = kBars + kHeldBuffers * 2u * kX + kStages * (2u * kY + kStats) + 16u * kOut;
 };
+
+// That power of two, from the largest squared norm (1 where there is none).
+__device__ __forceinline__ float score_grad_scale(float most)
+{
+    const int e = (int)(__float_as_uint(sqrtf(most)) >> 23) - 127;
+    return e < -100 || e > 100 ? 1.0f : __uint_as_float((uint32_t)(127 - e) << 23);
+}
 
 // The i-th item of a CTA: there and back over the list, which starts with the longest items, so that who got a long
 // one gets a short one next.
@@ -198,13 +208,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
         const int off = (int)a.Sk - (int)a.Sq;
         const uint64_t c2 = pair(a.scale_log2, a.scale_log2);
         GradItem<DKV> it;
-        float nl = 0.0f, nd = 0.0f;
+        float nl = 0.0f, nd = 0.0f, lift = 1.0f;                   // lift: what float16 multiplies dS by
+        constexpr bool F16 = __is_same(T, __half);
         // item number `turn`, and for dq what its row brings along; false behind the last one
         auto enter = [&](uint32_t &turn) {
             for (; turn * gridDim.x < p.items; turn++) {
                 const uint32_t item = grad_item(turn);
                 if (item >= p.items) continue;
                 it.set(p, item);
+                if (F16) lift = score_grad_scale(a.grad_max[it.b * a.Hkv + (DKV ? it.h : it.h / a.group)]);
                 if (!DKV && it.blocks) {
                     const uint64_t at = ((uint64_t)it.b * a.H + it.h) * a.rows_padded + it.first + lane_row;
                     nl = a.row_nl2[at];
@@ -259,7 +271,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                                 unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
                                 u = exp2_fast(u);
                                 v = exp2_fast(v);
-                                unpair(mul2(pair(u, v), add2(pair(e[c], e[c + 1]), d2[q])), x, y);
+                                const uint64_t pr = F16 ? mul2(pair(u, v), both(lift)) : pair(u, v);
+                                unpair(mul2(pr, add2(pair(e[c], e[c + 1]), d2[q])), x, y);
                                 r1[2 * k + q] = round2<T>(u, v);
                                 r2[2 * k + q] = round2<T>(x, y);
                             }
@@ -301,7 +314,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             // DKV: warpgroups 0 and 2 store dv, 1 and 3 dk, half of the columns each; dq: 32 columns each, as far as they go
             const uint32_t group = warp >> 2;
             const CUtensorMap *const to = &p.out[DKV ? group & 1u : 0u];
-            const float by = DKV && !(group & 1u) ? 1.0f : a.scale;
+            const float by = DKV && !(group & 1u) ? 1.0f : F16 ? __fdiv_rn(a.scale, lift) : a.scale;
             constexpr uint32_t WIDTH = DKV ? DP / 2 : 32;
             const uint32_t from = (DKV ? group >> 1 : group) * WIDTH;
             const uint32_t acc = tmem + (DKV ? (group & 1u) * DP : 0u) + from + quarter;

@@ -212,3 +212,21 @@ def test_gradients_against_differences():
             f.append((daf.attention(*y, causal=True)[0].double() * g.double()).sum())
         slope, want = float(f[0] - f[1]) * 32, float((grads[i].double() * d.double()).sum())
         assert abs(slope - want) <= 0.02 * float(grads[i].double().norm()), (i, slope, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [2.0 ** -13, 2.0 ** 10])
+def test_gradients_far_from_one(dtype, size):
+    """Gradients scale with grad_out: a power of two more or less in every element of grad_out is the same power of two in
+    every gradient, up to the results' own subnormals (float16 results are kept normal by the other inputs)."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    q, k, v, g = (torch.randn((2, 300, 2, 64), generator=gen, device="cuda").to(dtype) for _ in range(4))
+    g = (g.float().clamp(-4, 4) + 0.0).to(dtype)
+    out, lse = daf.attention(q, k, v)
+    base = daf.attention_grad(q, k, v, out, lse, g)
+    got = daf.attention_grad(q, k, v, out, lse, (g.float() * size).to(dtype))
+    tiny = 2.0 ** -24 if dtype == torch.float16 else 0.0           # half an ulp of a subnormal result
+    u = 0.0 if dtype != torch.float16 else 2.0 ** -10               # g * 2^-13 rounds where it falls below 2^-14
+    for a, b in zip(got, base):
+        a, b = a.double(), b.double() * size
+        assert torch.isfinite(a).all() and (a - b).norm() <= u * b.norm() + tiny * math.sqrt(b.numel())
