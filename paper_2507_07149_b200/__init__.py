@@ -1,15 +1,16 @@
 """B200-native activation compress / decompress (the DAF hot path): thin Python binding.
 
 Every function here only marshals arguments for the C ABI declared in ``include/daf.h``
-(``libdaf.so``, hand-written sm_100a kernels).  PyTorch supplies device memory and streams;
+(``libdaf.so``, hand-written sm_100a kernels), in Python through ctypes or, for the operators of a transformer's step, in the
+compiled module ``_marshal`` (``csrc/marshal.cpp``).  PyTorch supplies device memory and streams;
 all arithmetic of the path runs in the CUDA library.  There is no CPU fallback: if the
 library is missing or fails to load, the first call raises.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
-from array import array
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -567,115 +568,21 @@ def daf_clip_norm_batch(d_in, d_out, max_norm, eps, d_norm, d_workspace, workspa
     _check(status, "daf_clip_norm_batch")
 
 
-_MAX_REMEMBERED = 4096                                              # shapes whose parameter blocks are kept
+_native_module = None
 
 
-def _remember(cache: dict, key, value):
-    if len(cache) >= _MAX_REMEMBERED:
-        cache.clear()
-    cache[key] = value
-    return value
-
-
-def _one_device(where: str, index: int, tensors) -> None:
-    for t in tensors:
-        if t is not None and t.get_device() != index:
-            raise ValueError(f"{where}: all tensors belong on one CUDA device")
-
-
-def _template(shape, dtype, device):
-    """A tensor of that shape that owns one element: empty_like of it is the cheapest way to allocate the shape again."""
-    return _torch().empty((1,) * len(shape), dtype=dtype, device=device).expand(shape)
-
-
-def _fresh(template):
-    torch = _torch()
-    return torch.empty_like(template, memory_format=torch.contiguous_format)
-
-
-def _like(t, template):
-    """A contiguous tensor of t's shape and type; template: one of that shape from _template."""
-    return _torch().empty_like(t) if t.is_contiguous() else _fresh(template)
-
-
-_headers = {}                                                         # (device, stream) -> status workspace
-
-
-def _header(index: int, raw: int):
-    """The workspace of calls that only keep a status word there: one for each stream, whose calls do not overlap."""
-    ws = _headers.get((index, raw))
-    if ws is None:
-        torch = _torch()
-        ws = _remember(_headers, (index, raw), torch.empty(256, dtype=torch.uint8, device=f"cuda:{index}"))
-    return ws
-
-
-_attention_plans = {}
-
-
-class _AttentionPlan:
-    """What a call of attention / attention_grad derives from types, shapes and strides alone: remembered per shape, since a
-    model repeats the same ones every step.  `direct`: which of the tensors the kernels can address in place."""
-    __slots__ = ("params", "ref", "ws", "lse_shape", "direct", "like_q", "like_k", "like_lse", "like_ws")
-
-
-def _attention_plan(where: str, causal, scale, tensors) -> _AttentionPlan:
-    """tensors: q, k, v, out or None, and for the backward pass grad_out, grad_q, grad_k, grad_v (None: to be allocated)."""
-    torch = _torch()
-    q, k, v = tensors[:3]
-    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
-        raise ValueError(f"{where} expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
-    (b, sq, h, d), (bk, sk, hkv, dk) = q.shape, k.shape
-    if b != bk or d != dk or hkv == 0 or h % hkv:
-        raise ValueError(f"{where}: q {tuple(q.shape)} and k {tuple(k.shape)} do not belong together")
-    if q.dtype not in _dtype_codes():
-        raise ValueError(f"{where}: {q.dtype} is not supported")
-    like_q = (q, k, v, q, q, q, k, v)
-    names = ("q", "k", "v", "out", "grad_out", "grad_q", "grad_k", "grad_v")
-    for name, t, l in zip(names, tensors, like_q):
-        if t is not None and (t.dtype != q.dtype or t.shape != l.shape):
-            raise ValueError(f"{where}: {name} is {t.dtype} {tuple(t.shape)}, expected {q.dtype} {tuple(l.shape)}")
-    plan = _AttentionPlan()
-    p = daf_attention_params(ctypes.sizeof(daf_attention_params), dtype_code(q), b, sq, sk, h, hkv, d, 1 if causal else 0,
-                             d ** -0.5 if scale is None else scale)
-    unit, direct = 16 // q.element_size(), []
-    for i, (name, t, l) in enumerate(zip(names, tensors, like_q)):
-        dense = (l.shape[1] * l.shape[2] * d, l.shape[2] * d, d)
-        s = dense + (1,) if t is None else t.stride()
-        fine = s[3] == 1 and all(l.shape[j] <= 1 or (s[j] % unit == 0 and s[j] >= d) for j in range(3))
-        if not fine and t is not None and (i >= 5 or (i == 3 and len(tensors) == 4)):
-            raise ValueError(f"{where}: {name} needs a contiguous last dimension and rows on 16-byte boundaries")
-        getattr(p, name + "_stride")[:] = s[:3] if fine else dense
-        direct.append(fine)
-    plan.params, plan.ref, plan.direct = p, ctypes.byref(p), direct
-    plan.ws = daf_attention_workspace(p) if len(tensors) == 4 else daf_attention_grad_workspace(p)
-    plan.lse_shape = (b, h, sq)
-    plan.like_q, plan.like_k = _template(q.shape, q.dtype, q.device), _template(k.shape, q.dtype, q.device)
-    plan.like_lse, plan.like_ws = _template(plan.lse_shape, torch.float32, q.device), _template((plan.ws,), torch.uint8, q.device)
-    return plan
-
-
-def _addressable(t, direct: bool):
-    """(tensor, address) of t, or of a contiguous copy where the kernels cannot address it."""
-    if direct:
-        at = t.data_ptr()
-        if not at & 15:
-            return t, at
-    t = t.contiguous()
-    if t.data_ptr() & 15:
-        t = t.clone()
-    return t, t.data_ptr()
-
-
-def _check_lengths(where, lengths, q):
-    if lengths is not None and (lengths.dtype != _torch().int32 or lengths.get_device() != q.get_device()
-                                or tuple(lengths.shape) != (q.shape[0],) or not lengths.is_contiguous()):
-        raise ValueError(f"{where}: key_lengths is an int32 tensor of {q.shape[0]} lengths on {q.device}")
-
-
-def _check_lse(where, lse, shape, q):
-    if tuple(lse.shape) != shape or lse.dtype != _torch().float32 or lse.get_device() != q.get_device() or not lse.is_contiguous():
-        raise ValueError(f"{where}: lse is a contiguous float32 tensor [B, H, Sq] on {q.device}")
+def _native():
+    """The compiled marshalling module of the functions below; raises if it has not been built."""
+    global _native_module
+    if _native_module is None:
+        lib()
+        _torch()                                                     # its libraries are what the module links against
+        try:
+            _native_module = importlib.import_module("._marshal", __name__)
+        except ImportError as e:
+            raise RuntimeError(f"paper_2507_07149_b200/_marshal.so cannot be loaded ({e}): build it with "
+                               "`python -m paper_2507_07149_b200.build`") from e
+    return _native_module
 
 
 def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None, out=None, lse=None,
@@ -683,35 +590,13 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     """(out, lse): softmax attention of q [B, Sq, H, D] over k, v [B, Sk, Hkv, D] and the logarithm of each row's sum of
     exponentials [B, H, Sq] that the backward pass needs (daf_attention).  Slices of a packed projection are read in place;
     tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
-    first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq."""
-    index = q.get_device()
-    if index < 0:
-        raise ValueError("attention expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
-    if k.get_device() != index or v.get_device() != index:
-        _one_device("attention", index, (k, v))
-    key = (index, q.dtype, k.dtype, v.dtype, q.shape, k.shape, v.shape, q.stride(), k.stride(), v.stride(), causal, scale,
-           None if out is None else (out.dtype, out.shape, out.stride()))
-    plan = _attention_plans.get(key)
-    if plan is None:
-        plan = _remember(_attention_plans, key, _attention_plan("attention", causal, scale, (q, k, v, out)))
-    if key_lengths is not None:
-        _check_lengths("attention", key_lengths, q)
-    direct = plan.direct
-    (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
-    if out is None:
-        out = _like(q, plan.like_q)
-    else:
-        _one_device("attention", index, (out,))
-    if lse is None:
-        lse = _fresh(plan.like_lse)
-    else:
-        _check_lse("attention", lse, plan.lse_shape, q)
-    ws = _header(index, _raw_stream(index, stream)) if plan.ws <= 256 else _fresh(plan.like_ws)
-    status = _call(lib().daf_attention, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), out.data_ptr(), lse.data_ptr(),
-                   ws.data_ptr(), plan.ws)
+    first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq.  check waits
+    for the device and raises on an error there.  With a stream, results and scratch belong to that stream."""
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return attention(q, k, v, causal=causal, scale=scale, key_lengths=key_lengths, out=out, lse=lse, check=check)
+    out, lse, status = _native().attention(q, k, v, key_lengths, out, lse, causal, scale, check)
     _check(status, "daf_attention")
-    if check:
-        _check(daf_poll_status(ws, stream), "daf_attention (device status)")
     return out, lse
 
 
@@ -719,89 +604,22 @@ def attention_grad(q, k, v, out, lse, grad_out, *, causal: bool = False, scale: 
                    check: bool = False, stream=None):
     """(grad_q, grad_k, grad_v) of ``attention`` from its inputs, its two results and grad_out (daf_attention_grad).  grads:
     three tensors to write into (they may be slices of one packed gradient), fresh contiguous ones by default."""
-    index = q.get_device()
-    if index < 0:
-        raise ValueError("attention_grad expects CUDA tensors q [B, Sq, H, D], k and v [B, Sk, Hkv, D]")
-    _one_device("attention_grad", index, (k, v, out, grad_out))
-    key = (index, q.dtype, k.dtype, v.dtype, out.dtype, grad_out.dtype, q.shape, k.shape, v.shape, out.shape, grad_out.shape, q.stride(),
-           k.stride(), v.stride(), out.stride(), grad_out.stride(), causal, scale,
-           None if grads is None else tuple((t.dtype, t.shape, t.stride()) for t in grads))
-    plan = _attention_plans.get(key)
-    if plan is None:
-        plan = _remember(_attention_plans, key, _attention_plan("attention_grad", causal, scale,
-                                                                (q, k, v, out, grad_out) + tuple(grads or (None, None, None))))
-    if key_lengths is not None:
-        _check_lengths("attention_grad", key_lengths, q)
-    _check_lse("attention_grad", lse, plan.lse_shape, q)
-    direct = plan.direct
-    (q, qa), (k, ka), (v, va) = _addressable(q, direct[0]), _addressable(k, direct[1]), _addressable(v, direct[2])
-    (out, oa), (grad_out, ga) = _addressable(out, direct[3]), _addressable(grad_out, direct[4])
-    if grads is None:
-        gq, gk, gv = _like(q, plan.like_q), _like(k, plan.like_k), _like(v, plan.like_k)
-    else:
-        gq, gk, gv = grads
-        _one_device("attention_grad", index, grads)
-    ws = _fresh(plan.like_ws)
-    status = _call(lib().daf_attention_grad, q, stream, plan.ref, qa, ka, va, _ptr(key_lengths), oa, lse.data_ptr(), ga,
-                   gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), ws.data_ptr(), plan.ws)
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return attention_grad(q, k, v, out, lse, grad_out, causal=causal, scale=scale, key_lengths=key_lengths, grads=grads, check=check)
+    gq, gk, gv = (None, None, None) if grads is None else grads
+    gq, gk, gv, status = _native().attention_grad(q, k, v, out, lse, grad_out, key_lengths, gq, gk, gv, causal, scale, check)
     _check(status, "daf_attention_grad")
-    if check:
-        _check(daf_poll_status(ws, stream), "daf_attention_grad (device status)")
     return gq, gk, gv
 
 
-_norm_plans = {}
+_KINDS = {"layer": NORM_LAYER, "rms": NORM_RMS}
 
 
-class _NormPlan:
-    """Parameter block and workspace size of residual_norm / residual_norm_grad for one set of types and shapes."""
-    __slots__ = ("params", "ref", "ws", "like_ws")
-
-
-def _norm_plan(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps) -> _NormPlan:
-    if x.dim() < 1 or x.shape != y.shape or x.dtype != y.dtype or x.dtype not in _dtype_codes():
-        raise ValueError(f"{where} expects tensors of one shape and one of the supported types")
-    if kind not in ("layer", "rms"):
+def _kind(where: str, kind: str) -> int:
+    if kind not in _KINDS:
         raise ValueError(f"{where}: kind is 'layer' or 'rms'")
-    width = x.shape[-1]
-    rows = x.numel() // width if width else 0
-    for name, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias)):
-        if t is not None and (tuple(t.shape) != (width,) or t.dtype != weight.dtype):
-            raise ValueError(f"{where}: {name} is {t.dtype} {tuple(t.shape)}, expected {weight.dtype} ({width},)")
-    if weight.dtype not in _dtype_codes():
-        raise ValueError(f"{where}: parameters of {weight.dtype} are not supported")
-    gates = 0
-    if gate is not None:
-        gates = 1 if gate.dim() == 1 else int(gate.shape[0])
-        if tuple(gate.shape) not in ((width,), (gates, width)) or gates == 0 or gate.dtype != weight.dtype:
-            raise ValueError(f"{where}: gate must be [{width}] or [G, {width}] in the other parameters' type")
-    plan = _NormPlan()
-    plan.params = daf_norm_params(ctypes.sizeof(daf_norm_params), dtype_code(x), dtype_code(weight),
-                                  NORM_LAYER if kind == "layer" else NORM_RMS, rows, width, gates, residual_scale, eps, 0)
-    plan.ref = ctypes.byref(plan.params)
-    plan.ws = daf_residual_norm_grad_workspace(plan.params)
-    plan.like_ws = _template((plan.ws,), _torch().uint8, x.device)
-    return plan
-
-
-def _norm_call(where: str, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps, *more) -> _NormPlan:
-    """The plan for these tensors; `more` are activations of x's shape and type.  Every tensor is checked for its device and for
-    being contiguous."""
-    vectors = (weight, bias, gate, post_weight, post_bias)
-    index = x.get_device()
-    if index < 0:
-        raise ValueError(f"{where} expects CUDA tensors")
-    key = (index, x.dtype, y.dtype, x.shape, y.shape, residual_scale, kind, eps, *[None if t is None else (t.dtype, t.shape) for t in vectors])
-    plan = _norm_plans.get(key)
-    if plan is None:
-        plan = _remember(_norm_plans, key, _norm_plan(where, x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps))
-    for t in (x, y, *vectors, *more):
-        if t is not None and (t.get_device() != index or not t.is_contiguous()):
-            raise ValueError(f"{where} expects contiguous tensors on one CUDA device")
-    for t in more:
-        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
-            raise ValueError(f"{where}: a tensor differs from the activations in shape or type")
-    return plan
+    return _KINDS[kind]
 
 
 def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_bias=None, residual_scale: float = 1.0,
@@ -809,30 +627,27 @@ def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_
     """(z, h): z = x + residual_scale * gate * post_norm(y), h = norm(z) * weight + bias over the last dimension, in one pass
     (daf_residual_norm).  post_norm only with post_weight; gate [C], or [G, C] for G equal runs of rows; parameters in the
     activations' type or float32.  out: (z, h) to write into, z may be x and h may be y."""
-    plan = _norm_call("residual_norm", x, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps, *(out or ()))
-    if out is None:
-        empty = _torch().empty_like
-        out = empty(x), empty(x)
-    z, h = out
-    status = _call(lib().daf_residual_norm, x, stream, plan.ref, x.data_ptr(), y.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(gate),
-                   _ptr(post_weight), _ptr(post_bias), z.data_ptr(), h.data_ptr())
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return residual_norm(x, y, weight, bias, gate=gate, post_weight=post_weight, post_bias=post_bias, residual_scale=residual_scale,
+                                 kind=kind, eps=eps, out=out)
+    z, h = (None, None) if out is None else out
+    made_z, made_h, status = _native().residual_norm(x, y, weight, bias, gate, post_weight, post_bias, residual_scale,
+                                                     _kind("residual_norm", kind), eps, z, h)
     _check(status, "daf_residual_norm")
-    return z, h
+    return (made_z, made_h) if out is None else (z, h)
 
 
 def residual_norm_grad(z, y, weight, bias, grad_z, grad_h, *, gate=None, post_weight=None, post_bias=None,
                        residual_scale: float = 1.0, kind: str = "layer", eps: float = 1e-6, stream=None) -> dict:
     """Gradients of ``residual_norm`` from z, y and those of z (None: zero) and h (daf_residual_norm_grad): a dict with "x", "y",
     "weight", "bias", "gate", "post_weight" and "post_bias", None where there is no such parameter."""
-    torch = _torch()
-    plan = _norm_call("residual_norm_grad", z, y, weight, bias, gate, post_weight, post_bias, residual_scale, kind, eps, grad_z, grad_h)
-    empty = torch.empty_like
-    gx, gy, gw = empty(z), empty(z), empty(weight)
-    gb, gg, gpw, gpb = (None if t is None else empty(t) for t in (bias, gate, post_weight, post_bias))
-    ws = _fresh(plan.like_ws)
-    status = _call(lib().daf_residual_norm_grad, z, stream, plan.ref, z.data_ptr(), y.data_ptr(), weight.data_ptr(), _ptr(gate),
-                   _ptr(post_weight), _ptr(post_bias), _ptr(grad_z), grad_h.data_ptr(), gx.data_ptr(), gy.data_ptr(), gw.data_ptr(),
-                   _ptr(gb), _ptr(gg), _ptr(gpw), _ptr(gpb), ws.data_ptr(), plan.ws)
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return residual_norm_grad(z, y, weight, bias, grad_z, grad_h, gate=gate, post_weight=post_weight, post_bias=post_bias,
+                                      residual_scale=residual_scale, kind=kind, eps=eps)
+    gx, gy, gw, gb, gg, gpw, gpb, status = _native().residual_norm_grad(
+        z, y, weight, bias, gate, post_weight, post_bias, residual_scale, _kind("residual_norm_grad", kind), eps, grad_z, grad_h)
     _check(status, "daf_residual_norm_grad")
     return {"x": gx, "y": gy, "weight": gw, "bias": gb, "gate": gg, "post_weight": gpw, "post_bias": gpb}
 
@@ -841,36 +656,13 @@ def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, strea
     """Scales the tensors of ``grads`` in place (or into ``out``, tensors of the same types and sizes) by
     min(1, max_norm / (norm + eps)), norm being the 2-norm over all of them; returns the norm as a float32 scalar tensor on
     their device (daf_clip_norm_batch).  Nothing is read back."""
-    torch = _torch()
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return clip_grad_norm(grads, max_norm, eps=eps, out=out)
     grads = list(grads)
-    n = len(grads)
-    if n == 0:
-        return torch.zeros((), dtype=torch.float32)
-    tensor, codes = torch.Tensor, _dtype_codes()
-    numel = array("Q", map(tensor.numel, grads))
-    dtypes = [g.dtype for g in grads]
-    try:
-        code = array("I", [codes[t] for t in dtypes])
-    except KeyError as e:
-        raise ValueError(f"clip_grad_norm: {e.args[0]} is not supported") from None
-    index = grads[0].get_device()
-    if index < 0 or any(i != index for i in map(tensor.get_device, grads)) or not all(map(tensor.is_contiguous, grads)):
-        raise ValueError("clip_grad_norm expects contiguous CUDA tensors on one device")
-    src = array("Q", map(tensor.data_ptr, grads))
-    dst = src
-    if out is not None:
-        out = list(out)
-        if len(out) != n or array("Q", map(tensor.numel, out)) != numel or [o.dtype for o in out] != dtypes \
-                or any(i != index for i in map(tensor.get_device, out)) or not all(map(tensor.is_contiguous, out)):
-            raise ValueError("clip_grad_norm: an output differs from its gradient in size, type or device, or is not contiguous")
-        dst = array("Q", map(tensor.data_ptr, out))
-    dev = grads[0].device
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws_bytes = daf_clip_norm_workspace(n)
-    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-    at = [a.buffer_info()[0] for a in (code, src, dst, numel)]
-    status = _call(lib().daf_clip_norm_batch, norm, stream, n, at[0], at[1], at[2], at[3], max_norm, eps, norm.data_ptr(),
-                   ws.data_ptr(), ws_bytes)
+    if not grads:
+        return _torch().zeros((), dtype=_torch().float32)
+    norm, status = _native().clip_grad_norm(grads, None if out is None else list(out), max_norm, eps)
     _check(status, "daf_clip_norm_batch")
     return norm
 

@@ -19,6 +19,10 @@ CU_SOURCES = ["api.cu", "compress.cu", "compress_stream_f32.cu", "compress_strea
               "attention.cu", "attention_rows.cu", "attention_tc_f32.cu", "attention_tc_f16.cu", "attention_tc_bf16.cu", "residual_norm.cu", "clip_norm.cu"]
 CXX_SOURCES = ["pool.cpp", "store.cpp"]
 
+# The Python module that marshals torch tensors for the transformer operators (host code only).
+MARSHAL = os.path.join(HERE, "_marshal.so")
+MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
+
 # No fast-math, no flush-to-zero, no fused contraction beyond what the sources write out:
 # results must match IEEE binary32 arithmetic bit for bit.
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -68,7 +72,32 @@ def build(force: bool = False, verbose: bool = False) -> str:
     objs = [os.path.join(OBJ, s + ".o") for s in CU_SOURCES + CXX_SOURCES]
     if force or jobs or _stale(LIB, objs):
         subprocess.check_call([nvcc, "-shared", "-o", LIB, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
+    build_marshal(force)
     return LIB
+
+
+def build_marshal(force: bool = False) -> str:
+    """Compiles csrc/marshal.cpp against torch and libdaf.so (found beside it when the module is loaded)."""
+    if not (force or _stale(MARSHAL, [MARSHAL_SOURCE, HEADERS[-1]])):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    cxx = shutil.which("g++")
+    if cxx is None:
+        raise RuntimeError("g++ not found: the marshalling module cannot be built")
+    include = [f"-I{sysconfig.get_paths()['include']}"]
+    for path in [*cpp_extension.include_paths(), os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")]:
+        include += ["-isystem", path]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *include,
+           MARSHAL_SOURCE, "-o", MARSHAL, f"-L{libs}", "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-lc10_cuda", f"-L{HERE}",
+           "-l:libdaf.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on marshal.cpp:\n{r.stdout}\n{r.stderr}")
+    return MARSHAL
 
 
 if __name__ == "__main__":
