@@ -63,6 +63,15 @@ bool attn_store_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B
 
 static uint32_t padded_rows(uint32_t rows) { return (rows + kAttnRowPad - 1u) / kAttnRowPad * kAttnRowPad; }
 
+uint32_t attn_splits(const AttnArgs &a)
+{
+    constexpr uint32_t kSms = 148, kTileRows = 256, kKeys = 128, kMinBlocks = 8;
+    const uint64_t tiles = (uint64_t)((a.Sq + kTileRows - 1u) / kTileRows) * a.B * a.H, blocks = (a.Sk + kKeys - 1u) / kKeys;
+    if (tiles == 0 || 2u * tiles > kSms || blocks < kMinBlocks) return 1;
+    const uint64_t room = kSms / tiles, most = blocks / 2u;         // two blocks at least to a split
+    return (uint32_t)(room < most ? room : most);
+}
+
 // -lse and -delta of every row
 static uint64_t rows_bytes(const daf_attention_params *p) { return 2ull * p->batch * p->heads * padded_rows(p->queries) * sizeof(float); }
 static uint64_t maxima_bytes(const daf_attention_params *p)
@@ -94,7 +103,10 @@ using namespace daf;
 extern "C" uint64_t daf_attention_workspace(const daf_attention_params *params)
 {
     if (check_attention(params) != DAF_OK) return 0;
-    return sizeof(WorkspaceHeader) + (params->dtype == DAF_F32 ? attn_planes_workspace(args_of(params), false) : 0u);
+    const AttnArgs a = args_of(params);
+    if (params->dtype == DAF_F32) return sizeof(WorkspaceHeader) + attn_planes_workspace(a, false);
+    const uint64_t splits = attn_splits(a);
+    return sizeof(WorkspaceHeader) + (splits > 1u ? splits * a.B * a.H * a.Sq * (a.D + 1u) * sizeof(float) : 0u);
 }
 
 extern "C" daf_status daf_attention(const daf_attention_params *params, const void *d_q, const void *d_k, const void *d_v,

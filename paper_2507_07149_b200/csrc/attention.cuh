@@ -56,6 +56,10 @@ daf_status attn_forward_planes(const AttnArgs &a, char *planes_at, WorkspaceHead
 daf_status attn_backward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_zero(uint32_t dtype, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, cudaStream_t s);
+// Into how many runs of key blocks a 16-bit forward call cuts each of its row tiles: 1, or as many as fill a B200 where the
+// tiles alone leave half of it idle and eight blocks or more are walked.  (4 x 43 queries over 4740 keys, one head of 72: 65.5 us
+// on 4 CTAs, 21.5 on 148.)
+uint32_t attn_splits(const AttnArgs &a);
 template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 
 // Map of a tensor for copies of `rows` rows times 64 elements of one head; false if the driver refuses it.

@@ -33,7 +33,9 @@ struct AttnForwardArgs {
     CUtensorMap q, k, v, out;
     AttnArgs a;
     FastDiv heads, all_heads, tiles;             // H, B H, q_tiles
-    uint32_t items, q_tiles;
+    FastDiv split_div;                           // splits
+    uint32_t items, q_tiles, splits;             // splits: runs of key blocks of a row tile, each an item
+    float *part_out, *part_lse2;                 // with splits: [split, B, H, Sq, D] and [split, B, H, Sq], see attn_splits
     WorkspaceHeader *header;
 };
 
@@ -48,11 +50,17 @@ template <int DP> struct FwdSmem {
 
 // The item's head, batch entry and first query, and its number of key blocks per half.
 struct FwdItem {
-    uint32_t b, h, m0, n;
-    int blocks[2], both;
+    uint32_t b, h, m0, n, split;
+    int blocks[2], both, j0;                     // j0: the first key block
     __device__ __forceinline__ void set(const AttnForwardArgs &p, uint32_t item)
     {
         const AttnArgs &a = p.a;
+        split = 0;
+        if (p.splits > 1u) {
+            const uint32_t whole = p.split_div.div(item);
+            split = item - whole * p.splits;
+            item = whole;
+        }
         uint32_t bh, qt;
         if (a.causal) {                                            // longest rows first
             qt = p.all_heads.div(item);
@@ -75,6 +83,16 @@ struct FwdItem {
             }
         }
         both = blocks[0] > blocks[1] ? blocks[0] : blocks[1];
+        j0 = 0;
+        if (p.splits > 1u) {                                       // the split's share of the blocks
+            const int share = (both + (int)p.splits - 1) / (int)p.splits;
+            j0 = (int)split * share;
+            for (int w = 0; w < 2; w++) {
+                const int left = blocks[w] - j0;
+                blocks[w] = left < 0 ? 0 : left < share ? left : share;
+            }
+            both = blocks[0] > blocks[1] ? blocks[0] : blocks[1];
+        }
     }
 };
 
@@ -175,8 +193,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 s_ph ^= 1u;
                 if (!idle) {
                     tmem_after_sync();
-                    const int valid = (int)it.n - j * kBlock - 64 * (int)part;   // columns that hold scores, at least
-                    const int left = limit - j * kBlock - 64 * (int)part;
+                    const int valid = (int)it.n - (it.j0 + j) * kBlock - 64 * (int)part;   // columns that hold scores, at least
+                    const int left = limit - (it.j0 + j) * kBlock - 64 * (int)part;
                     const bool masked = __any_sync(0xffffffffu, left < 64);
                     // 32 scores at a time, once for the maximum and once more for the exponentials: reading tensor memory
                     // twice costs less than 64 registers
@@ -283,7 +301,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 tmem_after_sync();
             }
             if (idle) continue;
-            if (part == 0 && row < a.Sq) a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+            const uint64_t bh = (uint64_t)it.b * a.H + it.h, part_row = ((uint64_t)it.split * a.B * a.H + bh) * a.Sq + row;
+            if (part == 0 && row < a.Sq) {
+                const float lse2 = l > 0.0f ? m + log2f(l) : -INFINITY;
+                if (p.splits > 1u) p.part_lse2[part_row] = lse2;
+                else a.lse[bh * a.Sq + row] = lse2 * 0.69314718055994531f;
+            }
 #pragma unroll
             for (int i = 0; i < DP / 64; i++) {
                 const uint32_t from = part * (DP / 2) + 32u * i;
@@ -292,6 +315,15 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 if (blocks > 0) {
                     tmem_load32(to + 32 * i, o);
                     tmem_wait_loads();
+                }
+                if (p.splits > 1u) {                                // for attention_join_kernel, in binary32
+                    float4 *const to_part = reinterpret_cast<float4 *>(p.part_out + part_row * a.D + from);
+#pragma unroll
+                    for (int k = 0; k < 8; k++)
+                        if (row < a.Sq && from + 4u * k < a.D)
+                            to_part[k] = l > 0.0f ? make_float4(o[4 * k] * by, o[4 * k + 1] * by, o[4 * k + 2] * by, o[4 * k + 3] * by)
+                                                  : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    continue;
                 }
                 if (lane == 0) stores_read<0>();
                 __syncwarp();
@@ -333,7 +365,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                     q_ph ^= 1u;
                 }
                 for (int i = 0; i < 2 * it.both; i++) {                // K0 V0 K1 V1 ...
-                    const int j = i >> 1;
+                    const int j = it.j0 + (i >> 1);
                     const bool is_v = i & 1;
                     if (!bar_wait(&kv_empty[st], ph, stop)) break;
                     unsigned char *const dst = smem + Smem::kKeys + st * Smem::kTile;
@@ -384,7 +416,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                 }
                 // S of half w for the key block in stage `at`
                 auto scores = [&](int w, int j, uint32_t at) {
-                    const uint32_t valid = it.n - (uint32_t)j * kBlock, cols = valid < (uint32_t)kBlock ? (valid + 15u) & ~15u : kBlock;
+                    const uint32_t valid = it.n - (uint32_t)(it.j0 + j) * kBlock, cols = valid < (uint32_t)kBlock ? (valid + 15u) & ~15u : kBlock;
                     const uint32_t desc = product_desc(BF16, cols, false);
                     const uint32_t q = operand_low(q_smem + (2u * qb + w) * Smem::kTile, 16), k = operand_low(kv_smem + at * Smem::kTile, 16);
                     product_ss(one, tmem + w * 128u, q, k, desc, false);
@@ -417,7 +449,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                     next();
                     const bool more = j + 1 < it.both;
                     if (more && !bar_wait(&kv_full[st], ph, stop)) break;
-                    const uint32_t valid = it.n - (uint32_t)j * kBlock;
+                    const uint32_t valid = it.n - (uint32_t)(it.j0 + j) * kBlock;
                     const uint32_t pv_steps = valid < (uint32_t)kBlock ? (valid + 15u) / 16u : kBlock / 16;
 #pragma unroll
                     for (int w = 0; w < 2; w++) {
@@ -453,6 +485,40 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     if (warp == 0) tmem_free(tmem, 512);
 }
 
+// Joins the splits of each row, a warp per row, in the order of the keys: out = sum of 2^(lse2_s - lse2) out_s.
+template <typename T> __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ AttnForwardArgs p)
+{
+    const AttnArgs &a = p.a;
+    const uint64_t rows = (uint64_t)a.B * a.H * a.Sq, r = (uint64_t)blockIdx.x * 8u + (threadIdx.x >> 5);
+    const uint32_t lane = threadIdx.x & 31u;
+    if (r >= rows) return;
+    float top = -INFINITY;
+    for (uint32_t s = lane; s < p.splits; s += 32u) top = fmaxf(top, p.part_lse2[s * rows + r]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const bool some = top > -INFINITY, mine = lane * 4u < a.D;
+    float total = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t s = 0; some && s < p.splits; s++) {
+        const float w = exp2_fast(p.part_lse2[s * rows + r] - top);
+        total += w;
+        if (!mine || w == 0.0f) continue;
+        const float4 x = *reinterpret_cast<const float4 *>(p.part_out + (s * rows + r) * a.D + lane * 4u);
+        o.x = __fmaf_rn(w, x.x, o.x);
+        o.y = __fmaf_rn(w, x.y, o.y);
+        o.z = __fmaf_rn(w, x.z, o.z);
+        o.w = __fmaf_rn(w, x.w, o.w);
+    }
+    const float by = some ? __fdiv_rn(1.0f, total) : 0.0f;
+    const uint64_t bh = r / a.Sq;
+    const uint32_t i = (uint32_t)(r - bh * a.Sq), b = (uint32_t)(bh / a.H), h = (uint32_t)(bh - (uint64_t)b * a.H);
+    if (mine) {
+        const uint2 v = make_uint2(round2<T>(o.x * by, o.y * by), round2<T>(o.z * by, o.w * by));
+        *reinterpret_cast<uint2 *>(reinterpret_cast<char *>(a.out.p) + 2u * (a.out.sb * b + a.out.ss * i + a.out.sh * h + lane * 4u)) = v;
+    }
+    if (lane == 0) a.lse[r] = some ? (top + log2f(total)) * 0.69314718055994531f : -INFINITY;
+}
+
 template <typename T, int DP> static daf_status launch_forward(AttnForwardArgs &p, cudaStream_t s)
 {
     int ctas = 0;
@@ -464,11 +530,15 @@ template <typename T, int DP> static daf_status launch_forward(AttnForwardArgs &
 
 template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s)
 {
-    AttnForwardArgs p;
+    AttnForwardArgs p = {};
     p.a = a;
+    p.splits = attn_splits(a);
+    p.split_div.set(p.splits);
+    p.part_out = reinterpret_cast<float *>(header + 1);
+    p.part_lse2 = p.part_out + (uint64_t)p.splits * a.B * a.H * a.Sq * a.D;
     p.a.scale_log2 = fmaxf(fabsf(a.scale_log2), 0x1p-100f);       // the sign is applied to S; never 0, which masks would turn into NaN
     p.q_tiles = (a.Sq + kFwdRows - 1u) / kFwdRows;
-    p.items = p.q_tiles * a.B * a.H;
+    p.items = p.q_tiles * a.B * a.H * p.splits;
     p.header = header;
     const bool bf16 = __is_same(T, __nv_bfloat16);
     p.heads.set(a.H);
@@ -478,7 +548,10 @@ template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHea
     if (a.Sk == 0) p.k = p.v = p.q;                                // never read
     else if (!attn_tensor_map(&p.k, bf16, a.k, a.B, a.Sk, a.Hkv, a.D, 128) || !attn_tensor_map(&p.v, bf16, a.v, a.B, a.Sk, a.Hkv, a.D, 128))
         return DAF_ERR_CUDA;
-    return a.D <= 64u ? launch_forward<T, 64>(p, s) : launch_forward<T, 128>(p, s);
+    const daf_status st = a.D <= 64u ? launch_forward<T, 64>(p, s) : launch_forward<T, 128>(p, s);
+    if (st != DAF_OK || p.splits == 1u) return st;
+    attention_join_kernel<T><<<(uint32_t)(((uint64_t)a.B * a.H * a.Sq + 7u) / 8u), 256, 0, s>>>(p);
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 
 }  // namespace daf

@@ -230,3 +230,37 @@ def test_gradients_far_from_one(dtype, size):
     for a, b in zip(got, base):
         a, b = a.double(), b.double() * size
         assert torch.isfinite(a).all() and (a - b).norm() <= u * b.norm() + tiny * math.sqrt(b.numel())
+
+
+def test_a_stream_by_argument_takes_the_copies_along():
+    """Work that is asked for on a stream happens there, the copies of tensors the kernels cannot address included: that stream
+    holds everything up, the current one does not."""
+    s = torch.cuda.Stream()
+    base = torch.randn(2 * 90 * 2 * 64 + 1, device="cuda").bfloat16()
+    q = base[1:].view(2, 90, 2, 64)                                 # off its 16-byte boundary
+    want, want_lse = daf.attention(q, q, q, causal=True)
+    g = torch.randn(2, 90, 2, 64, device="cuda").bfloat16()
+    grads = daf.attention_grad(q, q, q, want, want_lse, g, causal=True)
+    torch.cuda.synchronize()
+    later = torch.zeros_like(base)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        later.copy_(base)
+    q = later[1:].view(2, 90, 2, 64)
+    out, lse = daf.attention(q, q, q, causal=True, stream=s)
+    got = daf.attention_grad(q, q, q, out, lse, g, causal=True, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_lse) and all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,D,causal,lengths", [
+    (1, 1, 8000, 2, 1, 128, False, None), (3, 5, 4100, 2, 2, 64, True, [0, 4100, 130]), (1, 300, 3000, 1, 1, 80, True, None),
+    (2, 1, 1153, 1, 1, 40, False, [1153, 1])])
+def test_few_rows_over_many_keys(dtype, B, Sq, Sk, H, Hkv, D, causal, lengths):
+    """Calls that leave most of the GPU idle are split over the keys and joined; the same bounds, and the same bits twice."""
+    q, k, v, g, out, lse, _ = run_case(dtype, B, Sq, Sk, H, Hkv, D, causal, lengths=lengths, poison=lengths is not None)
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    again, again_lse = daf.attention(q, k, v, causal=causal, key_lengths=lens)
+    assert torch.equal(again, out) and torch.equal(again_lse, lse)
