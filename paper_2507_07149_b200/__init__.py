@@ -245,6 +245,8 @@ def _call(fn, ref, stream, *args) -> int:
     current device) and, unless a stream is given, on torch's current stream OF THAT DEVICE.  Returns the status."""
     torch = _torch()
     index = ref.get_device()
+    if index < 0:                                                    # torch would take -1 for the current device
+        raise ValueError(f"expected a CUDA tensor, got one on {ref.device}")
     raw = _raw_stream(index, stream)
     if index == torch._C._cuda_getDevice():
         return int(fn(*args, raw))
