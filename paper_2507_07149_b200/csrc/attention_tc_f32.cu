@@ -34,7 +34,7 @@ template <int MODE, int DP> struct PlaneShape {
     static constexpr uint32_t kSum = MODE == kDkv ? 2u * DP : DP;                    // of the sums
     static constexpr uint32_t kAtW = 2u * kT, kAtSum = (kAtW + kW + 31u) & ~31u;
     static constexpr uint32_t kBars = 1024u;
-    static constexpr uint32_t kBytes = kBars + kHeldTiles * kX + kSlots * kY + kSlots / 2u * kStats + 8u * 32u * 4u;
+    static constexpr uint32_t kBytes = kBars + kHeldTiles * kX + kSlots * kY + kSlots / 2u * kStats + 2u * 8u * 32u * 4u;
     static_assert(kAtSum + kSum <= 512u && kBytes <= 232448u, "fits the SM");
 };
 
@@ -140,6 +140,16 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
         take_registers<232>();
         const uint32_t part = warp >> 2, quarter = (warp & 3u) << 21, lane_row = (warp & 3u) * 32u + lane, meeting = 1u + (warp & 3u);
         const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(meeting) : "memory"); };
+        // What the other warp of the rows says to this one's value.  Two places in turn: T of the next block may be there before
+        // the other warp has read, but who writes for exchange n + 2 has met, at n + 1, the warp that has read n.
+        uint32_t told = 0;
+        const auto exchange = [&](float value) {
+            float (*const at)[32] = s_told + told;
+            told ^= 8u;
+            at[warp][lane] = value;
+            meet();
+            return at[warp ^ 4u][lane];
+        };
         const int off = (int)a.Sk - (int)a.Sq;
         uint32_t buf = 0, t_ph = 0, sum_ph = 0, slot = 0, y_ph = 0;
         bool ok = true;
@@ -215,9 +225,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
                                 top = fmaxf(top, s[k]);
                             }
                         }
-                        s_told[warp][lane] = top;
-                        meet();
-                        const float next = fmaxf(m, fmaxf(top, s_told[warp ^ 4u][lane])), base = next == -INFINITY ? 0.0f : next;
+                        const float next = fmaxf(m, fmaxf(top, exchange(top))), base = next == -INFINITY ? 0.0f : next;
                         fade = exp2_fast(m - base);
                         m = next;
                         float total = 0.0f;
@@ -280,11 +288,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
             if (it.blocks && !(ok = fold(1.0f))) break;
             tmem_before_sync();
             if (FWD && !idle) {
-                meet();                                             // both have read the last maximum
-                s_told[warp][lane] = l;
-                meet();
-                l += s_told[warp ^ 4u][lane];
-                meet();                                             // and the sum, before the next item's maximum
+                l += exchange(l);
                 if (part == 0 && row < a.Sq)
                     a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
             }
