@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     extern __shared__ __align__(1024) unsigned char s_raw[];
     struct Bars {
         uint64_t kv_full[8], kv_empty[8], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], tail, drain;
-        uint32_t tmem, abort, busy[16];
+        uint32_t tmem, abort, busy[16], left[16];
     };
     static_assert(sizeof(Bars) <= Smem::kBars && STAGES <= 8, "barriers fit their places");
     Bars &bars = *reinterpret_cast<Bars *>(s_raw);
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     float (*const s_told)[32] = reinterpret_cast<float (*)[32]>(smem + Smem::kKeys + STAGES * Smem::kTile + 16u * Smem::kOut);
     const AttnArgs &a = p.a;
     const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
-    if (threadIdx.x < 16) bars.busy[threadIdx.x] = 0u;
+    if (threadIdx.x < 16) bars.busy[threadIdx.x] = bars.left[threadIdx.x] = 0u;
     if (threadIdx.x == 0) {
         s_abort = 0u;
         bar_init(&tail, 1);
@@ -173,12 +173,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
         const uint32_t w = warp >> 3, part = warp >> 2 & 1u, quarter = (warp & 3u) << 21;   // lane 32 (warp % 4) in the address's upper half
         const uint32_t ts = tmem + w * 128u + part * 64u + quarter, to = tmem + 256u + w * DP + part * (DP / 2) + quarter;
         volatile uint32_t *const busy = bars.busy;
-        const uint32_t meeting = 1u + w * 4u + (warp & 3u);         // barrier of the two warps that share 32 rows
-        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(meeting) : "memory"); };
+        WarpPair pair_of;                                           // the two warps that share 32 rows
+        pair_of.init(bars.left, 1u + w * 4u + (warp & 3u), warp ^ 4u);
         unsigned char *const s_out = smem + Smem::kKeys + STAGES * Smem::kTile + warp * Smem::kOut;
         uint32_t s_ph = 0, pv = 0;                                  // pv: products into O that were handed over, ever
         const float c = a.scale_log2;
-        for (uint32_t item = blockIdx.x; item < p.items; item += gridDim.x) {
+        uint32_t item = blockIdx.x;
+        for (; item < p.items; item += gridDim.x) {
             FwdItem it;
             it.set(p, item);
             const uint32_t first = it.m0 + 128u * w, row = first + (warp & 3u) * 32u + lane;
@@ -228,12 +229,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
                         row_max = fmaxf(fmax3(top[0], top[1], top[2]), top[3]);
                     }
                     s_told[warp][lane] = row_max;
-                    meet();
-                    row_max = fmaxf(row_max, s_told[warp ^ 4u][lane]);
-                    const float block_max = c * row_max;
+                    pair_of.meet_unseen();
+                    const float others = s_told[warp ^ 4u][lane], block_max = c * fmaxf(row_max, others);   // a maximum is never NaN
                     if (j == 0) {
+                        if (!(ok = !pair_of.gone(others))) break;
                         m = fmaxf(block_max, kNoMax);
-                    } else if (__any_sync(0xffffffffu, block_max > m + kLag)) {   // the same in both warps
+                    } else if (__any_sync(0xffffffffu, block_max > m + kLag || others != others)) {   // the same in both warps
+                        if (!(ok = !pair_of.gone(others))) break;
                         const float next = fmaxf(m, block_max), fade = exp2_fast(m - next);
                         m = next;
                         l *= fade;
@@ -289,11 +291,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
             }
             if (!ok) break;
             if (!idle) {
-                meet();                                             // both have read the last maximum
+                if (!pair_of.meet()) break;                         // both have read the last maximum
                 s_told[warp][lane] = l;
-                meet();
+                if (!pair_of.meet()) break;
                 l += s_told[warp ^ 4u][lane];
-                meet();                                             // and the sum, before the next item's maximum
+                if (!pair_of.meet()) break;                         // and the sum, before the next item's maximum
             }
             const float by = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
             if (blocks > 0) {
@@ -344,6 +346,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
             }
             tmem_before_sync();
         }
+        if (item < p.items) pair_of.give_up(warp, lane, &s_told[warp][lane]);
         if (lane == 0) stores_done();
     } else {
         leave_registers<64>();

@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
     extern __shared__ __align__(1024) unsigned char s_raw[];
     struct Bars {
         uint64_t y_full[8], y_empty[8], t_full[2], x_full, x_empty, w_ready, sum_full, drain;
-        uint32_t tmem, abort;
+        uint32_t tmem, abort, left[8];
     };
     static_assert(sizeof(Bars) <= Shape::kBars && SLOTS <= 8, "barriers fit their places");
     Bars &bars = *reinterpret_cast<Bars *>(s_raw);
@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
     float (*const s_told)[32] = reinterpret_cast<float (*)[32]>(s_y + SLOTS * Shape::kY + SLOTS / 2u * Shape::kStats);
     const AttnArgs &a = p.a;
     const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+    if (threadIdx.x < 8) bars.left[threadIdx.x] = 0u;
     if (threadIdx.x == 0) {
         bars.abort = 0u;
         for (uint32_t i = 0; i < SLOTS; i++) {
@@ -138,17 +139,19 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
 
     if (warp < 8) {                                                // ---- probabilities, score gradients, sums
         take_registers<232>();
-        const uint32_t part = warp >> 2, quarter = (warp & 3u) << 21, lane_row = (warp & 3u) * 32u + lane, meeting = 1u + (warp & 3u);
-        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(meeting) : "memory"); };
+        const uint32_t part = warp >> 2, quarter = (warp & 3u) << 21, lane_row = (warp & 3u) * 32u + lane;
+        WarpPair pair_of;                                           // the two warps of a row (they only meet forward)
+        pair_of.init(bars.left, 1u + (warp & 3u), warp ^ 4u);
         // What the other warp of the rows says to this one's value.  Two places in turn: T of the next block may be there before
         // the other warp has read, but who writes for exchange n + 2 has met, at n + 1, the warp that has read n.
         uint32_t told = 0;
-        const auto exchange = [&](float value) {
+        const auto exchange = [&](float value, float &others) {
             float (*const at)[32] = s_told + told;
             told ^= 8u;
             at[warp][lane] = value;
-            meet();
-            return at[warp ^ 4u][lane];
+            if (!pair_of.meet()) return false;
+            others = at[warp ^ 4u][lane];
+            return true;
         };
         const int off = (int)a.Sk - (int)a.Sq;
         uint32_t buf = 0, t_ph = 0, sum_ph = 0, slot = 0, y_ph = 0;
@@ -225,7 +228,9 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
                                 top = fmaxf(top, s[k]);
                             }
                         }
-                        const float next = fmaxf(m, fmaxf(top, exchange(top))), base = next == -INFINITY ? 0.0f : next;
+                        float others = 0.0f;
+                        if (!(ok = exchange(top, others))) break;
+                        const float next = fmaxf(m, fmaxf(top, others)), base = next == -INFINITY ? 0.0f : next;
                         fade = exp2_fast(m - base);
                         m = next;
                         float total = 0.0f;
@@ -288,7 +293,9 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
             if (it.blocks && !(ok = fold(1.0f))) break;
             tmem_before_sync();
             if (FWD && !idle) {
-                l += exchange(l);
+                float others = 0.0f;
+                if (!(ok = exchange(l, others))) break;
+                l += others;
                 if (part == 0 && row < a.Sq)
                     a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
             }
@@ -310,6 +317,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
                                                                   : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
         }
+        if (FWD && !ok) pair_of.give_up(warp, lane, &s_told[warp][lane]);
     } else {
         leave_registers<40>();
         if (warp == 9) {                                           // ---- copies

@@ -56,6 +56,43 @@ __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatil
     return true;
 }
 
+// Two warps that share rows and meet to exchange a number per row.  Either may find in a wait of its own that the CTA gives
+// up, while the other one comes to their next meeting; that must not wait for good.  So a warp that gives up (and only such a
+// one: the other may not have looked behind the last meeting yet) says so and arrives once more without waiting, and a meeting
+// that ended by such an arrival is the other warp's last.  left: a flag of each warp, cleared ahead of the first meeting.  A
+// warp that gives up also puts NaN in the place of its numbers: where those are never NaN themselves, their reader needs no
+// second look (8192 causal tokens, 16 heads of 128: the flag read behind every block's meeting costs 326 us against 315).
+struct WarpPair {
+    uint32_t barrier, other;
+    volatile uint32_t *left;
+    bool alone;
+    __device__ __forceinline__ void init(volatile uint32_t *flags, uint32_t id, uint32_t other_warp)
+    {
+        left = flags;
+        barrier = id;
+        other = other_warp;
+        alone = false;
+    }
+    // behind it, `gone` looks at the number that was read
+    __device__ __forceinline__ void meet_unseen() const { asm volatile("bar.sync %0, 64;" ::"r"(barrier) : "memory"); }
+    __device__ __forceinline__ bool gone(float read) { return alone = __any_sync(0xffffffffu, read != read); }
+    // false: the other warp is gone, and what it last wrote is not what was asked for
+    __device__ __forceinline__ bool meet()
+    {
+        meet_unseen();
+        alone = left[other] != 0u;
+        return !alone;
+    }
+    __device__ __forceinline__ void give_up(uint32_t warp, uint32_t lane, float *place)
+    {
+        if (alone) return;
+        *place = __uint_as_float(0x7FC00000u);
+        if (lane == 0) left[warp] = 1u;
+        __syncwarp();
+        asm volatile("bar.arrive %0, 64;" ::"r"(barrier) : "memory");
+    }
+};
+
 // ---------------------------------------------------------------------------------------------
 // Copies.  A tile is loaded as boxes of 64 16-bit elements (128 bytes, the swizzle's span) times some rows.
 // Coordinates: element (a multiple of 64), head, row, batch.
