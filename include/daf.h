@@ -339,7 +339,10 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
  *   S[i][j] = scale * q_i . k_j,   out_i = sum over visible j of softmax(S[i])[j] v_j,   lse_i = log sum exp S[i][j]
  * Query i of sequence b sees key j if j < key_lengths[b] (all keys when d_key_lengths is NULL; values are clamped to
  * [0, keys]) and, when causal, j <= i + keys - queries.  A row that sees no key has out = 0, lse = -inf and takes and
- * gives no gradient; what lies in k and v beyond a sequence's length is never used, whatever it holds.  Query head h
+ * gives no gradient; what lies in k and v beyond a sequence's length is never used, whatever it holds.  A visible score that
+ * is NaN or +inf, or scores that are all -inf, make the row's out NaN; so does NaN in v for the rows of its 256 queries' tile,
+ * even those that causality keeps from that key.  (Binary32: an infinite element of q, k or v counts as NaN.  16-bit:
+ * scores beyond 2^27 in magnitude may come out as NaN, too.)  Query head h
  * reads key head h / (heads / kv_heads); the gradients of shared heads are summed over their readers.
  *   d_q, d_out, d_grad_out, d_grad_q : [batch, queries, heads, head_dim]
  *   d_k, d_v, d_grad_k, d_grad_v     : [batch, keys, kv_heads, head_dim]

@@ -50,6 +50,13 @@ __device__ __forceinline__ int attn_limit(const AttnArgs &a, uint32_t n, int i)
     return c < (int)n ? c : (int)n;
 }
 
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // binary32 inputs in three bfloat16 planes (at `planes_at`, attn_planes_workspace bytes)
 uint64_t attn_planes_workspace(const AttnArgs &a, bool backward);
 daf_status attn_forward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s);

@@ -297,10 +297,11 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
                 if (!(ok = exchange(l, others))) break;
                 l += others;
                 if (part == 0 && row < a.Sq)
-                    a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+                    a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = limit > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
             }
             const uint32_t rows = DKV ? a.Sk : a.Sq;
-            const bool keep = it.blocks && row < live && (!FWD || l > 0.0f);
+            // forward, what a row sees is told by the mask: a sum that is NaN, or zero of scores that are all -inf, makes NaN
+            const bool keep = it.blocks && row < live && (!FWD || limit > 0);
             const float by = FWD ? __fdiv_rn(1.0f, l) : a.scale;
 #pragma unroll
             for (int c = 0; c < N / 32; c++) {
