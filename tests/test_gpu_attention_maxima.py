@@ -12,7 +12,7 @@ import paper_2507_07149_b200 as daf
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_attention import check, reference  # noqa: E402
+from test_gpu_attention import DTYPES, check, reference  # noqa: E402
 
 
 def moving(dtype, B, Sq, Sk, H, Hkv, D, causal, step, block, lengths=None, seed=0):
@@ -46,3 +46,38 @@ def moving(dtype, B, Sq, Sk, H, Hkv, D, causal, step, block, lengths=None, seed=
 def test_maxima_that_move_with_every_block_binary32(step, D, causal):
     """Blocks of 64 keys: the two warps of a row tell each other another maximum in every block."""
     moving(torch.float32, 2, 300, 450, 4, 2, D, causal, step, 64, lengths=[450, 333])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("step", [7.9, 8.1])
+@pytest.mark.parametrize("D", [40, 64, 80, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_maxima_that_pass_the_references_bound(dtype, step, D, causal):
+    """Blocks of 128 keys whose maxima rise by just less and just more than the 8 units of log2 that the 16-bit kernel lets a
+    maximum pass its reference by before it scales what it has (two steps of 7.9 make it move, too)."""
+    moving(dtype, 2, 300, 700, 4, 2, D, causal, step, 128)
+    moving(dtype, 3, 257, 900, 2, 1, D, causal, step, 128, lengths=[900, 0, 641], seed=1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("step", [0.75, 2.5])
+def test_maxima_that_move_in_calls_split_over_the_keys(dtype, step):
+    """Few rows over many keys: the splits' maxima differ, and move inside a split, too."""
+    moving(dtype, 1, 5, 2100, 2, 1, 64, False, step, 128)
+    moving(dtype, 2, 3, 2100, 1, 1, 128, True, step, 128, lengths=[2100, 1290], seed=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_key_above_all_that_came_before(dtype):
+    """A single late key takes over, in one row of a warp alone: the others' sums keep their bits."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn((1, S, 1, 64), generator=gen, device="cuda").to(dtype) for S in (128, 640, 640))
+    q[..., 0], k[..., 0] = 0, 0
+    want, want_lse = daf.attention(q, k, v)
+    q[0, 77, 0, 0], k[0, 600, 0, 0] = 16, 16                        # 256 / 8 = 32 more for one pair
+    out, lse = daf.attention(q, k, v)
+    rest = torch.arange(128, device="cuda") != 77
+    tell = 2.0 ** -20 * (4 + want_lse.abs())
+    assert ((lse - want_lse).abs() <= tell)[:, :, rest].all() and (lse[0, 0, 77] - (q[0, 77, 0].double() @ k[0, 600, 0].double() / 8)).abs() <= 1e-3
+    u = {torch.float32: 2.0 ** -16, torch.float16: 2.0 ** -10, torch.bfloat16: 2.0 ** -7}[dtype]
+    assert ((out - want).abs()[:, rest] <= u).all() and ((out - v[:, 600:601]).abs()[:, 77] <= u * v[:, 600].abs() + 1e-5).all()
