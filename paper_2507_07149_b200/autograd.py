@@ -145,6 +145,11 @@ class saved_activation_compression(torch.autograd.graph.saved_tensors_hooks):
         self.stats = {"tensors": 0, "bytes_in": 0, "bytes_kept": 0, "passed_through": 0, "dropped": 0, "launches": 0, "shared": 0}
         super().__init__(self._pack, self._unpack)
 
+    @property
+    def coarse(self) -> bool:
+        """Whether what is restored may be far from what was saved: below 8 bits, or with a store (which may drop it)."""
+        return self._store is not None or min(self.bit_budget, float(self.widths[-1])) < 8.0
+
     # ---------------------------------------------------------------------------------------- step bookkeeping
     def reseed(self, seed: int) -> None:
         """New Philox key and a fresh element counter (call once per training step, before the forward pass).  With a
@@ -355,6 +360,13 @@ class saved_activation_compression(torch.autograd.graph.saved_tensors_hooks):
         for i, (h, lay, at) in enumerate(zip(hs, lays, starts)):
             h.block, h.at, h.lay, h.params = block, at, lay[2], daf_params.from_buffer_copy(arr[i])
             h.x = None                                              # the uncompressed tensor can go now
+
+
+def active_compression():
+    """The ``saved_activation_compression`` that gets what is saved now (the innermost context of saved-tensor hooks), or None."""
+    hooks = torch._C._autograd._top_saved_tensors_default_hooks(True)
+    owner = getattr(hooks[0], "__self__", None) if hooks else None
+    return owner if isinstance(owner, saved_activation_compression) else None
 
 
 class _ReluSavedCompressed(torch.autograd.Function):

@@ -3,8 +3,9 @@
 ``attention``, ``residual_norm`` and ``clip_grad_norm_`` run the CUDA kernels behind the C ABI.  Attention keeps q, k, v, its
 output and one float per row for the backward pass, the join keeps its two activations; what they keep goes through
 autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is held in compressed form like every other
-activation.  (Attention's row statistics stay as they are: they are a few bytes per row, and an error there would scale
-whole rows of probabilities.)
+activation.  Attention's row statistics belong to the scores they were taken from: at 8 bits per value they are kept as they
+are, below that (or with a store, which may drop a tensor) the backward pass takes them, and the output, anew from the
+restored q, k and v, at the price of a second forward pass of attention and without keeping the output.
 
     python -m paper_2507_07149_b200.transformer --steps 20            # trains a small classifier on synthetic sequences
     python -m paper_2507_07149_b200.transformer --steps 20 --plain    # the same without compressed activations
@@ -20,21 +21,34 @@ from . import attention as _attention
 from . import attention_grad, clip_grad_norm
 from . import residual_norm as _residual_norm
 from . import residual_norm_grad
+from .autograd import active_compression
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, key_lengths, causal, scale):
         out, lse = _attention(q, k, v, causal=causal, scale=scale, key_lengths=key_lengths)
-        ctx.save_for_backward(q, k, v, out)
+        # Probabilities exp(S' - lse) of restored scores S' with the lse of the exact ones do not sum to one.  Relative error of
+        # the gradient of q (256 tokens, heads of 64, q and k of standard deviation 1 / 2 / 3), lse kept against taken anew:
+        # 8 bits 0.019 0.062 0.14 / 0.018 0.037 0.078, 4 bits 0.34 2.7 120 / 0.31 0.57 0.91, 2 bits 14 3e8 3e20 / 2.5 1.8 1.6.
+        compression = active_compression()
+        if compression is not None and compression.coarse:
+            ctx.save_for_backward(q, k, v)
+            lse = None
+        else:
+            ctx.save_for_backward(q, k, v, out)
         ctx.lse, ctx.key_lengths, ctx.how = lse, key_lengths, (causal, scale)
         return out
 
     @staticmethod
     def backward(ctx, grad_out):
-        q, k, v, out = ctx.saved_tensors
         causal, scale = ctx.how
-        return *attention_grad(q, k, v, out, ctx.lse, grad_out, causal=causal, scale=scale, key_lengths=ctx.key_lengths), None, None, None
+        if ctx.lse is None:
+            q, k, v = ctx.saved_tensors
+            out, lse = _attention(q, k, v, causal=causal, scale=scale, key_lengths=ctx.key_lengths)
+        else:
+            (q, k, v, out), lse = ctx.saved_tensors, ctx.lse
+        return *attention_grad(q, k, v, out, lse, grad_out, causal=causal, scale=scale, key_lengths=ctx.key_lengths), None, None, None
 
 
 def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None):
