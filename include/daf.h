@@ -350,7 +350,8 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
  * elements; the slices of one packed projection are fine): pointers 16-byte aligned, strides of extents above one multiples of
  * 16 bytes, at least head_dim and below 2^36.  d_lse: [batch, heads, queries] floats, contiguous.  d_key_lengths: batch
  * int32.  Softmax statistics and sums are kept in binary32.  16-bit inputs: probabilities and score gradients are rounded
- * to dtype where they enter the second products; binary32 inputs: every factor keeps its 24 bits (three bfloat16 parts).
+ * to dtype where they enter the second products (float16: scaled by powers of two, so that neither the size of v nor that of a
+ * row's grad_out matters to grad_q, nor the size of a head's largest row to grad_k); binary32 inputs: every factor keeps its 24 bits (three bfloat16 parts).
  * heads a multiple of kv_heads, head_dim a multiple of 8 (DAF_ERR_SHAPE), head_dim <= 128, queries and keys <= 2^24,
  * batch * heads <= 65535, batch * heads * queries and batch * kv_heads * keys <= 2^32 (DAF_ERR_UNSUPPORTED).
  * batch, queries or keys == 0 are valid.

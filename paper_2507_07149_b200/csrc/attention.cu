@@ -72,11 +72,14 @@ uint32_t attn_splits(const AttnArgs &a)
     return (uint32_t)(room < most ? room : most);
 }
 
-// -lse and -delta of every row
-static uint64_t rows_bytes(const daf_attention_params *p) { return 2ull * p->batch * p->heads * padded_rows(p->queries) * sizeof(float); }
+// -lse and -delta of every row, for float16 the squared norm of its grad_out, too
+static uint64_t rows_bytes(const daf_attention_params *p)
+{
+    return (p->dtype == DAF_F16 ? 3ull : 2ull) * p->batch * p->heads * padded_rows(p->queries) * sizeof(float);
+}
 static uint64_t maxima_bytes(const daf_attention_params *p)
 {
-    return p->dtype == DAF_F16 ? ((uint64_t)p->batch * p->kv_heads * sizeof(float) + 255u) & ~255ull : 0u;
+    return p->dtype == DAF_F16 ? (2ull * p->batch * p->kv_heads * sizeof(float) + 255u) & ~255ull : 0u;
 }
 
 static AttnArgs args_of(const daf_attention_params *p)
@@ -183,7 +186,9 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     a.row_ndelta = a.row_nl2 + (uint64_t)a.B * a.H * a.rows_padded;
     WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    a.grad_max = a.row_ndelta + (uint64_t)a.B * a.H * a.rows_padded;
+    a.row_norm2 = a.row_ndelta + (uint64_t)a.B * a.H * a.rows_padded;
+    a.grad_max = a.row_norm2 + (uint64_t)a.B * a.H * a.rows_padded;
+    a.value_max = a.grad_max + (uint64_t)a.B * a.Hkv;
     if (maxima_bytes(params) && cudaMemsetAsync(a.grad_max, 0, maxima_bytes(params), s) != cudaSuccess) return DAF_ERR_CUDA;
     if (p.queries) {
         const daf_status rows = attn_rows(p.dtype, a, header, s);

@@ -30,7 +30,9 @@ struct AttnArgs {
     float *lse;                  // [B, H, Sq]: natural logarithm of each row's sum of exponentials, -inf for a row that sees no key
     const int32_t *lengths;      // keys of each sequence, or null
     float *row_nl2, *row_ndelta; // backward workspace, [B, H, rows_padded]: see attention_rows_kernel
-    float *grad_max;             // float16 backward: [B, Hkv], the largest squared norm of the grad_out rows that meet a key head
+    // float16 backward: squared norms of the rows of grad_out, [B, H, rows_padded], and [B, Hkv] each their maximum over the rows
+    // that meet a key head and a bound of v's
+    float *row_norm2, *grad_max, *value_max;
     uint32_t B, Sq, Sk, H, Hkv, D, group, causal, rows_padded;
     float scale, scale_log2;     // scale_log2 = scale * log2(e)
 };
@@ -61,6 +63,8 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
 uint64_t attn_planes_workspace(const AttnArgs &a, bool backward);
 daf_status attn_forward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_backward_planes(const AttnArgs &a, char *planes_at, WorkspaceHeader *header, cudaStream_t s);
+// float16 backward: P is held 2^8 times its size, so that probabilities down to 2^-22 keep their bits.
+constexpr float kHalfLift = 8.0f;
 daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 daf_status attn_zero(uint32_t dtype, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, cudaStream_t s);
 // Into how many runs of key blocks a 16-bit forward call cuts each of its row tiles: 1, or as many as fill a B200 where the

@@ -19,8 +19,10 @@ template <typename T> __device__ __forceinline__ void load8_any(const void *p, f
 
 // What the backward kernels need of each row, D / 8 lanes (rounded up to a power of two) per row, 128 rows of a head per
 // CTA: -lse in units of log2, -inf for rows that see nothing and for the padding (their probabilities then come out as
-// exp2(-inf) = 0), and -delta = -sum(grad_out * out).  float16 also notes the largest |grad_out|^2 of a key head's readers
-// (a maximum of non-negative floats by their bits: the order of the atomics changes nothing).
+// exp2(-inf) = 0), and -delta = -sum(grad_out * out).  float16 also notes |grad_out|^2 of the row and the largest one of a key
+// head's readers, rows that see nothing left out, and a bound of a key head's |v|^2, D times the largest square (maxima of
+// non-negative floats by their bits: the order of the atomics changes nothing).  Reading v for that costs float16 calls 2 to 4 %
+// (16 x 509 tokens, 16 heads of 80: 145 -> 151 us); CTAs of their own for v 8 %.
 template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_rows_kernel(const __grid_constant__ AttnArgs a, uint32_t lanes, WorkspaceHeader *header)
 {
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) header->status = 0u;
@@ -29,6 +31,23 @@ template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_r
     const bool reads = lane * 8u < a.D;
     constexpr bool F16 = __is_same(T, __half);
     float most = 0.0f;
+    // the same rows of v, by the first of the query heads that read them
+    if (F16 && first < a.Sk && h % a.group == 0) {
+        const uint32_t n = attn_length(a, b), head = b * a.Hkv + h / a.group;
+        const T *const v = reinterpret_cast<const T *>(a.v.p) + a.v.sb * b + a.v.sh * (h / a.group) + lane * 8u;
+        uint32_t two = 0u;                                         // the largest |v|, by the bits, in each half
+#pragma unroll 8
+        for (uint32_t r = first + threadIdx.x / lanes; r < first + kRowsPerCta; r += per)
+            if (r < n && reads) {
+                const uint4 u = __ldg(reinterpret_cast<const uint4 *>(v + a.v.ss * r));
+                two = __vmaxu2(__vmaxu2(two, u.x & 0x7FFF7FFFu), u.y & 0x7FFF7FFFu);
+                two = __vmaxu2(__vmaxu2(two, u.z & 0x7FFF7FFFu), u.w & 0x7FFF7FFFu);
+            }
+        const uint32_t top = __reduce_max_sync(0xffffffffu, __vmaxu2(two, two >> 16) & 0xFFFFu);
+        const float largest = __half2float(__ushort_as_half((unsigned short)top));
+        if ((threadIdx.x & 31u) == 0) atomicMax(reinterpret_cast<uint32_t *>(a.value_max) + head, __float_as_uint((float)a.D * largest * largest));
+    }
+    if (F16 && first >= a.rows_padded) return;
     const T *const o = reinterpret_cast<const T *>(a.out.p) + a.out.sb * b + a.out.sh * h + lane * 8u;
     const T *const g = reinterpret_cast<const T *>(a.grad_out.p) + a.grad_out.sb * b + a.grad_out.sh * h + lane * 8u;
 #pragma unroll 4
@@ -37,7 +56,7 @@ template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_r
         float nl2 = -INFINITY, delta = 0.0f, norm = 0.0f;
         if (i < a.Sq) {
             const float l = a.lse[(uint64_t)bh * a.Sq + i];
-            if (l != -INFINITY) nl2 = -l * 1.4426950408889634f;
+            if (l != -INFINITY) nl2 = -l * 1.4426950408889634f + (F16 ? kHalfLift : 0.0f);
             if (reads) {
                 float x[8], y[8];
                 load8_any<T>(o + a.out.ss * i, x);
@@ -53,8 +72,10 @@ template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_r
             delta += __shfl_xor_sync(0xffffffffu, delta, d);
             if (F16) norm += __shfl_xor_sync(0xffffffffu, norm, d);
         }
+        if (F16 && nl2 == -INFINITY) norm = 0.0f;
         most = fmaxf(most, norm);
         if (lane == 0) {
+            if (F16) a.row_norm2[(uint64_t)bh * a.rows_padded + i] = norm;
             a.row_nl2[(uint64_t)bh * a.rows_padded + i] = nl2;
             a.row_ndelta[(uint64_t)bh * a.rows_padded + i] = -delta;
         }
@@ -69,7 +90,8 @@ daf_status attn_rows(uint32_t dtype, const AttnArgs &a, WorkspaceHeader *header,
 {
     uint32_t lanes = 1;
     while (lanes * 8u < a.D) lanes *= 2u;
-    const dim3 grid(a.rows_padded / kRowsPerCta, a.B * a.H);
+    const uint32_t tiles = a.rows_padded / kRowsPerCta, key_tiles = dtype == DAF_F16 ? (a.Sk + kRowsPerCta - 1u) / kRowsPerCta : 0u;
+    const dim3 grid(tiles > key_tiles ? tiles : key_tiles, a.B * a.H);
     if (dtype == DAF_F32) attention_rows_kernel<float><<<grid, kRowThreads, 0, s>>>(a, lanes, header);
     else if (dtype == DAF_F16) attention_rows_kernel<__half><<<grid, kRowThreads, 0, s>>>(a, lanes, header);
     else attention_rows_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, s>>>(a, lanes, header);

@@ -16,10 +16,10 @@
 // second product, about 2500 cycles of latency --, so blocks in flight matter more than the wider products that blocks
 // of 128 would give, and eight warps per block more than long rows in few threads.
 // P and dS are rounded to the input type, which the second products need; everything else is binary32.  float16 reaches
-// from 6e-5 (6e-8 with fewer bits) to 65504, and dS may lie anywhere -- a mean over many tokens or a loss scale moves all
-// of grad_out --, so there dS is multiplied by the power of two that brings the largest |grad_out| row of the head to
-// [16, 32), and the sums by its inverse: |dS| <= 2 |grad_out| |v| P stays below 65504 for rows of v up to 1000, and
-// probabilities of 1e-4 keep their bits.
+// from 6e-5 (6e-8 with fewer bits) to 65504, and dS may lie anywhere -- a mean over many tokens, a loss on a few of them or a
+// loss scale moves grad_out --, so there dS is multiplied by the power of two that brings its bound 2 |grad_out| max |v| to
+// [2^14, 2^15) (max |v| taken as sqrt(D) times the largest element), and the sums by its inverse: |grad_out| is the row's in dq, whose sums belong to one row, and the largest row's
+// of the head in dk.  P is held 2^8 times its size: probabilities down to 2^-22 keep their bits.
 #pragma once
 #include "attention.cuh"
 #include "tensor_core.cuh"
@@ -49,11 +49,11 @@ template <int DP, bool DKV> struct GradSmem {
     static constexpr uint32_t kBytes = kBars + kHeldBuffers * 2u * kX + kStages * (2u * kY + kStats) + 16u * kOut;
 };
 
-// That power of two, from the largest squared norm (1 where there is none).
-__device__ __forceinline__ float score_grad_scale(float most)
+// That power of two, from the squared norms of grad_out and v (1 where one is zero or not finite).
+__device__ __forceinline__ float score_grad_scale(float grad2, float value2)
 {
-    const int e = (int)(__float_as_uint(sqrtf(most)) >> 23) - 131;
-    return e < -100 || e > 100 ? 1.0f : __uint_as_float((uint32_t)(127 - e) << 23);
+    const int e = (int)(__float_as_uint(sqrtf(grad2) * sqrtf(value2)) >> 23) - 127;
+    return e < -100 || e > 100 ? 1.0f : __uint_as_float((uint32_t)(127 + 13 - e) << 23);
 }
 
 // The i-th item of a CTA: there and back over the list, which starts with the longest items, so that who got a long
@@ -217,7 +217,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 const uint32_t item = grad_item(turn);
                 if (item >= p.items) continue;
                 it.set(p, item);
-                if (F16) lift = score_grad_scale(a.grad_max[it.b * a.Hkv + (DKV ? it.h : it.h / a.group)]);
+                if (F16) {
+                    const uint32_t head = it.b * a.Hkv + (DKV ? it.h : it.h / a.group);
+                    const float grad2 = DKV ? a.grad_max[head] : a.row_norm2[((uint64_t)it.b * a.H + it.h) * a.rows_padded + it.first + lane_row];
+                    lift = score_grad_scale(grad2, a.value_max[head]);
+                }
                 if (!DKV && it.blocks) {
                     const uint64_t at = ((uint64_t)it.b * a.H + it.h) * a.rows_padded + it.first + lane_row;
                     nl = a.row_nl2[at];
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                                 unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
                                 u = exp2_fast(u);
                                 v = exp2_fast(v);
-                                const uint64_t pr = F16 ? mul2(pair(u, v), both(lift)) : pair(u, v);
+                                const uint64_t pr = F16 ? mul2(pair(u, v), both(lift * exp2f(-kHalfLift))) : pair(u, v);
                                 unpair(mul2(pr, add2(pair(e[c], e[c + 1]), d2[q])), x, y);
                                 r1[2 * k + q] = round2<T>(u, v);
                                 r2[2 * k + q] = round2<T>(x, y);
@@ -315,7 +319,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             // DKV: warpgroups 0 and 2 store dv, 1 and 3 dk, half of the columns each; dq: 32 columns each, as far as they go
             const uint32_t group = warp >> 2;
             const CUtensorMap *const to = &p.out[DKV ? group & 1u : 0u];
-            const float by = DKV && !(group & 1u) ? 1.0f : F16 ? __fdiv_rn(a.scale, lift) : a.scale;
+            const float by = DKV && !(group & 1u) ? (F16 ? exp2f(-kHalfLift) : 1.0f) : F16 ? __fdiv_rn(a.scale, lift) : a.scale;
             constexpr uint32_t WIDTH = DKV ? DP / 2 : 32;
             const uint32_t from = (DKV ? group >> 1 : group) * WIDTH;
             const uint32_t acc = tmem + (DKV ? (group & 1u) * DP : 0u) + from + quarter;
