@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t right_plane(uint32_t c) { return 0x001021u >
 struct SplitTensor {
     AttnTensor from;
     __nv_bfloat16 *to;                           // [B, S, H, 3, D]
-    uint32_t S, H, short_rows;                   // short_rows: rows behind the sequence's length become zero
+    uint32_t S, H, keys;                         // keys: a row is one of k or v, not of q or grad_out
     uint32_t rows;                               // B S H
 };
 struct SplitArgs {
@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(256) split_planes_kernel(const __grid_constant
     for (uint32_t r = blockIdx.x * lanes + first; r < t.rows; r += gridDim.x * lanes) {
         const uint32_t bs = r / t.H, h = r - bs * t.H, b = bs / t.S, s = bs - b * t.S;
         uint4 out[3] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
-        if (!t.short_rows || s < attn_length(p.a, b)) {
+        const uint32_t n = attn_length(p.a, b);
+        if (t.keys ? s < n : attn_limit(p.a, n, (int)s) > 0) {      // what nobody sees, and what sees nothing, becomes zero
             const float4 *src = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(t.from.p) + t.from.sb * b + t.from.ss * s + t.from.sh * h + d * 8u);
             const float4 x = __ldg(src), y = __ldg(src + 1);
             split3(x.x, x.y, out[0].x, out[1].x, out[2].x);
@@ -300,8 +301,8 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
                     a.lse[((uint64_t)it.b * a.H + it.h) * a.Sq + row] = limit > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
             }
             const uint32_t rows = DKV ? a.Sk : a.Sq;
-            // forward, what a row sees is told by the mask: a sum that is NaN, or zero of scores that are all -inf, makes NaN
-            const bool keep = it.blocks && row < live && (!FWD || limit > 0);
+            // what a row sees is told by the mask: forward, a sum that is NaN, or zero of scores that are all -inf, makes NaN
+            const bool keep = it.blocks && row < live && (DKV || limit > 0);
             const float by = FWD ? __fdiv_rn(1.0f, l) : a.scale;
 #pragma unroll
             for (int c = 0; c < N / 32; c++) {

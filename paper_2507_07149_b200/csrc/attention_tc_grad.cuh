@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             constexpr uint32_t WIDTH = DKV ? DP / 2 : 32;
             const uint32_t from = (DKV ? group >> 1 : group) * WIDTH;
             const uint32_t acc = tmem + (DKV ? (group & 1u) * DP : 0u) + from + quarter;
-            const bool some = it.blocks > 0, any = some && !idle, keep = any && row < live;
+            const bool some = it.blocks > 0, any = some && !idle, keep = any && row < live && (DKV || limit > 0);
             const uint32_t out_h = it.h, out_b = it.b, out_row = it.first + (warp & 3u) * 32u;
             const bool exists = out_row < rows && from < a.D;
             turn++;
@@ -393,9 +393,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 }
                 if (!bar_wait(&y_empty[st], ph, stop)) break;
                 const uint32_t cols = cur.cols(p), end = (cols + 15u) & ~15u;
-                // dS is zero in a masked column, but 0 * NaN is not: rows of k behind the sequence's end that the last
-                // product's steps of 16 keys still touch are cleared
-                const bool clear = !DKV && cur.it.n < a.Sk && cols != end;
+                // P and dS are zero in a masked column, but 0 * NaN is not.  Cleared are rows of k behind the sequence's end that
+                // the last product's steps of 16 keys still touch, and rows of q and grad_out that see no key at all.
+                const int dead = DKV && a.causal ? (int)(a.Sq - cur.row) - (int)a.Sk : 0;
+                const uint32_t clear_from = DKV ? 0u : cols, clear_to = !DKV ? (cur.it.n < a.Sk ? end : cols) : dead <= 0 ? 0u : dead < (int)kWalk ? (uint32_t)dead : kWalk;
+                const bool clear = clear_from != clear_to;
                 uint64_t *const bar = clear ? &tail : &y_full[st];
                 unsigned char *const dst = s_y + st * 2u * Smem::kY;
                 if (one) {
@@ -413,9 +415,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 if (clear) {
                     if (!bar_wait(&tail, tail_ph, stop)) break;
                     tail_ph ^= 1u;
-                    for (uint32_t i = lane; i < (end - cols) * 8u * (DP / 64); i += 32u)
-                        *reinterpret_cast<uint4 *>(dst + i / (8u * (end - cols)) * YBOX + (cols * 8u + i % (8u * (end - cols))) * 16u) =
-                            make_uint4(0u, 0u, 0u, 0u);
+                    const uint32_t pieces = 8u * (clear_to - clear_from);
+                    for (uint32_t i = lane; i < pieces * (DP / 64) * (DKV ? 2u : 1u); i += 32u)    // boxes follow one another
+                        *reinterpret_cast<uint4 *>(dst + i / pieces * YBOX + (clear_from * 8u + i % pieces) * 16u) = make_uint4(0u, 0u, 0u, 0u);
                     fence_async();
                     __syncwarp();
                     if (one) bar_arrive(&y_full[st]);

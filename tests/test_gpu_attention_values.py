@@ -112,3 +112,37 @@ def test_backward_follows(dtype):
     out, lse = daf.attention(q, k, v)
     for t in daf.attention_grad(q, k, v, out, lse, torch.ones_like(out)):
         assert t[:, :, 0].isnan().any() and t[:, :, 1].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Sq,Sk,lengths", [(300, 100, None), (130, 1, None), (200, 150, [150, 0])])
+def test_whatever_a_row_that_sees_nothing_holds(dtype, D, Sq, Sk, lengths):
+    """Causal rows ahead of the first key, sequences without keys: NaN and infinities in their q, out and grad_out change nothing."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    B = 1 if lengths is None else len(lengths)
+    q, g = (torch.randn((B, Sq, 2, D), generator=gen, device="cuda").to(dtype) for _ in range(2))
+    k, v = (torch.randn((B, Sk, 1, D), generator=gen, device="cuda").to(dtype) for _ in range(2))
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out, lse = daf.attention(q, k, v, causal=True, key_lengths=lens)
+    want = daf.attention_grad(q, k, v, out, lse, g, causal=True, key_lengths=lens)
+    dead = torch.zeros(B, Sq, dtype=torch.bool, device="cuda")
+    dead[:, :Sq - Sk] = True
+    if lengths is not None:
+        dead[1] = True
+    assert dead.any()
+    for bad in (math.nan, math.inf):
+        q2, g2, out2 = (t.clone() for t in (q, g, out))
+        q2[dead], g2[dead], out2[dead] = bad, bad, bad
+        a, b = daf.attention(q2, k, v, causal=True, key_lengths=lens)
+        assert torch.equal(a, out) and torch.equal(b, lse)
+        got = daf.attention_grad(q2, k, v, out2, lse, g2, causal=True, key_lengths=lens)
+        for t, w in zip(got, want):
+            assert torch.equal(t, w)
+    # and keys that are not numbers reach the rows that see them, not these
+    if Sk > 1 and lengths is None:
+        k2 = k.clone()
+        k2[:, -1] = math.nan
+        a, b = daf.attention(q, k2, v, causal=True)
+        gq, _, _ = daf.attention_grad(q, k2, v, a, b, g, causal=True)
+        assert (gq[dead] == 0).all() and (a[dead] == 0).all() and (b.transpose(1, 2)[dead] == -math.inf).all()
