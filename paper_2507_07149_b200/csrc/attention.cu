@@ -82,6 +82,13 @@ static uint64_t maxima_bytes(const daf_attention_params *p)
     return p->dtype == DAF_F16 ? (2ull * p->batch * p->kv_heads * sizeof(float) + 255u) & ~255ull : 0u;
 }
 
+// A call with nothing to do: its workspace, which may be missing, says so.
+static daf_status no_work(void *d_workspace, uint64_t workspace_bytes, daf_stream stream)
+{
+    if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 15u) || workspace_bytes < sizeof(uint32_t)) return DAF_OK;
+    return cudaMemsetAsync(d_workspace, 0, sizeof(uint32_t), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
+
 static AttnArgs args_of(const daf_attention_params *p)
 {
     AttnArgs a = {};
@@ -121,7 +128,7 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
     const daf_attention_params &p = *params;
     const uint32_t eb = p.dtype == DAF_F32 ? 4u : 2u;
     if (reinterpret_cast<uintptr_t>(d_key_lengths) & 3u) return DAF_ERR_INVALID_ARG;
-    if (p.batch == 0 || p.queries == 0) return DAF_OK;
+    if (p.batch == 0 || p.queries == 0) return no_work(d_workspace, workspace_bytes, stream);
     if (!tensor_ok(d_q, p.q_stride, p.batch, p.queries, p.heads, p.head_dim, eb) || !d_lse || (reinterpret_cast<uintptr_t>(d_lse) & 3u) ||
         !tensor_ok(d_out, p.out_stride, p.batch, p.queries, p.heads, p.head_dim, eb) ||
         (p.keys && (!tensor_ok(d_k, p.k_stride, p.batch, p.keys, p.kv_heads, p.head_dim, eb) ||
@@ -158,7 +165,7 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     const daf_attention_params &p = *params;
     const uint32_t eb = p.dtype == DAF_F32 ? 4u : 2u;
     if (reinterpret_cast<uintptr_t>(d_key_lengths) & 3u) return DAF_ERR_INVALID_ARG;
-    if (p.batch == 0 || (p.queries == 0 && p.keys == 0)) return DAF_OK;
+    if (p.batch == 0 || (p.queries == 0 && p.keys == 0)) return no_work(d_workspace, workspace_bytes, stream);
     if (p.queries && (!tensor_ok(d_q, p.q_stride, p.batch, p.queries, p.heads, p.head_dim, eb) || !d_lse || (reinterpret_cast<uintptr_t>(d_lse) & 3u) ||
                       !tensor_ok(d_out, p.out_stride, p.batch, p.queries, p.heads, p.head_dim, eb) ||
                       !tensor_ok(d_grad_out, p.grad_out_stride, p.batch, p.queries, p.heads, p.head_dim, eb) ||

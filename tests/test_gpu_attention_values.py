@@ -146,3 +146,20 @@ def test_whatever_a_row_that_sees_nothing_holds(dtype, D, Sq, Sk, lengths):
         a, b = daf.attention(q, k2, v, causal=True)
         gq, _, _ = daf.attention_grad(q, k2, v, a, b, g, causal=True)
         assert (gq[dead] == 0).all() and (a[dead] == 0).all() and (b.transpose(1, 2)[dead] == -math.inf).all()
+
+
+@pytest.mark.parametrize("batch,queries,keys", [(0, 5, 5), (2, 0, 5), (2, 0, 0), (2, 5, 0)])
+def test_a_call_without_work_leaves_a_status_too(batch, queries, keys):
+    """The workspace holds the status word behind every call that returned DAF_OK, whatever lay there before."""
+    import ctypes
+    p = daf.daf_attention_params(ctypes.sizeof(daf.daf_attention_params), daf.BF16, batch, queries, keys, 2, 2, 64, 0, 0.125)
+    for name, n in (("q", queries), ("k", keys), ("v", keys), ("out", queries), ("grad_out", queries), ("grad_q", queries), ("grad_k", keys), ("grad_v", keys)):
+        getattr(p, name + "_stride")[:] = (max(n, 1) * 128, 128, 64)
+    x = torch.zeros(2, 5, 2, 64, dtype=torch.bfloat16, device="cuda")
+    y, lse = torch.zeros_like(x), torch.zeros(2, 2, 5, device="cuda")
+    ws = torch.full((max(daf.daf_attention_workspace(p), daf.daf_attention_grad_workspace(p), 256),), 0xFF, dtype=torch.uint8, device="cuda")
+    daf.daf_attention(p, x, x, x, None, y, lse, ws, ws.numel())
+    assert daf.daf_poll_status(ws) == daf.OK
+    ws.fill_(0xFF)
+    daf.daf_attention_grad(p, x, x, x, None, x, lse, x, y, y, y, ws, ws.numel())
+    assert daf.daf_poll_status(ws) == daf.OK
