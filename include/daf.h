@@ -20,8 +20,8 @@
  *   - Device pointers must be 16-byte aligned unless stated otherwise.
  *   - No entry point throws.  State the library keeps between calls: a table, one entry per
  *     (kernel, device), of how many CTAs of that kernel the device holds at once, filled at
- *     the first launch on each device and guarded by a mutex; and the scratch array of
- *     daf_compress_static.  Entry points may be called from several threads and on several
+ *     the first launch on each device and guarded by a mutex; the scratch array of
+ *     daf_compress_static; and a word of each device for daf_device_status.  Entry points may be called from several threads and on several
  *     devices at once (work goes to the device that is current in the calling thread) as
  *     long as calls that overlap on the GPU use different workspaces.  daf_pool and
  *     daf_store objects are not thread safe: one thread at a time per object.
@@ -245,6 +245,15 @@ daf_status daf_group_offsets_diag(const uint8_t *d_bits, uint64_t n_groups, uint
  * DAF_ERR_TIMEOUT (DAF_ERR_CUDA if the copy itself fails).
  */
 daf_status daf_poll_status(const void *d_workspace, daf_stream stream);
+
+/*
+ * The same for callers who do not keep the workspaces of the calls they make (daf_attention, daf_attention_grad): waits for
+ * `stream` and returns the largest device-side error that any such call on the current device has recorded since the last
+ * daf_device_status, DAF_OK if none has.  daf_device_status_word: the address of that word (one uint32 in device memory), for
+ * who wants to look at it from the device or to read it together with results.
+ */
+daf_status daf_device_status(daf_stream stream);
+daf_status daf_device_status_word(uint32_t **d_word);
 
 /*
  * Batched forms for sets of activations (one launch per up to DAF_BATCH_MAX tensors): the

@@ -119,6 +119,8 @@ SIGNATURES = {
     "daf_tensor_compress": (ctypes.c_int, [ctypes.c_uint32, _vp, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint32,
                                            ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
     "daf_tensor_decompress": (ctypes.c_int, [ctypes.c_uint32, _vp, ctypes.c_uint64, ctypes.c_uint32, _vp, _vp, _vp]),
+    "daf_device_status": (ctypes.c_int, [_vp]),
+    "daf_device_status_word": (ctypes.c_int, [ctypes.POINTER(_vp)]),
     "daf_attention": (ctypes.c_int, [ctypes.POINTER(daf_attention_params)] + [_vp] * 7 + [ctypes.c_uint64, _vp]),
     "daf_attention_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_attention_params)]),
     "daf_attention_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_attention_params)]),
@@ -346,6 +348,28 @@ def daf_group_offsets_diag(d_bits, n_groups, group_size, d_offsets, d_ws, ws_byt
 
 def daf_poll_status(d_workspace, stream=None) -> int:
     return _call(lib().daf_poll_status, d_workspace, stream, _ptr(d_workspace))
+
+
+def daf_device_status(device=None, stream=None) -> int:
+    """The largest error that an attention call on `device` (the current one) has recorded since the last such question."""
+    torch = _torch()
+    with torch.cuda.device(device):                                  # None: stays
+        return int(lib().daf_device_status(_raw_stream(torch.cuda.current_device(), stream)))
+
+
+def daf_device_status_word(device=None) -> int:
+    """The device address of the word that daf_device_status reads."""
+    word = _vp()
+    with _torch().cuda.device(device):
+        _check(int(lib().daf_device_status_word(ctypes.byref(word))), "daf_device_status_word")
+    return word.value
+
+
+def check_device(device=None, stream=None) -> None:
+    """Waits for the stream and raises if an attention call on `device` gave up since the last question.  ``attention`` and
+    ``attention_grad`` do not wait for the device (unless called with check) and keep nothing that could be asked later, so ask
+    here once a step or once an epoch."""
+    _check(daf_device_status(device, stream), "attention (device status)")
 
 
 def _ptr_array(tensors):
@@ -593,7 +617,7 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     exponentials [B, H, Sq] that the backward pass needs (daf_attention).  Slices of a packed projection are read in place;
     tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
     first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq.  check waits
-    for the device and raises on an error there.  With a stream, results and scratch belong to that stream."""
+    for the device and raises on an error there (without it, ``check_device`` tells later).  With a stream, results and scratch belong to that stream."""
     if stream is not None:
         with _torch().cuda.stream(stream):
             return attention(q, k, v, causal=causal, scale=scale, key_lengths=key_lengths, out=out, lse=lse, check=check)

@@ -46,7 +46,7 @@ import torch
 
 import ctypes
 
-from . import (ACT_GELU, ACT_RELU, ACT_RELU6, BATCH_MAX, ROUND_STOCHASTIC, Store, _call, _check, daf_params, daf_poll_status,
+from . import (ACT_GELU, ACT_RELU, ACT_RELU6, BATCH_MAX, ROUND_STOCHASTIC, Store, _call, _check, check_device, daf_params, daf_poll_status,
                daf_sizes, dtype_code, lib, make_params)
 
 _DTYPES = (torch.float32, torch.float16, torch.bfloat16)
@@ -182,11 +182,14 @@ class saved_activation_compression(torch.autograd.graph.saved_tensors_hooks):
         return super().__enter__()
 
     def check_status(self) -> None:
-        """Waits for the work queued so far and raises if a batch recorded a device-side error."""
+        """Waits for the work queued so far and raises if a batch, or an attention call on its device or the current one, recorded
+        a device-side error."""
         self.flush()
         ws, self._workspaces = self._workspaces, []
         for w in ws:
             _check(daf_poll_status(w), "daf_compress_batch (device status)")
+        for index in sorted({w.get_device() for w in ws} | {torch.cuda.current_device()}):
+            check_device(index)
 
     def __exit__(self, *exc):
         out = super().__exit__(*exc)

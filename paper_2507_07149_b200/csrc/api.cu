@@ -33,6 +33,14 @@ cudaError_t persistent_ctas(const void *kernel, int threads, int dyn_smem, int *
     return (cudaError_t)err;
 }
 
+__device__ unsigned int g_device_status;
+
+unsigned int *device_status_word()
+{
+    void *word = nullptr;
+    return cudaGetSymbolAddress(&word, g_device_status) == cudaSuccess ? static_cast<unsigned int *>(word) : nullptr;
+}
+
 static bool is_pow2(uint32_t v) { return v && !(v & (v - 1)); }
 
 // Importance per stored bit of raising a group from width lo to width hi: with a uniform
@@ -131,6 +139,22 @@ extern "C" daf_status daf_poll_status(const void *d_workspace, daf_stream stream
     if (cudaMemcpyAsync(&status, d_workspace, sizeof(status), cudaMemcpyDeviceToHost, s) != cudaSuccess) return DAF_ERR_CUDA;
     if (cudaStreamSynchronize(s) != cudaSuccess) return DAF_ERR_CUDA;
     return status <= DAF_ERR_UNSUPPORTED ? (daf_status)status : DAF_ERR_CUDA;
+}
+
+extern "C" daf_status daf_device_status_word(uint32_t **d_word)
+{
+    if (!d_word) return DAF_ERR_INVALID_ARG;
+    *d_word = device_status_word();
+    return *d_word ? DAF_OK : DAF_ERR_CUDA;
+}
+
+extern "C" daf_status daf_device_status(daf_stream stream)
+{
+    uint32_t *const word = device_status_word();
+    if (!word) return DAF_ERR_CUDA;
+    const daf_status status = daf_poll_status(word, stream);
+    if (status != DAF_OK && cudaMemsetAsync(word, 0, sizeof(*word), reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) return DAF_ERR_CUDA;
+    return status;
 }
 
 extern "C" const char *daf_status_string(daf_status status)

@@ -143,6 +143,7 @@ extern "C" daf_status daf_attention(const daf_attention_params *params, const vo
     a.out = tensor_of(d_out, p.out_stride);
     a.lse = d_lse;
     a.lengths = d_key_lengths;
+    if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
     WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     return p.dtype == DAF_F32 ? attn_forward_planes(a, reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader), header, s)
@@ -189,6 +190,7 @@ extern "C" daf_status daf_attention_grad(const daf_attention_params *params, con
     a.dv = tensor_of(d_grad_v, p.grad_v_stride);
     a.lse = const_cast<float *>(d_lse);
     a.lengths = d_key_lengths;
+    if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
     a.row_nl2 = reinterpret_cast<float *>(reinterpret_cast<char *>(d_workspace) + sizeof(WorkspaceHeader));
     a.row_ndelta = a.row_nl2 + (uint64_t)a.B * a.H * a.rows_padded;
     WorkspaceHeader *const header = reinterpret_cast<WorkspaceHeader *>(d_workspace);

@@ -33,6 +33,7 @@ struct AttnArgs {
     // float16 backward: squared norms of the rows of grad_out, [B, H, rows_padded], and [B, Hkv] each their maximum over the rows
     // that meet a key head and a bound of v's
     float *row_norm2, *grad_max, *value_max;
+    unsigned int *device_status; // see record_error
     uint32_t B, Sq, Sk, H, Hkv, D, group, causal, rows_padded;
     float scale, scale_log2;     // scale_log2 = scale * log2(e)
 };

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     uint64_t &tail = bars.tail, &drain = bars.drain;
     uint32_t &s_tmem = bars.tmem, &s_abort = bars.abort;
     if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
-        if (threadIdx.x == 0) p.header->status = DAF_ERR_UNSUPPORTED;
+        if (threadIdx.x == 0) record_error(p.header, p.a.device_status, DAF_ERR_UNSUPPORTED);
         return;
     }
     unsigned char *const smem = s_raw + Smem::kBars;
@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_kernel(const __grid_
     }
     tmem_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && s_abort) p.header->status = DAF_ERR_TIMEOUT;
+    if (threadIdx.x == 0 && s_abort) record_error(p.header, p.a.device_status, DAF_ERR_TIMEOUT);
     if (warp == 0) tmem_free(tmem, 512);
 }
 

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
     static_assert(sizeof(Bars) <= Shape::kBars && SLOTS <= 8, "barriers fit their places");
     Bars &bars = *reinterpret_cast<Bars *>(s_raw);
     if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
-        if (threadIdx.x == 0) p.header->status = DAF_ERR_UNSUPPORTED;
+        if (threadIdx.x == 0) record_error(p.header, p.a.device_status, DAF_ERR_UNSUPPORTED);
         return;
     }
     unsigned char *const s_x = s_raw + Shape::kBars, *const s_y = s_x + Shape::kHeldTiles * Shape::kX;
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(kPlaneThreads, 1) attention_planes_kernel(cons
     }
     tmem_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && bars.abort) p.header->status = DAF_ERR_TIMEOUT;
+    if (threadIdx.x == 0 && bars.abort) record_error(p.header, p.a.device_status, DAF_ERR_TIMEOUT);
     if (warp == 0) tmem_free(tmem, 512);
 }
 

@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
     uint64_t &acc_full = bars.acc_full, &acc_empty = bars.acc_empty, &tail = bars.tail, &drain = bars.drain;
     uint32_t &s_tmem = bars.tmem, &s_abort = bars.abort;
     if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
-        if (threadIdx.x == 0) p.header->status = DAF_ERR_UNSUPPORTED;
+        if (threadIdx.x == 0) record_error(p.header, p.a.device_status, DAF_ERR_UNSUPPORTED);
         return;
     }
     unsigned char *const smem = s_raw + Smem::kBars;
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
     }
     tmem_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && s_abort) p.header->status = DAF_ERR_TIMEOUT;
+    if (threadIdx.x == 0 && s_abort) record_error(p.header, p.a.device_status, DAF_ERR_TIMEOUT);
     if (warp == 0) tmem_free(tmem, 512);
 }
 

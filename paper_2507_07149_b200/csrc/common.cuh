@@ -287,6 +287,15 @@ daf_status make_plan(const daf_params *p, Plan *plan);
 // (kernel, device) pair and are remembered per pair; safe to call from several host threads.
 cudaError_t persistent_ctas(const void *kernel, int threads, int dyn_smem, int *ctas);
 
+// The current device's word for daf_device_status (nullptr if there is none to be had).
+unsigned int *device_status_word();
+// A kernel's error: in its workspace and, for callers who have let go of that, in the device's word.
+__device__ __forceinline__ void record_error(WorkspaceHeader *header, unsigned int *device_status, unsigned int error)
+{
+    header->status = error;
+    atomicMax(device_status, error);
+}
+
 // Activations of the fused producers and consumers (Sec. 3.2.3 of the paper: the statistics are taken where the
 // activation is produced, the restored value is used where the gradient is formed).
 //   ReLU   y = max(x, +0)            what is compressed: y     gradient: g where restored y > 0

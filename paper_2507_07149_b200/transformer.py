@@ -6,6 +6,8 @@ autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is 
 activation.  Attention's row statistics belong to the scores they were taken from: at 8 bits per value they are kept as they
 are, below that (or with a store, which may drop a tensor) the backward pass takes them, and the output, anew from the
 restored q, k and v, at the price of a second forward pass of attention and without keeping the output.
+Nothing here waits for the device; ``check_device`` (and ``check_status`` of the compression) tell whether an attention kernel
+gave up.
 
     python -m paper_2507_07149_b200.transformer --steps 20            # trains a small classifier on synthetic sequences
     python -m paper_2507_07149_b200.transformer --steps 20 --plain    # the same without compressed activations
@@ -18,7 +20,7 @@ import math
 import torch
 
 from . import attention as _attention
-from . import attention_grad, clip_grad_norm
+from . import attention_grad, check_device, clip_grad_norm
 from . import residual_norm as _residual_norm
 from . import residual_norm_grad
 from .autograd import active_compression
@@ -182,6 +184,7 @@ def train(steps: int = 20, *, compressed: bool = True, bit_budget: float = 8.0, 
         losses.append((loss.detach(), norm))
     if ctx is not None:
         ctx.check_status()
+    check_device()
     return [(float(a), float(b)) for a, b in losses]
 
 
