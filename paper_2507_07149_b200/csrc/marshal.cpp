@@ -75,6 +75,12 @@ PyObject *answer(std::initializer_list<at::Tensor> ts, daf_status status)
     PyTuple_SET_ITEM(r, i, PyLong_FromLong(status));
     return r;
 }
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Refusal("a truth value was expected");
+    return v != 0;
+}
 double number(PyObject *o)
 {
     const double v = PyFloat_AsDouble(o);
@@ -161,7 +167,7 @@ struct Attention {
         p.heads = (uint32_t)q.size(2);
         p.kv_heads = (uint32_t)k.size(2);
         p.head_dim = (uint32_t)q.size(3);
-        p.causal = PyObject_IsTrue(causal) ? 1u : 0u;
+        p.causal = truth(causal) ? 1u : 0u;
         p.scale = scale == Py_None ? (float)(1.0 / std::sqrt((double)q.size(3))) : (float)number(scale);
         q = readable(q);
         k = readable(k);
@@ -196,7 +202,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor ws = bytes(size, t.q);
         daf_status st = daf_attention(&t.p, ptr(t.q), ptr(t.k), ptr(t.v), static_cast<const int32_t *>(ptr(t.lengths)), ptr(out),
                                       static_cast<float *>(ptr(lse)), ptr(ws), size, stream);
-        if (st == DAF_OK && a[8] == Py_True && out.numel()) st = daf_poll_status(ptr(ws), stream);
+        if (st == DAF_OK && truth(a[8]) && out.numel()) st = daf_poll_status(ptr(ws), stream);
         return answer({out, lse}, st);
     });
 }
@@ -233,7 +239,7 @@ PyObject *attention_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor ws = bytes(size, t.q);
         daf_status st = daf_attention_grad(&t.p, ptr(t.q), ptr(t.k), ptr(t.v), static_cast<const int32_t *>(ptr(t.lengths)), ptr(out),
                                            static_cast<const float *>(ptr(lse)), ptr(grad_out), ptr(g[0]), ptr(g[1]), ptr(g[2]), ptr(ws), size, stream);
-        if (st == DAF_OK && a[12] == Py_True && (g[0].numel() || g[1].numel())) st = daf_poll_status(ptr(ws), stream);
+        if (st == DAF_OK && truth(a[12]) && (g[0].numel() || g[1].numel())) st = daf_poll_status(ptr(ws), stream);
         return answer({g[0], g[1], g[2]}, st);
     });
 }
