@@ -1,6 +1,7 @@
 """The operators of a transformer's training step as differentiable functions and layers, and a small trainer.
 
-``attention``, ``residual_norm`` and ``clip_grad_norm_`` run the CUDA kernels behind the C ABI.  Attention keeps q, k, v, its
+``attention``, ``residual_norm`` and ``clip_grad_norm_`` run the CUDA kernels behind the C ABI; they can be differentiated
+once.  Attention keeps q, k, v, its
 output and one float per row for the backward pass, the join keeps its two activations; what they keep goes through
 autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is held in compressed form like every other
 activation.  Attention's row statistics belong to the scores they were taken from: at 8 bits per value they are kept as they
@@ -18,6 +19,7 @@ import argparse
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import attention as _attention
 from . import attention_grad, check_device, clip_grad_norm
@@ -43,6 +45,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         causal, scale = ctx.how
         if ctx.lse is None:
@@ -68,6 +71,7 @@ class _ResidualNorm(torch.autograd.Function):
         return z, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_z, grad_h):
         z, y, weight, bias, gate, post_weight, post_bias = ctx.saved_tensors
         if grad_h is None:                                          # h was not used
