@@ -1,10 +1,9 @@
 """The operators of a transformer's training step as differentiable functions and layers, and a small trainer.
 
 ``attention``, ``residual_norm`` and ``clip_grad_norm_`` run the CUDA kernels behind the C ABI; they can be differentiated
-once.  Attention keeps q, k, v, its
-output and one float per row for the backward pass, the join keeps its two activations; what they keep goes through
-autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is held in compressed form like every other
-activation.  Attention's row statistics belong to the scores they were taken from: at 8 bits per value they are kept as they
+once.  Attention keeps q, k, v, its output and one float per row for the backward pass, the join keeps its two activations;
+what they keep goes through autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is held in compressed
+form like every other activation.  Attention's row statistics belong to the scores they were taken from: at 8 bits per value they are kept as they
 are, below that (or with a store, which may drop a tensor) the backward pass takes them, and the output, anew from the
 restored q, k and v, at the price of a second forward pass of attention and without keeping the output.
 Nothing here waits for the device; ``check_device`` (and ``check_status`` of the compression) tell whether an attention kernel
@@ -37,23 +36,20 @@ class _Attention(torch.autograd.Function):
         # 8 bits 0.019 0.062 0.14 / 0.018 0.037 0.078, 4 bits 0.34 2.7 120 / 0.31 0.57 0.91, 2 bits 14 3e8 3e20 / 2.5 1.8 1.6.
         compression = active_compression()
         if compression is not None and compression.coarse:
-            ctx.save_for_backward(q, k, v)
+            ctx.save_for_backward(key_lengths, q, k, v)
             lse = None
         else:
-            ctx.save_for_backward(q, k, v, out)
-        ctx.lse, ctx.key_lengths, ctx.how = lse, key_lengths, (causal, scale)
+            ctx.save_for_backward(key_lengths, q, k, v, out)
+        ctx.lse, ctx.how = lse, (causal, scale)
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_out):
-        causal, scale = ctx.how
-        if ctx.lse is None:
-            q, k, v = ctx.saved_tensors
-            out, lse = _attention(q, k, v, causal=causal, scale=scale, key_lengths=ctx.key_lengths)
-        else:
-            (q, k, v, out), lse = ctx.saved_tensors, ctx.lse
-        return *attention_grad(q, k, v, out, lse, grad_out, causal=causal, scale=scale, key_lengths=ctx.key_lengths), None, None, None
+        key_lengths, q, k, v, *out = ctx.saved_tensors
+        how = dict(causal=ctx.how[0], scale=ctx.how[1], key_lengths=key_lengths)
+        out, lse = (out[0], ctx.lse) if out else _attention(q, k, v, **how)
+        return *attention_grad(q, k, v, out, lse, grad_out, **how), None, None, None
 
 
 def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_lengths=None):

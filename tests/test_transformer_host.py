@@ -52,3 +52,14 @@ def test_a_second_derivative_is_an_error(operator):
     g, = torch.autograd.grad(f, q, create_graph=True)
     with pytest.raises(RuntimeError, match="differentia"):
         g.square().sum().backward()
+
+
+def test_lengths_that_change_between_the_passes_are_an_error():
+    q, k, v = (torch.randn(2, 5, 2, 8, requires_grad=True) for _ in range(3))
+    lengths = torch.tensor([5, 3], dtype=torch.int32)
+    out = tr.attention(q, k, v, key_lengths=lengths)
+    out.sum().backward()
+    out = tr.attention(q, k, v, key_lengths=lengths)
+    lengths[1] = 4                                                  # a buffer that the next batch is read into
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
