@@ -62,6 +62,12 @@ bool aligned(const at::Tensor &t, uintptr_t to) { return (reinterpret_cast<uintp
 at::Tensor bytes(uint64_t n, const at::Tensor &like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
 at::Tensor dense(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options()); }
 
+// The caller's tensor is about to be written: autograd may keep it for something else.
+void modified(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject *wrap(const at::Tensor &t)
 {
     if (!t.defined()) Py_RETURN_NONE;
@@ -194,9 +200,9 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
         at::Tensor out = maybe(where, a[4]), lse = maybe(where, a[5]);
         if (!out.defined()) out = dense(t.q.sizes(), t.q);
-        else like(where, "out", out, t.q), writable(where, "out", out);
+        else like(where, "out", out, t.q), writable(where, "out", out), modified(out);
         if (!lse.defined()) lse = at::empty({t.q.size(0), t.q.size(2), t.q.size(1)}, t.q.options().dtype(at::kFloat));
-        else t.check_lse(where, lse);
+        else t.check_lse(where, lse), modified(lse);
         strides(t.p.out_stride, out);
         const uint64_t size = daf_attention_workspace(&t.p);
         const at::Tensor ws = bytes(size, t.q);
@@ -228,7 +234,7 @@ PyObject *attention_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
         for (int i = 0; i < 3; i++) {
             g[i] = maybe(where, a[7 + i]);
             if (!g[i].defined()) g[i] = dense(model[i]->sizes(), *model[i]);
-            else like(where, name[i], g[i], *model[i]), writable(where, name[i], g[i]);
+            else like(where, name[i], g[i], *model[i]), writable(where, name[i], g[i]), modified(g[i]);
         }
         strides(t.p.out_stride, out);
         strides(t.p.grad_out_stride, grad_out);
@@ -302,9 +308,9 @@ PyObject *residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Join t(where, a);
         const c10::cuda::CUDAGuard on(t.x.device());
         at::Tensor z = maybe(where, a[10]), h = maybe(where, a[11]);
-        if (z.defined()) t.activation(where, "z", z);
+        if (z.defined()) t.activation(where, "z", z), modified(z);
         else z = dense(t.x.sizes(), t.x);
-        if (h.defined()) t.activation(where, "h", h);
+        if (h.defined()) t.activation(where, "h", h), modified(h);
         else h = dense(t.x.sizes(), t.x);
         const daf_status st = daf_residual_norm(&t.p, ptr(t.x), ptr(t.y), ptr(t.weight), ptr(t.bias), ptr(t.gate), ptr(t.post_weight), ptr(t.post_bias),
                                                 ptr(z), ptr(h), c10::cuda::getCurrentCUDAStream().stream());
@@ -357,12 +363,16 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
             types[i] = code(where, g);
             numel[i] = (uint64_t)g.numel();
             src[i] = dst[i] = g.data_ptr();
-            if (a[1] == Py_None) continue;
+            if (a[1] == Py_None) {
+                modified(g);
+                continue;
+            }
             const at::Tensor &o = tensor(where, PyList_GET_ITEM(a[1], (Py_ssize_t)i));
             same_device(where, index, o);
             if (o.scalar_type() != g.scalar_type() || o.numel() != g.numel() || !o.is_contiguous())
                 refuse(where, "an output differs from its gradient in size or type, or is not contiguous");
             dst[i] = o.data_ptr();
+            modified(o);
         }
         const c10::cuda::CUDAGuard on(first.device());
         const at::Tensor norm = at::empty({}, first.options().dtype(at::kFloat));

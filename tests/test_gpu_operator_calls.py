@@ -26,3 +26,35 @@ def test_check_takes_any_truth_value(check, waits):
         daf.attention(q, k, v, check=torch.zeros(2))
     with pytest.raises(ValueError):
         daf.attention(q, k, v, causal=torch.zeros(2))
+
+
+def test_what_is_written_into_counts_as_modified():
+    """autograd tells by the version counter that a tensor it keeps has changed."""
+    q, k, v = qkv()
+    out, lse = daf.attention(q, k, v)
+    made = [torch.empty_like(t) for t in (out, q, k, v)] + [torch.empty_like(lse)]
+    versions = [t._version for t in made]
+    daf.attention(q, k, v, out=made[0], lse=made[4])
+    daf.attention_grad(q, k, v, out, lse, out, grads=made[1:4])
+    x, y, w = torch.randn(8, 64, device="cuda"), torch.randn(8, 64, device="cuda"), torch.ones(64, device="cuda")
+    z = torch.empty_like(x)
+    made, versions = made + [z, y], versions + [z._version, y._version]
+    daf.residual_norm(x, y, w, out=(z, y))
+    g = [torch.randn(100, device="cuda"), torch.randn(7, device="cuda")]
+    made, versions = made + g, versions + [t._version for t in g]
+    daf.clip_grad_norm(g, 1.0)
+    assert all(t._version > before for t, before in zip(made, versions))
+    into, read = [torch.empty_like(t) for t in g], [t._version for t in (x, q, k, v, lse, *g)]
+    versions = [t._version for t in into]
+    daf.clip_grad_norm(g, 1.0, out=into)
+    assert all(t._version > before for t, before in zip(into, versions))
+    assert read == [t._version for t in (x, q, k, v, lse, *g)]       # what is only read stays as it was
+    a = torch.randn(100, device="cuda", requires_grad=True)
+    f = (a * g[0]).sum()
+    daf.clip_grad_norm(g, 0.5)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        f.backward()
+    with torch.inference_mode():
+        h = [torch.randn(100, device="cuda")]
+        daf.clip_grad_norm(h, 1.0)
+    daf.clip_grad_norm(h, 1.0)                                      # tensors without a counter
