@@ -7,6 +7,7 @@
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -106,8 +107,8 @@ template <typename F> PyObject *guarded(Py_ssize_t given, Py_ssize_t wanted, F b
     } catch (const Refusal &e) {
         PyErr_Clear();
         PyErr_SetString(PyExc_ValueError, e.what());
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {                                                 // torch's own, as torch tells them (out of memory among them)
+        torch::translate_exception_to_python(std::current_exception());
     }
     return nullptr;
 }

@@ -58,3 +58,16 @@ def test_what_is_written_into_counts_as_modified():
         h = [torch.randn(100, device="cuda")]
         daf.clip_grad_norm(h, 1.0)
     daf.clip_grad_norm(h, 1.0)                                      # tensors without a counter
+
+
+def test_running_out_of_memory_is_told_apart():
+    """A copy of half a terabyte (a broadcast tensor, which the kernels cannot address) is refused by torch's allocator, by the
+    process's own limit."""
+    q, k, v = qkv()
+    torch.cuda.set_per_process_memory_fraction(0.05)
+    try:
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            daf.attention(q[:, :1, :1].expand(1, 1 << 23, 512, 64), k[:, :, :1], v[:, :, :1])
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert daf.attention(q, k, v)[0].isfinite().all()
