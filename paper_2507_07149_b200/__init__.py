@@ -652,7 +652,8 @@ def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_
                   kind: str = "layer", eps: float = 1e-6, out=None, stream=None):
     """(z, h): z = x + residual_scale * gate * post_norm(y), h = norm(z) * weight + bias over the last dimension, in one pass
     (daf_residual_norm).  post_norm only with post_weight; gate [C], or [G, C] for G equal runs of rows; parameters in the
-    activations' type or float32.  out: (z, h) to write into, z may be x and h may be y."""
+    activations' type or float32.  Tensors are contiguous; what does not start on the kernels' boundaries is copied first.  out:
+    (z, h) to write into, z may be x and h may be y."""
     if stream is not None:
         with _torch().cuda.stream(stream):
             return residual_norm(x, y, weight, bias, gate=gate, post_weight=post_weight, post_bias=post_bias, residual_scale=residual_scale,

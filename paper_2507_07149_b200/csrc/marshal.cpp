@@ -60,6 +60,10 @@ void same_device(const char *where, int index, const at::Tensor &t)
 }
 void *ptr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 bool aligned(const at::Tensor &t, uintptr_t to) { return (reinterpret_cast<uintptr_t>(t.data_ptr()) & (to - 1)) == 0; }
+void onto_boundary(at::Tensor &t, uintptr_t to)                     // t is contiguous
+{
+    if (t.defined() && !aligned(t, to)) t = t.clone();
+}
 at::Tensor bytes(uint64_t n, const at::Tensor &like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
 at::Tensor dense(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options()); }
 
@@ -287,6 +291,15 @@ struct Join {
             parameter(where, index, gate, (one && gate.size(0) == width) || (gate.dim() == 2 && gate.size(0) > 0 && gate.size(1) == width));
             p.gates = one ? 1u : (uint32_t)gate.size(0);
         }
+        for (at::Tensor *const v : {&x, &y}) onto_boundary(*v, boundary());
+        for (at::Tensor *const v : {&weight, &bias, &gate, &post_weight, &post_bias}) onto_boundary(*v, 16);
+    }
+    uintptr_t boundary() const { return p.dtype == DAF_F32 ? 32 : 16; }
+    void result(const char *where, const char *name, const at::Tensor &t) const
+    {
+        activation(where, name, t);
+        if (!aligned(t, boundary())) refuse(where, std::string(name) + " needs a start on a " + std::to_string(boundary()) + "-byte boundary");
+        modified(t);
     }
     void activation(const char *where, const char *name, const at::Tensor &t) const
     {
@@ -309,9 +322,9 @@ PyObject *residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Join t(where, a);
         const c10::cuda::CUDAGuard on(t.x.device());
         at::Tensor z = maybe(where, a[10]), h = maybe(where, a[11]);
-        if (z.defined()) t.activation(where, "z", z), modified(z);
+        if (z.defined()) t.result(where, "z", z);
         else z = dense(t.x.sizes(), t.x);
-        if (h.defined()) t.activation(where, "h", h), modified(h);
+        if (h.defined()) t.result(where, "h", h);
         else h = dense(t.x.sizes(), t.x);
         const daf_status st = daf_residual_norm(&t.p, ptr(t.x), ptr(t.y), ptr(t.weight), ptr(t.bias), ptr(t.gate), ptr(t.post_weight), ptr(t.post_bias),
                                                 ptr(z), ptr(h), c10::cuda::getCurrentCUDAStream().stream());
@@ -327,9 +340,11 @@ PyObject *residual_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
         const char *const where = "residual_norm_grad";
         const Join t(where, a);
         const c10::cuda::CUDAGuard on(t.x.device());
-        const at::Tensor grad_z = maybe(where, a[10]), &grad_h = tensor(where, a[11]);
+        at::Tensor grad_z = maybe(where, a[10]), grad_h = tensor(where, a[11]);
         if (grad_z.defined()) t.activation(where, "grad_z", grad_z);
         t.activation(where, "grad_h", grad_h);
+        onto_boundary(grad_z, t.boundary());
+        onto_boundary(grad_h, t.boundary());
         const auto as = [](const at::Tensor &v) { return v.defined() ? dense(v.sizes(), v) : at::Tensor(); };
         const at::Tensor gx = as(t.x), gy = as(t.x), gw = as(t.weight), gb = as(t.bias), gg = as(t.gate), gpw = as(t.post_weight), gpb = as(t.post_bias);
         const uint64_t size = daf_residual_norm_grad_workspace(&t.p);

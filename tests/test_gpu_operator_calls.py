@@ -71,3 +71,28 @@ def test_running_out_of_memory_is_told_apart():
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
     assert daf.attention(q, k, v)[0].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_join_reads_tensors_off_their_boundary(dtype):
+    """Like attention: what the kernels cannot address is copied first, what they write has to be addressable."""
+    def off(*shape):
+        n = 1
+        for s in shape:
+            n *= s
+        return torch.randn(n + 1, device="cuda").to(dtype)[1:].view(shape)
+    x, y, gz, gh = (off(6, 64) for _ in range(4))
+    w, b, g, pw, pb = (off(64) for _ in range(5))
+    how = dict(gate=g, post_weight=pw, post_bias=pb)
+    fit = {n: t.clone() for n, t in how.items()}
+    for a, c in zip(daf.residual_norm(x, y, w, b, **how), daf.residual_norm(x.clone(), y.clone(), w.clone(), b.clone(), **fit)):
+        assert torch.equal(a, c)
+    got = daf.residual_norm_grad(x, y, w, b, gz, gh, **how)
+    want = daf.residual_norm_grad(x.clone(), y.clone(), w.clone(), b.clone(), gz.clone(), gh.clone(), **fit)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    with pytest.raises(ValueError):
+        daf.residual_norm(x, y, w, b, out=(off(6, 64), torch.empty_like(x)))
+    half = torch.randn(6 * 64 + 8, device="cuda")[4:-4].view(6, 64)  # on 16 bytes, not on 32
+    assert half.data_ptr() % 32 == 16
+    for a, c in zip(daf.residual_norm(half, half, torch.ones(64, device="cuda")), daf.residual_norm(half.clone(), half.clone(), torch.ones(64, device="cuda"))):
+        assert torch.equal(a, c)
