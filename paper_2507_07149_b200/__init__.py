@@ -679,8 +679,13 @@ def residual_norm_grad(z, y, weight, bias, grad_z, grad_h, *, gate=None, post_we
     return {"x": gx, "y": gy, "weight": gw, "bias": gb, "gate": gg, "post_weight": gpw, "post_bias": gpb}
 
 
+def gap_free(t) -> bool:
+    """Whether a tensor fills its memory without gaps or overlaps, in whatever order of dimensions."""
+    return _native().gap_free(t)
+
+
 def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, stream=None):
-    """Scales the tensors of ``grads`` in place (or into ``out``, tensors of the same types and sizes) by
+    """Scales the tensors of ``grads`` in place (or into ``out``, tensors of the same types, sizes and orders) by
     min(1, max_norm / (norm + eps)), norm being the 2-norm over all of them; returns the norm as a float32 scalar tensor on
     their device (daf_clip_norm_batch).  Nothing is read back."""
     if stream is not None:

@@ -375,7 +375,7 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         for (size_t i = 0; i < count; i++) {
             const at::Tensor &g = tensor(where, PyList_GET_ITEM(a[0], (Py_ssize_t)i));
             same_device(where, index, g);
-            if (!g.is_contiguous()) refuse(where, "expects contiguous tensors");
+            if (!g.is_non_overlapping_and_dense()) refuse(where, "expects tensors without gaps, in any order");
             types[i] = code(where, g);
             numel[i] = (uint64_t)g.numel();
             src[i] = dst[i] = g.data_ptr();
@@ -385,8 +385,9 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
             }
             const at::Tensor &o = tensor(where, PyList_GET_ITEM(a[1], (Py_ssize_t)i));
             same_device(where, index, o);
-            if (o.scalar_type() != g.scalar_type() || o.numel() != g.numel() || !o.is_contiguous())
-                refuse(where, "an output differs from its gradient in size or type, or is not contiguous");
+            const bool alike = o.is_contiguous() ? g.is_contiguous() : o.sizes() == g.sizes() && o.strides() == g.strides();
+            if (o.scalar_type() != g.scalar_type() || o.numel() != g.numel() || !alike)
+                refuse(where, "an output differs from its gradient in size, type or order");
             dst[i] = o.data_ptr();
             modified(o);
         }
@@ -400,9 +401,15 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// (tensor) -> whether it fills its memory without gaps or overlaps, in any order
+PyObject *gap_free(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 1, [&]() { return PyBool_FromLong(tensor("gap_free", a[0]).is_non_overlapping_and_dense()); });
+}
+
 #define DAF_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DAF_METHOD(attention), DAF_METHOD(attention_grad), DAF_METHOD(residual_norm), DAF_METHOD(residual_norm_grad),
-                         DAF_METHOD(clip_grad_norm), {nullptr, nullptr, 0, nullptr}};
+                         DAF_METHOD(clip_grad_norm), DAF_METHOD(gap_free), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -21,7 +21,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import attention as _attention
-from . import attention_grad, check_device, clip_grad_norm
+from . import attention_grad, check_device, clip_grad_norm, gap_free
 from . import residual_norm as _residual_norm
 from . import residual_norm_grad
 from .autograd import active_compression
@@ -86,11 +86,11 @@ def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_
 
 def clip_grad_norm_(parameters, max_norm: float, *, eps: float = 1e-6):
     """Clips the gradients of ``parameters`` in place by their global 2-norm, two launches for all of them; returns the norm
-    as a scalar tensor on the device.  Gradients that are not contiguous are replaced by contiguous copies first."""
+    as a scalar tensor on the device.  Gradients with gaps in their memory are replaced by copies without first."""
     grads = []
     for p in parameters:
         if p.grad is not None:
-            if not p.grad.is_contiguous():
+            if not (p.grad.is_contiguous() or gap_free(p.grad)):
                 p.grad = p.grad.contiguous()
             grads.append(p.grad)
     return clip_grad_norm(grads, max_norm, eps=eps)

@@ -96,3 +96,32 @@ def test_the_join_reads_tensors_off_their_boundary(dtype):
     assert half.data_ptr() % 32 == 16
     for a, c in zip(daf.residual_norm(half, half, torch.ones(64, device="cuda")), daf.residual_norm(half.clone(), half.clone(), torch.ones(64, device="cuda"))):
         assert torch.equal(a, c)
+
+
+def test_gradients_in_other_orders_are_clipped_in_place():
+    """Channels-last and transposed gradients fill their memory without gaps: order does not matter to a norm."""
+    from paper_2507_07149_b200 import transformer as tr
+    torch.manual_seed(0)
+    ps = [torch.nn.Parameter(torch.randn(8, 6, 3, 3, device="cuda").to(memory_format=torch.channels_last)), torch.nn.Parameter(torch.randn(40, 30, device="cuda"))]
+    ps[0].grad = torch.randn(8, 6, 3, 3, device="cuda").to(memory_format=torch.channels_last)
+    ps[1].grad = torch.randn(30, 40, device="cuda").t()
+    keep = [(p.grad, p.grad.data_ptr(), p.grad.stride(), p.grad.clone()) for p in ps]
+    norm = tr.clip_grad_norm_(ps, 0.5)
+    want = torch.cat([k[3].reshape(-1) for k in keep]).double().norm()
+    assert abs(float(norm) - float(want)) <= 2.0 ** -16 * float(want)
+    for p, (grad, at, strides, before) in zip(ps, keep):
+        assert p.grad is grad and grad.data_ptr() == at and grad.stride() == strides
+        assert (grad.double() - before.double() * 0.5 / (want + 1e-6)).abs().max() <= 2.0 ** -16
+    out = [torch.empty_like(p.grad) for p in ps]
+    daf.clip_grad_norm([k[3] for k in keep], 0.5, out=out)
+    assert all(torch.equal(o, p.grad) for o, p in zip(out, ps))
+    with pytest.raises(ValueError):                                 # another order
+        daf.clip_grad_norm([keep[1][3]], 0.5, out=[torch.empty(40, 30, device="cuda")])
+    for gaps in (torch.randn(10, 10, device="cuda")[:, :5], torch.randn(10, 1, device="cuda").expand(10, 4)):
+        with pytest.raises(ValueError):
+            daf.clip_grad_norm([gaps], 0.5)
+    ps[1].grad = None
+    ps[1].grad = torch.randn(40, 60, device="cuda")[:, ::2]          # this one has to be copied
+    before = ps[1].grad.clone()
+    tr.clip_grad_norm_(ps[1:], 0.5)
+    assert (ps[1].grad.double() - before.double() * 0.5 / (before.double().norm() + 1e-6)).abs().max() <= 2.0 ** -16
