@@ -1,5 +1,6 @@
 // Host-side validation, size arithmetic and status plumbing of the C ABI.
 #include <math.h>
+#include <atomic>
 #include <string.h>
 
 #include "common.cuh"
@@ -37,8 +38,15 @@ __device__ unsigned int g_device_status;
 
 unsigned int *device_status_word()
 {
+    static std::atomic<unsigned int *> known[64];                  // a device's address never changes
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return nullptr;
+    if (device < 64)
+        if (unsigned int *const word = known[device].load(std::memory_order_relaxed)) return word;
     void *word = nullptr;
-    return cudaGetSymbolAddress(&word, g_device_status) == cudaSuccess ? static_cast<unsigned int *>(word) : nullptr;
+    if (cudaGetSymbolAddress(&word, g_device_status) != cudaSuccess) return nullptr;
+    if (device < 64) known[device].store(static_cast<unsigned int *>(word), std::memory_order_relaxed);
+    return static_cast<unsigned int *>(word);
 }
 
 static bool is_pow2(uint32_t v) { return v && !(v & (v - 1)); }
