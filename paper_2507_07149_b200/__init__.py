@@ -687,13 +687,14 @@ def gap_free(t) -> bool:
 def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, stream=None):
     """Scales the tensors of ``grads`` in place (or into ``out``, tensors of the same types, sizes and orders) by
     min(1, max_norm / (norm + eps)), norm being the 2-norm over all of them; returns the norm as a float32 scalar tensor on
-    their device (daf_clip_norm_batch).  Nothing is read back."""
+    their device, zero on the current one for no tensors (daf_clip_norm_batch).  Nothing is read back."""
     if stream is not None:
         with _torch().cuda.stream(stream):
             return clip_grad_norm(grads, max_norm, eps=eps, out=out)
     grads = list(grads)
     if not grads:
-        return _torch().zeros((), dtype=_torch().float32)
+        torch = _torch()
+        return torch.zeros((), dtype=torch.float32, device="cuda" if torch.cuda.is_available() else "cpu")
     norm, status = _native().clip_grad_norm(grads, None if out is None else list(out), max_norm, eps)
     _check(status, "daf_clip_norm_batch")
     return norm

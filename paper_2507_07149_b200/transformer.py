@@ -87,12 +87,14 @@ def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_
 def clip_grad_norm_(parameters, max_norm: float, *, eps: float = 1e-6):
     """Clips the gradients of ``parameters`` in place by their global 2-norm, two launches for all of them; returns the norm
     as a scalar tensor on the device.  Gradients with gaps in their memory are replaced by copies without first."""
-    grads = []
+    grads, parameters = [], list(parameters)
     for p in parameters:
         if p.grad is not None:
             if not (p.grad.is_contiguous() or gap_free(p.grad)):
                 p.grad = p.grad.contiguous()
             grads.append(p.grad)
+    if parameters and not grads:
+        return torch.zeros((), dtype=torch.float32, device=parameters[0].device)
     return clip_grad_norm(grads, max_norm, eps=eps)
 
 

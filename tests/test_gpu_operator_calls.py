@@ -125,3 +125,11 @@ def test_gradients_in_other_orders_are_clipped_in_place():
     before = ps[1].grad.clone()
     tr.clip_grad_norm_(ps[1:], 0.5)
     assert (ps[1].grad.double() - before.double() * 0.5 / (before.double().norm() + 1e-6)).abs().max() <= 2.0 ** -16
+
+
+def test_no_gradients_have_a_norm_on_their_device():
+    from paper_2507_07149_b200 import transformer as tr
+    norm = daf.clip_grad_norm([], 1.0)
+    assert norm.is_cuda and norm.dtype == torch.float32 and float(norm) == 0.0
+    norm = tr.clip_grad_norm_([torch.nn.Parameter(torch.randn(3, device="cuda"))], 1.0)
+    assert norm.is_cuda and float(norm) == 0.0
