@@ -79,7 +79,11 @@ class _ResidualNorm(torch.autograd.Function):
 
 def residual_norm(x, y, weight, bias=None, *, gate=None, post_weight=None, post_bias=None, residual_scale: float = 1.0,
                   kind: str = "layer", eps: float = 1e-6):
-    """Differentiable ``daf.residual_norm``: (z, h) of the join z = x + residual_scale * gate * post_norm(y), h = norm(z)."""
+    """Differentiable ``daf.residual_norm``: (z, h) of the join z = x + residual_scale * gate * post_norm(y), h = norm(z).  x and y
+    may differ in type (a block under autocast): both are then taken in the wider one."""
+    if x.dtype != y.dtype:
+        wide = torch.promote_types(x.dtype, y.dtype)
+        x, y = x.to(wide), y.to(wide)
     return _ResidualNorm.apply(x.contiguous(), y.contiguous(), weight, bias, gate, post_weight, post_bias,
                                dict(residual_scale=residual_scale, kind=kind, eps=eps))
 

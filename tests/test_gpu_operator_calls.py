@@ -133,3 +133,18 @@ def test_no_gradients_have_a_norm_on_their_device():
     assert norm.is_cuda and norm.dtype == torch.float32 and float(norm) == 0.0
     norm = tr.clip_grad_norm_([torch.nn.Parameter(torch.randn(3, device="cuda"))], 1.0)
     assert norm.is_cuda and float(norm) == 0.0
+
+
+def test_a_block_under_autocast():
+    """The stream stays in float32, the products run in bfloat16: within a few 2^-8 of the block in float32."""
+    from paper_2507_07149_b200 import transformer as tr
+    torch.manual_seed(0)
+    block = tr.Block(128, 2, 256, gate_init=0.5).cuda()
+    x, h = torch.randn(2, 30, 128, device="cuda"), torch.randn(2, 30, 128, device="cuda")
+    want = block(x, h)
+    with torch.autocast("cuda", torch.bfloat16):
+        got = block(x, h)
+    for a, b in zip(got, want):
+        assert a.dtype == torch.float32 and (a - b).norm() <= 2.0 ** -6 * b.norm()
+    sum(t.square().sum() for t in got).backward()
+    assert all(p.grad is not None and p.grad.isfinite().all() for p in block.parameters())

@@ -63,3 +63,14 @@ def test_lengths_that_change_between_the_passes_are_an_error():
     lengths[1] = 4                                                  # a buffer that the next batch is read into
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.sum().backward()
+
+
+@pytest.mark.parametrize("stream,block,wide", [(torch.float32, torch.bfloat16, torch.float32), (torch.bfloat16, torch.float32, torch.float32),
+                                               (torch.bfloat16, torch.bfloat16, torch.bfloat16)])
+def test_a_block_in_another_type_than_the_stream(stream, block, wide):
+    """As under autocast: the sum has the wider type, as torch's own has, and each gradient its tensor's."""
+    x, y = torch.randn(3, 8, dtype=stream, requires_grad=True), torch.randn(3, 8, dtype=block, requires_grad=True)
+    z, h = tr.residual_norm(x, y, torch.ones(8))
+    assert z.dtype == h.dtype == wide and torch.equal(z, x + y)
+    (z.sum() + h.sum()).backward()
+    assert x.grad.dtype == stream and y.grad.dtype == block
