@@ -144,7 +144,8 @@ class Block(torch.nn.Module):
 
 
 class Classifier(torch.nn.Module):
-    """Sequences of feature vectors in, class scores out: projection, blocks, mean over the tokens, head."""
+    """Sequences of feature vectors in, class scores out: projection, blocks, mean over the tokens (the first
+    key_lengths of each sequence), head."""
 
     def __init__(self, features: int, classes: int, tokens: int, width: int = 256, heads: int = 4, blocks: int = 4, hidden: int = 1024, **block):
         super().__init__()
@@ -159,7 +160,11 @@ class Classifier(torch.nn.Module):
         h = self.first(x)
         for block in self.blocks:
             x, h = block(x, h, key_lengths)
-        return self.head(h.mean(1))
+        if key_lengths is None:
+            return self.head(h.mean(1))
+        n = key_lengths.clamp(0, h.shape[1])[:, None]                # the padding takes no part
+        here = torch.arange(h.shape[1], device=h.device) < n
+        return self.head(h.where(here[..., None], 0).sum(1) / n.clamp(min=1).to(h.dtype))
 
 
 def train(steps: int = 20, *, compressed: bool = True, bit_budget: float = 8.0, batch: int = 64, tokens: int = 197, dtype=torch.bfloat16,

@@ -74,3 +74,20 @@ def test_a_block_in_another_type_than_the_stream(stream, block, wide):
     assert z.dtype == h.dtype == wide and torch.equal(z, x + y)
     (z.sum() + h.sum()).backward()
     assert x.grad.dtype == stream and y.grad.dtype == block
+
+
+def test_the_classifier_averages_over_the_tokens_that_exist():
+    """What lies in the padding changes neither the scores nor any gradient; a sequence of no tokens averages to zero."""
+    torch.manual_seed(0)
+    net = tr.Classifier(6, 3, 5, width=16, heads=2, blocks=2, hidden=16)
+    inputs, lengths = torch.randn(3, 5, 6), torch.tensor([5, 2, 0], dtype=torch.int32)
+    other = inputs.clone()
+    other[1, 2:], other[2] = 7.0, -3.0
+    a, b = net(inputs, lengths), net(other, lengths)
+    assert torch.equal(a, b) and torch.equal(a[2], net.head.bias)
+    assert torch.allclose(a[0], net(inputs)[0], atol=1e-6)
+    short = tr.Classifier(6, 3, 2, width=16, heads=2, blocks=2, hidden=16)
+    state = net.state_dict()
+    state["place"] = state["place"][:, :2]
+    short.load_state_dict(state)
+    assert torch.allclose(a[1], short(inputs[1:2, :2])[0], atol=1e-6)
