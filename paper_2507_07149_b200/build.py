@@ -1,6 +1,8 @@
 """Builds the CUDA library in-tree: nvcc for sm_100a -> paper_2507_07149_b200/libdaf.so."""
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -22,6 +24,7 @@ CXX_SOURCES = ["pool.cpp", "store.cpp"]
 # The Python module that marshals torch tensors for the transformer operators (host code only).
 MARSHAL = os.path.join(HERE, "_marshal.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
+MARSHAL_MADE = os.path.join(OBJ, "marshal.made")                 # which torch and Python it was built for
 
 # No fast-math, no flush-to-zero, no fused contraction beyond what the sources write out:
 # results must match IEEE binary32 arithmetic bit for bit.
@@ -77,7 +80,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 
 def build_marshal(force: bool = False) -> str:
-    """Compiles csrc/marshal.cpp against torch and libdaf.so (found beside it when the module is loaded)."""
+    """Compiles csrc/marshal.cpp against torch and libdaf.so (found beside it when the module is loaded).  Without torch there is
+    nothing to marshal: libdaf.so stands alone, and the Python functions that need the module say so."""
+    if importlib.util.find_spec("torch") is None:
+        return MARSHAL
+    made = f"torch {importlib.metadata.version('torch')}, {sys.implementation.cache_tag}"
+    if os.path.exists(MARSHAL_MADE):
+        with open(MARSHAL_MADE) as f:
+            force = force or f.read() != made
+    else:
+        force = True
     if not (force or _stale(MARSHAL, [MARSHAL_SOURCE, HEADERS[-1]])):
         return MARSHAL
     import sysconfig
@@ -97,6 +109,8 @@ def build_marshal(force: bool = False) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on marshal.cpp:\n{r.stdout}\n{r.stderr}")
+    with open(MARSHAL_MADE, "w") as f:
+        f.write(made)
     return MARSHAL
 
 
