@@ -21,8 +21,8 @@ template <typename T> __device__ __forceinline__ void load8_any(const void *p, f
 // CTA: -lse in units of log2, -inf for rows that see nothing and for the padding (their probabilities then come out as
 // exp2(-inf) = 0), and -delta = -sum(grad_out * out).  float16 also notes |grad_out|^2 of the row and the largest one of a key
 // head's readers, rows that see nothing left out, and a bound of a key head's |v|^2, D times the largest square (maxima of
-// non-negative floats by their bits: the order of the atomics changes nothing).  Reading v for that costs float16 calls 2 to 4 %
-// (16 x 509 tokens, 16 heads of 80: 145 -> 151 us); CTAs of their own for v 8 %.
+// non-negative floats by their bits: the order of the atomics changes nothing).  Reading v for that costs float16 calls 1 to 4 %
+// (16 x 509 tokens, 16 heads of 80: 145 -> 148 us); CTAs of their own for v 8 %.
 template <typename T> __global__ void __launch_bounds__(kRowThreads) attention_rows_kernel(const __grid_constant__ AttnArgs a, uint32_t lanes, WorkspaceHeader *header)
 {
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) header->status = 0u;

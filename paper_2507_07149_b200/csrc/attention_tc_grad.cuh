@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
         const int off = (int)a.Sk - (int)a.Sq;
         const uint64_t c2 = pair(a.scale_log2, a.scale_log2);
         GradItem<DKV> it;
-        float nl = 0.0f, nd = 0.0f, lift = 1.0f;                   // lift: what float16 multiplies dS by
+        float nl = 0.0f, nd = 0.0f, lift = 1.0f;                   // lift: what float16 multiplies its (lifted) P by for dS
         constexpr bool F16 = __is_same(T, __half);
         // item number `turn`, and for dq what its row brings along; false behind the last one
         auto enter = [&](uint32_t &turn) {
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 if (F16) {
                     const uint32_t head = it.b * a.Hkv + (DKV ? it.h : it.h / a.group);
                     const float grad2 = DKV ? a.grad_max[head] : a.row_norm2[((uint64_t)it.b * a.H + it.h) * a.rows_padded + it.first + lane_row];
-                    lift = score_grad_scale(grad2, a.value_max[head]);
+                    lift = score_grad_scale(grad2, a.value_max[head]) * exp2f(-kHalfLift);
                 }
                 if (!DKV && it.blocks) {
                     const uint64_t at = ((uint64_t)it.b * a.H + it.h) * a.rows_padded + it.first + lane_row;
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                                 unpair(fma2(pair(s[c], s[c + 1]), c2, l2[q]), u, v);
                                 u = exp2_fast(u);
                                 v = exp2_fast(v);
-                                const uint64_t pr = F16 ? mul2(pair(u, v), both(lift * exp2f(-kHalfLift))) : pair(u, v);
+                                const uint64_t pr = F16 ? mul2(pair(u, v), both(lift)) : pair(u, v);
                                 unpair(mul2(pr, add2(pair(e[c], e[c + 1]), d2[q])), x, y);
                                 r1[2 * k + q] = round2<T>(u, v);
                                 r2[2 * k + q] = round2<T>(x, y);
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
             // DKV: warpgroups 0 and 2 store dv, 1 and 3 dk, half of the columns each; dq: 32 columns each, as far as they go
             const uint32_t group = warp >> 2;
             const CUtensorMap *const to = &p.out[DKV ? group & 1u : 0u];
-            const float by = DKV && !(group & 1u) ? (F16 ? exp2f(-kHalfLift) : 1.0f) : F16 ? __fdiv_rn(a.scale, lift) : a.scale;
+            const float by = DKV && !(group & 1u) ? (F16 ? exp2f(-kHalfLift) : 1.0f) : F16 ? __fdiv_rn(a.scale * exp2f(-kHalfLift), lift) : a.scale;
             constexpr uint32_t WIDTH = DKV ? DP / 2 : 32;
             const uint32_t from = (DKV ? group >> 1 : group) * WIDTH;
             const uint32_t acc = tmem + (DKV ? (group & 1u) * DP : 0u) + from + quarter;
