@@ -351,8 +351,8 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
  * gives no gradient; what lies in k and v beyond a sequence's length is never used, whatever it holds.  A visible score that
  * is NaN or +inf, or scores that are all -inf, make the row's out NaN; so does NaN in v for the rows of its 256 queries' tile,
  * even those that causality keeps from that key.  (Binary32: an infinite element of q, k or v counts as NaN.  16-bit:
- * scores beyond 2^27 in magnitude may come out as NaN, too.)  Query head h
- * reads key head h / (heads / kv_heads); the gradients of shared heads are summed over their readers.
+ * scores beyond 2^27 in magnitude may come out as NaN, too.)  Query head h reads key head h / (heads / kv_heads); the
+ * gradients of shared heads are summed over their readers.
  *   d_q, d_out, d_grad_out, d_grad_q : [batch, queries, heads, head_dim]
  *   d_k, d_v, d_grad_k, d_grad_v     : [batch, keys, kv_heads, head_dim]
  * all of dtype, head_dim elements contiguous, the other dimensions by the strides below ({batch, sequence, head}, in
@@ -360,7 +360,8 @@ daf_status daf_tensor_decompress(uint32_t dtype, const void *d_packed, uint64_t 
  * 16 bytes, at least head_dim and below 2^36.  d_lse: [batch, heads, queries] floats, contiguous.  d_key_lengths: batch
  * int32.  Softmax statistics and sums are kept in binary32.  16-bit inputs: probabilities and score gradients are rounded
  * to dtype where they enter the second products (float16: scaled by powers of two, so that neither the size of v nor that of a
- * row's grad_out matters to grad_q, nor the size of a head's largest row to grad_k); binary32 inputs: every factor keeps its 24 bits (three bfloat16 parts).
+ * row's grad_out matters to grad_q, nor the size of a head's largest row to grad_k); binary32 inputs: every factor keeps its
+ * 24 bits (three bfloat16 parts).
  * heads a multiple of kv_heads, head_dim a multiple of 8 (DAF_ERR_SHAPE), head_dim <= 128, queries and keys <= 2^24,
  * batch * heads <= 65535, batch * heads * queries and batch * kv_heads * keys <= 2^32 (DAF_ERR_UNSUPPORTED).
  * batch, queries or keys == 0 are valid.

@@ -617,7 +617,8 @@ def attention(q, k, v, *, causal: bool = False, scale: float | None = None, key_
     exponentials [B, H, Sq] that the backward pass needs (daf_attention).  Slices of a packed projection are read in place;
     tensors the kernels cannot address (D not contiguous, rows off 16-byte boundaries, broadcast dimensions) are copied
     first.  scale: 1 / sqrt(D) by default; key_lengths: int32 [B]; causal: query i sees keys up to i + Sk - Sq.  check waits
-    for the device and raises on an error there (without it, ``check_device`` tells later).  With a stream, results and scratch belong to that stream."""
+    for the device and raises on an error there (without it, ``check_device`` tells later).  With a stream, results and scratch
+    belong to that stream."""
     if stream is not None:
         with _torch().cuda.stream(stream):
             return attention(q, k, v, causal=causal, scale=scale, key_lengths=key_lengths, out=out, lse=lse, check=check)

@@ -18,8 +18,9 @@
 // P and dS are rounded to the input type, which the second products need; everything else is binary32.  float16 reaches
 // from 6e-5 (6e-8 with fewer bits) to 65504, and dS may lie anywhere -- a mean over many tokens, a loss on a few of them or a
 // loss scale moves grad_out --, so there dS is multiplied by the power of two that brings its bound 2 |grad_out| max |v| to
-// [2^14, 2^15) (max |v| taken as sqrt(D) times the largest element), and the sums by its inverse: |grad_out| is the row's in dq, whose sums belong to one row, and the largest row's
-// of the head in dk.  P is held 2^8 times its size: probabilities down to 2^-22 keep their bits.
+// [2^14, 2^15) (max |v| taken as sqrt(D) times the largest element), and the sums by its inverse: |grad_out| is the row's in
+// dq, whose sums belong to one row, and the largest row's of the head in dk.  P is held 2^8 times its size: probabilities down
+// to 2^-22 keep their bits.
 #pragma once
 #include "attention.cuh"
 #include "tensor_core.cuh"
@@ -396,7 +397,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_kernel(const _
                 // P and dS are zero in a masked column, but 0 * NaN is not.  Cleared are rows of k behind the sequence's end that
                 // the last product's steps of 16 keys still touch, and rows of q and grad_out that see no key at all.
                 const int dead = DKV && a.causal ? (int)(a.Sq - cur.row) - (int)a.Sk : 0;
-                const uint32_t clear_from = DKV ? 0u : cols, clear_to = !DKV ? (cur.it.n < a.Sk ? end : cols) : dead <= 0 ? 0u : dead < (int)kWalk ? (uint32_t)dead : kWalk;
+                const uint32_t clear_from = DKV ? 0u : cols;
+                const uint32_t clear_to = !DKV ? (cur.it.n < a.Sk ? end : cols) : dead <= 0 ? 0u : dead < (int)kWalk ? (uint32_t)dead : kWalk;
                 const bool clear = clear_from != clear_to;
                 uint64_t *const bar = clear ? &tail : &y_full[st];
                 unsigned char *const dst = s_y + st * 2u * Smem::kY;
