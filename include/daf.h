@@ -452,6 +452,118 @@ daf_status daf_clip_norm_batch(uint32_t n, const uint32_t *dtypes, const void *c
                                uint64_t workspace_bytes, daf_stream stream);
 
 /*
+ * Token embedding: out[t] = scale * weight[token[t]], rounded once to dtype; and its gradient
+ *   grad_weight[v] = scale * sum over the t with token[t] == v of grad_out[t], zero for rows that no token names,
+ * summed in binary32 in the order of t (within pieces of a fixed length, and these in order), rounded once to table_dtype.
+ *   d_tokens : `tokens` signed integers of token_bytes;  d_weight, d_grad_weight : [vocabulary, width] of table_dtype;
+ *   d_out, d_grad_out : [tokens, width] of dtype; all contiguous, pointers on the boundary of their elements (faster: width a
+ *   multiple of 8 and both matrices on the boundary of 8 elements).  table_dtype is dtype or DAF_F32.
+ * padding: a token whose row takes no gradient (daf_embedding_grad; its row of the gradient is zero), negative: none.  A token
+ * outside [0, vocabulary) gives a row of zeros and no gradient, and is recorded as DAF_ERR_INVALID_ARG in the word of
+ * daf_device_status (and in the workspace of daf_embedding_grad).  d_workspace: daf_embedding_grad_workspace(params) bytes (0 for
+ * bad params), 32-byte aligned, contents irrelevant.  No output may overlap an input.  tokens == 0 is valid.
+ * vocabulary and width are positive (DAF_ERR_SHAPE); vocabulary < 2^31 - 1, tokens <= 2^31 - 256, width <= 2^24 (UNSUPPORTED).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
+ */
+typedef struct daf_embedding_params {
+    uint32_t struct_size;     /* sizeof(daf_embedding_params)                          */
+    uint32_t dtype;           /* daf_dtype of out and grad_out                         */
+    uint32_t table_dtype;     /* daf_dtype of weight and grad_weight: dtype or DAF_F32 */
+    uint32_t token_bytes;     /* 4 or 8                                                */
+    uint64_t tokens;
+    uint64_t vocabulary;
+    uint32_t width;
+    float    scale;           /* finite                                                */
+    int64_t  padding;         /* negative: none; below vocabulary                      */
+    uint64_t reserved;        /* 0                                                     */
+} daf_embedding_params;
+daf_status daf_embedding(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out,
+                         daf_stream stream);
+uint64_t   daf_embedding_grad_workspace(const daf_embedding_params *params);
+daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_tokens, const void *d_grad_out,
+                              void *d_grad_weight, void *d_workspace, uint64_t workspace_bytes, daf_stream stream);
+
+/*
+ * Norms of queries and keys for each head, with the rotation by position in the same pass.  For every row x of head_dim
+ * elements of q and of k:
+ *   n = x / sqrt(mean(x^2) + eps) * weight     (q_weight or k_weight; ones where that is NULL)
+ *   the first rotary_dim elements of n in pairs (a, b): a' = a cos t - b sin t, b' = a sin t + b cos t with
+ *   t = position * frequency[i] for pair i; the elements behind rotary_dim stay as they are.
+ * Pair i is (i, i + rotary_dim / 2) for DAF_ROTARY_HALVES, (2 i, 2 i + 1) for DAF_ROTARY_PAIRS.  frequencies: HOST array of
+ * rotary_dim / 2 finite numbers (radians per position), or NULL for base^(-2 i / rotary_dim).  Angles are exact products modulo a
+ * turn, for positions of any size and sign.  d_positions: signed integers of position_bytes, [batch, tokens], or [tokens] with
+ * shared_positions; position_bytes == 0: token s of every sequence is at first_position + s.  Arithmetic in binary32, one rounding.
+ *   d_q, d_q_out, d_grad_q_out, d_grad_q : [batch, tokens, heads, head_dim];  d_k, ... : the same with kv_heads (0: no keys, NULL)
+ * of dtype, by the strides below ({batch, token, head}, in elements; a row contiguous): pointers 16-byte aligned, strides of
+ * extents above one multiples of 16 bytes, at least head_dim and below 2^36.  d_q_out may be d_q, d_k_out d_k with the same
+ * strides, and d_grad_q, d_grad_k may be one of their two inputs; otherwise nothing overlaps.  Weights: head_dim elements of param_dtype
+ * (DAF_F32 or dtype), 16-byte aligned.
+ * daf_rotary_norm_grad takes the inputs (q, k, not what the forward pass made of them) and the gradients of both outputs (laid out
+ * by q_out_stride and k_out_stride); the weights' gradients have their type and may be NULL (not wanted).  d_workspace:
+ * daf_rotary_norm_grad_workspace(params) bytes (0 for bad params), 16-byte aligned, contents irrelevant.
+ * head_dim and rotary_dim multiples of 8, rotary_dim <= head_dim, heads > 0 (DAF_ERR_SHAPE); head_dim <= 256, tokens <= 2^24,
+ * heads <= 65535, batch * tokens * heads < 2^30 (DAF_ERR_UNSUPPORTED).  batch or tokens == 0 is valid.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
+ */
+typedef enum daf_rotary_style { DAF_ROTARY_HALVES = 0, DAF_ROTARY_PAIRS = 1 } daf_rotary_style;
+typedef struct daf_rotary_params {
+    uint32_t struct_size;     /* sizeof(daf_rotary_params)                     */
+    uint32_t dtype;           /* daf_dtype of every matrix                     */
+    uint32_t param_dtype;     /* daf_dtype of the weights: DAF_F32 or dtype    */
+    uint32_t style;           /* daf_rotary_style                              */
+    uint32_t batch, tokens, heads, kv_heads, head_dim, rotary_dim;
+    uint32_t position_bytes;  /* 0, 4 or 8                                     */
+    uint32_t shared_positions;/* 0 or 1                                        */
+    int64_t  first_position;  /* of token 0, with position_bytes == 0          */
+    double   base;            /* positive; usually 10000                       */
+    float    eps;             /* >= 0                                          */
+    uint32_t reserved[3];     /* 0                                             */
+    uint64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];       /* {batch, token, head}      */
+    uint64_t grad_q_stride[3], grad_k_stride[3];                               /* daf_rotary_norm_grad only */
+} daf_rotary_params;
+daf_status daf_rotary_norm(const daf_rotary_params *params, const double *frequencies, const void *d_q, const void *d_k,
+                           const void *d_q_weight, const void *d_k_weight, const void *d_positions, void *d_q_out, void *d_k_out,
+                           daf_stream stream);
+uint64_t   daf_rotary_norm_grad_workspace(const daf_rotary_params *params);
+daf_status daf_rotary_norm_grad(const daf_rotary_params *params, const double *frequencies, const void *d_q, const void *d_k,
+                                const void *d_q_weight, const void *d_k_weight, const void *d_positions,
+                                const void *d_grad_q_out, const void *d_grad_k_out, void *d_grad_q, void *d_grad_k,
+                                void *d_grad_q_weight, void *d_grad_k_weight, void *d_workspace, uint64_t workspace_bytes,
+                                daf_stream stream);
+
+/*
+ * Orthogonalised updates: for each of n matrices g [rows, cols], x = g / (norm(g) + eps) with the norm over all elements, then
+ * `steps` times
+ *   x = a x + (b (x x^T) + c (x x^T)^2) x          (x^T x and products from the right where rows > cols, which is the same)
+ * an odd polynomial in the singular values of x, with (a, b, c) = coefficients.  (3.4445, -4.7750, 2.0315) five times takes
+ * singular values from about 0.005 of the norm upwards to somewhere between 0.7 and 1.2: the update of an optimizer that steps
+ * by the nearest orthogonal matrix.
+ * HOST arrays of n entries: dtypes, d_in, d_out, rows, cols (0 is fine).  Matrices contiguous, pointers on the boundary of their
+ * elements; d_out[i] may be d_in[i], otherwise nothing overlaps.  Results have their input's type.
+ * Arithmetic: products of 16-bit operands on the tensor cores, summed in binary32; the norm is summed in binary64.  DAF_BF16: x and
+ * its Gram matrices are held in float16 between the products (x behind the first two steps with 22 bits where it is added), whose
+ * effect is below the result's own rounding; DAF_F16 and DAF_F32: in two float16 parts (22 bits) throughout.  Entries
+ * below 2^-24 of a matrix's norm lose bits.  Singular values must stay below 4 on the way (the default coefficients keep them below
+ * 1.3), otherwise the result is not a number; so it is for a matrix with an element that is none or infinite.
+ * d_workspace: daf_orthogonalize_workspace(...) bytes (0 for bad arguments), 256-byte aligned, contents irrelevant; it holds the
+ * device status word afterwards (daf_poll_status: DAF_OK, or DAF_ERR_TIMEOUT when a wait inside a kernel ran out).
+ * rows, cols <= 65536, steps 1 to 64, coefficients and eps finite, eps > 0.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
+ */
+typedef struct daf_orthogonalize_params {
+    uint32_t struct_size;     /* sizeof(daf_orthogonalize_params) */
+    uint32_t steps;
+    float    coefficients[3];
+    float    eps;
+    uint32_t reserved[2];     /* 0                                */
+} daf_orthogonalize_params;
+uint64_t   daf_orthogonalize_workspace(const daf_orthogonalize_params *params, uint32_t n, const uint32_t *dtypes,
+                                       const uint64_t *rows, const uint64_t *cols);
+daf_status daf_orthogonalize(const daf_orthogonalize_params *params, uint32_t n, const uint32_t *dtypes, const void *const *d_in,
+                             void *const *d_out, const uint64_t *rows, const uint64_t *cols, void *d_workspace,
+                             uint64_t workspace_bytes, daf_stream stream);
+
+/*
  * Host-side page pool for packed buffers (Sec. 3.4.2: one preallocated contiguous arena,
  * page-granular first-fit allocation; Sec. 3.4.3: every allocation carries an importance,
  * and the least important one is evicted first).  The pool does bookkeeping only: it never

@@ -80,6 +80,24 @@ class daf_norm_params(ctypes.Structure):
                 ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float), ("reserved", ctypes.c_uint32)]
 
 
+class daf_embedding_params(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_uint32), ("table_dtype", ctypes.c_uint32),
+                ("token_bytes", ctypes.c_uint32), ("tokens", ctypes.c_uint64), ("vocabulary", ctypes.c_uint64), ("width", ctypes.c_uint32),
+                ("scale", ctypes.c_float), ("padding", ctypes.c_int64), ("reserved", ctypes.c_uint64)]
+
+
+class daf_rotary_params(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_uint32) for n in ("struct_size", "dtype", "param_dtype", "style", "batch", "tokens", "heads", "kv_heads",
+                                                "head_dim", "rotary_dim", "position_bytes", "shared_positions")]
+                + [("first_position", ctypes.c_int64), ("base", ctypes.c_double), ("eps", ctypes.c_float), ("reserved", ctypes.c_uint32 * 3)]
+                + [(n, _u64x3) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride", "grad_q_stride", "grad_k_stride")])
+
+
+class daf_orthogonalize_params(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("steps", ctypes.c_uint32), ("coefficients", ctypes.c_float * 3), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_uint32 * 2)]
+
+
 class DafError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -131,6 +149,14 @@ SIGNATURES = {
     "daf_clip_norm_workspace": (ctypes.c_uint64, [ctypes.c_uint32]),
     "daf_clip_norm_batch": (ctypes.c_int, [ctypes.c_uint32, _vp, _vp, _vp, _vp, ctypes.c_float, ctypes.c_float, _vp, _vp,
                                            ctypes.c_uint64, _vp]),
+    "daf_embedding": (ctypes.c_int, [ctypes.POINTER(daf_embedding_params)] + [_vp] * 4),
+    "daf_embedding_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_embedding_params)]),
+    "daf_embedding_grad": (ctypes.c_int, [ctypes.POINTER(daf_embedding_params)] + [_vp] * 4 + [ctypes.c_uint64, _vp]),
+    "daf_rotary_norm": (ctypes.c_int, [ctypes.POINTER(daf_rotary_params)] + [_vp] * 9),
+    "daf_rotary_norm_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_rotary_params)]),
+    "daf_rotary_norm_grad": (ctypes.c_int, [ctypes.POINTER(daf_rotary_params)] + [_vp] * 13 + [ctypes.c_uint64, _vp]),
+    "daf_orthogonalize_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_orthogonalize_params), ctypes.c_uint32, _vp, _vp, _vp]),
+    "daf_orthogonalize": (ctypes.c_int, [ctypes.POINTER(daf_orthogonalize_params), ctypes.c_uint32] + [_vp] * 6 + [ctypes.c_uint64, _vp]),
     "daf_pool_create": (_vp, [ctypes.c_uint64, ctypes.c_uint64]),
     "daf_pool_destroy": (None, [_vp]),
     "daf_pool_alloc": (ctypes.c_uint64, [_vp, ctypes.c_uint64, ctypes.c_double, _u64p]),
@@ -351,7 +377,7 @@ def daf_poll_status(d_workspace, stream=None) -> int:
 
 
 def daf_device_status(device=None, stream=None) -> int:
-    """The largest error that an attention call on `device` (the current one) has recorded since the last such question."""
+    """The largest error that an operator's call on `device` (the current one) has recorded since the last such question."""
     torch = _torch()
     with torch.cuda.device(device):                                  # None: stays
         return int(lib().daf_device_status(_raw_stream(torch.cuda.current_device(), stream)))
@@ -366,10 +392,10 @@ def daf_device_status_word(device=None) -> int:
 
 
 def check_device(device=None, stream=None) -> None:
-    """Waits for the stream and raises if an attention call on `device` gave up since the last question.  ``attention`` and
-    ``attention_grad`` do not wait for the device (unless called with check) and keep nothing that could be asked later, so ask
-    here once a step or once an epoch."""
-    _check(daf_device_status(device, stream), "attention (device status)")
+    """Waits for the stream and raises if an attention or orthogonalisation call on `device` gave up, or an embedding call met a
+    token that is none, since the last question.  These calls do not wait for the device (unless called with check) and keep
+    nothing that could be asked later, so ask here once a step or once an epoch."""
+    _check(daf_device_status(device, stream), "operators (device status)")
 
 
 def _ptr_array(tensors):
@@ -594,6 +620,64 @@ def daf_clip_norm_batch(d_in, d_out, max_norm, eps, d_norm, d_workspace, workspa
     _check(status, "daf_clip_norm_batch")
 
 
+def daf_embedding(params, d_tokens, d_weight, d_out, stream=None):
+    _check(_call(lib().daf_embedding, d_out, stream, ctypes.byref(params), _ptr(d_tokens), _ptr(d_weight), _ptr(d_out)), "daf_embedding")
+
+
+def daf_embedding_grad_workspace(params) -> int:
+    return int(lib().daf_embedding_grad_workspace(ctypes.byref(params)))
+
+
+def daf_embedding_grad(params, d_tokens, d_grad_out, d_grad_weight, d_workspace, workspace_bytes, stream=None):
+    status = _call(lib().daf_embedding_grad, d_grad_weight, stream, ctypes.byref(params), _ptr(d_tokens), _ptr(d_grad_out),
+                   _ptr(d_grad_weight), _ptr(d_workspace), workspace_bytes)
+    _check(status, "daf_embedding_grad")
+
+
+def _frequencies(frequencies):
+    return None if frequencies is None else (ctypes.c_double * len(frequencies))(*frequencies)
+
+
+def daf_rotary_norm(params, frequencies, d_q, d_k, d_q_weight, d_k_weight, d_positions, d_q_out, d_k_out, stream=None):
+    """frequencies: rotary_dim / 2 numbers or None, as for ``rotary_norm``."""
+    status = _call(lib().daf_rotary_norm, d_q, stream, ctypes.byref(params), _frequencies(frequencies), _ptr(d_q), _ptr(d_k), _ptr(d_q_weight),
+                   _ptr(d_k_weight), _ptr(d_positions), _ptr(d_q_out), _ptr(d_k_out))
+    _check(status, "daf_rotary_norm")
+
+
+def daf_rotary_norm_grad_workspace(params) -> int:
+    return int(lib().daf_rotary_norm_grad_workspace(ctypes.byref(params)))
+
+
+def daf_rotary_norm_grad(params, frequencies, d_q, d_k, d_q_weight, d_k_weight, d_positions, d_grad_q_out, d_grad_k_out, d_grad_q, d_grad_k,
+                         d_grad_q_weight, d_grad_k_weight, d_workspace, workspace_bytes, stream=None):
+    status = _call(lib().daf_rotary_norm_grad, d_q, stream, ctypes.byref(params), _frequencies(frequencies), _ptr(d_q), _ptr(d_k),
+                   _ptr(d_q_weight), _ptr(d_k_weight), _ptr(d_positions), _ptr(d_grad_q_out), _ptr(d_grad_k_out), _ptr(d_grad_q),
+                   _ptr(d_grad_k), _ptr(d_grad_q_weight), _ptr(d_grad_k_weight), _ptr(d_workspace), workspace_bytes)
+    _check(status, "daf_rotary_norm_grad")
+
+
+def _matrices(tensors):
+    """Types, rows and columns of matrices (dimensions behind the first are one), as the C ABI takes them."""
+    n = len(tensors)
+    rows = [t.shape[0] for t in tensors]
+    return ((ctypes.c_uint32 * n)(*[dtype_code(t) for t in tensors]), (ctypes.c_uint64 * n)(*rows),
+            (ctypes.c_uint64 * n)(*[t.numel() // r if r else 0 for t, r in zip(tensors, rows)]))
+
+
+def daf_orthogonalize_workspace(params, d_in) -> int:
+    types, rows, cols = _matrices(d_in)
+    return int(lib().daf_orthogonalize_workspace(ctypes.byref(params), len(d_in), types, rows, cols))
+
+
+def daf_orthogonalize(params, d_in, d_out, d_workspace, workspace_bytes, stream=None):
+    """d_in, d_out: lists of contiguous matrices."""
+    types, rows, cols = _matrices(d_in)
+    status = _call(lib().daf_orthogonalize, d_workspace, stream, ctypes.byref(params), len(d_in), types, _ptr_array(d_in), _ptr_array(d_out), rows,
+                   cols, _ptr(d_workspace), workspace_bytes)
+    _check(status, "daf_orthogonalize")
+
+
 _native_module = None
 
 
@@ -699,6 +783,95 @@ def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, strea
     norm, status = _native().clip_grad_norm(grads, None if out is None else list(out), max_norm, eps)
     _check(status, "daf_clip_norm_batch")
     return norm
+
+
+def embedding(tokens, weight, *, scale: float = 1.0, dtype=None, out=None, check: bool = False, stream=None):
+    """scale * weight[tokens]: rows of weight [vocabulary, width] for int32 or int64 tokens of any shape (daf_embedding).  dtype:
+    the output's type, the weight's by default, any of the three where the weight is float32.  A token outside the vocabulary
+    gives zeros and is recorded for ``check_device``; check asks at once (and waits for the device)."""
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return embedding(tokens, weight, scale=scale, dtype=dtype, out=out, check=check)
+    made, status = _native().embedding(tokens, weight, scale, dtype, out)
+    _check(status, "daf_embedding")
+    if check:
+        _check(daf_device_status(made.device), "daf_embedding (device status)")
+    return made if out is None else out
+
+
+def embedding_grad(tokens, grad_out, vocabulary: int, *, scale: float = 1.0, padding: int | None = None, dtype=None, out=None,
+                   check: bool = False, stream=None):
+    """The gradient of ``embedding`` with respect to its weight, [vocabulary, width]: scale times the sum of grad_out's rows over
+    each token's places, in their order and in float32, zero for the others and for the padding token (daf_embedding_grad).
+    dtype: the gradient's type, grad_out's by default, or float32."""
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return embedding_grad(tokens, grad_out, vocabulary, scale=scale, padding=padding, dtype=dtype, out=out, check=check)
+    made, status = _native().embedding_grad(tokens, grad_out, vocabulary, scale, padding, dtype, out, check)
+    _check(status, "daf_embedding_grad")
+    return made if out is None else out
+
+
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+_STYLES = {"halves": ROTARY_HALVES, "pairs": ROTARY_PAIRS}
+
+
+def _style(where: str, style: str) -> int:
+    if style not in _STYLES:
+        raise ValueError(f"{where}: style is 'halves' or 'pairs'")
+    return _STYLES[style]
+
+
+def rotary_norm(q, k, q_weight=None, k_weight=None, *, positions=None, rotary_dim: int | None = None, base: float = 10000.0,
+                style: str = "halves", eps: float = 1e-6, frequencies=None, out=None, stream=None):
+    """(q, k): every row of q [B, S, H, D] and k [B, S, Hkv, D] (None: queries alone) divided by its root mean square, times
+    the weight [D], its first rotary_dim elements turned by position (daf_rotary_norm).  positions: int32 or int64, [B, S] or [S], a
+    whole number (the first token's position in every sequence), or None for 0.  style: pairs (i, i + rotary_dim / 2) or
+    (2 i, 2 i + 1), turned by position * base^(-2 i / rotary_dim), or by position * frequencies[i].  Slices of a packed projection
+    are read in place; what the kernels cannot address is copied first.  out: (q, k) to write into, which may be q and k."""
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return rotary_norm(q, k, q_weight, k_weight, positions=positions, rotary_dim=rotary_dim, base=base, style=style, eps=eps,
+                               frequencies=frequencies, out=out)
+    qo, ko = (None, None) if out is None else out
+    frequencies = None if frequencies is None else [float(f) for f in frequencies]
+    qo, ko, status = _native().rotary_norm(q, k, q_weight, k_weight, positions, rotary_dim, base, _style("rotary_norm", style), eps,
+                                           frequencies, qo, ko)
+    _check(status, "daf_rotary_norm")
+    return qo, ko
+
+
+def rotary_norm_grad(q, k, q_weight, k_weight, grad_q_out, grad_k_out, *, positions=None, rotary_dim: int | None = None,
+                     base: float = 10000.0, style: str = "halves", eps: float = 1e-6, frequencies=None, grads=None, stream=None):
+    """(grad_q, grad_k, grad_q_weight, grad_k_weight) of ``rotary_norm`` from its inputs and the gradients of its outputs
+    (daf_rotary_norm_grad); None where there is no such input.  grads: (grad_q, grad_k) to write into, e.g. slices of one packed
+    gradient."""
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return rotary_norm_grad(q, k, q_weight, k_weight, grad_q_out, grad_k_out, positions=positions, rotary_dim=rotary_dim, base=base,
+                                    style=style, eps=eps, frequencies=frequencies, grads=grads)
+    gq, gk = (None, None) if grads is None else grads
+    frequencies = None if frequencies is None else [float(f) for f in frequencies]
+    *made, status = _native().rotary_norm_grad(q, k, q_weight, k_weight, positions, rotary_dim, base, _style("rotary_norm_grad", style), eps,
+                                               frequencies, grad_q_out, grad_k_out, gq, gk)
+    _check(status, "daf_rotary_norm_grad")
+    return tuple(made)
+
+
+def orthogonalize(updates, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, check: bool = False,
+                  stream=None) -> list:
+    """The matrices of ``updates`` (dimensions behind the first count as one) with their singular values taken towards one: x =
+    g / (norm(g) + eps), then ``steps`` times x = a x + (b x x^T + c (x x^T)^2) x (daf_orthogonalize).  All matrices of a call run
+    together, so give them at once.  out: contiguous tensors to write into, which may be the updates themselves."""
+    if stream is not None:
+        with _torch().cuda.stream(stream):
+            return orthogonalize(updates, steps=steps, coefficients=coefficients, eps=eps, out=out, check=check)
+    updates = list(updates)
+    if not updates:
+        return []
+    made, status = _native().orthogonalize(updates, None if out is None else list(out), steps, tuple(coefficients), eps, check)
+    _check(status, "daf_orthogonalize")
+    return made if out is None else list(out)
 
 
 class Pool:

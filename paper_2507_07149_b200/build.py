@@ -18,7 +18,7 @@ HEADERS = [os.path.join(CSRC, h) for h in ("common.cuh", "compress_shared.cuh", 
 
 CU_SOURCES = ["api.cu", "compress.cu", "compress_stream_f32.cu", "compress_stream_f16.cu", "compress_stream_bf16.cu", "compress_twowidth_f32.cu", "compress_twowidth_f16.cu", "compress_twowidth_bf16.cu", "compress_twopass_f32.cu", "compress_twopass_f16.cu", "compress_twopass_bf16.cu", "compress_general_f32.cu", "compress_general_f16.cu",
               "compress_general_bf16.cu", "decompress.cu", "group_offsets.cu", "tensorwise.cu",
-              "attention.cu", "attention_rows.cu", "attention_tc_f32.cu", "attention_tc_f16.cu", "attention_tc_bf16.cu", "residual_norm.cu", "clip_norm.cu"]
+              "attention.cu", "attention_rows.cu", "attention_tc_f32.cu", "attention_tc_f16.cu", "attention_tc_bf16.cu", "residual_norm.cu", "clip_norm.cu", "embedding.cu", "rotary_norm.cu", "orthogonalize.cu"]
 CXX_SOURCES = ["pool.cpp", "store.cpp"]
 
 # The Python module that marshals torch tensors for the transformer operators (host code only).

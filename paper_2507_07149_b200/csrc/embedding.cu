@@ -1,0 +1,544 @@
+// Token embedding and its gradient.
+//
+//   out[t] = RNE(scale * weight[token[t]]),      grad_weight[v] = RNE(scale * sum over t with token[t] == v of grad_out[t])
+//
+// Forward: a gather of rows; bound by HBM (the rows named, read once from there, and the output).
+//
+// Backward: the sum of a row's tokens runs in the order of the tokens, in binary32 and without atomics on floats, so the
+// same inputs give the same bits.  Three launches:
+//   embedding_sort_kernel  one cluster of eight CTAs sorts (token, position) by token, keeping the order of positions: a radix
+//                          sort with digits of at most nine bits, whose histograms the CTAs read from one another's shared memory.
+//                          The other clusters meanwhile write the zeros of the whole gradient, so the sort costs time only
+//                          where it takes longer than that.
+//   embedding_sum_kernel   the sorted list is cut into chunks of equal length; a run of equal tokens inside a chunk is summed and
+//                          written, the part of one that crosses a chunk's border goes to the workspace.  Equal
+//                          chunks keep the SMs evenly busy however often one token occurs.
+//   embedding_join_kernel  the parts of a run that crosses borders are added up, in order.
+// Bound: HBM, grad_out read once and the table's gradient written once (rows that occur: twice).
+#include "common.cuh"
+
+namespace daf {
+
+constexpr uint32_t kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigitBits = 9, kDigits = 1u << kDigitBits;
+constexpr uint32_t kRowThreads = 256;
+constexpr uint32_t kLaneCols = 8;               // columns of a lane
+
+struct EmbeddingArgs {
+    const void *tokens, *weight, *grad_out;
+    void *out, *grad_weight;
+    uint64_t n, table_elems;
+    uint32_t wide_tokens, vocabulary, width, lanes_log2, slabs;   // lanes of a row, slabs of 8 * lanes columns
+    float scale;
+    long long padding;
+    // backward
+    uint32_t *keys[2], *places[2], *jobs;       // jobs[0]: how many; then the chunks in which a run that crosses a border begins
+    float *part;                                // [2][chunks][pitch]: runs that a chunk begins with | ends with
+    uint32_t chunk, n_chunks, pitch, digit_bits, passes;
+    WorkspaceHeader *header;
+    unsigned int *device_status;
+};
+
+__device__ __forceinline__ long long token_at(const EmbeddingArgs &a, uint64_t i)
+{
+    return a.wide_tokens ? __ldg(reinterpret_cast<const long long *>(a.tokens) + i) : (long long)__ldg(reinterpret_cast<const int *>(a.tokens) + i);
+}
+__device__ __forceinline__ float get1(float v) { return v; }
+__device__ __forceinline__ float get1(__half v) { return __half2float(v); }
+__device__ __forceinline__ float get1(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T put1(float v);
+template <> __device__ __forceinline__ float put1<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half put1<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 put1<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// The eight columns of a lane: consecutive ones in wide accesses where every row starts on their boundary (VEC), else
+// `lanes` apart, one element per access (a row's accesses are contiguous all the same).
+template <bool VEC> __device__ __forceinline__ uint32_t lane_column(uint32_t lane, uint32_t lanes, uint32_t e)
+{
+    return VEC ? lane * kLaneCols + e : lane + lanes * e;
+}
+template <typename T, bool VEC> __device__ __forceinline__ void load_columns(const T *row, uint32_t first, uint32_t lanes, uint32_t width, float (&x)[8])
+{
+    if constexpr (VEC) {
+        Elem<T>::load8(row + first, x);
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < kLaneCols; e++) x[e] = first + lanes * e < width ? get1(row[first + lanes * e]) : 0.0f;
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store_columns(T *row, uint32_t first, uint32_t lanes, uint32_t width, const float (&x)[8])
+{
+    if constexpr (VEC) {
+        Elem<T>::store8(row + first, x);
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < kLaneCols; e++)
+            if (first + lanes * e < width) row[first + lanes * e] = put1<T>(x[e]);
+    }
+}
+
+// --------------------------------------------------------------------------------------------- forward
+constexpr uint32_t kForwardSlabs = 4;           // slabs of a row in flight
+
+template <typename W, typename A, bool VEC> __global__ void __launch_bounds__(kRowThreads) embedding_kernel(const __grid_constant__ EmbeddingArgs a)
+{
+    const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u);
+    const uint32_t per_row = (a.slabs + kForwardSlabs - 1u) / kForwardSlabs;
+    const uint64_t items = a.n * per_row, step = (uint64_t)gridDim.x * (kRowThreads >> a.lanes_log2);
+    for (uint64_t i = (uint64_t)blockIdx.x * (kRowThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2); i < items; i += step) {
+        const uint64_t t = per_row == 1u ? i : i / per_row;
+        const uint32_t slab = (uint32_t)(i - t * per_row) * kForwardSlabs;
+        const long long token = token_at(a, t);
+        const bool known = token >= 0 && token < (long long)a.vocabulary;
+        if (!known && lane == 0 && slab == 0) atomicMax(a.device_status, (unsigned int)DAF_ERR_INVALID_ARG);
+        const W *src = reinterpret_cast<const W *>(a.weight) + (uint64_t)(known ? token : 0) * a.width;
+        A *dst = reinterpret_cast<A *>(a.out) + t * a.width;
+        float x[kForwardSlabs][8];
+#pragma unroll
+        for (uint32_t j = 0; j < kForwardSlabs; j++) {
+            const uint32_t col = (slab + j) * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
+            if (col < a.width && known) load_columns<W, VEC>(src, col, lanes, a.width, x[j]);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[j][e] = 0.0f;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kForwardSlabs; j++) {
+            const uint32_t col = (slab + j) * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
+            if (col >= a.width) continue;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) y[e] = x[j][e] * a.scale;
+            store_columns<A, VEC>(dst, col, lanes, a.width, y);
+        }
+    }
+}
+
+// --------------------------------------------------------------------------------------------- backward: the sort
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// All threads of the cluster; writes before it, to global memory too, are seen behind it.
+__device__ __forceinline__ void cluster_meet()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t read_peer(const uint32_t *mine, uint32_t rank)
+{
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+struct SortShared {
+    uint32_t count[kSortWarps][kDigits];        // of each warp; then where its next item of a digit goes, from the digit's base on
+    uint32_t total[kDigits], base[kDigits], warp_sum[kDigits / 32];
+    uint32_t unknown;
+};
+
+// Zeros from byte `from` to `to`, by `threads` threads.
+__device__ void fill_zeros(char *at, uint64_t bytes, uint64_t thread, uint64_t threads)
+{
+    const uint64_t off = (32u - (reinterpret_cast<uintptr_t>(at) & 31u)) & 31u, head = off < bytes ? off : bytes;
+    const uint64_t units = (bytes - head) / 32u, tail = head + units * 32u;
+    const float none[8] = {};
+    for (uint64_t u = thread; u < units; u += threads) Elem<float>::store8(at + head + u * 32u, none);
+    if (thread < head / 2u) reinterpret_cast<uint16_t *>(at)[thread] = 0;
+    if (thread < (bytes - tail) / 2u) reinterpret_cast<uint16_t *>(at + tail)[thread] = 0;
+}
+
+// One round of a warp: the lanes' digits, where each one's item lies among those of the digit in this warp so far, and the
+// count moved on.  Lanes without an item take part with a digit of their own.
+__device__ __forceinline__ uint32_t place_in_warp(uint32_t *count, uint32_t digit, bool item, uint32_t lane)
+{
+    const uint32_t same = __match_any_sync(0xffffffffu, item ? digit : kDigits + lane);
+    const uint32_t before = item ? count[digit] : 0u;
+    __syncwarp();
+    if (item && (same & ((1u << lane) - 1u)) == 0u) count[digit] = before + __popc(same);
+    __syncwarp();
+    return before + __popc(same & ((1u << lane) - 1u));
+}
+
+__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads) embedding_sort_kernel(const __grid_constant__ EmbeddingArgs a, uint32_t table_bytes)
+{
+    extern __shared__ __align__(16) unsigned char raw[];
+    SortShared &s = *reinterpret_cast<SortShared *>(raw);
+    if (blockIdx.x >= kSortCtas) {
+        fill_zeros(reinterpret_cast<char *>(a.grad_weight), a.table_elems * table_bytes, (uint64_t)(blockIdx.x - kSortCtas) * kSortThreads + threadIdx.x,
+                   (uint64_t)(gridDim.x - kSortCtas) * kSortThreads);
+        return;
+    }
+    const uint32_t rank = cluster_rank(), lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, digits = 1u << a.digit_bits;
+    // every warp has a run of the list, in the order of the warps
+    const uint64_t per_warp = (a.n + kSortCtas * kSortThreads - 1u) / (kSortCtas * kSortThreads) * 32u;
+    const uint64_t lo = (uint64_t)(rank * kSortWarps + warp) * per_warp, end = lo + per_warp < a.n ? lo + per_warp : a.n;
+    if (threadIdx.x == 0) {
+        s.unknown = 0;
+        if (rank == 0) {
+            a.jobs[0] = 0;
+            a.header->status = DAF_OK;
+        }
+    }
+    __syncthreads();
+    for (uint32_t pass = 0; pass < a.passes; pass++) {
+        const uint32_t shift = pass * a.digit_bits, from = (pass + 1u) & 1u, to = pass & 1u;
+        const auto key_of = [&](uint64_t i) -> uint32_t {
+            if (pass) return __ldcg(a.keys[from] + i);
+            const long long t = token_at(a, i);
+            return t < 0 || t >= (long long)a.vocabulary || t == a.padding ? a.vocabulary : (uint32_t)t;
+        };
+        for (uint32_t d = lane; d < digits; d += 32u) s.count[warp][d] = 0;
+        __syncwarp();
+        bool unknown = false;
+        for (uint64_t at = lo; at < end; at += 128u) {              // four rounds, their loads together
+            uint32_t key[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                const uint64_t i = at + j * 32u + lane;
+                key[j] = i < end ? key_of(i) : 0u;
+                if (pass == 0 && i < end && key[j] == a.vocabulary) {
+                    const long long t = token_at(a, i);
+                    unknown |= t < 0 || t >= (long long)a.vocabulary;
+                }
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++)
+                if (at + j * 32u < end) place_in_warp(s.count[warp], key[j] >> shift & (digits - 1u), at + j * 32u + lane < end, lane);
+        }
+        if (unknown) s.unknown = 1;
+        __syncthreads();
+        uint32_t all = 0, before = 0;
+        if (threadIdx.x < digits) {
+            uint32_t sum = 0;
+#pragma unroll 8
+            for (uint32_t w = 0; w < kSortWarps; w++) {
+                const uint32_t c = s.count[w][threadIdx.x];
+                s.count[w][threadIdx.x] = sum;
+                sum += c;
+            }
+            s.total[threadIdx.x] = sum;
+        }
+        cluster_meet();
+        if (threadIdx.x < digits) {
+#pragma unroll
+            for (uint32_t r = 0; r < kSortCtas; r++) {
+                const uint32_t c = read_peer(&s.total[threadIdx.x], r);
+                before += r < rank ? c : 0u;
+                all += c;
+            }
+        }
+        uint32_t upto = all;                                        // sum over this and the lower digits
+#pragma unroll
+        for (uint32_t d = 1; d < 32u; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 31u && warp < kDigits / 32u) s.warp_sum[warp] = upto;
+        __syncthreads();
+        if (threadIdx.x < digits) {
+            uint32_t lower = 0;
+            for (uint32_t w = 0; w < warp; w++) lower += s.warp_sum[w];
+            s.base[threadIdx.x] = lower + upto - all + before;
+        }
+        __syncthreads();
+        for (uint64_t at = lo; at < end; at += 128u) {
+            uint32_t key[4], place[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                const uint64_t i = at + j * 32u + lane;
+                key[j] = i < end ? key_of(i) : 0u;
+                place[j] = i < end ? (pass ? __ldcg(a.places[from] + i) : (uint32_t)i) : 0u;
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                if (at + j * 32u >= end) break;
+                const bool item = at + j * 32u + lane < end;
+                const uint32_t digit = key[j] >> shift & (digits - 1u);
+                const uint32_t p = place_in_warp(s.count[warp], digit, item, lane) + s.base[digit];
+                if (item) {
+                    a.keys[to][p] = key[j];
+                    a.places[to][p] = place[j];
+                }
+            }
+        }
+        cluster_meet();
+    }
+    if (threadIdx.x == 0 && s.unknown) record_error(a.header, a.device_status, DAF_ERR_INVALID_ARG);
+    // the lists end with tokens that are none, up to a whole number of chunks
+    const uint32_t last = (a.passes + 1u) & 1u;
+    for (uint64_t i = a.n + rank * kSortThreads + threadIdx.x; i < (uint64_t)a.n_chunks * a.chunk; i += kSortCtas * kSortThreads) {
+        a.keys[last][i] = a.vocabulary;
+        a.places[last][i] = 0;
+    }
+}
+
+// --------------------------------------------------------------------------------------------- backward: the sums
+template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) embedding_sum_kernel(const __grid_constant__ EmbeddingArgs a)
+{
+    const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u);
+    const uint64_t item = (uint64_t)blockIdx.x * (kRowThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    if (item >= (uint64_t)a.n_chunks * a.slabs) return;
+    const uint32_t chunk = (uint32_t)(item / a.slabs), slab = (uint32_t)(item - (uint64_t)chunk * a.slabs);
+    const uint32_t col = slab * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
+    const bool mine = col < a.width;
+    const uint32_t last = (a.passes + 1u) & 1u, none = a.vocabulary;
+    const uint64_t first = (uint64_t)chunk * a.chunk;
+    const uint32_t *keys = a.keys[last] + first, *places = a.places[last] + first;
+    const uint32_t ahead = chunk ? __ldg(keys - 1) : none, behind = chunk + 1u < a.n_chunks ? __ldg(keys + a.chunk) : none;
+    const A *grad = reinterpret_cast<const A *>(a.grad_out);
+    const uint64_t part_col = (uint64_t)slab * lanes * kLaneCols + lane * kLaneCols;    // parts are always held in runs of eight
+    float acc[8] = {};
+    uint32_t run = __ldg(keys);
+    bool open = run == ahead;                                       // the run began in an earlier chunk
+    const auto finish = [&](bool goes_on) {
+        if (run == none || !mine) return;
+        if (open || goes_on) {
+            Elem<float>::store8(a.part + ((uint64_t)(open ? 0u : a.n_chunks) + chunk) * a.pitch + part_col, acc);
+            return;
+        }
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] = acc[e] * a.scale;
+        store_columns<W, VEC>(reinterpret_cast<W *>(a.grad_weight) + (uint64_t)run * a.width, col, lanes, a.width, y);
+    };
+    for (uint32_t i = 0; i < a.chunk; i += 8u) {
+        uint32_t key[8], place[8];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            *reinterpret_cast<uint4 *>(key + 4 * h) = __ldg(reinterpret_cast<const uint4 *>(keys + i) + h);
+            *reinterpret_cast<uint4 *>(place + 4 * h) = __ldg(reinterpret_cast<const uint4 *>(places + i) + h);
+        }
+        if (key[0] == none) break;
+        float x[8][8];
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (mine && key[j] != none) load_columns<A, VEC>(grad + (uint64_t)place[j] * a.width, col, lanes, a.width, x[j]);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            if (key[j] != run) {
+                finish(false);
+                run = key[j];
+                open = false;
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[e] = 0.0f;
+            }
+            if (mine && run != none)
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[e] += x[j][e];
+        }
+    }
+    const bool goes_on = run != none && run == behind;
+    finish(goes_on);
+    if (goes_on && !open && slab == 0 && lane == 0) a.jobs[1u + atomicAdd(a.jobs, 1u)] = chunk;
+}
+
+// --------------------------------------------------------------------------------------------- backward: runs across chunks
+template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) embedding_join_kernel(const __grid_constant__ EmbeddingArgs a)
+{
+    constexpr uint32_t kWarps = kRowThreads / 32;
+    __shared__ float s_sum[kWarps][256];
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, blocks = (a.pitch + 255u) / 256u;
+    const uint32_t *keys = a.keys[(a.passes + 1u) & 1u];
+    const uint64_t work = (uint64_t)a.jobs[0] * blocks;
+    for (uint64_t i = blockIdx.x; i < work; i += gridDim.x) {
+        const uint32_t job = (uint32_t)(i / blocks), block = (uint32_t)(i - (uint64_t)job * blocks);
+        const uint32_t begin = a.jobs[1u + job], key = __ldg(keys + (uint64_t)(begin + 1u) * a.chunk);
+        // the last chunk that begins with the key, thirty-two probes at a time: it is in [lo, hi)
+        uint32_t lo = begin + 1u, hi = a.n_chunks;
+        while (hi - lo > 1u) {
+            const uint32_t step = (hi - lo + 31u) / 32u;
+            const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
+            const uint32_t yes = __ballot_sync(0xffffffffu, at < hi && __ldg(keys + at * a.chunk) == key);
+            const uint32_t most = 31u - __clz(yes);                 // lane 0 always says yes
+            const uint32_t next = lo + most * step;
+            hi = hi - next < step ? hi : next + step;
+            lo = next;
+        }
+        const uint32_t parts = lo - begin + 1u;                     // the first from the second half of the workspace
+        const uint32_t from = (uint32_t)((uint64_t)parts * warp / kWarps), to = (uint32_t)((uint64_t)parts * (warp + 1u) / kWarps);
+        const uint32_t col = block * 256u + lane * 8u;
+        float acc[8] = {};
+        if (col < a.pitch) {
+#pragma unroll 4
+            for (uint32_t p = from; p < to; p++) {
+                float x[8];
+                Elem<float>::load8(a.part + ((uint64_t)(p ? 0u : a.n_chunks) + begin + p) * a.pitch + col, x);
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[e] += x[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) s_sum[warp][e * 32u + lane] = acc[e];
+        __syncthreads();
+        float sum = 0.0f;                                           // thread: element threadIdx.x / 32 of lane threadIdx.x % 32
+#pragma unroll
+        for (uint32_t w = 0; w < kWarps; w++) sum += s_sum[w][threadIdx.x];
+        // where that is in the row: parts are held lane by lane, as the lanes of embedding_sum_kernel own them
+        const uint32_t lanes = 1u << a.lanes_log2, at = block * 256u + lane * 8u, e = warp;
+        const uint32_t slab = at / (lanes * 8u), owner = at / 8u % lanes;
+        const uint32_t c = slab * lanes * 8u + lane_column<VEC>(owner, lanes, 0) + (VEC ? e : lanes * e);
+        if (at < a.pitch && c < a.width) reinterpret_cast<W *>(a.grad_weight)[(uint64_t)key * a.width + c] = put1<W>(sum * a.scale);
+        __syncthreads();
+    }
+}
+
+// --------------------------------------------------------------------------------------------- host
+static uint32_t elem_bytes(uint32_t dtype) { return dtype == DAF_F32 ? 4u : 2u; }
+
+static daf_status check_embedding(const daf_embedding_params *p)
+{
+    if (!p || p->struct_size != sizeof(*p) || p->dtype > DAF_BF16 || p->table_dtype > DAF_BF16 || p->reserved != 0 ||
+        (p->table_dtype != p->dtype && p->table_dtype != DAF_F32) || (p->token_bytes != 4u && p->token_bytes != 8u) ||
+        !(p->scale - p->scale == 0.0f))
+        return DAF_ERR_INVALID_ARG;
+    if (p->vocabulary == 0 || p->width == 0) return DAF_ERR_SHAPE;
+    if (p->vocabulary > 0x7FFFFFFEull || p->tokens > 0x7FFFFF00ull || p->width > (1u << 24)) return DAF_ERR_UNSUPPORTED;
+    if (p->padding >= (int64_t)p->vocabulary) return DAF_ERR_INVALID_ARG;
+    return DAF_OK;
+}
+
+// Lanes of a row: as many as its units of eight columns, a power of two, 32 at most.
+static void row_shape(EmbeddingArgs *a)
+{
+    const uint32_t units = (a->width + kLaneCols - 1u) / kLaneCols;
+    a->lanes_log2 = 0;
+    while (a->lanes_log2 < 5u && (1u << a->lanes_log2) < units) a->lanes_log2++;
+    const uint32_t cols = kLaneCols << a->lanes_log2;
+    a->slabs = (a->width + cols - 1u) / cols;
+    a->pitch = a->slabs * cols;
+}
+
+// Chunks of the sorted list: 128 tokens, or as few (16 at least) as leave every SM 32 warps, each with eight rows on their way.
+static void chunk_shape(EmbeddingArgs *a)
+{
+    constexpr uint64_t kWarpsWanted = 148u * 32u;
+    const uint64_t warps_of_row = (uint64_t)a->slabs << a->lanes_log2;      // in lanes
+    a->chunk = 128u;
+    while (a->chunk > 16u && (a->n + a->chunk - 1u) / a->chunk * warps_of_row < kWarpsWanted * 32u) a->chunk /= 2u;
+    a->n_chunks = (uint32_t)((a->n + a->chunk - 1u) / a->chunk);
+}
+
+static uint64_t up256(uint64_t n) { return (n + 255u) & ~255ull; }
+
+static EmbeddingArgs embedding_args(const daf_embedding_params *p)
+{
+    EmbeddingArgs a = {};
+    a.n = p->tokens;
+    a.table_elems = p->vocabulary * p->width;
+    a.wide_tokens = p->token_bytes == 8u;
+    a.vocabulary = (uint32_t)p->vocabulary;
+    a.width = p->width;
+    a.scale = p->scale;
+    a.padding = p->padding;
+    row_shape(&a);
+    chunk_shape(&a);
+    uint32_t bits = 32u - (uint32_t)__builtin_clz(a.vocabulary);
+    a.passes = (bits + kDigitBits - 1u) / kDigitBits;
+    a.digit_bits = (bits + a.passes - 1u) / a.passes;
+    return a;
+}
+
+static uint64_t grad_workspace(const EmbeddingArgs &a)
+{
+    const uint64_t list = up256((uint64_t)a.n_chunks * a.chunk * sizeof(uint32_t));
+    return sizeof(WorkspaceHeader) + 4u * list + up256((a.n_chunks + 1ull) * sizeof(uint32_t)) + 2ull * a.n_chunks * a.pitch * sizeof(float);
+}
+
+// Wide accesses: rows of both sides start on the boundaries of eight elements.
+static bool wide(const EmbeddingArgs &a, const void *x, uint32_t dx, const void *y, uint32_t dy)
+{
+    return a.width % kLaneCols == 0 && reinterpret_cast<uintptr_t>(x) % (8u * elem_bytes(dx)) == 0 && reinterpret_cast<uintptr_t>(y) % (8u * elem_bytes(dy)) == 0;
+}
+static bool on_elements(const void *p, uint32_t bytes) { return p && reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+template <typename W, typename A, bool VEC> static void forward(const EmbeddingArgs &a, cudaStream_t s)
+{
+    const uint64_t items = a.n * ((a.slabs + kForwardSlabs - 1u) / kForwardSlabs), per_cta = kRowThreads >> a.lanes_log2;
+    const uint64_t ctas = (items + per_cta - 1u) / per_cta;
+    embedding_kernel<W, A, VEC><<<(uint32_t)(ctas < (1u << 30) ? ctas : 1u << 30), kRowThreads, 0, s>>>(a);
+}
+template <typename W, typename A, bool VEC> static void backward(const EmbeddingArgs &a, cudaStream_t s)
+{
+    const uint64_t items = (uint64_t)a.n_chunks * a.slabs, per_cta = kRowThreads >> a.lanes_log2;
+    embedding_sum_kernel<A, W, VEC><<<(uint32_t)((items + per_cta - 1u) / per_cta), kRowThreads, 0, s>>>(a);
+    const uint64_t most = (uint64_t)a.n_chunks * ((a.pitch + 255u) / 256u);
+    embedding_join_kernel<W, VEC><<<(uint32_t)(most < 148u * 4u ? most : 148u * 4u), kRowThreads, 0, s>>>(a);
+}
+template <bool BACK, bool VEC> static void by_type(uint32_t table, uint32_t act, const EmbeddingArgs &a, cudaStream_t s)
+{
+#define DAF_EMBEDDING(W, A) (BACK ? backward<W, A, VEC>(a, s) : forward<W, A, VEC>(a, s))
+    if (table == DAF_F16) DAF_EMBEDDING(__half, __half);
+    else if (table == DAF_BF16) DAF_EMBEDDING(__nv_bfloat16, __nv_bfloat16);
+    else if (act == DAF_F16) DAF_EMBEDDING(float, __half);
+    else if (act == DAF_BF16) DAF_EMBEDDING(float, __nv_bfloat16);
+    else DAF_EMBEDDING(float, float);
+#undef DAF_EMBEDDING
+}
+
+}  // namespace daf
+
+using namespace daf;
+
+extern "C" daf_status daf_embedding(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out, daf_stream stream)
+{
+    const daf_status st = check_embedding(params);
+    if (st != DAF_OK) return st;
+    if (params->tokens == 0) return DAF_OK;
+    if (!on_elements(d_tokens, params->token_bytes) || !on_elements(d_weight, elem_bytes(params->table_dtype)) || !on_elements(d_out, elem_bytes(params->dtype)))
+        return DAF_ERR_INVALID_ARG;
+    EmbeddingArgs a = embedding_args(params);
+    a.tokens = d_tokens;
+    a.weight = d_weight;
+    a.out = d_out;
+    if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (wide(a, d_weight, params->table_dtype, d_out, params->dtype)) by_type<false, true>(params->table_dtype, params->dtype, a, s);
+    else by_type<false, false>(params->table_dtype, params->dtype, a, s);
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
+
+extern "C" uint64_t daf_embedding_grad_workspace(const daf_embedding_params *params)
+{
+    return check_embedding(params) == DAF_OK ? grad_workspace(embedding_args(params)) : 0;
+}
+
+extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_tokens, const void *d_grad_out, void *d_grad_weight,
+                                         void *d_workspace, uint64_t workspace_bytes, daf_stream stream)
+{
+    const daf_status st = check_embedding(params);
+    if (st != DAF_OK) return st;
+    const daf_embedding_params &p = *params;
+    if (!on_elements(d_grad_weight, elem_bytes(p.table_dtype)) || !on_elements(d_workspace, 32u) ||
+        (p.tokens && (!on_elements(d_tokens, p.token_bytes) || !on_elements(d_grad_out, elem_bytes(p.dtype)))))
+        return DAF_ERR_INVALID_ARG;
+    EmbeddingArgs a = embedding_args(params);
+    if (workspace_bytes < grad_workspace(a)) return DAF_ERR_CAPACITY;
+    a.tokens = d_tokens;
+    a.grad_out = d_grad_out;
+    a.grad_weight = d_grad_weight;
+    char *at = reinterpret_cast<char *>(d_workspace);
+    a.header = reinterpret_cast<WorkspaceHeader *>(at);
+    at += sizeof(WorkspaceHeader);
+    const uint64_t list = up256((uint64_t)a.n_chunks * a.chunk * sizeof(uint32_t));
+    for (int i = 0; i < 2; i++, at += 2u * list) {
+        a.keys[i] = reinterpret_cast<uint32_t *>(at);
+        a.places[i] = reinterpret_cast<uint32_t *>(at + list);
+    }
+    a.jobs = reinterpret_cast<uint32_t *>(at);
+    a.part = reinterpret_cast<float *>(at + up256((a.n_chunks + 1ull) * sizeof(uint32_t)));
+    if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
+    int ctas = 0;                                                   // also raises the kernel's limit of shared memory
+    if (persistent_ctas(reinterpret_cast<const void *>(&embedding_sort_kernel), (int)kSortThreads, (int)sizeof(SortShared), &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const uint32_t eb = elem_bytes(p.table_dtype);
+    const uint64_t bytes = a.table_elems * eb, clusters = (bytes + (1u << 19) - 1u) >> 19;    // 64 KiB to a CTA
+    embedding_sort_kernel<<<kSortCtas * (uint32_t)(1u + (clusters < 17u ? clusters : 17u)), kSortThreads, sizeof(SortShared), s>>>(a, eb);
+    if (a.n) {
+        if (wide(a, d_grad_out, p.dtype, d_grad_weight, p.table_dtype)) by_type<true, true>(p.table_dtype, p.dtype, a, s);
+        else by_type<true, false>(p.table_dtype, p.dtype, a, s);
+    }
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}

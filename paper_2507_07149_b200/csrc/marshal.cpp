@@ -7,6 +7,7 @@
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -401,6 +402,307 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// --------------------------------------------------------------------------------------------- embedding
+uint32_t type_code(const char *where, PyObject *o, const at::Tensor &like)
+{
+    if (o == Py_None) return code(where, like);
+    if (!THPDtype_Check(o)) refuse(where, "dtype is a torch dtype");
+    switch (reinterpret_cast<THPDtype *>(o)->scalar_type) {
+    case at::kFloat: return DAF_F32;
+    case at::kHalf: return DAF_F16;
+    case at::kBFloat16: return DAF_BF16;
+    default: refuse(where, "dtype is float32, float16 or bfloat16");
+    }
+}
+at::ScalarType type_of(uint32_t dtype) { return dtype == DAF_F32 ? at::kFloat : dtype == DAF_F16 ? at::kHalf : at::kBFloat16; }
+int64_t whole(PyObject *o)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Refusal("a whole number was expected");
+    return v;
+}
+at::Tensor dense_copy(const at::Tensor &t) { return t.is_contiguous() ? t : t.contiguous(); }
+
+struct Embedding {
+    daf_embedding_params p{};
+    at::Tensor tokens;
+    Embedding(const char *where, PyObject *t, PyObject *scale)
+    {
+        tokens = tensor(where, t);
+        device(where, tokens);
+        if (tokens.scalar_type() != at::kInt && tokens.scalar_type() != at::kLong) refuse(where, "tokens are int32 or int64");
+        tokens = dense_copy(tokens);
+        p.struct_size = sizeof(p);
+        p.token_bytes = (uint32_t)tokens.element_size();
+        p.tokens = (uint64_t)tokens.numel();
+        p.scale = (float)number(scale);
+        p.padding = -1;
+    }
+    void width(const char *where, int64_t n)
+    {
+        if (n > 0x7FFFFFFF) refuse(where, "rows are too wide");
+        p.width = (uint32_t)n;
+    }
+};
+
+// (tokens, weight, scale, dtype, out) -> (out, status)
+PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 5, [&]() {
+        const char *const where = "embedding";
+        Embedding e(where, a[0], a[2]);
+        at::Tensor weight = tensor(where, a[1]);
+        same_device(where, e.tokens.get_device(), weight);
+        if (weight.dim() != 2) refuse(where, "weight is [vocabulary, width]");
+        weight = dense_copy(weight);
+        at::Tensor out = maybe(where, a[4]);
+        e.p.table_dtype = code(where, weight);
+        e.p.dtype = out.defined() && a[3] == Py_None ? code(where, out) : type_code(where, a[3], weight);
+        if (e.p.table_dtype != e.p.dtype && e.p.table_dtype != DAF_F32) refuse(where, "the output has the weight's type, or any where the weight is float32");
+        e.p.vocabulary = (uint64_t)weight.size(0);
+        e.width(where, weight.size(1));
+        const c10::cuda::CUDAGuard on(weight.device());
+        std::vector<int64_t> shape = e.tokens.sizes().vec();
+        shape.push_back(weight.size(1));
+        if (!out.defined()) {
+            out = at::empty(shape, weight.options().dtype(type_of(e.p.dtype)));
+        } else {
+            same_device(where, weight.get_device(), out);
+            if (out.scalar_type() != type_of(e.p.dtype) || out.sizes() != at::IntArrayRef(shape) || !out.is_contiguous())
+                refuse(where, "out is a contiguous tensor of the tokens' shape and the width, of the type that was asked for");
+            modified(out);
+        }
+        return answer({out}, daf_embedding(&e.p, ptr(e.tokens), ptr(weight), ptr(out), c10::cuda::getCurrentCUDAStream().stream()));
+    });
+}
+
+// (tokens, grad_out, vocabulary, scale, padding, dtype, out, check) -> (grad_weight, status)
+PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 8, [&]() {
+        const char *const where = "embedding_grad";
+        Embedding e(where, a[0], a[3]);
+        at::Tensor grad = tensor(where, a[1]);
+        same_device(where, e.tokens.get_device(), grad);
+        if (grad.dim() != e.tokens.dim() + 1 || grad.sizes().slice(0, (size_t)e.tokens.dim()) != e.tokens.sizes()) refuse(where, "grad_out has the tokens' shape and the width");
+        grad = dense_copy(grad);
+        at::Tensor out = maybe(where, a[6]);
+        e.p.dtype = code(where, grad);
+        e.p.table_dtype = out.defined() && a[5] == Py_None ? code(where, out) : type_code(where, a[5], grad);
+        if (e.p.table_dtype != e.p.dtype && e.p.table_dtype != DAF_F32) refuse(where, "the gradient has grad_out's type, or is float32");
+        const int64_t vocabulary = whole(a[2]);
+        if (vocabulary <= 0) refuse(where, "vocabulary is positive");
+        e.p.vocabulary = (uint64_t)vocabulary;
+        e.width(where, grad.size(-1));
+        if (a[4] != Py_None) {
+            e.p.padding = whole(a[4]);
+            if (e.p.padding < 0 || e.p.padding >= vocabulary) refuse(where, "padding is a token, or None");
+        }
+        const c10::cuda::CUDAGuard on(grad.device());
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+        const int64_t shape[2] = {vocabulary, grad.size(-1)};
+        if (!out.defined()) {
+            out = at::empty(shape, grad.options().dtype(type_of(e.p.table_dtype)));
+        } else {
+            same_device(where, grad.get_device(), out);
+            if (out.scalar_type() != type_of(e.p.table_dtype) || out.sizes() != at::IntArrayRef(shape) || !out.is_contiguous())
+                refuse(where, "out is a contiguous tensor [vocabulary, width] of the type that was asked for");
+            modified(out);
+        }
+        const uint64_t size = daf_embedding_grad_workspace(&e.p);
+        const at::Tensor ws = bytes(size, grad);
+        daf_status st = daf_embedding_grad(&e.p, ptr(e.tokens), ptr(grad), ptr(out), ptr(ws), size, stream);
+        if (st == DAF_OK && truth(a[7])) st = daf_poll_status(ptr(ws), stream);
+        return answer({out}, st);
+    });
+}
+
+// --------------------------------------------------------------------------------------------- norms and rotation of queries and keys
+struct Rotary {
+    daf_rotary_params p{};
+    at::Tensor q, k, weight[2], positions;
+    std::vector<double> frequencies;
+    // a: q, k, q_weight, k_weight, positions, rotary_dim, base, style, eps, frequencies
+    Rotary(const char *where, PyObject *const *a)
+    {
+        q = tensor(where, a[0]);
+        k = maybe(where, a[1]);
+        const int index = device(where, q);
+        if (q.dim() != 4 || (k.defined() && k.dim() != 4)) refuse(where, "expects q [B, S, H, D] and k [B, S, Hkv, D]");
+        if (k.defined() && (k.size(0) != q.size(0) || k.size(1) != q.size(1) || k.size(3) != q.size(3)))
+            refuse(where, "q " + shape_of(q) + " and k " + shape_of(k) + " do not belong together");
+        if (k.defined() && k.scalar_type() != q.scalar_type()) refuse(where, "q and k have one type");
+        same_device(where, index, k);
+        for (int64_t n : q.sizes())
+            if (n > 0x7FFFFFFF) refuse(where, "a dimension is too large");
+        p.struct_size = sizeof(p);
+        p.dtype = p.param_dtype = code(where, q);
+        p.batch = (uint32_t)q.size(0);
+        p.tokens = (uint32_t)q.size(1);
+        p.heads = (uint32_t)q.size(2);
+        p.kv_heads = k.defined() ? (uint32_t)k.size(2) : 0u;
+        p.head_dim = (uint32_t)q.size(3);
+        bool typed = false;
+        for (int i = 0; i < 2; i++) {
+            weight[i] = maybe(where, a[2 + i]);
+            if (!weight[i].defined()) continue;
+            same_device(where, index, weight[i]);
+            if (weight[i].dim() != 1 || weight[i].size(0) != q.size(3) || !weight[i].is_contiguous()) refuse(where, "weights are contiguous vectors of a head's size");
+            const uint32_t t = code(where, weight[i]);
+            if ((t != p.dtype && t != DAF_F32) || (typed && t != p.param_dtype)) refuse(where, "weights have the type of q and k, or float32, both the same");
+            p.param_dtype = t;
+            typed = true;
+            onto_boundary(weight[i], 16);
+        }
+        if (a[4] != Py_None && THPVariable_Check(a[4])) {
+            positions = tensor(where, a[4]);
+            same_device(where, index, positions);
+            if (positions.scalar_type() != at::kInt && positions.scalar_type() != at::kLong) refuse(where, "positions are int32 or int64");
+            const bool shared = positions.dim() == 1 && positions.size(0) == q.size(1);
+            if (!shared && (positions.dim() != 2 || positions.size(0) != q.size(0) || positions.size(1) != q.size(1)))
+                refuse(where, "positions are [B, S], or [S] for all sequences");
+            positions = dense_copy(positions);
+            p.shared_positions = shared ? 1u : 0u;
+            p.position_bytes = (uint32_t)positions.element_size();
+        } else if (a[4] != Py_None) {
+            p.first_position = whole(a[4]);
+        }
+        const int64_t rotary = a[5] == Py_None ? q.size(3) : whole(a[5]);
+        if (rotary < 0 || rotary > q.size(3)) refuse(where, "rotary_dim is between 0 and a head's size");
+        p.rotary_dim = (uint32_t)rotary;
+        p.base = number(a[6]);
+        p.style = (uint32_t)whole(a[7]);
+        p.eps = (float)number(a[8]);
+        if (a[9] != Py_None) {
+            if (!PyList_Check(a[9]) || PyList_GET_SIZE(a[9]) != rotary / 2) refuse(where, "frequencies is a list of rotary_dim / 2 numbers");
+            for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[9]); i++) frequencies.push_back(number(PyList_GET_ITEM(a[9], i)));
+        }
+        q = readable(q);
+        strides(p.q_stride, q);
+        if (k.defined()) {
+            k = readable(k);
+            strides(p.k_stride, k);
+        }
+    }
+    const double *turns() const { return frequencies.empty() ? nullptr : frequencies.data(); }
+};
+at::Tensor as_given(const char *where, const char *name, PyObject *o, const at::Tensor &model)
+{
+    at::Tensor t = maybe(where, o);
+    if (!model.defined()) {
+        if (t.defined()) refuse(where, std::string(name) + " without keys");
+        return t;
+    }
+    if (!t.defined()) return dense(model.sizes(), model);
+    like(where, name, t, model);
+    writable(where, name, t);
+    modified(t);
+    return t;
+}
+
+// (q, k, q_weight, k_weight, positions, rotary_dim, base, style, eps, frequencies, q_out, k_out) -> (q, k, status)
+PyObject *rotary_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 12, [&]() {
+        const char *const where = "rotary_norm";
+        Rotary r(where, a);
+        const c10::cuda::CUDAGuard on(r.q.device());
+        const at::Tensor qo = as_given(where, "q_out", a[10], r.q), ko = as_given(where, "k_out", a[11], r.k);
+        strides(r.p.q_out_stride, qo);
+        if (ko.defined()) strides(r.p.k_out_stride, ko);
+        return answer({qo, ko}, daf_rotary_norm(&r.p, r.turns(), ptr(r.q), ptr(r.k), ptr(r.weight[0]), ptr(r.weight[1]), ptr(r.positions), ptr(qo), ptr(ko),
+                                                c10::cuda::getCurrentCUDAStream().stream()));
+    });
+}
+
+// (q, k, q_weight, k_weight, positions, rotary_dim, base, style, eps, frequencies, grad_q_out, grad_k_out, grad_q, grad_k)
+//     -> (grad_q, grad_k, grad_q_weight, grad_k_weight, status)
+PyObject *rotary_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 14, [&]() {
+        const char *const where = "rotary_norm_grad";
+        Rotary r(where, a);
+        const c10::cuda::CUDAGuard on(r.q.device());
+        at::Tensor go[2] = {tensor(where, a[10]), maybe(where, a[11])};
+        like(where, "grad_q_out", go[0], r.q);
+        if (r.k.defined() != go[1].defined()) refuse(where, "keys come with the gradient of their output");
+        if (go[1].defined()) like(where, "grad_k_out", go[1], r.k);
+        for (at::Tensor &g : go)
+            if (g.defined()) g = readable(g);
+        const at::Tensor gq = as_given(where, "grad_q", a[12], r.q), gk = as_given(where, "grad_k", a[13], r.k);
+        strides(r.p.q_out_stride, go[0]);
+        strides(r.p.grad_q_stride, gq);
+        if (gk.defined()) {
+            strides(r.p.k_out_stride, go[1]);
+            strides(r.p.grad_k_stride, gk);
+        }
+        at::Tensor gw[2];
+        for (int i = 0; i < 2; i++)
+            if (r.weight[i].defined()) gw[i] = i == 0 || r.k.defined() ? dense(r.weight[i].sizes(), r.weight[i]) : at::zeros_like(r.weight[i]);
+        const uint64_t size = daf_rotary_norm_grad_workspace(&r.p);
+        const at::Tensor ws = bytes(size, r.q);
+        const daf_status st = daf_rotary_norm_grad(&r.p, r.turns(), ptr(r.q), ptr(r.k), ptr(r.weight[0]), ptr(r.weight[1]), ptr(r.positions), ptr(go[0]), ptr(go[1]),
+                                                   ptr(gq), ptr(gk), ptr(gw[0]), ptr(gw[1]), ptr(ws), size, c10::cuda::getCurrentCUDAStream().stream());
+        return answer({gq, gk, gw[0], gw[1]}, st);
+    });
+}
+
+// --------------------------------------------------------------------------------------------- orthogonalised updates
+// (updates: list, out: list or None, steps, (a, b, c), eps, check) -> (list, status)
+PyObject *orthogonalize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 6, [&]() {
+        const char *const where = "orthogonalize";
+        if (!PyList_Check(a[0]) || (a[1] != Py_None && !PyList_Check(a[1]))) refuse(where, "expects lists of tensors");
+        const size_t count = (size_t)PyList_GET_SIZE(a[0]);
+        if (count == 0) refuse(where, "expects at least one matrix");
+        if (a[1] != Py_None && (size_t)PyList_GET_SIZE(a[1]) != count) refuse(where, "out holds one tensor for each matrix");
+        daf_orthogonalize_params p{};
+        p.struct_size = sizeof(p);
+        const int64_t steps = whole(a[2]);
+        if (steps < 1 || steps > 64) refuse(where, "steps is between 1 and 64");
+        p.steps = (uint32_t)steps;
+        if (!PyTuple_Check(a[3]) || PyTuple_GET_SIZE(a[3]) != 3) refuse(where, "coefficients are three numbers");
+        for (int i = 0; i < 3; i++) p.coefficients[i] = (float)number(PyTuple_GET_ITEM(a[3], i));
+        p.eps = (float)number(a[4]);
+        std::vector<uint32_t> types(count);
+        std::vector<uint64_t> rows(count), cols(count);
+        std::vector<const void *> src(count);
+        std::vector<void *> dst(count);
+        std::vector<at::Tensor> in(count), out(count);
+        const at::Tensor &first = tensor(where, PyList_GET_ITEM(a[0], 0));
+        const int index = device(where, first);
+        const c10::cuda::CUDAGuard on(first.device());
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+        for (size_t i = 0; i < count; i++) {
+            in[i] = tensor(where, PyList_GET_ITEM(a[0], (Py_ssize_t)i));
+            same_device(where, index, in[i]);
+            if (in[i].dim() < 2) refuse(where, "expects matrices (dimensions behind the first are one)");
+            types[i] = code(where, in[i]);
+            rows[i] = (uint64_t)in[i].size(0);
+            cols[i] = rows[i] ? (uint64_t)(in[i].numel() / in[i].size(0)) : 0u;
+            if (a[1] == Py_None) {
+                out[i] = dense(in[i].sizes(), in[i]);
+            } else {
+                out[i] = tensor(where, PyList_GET_ITEM(a[1], (Py_ssize_t)i));
+                like(where, "an output", out[i], in[i]);
+                if (!out[i].is_contiguous()) refuse(where, "outputs are contiguous");
+                modified(out[i]);
+            }
+            in[i] = dense_copy(in[i]);
+            src[i] = ptr(in[i]);
+            dst[i] = ptr(out[i]);
+        }
+        const uint64_t size = daf_orthogonalize_workspace(&p, (uint32_t)count, types.data(), rows.data(), cols.data());
+        const at::Tensor ws = bytes(size, first);
+        daf_status st = daf_orthogonalize(&p, (uint32_t)count, types.data(), src.data(), dst.data(), rows.data(), cols.data(), ptr(ws), size, stream);
+        if (st == DAF_OK && truth(a[5])) st = daf_poll_status(ptr(ws), stream);
+        PyObject *const list = PyList_New((Py_ssize_t)count);
+        for (size_t i = 0; i < count; i++) PyList_SET_ITEM(list, (Py_ssize_t)i, wrap(out[i]));
+        return Py_BuildValue("(Ni)", list, (int)st);
+    });
+}
+
 // (tensor) -> whether it fills its memory without gaps or overlaps, in any order
 PyObject *gap_free(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -409,7 +711,8 @@ PyObject *gap_free(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 #define DAF_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DAF_METHOD(attention), DAF_METHOD(attention_grad), DAF_METHOD(residual_norm), DAF_METHOD(residual_norm_grad),
-                         DAF_METHOD(clip_grad_norm), DAF_METHOD(gap_free), {nullptr, nullptr, 0, nullptr}};
+                         DAF_METHOD(clip_grad_norm), DAF_METHOD(embedding), DAF_METHOD(embedding_grad), DAF_METHOD(rotary_norm),
+                         DAF_METHOD(rotary_norm_grad), DAF_METHOD(orthogonalize), DAF_METHOD(gap_free), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,758 @@
+// Orthogonalised updates: x = g / (|g| + eps), then `steps` times x = a x + (b G + c G^2) x with G = x x^T (x^T x and products
+// from the right for matrices with more rows than columns: neither is ever transposed in memory).
+//
+// Per step three products of each matrix, m its shorter and n its longer side:
+//   gram    G = x x^T            m m n multiply-adds, half of them by symmetry
+//   poly    P = b G + c G G      m m m, half of them by symmetry
+//   update  x' = a x + P x       2 m m n
+// Bound: the tensor cores.  What is held between the products is float16, not bfloat16: 11 bits instead of 8 at the same rate,
+// and the values' range is known (singular values below two), so powers of two keep them away from both ends of the type:
+// x is held K = |g| 2^s times its size, K in [2^12, 2^13), so that the first x is g itself times a power of two, exact for bfloat16;
+// G and P are held 2^12 times their size.  Relative error of the result in binary64 arithmetic with only these roundings
+// (768 x 2304, spectra from flat to strongly decaying): 1.3e-3 to 5.0e-3 with x rounded at the start, 0.9e-3 to 3.4e-3 so, and at most 1.4e-3 with
+// the linear term a x of the steps behind the first two taken from two float16 parts (the small singular values live there: what
+// rounds the large ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  float16 and
+// binary32 matrices are held in two parts throughout (three products instead of one): 2e-6.
+//
+// One persistent kernel runs all products of all steps and matrices.  CTAs take tiles of 128 x N by a ticket, in an order
+// in which whatever a tile needs comes before it; a tile waits until its matrix's tiles of the earlier products are done
+// (a counter), so a CTA that waits only ever waits for tiles that running CTAs hold, and the matrices of a call fill one
+// another's gaps.  Roles: one warp takes tickets, waits and copies operands (TMA), one issues products (two accumulators in
+// tensor memory), eight read results, form the polynomial or the update and store them.
+#include "attention.cuh"
+#include "tensor_core.cuh"
+
+namespace daf {
+
+constexpr uint32_t kOrthThreads = 384, kOrthStages = 4, kOrthBox = 8192, kOrthStage = 6u * kOrthBox, kOrthOut = 2048;
+constexpr uint32_t kOrthGroups = 24, kOrthMatrices = 192, kOrthSlots = 4;
+constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
+constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch: bounds the workspace (8 bytes and more per element)
+constexpr float kHeld = 4096.0f;                // G and P times this
+constexpr uint32_t kPrepUnits = 64;             // pieces of 256 columns of a row to a CTA of the preparing kernels
+
+struct OrthGroup {                              // matrices of one shape and type
+    CUtensorMap x[2], gram, poly;
+    __half *x_at[2], *gram_at, *poly_at;        // [matrix][plane][row][pitch]; x always has two planes
+    uint64_t x_plane, m_plane;                  // elements of a plane
+    uint32_t r, c, m, x_pitch, m_pitch, tall, planes, count, first, dtype;
+    uint32_t sym_tiles, sym_cols, upd_tiles, upd_rows;   // of one matrix
+    uint32_t sym_first, upd_first, prep_ctas, prep_first;
+};
+struct OrthArgs {
+    OrthGroup g[kOrthGroups];
+    const void *in[kOrthMatrices];
+    void *out[kOrthMatrices];
+    uint32_t groups, matrices, steps, sym_total, upd_total, sym_n, upd_n, prep_total, keep_status;
+    float a, b, c, eps;
+    double *partial;
+    float *scale;                               // K of each matrix
+    uint32_t *done;                             // finished eighths of tiles of each matrix
+    WorkspaceHeader *header;
+    unsigned int *device_status;
+};
+static_assert(sizeof(OrthArgs) <= 32000, "kernel arguments");
+
+// --------------------------------------------------------------------------------------------- norms, first operands
+__device__ __forceinline__ float orth_get(const void *p, uint32_t dtype, uint64_t i)
+{
+    if (dtype == DAF_F32) return __ldg(reinterpret_cast<const float *>(p) + i);
+    if (dtype == DAF_F16) return __half2float(reinterpret_cast<const __half *>(p)[i]);
+    return __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p)[i]);
+}
+// Eight columns of a row, zero behind its end.
+__device__ __forceinline__ void orth_load8(const OrthGroup &g, const void *p, uint32_t row, uint32_t col, float (&x)[8])
+{
+    const uint32_t eb = g.dtype == DAF_F32 ? 4u : 2u;
+    const uint64_t at = (uint64_t)row * g.c + col;
+    if (g.c % 8u == 0 && reinterpret_cast<uintptr_t>(p) % (8u * eb) == 0) {
+        if (g.dtype == DAF_F32) Elem<float>::load8(reinterpret_cast<const float *>(p) + at, x);
+        else if (g.dtype == DAF_F16) Elem<__half>::load8(reinterpret_cast<const __half *>(p) + at, x);
+        else Elem<__nv_bfloat16>::load8(reinterpret_cast<const __nv_bfloat16 *>(p) + at, x);
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; e++) x[e] = col + e < g.c ? orth_get(p, g.dtype, at + e) : 0.0f;
+}
+// The CTA's matrix and its share of it.
+struct PrepShare {
+    uint32_t group, matrix, cta, cols;          // cta: within the matrix; cols: pieces of 256 columns of a row
+    uint64_t units;
+};
+__device__ __forceinline__ PrepShare prep_share(const OrthArgs &a)
+{
+    PrepShare s = {};
+    while (s.group + 1u < a.groups && blockIdx.x >= a.g[s.group + 1u].prep_first) s.group++;
+    const OrthGroup &g = a.g[s.group];
+    const uint32_t at = blockIdx.x - g.prep_first;
+    s.matrix = at / g.prep_ctas;
+    s.cta = at - s.matrix * g.prep_ctas;
+    s.cols = (g.c + 255u) / 256u;
+    s.units = (uint64_t)g.r * s.cols;
+    return s;
+}
+__device__ __forceinline__ double cta_sum(double v, double *s_part)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if ((threadIdx.x & 31u) == 0) s_part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int w = 0; w < 8; w++) v += s_part[w];
+    return v;
+}
+
+__global__ void __launch_bounds__(256) orth_norm_kernel(const __grid_constant__ OrthArgs a)
+{
+    __shared__ double s_part[8];
+    if (blockIdx.x == 0) {
+        for (uint32_t i = threadIdx.x; i < a.matrices; i += 256u) a.done[i] = 0;
+        if (threadIdx.x == 0) {
+            a.header->ticket = 0;
+            if (!a.keep_status) a.header->status = DAF_OK;
+        }
+    }
+    const PrepShare s = prep_share(a);
+    const OrthGroup &g = a.g[s.group];
+    const void *in = a.in[g.first + s.matrix];
+    const uint32_t lane = threadIdx.x & 31u;
+    double sum = 0.0;
+    for (uint32_t j = threadIdx.x >> 5; j < kPrepUnits; j += 8u) {
+        const uint64_t unit = (uint64_t)s.cta * kPrepUnits + j;
+        const uint32_t row = (uint32_t)(unit / s.cols), col = (uint32_t)(unit - (uint64_t)row * s.cols) * 256u + lane * 8u;
+        if (unit >= s.units || col >= g.c) continue;
+        float x[8];
+        orth_load8(g, in, row, col, x);
+#pragma unroll
+        for (int e = 0; e < 8; e++) sum = fma((double)x[e], (double)x[e], sum);
+    }
+    sum = cta_sum(sum, s_part);
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = sum;
+}
+
+__global__ void __launch_bounds__(256) orth_start_kernel(const __grid_constant__ OrthArgs a)
+{
+    __shared__ double s_part[8];
+    const PrepShare s = prep_share(a);
+    const OrthGroup &g = a.g[s.group];
+    const uint32_t lane = threadIdx.x & 31u;
+    const double *parts = a.partial + g.prep_first + s.matrix * g.prep_ctas;
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < g.prep_ctas; i += 256u) sum += parts[i];
+    const double norm = sqrt(cta_sum(sum, s_part)) + (double)a.eps;
+    const bool finite = norm - norm == 0.0;
+    const int up = finite ? 12 - ilogb(norm) : 0;
+    if (s.cta == 0 && threadIdx.x == 0) a.scale[g.first + s.matrix] = finite ? (float)scalbn(norm, up) : __int_as_float(0x7FC00000);
+    const void *in = a.in[g.first + s.matrix];
+    __half *hi = g.x_at[0] + (uint64_t)s.matrix * 2u * g.x_plane, *lo = hi + g.x_plane;
+    for (uint32_t j = threadIdx.x >> 5; j < kPrepUnits; j += 8u) {
+        const uint64_t unit = (uint64_t)s.cta * kPrepUnits + j;
+        const uint32_t row = (uint32_t)(unit / s.cols), col = (uint32_t)(unit - (uint64_t)row * s.cols) * 256u + lane * 8u;
+        if (unit >= s.units || col >= g.c) continue;
+        float x[8], rest[8];
+        orth_load8(g, in, row, col, x);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            x[e] = finite ? scalbnf(x[e], up) : __int_as_float(0x7FC00000);
+            rest[e] = x[e] - __half2float(__float2half_rn(x[e]));
+        }
+        Elem<__half>::store8(hi + (uint64_t)row * g.x_pitch + col, x);
+        if (g.planes == 2u) Elem<__half>::store8(lo + (uint64_t)row * g.x_pitch + col, rest);
+    }
+}
+
+// --------------------------------------------------------------------------------------------- the products
+enum : uint32_t { kGram = 0, kPoly = 1, kUpdate = 2, kNoTile = 3 };
+struct OrthTile {
+    uint32_t kind, step, group, matrix, row, col;
+};
+
+__device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket)
+{
+    OrthTile t = {};
+    const uint32_t per_step = 2u * a.sym_total + a.upd_total;
+    t.step = ticket / per_step;
+    if (t.step >= a.steps) {
+        t.kind = kNoTile;
+        return t;
+    }
+    uint32_t i = ticket - t.step * per_step;
+    if (i >= 2u * a.sym_total) {
+        t.kind = kUpdate;
+        i -= 2u * a.sym_total;
+        while (t.group + 1u < a.groups && i >= a.g[t.group + 1u].upd_first) t.group++;
+        const OrthGroup &g = a.g[t.group];
+        i -= g.upd_first;
+        t.matrix = i / g.upd_tiles;
+        i -= t.matrix * g.upd_tiles;
+        const uint32_t col = i / g.upd_rows;
+        t.row = (i - col * g.upd_rows) * 128u;
+        t.col = col * a.upd_n;
+        return t;
+    }
+    if (i >= a.sym_total) {
+        t.kind = kPoly;
+        i -= a.sym_total;
+    }
+    while (t.group + 1u < a.groups && i >= a.g[t.group + 1u].sym_first) t.group++;
+    const OrthGroup &g = a.g[t.group];
+    i -= g.sym_first;
+    t.matrix = i / g.sym_tiles;
+    i -= t.matrix * g.sym_tiles;
+    // rows of tiles from the top; of each, the tiles that reach the diagonal or lie right of it
+    for (uint32_t first = 0;;) {
+        const uint32_t left = g.sym_cols - first;
+        if (i < left) {
+            t.col = (first + i) * a.sym_n;
+            return t;
+        }
+        i -= left;
+        t.row += 128u;
+        first = t.row / a.sym_n;
+    }
+}
+
+// Waits, with a limit, until `need` tiles of the matrix are done.
+__device__ __forceinline__ bool wait_tiles(const uint32_t *done, uint32_t need, volatile uint32_t *stop)
+{
+    uint64_t start = 0;
+    for (;;) {
+        uint32_t n;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(done) : "memory");
+        if (n >= need) return true;
+        if (*stop) return false;
+        const uint64_t now = now_ns();
+        if (!start) start = now;
+        if (now - start > kWaitNanoseconds) {
+            *stop = 1u;
+            return false;
+        }
+    }
+}
+
+// A 32 x 32 block of a float16 matrix between global memory (a quarter row of 64 bytes to four lanes) and one row to a lane,
+// through 2 KiB of shared memory.
+struct OrthBlock {
+    uint4 v[4];
+    __device__ __forceinline__ void load(const __half *at, uint32_t pitch, uint32_t row, uint32_t rows, uint32_t col, uint32_t lane)
+    {
+#pragma unroll
+        for (uint32_t q = 0; q < 4u; q++) {
+            const uint32_t r = row + (lane >> 2) + 8u * q, c = col + (lane & 3u) * 8u;
+            v[q] = make_uint4(0, 0, 0, 0);
+            if (r < rows && c < pitch) v[q] = __ldcg(reinterpret_cast<const uint4 *>(at + (uint64_t)r * pitch + c));
+        }
+    }
+    // afterwards the lane's own row
+    __device__ __forceinline__ void to_rows(unsigned char *stage, uint32_t lane)
+    {
+        __syncwarp();
+#pragma unroll
+        for (uint32_t q = 0; q < 4u; q++) stage_piece(stage, (lane >> 2) + 8u * q, lane & 3u, v[q]);
+        __syncwarp();
+#pragma unroll
+        for (uint32_t p = 0; p < 4u; p++) v[p] = *reinterpret_cast<const uint4 *>(stage + lane * 64u + ((p ^ (lane >> 1 & 3u)) * 16u));
+    }
+    __device__ __forceinline__ void add(float (&x)[32], float by) const
+    {
+#pragma unroll
+        for (uint32_t p = 0; p < 4u; p++) {
+            const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; i++) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+                x[8u * p + 2u * i] = __fmaf_rn(by, f.x, x[8u * p + 2u * i]);
+                x[8u * p + 2u * i + 1u] = __fmaf_rn(by, f.y, x[8u * p + 2u * i + 1u]);
+            }
+        }
+    }
+    // back: from rows to the quarters
+    __device__ __forceinline__ void to_quarters(unsigned char *stage, uint32_t lane)
+    {
+        __syncwarp();
+#pragma unroll
+        for (uint32_t p = 0; p < 4u; p++) stage_piece(stage, lane, p, v[p]);
+        __syncwarp();
+#pragma unroll
+        for (uint32_t q = 0; q < 4u; q++) {
+            const uint32_t r = (lane >> 2) + 8u * q;
+            v[q] = *reinterpret_cast<const uint4 *>(stage + r * 64u + (((lane & 3u) ^ (r >> 1 & 3u)) * 16u));
+        }
+    }
+    __device__ __forceinline__ void store(void *at, uint64_t pitch, uint32_t row, uint32_t rows, uint32_t col, uint32_t cols, uint32_t lane) const
+    {
+#pragma unroll
+        for (uint32_t q = 0; q < 4u; q++) {
+            const uint32_t r = row + (lane >> 2) + 8u * q, c = col + (lane & 3u) * 8u;
+            if (r < rows && c < cols) *reinterpret_cast<uint4 *>(reinterpret_cast<__half *>(at) + (uint64_t)r * pitch + c) = v[q];
+        }
+    }
+};
+template <typename T> __device__ __forceinline__ void round32(const float (&x)[32], uint4 (&v)[4])
+{
+#pragma unroll
+    for (uint32_t p = 0; p < 4u; p++)
+        v[p] = make_uint4(round2<T>(x[8u * p], x[8u * p + 1u]), round2<T>(x[8u * p + 2u], x[8u * p + 3u]), round2<T>(x[8u * p + 4u], x[8u * p + 5u]),
+                          round2<T>(x[8u * p + 6u], x[8u * p + 7u]));
+}
+// What the rounding to float16 (the row in v) has left of x.
+__device__ __forceinline__ void take_away(float (&x)[32], const uint4 (&v)[4])
+{
+#pragma unroll
+    for (uint32_t p = 0; p < 4u; p++) {
+        const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; i++) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            x[8u * p + 2u * i] -= f.x;
+            x[8u * p + 2u * i + 1u] -= f.y;
+        }
+    }
+}
+// The block's transpose: column c of it, the lanes' rows side by side, to row `col + c`.
+__device__ __forceinline__ void store_transposed(__half *at, uint32_t pitch, uint32_t row, uint32_t col, uint32_t m, uint32_t lane, const uint4 (&v)[4])
+{
+    if (row + lane >= m) return;
+#pragma unroll
+    for (uint32_t p = 0; p < 4u; p++) {
+        const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; i++)
+            if (col + 8u * p + i < m)
+                reinterpret_cast<uint16_t *>(at)[(uint64_t)(col + 8u * p + i) * pitch + row + lane] = (uint16_t)(w[i >> 1] >> (16u * (i & 1u)));
+    }
+}
+
+__global__ void __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
+{
+    extern __shared__ __align__(1024) unsigned char s_raw[];
+    struct Bars {
+        uint64_t full[kOrthStages], empty[kOrthStages], told[kOrthSlots], heard[kOrthSlots], acc_full[2], acc_empty[2], drain;
+        OrthTile tile[kOrthSlots];
+        uint32_t tmem, abort, late;
+    };
+    static_assert(sizeof(Bars) <= kOrthBars, "barriers fit their place");
+    Bars &bars = *reinterpret_cast<Bars *>(s_raw);
+    if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
+        if (threadIdx.x == 0) record_error(a.header, a.device_status, DAF_ERR_UNSUPPORTED);
+        return;
+    }
+    unsigned char *const stages = s_raw + kOrthBars;
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+    if (threadIdx.x == 0) {
+        bars.abort = bars.late = 0u;
+        for (uint32_t i = 0; i < kOrthStages; i++) {
+            bar_init(&bars.full[i], 1);
+            bar_init(&bars.empty[i], 1);
+        }
+        for (uint32_t i = 0; i < kOrthSlots; i++) {
+            bar_init(&bars.told[i], 1);
+            bar_init(&bars.heard[i], 9);
+        }
+        bar_init(&bars.drain, 1);
+        for (uint32_t i = 0; i < 2u; i++) {
+            bar_init(&bars.acc_full[i], 1);
+            bar_init(&bars.acc_empty[i], 8);
+        }
+        fence_async();
+    }
+    if (warp == 2) tmem_alloc(&bars.tmem, 512);
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = bars.tmem;
+    volatile uint32_t *const stop = &bars.abort;
+
+    if (warp == 0) {                                               // ---- tickets and copies
+        if (lane == 0) {
+            uint32_t ticket = atomicAdd(&a.header->ticket, 1u), st = 0, ph = 0, issued = 0;
+            for (uint32_t n = 0;; n++) {
+                const uint32_t slot = n % kOrthSlots;
+                if (n >= kOrthSlots && !bar_wait(&bars.heard[slot], (n / kOrthSlots - 1u) & 1u, stop)) break;
+                const OrthTile t = orth_tile(a, ticket);
+                bars.tile[slot] = t;
+                bar_arrive(&bars.told[slot]);
+                if (t.kind == kNoTile) break;
+                ticket = atomicAdd(&a.header->ticket, 1u);
+                const OrthGroup &g = a.g[t.group];
+                const uint32_t need = 8u * (t.step * (2u * g.sym_tiles + g.upd_tiles) + t.kind * g.sym_tiles);
+                if (need && !wait_tiles(a.done + g.first + t.matrix, need, stop)) break;
+                asm volatile("fence.proxy.async;" ::: "memory");    // what other CTAs wrote by stores is now read by copies
+                const CUtensorMap *ma, *mb;
+                uint32_t keys, plane_a, plane_b, boxes;             // the summed dimension; planes of a matrix in each map
+                bool cross_a = false, cross_b = false;              // the summed dimension is not the contiguous one
+                if (t.kind == kPoly) {
+                    ma = mb = &g.gram;
+                    keys = g.m;
+                    plane_a = plane_b = g.planes;
+                    boxes = a.sym_n / 64u;
+                } else if (t.kind == kGram) {
+                    ma = mb = &g.x[t.step & 1u];
+                    keys = g.tall ? g.r : g.c;
+                    plane_a = plane_b = 2u;
+                    cross_a = cross_b = g.tall;
+                    boxes = a.sym_n / 64u;
+                } else {
+                    ma = g.tall ? &g.x[t.step & 1u] : &g.poly;
+                    mb = g.tall ? &g.poly : &g.x[t.step & 1u];
+                    keys = g.m;
+                    plane_a = g.tall ? 2u : g.planes;
+                    plane_b = g.tall ? g.planes : 2u;
+                    cross_b = !g.tall;
+                    boxes = a.upd_n / 64u;
+                }
+                bool ok = true;
+                for (uint32_t part = g.planes == 2u ? 0u : 2u; part < 3u && ok; part++) {      // small parts first
+                    const int ba = (int)(t.matrix * plane_a + (part == 1u)), bb = (int)(t.matrix * plane_b + (part == 0u));
+                    for (uint32_t k = 0; k < keys; k += 64u) {
+                        if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) break;
+                        const uint32_t to = smem_u32(stages + st * kOrthStage);
+                        bar_expect(&bars.full[st], (2u + boxes) * kOrthBox);
+                        for (uint32_t i = 0; i < 2u; i++)
+                            tma_load(to + i * kOrthBox, ma, &bars.full[st], cross_a ? (int)(t.row + 64u * i) : (int)k, ba, cross_a ? (int)k : (int)(t.row + 64u * i), 0);
+                        for (uint32_t i = 0; i < boxes; i++)
+                            tma_load(to + (2u + i) * kOrthBox, mb, &bars.full[st], cross_b ? (int)(t.col + 64u * i) : (int)k, bb, cross_b ? (int)k : (int)(t.col + 64u * i), 0);
+                        issued++;
+                        if (++st == kOrthStages) st = 0, ph ^= 1u;
+                    }
+                }
+                if (!ok) break;
+            }
+            // nothing may be on its way into shared memory when the CTA ends (normally all has long arrived)
+            for (uint32_t i = 0; i < kOrthStages && i < issued; i++) {
+                const uint32_t last = issued - 1u - i;
+                bar_wait(&bars.full[last % kOrthStages], last / kOrthStages & 1u, &bars.late);
+            }
+        }
+    } else if (warp == 1) {                                        // ---- products
+        const uint32_t one = elect_lane();
+        uint32_t st = 0, ph = 0;
+        for (uint32_t n = 0;; n++) {
+            const uint32_t slot = n % kOrthSlots, buf = n & 1u;
+            if (!bar_wait(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
+            const OrthTile t = bars.tile[slot];
+            __syncwarp();
+            if (lane == 0) bar_arrive(&bars.heard[slot]);
+            if (t.kind == kNoTile) break;
+            if (n >= 2u && !bar_wait(&bars.acc_empty[buf], (n / 2u - 1u) & 1u, stop)) break;
+            tmem_after_sync();
+            const OrthGroup &g = a.g[t.group];
+            const bool cross_a = t.kind == kGram && g.tall, cross_b = cross_a || (t.kind == kUpdate && !g.tall);
+            const uint32_t keys = t.kind == kGram && g.tall ? g.r : t.kind == kGram ? g.c : g.m;
+            const uint32_t desc = product_desc(false, t.kind == kUpdate ? a.upd_n : a.sym_n, cross_b) | (cross_a ? 1u << 15 : 0u);
+            const uint32_t step_a = cross_a ? 128u : 2u, step_b = cross_b ? 128u : 2u;         // 16 of the summed dimension, in 16-byte units
+            const uint32_t rounds = (keys + 63u) / 64u * (g.planes == 2u ? 3u : 1u), d = tmem + buf * 256u;
+            bool ok = true;
+            for (uint32_t k = 0; k < rounds; k++) {
+                if (!(ok = bar_wait(&bars.full[st], ph, stop))) break;
+                tmem_after_sync();
+                const uint32_t at = smem_u32(stages + st * kOrthStage);
+                const uint32_t la = operand_low(at, kOrthBox), lb = operand_low(at + 2u * kOrthBox, kOrthBox);
+                product_ss(one, d, la, lb, desc, k > 0);
+#pragma unroll
+                for (uint32_t s = 1; s < 4u; s++) product_ss<true>(one, d, la + s * step_a, lb + s * step_b, desc);
+                products_done(one, &bars.empty[st]);
+                if (++st == kOrthStages) st = 0, ph ^= 1u;
+            }
+            products_done(one, &bars.acc_full[buf]);
+            if (!ok) break;
+        }
+        products_done(one, &bars.drain);
+        bar_wait(&bars.drain, 0, &bars.late);
+    } else if (warp >= 4) {                                        // ---- results
+        const uint32_t quarter = warp & 3u, half = (warp - 4u) >> 2;
+        unsigned char *const stage = stages + kOrthStages * kOrthStage + (warp - 4u) * kOrthOut;
+        for (uint32_t n = 0;; n++) {
+            const uint32_t slot = n % kOrthSlots, buf = n & 1u;
+            if (!bar_wait(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
+            const OrthTile t = bars.tile[slot];
+            __syncwarp();
+            if (lane == 0) bar_arrive(&bars.heard[slot]);
+            if (t.kind == kNoTile) break;
+            if (!bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
+            tmem_after_sync();
+            const OrthGroup &g = a.g[t.group];
+            const bool update = t.kind == kUpdate, last = t.step + 1u == a.steps;
+            const uint32_t width = update ? a.upd_n : a.sym_n, row = t.row + quarter * 32u;
+            const uint32_t rows = update ? g.r : g.m, pitch = update ? g.x_pitch : g.m_pitch, matrix = g.first + t.matrix;
+            const float k = __ldcg(a.scale + matrix);
+            // what is added to the product, and factors of both
+            const __half *with = update ? g.x_at[t.step & 1u] + (uint64_t)t.matrix * 2u * g.x_plane : g.gram_at + (uint64_t)t.matrix * g.planes * g.m_plane;
+            const uint64_t plane = update ? g.x_plane : g.m_plane;
+            const bool two = g.planes == 2u || (update && (t.step == 1u || t.step == 2u));
+            const float of_product = t.kind == kGram ? __fdiv_rn(kHeld, k * k) : t.kind == kPoly ? a.c / kHeld : 1.0f / kHeld;
+            const float of_with = update ? a.a : a.b;
+            __half *to = update ? g.x_at[(t.step + 1u) & 1u] + (uint64_t)t.matrix * 2u * g.x_plane
+                                : (t.kind == kGram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * g.planes * g.m_plane;
+            for (uint32_t j = half * (width / 64u); j < (half + 1u) * (width / 64u); j++) {
+                const uint32_t col = t.col + j * 32u;
+                if (row >= rows || col >= pitch) break;
+                float x[32];
+                OrthBlock w;
+                if (t.kind != kGram) w.load(with, pitch, row, rows, col, lane);
+                __syncwarp();
+                tmem_load32(tmem + buf * 256u + j * 32u + (quarter << 21), x);
+                tmem_wait_loads();
+#pragma unroll
+                for (int i = 0; i < 32; i++) x[i] *= of_product;
+                if (t.kind != kGram) {
+                    w.to_rows(stage, lane);
+                    w.add(x, of_with);
+                    if (two) {
+                        w.load(with + plane, pitch, row, rows, col, lane);
+                        w.to_rows(stage, lane);
+                        w.add(x, of_with);
+                    }
+                }
+                if (update && last) {
+                    const float by = __fdiv_rn(1.0f, k);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) x[i] *= by;
+                    char *const out = reinterpret_cast<char *>(a.out[matrix]);
+                    const uint32_t eb = g.dtype == DAF_F32 ? 4u : 2u;
+                    const bool wide = g.c * eb % 16u == 0 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+                    if (g.dtype == DAF_F32) {
+                        const uint32_t ends = row + lane < rows ? g.c : 0u;             // lanes without a row store nothing
+                        float *const at = reinterpret_cast<float *>(out) + (uint64_t)(row + lane) * g.c + col;
+#pragma unroll
+                        for (uint32_t i = 0; i < 32u; i += 4u) {
+                            if (wide && col + i < ends) {
+                                *reinterpret_cast<float4 *>(at + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                            } else {
+#pragma unroll
+                                for (uint32_t e = 0; e < 4u; e++)
+                                    if (col + i + e < ends) at[i + e] = x[i + e];
+                            }
+                        }
+                        continue;
+                    }
+                    if (g.dtype == DAF_F16) round32<__half>(x, w.v);
+                    else round32<__nv_bfloat16>(x, w.v);
+                    w.to_quarters(stage, lane);
+                    if (wide) w.store(out, g.c, row, rows, col, g.c, lane);
+                    else if (col + lane < g.c)
+                        for (uint32_t r = 0; r < 32u && row + r < rows; r++)
+                            reinterpret_cast<uint16_t *>(out)[(uint64_t)(row + r) * g.c + col + lane] =
+                                *reinterpret_cast<const uint16_t *>(stage + r * 64u + (((lane >> 3) ^ (r >> 1 & 3u)) * 16u) + (lane & 7u) * 2u);
+                    continue;
+                }
+                // the other half of a symmetric matrix: where no tile of its own covers it
+                const bool mirror = !update && (row / a.sym_n + 1u) * a.sym_n <= col / 128u * 128u;
+                const uint32_t planes = g.planes == 2u || (update && t.step < 2u) ? 2u : 1u;
+                for (uint32_t p = 0; p < planes; p++) {
+                    round32<__half>(x, w.v);
+                    if (p + 1u < planes) take_away(x, w.v);
+                    if (mirror) store_transposed(to + p * plane, pitch, row, col, rows, lane, w.v);
+                    w.to_quarters(stage, lane);
+                    w.store(to + p * plane, pitch, row, rows, col, pitch, lane);
+                }
+            }
+            tmem_before_sync();
+            __syncwarp();
+            if (lane == 0) bar_arrive(&bars.acc_empty[buf]);
+            if (update && last) continue;                          // nothing waits for the result
+            asm volatile("fence.proxy.async;" ::: "memory");
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) {                                       // each warp for itself: no meeting that one could miss
+                __threadfence();
+                atomicAdd(a.done + matrix, 1u);
+            }
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && (bars.abort || bars.late)) record_error(a.header, a.device_status, DAF_ERR_TIMEOUT);
+    if (warp == 2) tmem_free(tmem, 512);
+}
+
+// --------------------------------------------------------------------------------------------- host
+static uint64_t up_to(uint64_t n, uint64_t by) { return (n + by - 1u) / by * by; }
+
+static daf_status check_orth(const daf_orthogonalize_params *p, uint32_t n, const uint32_t *dtypes, const uint64_t *rows, const uint64_t *cols)
+{
+    if (!p || p->struct_size != sizeof(*p) || p->reserved[0] || p->reserved[1] || p->steps == 0 || !(p->eps > 0.0f) || !(p->eps - p->eps == 0.0f) ||
+        (n && (!dtypes || !rows || !cols)))
+        return DAF_ERR_INVALID_ARG;
+    for (const float c : p->coefficients)
+        if (!(c - c == 0.0f)) return DAF_ERR_INVALID_ARG;
+    if (p->steps > 64u) return DAF_ERR_UNSUPPORTED;
+    for (uint32_t i = 0; i < n; i++) {
+        if (dtypes[i] > DAF_BF16) return DAF_ERR_INVALID_ARG;
+        if (rows[i] > 65536u || cols[i] > 65536u) return DAF_ERR_UNSUPPORTED;
+    }
+    return DAF_OK;
+}
+
+// Tiles of 128 rows times N columns: N is 256 where that leaves every SM a tile, else as small as it takes (64 at least).
+static uint32_t orth_sym_tiles(uint32_t m, uint32_t width)
+{
+    const uint32_t cols = (m + width - 1u) / width;
+    uint32_t tiles = 0;
+    for (uint32_t row = 0; row < m; row += 128u) tiles += cols - row / width;
+    return tiles;
+}
+
+// The next matrices that go together, from *next on: the table without pointers to the workspace, and the bytes it needs.
+static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t n, const uint32_t *dtypes, const uint64_t *rows, const uint64_t *cols,
+                       uint32_t *next, uint32_t *index, uint64_t *workspace)
+{
+    uint32_t group_of[kOrthMatrices], taken[kOrthMatrices];
+    uint64_t elems = 0;
+    a->groups = a->matrices = 0;
+    for (; *next < n && a->matrices < kOrthMatrices; ++*next) {
+        const uint32_t i = *next, r = (uint32_t)rows[i], c = (uint32_t)cols[i];
+        if (r == 0 || c == 0) continue;
+        if (elems && elems + (uint64_t)r * c > kOrthBatch) break;
+        uint32_t k = 0;
+        while (k < a->groups && (a->g[k].r != r || a->g[k].c != c || a->g[k].dtype != dtypes[i])) k++;
+        if (k == kOrthGroups) break;
+        OrthGroup &g = a->g[k];
+        if (k == a->groups) {
+            a->groups++;
+            g.r = r;
+            g.c = c;
+            g.dtype = dtypes[i];
+            g.count = 0;
+        }
+        g.count++;
+        group_of[a->matrices] = k;
+        taken[a->matrices++] = i;
+        elems += (uint64_t)r * c;
+    }
+    uint32_t first[kOrthGroups], at = 0;
+    for (uint32_t k = 0; k < a->groups; k++) {
+        a->g[k].first = first[k] = at;
+        at += a->g[k].count;
+    }
+    for (uint32_t i = 0; i < a->matrices; i++) index[first[group_of[i]]++] = taken[i];
+    a->steps = p->steps;
+    a->a = p->coefficients[0];
+    a->b = p->coefficients[1];
+    a->c = p->coefficients[2];
+    a->eps = p->eps;
+    a->prep_total = 0;
+    for (a->sym_n = 256u;; a->sym_n /= 2u) {
+        a->sym_total = 0;
+        for (uint32_t k = 0; k < a->groups; k++) a->sym_total += a->g[k].count * orth_sym_tiles(a->g[k].r < a->g[k].c ? a->g[k].r : a->g[k].c, a->sym_n);
+        if (a->sym_total >= 148u || a->sym_n == 64u) break;
+    }
+    for (a->upd_n = 256u;; a->upd_n /= 2u) {
+        a->upd_total = 0;
+        for (uint32_t k = 0; k < a->groups; k++) a->upd_total += a->g[k].count * ((a->g[k].r + 127u) / 128u) * ((a->g[k].c + a->upd_n - 1u) / a->upd_n);
+        if (a->upd_total >= 148u || a->upd_n == 64u) break;
+    }
+    uint32_t sym = 0, upd = 0;
+    uint64_t bytes = sizeof(WorkspaceHeader) + up_to(2ull * kOrthMatrices * sizeof(uint32_t), 256u);
+    for (uint32_t k = 0; k < a->groups; k++) {
+        OrthGroup &g = a->g[k];
+        g.tall = g.r > g.c;
+        g.m = g.tall ? g.c : g.r;
+        g.planes = g.dtype == DAF_BF16 ? 1u : 2u;
+        g.x_pitch = (uint32_t)up_to(g.c, 64u);
+        g.m_pitch = (uint32_t)up_to(g.m, 64u);
+        g.x_plane = (uint64_t)g.r * g.x_pitch;
+        g.m_plane = (uint64_t)g.m * g.m_pitch;
+        g.sym_cols = (g.m + a->sym_n - 1u) / a->sym_n;
+        g.sym_tiles = orth_sym_tiles(g.m, a->sym_n);
+        g.upd_rows = (g.r + 127u) / 128u;
+        g.upd_tiles = g.upd_rows * ((g.c + a->upd_n - 1u) / a->upd_n);
+        g.sym_first = sym;
+        g.upd_first = upd;
+        sym += g.count * g.sym_tiles;
+        upd += g.count * g.upd_tiles;
+        g.prep_ctas = (uint32_t)(((uint64_t)g.r * ((g.c + 255u) / 256u) + kPrepUnits - 1u) / kPrepUnits);
+        g.prep_first = a->prep_total;
+        a->prep_total += g.count * g.prep_ctas;
+        bytes += g.count * 2u * (up_to(2u * g.x_plane * sizeof(__half), 256u) + up_to(g.planes * g.m_plane * sizeof(__half), 256u));
+    }
+    *workspace = bytes + up_to(a->prep_total * sizeof(double), 256u);
+}
+
+// Where a batch's buffers lie, and their maps.
+static bool orth_place(OrthArgs *a, char *at)
+{
+    a->header = reinterpret_cast<WorkspaceHeader *>(at);
+    at += sizeof(WorkspaceHeader);
+    a->done = reinterpret_cast<uint32_t *>(at);
+    a->scale = reinterpret_cast<float *>(a->done + kOrthMatrices);
+    at += up_to(2ull * kOrthMatrices * sizeof(uint32_t), 256u);
+    a->partial = reinterpret_cast<double *>(at);
+    at += up_to(a->prep_total * sizeof(double), 256u);
+    for (uint32_t k = 0; k < a->groups; k++) {
+        OrthGroup &g = a->g[k];
+        const auto take = [&](__half **p, CUtensorMap *map, uint64_t plane, uint32_t planes, uint32_t rows, uint32_t cols, uint32_t pitch) {
+            *p = reinterpret_cast<__half *>(at);
+            at += up_to(g.count * planes * plane * sizeof(__half), 256u);
+            const AttnTensor t = {*p, 0, pitch, plane};
+            return attn_tensor_map(map, false, t, 1, rows, g.count * planes, cols, 64);
+        };
+        for (int i = 0; i < 2; i++)
+            if (!take(&g.x_at[i], &g.x[i], g.x_plane, 2u, g.r, g.c, g.x_pitch)) return false;
+        if (!take(&g.gram_at, &g.gram, g.m_plane, g.planes, g.m, g.m, g.m_pitch) || !take(&g.poly_at, &g.poly, g.m_plane, g.planes, g.m, g.m, g.m_pitch))
+            return false;
+    }
+    return true;
+}
+
+}  // namespace daf
+
+using namespace daf;
+
+extern "C" uint64_t daf_orthogonalize_workspace(const daf_orthogonalize_params *params, uint32_t n, const uint32_t *dtypes, const uint64_t *rows,
+                                                const uint64_t *cols)
+{
+    if (check_orth(params, n, dtypes, rows, cols) != DAF_OK) return 0;
+    uint64_t most = sizeof(WorkspaceHeader);
+    uint32_t index[kOrthMatrices];
+    OrthArgs a;
+    for (uint32_t next = 0; next < n;) {
+        uint64_t bytes = 0;
+        orth_batch(&a, params, n, dtypes, rows, cols, &next, index, &bytes);
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
+
+extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, uint32_t n, const uint32_t *dtypes, const void *const *d_in,
+                                        void *const *d_out, const uint64_t *rows, const uint64_t *cols, void *d_workspace, uint64_t workspace_bytes,
+                                        daf_stream stream)
+{
+    const daf_status st = check_orth(params, n, dtypes, rows, cols);
+    if (st != DAF_OK) return st;
+    if ((n && (!d_in || !d_out)) || !d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u)) return DAF_ERR_INVALID_ARG;
+    for (uint32_t i = 0; i < n; i++) {
+        const uintptr_t mask = dtypes[i] == DAF_F32 ? 3u : 1u;
+        if (rows[i] && cols[i] && (!d_in[i] || !d_out[i] || ((reinterpret_cast<uintptr_t>(d_in[i]) | reinterpret_cast<uintptr_t>(d_out[i])) & mask)))
+            return DAF_ERR_INVALID_ARG;
+    }
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    uint32_t index[kOrthMatrices];
+    OrthArgs a;
+    int ctas = 0;
+    if (persistent_ctas(reinterpret_cast<const void *>(&orthogonalize_kernel), (int)kOrthThreads, (int)kOrthSmem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    bool any = false;
+    for (uint32_t next = 0; next < n;) {
+        uint64_t bytes = 0;
+        orth_batch(&a, params, n, dtypes, rows, cols, &next, index, &bytes);
+        if (a.matrices == 0) break;
+        if (workspace_bytes < bytes) return DAF_ERR_CAPACITY;
+        if (!orth_place(&a, reinterpret_cast<char *>(d_workspace)) || !(a.device_status = device_status_word())) return DAF_ERR_CUDA;
+        for (uint32_t i = 0; i < a.matrices; i++) {
+            a.in[i] = d_in[index[i]];
+            a.out[i] = d_out[index[i]];
+        }
+        a.keep_status = any;
+        any = true;
+        orth_norm_kernel<<<a.prep_total, 256, 0, s>>>(a);
+        orth_start_kernel<<<a.prep_total, 256, 0, s>>>(a);
+        const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total;
+        orthogonalize_kernel<<<most < (uint32_t)ctas ? most : (uint32_t)ctas, kOrthThreads, kOrthSmem, s>>>(a);
+    }
+    if (!any) {
+        if (workspace_bytes < sizeof(WorkspaceHeader)) return DAF_ERR_CAPACITY;
+        if (cudaMemsetAsync(d_workspace, 0, sizeof(uint32_t), s) != cudaSuccess) return DAF_ERR_CUDA;
+    }
+    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
