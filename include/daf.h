@@ -491,7 +491,7 @@ daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_
  *   t = position * frequency[i] for pair i; the elements behind rotary_dim stay as they are.
  * Pair i is (i, i + rotary_dim / 2) for DAF_ROTARY_HALVES, (2 i, 2 i + 1) for DAF_ROTARY_PAIRS.  frequencies: HOST array of
  * rotary_dim / 2 finite numbers (radians per position), or NULL for base^(-2 i / rotary_dim).  Angles are exact products modulo a
- * turn, for positions of any size and sign.  d_positions: signed integers of position_bytes, [batch, tokens], or [tokens] with
+ * turn, for positions of any size and sign.  A row with an element that is NaN or infinite may come out as NaN throughout.  d_positions: signed integers of position_bytes, [batch, tokens], or [tokens] with
  * shared_positions; position_bytes == 0: token s of every sequence is at first_position + s.  Arithmetic in binary32, one rounding.
  *   d_q, d_q_out, d_grad_q_out, d_grad_q : [batch, tokens, heads, head_dim];  d_k, ... : the same with kv_heads (0: no keys, NULL)
  * of dtype, by the strides below ({batch, token, head}, in elements; a row contiguous): pointers 16-byte aligned, strides of

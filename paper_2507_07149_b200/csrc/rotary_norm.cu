@@ -5,20 +5,25 @@
 // Backward, for the gradient g of the output and xhat = x / sqrt(mean(x^2) + eps): g' = g turned back, weight gradient
 // sum g' xhat over all rows, dx = (g' w - xhat mean(g' w xhat)) / sqrt(mean(x^2) + eps).
 //
-// Bound: HBM (each element read once, or x and g, and written once).  A row is held by a group of lanes, 2 V elements each:
-// both halves of its V pairs, so nothing but the sums crosses lanes.  A group takes several heads of ONE token, because the
-// angles are the token's: with cosines and sines of a lane's V pairs computed anew for each row the arithmetic would
-// bound the kernel.  Angles: a pair's frequency is held as turns per position, a 64-bit fraction of a turn; position * frequency modulo
+// Bound: HBM (each element read once, or x and g, and written once) as far as the instructions per row allow, which is why all of
+// it is done on pairs of binary32.  A row is held by a group of lanes, 2 V elements each: both sides of its V pairs, so nothing but the
+// sums crosses lanes.  A group takes several heads of ONE token, because the angles are the token's: cosines and sines of a lane's V pairs
+// cost as much as a row.  Angles: a pair's frequency is held as turns per position, a 64-bit fraction of a turn; position * frequency modulo
 // 2^64 is then exact in integers, however far the position, and the top 32 bits give the angle within 2^-31 half turns.
 //
 // The weights' gradients are summed in registers over the rows of a group, over the groups of a CTA in shared memory and over
 // the CTAs by a second launch, all in a fixed order.
 #include "attention.cuh"
+#include "pairs.cuh"
 
 namespace daf {
 
-constexpr uint32_t kRotaryThreads = 256, kRotaryMaxDim = 256, kRotaryRows = 4;  // rows of a group in flight
-constexpr uint32_t kRotaryCtas = 148u * 4u;     // backward: CTAs at most, and so rows of partial sums
+constexpr uint32_t kRotaryThreads = 256, kRotaryMaxDim = 256;
+// Shared memory of a thread for rows on their way and in work, and CTAs of an SM.  Measured with 4 x 8192 tokens, 16 and 4 heads of
+// 128 (forward) and 64 x 197 tokens, 12 and 12 of 64 (backward), bfloat16: 128 bytes and three CTAs 73.5, 256 and two 61.6 us;
+// rows held in registers instead of shared memory 72 to 76; backward 256 and two 34.0, 512 and one 42.7, three CTAs (80 registers) 38.4.
+constexpr uint32_t kRotaryBytes = 256, kRotaryCtasPerSm = 2;
+constexpr uint32_t kRotaryCtas = 148u * kRotaryCtasPerSm;       // backward: CTAs at most, and so rows of partial sums
 
 struct RotaryArgs {
     AttnTensor x[2], y[2], g[2];                // queries and keys: inputs; outputs, or gradients of the inputs; gradients of the outputs
@@ -29,31 +34,10 @@ struct RotaryArgs {
     long long first;
     FastDiv tokens, runs[2];                    // tokens of a sequence; runs of heads of a token
     uint32_t heads[2], run[2], items[2];        // heads of a run
-    uint32_t dim, rotary, lanes_log2, pairs_apart, position_bytes, shared_positions;
+    uint32_t dim, rotary, lanes_log2, position_bytes, shared_positions;
     float eps, inv_dim;
 };
 
-template <typename T, int V> struct Piece;      // V elements in one or two accesses
-template <> struct Piece<float, 4> {
-    static __device__ __forceinline__ void load(const float *p, float (&x)[4])
-    {
-        const float4 v = *reinterpret_cast<const float4 *>(p);
-        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-    }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]); }
-};
-template <> struct Piece<float, 8> {            // rows start on 16 bytes, not on 32
-    static __device__ __forceinline__ void load(const float *p, float (&x)[8])
-    {
-        const float4 u = *reinterpret_cast<const float4 *>(p), v = *reinterpret_cast<const float4 *>(p + 4);
-        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-    }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[8])
-    {
-        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-    }
-};
 template <typename T> __device__ __forceinline__ float2 widen2(uint32_t v);
 template <> __device__ __forceinline__ float2 widen2<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 template <> __device__ __forceinline__ float2 widen2<__nv_bfloat16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
@@ -68,28 +52,70 @@ template <> __device__ __forceinline__ uint32_t narrow2<__nv_bfloat16>(float a, 
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-template <typename T> struct Piece<T, 4> {
-    static __device__ __forceinline__ void load(const T *p, float (&x)[4])
+template <> __device__ __forceinline__ uint32_t narrow2<float>(float, float) { return 0u; }    // for code that a binary32 call does not reach
+
+// V elements of a row as they lie in memory (rows start on 16 bytes).  They come through shared memory: a thread copies its own
+// pieces of the rows ahead into places of its own, so nobody but the thread has to wait for them, and rows on their way take no registers.
+template <typename T, int V> struct Piece {
+    static constexpr int kWords = V * (int)sizeof(T) / 4, kAccess = kWords == 2 ? 8 : 16, kAccesses = kWords * 4 / kAccess;
+    uint32_t w[kWords];
+    // place: of access 0; the next one of the thread lies kRotaryThreads accesses behind
+    static __device__ __forceinline__ void fetch(uint32_t place, const T *p)
     {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        const float2 a = widen2<T>(v.x), b = widen2<T>(v.y);
-        x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+#pragma unroll
+        for (int i = 0; i < kAccesses; i++) {
+            const char *const from = reinterpret_cast<const char *>(p) + i * kAccess;
+            const uint32_t to = place + i * kRotaryThreads * kAccess;
+            if constexpr (kAccess == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+        }
     }
-    static __device__ __forceinline__ void store(T *p, const float (&x)[4])
+    __device__ __forceinline__ void take(uint32_t place)
     {
-        *reinterpret_cast<uint2 *>(p) = make_uint2(narrow2<T>(x[0], x[1]), narrow2<T>(x[2], x[3]));
+        if constexpr (kAccess == 8) {
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(place) : "memory");
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAccesses; i++)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "r"(place + i * kRotaryThreads * kAccess) : "memory");
+        }
     }
-};
-template <typename T> struct Piece<T, 8> {
-    static __device__ __forceinline__ void load(const T *p, float (&x)[8])
+    __device__ __forceinline__ void load(const T *p)
     {
-        const uint4 v = *reinterpret_cast<const uint4 *>(p);
-        const float2 a = widen2<T>(v.x), b = widen2<T>(v.y), c = widen2<T>(v.z), d = widen2<T>(v.w);
-        x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
+        if constexpr (kAccess == 8) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
+            w[0] = v.x; w[1] = v.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i / 4);
+                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+            }
+        }
     }
-    static __device__ __forceinline__ void store(T *p, const float (&x)[8])
+    __device__ __forceinline__ float2 two(int i) const             // elements 2 i and 2 i + 1
     {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(narrow2<T>(x[0], x[1]), narrow2<T>(x[2], x[3]), narrow2<T>(x[4], x[5]), narrow2<T>(x[6], x[7]));
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        else return widen2<T>(w[i]);
+    }
+    __device__ __forceinline__ void put_two(int i, float a, float b)
+    {
+        if constexpr (sizeof(T) == 4) {
+            w[2 * i] = __float_as_uint(a);
+            w[2 * i + 1] = __float_as_uint(b);
+        } else {
+            w[i] = narrow2<T>(a, b);
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const
+    {
+        if constexpr (kWords == 2) {
+            *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) *(reinterpret_cast<uint4 *>(p) + i / 4) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        }
     }
 };
 
@@ -107,10 +133,12 @@ template <typename T> __device__ __forceinline__ void turn_of(uint32_t top, floa
     }
 }
 
-__device__ __forceinline__ float group_sum(float v, uint32_t lanes)
+// Sums over the lanes of a group, of several values side by side.
+template <int N> __device__ __forceinline__ void group_sum(float (&v)[N], uint32_t lanes)
 {
-    for (uint32_t d = lanes >> 1; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
+    for (uint32_t d = lanes >> 1; d; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; i++) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
 }
 
 // What a lane holds of every row: two pieces of V elements, whether they turn, and as what.
@@ -118,21 +146,61 @@ struct LaneShare {
     uint32_t at0, at1, pair;                    // elements; the first pair's index
     bool here, turns;
 };
-template <int V> __device__ __forceinline__ LaneShare lane_share(const RotaryArgs &a, uint32_t lane)
+template <int V, bool HALVES> __device__ __forceinline__ LaneShare lane_share(const RotaryArgs &a, uint32_t lane)
 {
     LaneShare l;
-    const uint32_t turning = a.rotary / (2u * V);
     l.here = lane < a.dim / (2u * V);
-    l.turns = lane < turning;
+    l.turns = lane < a.rotary / (2u * V);
     l.pair = lane * V;
-    const bool apart = l.turns && a.pairs_apart;
+    const bool apart = HALVES && l.turns;
     l.at0 = apart ? lane * V : lane * 2u * V;
     l.at1 = apart ? a.rotary / 2u + lane * V : l.at0 + V;
     return l;
 }
 
+// A lane's elements of a row, as the two sides of its V pairs, two values to a register pair: all arithmetic below takes two elements an
+// instruction.  HALVES: the sides are the two pieces; else they alternate in memory.  In elements that do not turn the sides
+// mean nothing.
+template <int V> struct Sides {
+    uint64_t p[V / 2], q[V / 2];
+};
+template <typename T, int V, bool HALVES> __device__ __forceinline__ Sides<V> sides_of(const Piece<T, V> &u, const Piece<T, V> &v)
+{
+    Sides<V> x;
+#pragma unroll
+    for (int i = 0; i < V / 2; i++) {
+        const float2 a = HALVES ? u.two(i) : i < V / 4 ? u.two(2 * i) : v.two(2 * i - V / 2);
+        const float2 b = HALVES ? v.two(i) : i < V / 4 ? u.two(2 * i + 1) : v.two(2 * i + 1 - V / 2);
+        x.p[i] = HALVES ? pair(a.x, a.y) : pair(a.x, b.x);
+        x.q[i] = HALVES ? pair(b.x, b.y) : pair(a.y, b.y);
+    }
+    return x;
+}
+template <typename T, int V, bool HALVES> __device__ __forceinline__ void pieces_of(const Sides<V> &x, Piece<T, V> &u, Piece<T, V> &v)
+{
+#pragma unroll
+    for (int i = 0; i < V / 2; i++) {
+        if (HALVES) {
+            u.put_two(i, low(x.p[i]), high(x.p[i]));
+            v.put_two(i, low(x.q[i]), high(x.q[i]));
+        } else if (i < V / 4) {
+            u.put_two(2 * i, low(x.p[i]), low(x.q[i]));
+            u.put_two(2 * i + 1, high(x.p[i]), high(x.q[i]));
+        } else {
+            v.put_two(2 * i - V / 2, low(x.p[i]), low(x.q[i]));
+            v.put_two(2 * i + 1 - V / 2, high(x.p[i]), high(x.q[i]));
+        }
+    }
+}
+// The element of the row that value j (0 .. V-1: side p, then q) of the lane is.
+template <int V, bool HALVES> __device__ __forceinline__ uint32_t element_of(const LaneShare &l, uint32_t j)
+{
+    if (HALVES) return j < V ? l.at0 + j : l.at1 + j - V;
+    return l.at0 + (j < V ? 2u * j : 2u * (j - V) + 1u);
+}
+
 template <typename T, int V> struct TokenTurns {
-    float c[V], s[V];
+    uint64_t c[V / 2], s[V / 2];
     __device__ __forceinline__ void of(const RotaryArgs &a, const LaneShare &l, uint32_t token, uint32_t in_sequence)
     {
         if (!l.turns) return;
@@ -141,178 +209,306 @@ template <typename T, int V> struct TokenTurns {
         if (a.position_bytes == 4u) p = __ldg(reinterpret_cast<const int *>(a.positions) + at);
         if (a.position_bytes == 8u) p = __ldg(reinterpret_cast<const long long *>(a.positions) + at);
 #pragma unroll
-        for (int i = 0; i < V; i++) turn_of<T>((uint32_t)(((uint64_t)p * a.turns[l.pair + i]) >> 32), &c[i], &s[i]);
-    }
-    // forward (by +angle) or back (by -angle)
-    template <bool BACK> __device__ __forceinline__ void apply(const RotaryArgs &a, const LaneShare &l, float (&x0)[V], float (&x1)[V]) const
-    {
-        if (!l.turns) return;
-        if (a.pairs_apart) {
-#pragma unroll
-            for (int i = 0; i < V; i++) turn<BACK>(x0[i], x1[i], c[i], s[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V / 2; i++) {
-                turn<BACK>(x0[2 * i], x0[2 * i + 1], c[i], s[i]);
-                turn<BACK>(x1[2 * i], x1[2 * i + 1], c[V / 2 + i], s[V / 2 + i]);
-            }
+        for (int i = 0; i < V / 2; i++) {
+            float c0, s0, c1, s1;
+            turn_of<T>((uint32_t)(((uint64_t)p * a.turns[l.pair + 2 * i]) >> 32), &c0, &s0);
+            turn_of<T>((uint32_t)(((uint64_t)p * a.turns[l.pair + 2 * i + 1]) >> 32), &c1, &s1);
+            c[i] = pair(c0, c1);
+            s[i] = pair(s0, s1);
         }
     }
-    template <bool BACK> static __device__ __forceinline__ void turn(float &p, float &q, float c, float s)
+    // back (by -angle)
+    __device__ __forceinline__ void back(const LaneShare &l, Sides<V> &x) const
     {
-        const float u = BACK ? __fmaf_rn(p, c, q * s) : __fmaf_rn(p, c, -(q * s));
-        q = BACK ? __fmaf_rn(q, c, -(p * s)) : __fmaf_rn(q, c, p * s);
-        p = u;
+        if (!l.turns) return;
+#pragma unroll
+        for (int i = 0; i < V / 2; i++) {
+            const uint64_t p = fma2(x.q[i], s[i], mul2(x.p[i], c[i]));
+            x.q[i] = fma2(x.q[i], c[i], mul2(x.p[i], s[i] ^ 0x8000000080000000ull));
+            x.p[i] = p;
+        }
     }
 };
 
-template <typename P, int V> __device__ __forceinline__ void load_weight(const void *w, const LaneShare &l, float (&w0)[V], float (&w1)[V])
+template <typename P, int V, bool HALVES> __device__ __forceinline__ Sides<V> load_weight(const void *w, const LaneShare &l)
 {
+    Sides<V> x;
     if (w && l.here) {
-        Piece<P, V>::load(reinterpret_cast<const P *>(w) + l.at0, w0);
-        Piece<P, V>::load(reinterpret_cast<const P *>(w) + l.at1, w1);
-        return;
+        Piece<P, V> u, v;
+        u.load(reinterpret_cast<const P *>(w) + l.at0);
+        v.load(reinterpret_cast<const P *>(w) + l.at1);
+        return sides_of<P, V, HALVES>(u, v);
     }
 #pragma unroll
-    for (int i = 0; i < V; i++) w0[i] = w1[i] = 1.0f;
+    for (int i = 0; i < V / 2; i++) x.p[i] = x.q[i] = both(1.0f);
+    return x;
 }
 
-template <typename T> __device__ __forceinline__ T *row_at(const AttnTensor &t, uint32_t b, uint32_t s, uint32_t h)
-{
-    return reinterpret_cast<T *>(t.p) + (uint64_t)b * t.sb + (uint64_t)s * t.ss + (uint64_t)h * t.sh;
-}
-
-template <typename T, typename P, int V> __global__ void __launch_bounds__(kRotaryThreads) rotary_norm_kernel(const __grid_constant__ RotaryArgs a)
-{
-    const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u), all = a.items[0] + a.items[1];
-    const uint32_t item = blockIdx.x * (kRotaryThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
-    const bool busy = item < all;
-    const LaneShare l = lane_share<V>(a, lane);
-    const bool here = l.here && busy;
-    const uint32_t which = busy && item >= a.items[0] ? 1u : 0u, mine = busy ? item - (which ? a.items[0] : 0u) : 0u;
-    const uint32_t token = a.runs[which].div(mine), h0 = (mine - token * a.runs[which].d) * a.run[which];
-    const uint32_t b = a.tokens.div(token), s = token - b * a.tokens.d;
-    const uint32_t h1 = h0 + a.run[which] < a.heads[which] ? h0 + a.run[which] : a.heads[which];
-    // a warp's groups take as many turns as the longest of them (their sums cross lanes together)
-    uint32_t most = a.run[0] > a.run[1] ? a.run[0] : a.run[1];
-    TokenTurns<T, V> turns;
-    float w0[V], w1[V];
-    load_weight<P, V>(a.weight[which], l, w0, w1);
-    bool first = true;
-    for (uint32_t k = 0; k < most; k += kRotaryRows) {
-        float x0[kRotaryRows][V], x1[kRotaryRows][V];
-#pragma unroll
-        for (uint32_t u = 0; u < kRotaryRows; u++) {
-            if (here && h0 + k + u < h1) {
-                const T *row = row_at<T>(a.x[which], b, s, h0 + k + u);
-                Piece<T, V>::load(row + l.at0, x0[u]);
-                Piece<T, V>::load(row + l.at1, x1[u]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; i++) x0[u][i] = x1[u][i] = 0.0f;
-            }
-        }
-        if (first && here) turns.of(a, l, token, s);
-        first = false;
-#pragma unroll
-        for (uint32_t u = 0; u < kRotaryRows; u++) {
-            float ss = 0.0f;
-#pragma unroll
-            for (int i = 0; i < V; i++) ss = __fmaf_rn(x0[u][i], x0[u][i], __fmaf_rn(x1[u][i], x1[u][i], ss));
-            const float r = rsqrtf(__fmaf_rn(group_sum(ss, lanes), a.inv_dim, a.eps));
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                x0[u][i] = x0[u][i] * r * w0[i];
-                x1[u][i] = x1[u][i] * r * w1[i];
-            }
-            if (here && h0 + k + u < h1) {
-                turns.template apply<false>(a, l, x0[u], x1[u]);
-                T *row = row_at<T>(a.y[which], b, s, h0 + k + u);
-                Piece<T, V>::store(row + l.at0, x0[u]);
-                Piece<T, V>::store(row + l.at1, x1[u]);
-            }
-        }
+// A group's way through its items of work, each some heads of one token, in units of UNIT of them.  All groups of a CTA
+// take the same number of units.
+template <int UNIT> struct Walk {
+    uint32_t item, at, rows, which, token, b, s, h;                 // at: rows ahead of the unit; rows: of the item
+    __device__ __forceinline__ void enter(const RotaryArgs &a, bool here)
+    {
+        const uint32_t all = a.items[0] + a.items[1];
+        at = 0;
+        rows = 0;
+        if (item >= all) return;
+        which = item >= a.items[0] ? 1u : 0u;
+        const uint32_t mine = which ? item - a.items[0] : item;
+        const uint32_t runs = which ? a.runs[1].d : a.runs[0].d, run = which ? a.run[1] : a.run[0], heads = which ? a.heads[1] : a.heads[0];
+        token = which ? a.runs[1].div(mine) : a.runs[0].div(mine);
+        h = (mine - token * runs) * run;
+        b = a.tokens.div(token);
+        s = token - b * a.tokens.d;
+        rows = !here ? 0u : heads - h < run ? heads - h : run;
     }
+    __device__ __forceinline__ void next(const RotaryArgs &a, uint32_t most, uint32_t stride, bool here)
+    {
+        at += UNIT;
+        if (at < most) return;
+        item += stride;
+        enter(a, here);
+    }
+    template <typename T> __device__ __forceinline__ T *first_row(const AttnTensor (&t)[2]) const
+    {
+        const AttnTensor &x = t[which];
+        return reinterpret_cast<T *>(x.p) + (uint64_t)b * x.sb + (uint64_t)s * x.ss + (uint64_t)(h + at) * x.sh;
+    }
+};
+__device__ __forceinline__ void fetch_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Units of a CTA: as many rounds over the grid as its first group needs.
+template <int UNIT> __device__ __forceinline__ uint32_t walk_units(const RotaryArgs &a, uint32_t groups, uint32_t most)
+{
+    const uint32_t all = a.items[0] + a.items[1], first = blockIdx.x * groups, stride = gridDim.x * groups;
+    return first < all ? ((all - first + stride - 1u) / stride) * ((most + UNIT - 1u) / UNIT) : 0u;
 }
 
-template <typename T, typename P, int V> __global__ void __launch_bounds__(kRotaryThreads) rotary_norm_grad_kernel(const __grid_constant__ RotaryArgs a)
+// Two units of a thread's rows lie in shared memory, one worked on, the next on its way.
+template <typename T, typename P, int V, bool HALVES> __global__ void __launch_bounds__(kRotaryThreads, kRotaryCtasPerSm) rotary_norm_kernel(const __grid_constant__ RotaryArgs a)
 {
-    __shared__ float s_sum[kRotaryThreads][2 * V + 1];
-    const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u), groups = kRotaryThreads >> a.lanes_log2;
-    const LaneShare l = lane_share<V>(a, lane);
-    constexpr uint32_t kRows = kRotaryRows / 2;
-    for (uint32_t which = 0; which < 2; which++) {
-        float w0[V], w1[V], sum0[V] = {}, sum1[V] = {};
-        load_weight<P, V>(a.weight[which], l, w0, w1);
-        // the whole CTA walks together: sums cross lanes, and a warp's groups must not part
-        for (uint32_t first = blockIdx.x * groups; first < a.items[which]; first += gridDim.x * groups) {
-            const uint32_t item = first + (threadIdx.x >> a.lanes_log2);
-            const bool here = l.here && item < a.items[which];
-            const uint32_t mine = here ? item : 0u, token = a.runs[which].div(mine), h0 = (mine - token * a.runs[which].d) * a.run[which];
-            const uint32_t b = a.tokens.div(token), s = token - b * a.tokens.d;
-            const uint32_t h1 = h0 + a.run[which] < a.heads[which] ? h0 + a.run[which] : a.heads[which];
+    using Part = Piece<T, V>;
+    constexpr int kUnit = (int)(kRotaryBytes / (2u * 2u * Part::kWords * 4u));
+    constexpr uint32_t kPlace = Part::kWords * 4 * kRotaryThreads, kRow = 2u * kPlace;
+    extern __shared__ __align__(16) unsigned char s_rows[];
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_rows) + threadIdx.x * Part::kAccess;
+    const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u), groups = kRotaryThreads >> a.lanes_log2, stride = gridDim.x * groups;
+    const uint32_t most = a.run[0] > a.run[1] ? a.run[0] : a.run[1], units = walk_units<kUnit>(a, groups, most);
+    const LaneShare l = lane_share<V, HALVES>(a, lane);
+    Walk<kUnit> now = {};
+    now.item = blockIdx.x * groups + (threadIdx.x >> a.lanes_log2);
+    now.enter(a, l.here);
+    Walk<kUnit> then = now;
+    const auto ahead = [&](uint32_t half) {
+        if (then.at < then.rows) {
+            const T *from = then.template first_row<const T>(a.x);
+            const uint64_t apart = a.x[then.which].sh;
+#pragma unroll
+            for (int u = 0; u < kUnit; u++) {
+                if (then.at + u < then.rows) {
+                    Part::fetch(ring + (half * kUnit + u) * kRow, from + l.at0);
+                    Part::fetch(ring + (half * kUnit + u) * kRow + kPlace, from + l.at1);
+                }
+                from += apart;
+            }
+        }
+        fetch_done();
+        then.next(a, most, stride, l.here);
+    };
+    ahead(0);
+    // weights and turns of a token as one two by two matrix for each pair: (p, q) -> (pp p + qp q, pq p + qq q)
+    uint64_t pp[V / 2], qp[V / 2], pq[V / 2], qq[V / 2];
+    for (uint32_t i = 0, half = 0; i < units; i++, half ^= 1u) {
+        ahead(half ^ 1u);
+        if (now.at == 0 && now.rows) {
+            const Sides<V> w = load_weight<P, V, HALVES>(a.weight[now.which], l);
             TokenTurns<T, V> turns;
-            for (uint32_t k = 0; k < a.run[which]; k += kRows) {
-                float x0[kRows][V], x1[kRows][V], g0[kRows][V], g1[kRows][V];
+            turns.of(a, l, now.token, now.s);
 #pragma unroll
-                for (uint32_t u = 0; u < kRows; u++) {
-                    if (here && h0 + k + u < h1) {
-                        const T *row = row_at<T>(a.x[which], b, s, h0 + k + u), *grad = row_at<T>(a.g[which], b, s, h0 + k + u);
-                        Piece<T, V>::load(row + l.at0, x0[u]);
-                        Piece<T, V>::load(row + l.at1, x1[u]);
-                        Piece<T, V>::load(grad + l.at0, g0[u]);
-                        Piece<T, V>::load(grad + l.at1, g1[u]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < V; i++) x0[u][i] = x1[u][i] = g0[u][i] = g1[u][i] = 0.0f;
-                    }
-                }
-                if (k == 0 && here) turns.of(a, l, token, s);
-#pragma unroll
-                for (uint32_t u = 0; u < kRows; u++) {
-                    const bool row_here = here && h0 + k + u < h1;
-                    if (row_here) turns.template apply<true>(a, l, g0[u], g1[u]);
-                    float ss = 0.0f, dot = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        ss = __fmaf_rn(x0[u][i], x0[u][i], __fmaf_rn(x1[u][i], x1[u][i], ss));
-                        dot = __fmaf_rn(g0[u][i] * w0[i], x0[u][i], __fmaf_rn(g1[u][i] * w1[i], x1[u][i], dot));
-                    }
-                    const float r = rsqrtf(__fmaf_rn(group_sum(ss, lanes), a.inv_dim, a.eps));
-                    const float mean = group_sum(dot, lanes) * r * a.inv_dim;          // of g' w xhat
-                    if (!row_here) continue;
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        const float h0_ = x0[u][i] * r, h1_ = x1[u][i] * r;
-                        sum0[i] = __fmaf_rn(g0[u][i], h0_, sum0[i]);
-                        sum1[i] = __fmaf_rn(g1[u][i], h1_, sum1[i]);
-                        x0[u][i] = r * __fmaf_rn(-h0_, mean, g0[u][i] * w0[i]);
-                        x1[u][i] = r * __fmaf_rn(-h1_, mean, g1[u][i] * w1[i]);
-                    }
-                    T *row = row_at<T>(a.y[which], b, s, h0 + k + u);
-                    Piece<T, V>::store(row + l.at0, x0[u]);
-                    Piece<T, V>::store(row + l.at1, x1[u]);
+            for (int e = 0; e < V / 2; e++) {
+                pp[e] = w.p[e];
+                qq[e] = w.q[e];
+                qp[e] = pq[e] = 0ull;
+                if (l.turns) {
+                    pp[e] = mul2(w.p[e], turns.c[e]);
+                    pq[e] = mul2(w.p[e], turns.s[e]);
+                    qp[e] = mul2(w.q[e], turns.s[e]) ^ 0x8000000080000000ull;
+                    qq[e] = mul2(w.q[e], turns.c[e]);
                 }
             }
         }
-        if (!a.weight[which]) continue;
+        fetched<1>();
+        const uint32_t rows = now.at < now.rows ? now.rows - now.at : 0u, place = ring + half * kUnit * kRow;
+        float ss[kUnit];
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            s_sum[threadIdx.x][i] = sum0[i];
-            s_sum[threadIdx.x][V + i] = sum1[i];
+        for (int u = 0; u < kUnit; u++) {
+            ss[u] = 0.0f;
+            if ((uint32_t)u >= rows) continue;
+            Part c, d;
+            c.take(place + u * kRow);
+            d.take(place + u * kRow + kPlace);
+            const Sides<V> x = sides_of<T, V, HALVES>(c, d);
+            uint64_t sum = 0ull;
+#pragma unroll
+            for (int e = 0; e < V / 2; e++) sum = fma2(x.q[e], x.q[e], fma2(x.p[e], x.p[e], sum));
+            ss[u] = low(sum) + high(sum);
         }
-        __syncthreads();
-        // element j of lane t % lanes, by the threads in turn
-        for (uint32_t t = threadIdx.x; t < lanes * 2u * V; t += kRotaryThreads) {
-            const uint32_t owner = t & (lanes - 1u), j = t >> a.lanes_log2;
-            const LaneShare o = lane_share<V>(a, owner);
-            if (!o.here) continue;
-            float sum = 0.0f;
-            for (uint32_t g = 0; g < groups; g++) sum += s_sum[(g << a.lanes_log2) + owner][j];
-            a.partial[((uint64_t)blockIdx.x * 2u + which) * a.dim + (j < V ? o.at0 + j : o.at1 + j - V)] = sum;
+        __syncwarp();
+        group_sum(ss, lanes);
+        if (rows) {
+            T *to = now.template first_row<T>(a.y);
+            const uint64_t apart = a.y[now.which].sh;
+#pragma unroll
+            for (int u = 0; u < kUnit; u++) {
+                if ((uint32_t)u < rows) {
+                    Part c, d;
+                    c.take(place + u * kRow);
+                    d.take(place + u * kRow + kPlace);
+                    Sides<V> x = sides_of<T, V, HALVES>(c, d);
+                    const uint64_t r = both(rsqrtf(__fmaf_rn(ss[u], a.inv_dim, a.eps)));
+#pragma unroll
+                    for (int e = 0; e < V / 2; e++) {
+                        const uint64_t p = mul2(r, fma2(x.q[e], qp[e], mul2(x.p[e], pp[e])));
+                        x.q[e] = mul2(r, fma2(x.q[e], qq[e], mul2(x.p[e], pq[e])));
+                        x.p[e] = p;
+                    }
+                    pieces_of<T, V, HALVES>(x, c, d);
+                    c.store(to + l.at0);
+                    d.store(to + l.at1);
+                }
+                to += apart;
+            }
         }
-        __syncthreads();
+        now.next(a, most, stride, l.here);
     }
+    fetched<0>();
+}
+
+template <typename T, typename P, int V, bool HALVES> __global__ void __launch_bounds__(kRotaryThreads, kRotaryCtasPerSm) rotary_norm_grad_kernel(const __grid_constant__ RotaryArgs a)
+{
+    using Part = Piece<T, V>;
+    constexpr int kUnit = (int)(kRotaryBytes / (2u * 4u * Part::kWords * 4u));
+    constexpr uint32_t kPlace = Part::kWords * 4 * kRotaryThreads, kRow = 4u * kPlace;
+    extern __shared__ __align__(16) unsigned char s_rows[];
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_rows) + threadIdx.x * Part::kAccess;
+    float *const s_sum = reinterpret_cast<float *>(s_rows + 2u * kUnit * kRow);       // [2][2 V][thread]
+    const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u), groups = kRotaryThreads >> a.lanes_log2, stride = gridDim.x * groups;
+    const uint32_t most = a.run[0] > a.run[1] ? a.run[0] : a.run[1], units = walk_units<kUnit>(a, groups, most);
+    const LaneShare l = lane_share<V, HALVES>(a, lane);
+    Walk<kUnit> now = {};
+    now.item = blockIdx.x * groups + (threadIdx.x >> a.lanes_log2);
+    now.enter(a, l.here);
+    Walk<kUnit> then = now;
+    const auto ahead = [&](uint32_t half) {
+        if (then.at < then.rows) {
+            const T *from = then.template first_row<const T>(a.x), *up = then.template first_row<const T>(a.g);
+            const uint64_t apart = a.x[then.which].sh, up_apart = a.g[then.which].sh;
+#pragma unroll
+            for (int u = 0; u < kUnit; u++) {
+                if (then.at + u < then.rows) {
+                    const uint32_t place = ring + (half * kUnit + u) * kRow;
+                    Part::fetch(place, from + l.at0);
+                    Part::fetch(place + kPlace, from + l.at1);
+                    Part::fetch(place + 2u * kPlace, up + l.at0);
+                    Part::fetch(place + 3u * kPlace, up + l.at1);
+                }
+                from += apart;
+                up += up_apart;
+            }
+        }
+        fetch_done();
+        then.next(a, most, stride, l.here);
+    };
+    ahead(0);
+    Sides<V> sum, w;
+#pragma unroll
+    for (int e = 0; e < V / 2; e++) sum.p[e] = sum.q[e] = w.p[e] = w.q[e] = 0ull;
+    const auto keep_sum = [&](uint32_t which) {                     // to the thread's own places; the next sums begin at zero
+#pragma unroll
+        for (int e = 0; e < V / 2; e++) {
+            float *const at = s_sum + which * 2u * V * kRotaryThreads + threadIdx.x;
+            at[(2 * e) * kRotaryThreads] = low(sum.p[e]);
+            at[(2 * e + 1) * kRotaryThreads] = high(sum.p[e]);
+            at[(V + 2 * e) * kRotaryThreads] = low(sum.q[e]);
+            at[(V + 2 * e + 1) * kRotaryThreads] = high(sum.q[e]);
+            sum.p[e] = sum.q[e] = 0ull;
+        }
+    };
+    TokenTurns<T, V> turns;
+    uint32_t side = 0;                                              // queries first, then keys
+    bool weighed = false;
+    for (uint32_t i = 0, half = 0; i < units; i++, half ^= 1u) {
+        ahead(half ^ 1u);
+        if (now.at == 0 && now.rows) {
+            turns.of(a, l, now.token, now.s);
+            if (now.which != side) {
+                keep_sum(0);
+                side = 1;
+                weighed = false;
+            }
+            if (!weighed) w = load_weight<P, V, HALVES>(a.weight[side], l);
+            weighed = true;
+        }
+        fetched<1>();
+        const uint32_t rows = now.at < now.rows ? now.rows - now.at : 0u;
+        T *to = now.template first_row<T>(a.y);
+#pragma unroll
+        for (int u = 0; u < kUnit; u++) {
+            const bool row = (uint32_t)u < rows;
+            if (!__any_sync(0xffffffffu, row)) break;
+            const uint32_t place = ring + (half * kUnit + u) * kRow;
+            Part c, d;
+            c.take(place + 2u * kPlace);
+            d.take(place + 3u * kPlace);
+            Sides<V> g = sides_of<T, V, HALVES>(c, d);
+            if (row) turns.back(l, g);
+            c.take(place);
+            d.take(place + kPlace);
+            Sides<V> x = sides_of<T, V, HALVES>(c, d);
+            uint64_t ss = 0ull, dot = 0ull;
+#pragma unroll
+            for (int e = 0; e < V / 2; e++) {
+                ss = fma2(x.q[e], x.q[e], fma2(x.p[e], x.p[e], ss));
+                dot = fma2(mul2(g.q[e], w.q[e]), x.q[e], fma2(mul2(g.p[e], w.p[e]), x.p[e], dot));
+            }
+            float sums[2] = {row ? low(ss) + high(ss) : 0.0f, row ? low(dot) + high(dot) : 0.0f};
+            __syncwarp();
+            group_sum(sums, lanes);
+            if (row) {
+                const float r1 = rsqrtf(__fmaf_rn(sums[0], a.inv_dim, a.eps));
+                const uint64_t r = both(r1), mean = both(-(sums[1] * r1 * a.inv_dim));      // -(mean of g' w xhat)
+#pragma unroll
+                for (int e = 0; e < V / 2; e++) {
+                    const uint64_t hp = mul2(x.p[e], r), hq = mul2(x.q[e], r);
+                    sum.p[e] = fma2(g.p[e], hp, sum.p[e]);
+                    sum.q[e] = fma2(g.q[e], hq, sum.q[e]);
+                    x.p[e] = mul2(r, fma2(hp, mean, mul2(g.p[e], w.p[e])));
+                    x.q[e] = mul2(r, fma2(hq, mean, mul2(g.q[e], w.q[e])));
+                }
+                pieces_of<T, V, HALVES>(x, c, d);
+                c.store(to + l.at0);
+                d.store(to + l.at1);
+            }
+            to += a.y[now.which].sh;
+        }
+        now.next(a, most, stride, l.here);
+    }
+    fetched<0>();
+    keep_sum(side);
+    if (side == 0) keep_sum(1);                                     // no keys here: zeros
+    __syncthreads();
+    // value j of lane t % lanes, by the threads in turn
+    for (uint32_t which = 0; which < 2u; which++)
+        for (uint32_t t = threadIdx.x; a.weight[which] && t < lanes * 2u * V; t += kRotaryThreads) {
+            const uint32_t owner = t & (lanes - 1u), j = t >> a.lanes_log2;
+            const LaneShare o = lane_share<V, HALVES>(a, owner);
+            if (!o.here) continue;
+            float all = 0.0f;
+            for (uint32_t g = 0; g < groups; g++) all += s_sum[(which * 2u * V + j) * kRotaryThreads + (g << a.lanes_log2) + owner];
+            a.partial[((uint64_t)blockIdx.x * 2u + which) * a.dim + element_of<V, HALVES>(o, j)] = all;
+        }
 }
 
 // Sums the CTAs' partial sums of one weight's gradient: 32 columns to a CTA, every 32nd row to a warp.
@@ -335,7 +531,6 @@ template <typename P> __global__ void __launch_bounds__(1024) rotary_weight_kern
     if (sizeof(P) == 4) reinterpret_cast<float *>(out)[col] = sum;
     else reinterpret_cast<uint16_t *>(out)[col] = (uint16_t)narrow2<P>(sum, 0.0f);
 }
-template <> __device__ __forceinline__ uint32_t narrow2<float>(float, float) { return 0u; }    // never called: the branch above
 
 // --------------------------------------------------------------------------------------------- host
 static daf_status check_rotary(const daf_rotary_params *p, const double *frequencies)
@@ -397,7 +592,6 @@ static RotaryArgs rotary_args(const daf_rotary_params &p, const double *frequenc
     a.heads[1] = p.kv_heads;
     a.dim = p.head_dim;
     a.rotary = p.rotary_dim;
-    a.pairs_apart = p.style == DAF_ROTARY_HALVES;
     a.position_bytes = p.position_bytes;
     a.shared_positions = p.shared_positions;
     a.eps = p.eps;
@@ -406,7 +600,7 @@ static RotaryArgs rotary_args(const daf_rotary_params &p, const double *frequenc
     while ((1u << a.lanes_log2) < units) a.lanes_log2++;
     a.tokens.set(p.tokens);
     // Heads of a run: eight share a token's angles; fewer where the call is small, so that its rows spread over the SMs.
-    const uint64_t tokens = (uint64_t)p.batch * p.tokens, wanted = 148u * 1024u >> a.lanes_log2;
+    const uint64_t tokens = (uint64_t)p.batch * p.tokens, wanted = 148u * 512u >> a.lanes_log2;
     uint32_t run = 8u;
     while (run > 1u && tokens * ((p.heads + run - 1u) / run) < wanted) run /= 2u;
     for (int i = 0; i < 2; i++) {
@@ -418,28 +612,29 @@ static RotaryArgs rotary_args(const daf_rotary_params &p, const double *frequenc
     return a;
 }
 
-template <typename T, typename P, int V> static daf_status rotary_launch(const RotaryArgs &a, bool back, void *gqw, void *gkw, cudaStream_t s)
+template <typename T, typename P, int V, bool HALVES> static daf_status rotary_launch(const RotaryArgs &a, bool back, void *gqw, void *gkw, cudaStream_t s)
 {
-    const uint32_t groups = kRotaryThreads >> a.lanes_log2;
-    if (!back) {
-        rotary_norm_kernel<T, P, V><<<(a.items[0] + a.items[1] + groups - 1u) / groups, kRotaryThreads, 0, s>>>(a);
-        return DAF_OK;
-    }
-    const uint32_t most = a.items[0] > a.items[1] ? a.items[0] : a.items[1];
-    uint32_t ctas = (most + groups - 1u) / groups;
-    if (ctas > kRotaryCtas) ctas = kRotaryCtas;
-    rotary_norm_grad_kernel<T, P, V><<<ctas, kRotaryThreads, 0, s>>>(a);
+    const auto kernel = back ? &rotary_norm_grad_kernel<T, P, V, HALVES> : &rotary_norm_kernel<T, P, V, HALVES>;
+    const uint32_t groups = kRotaryThreads >> a.lanes_log2, wanted = (a.items[0] + a.items[1] + groups - 1u) / groups;
+    const uint32_t smem = (kRotaryBytes + (back ? 4u * V * (uint32_t)sizeof(float) : 0u)) * kRotaryThreads;
+    int most = 0;
+    if (persistent_ctas(reinterpret_cast<const void *>(kernel), (int)kRotaryThreads, (int)smem, &most) != cudaSuccess) return DAF_ERR_CUDA;
+    if (back && most > (int)kRotaryCtas) most = (int)kRotaryCtas;
+    const uint32_t ctas = wanted < (uint32_t)most ? wanted : (uint32_t)most;
+    kernel<<<ctas, kRotaryThreads, smem, s>>>(a);
     if (gqw || gkw) rotary_weight_kernel<P><<<dim3((a.dim + 31u) / 32u, 2), 1024, 0, s>>>(a.partial, ctas, a.dim, reinterpret_cast<P *>(gqw), reinterpret_cast<P *>(gkw));
     return DAF_OK;
 }
 static daf_status rotary_by_type(const daf_rotary_params &p, const RotaryArgs &a, bool back, void *gqw, void *gkw, cudaStream_t s)
 {
-    const bool wide = rotary_piece(p) == 8, f32 = p.param_dtype == DAF_F32;
-#define DAF_ROTARY(T, P) (wide ? rotary_launch<T, P, 8>(a, back, gqw, gkw, s) : rotary_launch<T, P, 4>(a, back, gqw, gkw, s))
+    const bool wide = rotary_piece(p) == 8, f32 = p.param_dtype == DAF_F32, halves = p.style == DAF_ROTARY_HALVES;
+#define DAF_ROTARY_V(T, P, V) (halves ? rotary_launch<T, P, V, true>(a, back, gqw, gkw, s) : rotary_launch<T, P, V, false>(a, back, gqw, gkw, s))
+#define DAF_ROTARY(T, P) (wide ? DAF_ROTARY_V(T, P, 8) : DAF_ROTARY_V(T, P, 4))
     if (p.dtype == DAF_F32) return DAF_ROTARY(float, float);
     if (p.dtype == DAF_F16) return f32 ? DAF_ROTARY(__half, float) : DAF_ROTARY(__half, __half);
     return f32 ? DAF_ROTARY(__nv_bfloat16, float) : DAF_ROTARY(__nv_bfloat16, __nv_bfloat16);
 #undef DAF_ROTARY
+#undef DAF_ROTARY_V
 }
 
 }  // namespace daf
