@@ -32,8 +32,7 @@ static AttnTensor tensor_of(const void *p, const uint64_t (&st)[3])
     return {const_cast<void *>(p), st[0], st[1], st[2]};
 }
 
-static bool encode_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows, uint32_t elems,
-                       CUtensorMapSwizzle swizzle)
+bool tile_map(CUtensorMap *map, bool bf16, void *at, const uint64_t (&extent)[4], const uint64_t (&stride)[3], const uint32_t (&box)[4], CUtensorMapSwizzle swizzle)
 {
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -44,12 +43,19 @@ static bool encode_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_
         return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(fn) : nullptr;
     }();
     if (!encode) return false;
-    const cuuint64_t extent[4] = {D, H, S, B}, none = (2ull * D + 15u) & ~15ull;     // an extent of one has no stride of its own
-    const cuuint64_t stride[3] = {H > 1u ? 2ull * t.sh : none, S > 1u ? 2ull * t.ss : none, B > 1u ? 2ull * t.sb : none};
-    const cuuint32_t box[4] = {elems, 1, rows, 1}, step[4] = {1, 1, 1, 1};
-    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride, box, step,
+    const cuuint64_t extents[4] = {extent[0], extent[1], extent[2], extent[3]}, strides[3] = {stride[0], stride[1], stride[2]};
+    const cuuint32_t step[4] = {1, 1, 1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, at, extents, strides, box, step,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static bool encode_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows, uint32_t elems,
+                       CUtensorMapSwizzle swizzle)
+{
+    const uint64_t extent[4] = {D, H, S, B}, none = (2ull * D + 15u) & ~15ull;     // an extent of one has no stride of its own
+    const uint64_t stride[3] = {H > 1u ? 2ull * t.sh : none, S > 1u ? 2ull * t.ss : none, B > 1u ? 2ull * t.sb : none};
+    return tile_map(map, bf16, t.p, extent, stride, {elems, 1, rows, 1}, swizzle);
 }
 
 bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows)

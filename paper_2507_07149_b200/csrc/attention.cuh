@@ -74,6 +74,9 @@ daf_status attn_zero(uint32_t dtype, const AttnTensor &t, uint32_t B, uint32_t S
 uint32_t attn_splits(const AttnArgs &a);
 template <typename T> daf_status attn_forward_tc(const AttnArgs &a, WorkspaceHeader *header, cudaStream_t s);
 
+// Map of a four-dimensional tensor of 16-bit elements (extents from the innermost on, strides of the other three in bytes) for copies of
+// `box`; false if the driver refuses it.
+bool tile_map(CUtensorMap *map, bool bf16, void *at, const uint64_t (&extent)[4], const uint64_t (&stride)[3], const uint32_t (&box)[4], CUtensorMapSwizzle swizzle);
 // Map of a tensor for copies of `rows` rows times 64 elements of one head; false if the driver refuses it.
 bool attn_tensor_map(CUtensorMap *map, bool bf16, const AttnTensor &t, uint32_t B, uint32_t S, uint32_t H, uint32_t D, uint32_t rows);
 // The same for storing 32 rows times 32 elements.

@@ -14,40 +14,44 @@
 // rounds the large ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  float16 and
 // binary32 matrices are held in two parts throughout (three products instead of one): 2e-6.
 //
-// One persistent kernel runs all products of all steps and matrices.  CTAs take tiles of 128 x N by a ticket, in an order
+// One persistent kernel runs all products of all steps and matrices.  Pairs of CTAs take tiles of 256 x N by a ticket, in an order
 // in which whatever a tile needs comes before it; a tile waits until its matrix's tiles of the earlier products are done
-// (a counter), so a CTA that waits only ever waits for tiles that running CTAs hold, and the matrices of a call fill one
-// another's gaps.  Roles: one warp takes tickets, waits and copies operands (TMA), one issues products (two accumulators in
-// tensor memory), eight read results, form the polynomial or the update and store them.
+// (a counter), so a pair that waits only ever waits for tiles that running pairs hold, and the matrices of a call fill one
+// another's gaps.  A pair, because one SM's shared memory cannot feed its tensor core: of a product of 256 x 256 each CTA holds half of
+// either operand.  Roles: the first CTA's warp 0 takes tickets, waits and tells both; warp 0 of each copies its halves of the operands
+// (TMA, a copy of 16 KB for each operand and 64 of the summed dimension: a copy takes some 200 cycles to issue whatever its
+// size, and copies of 8 KB took longer than the products, 0.45 against 0.31 us); the first CTA's warp 1 issues the products (two accumulators in tensor memory); eight warps of each read its half of
+// the result's rows, form the polynomial or the update and store them.
 #include "attention.cuh"
 #include "tensor_core.cuh"
 
 namespace daf {
 
-constexpr uint32_t kOrthThreads = 384, kOrthStages = 4, kOrthBox = 8192, kOrthStage = 6u * kOrthBox, kOrthOut = 2048;
-constexpr uint32_t kOrthGroups = 24, kOrthMatrices = 192, kOrthSlots = 4;
+constexpr uint32_t kOrthThreads = 384, kOrthStages = 6, kOrthBox = 8192, kOrthStage = 4u * kOrthBox, kOrthOut = 2048, kOrthRows = 256;
+constexpr uint32_t kOrthGroups = 20, kOrthMatrices = 192, kOrthSlots = 4;
 constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
 constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch: bounds the workspace (8 bytes and more per element)
 constexpr float kHeld = 4096.0f;                // G and P times this
 constexpr uint32_t kPrepUnits = 64;             // pieces of 256 columns of a row to a CTA of the preparing kernels
 
 struct OrthGroup {                              // matrices of one shape and type
-    CUtensorMap x[2], gram, poly;
+    // operands of the products, for each of x's two places: the Gram matrix's (of x), the polynomial's (of G), the update's
+    CUtensorMap gram_a[2], gram_b[2], poly_a, poly_b, upd_x[2], upd_poly;
     __half *x_at[2], *gram_at, *poly_at;        // [matrix][plane][row][pitch]; x always has two planes
     uint64_t x_plane, m_plane;                  // elements of a plane
     uint32_t r, c, m, x_pitch, m_pitch, tall, planes, count, first, dtype;
-    uint32_t sym_tiles, sym_cols, upd_tiles, upd_rows;   // of one matrix
+    uint32_t sym_tiles, sym_cols, upd_tiles, upd_rows, n;   // of one matrix; columns of a tile
     uint32_t sym_first, upd_first, prep_ctas, prep_first;
 };
 struct OrthArgs {
     OrthGroup g[kOrthGroups];
     const void *in[kOrthMatrices];
     void *out[kOrthMatrices];
-    uint32_t groups, matrices, steps, sym_total, upd_total, sym_n, upd_n, prep_total, keep_status;
+    uint32_t groups, matrices, steps, sym_total, upd_total, prep_total, keep_status;
     float a, b, c, eps;
     double *partial;
     float *scale;                               // K of each matrix
-    uint32_t *done;                             // finished eighths of tiles of each matrix
+    uint32_t *done;                             // finished sixteenths of tiles of each matrix
     WorkspaceHeader *header;
     unsigned int *device_status;
 };
@@ -65,7 +69,7 @@ __device__ __forceinline__ void orth_load8(const OrthGroup &g, const void *p, ui
 {
     const uint32_t eb = g.dtype == DAF_F32 ? 4u : 2u;
     const uint64_t at = (uint64_t)row * g.c + col;
-    if (g.c % 8u == 0 && reinterpret_cast<uintptr_t>(p) % (8u * eb) == 0) {
+    if (g.c % 8u == 0 && reinterpret_cast<uintptr_t>(p) % (8u * eb) == 0 && col < g.c) {
         if (g.dtype == DAF_F32) Elem<float>::load8(reinterpret_cast<const float *>(p) + at, x);
         else if (g.dtype == DAF_F16) Elem<__half>::load8(reinterpret_cast<const __half *>(p) + at, x);
         else Elem<__nv_bfloat16>::load8(reinterpret_cast<const __nv_bfloat16 *>(p) + at, x);
@@ -149,7 +153,7 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const __grid_constant__
     for (uint32_t j = threadIdx.x >> 5; j < kPrepUnits; j += 8u) {
         const uint64_t unit = (uint64_t)s.cta * kPrepUnits + j;
         const uint32_t row = (uint32_t)(unit / s.cols), col = (uint32_t)(unit - (uint64_t)row * s.cols) * 256u + lane * 8u;
-        if (unit >= s.units || col >= g.c) continue;
+        if (unit >= s.units || col >= g.x_pitch) continue;             // zeros behind the end: products read them
         float x[8], rest[8];
         orth_load8(g, in, row, col, x);
 #pragma unroll
@@ -166,7 +170,67 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const __grid_constant__
 enum : uint32_t { kGram = 0, kPoly = 1, kUpdate = 2, kNoTile = 3 };
 struct OrthTile {
     uint32_t kind, step, group, matrix, row, col;
+    __device__ __forceinline__ uint4 packed() const { return make_uint4(kind | step << 8 | group << 16, matrix, row, col); }
+    static __device__ __forceinline__ OrthTile from(uint4 v) { return {v.x & 255u, v.x >> 8 & 255u, v.x >> 16, v.y, v.z, v.w}; }
 };
+
+// ---- a pair of CTAs
+__device__ __forceinline__ uint32_t pair_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void pair_meet() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// The address of the CTA `rank`'s copy of something in this CTA's shared memory.
+__device__ __forceinline__ uint32_t in_cta(const void *mine, uint32_t rank)
+{
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ void arrive_in(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool try_from_pair(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// bar_wait for a barrier at which the other CTA arrives, too.
+__device__ __forceinline__ bool wait_from_pair(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag)
+{
+    if (try_from_pair(bar, parity)) return true;
+    const uint64_t start = now_ns();
+    while (!try_from_pair(bar, parity)) {
+        if (*abort_flag) return false;
+        if (now_ns() - start > kWaitNanoseconds) {
+            *abort_flag = 1u;
+            return false;
+        }
+    }
+    return true;
+}
+// A copy into this CTA's shared memory that is counted at a barrier of either CTA.
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int elem, int row, int span, int matrix)
+{
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(elem), "r"(row), "r"(span), "r"(matrix) : "memory");
+}
+template <bool ADD_ALWAYS = false>
+__device__ __forceinline__ void pair_product(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add = true)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 q, %4, 0;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 da, {%1, %5};\n\t"
+                 "mov.b64 db, {%2, %5};\n\t@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(one), "n"(kOperandHigh), "r"((uint32_t)(ADD_ALWAYS || add)) : "memory");
+}
+// The barrier of each CTA in `mask` is arrived at when every product issued so far by this lane is done.
+__device__ __forceinline__ void pair_done(uint32_t one, uint64_t *bar, uint32_t mask)
+{
+    asm volatile("{\n\t.reg .pred q;\n\t.reg .b16 m;\n\tsetp.ne.b32 q, %1, 0;\n\tcvt.u16.u32 m, %2;\n\t"
+                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
+                 ::"r"(smem_u32(bar)), "r"(one), "r"(mask) : "memory");
+}
 
 __device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket)
 {
@@ -187,8 +251,8 @@ __device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket
         t.matrix = i / g.upd_tiles;
         i -= t.matrix * g.upd_tiles;
         const uint32_t col = i / g.upd_rows;
-        t.row = (i - col * g.upd_rows) * 128u;
-        t.col = col * a.upd_n;
+        t.row = (i - col * g.upd_rows) * kOrthRows;
+        t.col = col * g.n;
         return t;
     }
     if (i >= a.sym_total) {
@@ -204,12 +268,12 @@ __device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket
     for (uint32_t first = 0;;) {
         const uint32_t left = g.sym_cols - first;
         if (i < left) {
-            t.col = (first + i) * a.sym_n;
+            t.col = (first + i) * g.n;
             return t;
         }
         i -= left;
-        t.row += 128u;
-        first = t.row / a.sym_n;
+        t.row += kOrthRows;
+        first = t.row / g.n;
     }
 }
 
@@ -324,22 +388,23 @@ __device__ __forceinline__ void store_transposed(__half *at, uint32_t pitch, uin
     }
 }
 
-__global__ void __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
 {
     extern __shared__ __align__(1024) unsigned char s_raw[];
     struct Bars {
-        uint64_t full[kOrthStages], empty[kOrthStages], told[kOrthSlots], heard[kOrthSlots], acc_full[2], acc_empty[2], drain;
-        OrthTile tile[kOrthSlots];
+        // full, heard, acc_empty, drain: the first CTA's count for both
+        uint64_t full[kOrthStages], empty[kOrthStages], told[kOrthSlots], heard[kOrthSlots], acc_full[2], acc_empty[2], drain, pad;
+        uint4 tile[kOrthSlots];
         uint32_t tmem, abort, late;
     };
     static_assert(sizeof(Bars) <= kOrthBars, "barriers fit their place");
     Bars &bars = *reinterpret_cast<Bars *>(s_raw);
-    if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread
+    if (smem_u32(s_raw) & 1023u) {                                 // the same for every thread of both
         if (threadIdx.x == 0) record_error(a.header, a.device_status, DAF_ERR_UNSUPPORTED);
         return;
     }
     unsigned char *const stages = s_raw + kOrthBars;
-    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u, rank = pair_rank();
     if (threadIdx.x == 0) {
         bars.abort = bars.late = 0u;
         for (uint32_t i = 0; i < kOrthStages; i++) {
@@ -348,162 +413,208 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __
         }
         for (uint32_t i = 0; i < kOrthSlots; i++) {
             bar_init(&bars.told[i], 1);
-            bar_init(&bars.heard[i], 9);
+            bar_init(&bars.heard[i], 18);                           // eight warps of each, the products, the other's copies
         }
         bar_init(&bars.drain, 1);
         for (uint32_t i = 0; i < 2u; i++) {
             bar_init(&bars.acc_full[i], 1);
-            bar_init(&bars.acc_empty[i], 8);
+            bar_init(&bars.acc_empty[i], 16);
         }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
     }
-    if (warp == 2) tmem_alloc(&bars.tmem, 512);
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
     tmem_before_sync();
     __syncthreads();
+    pair_meet();
     tmem_after_sync();
     const uint32_t tmem = bars.tmem;
     volatile uint32_t *const stop = &bars.abort;
 
     if (warp == 0) {                                               // ---- tickets and copies
         if (lane == 0) {
-            uint32_t ticket = atomicAdd(&a.header->ticket, 1u), st = 0, ph = 0, issued = 0;
+            uint32_t ticket = rank == 0 ? atomicAdd(&a.header->ticket, 1u) : 0u, st = 0, ph = 0, issued = 0;
             for (uint32_t n = 0;; n++) {
                 const uint32_t slot = n % kOrthSlots;
-                if (n >= kOrthSlots && !bar_wait(&bars.heard[slot], (n / kOrthSlots - 1u) & 1u, stop)) break;
-                const OrthTile t = orth_tile(a, ticket);
-                bars.tile[slot] = t;
-                bar_arrive(&bars.told[slot]);
+                OrthTile t;
+                if (rank == 0) {
+                    if (n >= kOrthSlots && !wait_from_pair(&bars.heard[slot], (n / kOrthSlots - 1u) & 1u, stop)) break;
+                    t = orth_tile(a, ticket);
+                    if (t.kind != kNoTile) {
+                        ticket = atomicAdd(&a.header->ticket, 1u);
+                        const OrthGroup &g = a.g[t.group];
+                        const uint32_t need = 16u * (t.step * (2u * g.sym_tiles + g.upd_tiles) + t.kind * g.sym_tiles);
+                        if (need && !wait_tiles(a.done + g.first + t.matrix, need, stop)) break;
+                    }
+                    const uint4 v = t.packed();
+                    bars.tile[slot] = v;
+                    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(in_cta(&bars.tile[slot], 1)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                    bar_arrive(&bars.told[slot]);
+                    arrive_in(in_cta(&bars.told[slot], 1));
+                } else {
+                    if (!wait_from_pair(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
+                    t = OrthTile::from(bars.tile[slot]);
+                    arrive_in(in_cta(&bars.heard[slot], 0));
+                }
                 if (t.kind == kNoTile) break;
-                ticket = atomicAdd(&a.header->ticket, 1u);
                 const OrthGroup &g = a.g[t.group];
-                const uint32_t need = 8u * (t.step * (2u * g.sym_tiles + g.upd_tiles) + t.kind * g.sym_tiles);
-                if (need && !wait_tiles(a.done + g.first + t.matrix, need, stop)) break;
                 asm volatile("fence.proxy.async;" ::: "memory");    // what other CTAs wrote by stores is now read by copies
+                const uint32_t buf = t.step & 1u;
                 const CUtensorMap *ma, *mb;
-                uint32_t keys, plane_a, plane_b, boxes;             // the summed dimension; planes of a matrix in each map
+                uint32_t keys = g.m, plane_a = g.planes, plane_b = g.planes;   // the summed dimension; planes of a matrix in each map
                 bool cross_a = false, cross_b = false;              // the summed dimension is not the contiguous one
                 if (t.kind == kPoly) {
-                    ma = mb = &g.gram;
-                    keys = g.m;
-                    plane_a = plane_b = g.planes;
-                    boxes = a.sym_n / 64u;
+                    ma = &g.poly_a;
+                    mb = &g.poly_b;
                 } else if (t.kind == kGram) {
-                    ma = mb = &g.x[t.step & 1u];
+                    ma = &g.gram_a[buf];
+                    mb = &g.gram_b[buf];
                     keys = g.tall ? g.r : g.c;
                     plane_a = plane_b = 2u;
                     cross_a = cross_b = g.tall;
-                    boxes = a.sym_n / 64u;
                 } else {
-                    ma = g.tall ? &g.x[t.step & 1u] : &g.poly;
-                    mb = g.tall ? &g.poly : &g.x[t.step & 1u];
-                    keys = g.m;
-                    plane_a = g.tall ? 2u : g.planes;
-                    plane_b = g.tall ? g.planes : 2u;
+                    ma = g.tall ? &g.upd_x[buf] : &g.upd_poly;
+                    mb = g.tall ? &g.upd_poly : &g.upd_x[buf];
+                    (g.tall ? plane_a : plane_b) = 2u;
                     cross_b = !g.tall;
-                    boxes = a.upd_n / 64u;
                 }
+                const int row = (int)(t.row + 128u * rank), col = (int)(t.col + g.n / 2u * rank);
+                const uint32_t bytes = 2u * (2u * kOrthBox + g.n / 128u * kOrthBox);
                 bool ok = true;
-                for (uint32_t part = g.planes == 2u ? 0u : 2u; part < 3u && ok; part++) {      // small parts first
-                    const int ba = (int)(t.matrix * plane_a + (part == 1u)), bb = (int)(t.matrix * plane_b + (part == 0u));
-                    for (uint32_t k = 0; k < keys; k += 64u) {
+                for (int k = 0; k < (int)keys && ok; k += 64)
+                    for (uint32_t part = 0; part < g.planes; part++) {
                         if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) break;
-                        const uint32_t to = smem_u32(stages + st * kOrthStage);
-                        bar_expect(&bars.full[st], (2u + boxes) * kOrthBox);
-                        for (uint32_t i = 0; i < 2u; i++)
-                            tma_load(to + i * kOrthBox, ma, &bars.full[st], cross_a ? (int)(t.row + 64u * i) : (int)k, ba, cross_a ? (int)k : (int)(t.row + 64u * i), 0);
-                        for (uint32_t i = 0; i < boxes; i++)
-                            tma_load(to + (2u + i) * kOrthBox, mb, &bars.full[st], cross_b ? (int)(t.col + 64u * i) : (int)k, bb, cross_b ? (int)k : (int)(t.col + 64u * i), 0);
+                        const uint32_t to = smem_u32(stages + st * kOrthStage), bar = in_cta(&bars.full[st], 0);
+                        if (rank == 0) bar_expect(&bars.full[st], bytes);
+                        pair_load(to, ma, bar, cross_a ? 0 : k, cross_a ? k : row, cross_a ? row / 64 : 0, (int)(t.matrix * plane_a + part));
+                        pair_load(to + 2u * kOrthBox, mb, bar, cross_b ? 0 : k, cross_b ? k : col, cross_b ? col / 64 : 0, (int)(t.matrix * plane_b + part));
                         issued++;
                         if (++st == kOrthStages) st = 0, ph ^= 1u;
                     }
-                }
                 if (!ok) break;
             }
-            // nothing may be on its way into shared memory when the CTA ends (normally all has long arrived)
-            for (uint32_t i = 0; i < kOrthStages && i < issued; i++) {
-                const uint32_t last = issued - 1u - i;
-                bar_wait(&bars.full[last % kOrthStages], last / kOrthStages & 1u, &bars.late);
-            }
+            // Nothing may be on its way into shared memory when the CTA ends.  Normally all has long arrived: the products took it.
+            if (*stop)
+                for (const uint64_t start = now_ns(); now_ns() - start < 1000000u;) {}
         }
-    } else if (warp == 1) {                                        // ---- products
+    } else if (warp == 1 && rank == 0) {                           // ---- products
         const uint32_t one = elect_lane();
         uint32_t st = 0, ph = 0;
+        const auto step_on = [&]() {
+            if (++st == kOrthStages) st = 0, ph ^= 1u;
+        };
         for (uint32_t n = 0;; n++) {
             const uint32_t slot = n % kOrthSlots, buf = n & 1u;
             if (!bar_wait(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
-            const OrthTile t = bars.tile[slot];
+            const OrthTile t = OrthTile::from(bars.tile[slot]);
             __syncwarp();
             if (lane == 0) bar_arrive(&bars.heard[slot]);
             if (t.kind == kNoTile) break;
-            if (n >= 2u && !bar_wait(&bars.acc_empty[buf], (n / 2u - 1u) & 1u, stop)) break;
+            if (n >= 2u && !wait_from_pair(&bars.acc_empty[buf], (n / 2u - 1u) & 1u, stop)) break;
             tmem_after_sync();
             const OrthGroup &g = a.g[t.group];
             const bool cross_a = t.kind == kGram && g.tall, cross_b = cross_a || (t.kind == kUpdate && !g.tall);
             const uint32_t keys = t.kind == kGram && g.tall ? g.r : t.kind == kGram ? g.c : g.m;
-            const uint32_t desc = product_desc(false, t.kind == kUpdate ? a.upd_n : a.sym_n, cross_b) | (cross_a ? 1u << 15 : 0u);
+            // M = 256: product_desc says 128
+            const uint32_t desc = product_desc(false, g.n, cross_b) + ((256u - 128u) >> 4 << 24) + (cross_a ? 1u << 15 : 0u);
             const uint32_t step_a = cross_a ? 128u : 2u, step_b = cross_b ? 128u : 2u;         // 16 of the summed dimension, in 16-byte units
-            const uint32_t rounds = (keys + 63u) / 64u * (g.planes == 2u ? 3u : 1u), d = tmem + buf * 256u;
+            const uint32_t rounds = (keys + 63u) / 64u, d = tmem + buf * 256u;
             bool ok = true;
             for (uint32_t k = 0; k < rounds; k++) {
-                if (!(ok = bar_wait(&bars.full[st], ph, stop))) break;
+                if (!(ok = wait_from_pair(&bars.full[st], ph, stop))) break;
                 tmem_after_sync();
                 const uint32_t at = smem_u32(stages + st * kOrthStage);
                 const uint32_t la = operand_low(at, kOrthBox), lb = operand_low(at + 2u * kOrthBox, kOrthBox);
-                product_ss(one, d, la, lb, desc, k > 0);
+                pair_product(one, d, la, lb, desc, k > 0);
 #pragma unroll
-                for (uint32_t s = 1; s < 4u; s++) product_ss<true>(one, d, la + s * step_a, lb + s * step_b, desc);
-                products_done(one, &bars.empty[st]);
-                if (++st == kOrthStages) st = 0, ph ^= 1u;
+                for (uint32_t s = 1; s < 4u; s++) pair_product<true>(one, d, la + s * step_a, lb + s * step_b, desc);
+                if (g.planes == 2u) {
+                    // the small parts' stage behind it; their products have an accumulator of their own, where they are not cut
+                    // to the large sum's last place
+                    uint64_t *const first = &bars.empty[st];
+                    step_on();
+                    if (!(ok = wait_from_pair(&bars.full[st], ph, stop))) break;
+                    tmem_after_sync();
+                    const uint32_t small = smem_u32(stages + st * kOrthStage);
+                    const uint32_t sa = operand_low(small, kOrthBox), sb = operand_low(small + 2u * kOrthBox, kOrthBox);
+                    pair_product(one, d + 128u, la, sb, desc, k > 0);
+                    pair_product<true>(one, d + 128u, sa, lb, desc);
+#pragma unroll
+                    for (uint32_t s = 1; s < 4u; s++) {
+                        pair_product<true>(one, d + 128u, la + s * step_a, sb + s * step_b, desc);
+                        pair_product<true>(one, d + 128u, sa + s * step_a, lb + s * step_b, desc);
+                    }
+                    pair_done(one, first, 3u);
+                }
+                pair_done(one, &bars.empty[st], 3u);
+                step_on();
             }
-            products_done(one, &bars.acc_full[buf]);
+            pair_done(one, &bars.acc_full[buf], 3u);
             if (!ok) break;
         }
-        products_done(one, &bars.drain);
+        pair_done(one, &bars.drain, 1u);
         bar_wait(&bars.drain, 0, &bars.late);
     } else if (warp >= 4) {                                        // ---- results
         const uint32_t quarter = warp & 3u, half = (warp - 4u) >> 2;
         unsigned char *const stage = stages + kOrthStages * kOrthStage + (warp - 4u) * kOrthOut;
         for (uint32_t n = 0;; n++) {
             const uint32_t slot = n % kOrthSlots, buf = n & 1u;
-            if (!bar_wait(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
-            const OrthTile t = bars.tile[slot];
+            if (!wait_from_pair(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
+            const OrthTile t = OrthTile::from(bars.tile[slot]);
             __syncwarp();
-            if (lane == 0) bar_arrive(&bars.heard[slot]);
+            if (lane == 0) arrive_in(in_cta(&bars.heard[slot], 0));
             if (t.kind == kNoTile) break;
-            if (!bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
-            tmem_after_sync();
             const OrthGroup &g = a.g[t.group];
-            const bool update = t.kind == kUpdate, last = t.step + 1u == a.steps;
-            const uint32_t width = update ? a.upd_n : a.sym_n, row = t.row + quarter * 32u;
+            const bool update = t.kind == kUpdate, gram = t.kind == kGram, last = t.step + 1u == a.steps;
+            const uint32_t chunks = g.n / 64u, row = t.row + 128u * rank + quarter * 32u;
             const uint32_t rows = update ? g.r : g.m, pitch = update ? g.x_pitch : g.m_pitch, matrix = g.first + t.matrix;
             const float k = __ldcg(a.scale + matrix);
             // what is added to the product, and factors of both
             const __half *with = update ? g.x_at[t.step & 1u] + (uint64_t)t.matrix * 2u * g.x_plane : g.gram_at + (uint64_t)t.matrix * g.planes * g.m_plane;
             const uint64_t plane = update ? g.x_plane : g.m_plane;
             const bool two = g.planes == 2u || (update && (t.step == 1u || t.step == 2u));
-            const float of_product = t.kind == kGram ? __fdiv_rn(kHeld, k * k) : t.kind == kPoly ? a.c / kHeld : 1.0f / kHeld;
+            const float of_product = gram ? __fdiv_rn(kHeld, k * k) : t.kind == kPoly ? a.c / kHeld : 1.0f / kHeld;
             const float of_with = update ? a.a : a.b;
             __half *to = update ? g.x_at[(t.step + 1u) & 1u] + (uint64_t)t.matrix * 2u * g.x_plane
-                                : (t.kind == kGram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * g.planes * g.m_plane;
-            for (uint32_t j = half * (width / 64u); j < (half + 1u) * (width / 64u); j++) {
-                const uint32_t col = t.col + j * 32u;
+                                : (gram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * g.planes * g.m_plane;
+            OrthBlock ahead, ahead2;                                // of the next 32 columns, on their way during the products
+            const auto look_ahead = [&](uint32_t j) {
+                if (gram) return;
+                const uint32_t col = t.col + (half * chunks + j) * 32u;
+                ahead.load(with, pitch, row, rows, j < chunks ? col : pitch, lane);
+                if (two) ahead2.load(with + plane, pitch, row, rows, j < chunks ? col : pitch, lane);
+            };
+            look_ahead(0);
+            if (!bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
+            tmem_after_sync();
+            for (uint32_t j = 0; j < chunks; j++) {
+                const uint32_t col = t.col + (half * chunks + j) * 32u, acc = tmem + buf * 256u + (half * chunks + j) * 32u + (quarter << 21);
                 if (row >= rows || col >= pitch) break;
                 float x[32];
-                OrthBlock w;
-                if (t.kind != kGram) w.load(with, pitch, row, rows, col, lane);
+                OrthBlock w = ahead, w2 = ahead2;
+                look_ahead(j + 1u);
                 __syncwarp();
-                tmem_load32(tmem + buf * 256u + j * 32u + (quarter << 21), x);
+                tmem_load32(acc, x);
                 tmem_wait_loads();
+                if (g.planes == 2u) {
+                    float small[32];
+                    tmem_load32(acc + 128u, small);
+                    tmem_wait_loads();
+#pragma unroll
+                    for (int i = 0; i < 32; i++) x[i] += small[i];
+                }
 #pragma unroll
                 for (int i = 0; i < 32; i++) x[i] *= of_product;
-                if (t.kind != kGram) {
+                if (!gram) {
+                    if (two) {
+                        w2.to_rows(stage, lane);
+                        w2.add(x, of_with);
+                    }
                     w.to_rows(stage, lane);
                     w.add(x, of_with);
-                    if (two) {
-                        w.load(with + plane, pitch, row, rows, col, lane);
-                        w.to_rows(stage, lane);
-                        w.add(x, of_with);
-                    }
                 }
                 if (update && last) {
                     const float by = __fdiv_rn(1.0f, k);
@@ -538,7 +649,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __
                     continue;
                 }
                 // the other half of a symmetric matrix: where no tile of its own covers it
-                const bool mirror = !update && (row / a.sym_n + 1u) * a.sym_n <= col / 128u * 128u;
+                const bool mirror = !update && row / g.n < col / kOrthRows * kOrthRows / g.n;
                 const uint32_t planes = g.planes == 2u || (update && t.step < 2u) ? 2u : 1u;
                 for (uint32_t p = 0; p < planes; p++) {
                     round32<__half>(x, w.v);
@@ -550,7 +661,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __
             }
             tmem_before_sync();
             __syncwarp();
-            if (lane == 0) bar_arrive(&bars.acc_empty[buf]);
+            if (lane == 0) arrive_in(in_cta(&bars.acc_empty[buf], 0));
             if (update && last) continue;                          // nothing waits for the result
             asm volatile("fence.proxy.async;" ::: "memory");
             __threadfence();
@@ -561,10 +672,12 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __
             }
         }
     }
+    __syncwarp();
     tmem_before_sync();
     __syncthreads();
     if (threadIdx.x == 0 && (bars.abort || bars.late)) record_error(a.header, a.device_status, DAF_ERR_TIMEOUT);
-    if (warp == 2) tmem_free(tmem, 512);
+    pair_meet();                                                   // neither reaches into the other behind this
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
 // --------------------------------------------------------------------------------------------- host
@@ -585,12 +698,12 @@ static daf_status check_orth(const daf_orthogonalize_params *p, uint32_t n, cons
     return DAF_OK;
 }
 
-// Tiles of 128 rows times N columns: N is 256 where that leaves every SM a tile, else as small as it takes (64 at least).
+// Tiles of a symmetric matrix: of each 256 rows, those that reach the diagonal or lie right of it.
 static uint32_t orth_sym_tiles(uint32_t m, uint32_t width)
 {
     const uint32_t cols = (m + width - 1u) / width;
     uint32_t tiles = 0;
-    for (uint32_t row = 0; row < m; row += 128u) tiles += cols - row / width;
+    for (uint32_t row = 0; row < m; row += kOrthRows) tiles += cols - row / width;
     return tiles;
 }
 
@@ -633,16 +746,15 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     a->c = p->coefficients[2];
     a->eps = p->eps;
     a->prep_total = 0;
-    for (a->sym_n = 256u;; a->sym_n /= 2u) {
-        a->sym_total = 0;
-        for (uint32_t k = 0; k < a->groups; k++) a->sym_total += a->g[k].count * orth_sym_tiles(a->g[k].r < a->g[k].c ? a->g[k].r : a->g[k].c, a->sym_n);
-        if (a->sym_total >= 148u || a->sym_n == 64u) break;
+    // Tiles are 256 columns wide where that leaves every pair of SMs one, else 128; matrices in two parts need the other half of an
+    // accumulator for the small products.
+    uint32_t tiles = 0;
+    for (uint32_t k = 0; k < a->groups; k++) {
+        const uint32_t r = a->g[k].r, c = a->g[k].c, m = r < c ? r : c, sym = orth_sym_tiles(m, 256u);
+        const uint32_t upd = ((r + kOrthRows - 1u) / kOrthRows) * ((c + 255u) / 256u);
+        tiles += a->g[k].count * (sym < upd ? sym : upd);
     }
-    for (a->upd_n = 256u;; a->upd_n /= 2u) {
-        a->upd_total = 0;
-        for (uint32_t k = 0; k < a->groups; k++) a->upd_total += a->g[k].count * ((a->g[k].r + 127u) / 128u) * ((a->g[k].c + a->upd_n - 1u) / a->upd_n);
-        if (a->upd_total >= 148u || a->upd_n == 64u) break;
-    }
+    const uint32_t width = tiles >= 74u ? 256u : 128u;
     uint32_t sym = 0, upd = 0;
     uint64_t bytes = sizeof(WorkspaceHeader) + up_to(2ull * kOrthMatrices * sizeof(uint32_t), 256u);
     for (uint32_t k = 0; k < a->groups; k++) {
@@ -654,10 +766,11 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
         g.m_pitch = (uint32_t)up_to(g.m, 64u);
         g.x_plane = (uint64_t)g.r * g.x_pitch;
         g.m_plane = (uint64_t)g.m * g.m_pitch;
-        g.sym_cols = (g.m + a->sym_n - 1u) / a->sym_n;
-        g.sym_tiles = orth_sym_tiles(g.m, a->sym_n);
-        g.upd_rows = (g.r + 127u) / 128u;
-        g.upd_tiles = g.upd_rows * ((g.c + a->upd_n - 1u) / a->upd_n);
+        g.n = g.planes == 2u ? 128u : width;
+        g.sym_cols = (g.m + g.n - 1u) / g.n;
+        g.sym_tiles = orth_sym_tiles(g.m, g.n);
+        g.upd_rows = (g.r + kOrthRows - 1u) / kOrthRows;
+        g.upd_tiles = g.upd_rows * ((g.c + g.n - 1u) / g.n);
         g.sym_first = sym;
         g.upd_first = upd;
         sym += g.count * g.sym_tiles;
@@ -665,9 +778,21 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
         g.prep_ctas = (uint32_t)(((uint64_t)g.r * ((g.c + 255u) / 256u) + kPrepUnits - 1u) / kPrepUnits);
         g.prep_first = a->prep_total;
         a->prep_total += g.count * g.prep_ctas;
-        bytes += g.count * 2u * (up_to(2u * g.x_plane * sizeof(__half), 256u) + up_to(g.planes * g.m_plane * sizeof(__half), 256u));
+        bytes += 2u * (up_to(g.count * 2u * g.x_plane * sizeof(__half), 256u) + up_to(g.count * g.planes * g.m_plane * sizeof(__half), 256u));
     }
+    a->sym_total = sym;
+    a->upd_total = upd;
     *workspace = bytes + up_to(a->prep_total * sizeof(double), 256u);
+}
+
+// Maps of `matrices` float16 matrices for copies of a tile's share of an operand, 64 of the summed dimension at a time: along the rows
+// (`lines` rows of 64 columns; what lies behind the last row or column comes as zeros) or, where rows are summed over, across
+// them (64 rows of `lines` columns in spans of 64; the columns up to the pitch are zeros in memory).
+static bool orth_map(CUtensorMap *map, __half *at, uint64_t plane, uint32_t matrices, uint32_t rows, uint32_t cols, uint32_t pitch, bool across, uint32_t lines)
+{
+    if (across)
+        return tile_map(map, false, at, {64u, rows, pitch / 64u, matrices}, {2ull * pitch, 128u, 2ull * plane}, {64u, 64u, lines / 64u, 1u}, CU_TENSOR_MAP_SWIZZLE_128B);
+    return tile_map(map, false, at, {cols, rows, 1u, matrices}, {2ull * pitch, 2ull * plane, 2ull * plane}, {64u, lines, 1u, 1u}, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // Where a batch's buffers lie, and their maps.
@@ -680,18 +805,25 @@ static bool orth_place(OrthArgs *a, char *at)
     at += up_to(2ull * kOrthMatrices * sizeof(uint32_t), 256u);
     a->partial = reinterpret_cast<double *>(at);
     at += up_to(a->prep_total * sizeof(double), 256u);
+    const auto take = [&](uint64_t halves) {
+        __half *const p = reinterpret_cast<__half *>(at);
+        at += up_to(halves * sizeof(__half), 256u);
+        return p;
+    };
     for (uint32_t k = 0; k < a->groups; k++) {
         OrthGroup &g = a->g[k];
-        const auto take = [&](__half **p, CUtensorMap *map, uint64_t plane, uint32_t planes, uint32_t rows, uint32_t cols, uint32_t pitch) {
-            *p = reinterpret_cast<__half *>(at);
-            at += up_to(g.count * planes * plane * sizeof(__half), 256u);
-            const AttnTensor t = {*p, 0, pitch, plane};
-            return attn_tensor_map(map, false, t, 1, rows, g.count * planes, cols, 64);
-        };
-        for (int i = 0; i < 2; i++)
-            if (!take(&g.x_at[i], &g.x[i], g.x_plane, 2u, g.r, g.c, g.x_pitch)) return false;
-        if (!take(&g.gram_at, &g.gram, g.m_plane, g.planes, g.m, g.m, g.m_pitch) || !take(&g.poly_at, &g.poly, g.m_plane, g.planes, g.m, g.m, g.m_pitch))
-            return false;
+        const uint32_t half = g.n / 2u, xs = g.count * 2u, ms = g.count * g.planes;      // columns of a tile in each CTA; planes in all
+        for (int i = 0; i < 2; i++) g.x_at[i] = take(xs * g.x_plane);
+        g.gram_at = take(ms * g.m_plane);
+        g.poly_at = take(ms * g.m_plane);
+        bool ok = orth_map(&g.poly_a, g.gram_at, g.m_plane, ms, g.m, g.m, g.m_pitch, false, 128u) &&
+                  orth_map(&g.poly_b, g.gram_at, g.m_plane, ms, g.m, g.m, g.m_pitch, false, half) &&
+                  orth_map(&g.upd_poly, g.poly_at, g.m_plane, ms, g.m, g.m, g.m_pitch, false, g.tall ? half : 128u);
+        for (int i = 0; i < 2 && ok; i++)
+            ok = orth_map(&g.gram_a[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, g.tall, 128u) &&
+                 orth_map(&g.gram_b[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, g.tall, half) &&
+                 orth_map(&g.upd_x[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, !g.tall, g.tall ? 128u : half);
+        if (!ok) return false;
     }
     return true;
 }
@@ -747,8 +879,8 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
         any = true;
         orth_norm_kernel<<<a.prep_total, 256, 0, s>>>(a);
         orth_start_kernel<<<a.prep_total, 256, 0, s>>>(a);
-        const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total;
-        orthogonalize_kernel<<<most < (uint32_t)ctas ? most : (uint32_t)ctas, kOrthThreads, kOrthSmem, s>>>(a);
+        const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total, pairs = (uint32_t)ctas / 2u;
+        orthogonalize_kernel<<<2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s>>>(a);
     }
     if (!any) {
         if (workspace_bytes < sizeof(WorkspaceHeader)) return DAF_ERR_CAPACITY;
