@@ -19,8 +19,8 @@
 // (a counter), so a pair that waits only ever waits for tiles that running pairs hold, and the matrices of a call fill one
 // another's gaps.  A pair, because one SM's shared memory cannot feed its tensor core: of a product of 256 x 256 each CTA holds half of
 // either operand.  Roles: the first CTA's warp 0 takes tickets, waits and tells both; warp 0 of each copies its halves of the operands
-// (TMA, a copy of 16 KB for each operand and 64 of the summed dimension: a copy takes some 200 cycles to issue whatever its
-// size, and copies of 8 KB took longer than the products, 0.45 against 0.31 us); the first CTA's warp 1 issues the products (two accumulators in tensor memory); eight warps of each read its half of
+// (TMA, a copy of 16 KB for each operand and 64 of the summed dimension, warp 3 those of the second operand: a copy takes some 200
+// cycles to issue whatever its size, and copies of 8 KB took longer than the products, 0.45 against 0.31 us); the first CTA's warp 1 issues the products (two accumulators in tensor memory); eight warps of each read its half of
 // the result's rows, form the polynomial or the update and store them.
 #include "attention.cuh"
 #include "tensor_core.cuh"
@@ -28,7 +28,7 @@
 namespace daf {
 
 constexpr uint32_t kOrthThreads = 384, kOrthStages = 6, kOrthBox = 8192, kOrthStage = 4u * kOrthBox, kOrthOut = 2048, kOrthRows = 256;
-constexpr uint32_t kOrthGroups = 20, kOrthMatrices = 192, kOrthSlots = 4;
+constexpr uint32_t kOrthGroups = 16, kOrthMatrices = 192, kOrthSlots = 4;
 constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
 constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch: bounds the workspace (8 bytes and more per element)
 constexpr float kHeld = 4096.0f;                // G and P times this
@@ -36,8 +36,10 @@ constexpr uint32_t kPrepUnits = 64;             // pieces of 256 columns of a ro
 
 struct OrthGroup {                              // matrices of one shape and type
     // operands of the products, for each of x's two places: the Gram matrix's (of x), the polynomial's (of G), the update's
-    CUtensorMap gram_a[2], gram_b[2], poly_a, poly_b, upd_x[2], upd_poly;
-    __half *x_at[2], *gram_at, *poly_at;        // [matrix][plane][row][pitch]; x always has two planes
+    // (across: what of a symmetric matrix lies left of its stored half)
+    CUtensorMap gram_a[2], gram_b[2], poly_a, poly_b, poly_a_across, poly_b_across, upd_x[2], upd_poly, upd_poly_across;
+    __half *x_at[2], *gram_at, *poly_at;        // [matrix][plane][row][pitch]; x always has two planes; of the others only tiles that
+                                                // reach the diagonal or lie right of it
     uint64_t x_plane, m_plane;                  // elements of a plane
     uint32_t r, c, m, x_pitch, m_pitch, tall, planes, count, first, dtype;
     uint32_t sym_tiles, sym_cols, upd_tiles, upd_rows, n;   // of one matrix; columns of a tile
@@ -277,6 +279,28 @@ __device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket
     }
 }
 
+// What of a tile's operands lies how: keys, the length of the summed dimension; from which of its elements on an operand is
+// copied along its rows.  Ahead of that it is copied across them, rows summed over: all of x where it stands that way,
+// and of a symmetric matrix the part left of the stored half, whose mirror image lies in the columns of the earlier rows.
+struct OrthOperands {
+    uint32_t keys, along_a, along_b;
+    static __device__ __forceinline__ OrthOperands of(const OrthGroup &g, const OrthTile &t)
+    {
+        OrthOperands o = {g.m, 0u, 0u};
+        if (t.kind == kGram) {
+            o.keys = g.tall ? g.r : g.c;
+            o.along_a = o.along_b = g.tall ? o.keys : 0u;
+        } else {
+            if (t.kind == kPoly || !g.tall) o.along_a = t.row;      // a multiple of 256
+            if (t.kind == kPoly || g.tall) o.along_b = t.col & ~(kOrthRows - 1u);
+            if (t.kind == kUpdate && !g.tall) o.along_b = o.keys;
+        }
+        return o;
+    }
+    __device__ __forceinline__ bool cross_a(uint32_t k) const { return k < along_a; }
+    __device__ __forceinline__ bool cross_b(uint32_t k) const { return k < along_b; }
+};
+
 // Waits, with a limit, until `need` tiles of the matrix are done.
 __device__ __forceinline__ bool wait_tiles(const uint32_t *done, uint32_t need, volatile uint32_t *stop)
 {
@@ -374,20 +398,6 @@ __device__ __forceinline__ void take_away(float (&x)[32], const uint4 (&v)[4])
         }
     }
 }
-// The block's transpose: column c of it, the lanes' rows side by side, to row `col + c`.
-__device__ __forceinline__ void store_transposed(__half *at, uint32_t pitch, uint32_t row, uint32_t col, uint32_t m, uint32_t lane, const uint4 (&v)[4])
-{
-    if (row + lane >= m) return;
-#pragma unroll
-    for (uint32_t p = 0; p < 4u; p++) {
-        const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
-#pragma unroll
-        for (uint32_t i = 0; i < 8u; i++)
-            if (col + 8u * p + i < m)
-                reinterpret_cast<uint16_t *>(at)[(uint64_t)(col + 8u * p + i) * pitch + row + lane] = (uint16_t)(w[i >> 1] >> (16u * (i & 1u)));
-    }
-}
-
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
 {
     extern __shared__ __align__(1024) unsigned char s_raw[];
@@ -413,7 +423,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
         }
         for (uint32_t i = 0; i < kOrthSlots; i++) {
             bar_init(&bars.told[i], 1);
-            bar_init(&bars.heard[i], 18);                           // eight warps of each, the products, the other's copies
+            bar_init(&bars.heard[i], 20);                           // eight warps of each, the products, three copiers
         }
         bar_init(&bars.drain, 1);
         for (uint32_t i = 0; i < 2u; i++) {
@@ -434,13 +444,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
     const uint32_t tmem = bars.tmem;
     volatile uint32_t *const stop = &bars.abort;
 
-    if (warp == 0) {                                               // ---- tickets and copies
+    if (warp == 0 || warp == 3) {                                  // ---- tickets and copies
+        // warp 0 copies the first operand, warp 3 the second; the first CTA's warp 0 also takes tickets and says how many bytes come
         if (lane == 0) {
-            uint32_t ticket = rank == 0 ? atomicAdd(&a.header->ticket, 1u) : 0u, st = 0, ph = 0, issued = 0;
+            const bool second = warp == 3, leads = rank == 0 && !second;
+            uint32_t ticket = leads ? atomicAdd(&a.header->ticket, 1u) : 0u, st = 0, ph = 0, issued = 0;
             for (uint32_t n = 0;; n++) {
                 const uint32_t slot = n % kOrthSlots;
                 OrthTile t;
-                if (rank == 0) {
+                if (leads) {
                     if (n >= kOrthSlots && !wait_from_pair(&bars.heard[slot], (n / kOrthSlots - 1u) & 1u, stop)) break;
                     t = orth_tile(a, ticket);
                     if (t.kind != kNoTile) {
@@ -463,37 +475,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                 const OrthGroup &g = a.g[t.group];
                 asm volatile("fence.proxy.async;" ::: "memory");    // what other CTAs wrote by stores is now read by copies
                 const uint32_t buf = t.step & 1u;
-                const CUtensorMap *ma, *mb;
-                uint32_t keys = g.m, plane_a = g.planes, plane_b = g.planes;   // the summed dimension; planes of a matrix in each map
-                bool cross_a = false, cross_b = false;              // the summed dimension is not the contiguous one
-                if (t.kind == kPoly) {
-                    ma = &g.poly_a;
-                    mb = &g.poly_b;
-                } else if (t.kind == kGram) {
-                    ma = &g.gram_a[buf];
-                    mb = &g.gram_b[buf];
-                    keys = g.tall ? g.r : g.c;
-                    plane_a = plane_b = 2u;
-                    cross_a = cross_b = g.tall;
-                } else {
-                    ma = g.tall ? &g.upd_x[buf] : &g.upd_poly;
-                    mb = g.tall ? &g.upd_poly : &g.upd_x[buf];
-                    (g.tall ? plane_a : plane_b) = 2u;
-                    cross_b = !g.tall;
-                }
-                const int row = (int)(t.row + 128u * rank), col = (int)(t.col + g.n / 2u * rank);
-                const uint32_t bytes = 2u * (2u * kOrthBox + g.n / 128u * kOrthBox);
+                const OrthOperands o = OrthOperands::of(g, t);
+                const int lines = (int)(second ? t.col + g.n / 2u * rank : t.row + 128u * rank);
+                // x, held in two planes, or a symmetric matrix, in as many as the group's products take
+                const bool of_x = t.kind == kGram || (t.kind == kUpdate && second != (g.tall != 0u));
+                const int matrix = (int)(t.matrix * (of_x ? 2u : g.planes));
+                const uint32_t to = smem_u32(stages) + (second ? 2u * kOrthBox : 0u), bytes = 2u * (2u * kOrthBox + g.n / 128u * kOrthBox);
                 bool ok = true;
-                for (int k = 0; k < (int)keys && ok; k += 64)
-                    for (uint32_t part = 0; part < g.planes; part++) {
-                        if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) break;
-                        const uint32_t to = smem_u32(stages + st * kOrthStage), bar = in_cta(&bars.full[st], 0);
-                        if (rank == 0) bar_expect(&bars.full[st], bytes);
-                        pair_load(to, ma, bar, cross_a ? 0 : k, cross_a ? k : row, cross_a ? row / 64 : 0, (int)(t.matrix * plane_a + part));
-                        pair_load(to + 2u * kOrthBox, mb, bar, cross_b ? 0 : k, cross_b ? k : col, cross_b ? col / 64 : 0, (int)(t.matrix * plane_b + part));
-                        issued++;
-                        if (++st == kOrthStages) st = 0, ph ^= 1u;
-                    }
+                const auto copy = [&](const CUtensorMap *map, bool across, int from, int end) {
+                    for (int k = from; k < end; k += 64)
+                        for (uint32_t part = 0; part < g.planes; part++) {
+                            if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) return;
+                            if (leads) bar_expect(&bars.full[st], bytes);
+                            pair_load(to + st * kOrthStage, map, in_cta(&bars.full[st], 0), across ? 0 : k, across ? k : lines, across ? lines / 64 : 0, matrix + (int)part);
+                            issued++;
+                            if (++st == kOrthStages) st = 0, ph ^= 1u;
+                        }
+                };
+                const int along = (int)(second ? o.along_b : o.along_a);
+                const CUtensorMap *map, *map_across;
+                if (t.kind == kPoly) {
+                    map = second ? &g.poly_b : &g.poly_a;
+                    map_across = second ? &g.poly_b_across : &g.poly_a_across;
+                } else if (t.kind == kGram) {
+                    map = map_across = second ? &g.gram_b[buf] : &g.gram_a[buf];
+                } else {
+                    map = of_x ? &g.upd_x[buf] : &g.upd_poly;
+                    map_across = of_x ? &g.upd_x[buf] : &g.upd_poly_across;
+                }
+                copy(map_across, true, 0, along);
+                if (ok) copy(map, false, along, (int)o.keys);
                 if (!ok) break;
             }
             // Nothing may be on its way into shared memory when the CTA ends.  Normally all has long arrived: the products took it.
@@ -516,16 +527,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
             if (n >= 2u && !wait_from_pair(&bars.acc_empty[buf], (n / 2u - 1u) & 1u, stop)) break;
             tmem_after_sync();
             const OrthGroup &g = a.g[t.group];
-            const bool cross_a = t.kind == kGram && g.tall, cross_b = cross_a || (t.kind == kUpdate && !g.tall);
-            const uint32_t keys = t.kind == kGram && g.tall ? g.r : t.kind == kGram ? g.c : g.m;
-            // M = 256: product_desc says 128
-            const uint32_t desc = product_desc(false, g.n, cross_b) + ((256u - 128u) >> 4 << 24) + (cross_a ? 1u << 15 : 0u);
-            const uint32_t step_a = cross_a ? 128u : 2u, step_b = cross_b ? 128u : 2u;         // 16 of the summed dimension, in 16-byte units
-            const uint32_t rounds = (keys + 63u) / 64u, d = tmem + buf * 256u;
+            const OrthOperands o = OrthOperands::of(g, t);
+            const uint32_t plain = product_desc(false, g.n, false) + ((256u - 128u) >> 4 << 24);   // M = 256, where product_desc says 128
+            const uint32_t rounds = (o.keys + 63u) / 64u, d = tmem + buf * 256u;
             bool ok = true;
             for (uint32_t k = 0; k < rounds; k++) {
                 if (!(ok = wait_from_pair(&bars.full[st], ph, stop))) break;
                 tmem_after_sync();
+                // 16 of the summed dimension, in 16-byte units, and which dimension is the contiguous one
+                const bool ca = o.cross_a(k * 64u), cb = o.cross_b(k * 64u);
+                const uint32_t step_a = ca ? 128u : 2u, step_b = cb ? 128u : 2u, desc = plain | (ca ? 1u << 15 : 0u) | (cb ? 1u << 16 : 0u);
                 const uint32_t at = smem_u32(stages + st * kOrthStage);
                 const uint32_t la = operand_low(at, kOrthBox), lb = operand_low(at + 2u * kOrthBox, kOrthBox);
                 pair_product(one, d, la, lb, desc, k > 0);
@@ -648,13 +659,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                                 *reinterpret_cast<const uint16_t *>(stage + r * 64u + (((lane >> 3) ^ (r >> 1 & 3u)) * 16u) + (lane & 7u) * 2u);
                     continue;
                 }
-                // the other half of a symmetric matrix: where no tile of its own covers it
-                const bool mirror = !update && row / g.n < col / kOrthRows * kOrthRows / g.n;
                 const uint32_t planes = g.planes == 2u || (update && t.step < 2u) ? 2u : 1u;
                 for (uint32_t p = 0; p < planes; p++) {
                     round32<__half>(x, w.v);
                     if (p + 1u < planes) take_away(x, w.v);
-                    if (mirror) store_transposed(to + p * plane, pitch, row, col, rows, lane, w.v);
                     w.to_quarters(stage, lane);
                     w.store(to + p * plane, pitch, row, rows, col, pitch, lane);
                 }
@@ -664,7 +672,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
             if (lane == 0) arrive_in(in_cta(&bars.acc_empty[buf], 0));
             if (update && last) continue;                          // nothing waits for the result
             asm volatile("fence.proxy.async;" ::: "memory");
-            __threadfence();
             __syncwarp();
             if (lane == 0) {                                       // each warp for itself: no meeting that one could miss
                 __threadfence();
@@ -816,9 +823,10 @@ static bool orth_place(OrthArgs *a, char *at)
         for (int i = 0; i < 2; i++) g.x_at[i] = take(xs * g.x_plane);
         g.gram_at = take(ms * g.m_plane);
         g.poly_at = take(ms * g.m_plane);
-        bool ok = orth_map(&g.poly_a, g.gram_at, g.m_plane, ms, g.m, g.m, g.m_pitch, false, 128u) &&
-                  orth_map(&g.poly_b, g.gram_at, g.m_plane, ms, g.m, g.m, g.m_pitch, false, half) &&
-                  orth_map(&g.upd_poly, g.poly_at, g.m_plane, ms, g.m, g.m, g.m_pitch, false, g.tall ? half : 128u);
+        const auto square = [&](CUtensorMap *map, __half *p, bool across, uint32_t lines) { return orth_map(map, p, g.m_plane, ms, g.m, g.m, g.m_pitch, across, lines); };
+        bool ok = square(&g.poly_a, g.gram_at, false, 128u) && square(&g.poly_a_across, g.gram_at, true, 128u) && square(&g.poly_b, g.gram_at, false, half) &&
+                  square(&g.poly_b_across, g.gram_at, true, half) && square(&g.upd_poly, g.poly_at, false, g.tall ? half : 128u) &&
+                  square(&g.upd_poly_across, g.poly_at, true, g.tall ? half : 128u);
         for (int i = 0; i < 2 && ok; i++)
             ok = orth_map(&g.gram_a[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, g.tall, 128u) &&
                  orth_map(&g.gram_b[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, g.tall, half) &&
