@@ -60,30 +60,51 @@ struct OrthArgs {
 static_assert(sizeof(OrthArgs) <= 32000, "kernel arguments");
 
 // --------------------------------------------------------------------------------------------- norms, first operands
-__device__ __forceinline__ float orth_get(const void *p, uint32_t dtype, uint64_t i)
-{
-    if (dtype == DAF_F32) return __ldg(reinterpret_cast<const float *>(p) + i);
-    if (dtype == DAF_F16) return __half2float(reinterpret_cast<const __half *>(p)[i]);
-    return __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p)[i]);
-}
-// Eight columns of a row, zero behind its end.
-__device__ __forceinline__ void orth_load8(const OrthGroup &g, const void *p, uint32_t row, uint32_t col, float (&x)[8])
-{
-    const uint32_t eb = g.dtype == DAF_F32 ? 4u : 2u;
-    const uint64_t at = (uint64_t)row * g.c + col;
-    if (g.c % 8u == 0 && reinterpret_cast<uintptr_t>(p) % (8u * eb) == 0 && col < g.c) {
-        if (g.dtype == DAF_F32) Elem<float>::load8(reinterpret_cast<const float *>(p) + at, x);
-        else if (g.dtype == DAF_F16) Elem<__half>::load8(reinterpret_cast<const __half *>(p) + at, x);
-        else Elem<__nv_bfloat16>::load8(reinterpret_cast<const __nv_bfloat16 *>(p) + at, x);
-        return;
-    }
+// Eight columns of a row as they lie in memory, zeros behind its end.
+template <typename T> struct OrthEight {
+    static constexpr int kVectors = (int)sizeof(T) / 2;
+    uint4 v[kVectors];
+    __device__ __forceinline__ void load(const OrthGroup &g, const T *p, uint32_t row, uint32_t col, bool here, bool wide)
+    {
+        const uint64_t at = (uint64_t)row * g.c + col;
 #pragma unroll
-    for (uint32_t e = 0; e < 8u; e++) x[e] = col + e < g.c ? orth_get(p, g.dtype, at + e) : 0.0f;
-}
-// The CTA's matrix and its share of it.
+        for (int i = 0; i < kVectors; i++) v[i] = make_uint4(0, 0, 0, 0);
+        if (!here || col >= g.c) return;
+        if (wide) {
+#pragma unroll
+            for (int i = 0; i < kVectors; i++) v[i] = __ldg(reinterpret_cast<const uint4 *>(p + at) + i);
+            return;
+        }
+        T e[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; i++) e[i] = col + i < g.c ? p[at + i] : T(0.0f);
+#pragma unroll
+        for (int i = 0; i < kVectors; i++) v[i] = *(reinterpret_cast<const uint4 *>(e) + i);
+    }
+    __device__ __forceinline__ void widen(float (&x)[8]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            Elem<T>::widen8(v[0], x);
+        } else {
+            x[0] = __uint_as_float(v[0].x); x[1] = __uint_as_float(v[0].y); x[2] = __uint_as_float(v[0].z); x[3] = __uint_as_float(v[0].w);
+            x[4] = __uint_as_float(v[1].x); x[5] = __uint_as_float(v[1].y); x[6] = __uint_as_float(v[1].z); x[7] = __uint_as_float(v[1].w);
+        }
+    }
+    static __device__ __forceinline__ bool wide(const OrthGroup &g, const void *p)
+    {
+        return g.c % 8u == 0 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+    }
+};
+// The CTA's matrix and its share of it: units, pieces of 256 columns of a row, of which a warp takes kPrepUnits / 8 at a time.
 struct PrepShare {
-    uint32_t group, matrix, cta, cols;          // cta: within the matrix; cols: pieces of 256 columns of a row
-    uint64_t units;
+    uint32_t group, matrix, cta, cols, units;   // cta: within the matrix; cols: units of a row
+    __device__ __forceinline__ bool place(const OrthGroup &g, uint32_t j, uint32_t *row, uint32_t *col) const      // false: no such columns
+    {
+        const uint32_t unit = cta * kPrepUnits + (threadIdx.x >> 5) + 8u * j;
+        *row = cols == 1u ? unit : unit / cols;
+        *col = (unit - *row * cols) * 256u + (threadIdx.x & 31u) * 8u;
+        return unit < units && *col < g.x_pitch;
+    }
 };
 __device__ __forceinline__ PrepShare prep_share(const OrthArgs &a)
 {
@@ -94,7 +115,7 @@ __device__ __forceinline__ PrepShare prep_share(const OrthArgs &a)
     s.matrix = at / g.prep_ctas;
     s.cta = at - s.matrix * g.prep_ctas;
     s.cols = (g.c + 255u) / 256u;
-    s.units = (uint64_t)g.r * s.cols;
+    s.units = g.r * s.cols;                                         // 2^24 at most
     return s;
 }
 __device__ __forceinline__ double cta_sum(double v, double *s_part)
@@ -109,7 +130,32 @@ __device__ __forceinline__ double cta_sum(double v, double *s_part)
     return v;
 }
 
-__global__ void __launch_bounds__(256) orth_norm_kernel(const __grid_constant__ OrthArgs a)
+constexpr uint32_t kPrepFlight = 4;             // units of a warp on their way
+template <typename T> __device__ __forceinline__ double sum_squares(const OrthGroup &g, const PrepShare &s, const void *in)
+{
+    const bool wide = OrthEight<T>::wide(g, in);
+    double sum = 0.0;
+#pragma unroll 1
+    for (uint32_t j0 = 0; j0 < kPrepUnits / 8u; j0 += kPrepFlight) {
+        OrthEight<T> v[kPrepFlight];
+#pragma unroll
+        for (uint32_t j = 0; j < kPrepFlight; j++) {
+            uint32_t row, col;
+            const bool here = s.place(g, j0 + j, &row, &col);
+            v[j].load(g, static_cast<const T *>(in), row, col, here, wide);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kPrepFlight; j++) {
+            float x[8];
+            v[j].widen(x);
+#pragma unroll
+            for (int e = 0; e < 8; e++) sum = fma((double)x[e], (double)x[e], sum);
+        }
+    }
+    return sum;
+}
+
+__global__ void __launch_bounds__(256, 5) orth_norm_kernel(const __grid_constant__ OrthArgs a)
 {
     __shared__ double s_part[8];
     if (blockIdx.x == 0) {
@@ -122,50 +168,64 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const __grid_constant__ 
     const PrepShare s = prep_share(a);
     const OrthGroup &g = a.g[s.group];
     const void *in = a.in[g.first + s.matrix];
-    const uint32_t lane = threadIdx.x & 31u;
-    double sum = 0.0;
-    for (uint32_t j = threadIdx.x >> 5; j < kPrepUnits; j += 8u) {
-        const uint64_t unit = (uint64_t)s.cta * kPrepUnits + j;
-        const uint32_t row = (uint32_t)(unit / s.cols), col = (uint32_t)(unit - (uint64_t)row * s.cols) * 256u + lane * 8u;
-        if (unit >= s.units || col >= g.c) continue;
-        float x[8];
-        orth_load8(g, in, row, col, x);
-#pragma unroll
-        for (int e = 0; e < 8; e++) sum = fma((double)x[e], (double)x[e], sum);
-    }
+    double sum = g.dtype == DAF_F32 ? sum_squares<float>(g, s, in) : g.dtype == DAF_F16 ? sum_squares<__half>(g, s, in) : sum_squares<__nv_bfloat16>(g, s, in);
     sum = cta_sum(sum, s_part);
     if (threadIdx.x == 0) a.partial[blockIdx.x] = sum;
 }
 
-__global__ void __launch_bounds__(256) orth_start_kernel(const __grid_constant__ OrthArgs a)
+template <typename T> __device__ __forceinline__ void first_operand(const OrthArgs &a, const OrthGroup &g, const PrepShare &s, double *s_part)
+{
+    const T *in = static_cast<const T *>(a.in[g.first + s.matrix]);
+    const bool wide = OrthEight<T>::wide(g, in);
+    const double *parts = a.partial + g.prep_first + s.matrix * g.prep_ctas;
+    __half *hi = g.x_at[0] + (uint64_t)s.matrix * 2u * g.x_plane, *lo = hi + g.x_plane;
+    float by = 0.0f, by2 = 0.0f;
+#pragma unroll 1
+    for (uint32_t j0 = 0; j0 < kPrepUnits / 8u; j0 += kPrepFlight) {
+        OrthEight<T> v[kPrepFlight];                                // on their way while the norm is summed up
+#pragma unroll
+        for (uint32_t j = 0; j < kPrepFlight; j++) {
+            uint32_t row, col;
+            const bool here = s.place(g, j0 + j, &row, &col);
+            v[j].load(g, in, row, col, here, wide);
+        }
+        if (j0 == 0) {
+            double sum = 0.0;
+#pragma unroll 4
+            for (uint32_t i = threadIdx.x; i < g.prep_ctas; i += 256u) sum += parts[i];
+            const double norm = sqrt(cta_sum(sum, s_part)) + (double)a.eps;
+            const bool finite = norm - norm == 0.0;
+            const int up = finite ? 12 - ilogb(norm) : 0;
+            if (s.cta == 0 && threadIdx.x == 0) a.scale[g.first + s.matrix] = finite ? (float)scalbn(norm, up) : __int_as_float(0x7FC00000);
+            // 2^up as two factors that binary32 holds
+            by = finite ? scalbnf(1.0f, up / 2) : __int_as_float(0x7FC00000);
+            by2 = scalbnf(1.0f, up - up / 2);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kPrepFlight; j++) {
+            uint32_t row, col;
+            if (!s.place(g, j0 + j, &row, &col)) continue;          // columns up to the pitch: products read the zeros behind the end
+            float x[8], rest[8];
+            v[j].widen(x);
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                x[e] = x[e] * by * by2;
+                rest[e] = x[e] - __half2float(__float2half_rn(x[e]));
+            }
+            Elem<__half>::store8(hi + (uint64_t)row * g.x_pitch + col, x);
+            if (g.planes == 2u) Elem<__half>::store8(lo + (uint64_t)row * g.x_pitch + col, rest);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256, 5) orth_start_kernel(const __grid_constant__ OrthArgs a)
 {
     __shared__ double s_part[8];
     const PrepShare s = prep_share(a);
     const OrthGroup &g = a.g[s.group];
-    const uint32_t lane = threadIdx.x & 31u;
-    const double *parts = a.partial + g.prep_first + s.matrix * g.prep_ctas;
-    double sum = 0.0;
-    for (uint32_t i = threadIdx.x; i < g.prep_ctas; i += 256u) sum += parts[i];
-    const double norm = sqrt(cta_sum(sum, s_part)) + (double)a.eps;
-    const bool finite = norm - norm == 0.0;
-    const int up = finite ? 12 - ilogb(norm) : 0;
-    if (s.cta == 0 && threadIdx.x == 0) a.scale[g.first + s.matrix] = finite ? (float)scalbn(norm, up) : __int_as_float(0x7FC00000);
-    const void *in = a.in[g.first + s.matrix];
-    __half *hi = g.x_at[0] + (uint64_t)s.matrix * 2u * g.x_plane, *lo = hi + g.x_plane;
-    for (uint32_t j = threadIdx.x >> 5; j < kPrepUnits; j += 8u) {
-        const uint64_t unit = (uint64_t)s.cta * kPrepUnits + j;
-        const uint32_t row = (uint32_t)(unit / s.cols), col = (uint32_t)(unit - (uint64_t)row * s.cols) * 256u + lane * 8u;
-        if (unit >= s.units || col >= g.x_pitch) continue;             // zeros behind the end: products read them
-        float x[8], rest[8];
-        orth_load8(g, in, row, col, x);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            x[e] = finite ? scalbnf(x[e], up) : __int_as_float(0x7FC00000);
-            rest[e] = x[e] - __half2float(__float2half_rn(x[e]));
-        }
-        Elem<__half>::store8(hi + (uint64_t)row * g.x_pitch + col, x);
-        if (g.planes == 2u) Elem<__half>::store8(lo + (uint64_t)row * g.x_pitch + col, rest);
-    }
+    if (g.dtype == DAF_F32) first_operand<float>(a, g, s, s_part);
+    else if (g.dtype == DAF_F16) first_operand<__half>(a, g, s, s_part);
+    else first_operand<__nv_bfloat16>(a, g, s, s_part);
 }
 
 // --------------------------------------------------------------------------------------------- the products
@@ -718,6 +778,10 @@ static uint32_t orth_sym_tiles(uint32_t m, uint32_t width)
 static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t n, const uint32_t *dtypes, const uint64_t *rows, const uint64_t *cols,
                        uint32_t *next, uint32_t *index, uint64_t *workspace)
 {
+    struct Shape {
+        uint32_t r, c, dtype, count, rank;
+        bool ahead(const Shape &o) const { return (r > c ? r : c) > (o.r > o.c ? o.r : o.c); }
+    } shape[kOrthGroups];
     uint32_t group_of[kOrthMatrices], taken[kOrthMatrices];
     uint64_t elems = 0;
     a->groups = a->matrices = 0;
@@ -726,27 +790,31 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
         if (r == 0 || c == 0) continue;
         if (elems && elems + (uint64_t)r * c > kOrthBatch) break;
         uint32_t k = 0;
-        while (k < a->groups && (a->g[k].r != r || a->g[k].c != c || a->g[k].dtype != dtypes[i])) k++;
+        while (k < a->groups && (shape[k].r != r || shape[k].c != c || shape[k].dtype != dtypes[i])) k++;
         if (k == kOrthGroups) break;
-        OrthGroup &g = a->g[k];
-        if (k == a->groups) {
-            a->groups++;
-            g.r = r;
-            g.c = c;
-            g.dtype = dtypes[i];
-            g.count = 0;
-        }
-        g.count++;
+        if (k == a->groups) shape[a->groups++] = {r, c, dtypes[i], 0u, 0u};
+        shape[k].count++;
         group_of[a->matrices] = k;
         taken[a->matrices++] = i;
         elems += (uint64_t)r * c;
     }
+    // Longest side first: the Gram matrix's tiles take as long as that is, and what waits for the last of them waits least so (two
+    // blocks of width 2048: a tenth of the time).
     uint32_t first[kOrthGroups], at = 0;
+    for (uint32_t k = 0; k < a->groups; k++)
+        for (uint32_t j = 0; j < a->groups; j++) shape[k].rank += shape[j].ahead(shape[k]) || (j < k && !shape[k].ahead(shape[j]));
+    for (uint32_t k = 0; k < a->groups; k++) {
+        OrthGroup &g = a->g[shape[k].rank];
+        g.r = shape[k].r;
+        g.c = shape[k].c;
+        g.dtype = shape[k].dtype;
+        g.count = shape[k].count;
+    }
     for (uint32_t k = 0; k < a->groups; k++) {
         a->g[k].first = first[k] = at;
         at += a->g[k].count;
     }
-    for (uint32_t i = 0; i < a->matrices; i++) index[first[group_of[i]]++] = taken[i];
+    for (uint32_t i = 0; i < a->matrices; i++) index[first[shape[group_of[i]].rank]++] = taken[i];
     a->steps = p->steps;
     a->a = p->coefficients[0];
     a->b = p->coefficients[1];
