@@ -18,7 +18,7 @@
 // in which whatever a tile needs comes before it; a tile waits until its matrix's tiles of the earlier products are done
 // (a counter), so a pair that waits only ever waits for tiles that running pairs hold, and the matrices of a call fill one
 // another's gaps.  A pair, because one SM's shared memory cannot feed its tensor core: of a product of 256 x 256 each CTA holds half of
-// either operand.  Roles: the first CTA's warp 0 takes tickets, waits and tells both; warp 0 of each copies its halves of the operands
+// either operand.  Roles: the first CTA's warp 2 takes tickets, waits and tells both; warp 0 of each copies its halves of the operands
 // (TMA, a copy of 16 KB for each operand and 64 of the summed dimension, warp 3 those of the second operand: a copy takes some 200
 // cycles to issue whatever its size, and copies of 8 KB took longer than the products, 0.45 against 0.31 us); the first CTA's warp 1 issues the products (two accumulators in tensor memory); eight warps of each read its half of
 // the result's rows, form the polynomial or the update and store them.
@@ -28,7 +28,7 @@
 namespace daf {
 
 constexpr uint32_t kOrthThreads = 384, kOrthStages = 6, kOrthBox = 8192, kOrthStage = 4u * kOrthBox, kOrthOut = 2048, kOrthRows = 256;
-constexpr uint32_t kOrthGroups = 16, kOrthMatrices = 192, kOrthSlots = 4;
+constexpr uint32_t kOrthGroups = 16, kOrthMatrices = 192, kOrthSlots = 2;
 constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
 constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch: bounds the workspace (8 bytes and more per element)
 constexpr float kHeld = 4096.0f;                // G and P times this
@@ -483,7 +483,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
         }
         for (uint32_t i = 0; i < kOrthSlots; i++) {
             bar_init(&bars.told[i], 1);
-            bar_init(&bars.heard[i], 20);                           // eight warps of each, the products, three copiers
+            bar_init(&bars.heard[i], 21);                           // eight warps of each, the products, four copiers
         }
         bar_init(&bars.drain, 1);
         for (uint32_t i = 0; i < 2u; i++) {
@@ -504,33 +504,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
     const uint32_t tmem = bars.tmem;
     volatile uint32_t *const stop = &bars.abort;
 
-    if (warp == 0 || warp == 3) {                                  // ---- tickets and copies
-        // warp 0 copies the first operand, warp 3 the second; the first CTA's warp 0 also takes tickets and says how many bytes come
+    if (warp == 2 && rank == 0) {                                  // ---- tickets, one tile ahead of the copies
         if (lane == 0) {
-            const bool second = warp == 3, leads = rank == 0 && !second;
-            uint32_t ticket = leads ? atomicAdd(&a.header->ticket, 1u) : 0u, st = 0, ph = 0, issued = 0;
+            uint32_t ticket = atomicAdd(&a.header->ticket, 1u);
             for (uint32_t n = 0;; n++) {
                 const uint32_t slot = n % kOrthSlots;
-                OrthTile t;
-                if (leads) {
-                    if (n >= kOrthSlots && !wait_from_pair(&bars.heard[slot], (n / kOrthSlots - 1u) & 1u, stop)) break;
-                    t = orth_tile(a, ticket);
-                    if (t.kind != kNoTile) {
-                        ticket = atomicAdd(&a.header->ticket, 1u);
-                        const OrthGroup &g = a.g[t.group];
-                        const uint32_t need = 16u * (t.step * (2u * g.sym_tiles + g.upd_tiles) + t.kind * g.sym_tiles);
-                        if (need && !wait_tiles(a.done + g.first + t.matrix, need, stop)) break;
-                    }
-                    const uint4 v = t.packed();
-                    bars.tile[slot] = v;
-                    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(in_cta(&bars.tile[slot], 1)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-                    bar_arrive(&bars.told[slot]);
-                    arrive_in(in_cta(&bars.told[slot], 1));
-                } else {
-                    if (!wait_from_pair(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
-                    t = OrthTile::from(bars.tile[slot]);
-                    arrive_in(in_cta(&bars.heard[slot], 0));
+                const OrthTile t = orth_tile(a, ticket);
+                if (n >= kOrthSlots && !wait_from_pair(&bars.heard[slot], (n / kOrthSlots - 1u) & 1u, stop)) break;
+                if (t.kind != kNoTile) {
+                    ticket = atomicAdd(&a.header->ticket, 1u);
+                    const OrthGroup &g = a.g[t.group];
+                    const uint32_t need = 16u * (t.step * (2u * g.sym_tiles + g.upd_tiles) + t.kind * g.sym_tiles);
+                    if (need && !wait_tiles(a.done + g.first + t.matrix, need, stop)) break;
                 }
+                const uint4 v = t.packed();
+                bars.tile[slot] = v;
+                asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(in_cta(&bars.tile[slot], 1)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                bar_arrive(&bars.told[slot]);
+                arrive_in(in_cta(&bars.told[slot], 1));
+                if (t.kind == kNoTile) break;
+            }
+        }
+    } else if (warp == 0 || warp == 3) {                           // ---- copies: warp 0 the first operand's, warp 3 the second's
+        if (lane == 0) {
+            const bool second = warp == 3, counts = rank == 0 && !second;       // counts: says how many bytes come
+            uint32_t st = 0, ph = 0, issued = 0;
+            for (uint32_t n = 0;; n++) {
+                const uint32_t slot = n % kOrthSlots;
+                if (!wait_from_pair(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
+                const OrthTile t = OrthTile::from(bars.tile[slot]);
+                arrive_in(in_cta(&bars.heard[slot], 0));
                 if (t.kind == kNoTile) break;
                 const OrthGroup &g = a.g[t.group];
                 asm volatile("fence.proxy.async;" ::: "memory");    // what other CTAs wrote by stores is now read by copies
@@ -546,7 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                     for (int k = from; k < end; k += 64)
                         for (uint32_t part = 0; part < g.planes; part++) {
                             if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) return;
-                            if (leads) bar_expect(&bars.full[st], bytes);
+                            if (counts) bar_expect(&bars.full[st], bytes);
                             pair_load(to + st * kOrthStage, map, in_cta(&bars.full[st], 0), across ? 0 : k, across ? k : lines, across ? lines / 64 : 0, matrix + (int)part);
                             issued++;
                             if (++st == kOrthStages) st = 0, ph ^= 1u;
