@@ -139,36 +139,61 @@ struct SortShared {
     uint32_t unknown;
 };
 
-// Zeros from byte `from` to `to`, by `threads` threads.
-__device__ void fill_zeros(char *at, uint64_t bytes, uint64_t thread, uint64_t threads)
+// Zeros to `bytes` bytes, by CTA `cta` of `ctas`: copies of a zeroed piece of shared memory, which keep the memory busier than the
+// threads' own stores, and those for what lies off the copies' boundaries.
+constexpr uint32_t kFillPiece = 32768;
+__device__ void fill_zeros(char *at, uint64_t bytes, unsigned char *zeros, uint32_t cta, uint32_t ctas)
 {
-    const uint64_t off = (32u - (reinterpret_cast<uintptr_t>(at) & 31u)) & 31u, head = off < bytes ? off : bytes;
-    const uint64_t units = (bytes - head) / 32u, tail = head + units * 32u;
-    const float none[8] = {};
-    for (uint64_t u = thread; u < units; u += threads) Elem<float>::store8(at + head + u * 32u, none);
-    if (thread < head / 2u) reinterpret_cast<uint16_t *>(at)[thread] = 0;
-    if (thread < (bytes - tail) / 2u) reinterpret_cast<uint16_t *>(at + tail)[thread] = 0;
+    for (uint32_t i = threadIdx.x; i < kFillPiece / 16u; i += kSortThreads) reinterpret_cast<uint4 *>(zeros)[i] = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    const uint64_t off = (16u - (reinterpret_cast<uintptr_t>(at) & 15u)) & 15u, head = off < bytes ? off : bytes;
+    const uint64_t middle = (bytes - head) & ~15ull, tail = head + middle;
+    if (cta == 0) {
+        if (threadIdx.x < head / 2u) reinterpret_cast<uint16_t *>(at)[threadIdx.x] = 0;
+        if (threadIdx.x < (bytes - tail) / 2u) reinterpret_cast<uint16_t *>(at + tail)[threadIdx.x] = 0;
+    }
+    if (threadIdx.x) return;
+    for (uint64_t piece = (uint64_t)cta * kFillPiece; piece < middle; piece += (uint64_t)ctas * kFillPiece) {
+        const uint32_t n = middle - piece < kFillPiece ? (uint32_t)(middle - piece) : kFillPiece;
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                     ::"l"(at + head + piece), "r"((uint32_t)__cvta_generic_to_shared(zeros)), "r"(n) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group 4;" ::: "memory");
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
-// One round of a warp: the lanes' digits, where each one's item lies among those of the digit in this warp so far, and the
-// count moved on.  Lanes without an item take part with a digit of their own.
-__device__ __forceinline__ uint32_t place_in_warp(uint32_t *count, uint32_t digit, bool item, uint32_t lane)
+// The lanes with the same digit as this one, among those with an item, from a vote on each bit (one instruction that compares all
+// lanes takes the distinct digits one after the other: 131072 tokens 99 us instead of the 45 of the votes).
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, uint32_t bits, uint32_t items)
 {
-    const uint32_t same = __match_any_sync(0xffffffffu, item ? digit : kDigits + lane);
-    const uint32_t before = item ? count[digit] : 0u;
+    uint32_t same = items;
+#pragma unroll
+    for (uint32_t b = 0; b < kDigitBits; b++) {
+        if (b >= bits) break;
+        const uint32_t set = __ballot_sync(0xffffffffu, digit >> b & 1u);
+        same &= digit >> b & 1u ? set : ~set;
+    }
+    return same;
+}
+// One round of a warp: where each lane's item lies among those of the digit in this warp so far, and the count moved on.
+__device__ __forceinline__ uint32_t place_in_warp(uint32_t *count, uint32_t digit, uint32_t bits, bool item, uint32_t lane)
+{
+    const uint32_t same = same_digit(digit, bits, __ballot_sync(0xffffffffu, item));
+    const uint32_t below = __popc(same & ((1u << lane) - 1u)), before = item ? count[digit] : 0u;
     __syncwarp();
-    if (item && (same & ((1u << lane) - 1u)) == 0u) count[digit] = before + __popc(same);
+    if (item && below == 0u) count[digit] = before + __popc(same);
     __syncwarp();
-    return before + __popc(same & ((1u << lane) - 1u));
+    return before + below;
 }
 
 __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads) embedding_sort_kernel(const __grid_constant__ EmbeddingArgs a, uint32_t table_bytes)
 {
-    extern __shared__ __align__(16) unsigned char raw[];
+    extern __shared__ __align__(128) unsigned char raw[];
     SortShared &s = *reinterpret_cast<SortShared *>(raw);
     if (blockIdx.x >= kSortCtas) {
-        fill_zeros(reinterpret_cast<char *>(a.grad_weight), a.table_elems * table_bytes, (uint64_t)(blockIdx.x - kSortCtas) * kSortThreads + threadIdx.x,
-                   (uint64_t)(gridDim.x - kSortCtas) * kSortThreads);
+        fill_zeros(reinterpret_cast<char *>(a.grad_weight), a.table_elems * table_bytes, raw, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
         return;
     }
     const uint32_t rank = cluster_rank(), lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, digits = 1u << a.digit_bits;
@@ -206,7 +231,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
             }
 #pragma unroll
             for (uint32_t j = 0; j < 4; j++)
-                if (at + j * 32u < end) place_in_warp(s.count[warp], key[j] >> shift & (digits - 1u), at + j * 32u + lane < end, lane);
+                if (at + j * 32u < end) place_in_warp(s.count[warp], key[j] >> shift & (digits - 1u), a.digit_bits, at + j * 32u + lane < end, lane);
         }
         if (unknown) s.unknown = 1;
         __syncthreads();
@@ -257,7 +282,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
                 if (at + j * 32u >= end) break;
                 const bool item = at + j * 32u + lane < end;
                 const uint32_t digit = key[j] >> shift & (digits - 1u);
-                const uint32_t p = place_in_warp(s.count[warp], digit, item, lane) + s.base[digit];
+                const uint32_t p = place_in_warp(s.count[warp], digit, a.digit_bits, item, lane) + s.base[digit];
                 if (item) {
                     a.keys[to][p] = key[j];
                     a.places[to][p] = place[j];
@@ -276,8 +301,50 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
 }
 
 // --------------------------------------------------------------------------------------------- backward: the sums
-template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) embedding_sum_kernel(const __grid_constant__ EmbeddingArgs a)
+// Rows of a chunk on their way, VEC: two blocks of them lie in shared memory, every thread's part in places of its own, so that
+// rows on their way take no registers; else in registers, a block at a time.
+constexpr uint32_t kSumBytes = 256;             // of a thread, for both blocks
+template <typename A, bool VEC> struct RowBlock {
+    static constexpr int kRows = VEC ? (int)(kSumBytes / 2u / (8u * sizeof(A))) : 8, kAccesses = (int)sizeof(A) / 2;
+    uint32_t place;                             // of the thread's first 16 bytes
+    float x[VEC ? 1 : kRows][8];
+    __device__ __forceinline__ void fetch(int half, int j, const A *row, uint32_t first, uint32_t lanes, uint32_t width)
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < kAccesses; i++)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + ((half * kRows + j) * kAccesses + i) * kRowThreads * 16u),
+                             "l"(reinterpret_cast<const char *>(row + first) + 16 * i) : "memory");
+        } else {
+            load_columns<A, false>(row, first, lanes, width, x[j]);
+        }
+    }
+    __device__ __forceinline__ void take(int half, int j, float (&y)[8]) const
+    {
+        if constexpr (VEC) {
+            uint4 v[kAccesses];
+#pragma unroll
+            for (int i = 0; i < kAccesses; i++)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                             : "r"(place + ((half * kRows + j) * kAccesses + i) * kRowThreads * 16u) : "memory");
+            if constexpr (sizeof(A) == 2) {
+                Elem<A>::widen8(v[0], y);
+            } else {
+                y[0] = __uint_as_float(v[0].x); y[1] = __uint_as_float(v[0].y); y[2] = __uint_as_float(v[0].z); y[3] = __uint_as_float(v[0].w);
+                y[4] = __uint_as_float(v[1].x); y[5] = __uint_as_float(v[1].y); y[6] = __uint_as_float(v[1].z); y[7] = __uint_as_float(v[1].w);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) y[e] = x[j][e];
+        }
+    }
+};
+
+template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads, VEC ? 3 : 2) embedding_sum_kernel(const __grid_constant__ EmbeddingArgs a)
 {
+    extern __shared__ __align__(128) unsigned char raw[];
+    using Block = RowBlock<A, VEC>;
+    constexpr int kRows = Block::kRows;
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u);
     const uint64_t item = (uint64_t)blockIdx.x * (kRowThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
     if (item >= (uint64_t)a.n_chunks * a.slabs) return;
@@ -304,20 +371,43 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
         for (int e = 0; e < 8; e++) y[e] = acc[e] * a.scale;
         store_columns<W, VEC>(reinterpret_cast<W *>(a.grad_weight) + (uint64_t)run * a.width, col, lanes, a.width, y);
     };
-    for (uint32_t i = 0; i < a.chunk; i += 8u) {
-        uint32_t key[8], place[8];
+    Block block;
+    block.place = (uint32_t)__cvta_generic_to_shared(raw) + threadIdx.x * 16u;
+    uint32_t key[kRows], next[kRows];
+    const auto list = [](const uint32_t *from, uint32_t (&to)[kRows]) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            *reinterpret_cast<uint4 *>(key + 4 * h) = __ldg(reinterpret_cast<const uint4 *>(keys + i) + h);
-            *reinterpret_cast<uint4 *>(place + 4 * h) = __ldg(reinterpret_cast<const uint4 *>(places + i) + h);
-        }
+        for (int h = 0; h < kRows; h += 4) *reinterpret_cast<uint4 *>(to + h) = __ldg(reinterpret_cast<const uint4 *>(from + h));
+    };
+    const auto fetch = [&](uint32_t i, int half) {                  // the rows of next, from place i of the chunk on
+        uint32_t place[kRows];
+        list(places + i, place);
+#pragma unroll
+        for (int j = 0; j < kRows; j++)
+            if (mine && next[j] != none) block.fetch(half, j, grad + (uint64_t)place[j] * a.width, col, lanes, a.width);
+    };
+    list(keys, next);
+    if (VEC) {
+        fetch(0, 0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    int half = 0;
+    for (uint32_t i = 0; i < a.chunk; i += kRows) {
+#pragma unroll
+        for (int j = 0; j < kRows; j++) key[j] = next[j];
         if (key[0] == none) break;
-        float x[8][8];
+        if (VEC) {
+            if (i + kRows < a.chunk) {
+                list(keys + i + kRows, next);
+                fetch(i + kRows, half ^ 1);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            fetch(i, 0);
+            if (i + kRows < a.chunk) list(keys + i + kRows, next);
+        }
 #pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (mine && key[j] != none) load_columns<A, VEC>(grad + (uint64_t)place[j] * a.width, col, lanes, a.width, x[j]);
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
+        for (int j = 0; j < kRows; j++) {
             if (key[j] != run) {
                 finish(false);
                 run = key[j];
@@ -325,11 +415,16 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
 #pragma unroll
                 for (int e = 0; e < 8; e++) acc[e] = 0.0f;
             }
-            if (mine && run != none)
+            if (mine && run != none) {
+                float y[8];
+                block.take(half, j, y);
 #pragma unroll
-                for (int e = 0; e < 8; e++) acc[e] += x[j][e];
+                for (int e = 0; e < 8; e++) acc[e] += y[e];
+            }
         }
+        half ^= 1;
     }
+    if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
     const bool goes_on = run != none && run == behind;
     finish(goes_on);
     if (goes_on && !open && slab == 0 && lane == 0) a.jobs[1u + atomicAdd(a.jobs, 1u)] = chunk;
@@ -454,27 +549,33 @@ static bool wide(const EmbeddingArgs &a, const void *x, uint32_t dx, const void 
 }
 static bool on_elements(const void *p, uint32_t bytes) { return p && reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
-template <typename W, typename A, bool VEC> static void forward(const EmbeddingArgs &a, cudaStream_t s)
+template <typename W, typename A, bool VEC> static daf_status forward(const EmbeddingArgs &a, cudaStream_t s)
 {
     const uint64_t items = a.n * ((a.slabs + kForwardSlabs - 1u) / kForwardSlabs), per_cta = kRowThreads >> a.lanes_log2;
     const uint64_t ctas = (items + per_cta - 1u) / per_cta;
     embedding_kernel<W, A, VEC><<<(uint32_t)(ctas < (1u << 30) ? ctas : 1u << 30), kRowThreads, 0, s>>>(a);
+    return DAF_OK;
 }
-template <typename W, typename A, bool VEC> static void backward(const EmbeddingArgs &a, cudaStream_t s)
+template <typename W, typename A, bool VEC> static daf_status backward(const EmbeddingArgs &a, cudaStream_t s)
 {
     const uint64_t items = (uint64_t)a.n_chunks * a.slabs, per_cta = kRowThreads >> a.lanes_log2;
-    embedding_sum_kernel<A, W, VEC><<<(uint32_t)((items + per_cta - 1u) / per_cta), kRowThreads, 0, s>>>(a);
+    const auto sum = &embedding_sum_kernel<A, W, VEC>;
+    const uint32_t smem = VEC ? kSumBytes * kRowThreads : 0u;
+    int ctas = 0;                                                   // also raises the kernel's limit of shared memory
+    if (persistent_ctas(reinterpret_cast<const void *>(sum), (int)kRowThreads, (int)smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    sum<<<(uint32_t)((items + per_cta - 1u) / per_cta), kRowThreads, smem, s>>>(a);
     const uint64_t most = (uint64_t)a.n_chunks * ((a.pitch + 255u) / 256u);
     embedding_join_kernel<W, VEC><<<(uint32_t)(most < 148u * 4u ? most : 148u * 4u), kRowThreads, 0, s>>>(a);
+    return DAF_OK;
 }
-template <bool BACK, bool VEC> static void by_type(uint32_t table, uint32_t act, const EmbeddingArgs &a, cudaStream_t s)
+template <bool BACK, bool VEC> static daf_status by_type(uint32_t table, uint32_t act, const EmbeddingArgs &a, cudaStream_t s)
 {
 #define DAF_EMBEDDING(W, A) (BACK ? backward<W, A, VEC>(a, s) : forward<W, A, VEC>(a, s))
-    if (table == DAF_F16) DAF_EMBEDDING(__half, __half);
-    else if (table == DAF_BF16) DAF_EMBEDDING(__nv_bfloat16, __nv_bfloat16);
-    else if (act == DAF_F16) DAF_EMBEDDING(float, __half);
-    else if (act == DAF_BF16) DAF_EMBEDDING(float, __nv_bfloat16);
-    else DAF_EMBEDDING(float, float);
+    if (table == DAF_F16) return DAF_EMBEDDING(__half, __half);
+    if (table == DAF_BF16) return DAF_EMBEDDING(__nv_bfloat16, __nv_bfloat16);
+    if (act == DAF_F16) return DAF_EMBEDDING(float, __half);
+    if (act == DAF_BF16) return DAF_EMBEDDING(float, __nv_bfloat16);
+    return DAF_EMBEDDING(float, float);
 #undef DAF_EMBEDDING
 }
 
@@ -495,9 +596,9 @@ extern "C" daf_status daf_embedding(const daf_embedding_params *params, const vo
     a.out = d_out;
     if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (wide(a, d_weight, params->table_dtype, d_out, params->dtype)) by_type<false, true>(params->table_dtype, params->dtype, a, s);
-    else by_type<false, false>(params->table_dtype, params->dtype, a, s);
-    return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+    const daf_status ran = wide(a, d_weight, params->table_dtype, d_out, params->dtype) ? by_type<false, true>(params->table_dtype, params->dtype, a, s)
+                                                                                       : by_type<false, false>(params->table_dtype, params->dtype, a, s);
+    return ran != DAF_OK ? ran : cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 
 extern "C" uint64_t daf_embedding_grad_workspace(const daf_embedding_params *params)
@@ -537,8 +638,9 @@ extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, con
     const uint64_t bytes = a.table_elems * eb, clusters = (bytes + (1u << 19) - 1u) >> 19;    // 64 KiB to a CTA
     embedding_sort_kernel<<<kSortCtas * (uint32_t)(1u + (clusters < 17u ? clusters : 17u)), kSortThreads, sizeof(SortShared), s>>>(a, eb);
     if (a.n) {
-        if (wide(a, d_grad_out, p.dtype, d_grad_weight, p.table_dtype)) by_type<true, true>(p.table_dtype, p.dtype, a, s);
-        else by_type<true, false>(p.table_dtype, p.dtype, a, s);
+        const daf_status ran = wide(a, d_grad_out, p.dtype, d_grad_weight, p.table_dtype) ? by_type<true, true>(p.table_dtype, p.dtype, a, s)
+                                                                                         : by_type<true, false>(p.table_dtype, p.dtype, a, s);
+        if (ran != DAF_OK) return ran;
     }
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
