@@ -287,6 +287,27 @@ daf_status make_plan(const daf_params *p, Plan *plan);
 // (kernel, device) pair and are remembered per pair; safe to call from several host threads.
 cudaError_t persistent_ctas(const void *kernel, int threads, int dyn_smem, int *ctas);
 
+// A kernel that may be set up while the one ahead of it in the stream still runs, for chains of small launches (saves 1 to 2 us each): the
+// one ahead says next_may_start() early, this one says wait_for_ahead() before it touches memory; behind that everything the
+// other wrote is there.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, uint32_t smem, cudaStream_t s, const Args &...args)
+{
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = block;
+    config.dynamicSmemBytes = smem;
+    config.stream = s;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, Params(args)...);
+}
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_ahead() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // The current device's word for daf_device_status (nullptr if there is none to be had).
 unsigned int *device_status_word();
 // A kernel's error: in its workspace and, for callers who have let go of that, in the device's word.

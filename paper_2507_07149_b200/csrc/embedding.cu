@@ -6,27 +6,27 @@
 //
 // Backward: the sum of a row's tokens runs in the order of the tokens, in binary32 and without atomics on floats, so the
 // same inputs give the same bits.  Three launches:
-//   embedding_sort_kernel  one cluster of eight CTAs sorts (token, position) by token, keeping the order of positions: a radix
+//   embedding_sort_kernel  one cluster of sixteen CTAs sorts (token, position) by token, keeping the order of positions: a radix
 //                          sort with digits of at most nine bits, whose histograms the CTAs read from one another's shared memory.
-//                          The other clusters meanwhile write the zeros of the whole gradient, so the sort costs time only
-//                          where it takes longer than that.
+//                          The other clusters meanwhile write zeros to the first rows of the gradient, as many as that takes.
 //   embedding_sum_kernel   the sorted list is cut into chunks of equal length; a run of equal tokens inside a chunk is summed and
 //                          written, the part of one that crosses a chunk's border goes to the workspace.  Equal
-//                          chunks keep the SMs evenly busy however often one token occurs.
+//                          chunks keep the SMs evenly busy however often one token occurs.  CTAs among these write zeros to the
+//                          other rows that no token names, so that reads and writes share the memory.
 //   embedding_join_kernel  the parts of a run that crosses borders are added up, in order.
-// Bound: HBM, grad_out read once and the table's gradient written once (rows that occur: twice).
+// Bound: HBM, grad_out read once and the table's gradient written once (named rows among the first: twice).
 #include "common.cuh"
 
 namespace daf {
 
-constexpr uint32_t kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigitBits = 9, kDigits = 1u << kDigitBits;
+constexpr uint32_t kSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigitBits = 9, kDigits = 1u << kDigitBits;
 constexpr uint32_t kRowThreads = 256;
 constexpr uint32_t kLaneCols = 8;               // columns of a lane
 
 struct EmbeddingArgs {
     const void *tokens, *weight, *grad_out;
     void *out, *grad_weight;
-    uint64_t n, table_elems;
+    uint64_t n;
     uint32_t wide_tokens, vocabulary, width, lanes_log2, slabs;   // lanes of a row, slabs of 8 * lanes columns
     float scale;
     long long padding;
@@ -34,6 +34,7 @@ struct EmbeddingArgs {
     uint32_t *keys[2], *places[2], *jobs;       // jobs[0]: how many; then the chunks in which a run that crosses a border begins
     float *part;                                // [2][chunks][pitch]: runs that a chunk begins with | ends with
     uint32_t chunk, n_chunks, pitch, digit_bits, passes;
+    uint32_t early_rows, fill_rows, fill_ctas, sum_ctas;   // rows cleared beside the sort; rows of a clearing CTA beside the sums, and how many of each
     WorkspaceHeader *header;
     unsigned int *device_status;
 };
@@ -165,7 +166,7 @@ __device__ void fill_zeros(char *at, uint64_t bytes, unsigned char *zeros, uint3
 }
 
 // The lanes with the same digit as this one, among those with an item, from a vote on each bit (one instruction that compares all
-// lanes takes the distinct digits one after the other: 131072 tokens 99 us instead of the 45 of the votes).
+// lanes takes the distinct digits one after the other: 131072 tokens, eight CTAs, 76 us instead of 67).
 __device__ __forceinline__ uint32_t same_digit(uint32_t digit, uint32_t bits, uint32_t items)
 {
     uint32_t same = items;
@@ -192,8 +193,9 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
 {
     extern __shared__ __align__(128) unsigned char raw[];
     SortShared &s = *reinterpret_cast<SortShared *>(raw);
+    next_may_start();
     if (blockIdx.x >= kSortCtas) {
-        fill_zeros(reinterpret_cast<char *>(a.grad_weight), a.table_elems * table_bytes, raw, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+        fill_zeros(reinterpret_cast<char *>(a.grad_weight), (uint64_t)a.early_rows * a.width * table_bytes, raw, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
         return;
     }
     const uint32_t rank = cluster_rank(), lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, digits = 1u << a.digit_bits;
@@ -340,13 +342,73 @@ template <typename A, bool VEC> struct RowBlock {
     }
 };
 
+// The first place in keys[0, n) whose key is at least `key`, by a warp, thirty-two probes at a time.
+__device__ __forceinline__ uint64_t warp_lower_bound(const uint32_t *keys, uint64_t n, uint32_t key, uint32_t lane)
+{
+    uint64_t lo = 0, hi = n;                                        // in [lo, hi]
+    while (lo < hi) {
+        const uint64_t step = (hi - lo + 31u) / 32u, at = lo + lane * step;
+        const uint32_t less = __ballot_sync(0xffffffffu, at < hi && __ldg(keys + at) < key);       // a run from lane 0 on
+        if (!less) return lo;
+        const uint32_t most = 31u - __clz(less);
+        lo += most * step + 1u;
+        hi = most == 31u || lo + step - 1u > hi ? hi : lo + step - 1u;
+    }
+    return lo;
+}
+// Zeros to the rows of a clearing CTA that no token names.
+template <typename W> __device__ void clear_rows(const EmbeddingArgs &a, uint32_t cta, uint64_t *range, uint32_t *absent)
+{
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t *keys = a.keys[(a.passes + 1u) & 1u];
+    const uint32_t r0 = a.early_rows + cta * a.fill_rows, rows = a.vocabulary - r0 < a.fill_rows ? a.vocabulary - r0 : a.fill_rows;
+    if (warp < 2u) {
+        const uint64_t at = warp_lower_bound(keys, a.n, r0 + warp * rows, lane);
+        if (lane == 0) range[warp] = at;
+    }
+    __syncthreads();
+    for (uint32_t t = threadIdx.x; t < rows; t += kRowThreads) {
+        uint64_t lo = range[0], hi = range[1];
+        while (lo < hi) {
+            const uint64_t mid = (lo + hi) / 2u;
+            if (__ldg(keys + mid) < r0 + t) lo = mid + 1u;
+            else hi = mid;
+        }
+        absent[t] = lo == range[1] || __ldg(keys + lo) != r0 + t;
+    }
+    __syncthreads();
+    const float none[8] = {};
+    for (uint32_t t = warp; t < rows; t += kRowThreads / 32u) {
+        if (!absent[t]) continue;
+        W *const row = reinterpret_cast<W *>(a.grad_weight) + (uint64_t)(r0 + t) * a.width;
+        const uint32_t off = (uint32_t)((32u - (reinterpret_cast<uintptr_t>(row) & 31u)) & 31u) / (uint32_t)sizeof(W);
+        const uint32_t head = off < a.width ? off : a.width, per = 32u / (uint32_t)sizeof(W), units = (a.width - head) / per, tail = head + units * per;
+        for (uint32_t u = lane; u < units; u += 32u) Elem<float>::store8(row + head + u * per, none);
+        if (lane < head) row[lane] = put1<W>(0.0f);
+        if (lane < a.width - tail) row[tail + lane] = put1<W>(0.0f);
+    }
+}
+
+constexpr uint32_t kFillRows = 256;             // of a clearing CTA at most
+
 template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads, VEC ? 3 : 2) embedding_sum_kernel(const __grid_constant__ EmbeddingArgs a)
 {
     extern __shared__ __align__(128) unsigned char raw[];
     using Block = RowBlock<A, VEC>;
     constexpr int kRows = Block::kRows;
+    next_may_start();
+    wait_for_ahead();
+    // clearing CTAs lie evenly among the others
+    const uint64_t both = (uint64_t)a.sum_ctas + a.fill_ctas;
+    const uint32_t fills = (uint32_t)((uint64_t)blockIdx.x * a.fill_ctas / both);
+    if ((uint32_t)((blockIdx.x + 1ull) * a.fill_ctas / both) > fills) {
+        __shared__ uint64_t range[2];
+        __shared__ uint32_t absent[kFillRows];
+        clear_rows<W>(a, fills, range, absent);
+        return;
+    }
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u);
-    const uint64_t item = (uint64_t)blockIdx.x * (kRowThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    const uint64_t item = (uint64_t)(blockIdx.x - fills) * (kRowThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
     if (item >= (uint64_t)a.n_chunks * a.slabs) return;
     const uint32_t chunk = (uint32_t)(item / a.slabs), slab = (uint32_t)(item - (uint64_t)chunk * a.slabs);
     const uint32_t col = slab * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
@@ -437,6 +499,7 @@ template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) e
     __shared__ float s_sum[kWarps][256];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, blocks = (a.pitch + 255u) / 256u;
     const uint32_t *keys = a.keys[(a.passes + 1u) & 1u];
+    wait_for_ahead();
     const uint64_t work = (uint64_t)a.jobs[0] * blocks;
     for (uint64_t i = blockIdx.x; i < work; i += gridDim.x) {
         const uint32_t job = (uint32_t)(i / blocks), block = (uint32_t)(i - (uint64_t)job * blocks);
@@ -522,7 +585,6 @@ static EmbeddingArgs embedding_args(const daf_embedding_params *p)
 {
     EmbeddingArgs a = {};
     a.n = p->tokens;
-    a.table_elems = p->vocabulary * p->width;
     a.wide_tokens = p->token_bytes == 8u;
     a.vocabulary = (uint32_t)p->vocabulary;
     a.width = p->width;
@@ -558,15 +620,14 @@ template <typename W, typename A, bool VEC> static daf_status forward(const Embe
 }
 template <typename W, typename A, bool VEC> static daf_status backward(const EmbeddingArgs &a, cudaStream_t s)
 {
-    const uint64_t items = (uint64_t)a.n_chunks * a.slabs, per_cta = kRowThreads >> a.lanes_log2;
     const auto sum = &embedding_sum_kernel<A, W, VEC>;
     const uint32_t smem = VEC ? kSumBytes * kRowThreads : 0u;
     int ctas = 0;                                                   // also raises the kernel's limit of shared memory
     if (persistent_ctas(reinterpret_cast<const void *>(sum), (int)kRowThreads, (int)smem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
-    sum<<<(uint32_t)((items + per_cta - 1u) / per_cta), kRowThreads, smem, s>>>(a);
+    if (launch_behind(sum, a.sum_ctas + a.fill_ctas, kRowThreads, smem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
     const uint64_t most = (uint64_t)a.n_chunks * ((a.pitch + 255u) / 256u);
-    embedding_join_kernel<W, VEC><<<(uint32_t)(most < 148u * 4u ? most : 148u * 4u), kRowThreads, 0, s>>>(a);
-    return DAF_OK;
+    const auto join = &embedding_join_kernel<W, VEC>;
+    return launch_behind(join, (uint32_t)(most < 148u * 4u ? most : 148u * 4u), kRowThreads, 0, s, a) == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 template <bool BACK, bool VEC> static daf_status by_type(uint32_t table, uint32_t act, const EmbeddingArgs &a, cudaStream_t s)
 {
@@ -631,12 +692,22 @@ extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, con
     a.jobs = reinterpret_cast<uint32_t *>(at);
     a.part = reinterpret_cast<float *>(at + up256((a.n_chunks + 1ull) * sizeof(uint32_t)));
     if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
-    int ctas = 0;                                                   // also raises the kernel's limit of shared memory
-    if (persistent_ctas(reinterpret_cast<const void *>(&embedding_sort_kernel), (int)kSortThreads, (int)sizeof(SortShared), &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+    int ctas = 0;                                                   // also raises the kernel's limits
+    if (persistent_ctas(reinterpret_cast<const void *>(&embedding_sort_kernel), (int)kSortThreads, (int)sizeof(SortShared), &ctas) != cudaSuccess ||
+        cudaFuncSetAttribute(embedding_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+        return DAF_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    // Rows to clear beside the sort: about as much as its own time writes (measured 8 us and 0.3 ns a token; 4 GB a ms), all without
+    // tokens; the rest beside the sums, 64 KiB to a CTA.
     const uint32_t eb = elem_bytes(p.table_dtype);
-    const uint64_t bytes = a.table_elems * eb, clusters = (bytes + (1u << 19) - 1u) >> 19;    // 64 KiB to a CTA
-    embedding_sort_kernel<<<kSortCtas * (uint32_t)(1u + (clusters < 17u ? clusters : 17u)), kSortThreads, sizeof(SortShared), s>>>(a, eb);
+    const uint64_t row_bytes = (uint64_t)a.width * eb, early = (32000000ull + 1200ull * a.n) / row_bytes;
+    a.early_rows = a.n == 0 || early > a.vocabulary ? a.vocabulary : (uint32_t)early;
+    a.fill_rows = row_bytes >= 65536u ? 1u : 65536u / row_bytes > kFillRows ? kFillRows : (uint32_t)(65536u / row_bytes);
+    a.fill_ctas = (a.vocabulary - a.early_rows + a.fill_rows - 1u) / a.fill_rows;
+    const uint64_t per_cta = kRowThreads >> a.lanes_log2;
+    a.sum_ctas = (uint32_t)(((uint64_t)a.n_chunks * a.slabs + per_cta - 1u) / per_cta);
+    const uint64_t bytes = a.early_rows * row_bytes, clusters = (bytes + (1u << 20) - 1u) >> 20;      // 64 KiB to a CTA
+    embedding_sort_kernel<<<kSortCtas * (uint32_t)(1u + (clusters < 8u ? clusters : 8u)), kSortThreads, sizeof(SortShared), s>>>(a, eb);
     if (a.n) {
         const daf_status ran = wide(a, d_grad_out, p.dtype, d_grad_weight, p.table_dtype) ? by_type<true, true>(p.table_dtype, p.dtype, a, s)
                                                                                          : by_type<true, false>(p.table_dtype, p.dtype, a, s);

@@ -158,6 +158,7 @@ template <typename T> __device__ __forceinline__ double sum_squares(const OrthGr
 __global__ void __launch_bounds__(256, 5) orth_norm_kernel(const __grid_constant__ OrthArgs a)
 {
     __shared__ double s_part[8];
+    next_may_start();
     if (blockIdx.x == 0) {
         for (uint32_t i = threadIdx.x; i < a.matrices; i += 256u) a.done[i] = 0;
         if (threadIdx.x == 0) {
@@ -221,6 +222,8 @@ template <typename T> __device__ __forceinline__ void first_operand(const OrthAr
 __global__ void __launch_bounds__(256, 5) orth_start_kernel(const __grid_constant__ OrthArgs a)
 {
     __shared__ double s_part[8];
+    next_may_start();
+    wait_for_ahead();
     const PrepShare s = prep_share(a);
     const OrthGroup &g = a.g[s.group];
     if (g.dtype == DAF_F32) first_operand<float>(a, g, s, s_part);
@@ -503,6 +506,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
     tmem_after_sync();
     const uint32_t tmem = bars.tmem;
     volatile uint32_t *const stop = &bars.abort;
+    wait_for_ahead();
 
     if (warp == 2 && rank == 0) {                                  // ---- tickets, one tile ahead of the copies
         if (lane == 0) {
@@ -957,9 +961,9 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
         a.keep_status = any;
         any = true;
         orth_norm_kernel<<<a.prep_total, 256, 0, s>>>(a);
-        orth_start_kernel<<<a.prep_total, 256, 0, s>>>(a);
+        if (launch_behind(&orth_start_kernel, a.prep_total, 256, 0, s, a) != cudaSuccess) return DAF_ERR_CUDA;
         const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total, pairs = (uint32_t)ctas / 2u;
-        orthogonalize_kernel<<<2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s>>>(a);
+        if (launch_behind(&orthogonalize_kernel, 2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
     }
     if (!any) {
         if (workspace_bytes < sizeof(WorkspaceHeader)) return DAF_ERR_CAPACITY;

@@ -388,6 +388,7 @@ template <typename T, typename P, int V, bool HALVES> __global__ void __launch_b
 
 template <typename T, typename P, int V, bool HALVES> __global__ void __launch_bounds__(kRotaryThreads, kRotaryCtasPerSm) rotary_norm_grad_kernel(const __grid_constant__ RotaryArgs a)
 {
+    next_may_start();
     using Part = Piece<T, V>;
     constexpr int kUnit = (int)(kRotaryBytes / (2u * 4u * Part::kWords * 4u));
     constexpr uint32_t kPlace = Part::kWords * 4 * kRotaryThreads, kRow = 4u * kPlace;
@@ -517,6 +518,7 @@ template <typename P> __global__ void __launch_bounds__(1024) rotary_weight_kern
     __shared__ float s_part[32][33];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, col = blockIdx.x * 32u + lane;
     P *const out = blockIdx.y ? k_out : q_out;
+    wait_for_ahead();
     if (!out) return;
     float sum = 0.0f;
     if (col < dim)
@@ -622,8 +624,9 @@ template <typename T, typename P, int V, bool HALVES> static daf_status rotary_l
     if (back && most > (int)kRotaryCtas) most = (int)kRotaryCtas;
     const uint32_t ctas = wanted < (uint32_t)most ? wanted : (uint32_t)most;
     kernel<<<ctas, kRotaryThreads, smem, s>>>(a);
-    if (gqw || gkw) rotary_weight_kernel<P><<<dim3((a.dim + 31u) / 32u, 2), 1024, 0, s>>>(a.partial, ctas, a.dim, reinterpret_cast<P *>(gqw), reinterpret_cast<P *>(gkw));
-    return DAF_OK;
+    if (!gqw && !gkw) return DAF_OK;
+    return launch_behind(&rotary_weight_kernel<P>, dim3((a.dim + 31u) / 32u, 2), 1024, 0, s, static_cast<const float *>(a.partial), ctas, a.dim,
+                         reinterpret_cast<P *>(gqw), reinterpret_cast<P *>(gkw)) == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 static daf_status rotary_by_type(const daf_rotary_params &p, const RotaryArgs &a, bool back, void *gqw, void *gkw, cudaStream_t s)
 {
