@@ -942,6 +942,7 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
         if (rows[i] && cols[i] && (!d_in[i] || !d_out[i] || ((reinterpret_cast<uintptr_t>(d_in[i]) | reinterpret_cast<uintptr_t>(d_out[i])) & mask)))
             return DAF_ERR_INVALID_ARG;
     }
+    if (workspace_bytes < daf_orthogonalize_workspace(params, n, dtypes, rows, cols)) return DAF_ERR_CAPACITY;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     uint32_t index[kOrthMatrices];
     OrthArgs a;
@@ -952,7 +953,6 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
         uint64_t bytes = 0;
         orth_batch(&a, params, n, dtypes, rows, cols, &next, index, &bytes);
         if (a.matrices == 0) break;
-        if (workspace_bytes < bytes) return DAF_ERR_CAPACITY;
         if (!orth_place(&a, reinterpret_cast<char *>(d_workspace)) || !(a.device_status = device_status_word())) return DAF_ERR_CUDA;
         for (uint32_t i = 0; i < a.matrices; i++) {
             a.in[i] = d_in[index[i]];
@@ -965,9 +965,6 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
         const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total, pairs = (uint32_t)ctas / 2u;
         if (launch_behind(&orthogonalize_kernel, 2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
     }
-    if (!any) {
-        if (workspace_bytes < sizeof(WorkspaceHeader)) return DAF_ERR_CAPACITY;
-        if (cudaMemsetAsync(d_workspace, 0, sizeof(uint32_t), s) != cudaSuccess) return DAF_ERR_CUDA;
-    }
+    if (!any && cudaMemsetAsync(d_workspace, 0, sizeof(uint32_t), s) != cudaSuccess) return DAF_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
