@@ -7,12 +7,12 @@
 //   update  x' = a x + P x       2 m m n
 // Bound: the tensor cores.  What is held between the products is float16, not bfloat16: 11 bits instead of 8 at the same rate,
 // and the values' range is known (singular values below two), so powers of two keep them away from both ends of the type:
-// x is held K = |g| 2^s times its size, K in [2^12, 2^13), so that the first x is g itself times a power of two, exact for bfloat16;
-// G and P are held 2^12 times their size.  Relative error of the result in binary64 arithmetic with only these roundings
+// x is held K times its size, G and P 2^12 times; K = |g| 2^s in [2^12, 2^13), so that the first x is g itself times a power of two, exact
+// for bfloat16 (two parts: 2^12, so that no rounded factor moves all singular values at once: five steps multiply that by a hundred).  Relative error of the result in binary64 arithmetic with only these roundings
 // (768 x 2304, spectra from flat to strongly decaying): 1.3e-3 to 5.0e-3 with x rounded at the start, 0.9e-3 to 3.4e-3 so, and at most 1.4e-3 with
 // the linear term a x of the steps behind the first two taken from two float16 parts (the small singular values live there: what
 // rounds the large ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  float16 and
-// binary32 matrices are held in two parts throughout (three products instead of one): 2e-6.
+// binary32 matrices are held in two parts throughout (three products instead of one): 7e-7.
 //
 // One persistent kernel runs all products of all steps and matrices.  Pairs of CTAs take tiles of 256 x N by a ticket, in an order
 // in which whatever a tile needs comes before it; a tile waits until its matrix's tiles of the earlier products are done
@@ -31,6 +31,10 @@ constexpr uint32_t kOrthThreads = 384, kOrthStages = 6, kOrthBox = 8192, kOrthSt
 constexpr uint32_t kOrthGroups = 16, kOrthMatrices = 192, kOrthSlots = 2;
 constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
 constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch: bounds the workspace (8 bytes and more per element)
+// Binary32: sums of 128 of the summed dimension are taken in tensor memory and added up in registers.  A tensor memory sum loses about two
+// units of its 24th bit at every addition, always downwards: 4096 columns of one row 2e-5 without, 5e-7 so; segments of 64 cost a fifth
+// of the time (results cannot run as far ahead), of 256 are 2.5 times as far off.
+constexpr uint32_t kOrthSegment = 2;            // copies of 64
 constexpr float kHeld = 4096.0f;                // G and P times this
 constexpr uint32_t kPrepUnits = 64;             // pieces of 256 columns of a row to a CTA of the preparing kernels
 
@@ -42,8 +46,8 @@ struct OrthGroup {                              // matrices of one shape and typ
                                                 // reach the diagonal or lie right of it
     uint64_t x_plane, m_plane;                  // elements of a plane
     uint32_t r, c, m, x_pitch, m_pitch, tall, planes, count, first, dtype;
-    uint32_t sym_tiles, sym_cols, upd_tiles, upd_rows, n;   // of one matrix; columns of a tile
-    uint32_t sym_first, upd_first, prep_ctas, prep_first;
+    uint32_t sym_tiles, sym_cols, sym_n, upd_tiles, upd_rows, upd_n;     // of one matrix; columns of a tile
+    uint32_t sym_first, upd_first, prep_ctas, prep_first, segment;
 };
 struct OrthArgs {
     OrthGroup g[kOrthGroups];
@@ -181,6 +185,7 @@ template <typename T> __device__ __forceinline__ void first_operand(const OrthAr
     const double *parts = a.partial + g.prep_first + s.matrix * g.prep_ctas;
     __half *hi = g.x_at[0] + (uint64_t)s.matrix * 2u * g.x_plane, *lo = hi + g.x_plane;
     float by = 0.0f, by2 = 0.0f;
+    double factor = 0.0;
 #pragma unroll 1
     for (uint32_t j0 = 0; j0 < kPrepUnits / 8u; j0 += kPrepFlight) {
         OrthEight<T> v[kPrepFlight];                                // on their way while the norm is summed up
@@ -197,10 +202,12 @@ template <typename T> __device__ __forceinline__ void first_operand(const OrthAr
             const double norm = sqrt(cta_sum(sum, s_part)) + (double)a.eps;
             const bool finite = norm - norm == 0.0;
             const int up = finite ? 12 - ilogb(norm) : 0;
-            if (s.cta == 0 && threadIdx.x == 0) a.scale[g.first + s.matrix] = finite ? (float)scalbn(norm, up) : __int_as_float(0x7FC00000);
-            // 2^up as two factors that binary32 holds
+            if (s.cta == 0 && threadIdx.x == 0)
+                a.scale[g.first + s.matrix] = !finite ? __int_as_float(0x7FC00000) : g.planes == 2u ? kHeld : (float)scalbn(norm, up);
+            // one part: 2^up as two factors that binary32 holds; two: any factor
             by = finite ? scalbnf(1.0f, up / 2) : __int_as_float(0x7FC00000);
             by2 = scalbnf(1.0f, up - up / 2);
+            factor = (double)kHeld / norm;
         }
 #pragma unroll
         for (uint32_t j = 0; j < kPrepFlight; j++) {
@@ -210,7 +217,7 @@ template <typename T> __device__ __forceinline__ void first_operand(const OrthAr
             v[j].widen(x);
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                x[e] = x[e] * by * by2;
+                x[e] = g.planes == 2u ? (float)((double)x[e] * factor) * (by == by ? 1.0f : by) : x[e] * by * by2;
                 rest[e] = x[e] - __half2float(__float2half_rn(x[e]));
             }
             Elem<__half>::store8(hi + (uint64_t)row * g.x_pitch + col, x);
@@ -236,6 +243,7 @@ enum : uint32_t { kGram = 0, kPoly = 1, kUpdate = 2, kNoTile = 3 };
 struct OrthTile {
     uint32_t kind, step, group, matrix, row, col;
     __device__ __forceinline__ uint4 packed() const { return make_uint4(kind | step << 8 | group << 16, matrix, row, col); }
+    __device__ __forceinline__ uint32_t width(const OrthGroup &g) const { return kind == kUpdate ? g.upd_n : g.sym_n; }
     static __device__ __forceinline__ OrthTile from(uint4 v) { return {v.x & 255u, v.x >> 8 & 255u, v.x >> 16, v.y, v.z, v.w}; }
 };
 
@@ -317,7 +325,7 @@ __device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket
         i -= t.matrix * g.upd_tiles;
         const uint32_t col = i / g.upd_rows;
         t.row = (i - col * g.upd_rows) * kOrthRows;
-        t.col = col * g.n;
+        t.col = col * g.upd_n;
         return t;
     }
     if (i >= a.sym_total) {
@@ -333,12 +341,12 @@ __device__ __forceinline__ OrthTile orth_tile(const OrthArgs &a, uint32_t ticket
     for (uint32_t first = 0;;) {
         const uint32_t left = g.sym_cols - first;
         if (i < left) {
-            t.col = (first + i) * g.n;
+            t.col = (first + i) * g.sym_n;
             return t;
         }
         i -= left;
         t.row += kOrthRows;
-        first = t.row / g.n;
+        first = t.row / g.sym_n;
     }
 }
 
@@ -461,12 +469,12 @@ __device__ __forceinline__ void take_away(float (&x)[32], const uint4 (&v)[4])
         }
     }
 }
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
+template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
 {
     extern __shared__ __align__(1024) unsigned char s_raw[];
     struct Bars {
-        // full, heard, acc_empty, drain: the first CTA's count for both
-        uint64_t full[kOrthStages], empty[kOrthStages], told[kOrthSlots], heard[kOrthSlots], acc_full[2], acc_empty[2], drain, pad;
+        // full, heard, acc_empty, seg_empty, drain: the first CTA's count for both
+        uint64_t full[kOrthStages], empty[kOrthStages], told[kOrthSlots], heard[kOrthSlots], acc_full[2], acc_empty[2], seg_full[2], seg_empty[2], drain, pad;
         uint4 tile[kOrthSlots];
         uint32_t tmem, abort, late;
     };
@@ -492,6 +500,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
         for (uint32_t i = 0; i < 2u; i++) {
             bar_init(&bars.acc_full[i], 1);
             bar_init(&bars.acc_empty[i], 16);
+            bar_init(&bars.seg_full[i], 1);
+            bar_init(&bars.seg_empty[i], 16);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
@@ -543,15 +553,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                 asm volatile("fence.proxy.async;" ::: "memory");    // what other CTAs wrote by stores is now read by copies
                 const uint32_t buf = t.step & 1u;
                 const OrthOperands o = OrthOperands::of(g, t);
-                const int lines = (int)(second ? t.col + g.n / 2u * rank : t.row + 128u * rank);
+                const uint32_t width = t.width(g);
+                const int lines = (int)(second ? t.col + width / 2u * rank : t.row + 128u * rank);
                 // x, held in two planes, or a symmetric matrix, in as many as the group's products take
                 const bool of_x = t.kind == kGram || (t.kind == kUpdate && second != (g.tall != 0u));
-                const int matrix = (int)(t.matrix * (of_x ? 2u : g.planes));
-                const uint32_t to = smem_u32(stages) + (second ? 2u * kOrthBox : 0u), bytes = 2u * (2u * kOrthBox + g.n / 128u * kOrthBox);
+                const int matrix = (int)(t.matrix * (of_x ? 2u : (uint32_t)PLANES));
+                const uint32_t to = smem_u32(stages) + (second ? 2u * kOrthBox : 0u), bytes = 2u * (2u * kOrthBox + width / 128u * kOrthBox);
                 bool ok = true;
                 const auto copy = [&](const CUtensorMap *map, bool across, int from, int end) {
                     for (int k = from; k < end; k += 64)
-                        for (uint32_t part = 0; part < g.planes; part++) {
+                        for (uint32_t part = 0; part < (uint32_t)PLANES; part++) {
                             if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) return;
                             if (counts) bar_expect(&bars.full[st], bytes);
                             pair_load(to + st * kOrthStage, map, in_cta(&bars.full[st], 0), across ? 0 : k, across ? k : lines, across ? lines / 64 : 0, matrix + (int)part);
@@ -580,7 +591,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
         }
     } else if (warp == 1 && rank == 0) {                           // ---- products
         const uint32_t one = elect_lane();
-        uint32_t st = 0, ph = 0;
+        uint32_t st = 0, ph = 0, segment = 0;                       // segment: of all tiles
         const auto step_on = [&]() {
             if (++st == kOrthStages) st = 0, ph ^= 1u;
         };
@@ -595,7 +606,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
             tmem_after_sync();
             const OrthGroup &g = a.g[t.group];
             const OrthOperands o = OrthOperands::of(g, t);
-            const uint32_t plain = product_desc(false, g.n, false) + ((256u - 128u) >> 4 << 24);   // M = 256, where product_desc says 128
+            const uint32_t plain = product_desc(false, t.width(g), false) + ((256u - 128u) >> 4 << 24);   // M = 256, where product_desc says 128
             const uint32_t rounds = (o.keys + 63u) / 64u, d = tmem + buf * 256u;
             bool ok = true;
             for (uint32_t k = 0; k < rounds; k++) {
@@ -606,24 +617,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                 const uint32_t step_a = ca ? 128u : 2u, step_b = cb ? 128u : 2u, desc = plain | (ca ? 1u << 15 : 0u) | (cb ? 1u << 16 : 0u);
                 const uint32_t at = smem_u32(stages + st * kOrthStage);
                 const uint32_t la = operand_low(at, kOrthBox), lb = operand_low(at + 2u * kOrthBox, kOrthBox);
-                pair_product(one, d, la, lb, desc, k > 0);
+                if constexpr (PLANES == 1) {
+                    pair_product(one, d, la, lb, desc, k > 0);
 #pragma unroll
-                for (uint32_t s = 1; s < 4u; s++) pair_product<true>(one, d, la + s * step_a, lb + s * step_b, desc);
-                if (g.planes == 2u) {
-                    // the small parts' stage behind it; their products have an accumulator of their own, where they are not cut
-                    // to the large sum's last place
+                    for (uint32_t s = 1; s < 4u; s++) pair_product<true>(one, d, la + s * step_a, lb + s * step_b, desc);
+                } else {
+                    // The large parts' products, a segment at a time: the accumulator cuts every sum at its last place, so results add segments
+                    // up in registers.  The stage behind holds the small parts; their products have an accumulator for the whole tile.
+                    const uint32_t main = tmem + (segment & 1u) * 128u, cross = tmem + 256u + buf * 128u;
+                    const bool begins = k % g.segment == 0;
+                    if (begins && segment >= 2u && !(ok = wait_from_pair(&bars.seg_empty[segment & 1u], (segment / 2u - 1u) & 1u, stop))) break;
+                    if (begins) tmem_after_sync();
+                    pair_product(one, main, la, lb, desc, !begins);
+#pragma unroll
+                    for (uint32_t s = 1; s < 4u; s++) pair_product<true>(one, main, la + s * step_a, lb + s * step_b, desc);
+                    if (k % g.segment == g.segment - 1u || k + 1u == rounds) {
+                        pair_done(one, &bars.seg_full[segment & 1u], 3u);
+                        segment++;
+                    }
                     uint64_t *const first = &bars.empty[st];
                     step_on();
                     if (!(ok = wait_from_pair(&bars.full[st], ph, stop))) break;
                     tmem_after_sync();
                     const uint32_t small = smem_u32(stages + st * kOrthStage);
                     const uint32_t sa = operand_low(small, kOrthBox), sb = operand_low(small + 2u * kOrthBox, kOrthBox);
-                    pair_product(one, d + 128u, la, sb, desc, k > 0);
-                    pair_product<true>(one, d + 128u, sa, lb, desc);
+                    pair_product(one, cross, la, sb, desc, k > 0);
+                    pair_product<true>(one, cross, sa, lb, desc);
 #pragma unroll
                     for (uint32_t s = 1; s < 4u; s++) {
-                        pair_product<true>(one, d + 128u, la + s * step_a, sb + s * step_b, desc);
-                        pair_product<true>(one, d + 128u, sa + s * step_a, lb + s * step_b, desc);
+                        pair_product<true>(one, cross, la + s * step_a, sb + s * step_b, desc);
+                        pair_product<true>(one, cross, sa + s * step_a, lb + s * step_b, desc);
                     }
                     pair_done(one, first, 3u);
                 }
@@ -638,6 +661,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
     } else if (warp >= 4) {                                        // ---- results
         const uint32_t quarter = warp & 3u, half = (warp - 4u) >> 2;
         unsigned char *const stage = stages + kOrthStages * kOrthStage + (warp - 4u) * kOrthOut;
+        uint32_t segment = 0;
         for (uint32_t n = 0;; n++) {
             const uint32_t slot = n % kOrthSlots, buf = n & 1u;
             if (!wait_from_pair(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
@@ -647,17 +671,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
             if (t.kind == kNoTile) break;
             const OrthGroup &g = a.g[t.group];
             const bool update = t.kind == kUpdate, gram = t.kind == kGram, last = t.step + 1u == a.steps;
-            const uint32_t chunks = g.n / 64u, row = t.row + 128u * rank + quarter * 32u;
+            const uint32_t chunks = PLANES == 2 ? 2u : t.width(g) / 64u, row = t.row + 128u * rank + quarter * 32u;
             const uint32_t rows = update ? g.r : g.m, pitch = update ? g.x_pitch : g.m_pitch, matrix = g.first + t.matrix;
             const float k = __ldcg(a.scale + matrix);
             // what is added to the product, and factors of both
-            const __half *with = update ? g.x_at[t.step & 1u] + (uint64_t)t.matrix * 2u * g.x_plane : g.gram_at + (uint64_t)t.matrix * g.planes * g.m_plane;
+            const __half *with = update ? g.x_at[t.step & 1u] + (uint64_t)t.matrix * 2u * g.x_plane : g.gram_at + (uint64_t)t.matrix * (uint32_t)PLANES * g.m_plane;
             const uint64_t plane = update ? g.x_plane : g.m_plane;
-            const bool two = g.planes == 2u || (update && (t.step == 1u || t.step == 2u));
+            const bool two = PLANES == 2 || (update && (t.step == 1u || t.step == 2u));
             const float of_product = gram ? __fdiv_rn(kHeld, k * k) : t.kind == kPoly ? a.c / kHeld : 1.0f / kHeld;
             const float of_with = update ? a.a : a.b;
             __half *to = update ? g.x_at[(t.step + 1u) & 1u] + (uint64_t)t.matrix * 2u * g.x_plane
-                                : (gram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * g.planes * g.m_plane;
+                                : (gram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * (uint32_t)PLANES * g.m_plane;
             OrthBlock ahead, ahead2;                                // of the next 32 columns, on their way during the products
             const auto look_ahead = [&](uint32_t j) {
                 if (gram) return;
@@ -666,34 +690,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                 if (two) ahead2.load(with + plane, pitch, row, rows, j < chunks ? col : pitch, lane);
             };
             look_ahead(0);
-            if (!bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
-            tmem_after_sync();
-            for (uint32_t j = 0; j < chunks; j++) {
-                const uint32_t col = t.col + (half * chunks + j) * 32u, acc = tmem + buf * 256u + (half * chunks + j) * 32u + (quarter << 21);
-                if (row >= rows || col >= pitch) break;
-                float x[32];
-                OrthBlock w = ahead, w2 = ahead2;
-                look_ahead(j + 1u);
-                __syncwarp();
-                tmem_load32(acc, x);
-                tmem_wait_loads();
-                if (g.planes == 2u) {
-                    float small[32];
-                    tmem_load32(acc + 128u, small);
-                    tmem_wait_loads();
-#pragma unroll
-                    for (int i = 0; i < 32; i++) x[i] += small[i];
+            // one 32 x 32 block of the result, given its product
+            const auto block = [&](uint32_t j, float (&x)[32]) {
+                const uint32_t col = t.col + (half * chunks + j) * 32u;
+                if (row >= rows || col >= pitch) return;
+                OrthBlock w, w2;
+                if constexpr (PLANES == 1) {
+                    w = ahead;
+                    w2 = ahead2;
+                    look_ahead(j + 1u);
                 }
 #pragma unroll
                 for (int i = 0; i < 32; i++) x[i] *= of_product;
                 if (!gram) {
+                    OrthBlock &high = PLANES == 1 ? w : ahead, &low = PLANES == 1 ? w2 : ahead2;
                     if (two) {
-                        w2.to_rows(stage, lane);
-                        w2.add(x, of_with);
+                        low.to_rows(stage, lane);
+                        low.add(x, of_with);
                     }
-                    w.to_rows(stage, lane);
-                    w.add(x, of_with);
+                    high.to_rows(stage, lane);
+                    high.add(x, of_with);
                 }
+                if constexpr (PLANES == 2) look_ahead(j + 1u);      // here: before it there are no registers to be had
                 if (update && last) {
                     const float by = __fdiv_rn(1.0f, k);
 #pragma unroll
@@ -714,7 +732,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                                     if (col + i + e < ends) at[i + e] = x[i + e];
                             }
                         }
-                        continue;
+                        return;
                     }
                     if (g.dtype == DAF_F16) round32<__half>(x, w.v);
                     else round32<__nv_bfloat16>(x, w.v);
@@ -724,15 +742,55 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) ort
                         for (uint32_t r = 0; r < 32u && row + r < rows; r++)
                             reinterpret_cast<uint16_t *>(out)[(uint64_t)(row + r) * g.c + col + lane] =
                                 *reinterpret_cast<const uint16_t *>(stage + r * 64u + (((lane >> 3) ^ (r >> 1 & 3u)) * 16u) + (lane & 7u) * 2u);
-                    continue;
+                    return;
                 }
-                const uint32_t planes = g.planes == 2u || (update && t.step < 2u) ? 2u : 1u;
+                const uint32_t planes = PLANES == 2 || (update && t.step < 2u) ? 2u : 1u;
                 for (uint32_t p = 0; p < planes; p++) {
                     round32<__half>(x, w.v);
                     if (p + 1u < planes) take_away(x, w.v);
                     w.to_quarters(stage, lane);
                     w.store(to + p * plane, pitch, row, rows, col, pitch, lane);
                 }
+            };
+            const uint32_t own = (half * chunks) * 32u + (quarter << 21);                      // the warp's first column, its lanes
+            if constexpr (PLANES == 1) {
+                if (!bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
+                tmem_after_sync();
+                for (uint32_t j = 0; j < chunks; j++) {
+                    float x[32];
+                    __syncwarp();
+                    tmem_load32(tmem + buf * 256u + own + j * 32u, x);
+                    tmem_wait_loads();
+                    block(j, x);
+                }
+            } else {
+                float x[2][32] = {}, part[32];
+                const auto add = [&](uint32_t at) {
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+                        tmem_load32(at + own + 32u * j, part);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (int i = 0; i < 32; i++) x[j][i] += part[i];
+                    }
+                };
+                const uint32_t rounds = (OrthOperands::of(g, t).keys + 63u) / 64u, segments = (rounds + g.segment - 1u) / g.segment;
+                bool ok = true;
+                for (uint32_t i = 0; i < segments; i++, segment++) {
+                    if (!(ok = bar_wait(&bars.seg_full[segment & 1u], segment / 2u & 1u, stop))) break;
+                    tmem_after_sync();
+                    __syncwarp();
+                    add(tmem + (segment & 1u) * 128u);
+                    tmem_before_sync();
+                    __syncwarp();
+                    if (lane == 0) arrive_in(in_cta(&bars.seg_empty[segment & 1u], 0));
+                }
+                if (!ok || !bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
+                tmem_after_sync();
+                __syncwarp();
+                add(tmem + 256u + buf * 128u);
+                block(0, x[0]);
+                block(1, x[1]);
             }
             tmem_before_sync();
             __syncwarp();
@@ -781,9 +839,11 @@ static uint32_t orth_sym_tiles(uint32_t m, uint32_t width)
     return tiles;
 }
 
-// The next matrices that go together, from *next on: the table without pointers to the workspace, and the bytes it needs.
+static uint32_t orth_planes(uint32_t dtype) { return dtype == DAF_BF16 ? 1u : 2u; }
+
+// The next matrices of `planes` parts that go together, from *next on: the table without pointers to the workspace, and the bytes it needs.
 static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t n, const uint32_t *dtypes, const uint64_t *rows, const uint64_t *cols,
-                       uint32_t *next, uint32_t *index, uint64_t *workspace)
+                       uint32_t planes, uint32_t *next, uint32_t *index, uint64_t *workspace)
 {
     struct Shape {
         uint32_t r, c, dtype, count, rank;
@@ -794,7 +854,7 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     a->groups = a->matrices = 0;
     for (; *next < n && a->matrices < kOrthMatrices; ++*next) {
         const uint32_t i = *next, r = (uint32_t)rows[i], c = (uint32_t)cols[i];
-        if (r == 0 || c == 0) continue;
+        if (r == 0 || c == 0 || orth_planes(dtypes[i]) != planes) continue;
         if (elems && elems + (uint64_t)r * c > kOrthBatch) break;
         uint32_t k = 0;
         while (k < a->groups && (shape[k].r != r || shape[k].c != c || shape[k].dtype != dtypes[i])) k++;
@@ -828,31 +888,45 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     a->c = p->coefficients[2];
     a->eps = p->eps;
     a->prep_total = 0;
-    // Tiles are 256 columns wide where that leaves every pair of SMs one, else 128; matrices in two parts need the other half of an
-    // accumulator for the small products.
-    uint32_t tiles = 0;
-    for (uint32_t k = 0; k < a->groups; k++) {
-        const uint32_t r = a->g[k].r, c = a->g[k].c, m = r < c ? r : c, sym = orth_sym_tiles(m, 256u);
-        const uint32_t upd = ((r + kOrthRows - 1u) / kOrthRows) * ((c + 255u) / 256u);
-        tiles += a->g[k].count * (sym < upd ? sym : upd);
-    }
-    const uint32_t width = tiles >= 74u ? 256u : 128u;
+    // Columns of a tile, 256 or 128, as what takes less by what was measured: a wave of tiles takes 0.31 or 0.29 us for 64 of the
+    // longest summed dimension, or as long as its results where that is more (3.5 or 1.8 us of a symmetric matrix, 6.5 or 2.7 of an
+    // update), and once the other.  Matrices in two parts take 128: the small parts' products and segments fill the rest of tensor memory.
+    const auto width = [&](bool update) {
+        double cost[2] = {0.0, 0.0};
+        for (int i = 0; i < 2; i++) {
+            const uint32_t w = i ? 128u : 256u;
+            uint64_t tiles = 0;
+            uint32_t keys = 0;
+            for (uint32_t k = 0; k < a->groups; k++) {
+                const uint32_t r = a->g[k].r, c = a->g[k].c, m = r < c ? r : c, n = r < c ? c : r;
+                tiles += (uint64_t)a->g[k].count * (update ? (uint64_t)((r + kOrthRows - 1u) / kOrthRows) * ((c + w - 1u) / w) : orth_sym_tiles(m, w));
+                keys = keys > (update ? m : n) ? keys : update ? m : n;
+            }
+            const double products = (double)keys / 64.0 * (i ? 0.29 : 0.31), results = update ? (i ? 2.7 : 6.5) : i ? 1.8 : 3.5;
+            const double more = products > results ? products : results, waves = (double)((tiles + 73u) / 74u);
+            cost[i] = waves * more + products + results - more;
+        }
+        return planes == 2u || cost[1] < cost[0] ? 128u : 256u;
+    };
+    const uint32_t sym_n = width(false), upd_n = width(true);
     uint32_t sym = 0, upd = 0;
     uint64_t bytes = sizeof(WorkspaceHeader) + up_to(2ull * kOrthMatrices * sizeof(uint32_t), 256u);
     for (uint32_t k = 0; k < a->groups; k++) {
         OrthGroup &g = a->g[k];
         g.tall = g.r > g.c;
         g.m = g.tall ? g.c : g.r;
-        g.planes = g.dtype == DAF_BF16 ? 1u : 2u;
+        g.planes = planes;
+        g.segment = g.dtype == DAF_F32 ? kOrthSegment : 1024u;
         g.x_pitch = (uint32_t)up_to(g.c, 64u);
         g.m_pitch = (uint32_t)up_to(g.m, 64u);
         g.x_plane = (uint64_t)g.r * g.x_pitch;
         g.m_plane = (uint64_t)g.m * g.m_pitch;
-        g.n = g.planes == 2u ? 128u : width;
-        g.sym_cols = (g.m + g.n - 1u) / g.n;
-        g.sym_tiles = orth_sym_tiles(g.m, g.n);
+        g.sym_n = sym_n;
+        g.upd_n = upd_n;
+        g.sym_cols = (g.m + sym_n - 1u) / sym_n;
+        g.sym_tiles = orth_sym_tiles(g.m, sym_n);
         g.upd_rows = (g.r + kOrthRows - 1u) / kOrthRows;
-        g.upd_tiles = g.upd_rows * ((g.c + g.n - 1u) / g.n);
+        g.upd_tiles = g.upd_rows * ((g.c + upd_n - 1u) / upd_n);
         g.sym_first = sym;
         g.upd_first = upd;
         sym += g.count * g.sym_tiles;
@@ -894,18 +968,18 @@ static bool orth_place(OrthArgs *a, char *at)
     };
     for (uint32_t k = 0; k < a->groups; k++) {
         OrthGroup &g = a->g[k];
-        const uint32_t half = g.n / 2u, xs = g.count * 2u, ms = g.count * g.planes;      // columns of a tile in each CTA; planes in all
+        const uint32_t half = g.sym_n / 2u, upd_half = g.upd_n / 2u, xs = g.count * 2u, ms = g.count * g.planes;      // columns of a tile in each CTA; planes in all
         for (int i = 0; i < 2; i++) g.x_at[i] = take(xs * g.x_plane);
         g.gram_at = take(ms * g.m_plane);
         g.poly_at = take(ms * g.m_plane);
         const auto square = [&](CUtensorMap *map, __half *p, bool across, uint32_t lines) { return orth_map(map, p, g.m_plane, ms, g.m, g.m, g.m_pitch, across, lines); };
         bool ok = square(&g.poly_a, g.gram_at, false, 128u) && square(&g.poly_a_across, g.gram_at, true, 128u) && square(&g.poly_b, g.gram_at, false, half) &&
-                  square(&g.poly_b_across, g.gram_at, true, half) && square(&g.upd_poly, g.poly_at, false, g.tall ? half : 128u) &&
-                  square(&g.upd_poly_across, g.poly_at, true, g.tall ? half : 128u);
+                  square(&g.poly_b_across, g.gram_at, true, half) && square(&g.upd_poly, g.poly_at, false, g.tall ? upd_half : 128u) &&
+                  square(&g.upd_poly_across, g.poly_at, true, g.tall ? upd_half : 128u);
         for (int i = 0; i < 2 && ok; i++)
             ok = orth_map(&g.gram_a[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, g.tall, 128u) &&
                  orth_map(&g.gram_b[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, g.tall, half) &&
-                 orth_map(&g.upd_x[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, !g.tall, g.tall ? 128u : half);
+                 orth_map(&g.upd_x[i], g.x_at[i], g.x_plane, xs, g.r, g.c, g.x_pitch, !g.tall, g.tall ? 128u : upd_half);
         if (!ok) return false;
     }
     return true;
@@ -922,11 +996,12 @@ extern "C" uint64_t daf_orthogonalize_workspace(const daf_orthogonalize_params *
     uint64_t most = sizeof(WorkspaceHeader);
     uint32_t index[kOrthMatrices];
     OrthArgs a;
-    for (uint32_t next = 0; next < n;) {
-        uint64_t bytes = 0;
-        orth_batch(&a, params, n, dtypes, rows, cols, &next, index, &bytes);
-        if (bytes > most) most = bytes;
-    }
+    for (uint32_t planes = 1; planes <= 2u; planes++)
+        for (uint32_t next = 0; next < n;) {
+            uint64_t bytes = 0;
+            orth_batch(&a, params, n, dtypes, rows, cols, planes, &next, index, &bytes);
+            if (bytes > most) most = bytes;
+        }
     return most;
 }
 
@@ -946,24 +1021,27 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     uint32_t index[kOrthMatrices];
     OrthArgs a;
-    int ctas = 0;
-    if (persistent_ctas(reinterpret_cast<const void *>(&orthogonalize_kernel), (int)kOrthThreads, (int)kOrthSmem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
     bool any = false;
-    for (uint32_t next = 0; next < n;) {
-        uint64_t bytes = 0;
-        orth_batch(&a, params, n, dtypes, rows, cols, &next, index, &bytes);
-        if (a.matrices == 0) break;
-        if (!orth_place(&a, reinterpret_cast<char *>(d_workspace)) || !(a.device_status = device_status_word())) return DAF_ERR_CUDA;
-        for (uint32_t i = 0; i < a.matrices; i++) {
-            a.in[i] = d_in[index[i]];
-            a.out[i] = d_out[index[i]];
+    for (uint32_t planes = 1; planes <= 2u; planes++) {
+        const auto kernel = planes == 1u ? &orthogonalize_kernel<1> : &orthogonalize_kernel<2>;
+        for (uint32_t next = 0; next < n;) {
+            uint64_t bytes = 0;
+            orth_batch(&a, params, n, dtypes, rows, cols, planes, &next, index, &bytes);
+            if (a.matrices == 0) break;
+            int ctas = 0;
+            if (persistent_ctas(reinterpret_cast<const void *>(kernel), (int)kOrthThreads, (int)kOrthSmem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+            if (!orth_place(&a, reinterpret_cast<char *>(d_workspace)) || !(a.device_status = device_status_word())) return DAF_ERR_CUDA;
+            for (uint32_t i = 0; i < a.matrices; i++) {
+                a.in[i] = d_in[index[i]];
+                a.out[i] = d_out[index[i]];
+            }
+            a.keep_status = any;
+            any = true;
+            orth_norm_kernel<<<a.prep_total, 256, 0, s>>>(a);
+            if (launch_behind(&orth_start_kernel, a.prep_total, 256, 0, s, a) != cudaSuccess) return DAF_ERR_CUDA;
+            const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total, pairs = (uint32_t)ctas / 2u;
+            if (launch_behind(kernel, 2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
         }
-        a.keep_status = any;
-        any = true;
-        orth_norm_kernel<<<a.prep_total, 256, 0, s>>>(a);
-        if (launch_behind(&orth_start_kernel, a.prep_total, 256, 0, s, a) != cudaSuccess) return DAF_ERR_CUDA;
-        const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total, pairs = (uint32_t)ctas / 2u;
-        if (launch_behind(&orthogonalize_kernel, 2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
     }
     if (!any && cudaMemsetAsync(d_workspace, 0, sizeof(uint32_t), s) != cudaSuccess) return DAF_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
