@@ -31,7 +31,8 @@ struct EmbeddingArgs {
     float scale;
     long long padding;
     // backward
-    uint32_t *keys[2], *places[2], *jobs;       // jobs[0]: how many; then the chunks in which a run that crosses a border begins
+    uint32_t *keys[2], *places[2], *n_jobs;
+    uint4 *jobs;                                // runs that cross borders: the chunk in which one begins, how many it touches, its token
     float *part;                                // [2][chunks][pitch]: runs that a chunk begins with | ends with
     uint32_t chunk, n_chunks, pitch, digit_bits, passes;
     uint32_t early_rows, fill_rows, fill_ctas, sum_ctas;   // rows cleared beside the sort; rows of a clearing CTA beside the sums, and how many of each
@@ -78,15 +79,17 @@ template <typename T, bool VEC> __device__ __forceinline__ void store_columns(T 
 }
 
 // --------------------------------------------------------------------------------------------- forward
-constexpr uint32_t kForwardSlabs = 4;           // slabs of a row in flight
+// Slabs of a row in flight, and CTAs of an SM (48 registers): 131072 rows of 2048 from binary32 153 us; without the bound (60 registers)
+// 162, two slabs 174, eight 173, one 202.
+constexpr uint32_t kForwardSlabs = 4, kForwardCtas = 5;
 
-template <typename W, typename A, bool VEC> __global__ void __launch_bounds__(kRowThreads) embedding_kernel(const __grid_constant__ EmbeddingArgs a)
+template <typename W, typename A, bool VEC> __global__ void __launch_bounds__(kRowThreads, kForwardCtas) embedding_kernel(const __grid_constant__ EmbeddingArgs a)
 {
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1u);
     const uint32_t per_row = (a.slabs + kForwardSlabs - 1u) / kForwardSlabs;
     const uint64_t items = a.n * per_row, step = (uint64_t)gridDim.x * (kRowThreads >> a.lanes_log2);
     for (uint64_t i = (uint64_t)blockIdx.x * (kRowThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2); i < items; i += step) {
-        const uint64_t t = per_row == 1u ? i : i / per_row;
+        const uint64_t t = items >> 32 ? i / per_row : (uint64_t)((uint32_t)i / per_row);
         const uint32_t slab = (uint32_t)(i - t * per_row) * kForwardSlabs;
         const long long token = token_at(a, t);
         const bool known = token >= 0 && token < (long long)a.vocabulary;
@@ -205,7 +208,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
     if (threadIdx.x == 0) {
         s.unknown = 0;
         if (rank == 0) {
-            a.jobs[0] = 0;
+            *a.n_jobs = 0;
             a.header->status = DAF_OK;
         }
     }
@@ -220,8 +223,8 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
         for (uint32_t d = lane; d < digits; d += 32u) s.count[warp][d] = 0;
         __syncwarp();
         bool unknown = false;
+        uint32_t key[4], rank_in_warp[4];                           // of the last four rounds
         for (uint64_t at = lo; at < end; at += 128u) {              // four rounds, their loads together
-            uint32_t key[4];
 #pragma unroll
             for (uint32_t j = 0; j < 4; j++) {
                 const uint64_t i = at + j * 32u + lane;
@@ -233,7 +236,8 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
             }
 #pragma unroll
             for (uint32_t j = 0; j < 4; j++)
-                if (at + j * 32u < end) place_in_warp(s.count[warp], key[j] >> shift & (digits - 1u), a.digit_bits, at + j * 32u + lane < end, lane);
+                if (at + j * 32u < end)
+                    rank_in_warp[j] = place_in_warp(s.count[warp], key[j] >> shift & (digits - 1u), a.digit_bits, at + j * 32u + lane < end, lane);
         }
         if (unknown) s.unknown = 1;
         __syncthreads();
@@ -271,12 +275,13 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
             s.base[threadIdx.x] = lower + upto - all + before;
         }
         __syncthreads();
+        const bool once = per_warp <= 128u;                         // what the first look found is still at hand
         for (uint64_t at = lo; at < end; at += 128u) {
-            uint32_t key[4], place[4];
+            uint32_t place[4];
 #pragma unroll
             for (uint32_t j = 0; j < 4; j++) {
                 const uint64_t i = at + j * 32u + lane;
-                key[j] = i < end ? key_of(i) : 0u;
+                if (!once) key[j] = i < end ? key_of(i) : 0u;
                 place[j] = i < end ? (pass ? __ldcg(a.places[from] + i) : (uint32_t)i) : 0u;
             }
 #pragma unroll
@@ -284,7 +289,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
                 if (at + j * 32u >= end) break;
                 const bool item = at + j * 32u + lane < end;
                 const uint32_t digit = key[j] >> shift & (digits - 1u);
-                const uint32_t p = place_in_warp(s.count[warp], digit, a.digit_bits, item, lane) + s.base[digit];
+                const uint32_t p = (once ? rank_in_warp[j] + s.count[warp][digit] : place_in_warp(s.count[warp], digit, a.digit_bits, item, lane)) + s.base[digit];
                 if (item) {
                     a.keys[to][p] = key[j];
                     a.places[to][p] = place[j];
@@ -489,7 +494,18 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
     if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
     const bool goes_on = run != none && run == behind;
     finish(goes_on);
-    if (goes_on && !open && slab == 0 && lane == 0) a.jobs[1u + atomicAdd(a.jobs, 1u)] = chunk;
+    if (goes_on && !open && slab == 0 && lane == 0) {
+        // the last chunk that begins with the token: most runs end soon, so in growing steps first
+        const uint32_t *const list = a.keys[last];
+        uint32_t lo = chunk + 1u, step = 1u;
+        while (lo + step < a.n_chunks && __ldg(list + (uint64_t)(lo + step) * a.chunk) == run) {
+            lo += step;
+            step *= 2u;
+        }
+        for (; step; step /= 2u)
+            if (lo + step < a.n_chunks && __ldg(list + (uint64_t)(lo + step) * a.chunk) == run) lo += step;
+        a.jobs[atomicAdd(a.n_jobs, 1u)] = make_uint4(chunk, lo - chunk + 1u, run, 0u);
+    }
 }
 
 // --------------------------------------------------------------------------------------------- backward: runs across chunks
@@ -498,24 +514,12 @@ template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) e
     constexpr uint32_t kWarps = kRowThreads / 32;
     __shared__ float s_sum[kWarps][256];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, blocks = (a.pitch + 255u) / 256u;
-    const uint32_t *keys = a.keys[(a.passes + 1u) & 1u];
     wait_for_ahead();
-    const uint64_t work = (uint64_t)a.jobs[0] * blocks;
+    const uint64_t work = (uint64_t)*a.n_jobs * blocks;
     for (uint64_t i = blockIdx.x; i < work; i += gridDim.x) {
         const uint32_t job = (uint32_t)(i / blocks), block = (uint32_t)(i - (uint64_t)job * blocks);
-        const uint32_t begin = a.jobs[1u + job], key = __ldg(keys + (uint64_t)(begin + 1u) * a.chunk);
-        // the last chunk that begins with the key, thirty-two probes at a time: it is in [lo, hi)
-        uint32_t lo = begin + 1u, hi = a.n_chunks;
-        while (hi - lo > 1u) {
-            const uint32_t step = (hi - lo + 31u) / 32u;
-            const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
-            const uint32_t yes = __ballot_sync(0xffffffffu, at < hi && __ldg(keys + at * a.chunk) == key);
-            const uint32_t most = 31u - __clz(yes);                 // lane 0 always says yes
-            const uint32_t next = lo + most * step;
-            hi = hi - next < step ? hi : next + step;
-            lo = next;
-        }
-        const uint32_t parts = lo - begin + 1u;                     // the first from the second half of the workspace
+        const uint4 run = a.jobs[job];
+        const uint32_t begin = run.x, parts = run.y, key = run.z;   // the first part from the second half of the workspace
         const uint32_t from = (uint32_t)((uint64_t)parts * warp / kWarps), to = (uint32_t)((uint64_t)parts * (warp + 1u) / kWarps);
         const uint32_t col = block * 256u + lane * 8u;
         float acc[8] = {};
@@ -601,7 +605,7 @@ static EmbeddingArgs embedding_args(const daf_embedding_params *p)
 static uint64_t grad_workspace(const EmbeddingArgs &a)
 {
     const uint64_t list = up256((uint64_t)a.n_chunks * a.chunk * sizeof(uint32_t));
-    return sizeof(WorkspaceHeader) + 4u * list + up256((a.n_chunks + 1ull) * sizeof(uint32_t)) + 2ull * a.n_chunks * a.pitch * sizeof(float);
+    return sizeof(WorkspaceHeader) + 4u * list + 256u + up256(a.n_chunks * sizeof(uint4)) + 2ull * a.n_chunks * a.pitch * sizeof(float);
 }
 
 // Wide accesses: rows of both sides start on the boundaries of eight elements.
@@ -689,8 +693,9 @@ extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, con
         a.keys[i] = reinterpret_cast<uint32_t *>(at);
         a.places[i] = reinterpret_cast<uint32_t *>(at + list);
     }
-    a.jobs = reinterpret_cast<uint32_t *>(at);
-    a.part = reinterpret_cast<float *>(at + up256((a.n_chunks + 1ull) * sizeof(uint32_t)));
+    a.n_jobs = reinterpret_cast<uint32_t *>(at);
+    a.jobs = reinterpret_cast<uint4 *>(at + 256);
+    a.part = reinterpret_cast<float *>(at + 256 + up256(a.n_chunks * sizeof(uint4)));
     if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
     int ctas = 0;                                                   // also raises the kernel's limits
     if (persistent_ctas(reinterpret_cast<const void *>(&embedding_sort_kernel), (int)kSortThreads, (int)sizeof(SortShared), &ctas) != cudaSuccess ||
