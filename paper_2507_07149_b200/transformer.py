@@ -264,7 +264,7 @@ class Muon(torch.optim.Optimizer):
     buffer = momentum * buffer + gradient, update = gradient + momentum * buffer (nesterov) or buffer, and
     p = (1 - lr * weight_decay) p - lr * sqrt(max(1, rows / columns)) * orthogonalised(update).
     Dimensions behind the first count as columns.  Buffers are float32; the matrices are orthogonalised in ``dtype``, all of a
-    group in one call."""
+    group on one device in one call."""
 
     def __init__(self, params, lr: float = 0.02, *, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5,
                  dtype=torch.bfloat16):
@@ -278,6 +278,13 @@ class Muon(torch.optim.Optimizer):
             self.param_groups.pop()
             raise ValueError("Muon: steps matrices; give vectors to another optimizer")
 
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)                         # takes states in their parameter's type
+        saved = [i for g in state_dict["param_groups"] for i in g["params"]]
+        for i, p in zip(saved, [p for g in self.param_groups for p in g["params"]]):
+            if "momentum" in state_dict["state"].get(i, {}):
+                self.state[p]["momentum"] = state_dict["state"][i]["momentum"].to(p.device, torch.float32, copy=True)
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
@@ -285,23 +292,28 @@ class Muon(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for group in self.param_groups:
-            params = [p for p in group["params"] if p.grad is not None and p.numel()]
-            if not params:
-                continue
-            grads = [p.grad.float() for p in params]
-            for p in params:
-                if "momentum" not in self.state[p]:
-                    self.state[p]["momentum"] = torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format)
-            buffers = [self.state[p]["momentum"] for p in params]
-            torch._foreach_mul_(buffers, group["momentum"])
-            torch._foreach_add_(buffers, grads)
-            updates = torch._foreach_add(grads, buffers, alpha=group["momentum"]) if group["nesterov"] else buffers
-            made = orthogonalize([u.to(group["dtype"]).contiguous() for u in updates], steps=group["steps"])
-            if group["weight_decay"]:
-                torch._foreach_mul_(params, 1.0 - group["lr"] * group["weight_decay"])
-            for p, u in zip(params, made):
-                p.add_(u, alpha=-group["lr"] * math.sqrt(max(1.0, p.shape[0] * p.shape[0] / p.numel())))
+            devices = {}
+            for p in group["params"]:
+                if p.grad is not None and p.numel():
+                    devices.setdefault(p.device, []).append(p)
+            for params in devices.values():
+                self._step(params, group)
         return loss
+
+    def _step(self, params, group):
+        grads = [p.grad.float() for p in params]
+        for p in params:
+            if "momentum" not in self.state[p]:
+                self.state[p]["momentum"] = torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format)
+        buffers = [self.state[p]["momentum"] for p in params]
+        torch._foreach_mul_(buffers, group["momentum"])
+        torch._foreach_add_(buffers, grads)
+        updates = torch._foreach_add(grads, buffers, alpha=group["momentum"]) if group["nesterov"] else buffers
+        made = orthogonalize([u.to(group["dtype"]).contiguous() for u in updates], steps=group["steps"])
+        if group["weight_decay"]:
+            torch._foreach_mul_(params, 1.0 - group["lr"] * group["weight_decay"])
+        for p, u in zip(params, made):
+            p.add_(u, alpha=-group["lr"] * math.sqrt(max(1.0, p.shape[0] * p.shape[0] / p.numel())))
 
 
 def train_language(steps: int = 20, *, compressed: bool = True, bit_budget: float = 8.0, batch: int = 16, tokens: int = 256, vocabulary: int = 4096,

@@ -176,8 +176,23 @@ def test_muon_steps_by_its_formula():
             assert (p.double() - w).norm() <= 2e-2 * (w - b).norm() * (step + 1)
     with pytest.raises(ValueError):
         tr.Muon([torch.nn.Parameter(torch.zeros(4, device="cuda"))])
-    state = opt.state_dict()
-    tr.Muon(ps, 0.1).load_state_dict(state)
+
+
+def test_muon_keeps_its_momentum_in_32_bits_through_a_checkpoint():
+    torch.manual_seed(8)
+    ps = [torch.nn.Parameter(torch.randn(16, 24, device="cuda").bfloat16()) for _ in range(2)]
+    opt = tr.Muon(ps, 0.1)
+    ps[0].grad = torch.randn_like(ps[0])                            # the other one has no gradient yet
+    for _ in range(3):
+        opt.step()
+    kept = opt.state[ps[0]]["momentum"].clone()
+    assert kept.dtype == torch.float32 and ps[1] not in opt.state
+    other = tr.Muon(ps, 0.5)
+    other.load_state_dict(opt.state_dict())
+    got = other.state[ps[0]]["momentum"]
+    assert got.dtype == torch.float32 and torch.equal(got, kept) and got.data_ptr() != opt.state[ps[0]]["momentum"].data_ptr()
+    assert other.param_groups[0]["lr"] == 0.1
+    other.step()
 
 
 @pytest.mark.parametrize("bits", [None, 8.0, 4.0])

@@ -100,6 +100,16 @@ def test_one_step_element_by_element(shape, dtype):
     assert ((got.double() - want).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("shape,dtype", [((1, 65536), "f32"), ((65536, 2), "bf16"), ((40000, 24), "f16"), ((24, 16000), "f32")], ids=lambda s: str(s))
+def test_long_sides(shape, dtype):
+    """As above; sums in segments keep binary32's loss per addition from adding up, float16 takes them above 8192."""
+    g = gradient(shape, dtype, 7, "flat")
+    got, = daf.orthogonalize([g], check=True)
+    want = exact(g)
+    segments = 100 * 2.0 ** -23 * (max(shape) / 16 if dtype == "bf16" else 8 + max(shape) ** 0.5 / 16)
+    assert apart(got, want) <= torch.finfo(g.dtype).eps / 2 + 2 * apart(model(g, 1 if dtype == "bf16" else 2), want) + segments
+
+
 def test_singular_values_end_near_one():
     for shape in ((768, 2304), (900, 500)):
         got, = daf.orthogonalize([gradient(shape, "bf16", 1, "flat")])
