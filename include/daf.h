@@ -542,7 +542,8 @@ daf_status daf_rotary_norm_grad(const daf_rotary_params *params, const double *f
  * elements; d_out[i] may be d_in[i], otherwise nothing overlaps.  Results have their input's type.
  * Arithmetic: products of 16-bit operands on the tensor cores, summed in binary32; the norm is summed in binary64.  DAF_BF16: x and
  * its Gram matrices are held in float16 between the products (x behind the first two steps with 22 bits where it is added), whose
- * effect is below the result's own rounding; DAF_F16 and DAF_F32: in two float16 parts (22 bits) throughout.  Entries
+ * effect is below the result's own rounding; DAF_F16 and DAF_F32, and DAF_BF16 up to 32 rows or columns: in two float16 parts (22 bits)
+ * throughout.  Entries
  * below 2^-24 of a matrix's norm lose bits.  On the way x must stay below 7 in magnitude, x x^T and b (x x^T) + c (x x^T)^2 below 15
  * (the default coefficients keep them below 1.3, 1.6 and 2.9), otherwise the result is not finite; neither is it for a matrix with an
  * element that is not.  The same matrices give the same bits, alone or with others.

@@ -32,7 +32,7 @@ struct EmbeddingArgs {
     long long padding;
     // backward
     uint32_t *keys[2], *places[2], *n_jobs;
-    uint4 *jobs;                                // runs that cross borders: the chunk in which one begins, how many it touches, its token
+    uint4 *jobs;                                // runs that cross borders: the chunk in which one begins, how many it touches (0: more than two), its token
     float *part;                                // [2][chunks][pitch]: runs that a chunk begins with | ends with
     uint32_t chunk, n_chunks, pitch, digit_bits, passes;
     uint32_t early_rows, fill_rows, fill_ctas, sum_ctas;   // rows cleared beside the sort; rows of a clearing CTA beside the sums, and how many of each
@@ -314,7 +314,7 @@ constexpr uint32_t kSumBytes = 256;             // of a thread, for both blocks
 template <typename A, bool VEC> struct RowBlock {
     static constexpr int kRows = VEC ? (int)(kSumBytes / 2u / (8u * sizeof(A))) : 8, kAccesses = (int)sizeof(A) / 2;
     uint32_t place;                             // of the thread's first 16 bytes
-    float x[VEC ? 1 : kRows][8];
+    A x[VEC ? 1 : kRows][8];
     __device__ __forceinline__ void fetch(int half, int j, const A *row, uint32_t first, uint32_t lanes, uint32_t width)
     {
         if constexpr (VEC) {
@@ -323,7 +323,9 @@ template <typename A, bool VEC> struct RowBlock {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + ((half * kRows + j) * kAccesses + i) * kRowThreads * 16u),
                              "l"(reinterpret_cast<const char *>(row + first) + 16 * i) : "memory");
         } else {
-            load_columns<A, false>(row, first, lanes, width, x[j]);
+            // all of them together, whatever is behind the row's end or belongs to no token: nothing may wait for one of the loads
+#pragma unroll
+            for (uint32_t e = 0; e < kLaneCols; e++) x[j][e] = row[first + lanes * e < width ? first + lanes * e : width - 1u];
         }
     }
     __device__ __forceinline__ void take(int half, int j, float (&y)[8]) const
@@ -342,7 +344,7 @@ template <typename A, bool VEC> struct RowBlock {
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) y[e] = x[j][e];
+            for (int e = 0; e < 8; e++) y[e] = get1(x[j][e]);
         }
     }
 };
@@ -450,7 +452,7 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
         list(places + i, place);
 #pragma unroll
         for (int j = 0; j < kRows; j++)
-            if (mine && next[j] != none) block.fetch(half, j, grad + (uint64_t)place[j] * a.width, col, lanes, a.width);
+            if (!VEC || (mine && next[j] != none)) block.fetch(half, j, grad + (uint64_t)place[j] * a.width, col, lanes, a.width);
     };
     list(keys, next);
     if (VEC) {
@@ -495,16 +497,9 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
     const bool goes_on = run != none && run == behind;
     finish(goes_on);
     if (goes_on && !open && slab == 0 && lane == 0) {
-        // the last chunk that begins with the token: most runs end soon, so in growing steps first
-        const uint32_t *const list = a.keys[last];
-        uint32_t lo = chunk + 1u, step = 1u;
-        while (lo + step < a.n_chunks && __ldg(list + (uint64_t)(lo + step) * a.chunk) == run) {
-            lo += step;
-            step *= 2u;
-        }
-        for (; step; step /= 2u)
-            if (lo + step < a.n_chunks && __ldg(list + (uint64_t)(lo + step) * a.chunk) == run) lo += step;
-        a.jobs[atomicAdd(a.n_jobs, 1u)] = make_uint4(chunk, lo - chunk + 1u, run, 0u);
+        // most such runs end in the next chunk; the others' ends are looked for by those who join them (0)
+        const bool on = chunk + 2u < a.n_chunks && __ldg(keys + 2u * a.chunk) == run;
+        a.jobs[atomicAdd(a.n_jobs, 1u)] = make_uint4(chunk, on ? 0u : 2u, run, 0u);
     }
 }
 
@@ -519,12 +514,26 @@ template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) e
     for (uint64_t i = blockIdx.x; i < work; i += gridDim.x) {
         const uint32_t job = (uint32_t)(i / blocks), block = (uint32_t)(i - (uint64_t)job * blocks);
         const uint4 run = a.jobs[job];
-        const uint32_t begin = run.x, parts = run.y, key = run.z;   // the first part from the second half of the workspace
+        const uint32_t begin = run.x, key = run.z;                  // the first part comes from the second half of the workspace
+        uint32_t parts = run.y;
+        if (parts == 0u) {                                          // the last chunk that begins with the key is in [lo, hi): 32 probes at a time
+            const uint32_t *keys = a.keys[(a.passes + 1u) & 1u];
+            uint32_t lo = begin + 2u, hi = a.n_chunks;
+            while (hi - lo > 1u) {
+                const uint32_t step = (hi - lo + 31u) / 32u;
+                const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
+                const uint32_t yes = __ballot_sync(0xffffffffu, at < hi && __ldg(keys + at * a.chunk) == key);
+                const uint32_t next = lo + (31u - __clz(yes)) * step;       // lane 0 always says yes
+                hi = hi - next < step ? hi : next + step;
+                lo = next;
+            }
+            parts = lo - begin + 1u;
+        }
         const uint32_t from = (uint32_t)((uint64_t)parts * warp / kWarps), to = (uint32_t)((uint64_t)parts * (warp + 1u) / kWarps);
         const uint32_t col = block * 256u + lane * 8u;
         float acc[8] = {};
         if (col < a.pitch) {
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t p = from; p < to; p++) {
                 float x[8];
                 Elem<float>::load8(a.part + ((uint64_t)(p ? 0u : a.n_chunks) + begin + p) * a.pitch + col, x);
@@ -562,11 +571,12 @@ static daf_status check_embedding(const daf_embedding_params *p)
     return DAF_OK;
 }
 
-// Lanes of a row: as many as its units of eight columns, a power of two, 32 at most.
-static void row_shape(EmbeddingArgs *a)
+// Lanes of a row: as many as its units of eight columns, a power of two, 32 at most.  The sums of rows that cannot be read in wide
+// accesses take a warp to a row: 37202 tokens of 28 columns 20 us on four lanes a row (few warps, many small accesses each).
+static void row_shape(EmbeddingArgs *a, bool backward)
 {
     const uint32_t units = (a->width + kLaneCols - 1u) / kLaneCols;
-    a->lanes_log2 = 0;
+    a->lanes_log2 = backward && a->width % kLaneCols ? 5u : 0u;
     while (a->lanes_log2 < 5u && (1u << a->lanes_log2) < units) a->lanes_log2++;
     const uint32_t cols = kLaneCols << a->lanes_log2;
     a->slabs = (a->width + cols - 1u) / cols;
@@ -585,7 +595,7 @@ static void chunk_shape(EmbeddingArgs *a)
 
 static uint64_t up256(uint64_t n) { return (n + 255u) & ~255ull; }
 
-static EmbeddingArgs embedding_args(const daf_embedding_params *p)
+static EmbeddingArgs embedding_args(const daf_embedding_params *p, bool backward)
 {
     EmbeddingArgs a = {};
     a.n = p->tokens;
@@ -594,7 +604,7 @@ static EmbeddingArgs embedding_args(const daf_embedding_params *p)
     a.width = p->width;
     a.scale = p->scale;
     a.padding = p->padding;
-    row_shape(&a);
+    row_shape(&a, backward);
     chunk_shape(&a);
     uint32_t bits = 32u - (uint32_t)__builtin_clz(a.vocabulary);
     a.passes = (bits + kDigitBits - 1u) / kDigitBits;
@@ -631,7 +641,7 @@ template <typename W, typename A, bool VEC> static daf_status backward(const Emb
     if (launch_behind(sum, a.sum_ctas + a.fill_ctas, kRowThreads, smem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
     const uint64_t most = (uint64_t)a.n_chunks * ((a.pitch + 255u) / 256u);
     const auto join = &embedding_join_kernel<W, VEC>;
-    return launch_behind(join, (uint32_t)(most < 148u * 4u ? most : 148u * 4u), kRowThreads, 0, s, a) == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+    return launch_behind(join, (uint32_t)(most < 148u * 8u ? most : 148u * 8u), kRowThreads, 0, s, a) == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }
 template <bool BACK, bool VEC> static daf_status by_type(uint32_t table, uint32_t act, const EmbeddingArgs &a, cudaStream_t s)
 {
@@ -655,7 +665,7 @@ extern "C" daf_status daf_embedding(const daf_embedding_params *params, const vo
     if (params->tokens == 0) return DAF_OK;
     if (!on_elements(d_tokens, params->token_bytes) || !on_elements(d_weight, elem_bytes(params->table_dtype)) || !on_elements(d_out, elem_bytes(params->dtype)))
         return DAF_ERR_INVALID_ARG;
-    EmbeddingArgs a = embedding_args(params);
+    EmbeddingArgs a = embedding_args(params, false);
     a.tokens = d_tokens;
     a.weight = d_weight;
     a.out = d_out;
@@ -668,7 +678,7 @@ extern "C" daf_status daf_embedding(const daf_embedding_params *params, const vo
 
 extern "C" uint64_t daf_embedding_grad_workspace(const daf_embedding_params *params)
 {
-    return check_embedding(params) == DAF_OK ? grad_workspace(embedding_args(params)) : 0;
+    return check_embedding(params) == DAF_OK ? grad_workspace(embedding_args(params, true)) : 0;
 }
 
 extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_tokens, const void *d_grad_out, void *d_grad_weight,
@@ -680,7 +690,7 @@ extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, con
     if (!on_elements(d_grad_weight, elem_bytes(p.table_dtype)) || !on_elements(d_workspace, 32u) ||
         (p.tokens && (!on_elements(d_tokens, p.token_bytes) || !on_elements(d_grad_out, elem_bytes(p.dtype)))))
         return DAF_ERR_INVALID_ARG;
-    EmbeddingArgs a = embedding_args(params);
+    EmbeddingArgs a = embedding_args(params, true);
     if (workspace_bytes < grad_workspace(a)) return DAF_ERR_CAPACITY;
     a.tokens = d_tokens;
     a.grad_out = d_grad_out;

@@ -48,7 +48,7 @@ struct OrthGroup {                              // matrices of one shape and typ
     uint64_t x_plane, m_plane;                  // elements of a plane
     uint32_t r, c, m, x_pitch, m_pitch, tall, planes, count, first, dtype;
     uint32_t sym_tiles, sym_cols, sym_n, upd_tiles, upd_rows, upd_n;     // of one matrix; columns of a tile
-    uint32_t sym_first, upd_first, prep_ctas, prep_first, segment;    // segment: two parts, copies summed in tensor memory at a time
+    uint32_t sym_first, upd_first, prep_ctas, prep_first;
 };
 struct OrthArgs {
     OrthGroup g[kOrthGroups];
@@ -471,7 +471,8 @@ __device__ __forceinline__ void take_away(float (&x)[32], const uint4 (&v)[4])
         }
     }
 }
-template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
+// SEGMENTS: two parts throughout, sums added up in registers every kOrthSegment copies; else as many parts as the group has.
+template <bool SEGMENTS> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthThreads, 1) orthogonalize_kernel(const __grid_constant__ OrthArgs a)
 {
     extern __shared__ __align__(1024) unsigned char s_raw[];
     struct Bars {
@@ -559,12 +560,13 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                 const int lines = (int)(second ? t.col + width / 2u * rank : t.row + 128u * rank);
                 // x, held in two planes, or a symmetric matrix, in as many as the group's products take
                 const bool of_x = t.kind == kGram || (t.kind == kUpdate && second != (g.tall != 0u));
-                const int matrix = (int)(t.matrix * (of_x ? 2u : (uint32_t)PLANES));
+                const uint32_t planes = SEGMENTS ? 2u : g.planes;
+                const int matrix = (int)(t.matrix * (of_x ? 2u : planes));
                 const uint32_t to = smem_u32(stages) + (second ? 2u * kOrthBox : 0u), bytes = 2u * (2u * kOrthBox + width / 128u * kOrthBox);
                 bool ok = true;
                 const auto copy = [&](const CUtensorMap *map, bool across, int from, int end) {
                     for (int k = from; k < end; k += 64)
-                        for (uint32_t part = 0; part < (uint32_t)PLANES; part++) {
+                        for (uint32_t part = 0; part < planes; part++) {
                             if (issued >= kOrthStages && !(ok = bar_wait(&bars.empty[st], ph ^ 1u, stop))) return;
                             if (counts) bar_expect(&bars.full[st], bytes);
                             pair_load(to + st * kOrthStage, map, in_cta(&bars.full[st], 0), across ? 0 : k, across ? k : lines, across ? lines / 64 : 0, matrix + (int)part);
@@ -597,6 +599,18 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
         const auto step_on = [&]() {
             if (++st == kOrthStages) st = 0, ph ^= 1u;
         };
+        // the large parts of one operand with the small ones of the other, which lie in the stage `st`
+        const auto small_parts = [&](uint32_t la, uint32_t lb, uint32_t step_a, uint32_t step_b, uint32_t desc, uint32_t to, bool add) {
+            const uint32_t at = smem_u32(stages + st * kOrthStage);
+            const uint32_t sa = operand_low(at, kOrthBox), sb = operand_low(at + 2u * kOrthBox, kOrthBox);
+            pair_product(one, to, la, sb, desc, add);
+            pair_product<true>(one, to, sa, lb, desc);
+#pragma unroll
+            for (uint32_t s = 1; s < 4u; s++) {
+                pair_product<true>(one, to, la + s * step_a, sb + s * step_b, desc);
+                pair_product<true>(one, to, sa + s * step_a, lb + s * step_b, desc);
+            }
+        };
         for (uint32_t n = 0;; n++) {
             const uint32_t slot = n % kOrthSlots, buf = n & 1u;
             if (!bar_wait(&bars.told[slot], n / kOrthSlots & 1u, stop)) break;
@@ -619,21 +633,29 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                 const uint32_t step_a = ca ? 128u : 2u, step_b = cb ? 128u : 2u, desc = plain | (ca ? 1u << 15 : 0u) | (cb ? 1u << 16 : 0u);
                 const uint32_t at = smem_u32(stages + st * kOrthStage);
                 const uint32_t la = operand_low(at, kOrthBox), lb = operand_low(at + 2u * kOrthBox, kOrthBox);
-                if constexpr (PLANES == 1) {
+                if constexpr (!SEGMENTS) {
                     pair_product(one, d, la, lb, desc, k > 0);
 #pragma unroll
                     for (uint32_t s = 1; s < 4u; s++) pair_product<true>(one, d, la + s * step_a, lb + s * step_b, desc);
+                    if (g.planes == 2u) {                           // the stage behind holds the small parts
+                        uint64_t *const first = &bars.empty[st];
+                        step_on();
+                        if (!(ok = wait_from_pair(&bars.full[st], ph, stop))) break;
+                        tmem_after_sync();
+                        small_parts(la, lb, step_a, step_b, desc, d + 128u, k > 0);
+                        pair_done(one, first, 3u);
+                    }
                 } else {
                     // The large parts' products, a segment at a time: the accumulator cuts every sum at its last place, so results add segments
                     // up in registers.  The stage behind holds the small parts; their products have an accumulator for the whole tile.
                     const uint32_t main = tmem + (segment & 1u) * 128u, cross = tmem + 256u + buf * 128u;
-                    const bool begins = k % g.segment == 0;
+                    const bool begins = k % kOrthSegment == 0;
                     if (begins && segment >= 2u && !(ok = wait_from_pair(&bars.seg_empty[segment & 1u], (segment / 2u - 1u) & 1u, stop))) break;
                     if (begins) tmem_after_sync();
                     pair_product(one, main, la, lb, desc, !begins);
 #pragma unroll
                     for (uint32_t s = 1; s < 4u; s++) pair_product<true>(one, main, la + s * step_a, lb + s * step_b, desc);
-                    if (k % g.segment == g.segment - 1u || k + 1u == rounds) {
+                    if (k % kOrthSegment == kOrthSegment - 1u || k + 1u == rounds) {
                         pair_done(one, &bars.seg_full[segment & 1u], 3u);
                         segment++;
                     }
@@ -641,15 +663,7 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                     step_on();
                     if (!(ok = wait_from_pair(&bars.full[st], ph, stop))) break;
                     tmem_after_sync();
-                    const uint32_t small = smem_u32(stages + st * kOrthStage);
-                    const uint32_t sa = operand_low(small, kOrthBox), sb = operand_low(small + 2u * kOrthBox, kOrthBox);
-                    pair_product(one, cross, la, sb, desc, k > 0);
-                    pair_product<true>(one, cross, sa, lb, desc);
-#pragma unroll
-                    for (uint32_t s = 1; s < 4u; s++) {
-                        pair_product<true>(one, cross, la + s * step_a, sb + s * step_b, desc);
-                        pair_product<true>(one, cross, sa + s * step_a, lb + s * step_b, desc);
-                    }
+                    small_parts(la, lb, step_a, step_b, desc, cross, k > 0);
                     pair_done(one, first, 3u);
                 }
                 pair_done(one, &bars.empty[st], 3u);
@@ -673,17 +687,17 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
             if (t.kind == kNoTile) break;
             const OrthGroup &g = a.g[t.group];
             const bool update = t.kind == kUpdate, gram = t.kind == kGram, last = t.step + 1u == a.steps;
-            const uint32_t chunks = PLANES == 2 ? 2u : t.width(g) / 64u, row = t.row + 128u * rank + quarter * 32u;
+            const uint32_t planes = SEGMENTS ? 2u : g.planes, chunks = SEGMENTS ? 2u : t.width(g) / 64u, row = t.row + 128u * rank + quarter * 32u;
             const uint32_t rows = update ? g.r : g.m, pitch = update ? g.x_pitch : g.m_pitch, matrix = g.first + t.matrix;
             const float k = __ldcg(a.scale + matrix);
             // what is added to the product, and factors of both
-            const __half *with = update ? g.x_at[t.step & 1u] + (uint64_t)t.matrix * 2u * g.x_plane : g.gram_at + (uint64_t)t.matrix * (uint32_t)PLANES * g.m_plane;
+            const __half *with = update ? g.x_at[t.step & 1u] + (uint64_t)t.matrix * 2u * g.x_plane : g.gram_at + (uint64_t)t.matrix * planes * g.m_plane;
             const uint64_t plane = update ? g.x_plane : g.m_plane;
-            const bool two = PLANES == 2 || (update && (t.step == 1u || t.step == 2u));
+            const bool two = planes == 2u || (update && (t.step == 1u || t.step == 2u));
             const float of_product = gram ? __fdiv_rn(kHeld, k * k) : t.kind == kPoly ? a.c / kHeld : 1.0f / kHeld;
             const float of_with = update ? a.a : a.b;
             __half *to = update ? g.x_at[(t.step + 1u) & 1u] + (uint64_t)t.matrix * 2u * g.x_plane
-                                : (gram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * (uint32_t)PLANES * g.m_plane;
+                                : (gram ? g.gram_at : g.poly_at) + (uint64_t)t.matrix * planes * g.m_plane;
             OrthBlock ahead, ahead2;                                // of the next 32 columns, on their way during the products
             const auto look_ahead = [&](uint32_t j) {
                 if (gram) return;
@@ -697,7 +711,7 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                 const uint32_t col = t.col + (half * chunks + j) * 32u;
                 if (row >= rows || col >= pitch) return;
                 OrthBlock w, w2;
-                if constexpr (PLANES == 1) {
+                if constexpr (!SEGMENTS) {
                     w = ahead;
                     w2 = ahead2;
                     look_ahead(j + 1u);
@@ -705,7 +719,7 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
 #pragma unroll
                 for (int i = 0; i < 32; i++) x[i] *= of_product;
                 if (!gram) {
-                    OrthBlock &high = PLANES == 1 ? w : ahead, &low = PLANES == 1 ? w2 : ahead2;
+                    OrthBlock &high = !SEGMENTS ? w : ahead, &low = !SEGMENTS ? w2 : ahead2;
                     if (two) {
                         low.to_rows(stage, lane);
                         low.add(x, of_with);
@@ -713,7 +727,7 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                     high.to_rows(stage, lane);
                     high.add(x, of_with);
                 }
-                if constexpr (PLANES == 2) look_ahead(j + 1u);      // here: before it there are no registers to be had
+                if constexpr (SEGMENTS) look_ahead(j + 1u);         // here: before it there are no registers to be had
                 if (update && last) {
                     const float by = __fdiv_rn(1.0f, k);
 #pragma unroll
@@ -746,16 +760,16 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                                 *reinterpret_cast<const uint16_t *>(stage + r * 64u + (((lane >> 3) ^ (r >> 1 & 3u)) * 16u) + (lane & 7u) * 2u);
                     return;
                 }
-                const uint32_t planes = PLANES == 2 || (update && t.step < 2u) ? 2u : 1u;
-                for (uint32_t p = 0; p < planes; p++) {
+                const uint32_t kept = planes == 2u || (update && t.step < 2u) ? 2u : 1u;
+                for (uint32_t p = 0; p < kept; p++) {
                     round32<__half>(x, w.v);
-                    if (p + 1u < planes) take_away(x, w.v);
+                    if (p + 1u < kept) take_away(x, w.v);
                     w.to_quarters(stage, lane);
                     w.store(to + p * plane, pitch, row, rows, col, pitch, lane);
                 }
             };
             const uint32_t own = (half * chunks) * 32u + (quarter << 21);                      // the warp's first column, its lanes
-            if constexpr (PLANES == 1) {
+            if constexpr (!SEGMENTS) {
                 if (!bar_wait(&bars.acc_full[buf], n / 2u & 1u, stop)) break;
                 tmem_after_sync();
                 for (uint32_t j = 0; j < chunks; j++) {
@@ -763,6 +777,13 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                     __syncwarp();
                     tmem_load32(tmem + buf * 256u + own + j * 32u, x);
                     tmem_wait_loads();
+                    if (planes == 2u) {                             // the small parts' products
+                        float small[32];
+                        tmem_load32(tmem + buf * 256u + 128u + own + j * 32u, small);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (int i = 0; i < 32; i++) x[i] += small[i];
+                    }
                     block(j, x);
                 }
             } else {
@@ -776,7 +797,7 @@ template <int PLANES> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                         for (int i = 0; i < 32; i++) x[j][i] += part[i];
                     }
                 };
-                const uint32_t rounds = (OrthOperands::of(g, t).keys + 63u) / 64u, segments = (rounds + g.segment - 1u) / g.segment;
+                const uint32_t rounds = (OrthOperands::of(g, t).keys + 63u) / 64u, segments = (rounds + kOrthSegment - 1u) / kOrthSegment;
                 bool ok = true;
                 for (uint32_t i = 0; i < segments; i++, segment++) {
                     if (!(ok = bar_wait(&bars.seg_full[segment & 1u], segment / 2u & 1u, stop))) break;
@@ -839,11 +860,16 @@ static uint32_t orth_sym_tiles(uint32_t m, uint32_t width)
     return tiles;
 }
 
-static uint32_t orth_planes(uint32_t dtype) { return dtype == DAF_BF16 ? 1u : 2u; }
+// Parts of a matrix's operands.  With few rows roundings do not average out: one row's polynomial is one number, and five steps with it in
+// one part are up to 4e-3 off; so small matrices take two, which costs them nothing to speak of.
+static uint32_t orth_planes(uint32_t dtype, uint32_t rows, uint32_t cols) { return dtype == DAF_BF16 && rows > 32u && cols > 32u ? 1u : 2u; }
+// Whether sums are taken in segments.
+static bool orth_segments(uint32_t dtype, uint64_t rows, uint64_t cols) { return dtype == DAF_F32 || (dtype == DAF_F16 && (rows > 8192u || cols > 8192u)); }
 
-// The next matrices of `planes` parts that go together, from *next on: the table without pointers to the workspace, and the bytes it needs.
+// The next matrices, of those that take segments or of the others, that go together, from *next on: the table without pointers to
+// the workspace, and the bytes it needs.
 static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t n, const uint32_t *dtypes, const uint64_t *rows, const uint64_t *cols,
-                       uint32_t planes, uint32_t *next, uint32_t *index, uint64_t *workspace)
+                       bool segments, uint32_t *next, uint32_t *index, uint64_t *workspace)
 {
     struct Shape {
         uint32_t r, c, dtype, count, rank;
@@ -854,7 +880,7 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     a->groups = a->matrices = 0;
     for (; *next < n && a->matrices < kOrthMatrices; ++*next) {
         const uint32_t i = *next, r = (uint32_t)rows[i], c = (uint32_t)cols[i];
-        if (r == 0 || c == 0 || orth_planes(dtypes[i]) != planes) continue;
+        if (r == 0 || c == 0 || orth_segments(dtypes[i], r, c) != segments) continue;
         if (elems && elems + (uint64_t)r * c > kOrthBatch) break;
         uint32_t k = 0;
         while (k < a->groups && (shape[k].r != r || shape[k].c != c || shape[k].dtype != dtypes[i])) k++;
@@ -890,7 +916,8 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     a->prep_total = 0;
     // Columns of a tile, 256 or 128, as what takes less by what was measured: a wave of tiles takes 0.31 or 0.29 us for 64 of the
     // longest summed dimension, or as long as its results where that is more (3.5 or 1.8 us of a symmetric matrix, 6.5 or 2.7 of an
-    // update), and once the other.  Matrices in two parts take 128: the small parts' products and segments fill the rest of tensor memory.
+    // update), and once the other.  Matrices in two parts take 128: the small parts' products and segments fill the rest of tensor memory
+    // (and 256 with all products in one accumulator was slower, 426 us against 403 for the set of 768 and 2304 in float16).
     const auto width = [&](bool update) {
         double cost[2] = {0.0, 0.0};
         for (int i = 0; i < 2; i++) {
@@ -899,6 +926,7 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
             uint32_t keys = 0;
             for (uint32_t k = 0; k < a->groups; k++) {
                 const uint32_t r = a->g[k].r, c = a->g[k].c, m = r < c ? r : c, n = r < c ? c : r;
+                if (orth_planes(a->g[k].dtype, r, c) == 2u) continue;
                 tiles += (uint64_t)a->g[k].count * (update ? (uint64_t)((r + kOrthRows - 1u) / kOrthRows) * ((c + w - 1u) / w) : orth_sym_tiles(m, w));
                 keys = keys > (update ? m : n) ? keys : update ? m : n;
             }
@@ -906,7 +934,7 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
             const double more = products > results ? products : results, waves = (double)((tiles + 73u) / 74u);
             cost[i] = waves * more + products + results - more;
         }
-        return planes == 2u || cost[1] < cost[0] ? 128u : 256u;
+        return cost[1] < cost[0] ? 128u : 256u;
     };
     const uint32_t sym_n = width(false), upd_n = width(true);
     uint32_t sym = 0, upd = 0;
@@ -915,18 +943,17 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
         OrthGroup &g = a->g[k];
         g.tall = g.r > g.c;
         g.m = g.tall ? g.c : g.r;
-        g.planes = planes;
-        g.segment = g.dtype == DAF_F16 && g.r <= 8192u && g.c <= 8192u ? 1024u : kOrthSegment;
+        g.planes = orth_planes(g.dtype, g.r, g.c);
         g.x_pitch = (uint32_t)up_to(g.c, 64u);
         g.m_pitch = (uint32_t)up_to(g.m, 64u);
         g.x_plane = (uint64_t)g.r * g.x_pitch;
         g.m_plane = (uint64_t)g.m * g.m_pitch;
-        g.sym_n = sym_n;
-        g.upd_n = upd_n;
-        g.sym_cols = (g.m + sym_n - 1u) / sym_n;
-        g.sym_tiles = orth_sym_tiles(g.m, sym_n);
+        g.sym_n = g.planes == 2u ? 128u : sym_n;
+        g.upd_n = g.planes == 2u ? 128u : upd_n;
+        g.sym_cols = (g.m + g.sym_n - 1u) / g.sym_n;
+        g.sym_tiles = orth_sym_tiles(g.m, g.sym_n);
         g.upd_rows = (g.r + kOrthRows - 1u) / kOrthRows;
-        g.upd_tiles = g.upd_rows * ((g.c + upd_n - 1u) / upd_n);
+        g.upd_tiles = g.upd_rows * ((g.c + g.upd_n - 1u) / g.upd_n);
         g.sym_first = sym;
         g.upd_first = upd;
         sym += g.count * g.sym_tiles;
@@ -996,10 +1023,10 @@ extern "C" uint64_t daf_orthogonalize_workspace(const daf_orthogonalize_params *
     uint64_t most = sizeof(WorkspaceHeader);
     uint32_t index[kOrthMatrices];
     OrthArgs a;
-    for (uint32_t planes = 1; planes <= 2u; planes++)
+    for (const bool segments : {false, true})
         for (uint32_t next = 0; next < n;) {
             uint64_t bytes = 0;
-            orth_batch(&a, params, n, dtypes, rows, cols, planes, &next, index, &bytes);
+            orth_batch(&a, params, n, dtypes, rows, cols, segments, &next, index, &bytes);
             if (bytes > most) most = bytes;
         }
     return most;
@@ -1022,11 +1049,11 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
     uint32_t index[kOrthMatrices];
     OrthArgs a;
     bool any = false;
-    for (uint32_t planes = 1; planes <= 2u; planes++) {
-        const auto kernel = planes == 1u ? &orthogonalize_kernel<1> : &orthogonalize_kernel<2>;
+    for (const bool segments : {false, true}) {
+        const auto kernel = segments ? &orthogonalize_kernel<true> : &orthogonalize_kernel<false>;
         for (uint32_t next = 0; next < n;) {
             uint64_t bytes = 0;
-            orth_batch(&a, params, n, dtypes, rows, cols, planes, &next, index, &bytes);
+            orth_batch(&a, params, n, dtypes, rows, cols, segments, &next, index, &bytes);
             if (a.matrices == 0) break;
             int ctas = 0;
             if (persistent_ctas(reinterpret_cast<const void *>(kernel), (int)kOrthThreads, (int)kOrthSmem, &ctas) != cudaSuccess) return DAF_ERR_CUDA;
