@@ -544,7 +544,7 @@ static daf_status check_rotary(const daf_rotary_params *p, const double *frequen
         return DAF_ERR_INVALID_ARG;
     if (p->head_dim == 0 || p->head_dim % 8u || p->rotary_dim % 8u || p->rotary_dim > p->head_dim || p->heads == 0) return DAF_ERR_SHAPE;
     if (p->head_dim > kRotaryMaxDim || p->tokens > (1u << 24) || p->heads > 65535u || p->kv_heads > 65535u ||
-        (uint64_t)p->batch * p->tokens * (p->heads > p->kv_heads ? p->heads : p->kv_heads) > 0x3FFFFFFFull)
+        (uint64_t)p->batch * p->tokens > 0x3FFFFFFFull / (p->heads > p->kv_heads ? p->heads : p->kv_heads))       // heads > 0; the product may pass 2^64
         return DAF_ERR_UNSUPPORTED;
     if (frequencies)
         for (uint32_t i = 0; i < p->rotary_dim / 2u; i++)

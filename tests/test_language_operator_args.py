@@ -79,7 +79,8 @@ def rotary_grad(p, f=None, *, q=A, k=A, wq=A, wk=A, at=A, gqo=A, gko=A, gq=A, gk
     (dict(shared_positions=2), INV), (dict(base=0.0), INV), (dict(base=math.inf), INV), (dict(eps=-1.0), INV), (dict(eps=math.nan), INV),
     (dict(reserved=(0, 0, 1)), INV), (dict(head_dim=60), SHAPE), (dict(head_dim=0), SHAPE), (dict(rotary_dim=20), SHAPE), (dict(rotary_dim=72), SHAPE),
     (dict(heads=0), SHAPE), (dict(head_dim=264, rotary_dim=64), UNS), (dict(tokens=2 ** 24 + 1), UNS), (dict(heads=65536), UNS),
-    (dict(batch=2 ** 20, tokens=2 ** 10), UNS)])
+    (dict(batch=2 ** 20, tokens=2 ** 10), UNS),
+    (dict(batch=2 ** 31, tokens=2 ** 24, heads=512), UNS), (dict(batch=2 ** 31, tokens=2 ** 24, kv_heads=512), UNS)])
 def test_rotary_parameters(change, status):
     p = rotary_params(**change)
     assert rotary(p) == status and rotary_grad(p) == status
