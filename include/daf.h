@@ -454,7 +454,7 @@ daf_status daf_clip_norm_batch(uint32_t n, const uint32_t *dtypes, const void *c
 /*
  * Token embedding: out[t] = scale * weight[token[t]], rounded once to dtype; and its gradient
  *   grad_weight[v] = scale * sum over the t with token[t] == v of grad_out[t], zero for rows that no token names,
- * summed in binary32 in the order of t (within pieces of a fixed length, and these in order), rounded once to table_dtype.
+ * summed in binary32 in the order of t (within pieces of the list, and these in order), rounded once to table_dtype.
  *   d_tokens : `tokens` signed integers of token_bytes;  d_weight, d_grad_weight : [vocabulary, width] of table_dtype;
  *   d_out, d_grad_out : [tokens, width] of dtype; all contiguous, pointers on the boundary of their elements (faster: width a
  *   multiple of 8 and both matrices on the boundary of 8 elements).  table_dtype is dtype or DAF_F32.

@@ -36,6 +36,7 @@ struct EmbeddingArgs {
     float *part;                                // [2][chunks][pitch]: runs that a chunk begins with | ends with
     uint32_t chunk, n_chunks, pitch, digit_bits, passes;
     uint32_t early_rows, fill_rows, fill_ctas, sum_ctas;   // rows cleared beside the sort; rows of a clearing CTA beside the sums, and how many of each
+    uint32_t across;                            // few tokens: slabs of a CTA
     WorkspaceHeader *header;
     unsigned int *device_status;
 };
@@ -363,6 +364,22 @@ __device__ __forceinline__ uint64_t warp_lower_bound(const uint32_t *keys, uint6
     }
     return lo;
 }
+// Zeros to those of the rows from r0 on that are absent, by a CTA.
+template <typename W> __device__ __forceinline__ void zero_rows(const EmbeddingArgs &a, uint32_t r0, uint32_t rows, const uint32_t *absent)
+{
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const float none[8] = {};
+    for (uint32_t t = warp; t < rows; t += kRowThreads / 32u) {
+        if (!absent[t]) continue;
+        W *const row = reinterpret_cast<W *>(a.grad_weight) + (uint64_t)(r0 + t) * a.width;
+        const uint32_t off = (uint32_t)((32u - (reinterpret_cast<uintptr_t>(row) & 31u)) & 31u) / (uint32_t)sizeof(W);
+        const uint32_t head = off < a.width ? off : a.width, per = 32u / (uint32_t)sizeof(W), units = (a.width - head) / per, tail = head + units * per;
+        for (uint32_t u = lane; u < units; u += 32u) Elem<float>::store8(row + head + u * per, none);
+        if (lane < head) row[lane] = put1<W>(0.0f);
+        if (lane < a.width - tail) row[tail + lane] = put1<W>(0.0f);
+    }
+}
+
 // Zeros to the rows of a clearing CTA that no token names.
 template <typename W> __device__ void clear_rows(const EmbeddingArgs &a, uint32_t cta, uint64_t *range, uint32_t *absent)
 {
@@ -384,16 +401,7 @@ template <typename W> __device__ void clear_rows(const EmbeddingArgs &a, uint32_
         absent[t] = lo == range[1] || __ldg(keys + lo) != r0 + t;
     }
     __syncthreads();
-    const float none[8] = {};
-    for (uint32_t t = warp; t < rows; t += kRowThreads / 32u) {
-        if (!absent[t]) continue;
-        W *const row = reinterpret_cast<W *>(a.grad_weight) + (uint64_t)(r0 + t) * a.width;
-        const uint32_t off = (uint32_t)((32u - (reinterpret_cast<uintptr_t>(row) & 31u)) & 31u) / (uint32_t)sizeof(W);
-        const uint32_t head = off < a.width ? off : a.width, per = 32u / (uint32_t)sizeof(W), units = (a.width - head) / per, tail = head + units * per;
-        for (uint32_t u = lane; u < units; u += 32u) Elem<float>::store8(row + head + u * per, none);
-        if (lane < head) row[lane] = put1<W>(0.0f);
-        if (lane < a.width - tail) row[tail + lane] = put1<W>(0.0f);
-    }
+    zero_rows<W>(a, r0, rows, absent);
 }
 
 constexpr uint32_t kFillRows = 256;             // of a clearing CTA at most
@@ -556,6 +564,97 @@ template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) e
     }
 }
 
+// --------------------------------------------------------------------------------------------- backward: few tokens
+// Few of them are looked through instead of sorted, in one launch: a CTA for every token and `across` slabs of the row ends if
+// the token came earlier, or finds its other places and sums their rows, in pieces of that list that its groups of lanes take;
+// clearing CTAs find which of their rows are named.  That grows with tokens times CTAs, so it is for up to kFewTokens of
+// up to kFewItems CTAs.  Against the sorted way: 47 tokens of 60000 x 344 from binary32 15 and 21 us, of 4000 x 2048 7.3 and 16.8,
+// 512 of those 13.4 and 18.0, 1024 20.9 and 18.3 (4096 CTAs), 1024 of 11327 x 135 9.8 and 19.9, 2048 17.6 and 20.2; the worst,
+// 256 times the same token of 1000 x 4048, 16.0 and 13.4.
+constexpr uint32_t kFewTokens = 1024, kFewItems = 2048;
+
+template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads, 4) embedding_few_kernel(const __grid_constant__ EmbeddingArgs a)
+{
+    __shared__ uint32_t key[kFewTokens], list[kFewTokens], warp_count[kRowThreads / 32];
+    __shared__ float s_sum[kLaneCols][kRowThreads];
+    const uint32_t n = (uint32_t)a.n, tid = threadIdx.x;
+    bool unknown = false;
+    for (uint32_t t = tid; t < n; t += kRowThreads) {
+        const long long token = token_at(a, t);
+        const bool known = token >= 0 && token < (long long)a.vocabulary;
+        key[t] = known && token != a.padding ? (uint32_t)token : a.vocabulary;
+        unknown |= !known;
+    }
+    const bool bad = __syncthreads_or(unknown);
+    if (blockIdx.x == 0 && tid == 0) {
+        a.header->status = DAF_OK;
+        if (bad) record_error(a.header, a.device_status, DAF_ERR_INVALID_ARG);
+    }
+    if (blockIdx.x >= a.sum_ctas) {
+        uint32_t *const absent = list;
+        const uint32_t r0 = (blockIdx.x - a.sum_ctas) * a.fill_rows, rows = a.vocabulary - r0 < a.fill_rows ? a.vocabulary - r0 : a.fill_rows;
+        if (tid < rows) absent[tid] = 1u;
+        __syncthreads();
+        for (uint32_t t = tid; t < n; t += kRowThreads)
+            if (key[t] - r0 < rows) absent[key[t] - r0] = 0u;
+        __syncthreads();
+        zero_rows<W>(a, r0, rows, absent);
+        return;
+    }
+    const uint32_t blocks = (a.slabs + a.across - 1u) / a.across, first = blockIdx.x / blocks, mine = key[first];
+    if (mine == a.vocabulary) return;
+    bool earlier = false;
+    for (uint32_t t = tid; t < first; t += kRowThreads) earlier |= key[t] == mine;
+    if (__syncthreads_or(earlier)) return;
+    uint32_t m = 0;                                                 // places of the token so far
+    for (uint32_t base = first; base < n; base += kRowThreads) {
+        const bool hit = base + tid < n && key[base + tid] == mine;
+        const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+        if ((tid & 31u) == 0) warp_count[tid >> 5] = __popc(hits);
+        __syncthreads();
+        uint32_t before = m;
+#pragma unroll
+        for (uint32_t w = 0; w < kRowThreads / 32u; w++) {
+            before += w < tid >> 5 ? warp_count[w] : 0u;
+            m += warp_count[w];
+        }
+        if (hit) list[before + __popc(hits & ((1u << (tid & 31u)) - 1u))] = base + tid;
+        __syncthreads();
+    }
+    const uint32_t lanes = 1u << a.lanes_log2, lane = tid & (lanes - 1u), group = tid >> a.lanes_log2, most = (kRowThreads >> a.lanes_log2) / a.across;
+    const uint32_t pieces = m < most ? m : most, piece = group % most, slab = (blockIdx.x - first * blocks) * a.across + group / most;
+    const uint32_t col = slab * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
+    const bool here = slab < a.slabs && col < a.width && piece < pieces;
+    float acc[8] = {};
+    if (here) {
+        const A *const grad = reinterpret_cast<const A *>(a.grad_out);
+        const uint32_t to = m * (piece + 1u) / pieces;
+        constexpr uint32_t kRows = 4;                               // together
+        for (uint32_t i = m * piece / pieces; i < to; i += kRows) {
+            float x[kRows][8];
+#pragma unroll
+            for (uint32_t j = 0; j < kRows; j++)
+                load_columns<A, VEC>(grad + (uint64_t)list[i + j < to ? i + j : i] * a.width, col, lanes, a.width, x[j]);
+#pragma unroll
+            for (uint32_t j = 0; j < kRows; j++) {
+                if (i + j >= to) break;
+#pragma unroll
+                for (int e = 0; e < 8; e++) acc[e] += x[j][e];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) s_sum[e][tid] = acc[e];
+    __syncthreads();
+    if (!here || piece) return;
+    for (uint32_t p = 1; p < pieces; p++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[e] += s_sum[e][tid + p * lanes];
+#pragma unroll
+    for (int e = 0; e < 8; e++) acc[e] *= a.scale;
+    store_columns<W, VEC>(reinterpret_cast<W *>(a.grad_weight) + (uint64_t)mine * a.width, col, lanes, a.width, acc);
+}
+
 // --------------------------------------------------------------------------------------------- host
 static uint32_t elem_bytes(uint32_t dtype) { return dtype == DAF_F32 ? 4u : 2u; }
 
@@ -634,6 +733,10 @@ template <typename W, typename A, bool VEC> static daf_status forward(const Embe
 }
 template <typename W, typename A, bool VEC> static daf_status backward(const EmbeddingArgs &a, cudaStream_t s)
 {
+    if (a.across) {
+        embedding_few_kernel<A, W, VEC><<<a.sum_ctas + a.fill_ctas, kRowThreads, 0, s>>>(a);
+        return DAF_OK;
+    }
     const auto sum = &embedding_sum_kernel<A, W, VEC>;
     const uint32_t smem = VEC ? kSumBytes * kRowThreads : 0u;
     int ctas = 0;                                                   // also raises the kernel's limit of shared memory
@@ -707,26 +810,35 @@ extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, con
     a.jobs = reinterpret_cast<uint4 *>(at + 256);
     a.part = reinterpret_cast<float *>(at + 256 + up256(a.n_chunks * sizeof(uint4)));
     if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
-    int ctas = 0;                                                   // also raises the kernel's limits
-    if (persistent_ctas(reinterpret_cast<const void *>(&embedding_sort_kernel), (int)kSortThreads, (int)sizeof(SortShared), &ctas) != cudaSuccess ||
-        cudaFuncSetAttribute(embedding_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
-        return DAF_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    // Rows to clear beside the sort: about as much as its own time writes (measured 8 us and 0.3 ns a token; 4 GB a ms), all without
-    // tokens; the rest beside the sums, 64 KiB to a CTA.
     const uint32_t eb = elem_bytes(p.table_dtype);
-    const uint64_t row_bytes = (uint64_t)a.width * eb, early = (32000000ull + 1200ull * a.n) / row_bytes;
-    a.early_rows = a.n == 0 || early > a.vocabulary ? a.vocabulary : (uint32_t)early;
-    a.fill_rows = row_bytes >= 65536u ? 1u : 65536u / row_bytes > kFillRows ? kFillRows : (uint32_t)(65536u / row_bytes);
-    a.fill_ctas = (a.vocabulary - a.early_rows + a.fill_rows - 1u) / a.fill_rows;
-    const uint64_t per_cta = kRowThreads >> a.lanes_log2;
-    a.sum_ctas = (uint32_t)(((uint64_t)a.n_chunks * a.slabs + per_cta - 1u) / per_cta);
-    const uint64_t bytes = a.early_rows * row_bytes, clusters = (bytes + (1u << 20) - 1u) >> 20;      // 64 KiB to a CTA
-    embedding_sort_kernel<<<kSortCtas * (uint32_t)(1u + (clusters < 8u ? clusters : 8u)), kSortThreads, sizeof(SortShared), s>>>(a, eb);
-    if (a.n) {
-        const daf_status ran = wide(a, d_grad_out, p.dtype, d_grad_weight, p.table_dtype) ? by_type<true, true>(p.table_dtype, p.dtype, a, s)
-                                                                                         : by_type<true, false>(p.table_dtype, p.dtype, a, s);
-        if (ran != DAF_OK) return ran;
+    const uint64_t row_bytes = (uint64_t)a.width * eb;
+    const uint32_t across = a.slabs > 1u ? 2u : 1u;                 // so that a warp sums a quarter of a token's rows
+    const uint64_t items = a.n * ((a.slabs + across - 1u) / across);
+    if (a.n <= kFewTokens && items <= kFewItems) {
+        a.across = across;
+        a.sum_ctas = (uint32_t)items;
+        const uint64_t share = a.vocabulary * row_bytes / (148u * 8u), piece = share < 4096u ? 4096u : share < 65536u ? share : 65536u;
+        a.fill_rows = row_bytes >= piece ? 1u : piece / row_bytes > kFillRows ? kFillRows : (uint32_t)(piece / row_bytes);
+        a.fill_ctas = (a.vocabulary + a.fill_rows - 1u) / a.fill_rows;
+    } else {
+        int ctas = 0;                                               // also raises the kernel's limits
+        if (persistent_ctas(reinterpret_cast<const void *>(&embedding_sort_kernel), (int)kSortThreads, (int)sizeof(SortShared), &ctas) != cudaSuccess ||
+            cudaFuncSetAttribute(embedding_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+            return DAF_ERR_CUDA;
+        // Rows to clear beside the sort: about as much as its own time writes (measured 8 us and 0.3 ns a token; 4 GB a ms), all without
+        // tokens; the rest beside the sums, 64 KiB to a CTA.
+        const uint64_t early = (32000000ull + 1200ull * a.n) / row_bytes;
+        a.early_rows = early > a.vocabulary ? a.vocabulary : (uint32_t)early;
+        a.fill_rows = row_bytes >= 65536u ? 1u : 65536u / row_bytes > kFillRows ? kFillRows : (uint32_t)(65536u / row_bytes);
+        a.fill_ctas = (a.vocabulary - a.early_rows + a.fill_rows - 1u) / a.fill_rows;
+        const uint64_t per_cta = kRowThreads >> a.lanes_log2;
+        a.sum_ctas = (uint32_t)(((uint64_t)a.n_chunks * a.slabs + per_cta - 1u) / per_cta);
+        const uint64_t bytes = a.early_rows * row_bytes, clusters = (bytes + (1u << 20) - 1u) >> 20;      // 64 KiB to a CTA
+        embedding_sort_kernel<<<kSortCtas * (uint32_t)(1u + (clusters < 8u ? clusters : 8u)), kSortThreads, sizeof(SortShared), s>>>(a, eb);
     }
+    const daf_status ran = wide(a, d_grad_out, p.dtype, d_grad_weight, p.table_dtype) ? by_type<true, true>(p.table_dtype, p.dtype, a, s)
+                                                                                     : by_type<true, false>(p.table_dtype, p.dtype, a, s);
+    if (ran != DAF_OK) return ran;
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
 }

@@ -79,6 +79,51 @@ def test_gradient(table, act, n, vocabulary, width, kind):
     assert torch.equal(got, again)                                 # the same bits
 
 
+# on both sides of where tokens are looked through (1024 of them, 2048 pairs of slabs of 256 columns) and sorted
+@pytest.mark.parametrize("table,act", [("f32", "f32"), ("bf16", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("n,vocabulary,width,kind", [
+    (2, 70001, 3, "one"), (255, 31, 8, "few"), (256, 400, 264, "other"), (257, 9, 16, "one"), (1023, 2000, 135, "few"), (1024, 5, 256, "even"), (1024, 5000, 520, "few"),
+    (1025, 5000, 512, "few"), (1024, 300, 513, "one"), (409, 300, 2056, "few"), (410, 300, 2056, "few"), (600, 3, 1031, "even")])
+def test_gradient_of_few_tokens(table, act, n, vocabulary, width, kind):
+    test_gradient(table, act, n, vocabulary, width, kind)
+
+
+def test_sorted_tokens_in_their_places():
+    # the calls of the tests below with a few tokens, among enough others for them to be sorted
+    g = torch.Generator(device="cuda").manual_seed(9)
+    grad = torch.full((1500, 8), 2.0 ** -24, device="cuda")
+    grad[0] = 1.0
+    t = torch.cat((torch.zeros(4, dtype=torch.int64), torch.randint(1, 50, (1496,)))).cuda()
+    assert (daf.embedding_grad(t, grad, 50)[0] == 1.0).all()
+    order = torch.tensor([3, 2, 1, 0, *range(4, 1500)], device="cuda")
+    assert (daf.embedding_grad(t, grad[order], 50)[0] == 1.0 + 2.0 ** -22).all()
+    for bad in (-1, 50, 1 << 40):
+        where = torch.arange(1500, device="cuda") % 7 == 3
+        got = daf.embedding_grad(t.where(~where, bad), grad, 50)
+        check_grad(t, grad.where(~where[:, None], 0), 50, got, 1.0, None)
+        with pytest.raises(daf.DafError) as e:
+            daf.check_device()
+        assert e.value.status == daf.ERR_INVALID_ARG
+        with pytest.raises(daf.DafError):
+            daf.embedding_grad(t.where(~where, bad), grad, 50, check=True)
+        daf.daf_device_status()
+    for width in (24, 29):
+        for dt in (torch.float32, torch.bfloat16):
+            for off in (0, 1, 4):
+                grad = torch.randn((1500, width), generator=g, device="cuda").to(dt)
+                room = torch.full((off + 50 * width + 64,), 7.0, dtype=dt, device="cuda")
+                gw = room[off:off + 50 * width].view(50, width)
+                daf.embedding_grad(t, grad, 50, out=gw)
+                check_grad(t, grad, 50, gw, 1.0, None)
+                assert (room[:off] == 7).all() and (room[off + 50 * width:] == 7).all()
+        grad = torch.ones((1500, width), device="cuda")
+        grad[0, 0], grad[1400, 1] = math.nan, -math.inf
+        got, want = daf.embedding_grad(t, grad, 50), torch.bincount(t, minlength=50)[:, None].float().repeat(1, width)
+        want[0, 0], want[t[1400], 1] = math.nan, -math.inf
+        assert torch.equal(got.nan_to_num(nan=77.0), want.nan_to_num(nan=77.0))
+        assert daf.embedding_grad(t, grad, 50, padding=0)[0].eq(0).all()
+
+
 def test_gradient_of_every_chunk_length_and_border():
     # runs that begin and end everywhere relative to the chunks' borders
     g = torch.Generator(device="cuda").manual_seed(4)
