@@ -491,13 +491,14 @@ daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_
  *   t = position * frequency[i] for pair i; the elements behind rotary_dim stay as they are.
  * Pair i is (i, i + rotary_dim / 2) for DAF_ROTARY_HALVES, (2 i, 2 i + 1) for DAF_ROTARY_PAIRS.  frequencies: HOST array of
  * rotary_dim / 2 finite numbers (radians per position), or NULL for base^(-2 i / rotary_dim).  Angles are exact products modulo a
- * turn, for positions of any size and sign.  A row with an element that is NaN or infinite may come out as NaN throughout.  d_positions: signed integers of position_bytes, [batch, tokens], or [tokens] with
- * shared_positions; position_bytes == 0: token s of every sequence is at first_position + s.  Arithmetic in binary32, one rounding.
+ * turn, for positions of any size and sign.  A row with an element that is NaN or infinite may come out as NaN throughout.
+ * d_positions: signed integers of position_bytes, [batch, tokens], or [tokens] with shared_positions; position_bytes == 0: token s
+ * of every sequence is at first_position + s.  Arithmetic in binary32, one rounding.
  *   d_q, d_q_out, d_grad_q_out, d_grad_q : [batch, tokens, heads, head_dim];  d_k, ... : the same with kv_heads (0: no keys, NULL)
  * of dtype, by the strides below ({batch, token, head}, in elements; a row contiguous): pointers 16-byte aligned, strides of
  * extents above one multiples of 16 bytes, at least head_dim and below 2^36.  d_q_out may be d_q, d_k_out d_k with the same
- * strides, and d_grad_q, d_grad_k may be one of their two inputs; otherwise nothing overlaps.  Squares must stay in binary32's range.  Weights: head_dim elements of param_dtype
- * (DAF_F32 or dtype), 16-byte aligned.
+ * strides, and d_grad_q, d_grad_k may be one of their two inputs; otherwise nothing overlaps.  Squares must stay in binary32's
+ * range.  Weights: head_dim elements of param_dtype (DAF_F32 or dtype), 16-byte aligned.
  * daf_rotary_norm_grad takes the inputs (q, k, not what the forward pass made of them) and the gradients of both outputs (laid out
  * by q_out_stride and k_out_stride); the weights' gradients have their type and may be NULL (not wanted).  d_workspace:
  * daf_rotary_norm_grad_workspace(params) bytes (0 for bad params), 16-byte aligned, contents irrelevant.
@@ -542,11 +543,11 @@ daf_status daf_rotary_norm_grad(const daf_rotary_params *params, const double *f
  * elements; d_out[i] may be d_in[i], otherwise nothing overlaps.  Results have their input's type.
  * Arithmetic: products of 16-bit operands on the tensor cores, summed in binary32; the norm is summed in binary64.  DAF_BF16: x and
  * its Gram matrices are held in float16 between the products (x behind the first two steps with 22 bits where it is added), whose
- * effect is below the result's own rounding; DAF_F16 and DAF_F32, and DAF_BF16 up to 32 rows or columns: in two float16 parts (22 bits)
- * throughout.  Entries
- * below 2^-24 of a matrix's norm lose bits.  On the way x must stay below 7 in magnitude, x x^T and b (x x^T) + c (x x^T)^2 below 15
- * (the default coefficients keep them below 1.3, 1.6 and 2.9), otherwise the result is not finite; neither is it for a matrix with an
- * element that is not.  The same matrices give the same bits, alone or with others.
+ * effect is below the result's own rounding; DAF_F16 and DAF_F32, and DAF_BF16 up to 32 rows or columns: in two float16 parts
+ * (22 bits) throughout.  Matrices of up to 32 rows or columns and about 16000 elements are computed in binary32, the smallest in
+ * binary64.  Entries below 2^-24 of a matrix's norm lose bits.  On the way x must stay below 7 in magnitude, x x^T and
+ * b (x x^T) + c (x x^T)^2 below 15 (the default coefficients keep them below 1.3, 1.6 and 2.9), otherwise the result is not finite;
+ * neither is it for a matrix with an element that is not.  The same matrices give the same bits, alone or with others.
  * d_workspace: daf_orthogonalize_workspace(...) bytes (0 for bad arguments), 256-byte aligned, contents irrelevant; it holds the
  * device status word afterwards (daf_poll_status: DAF_OK, or DAF_ERR_TIMEOUT when a wait inside a kernel ran out).
  * rows, cols <= 65536, steps 1 to 64, coefficients and eps finite, eps > 0.

@@ -7,12 +7,13 @@
 //   update  x' = a x + P x       2 m m n
 // Bound: the tensor cores.  What is held between the products is float16, not bfloat16: 11 bits instead of 8 at the same rate,
 // and the values' range is known (singular values below two), so powers of two keep them away from both ends of the type:
-// x is held K times its size, G and P 2^12 times; K = |g| 2^s in [2^12, 2^13), so that the first x is g itself times a power of two, exact
-// for bfloat16 (two parts: 2^12, so that no rounded factor moves all singular values at once: five steps multiply that by a hundred).  Relative error of the result in binary64 arithmetic with only these roundings
-// (768 x 2304, spectra from flat to strongly decaying): 1.3e-3 to 5.0e-3 with x rounded at the start, 0.9e-3 to 3.4e-3 so, and at most 1.4e-3 with
-// the linear term a x of the steps behind the first two taken from two float16 parts (the small singular values live there: what
-// rounds the large ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  float16 and
-// binary32 matrices are held in two parts throughout (three products instead of one): 7e-7.
+// x is held K times its size, G and P 2^12 times; K = |g| 2^s in [2^12, 2^13), so that the first x is g itself times a power of
+// two, exact for bfloat16 (two parts: 2^12, so that no rounded factor moves all singular values at once: five steps multiply that
+// by a hundred).  Relative error of the result in binary64 arithmetic with only these roundings (768 x 2304, spectra from flat to
+// strongly decaying): 1.3e-3 to 5.0e-3 with x rounded at the start, 0.9e-3 to 3.4e-3 so, and at most 1.4e-3 with the linear term
+// a x of the steps behind the first two taken from two float16 parts (the small singular values live there: what rounds the large
+// ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  float16 and binary32 matrices are held in
+// two parts throughout (three products instead of one): 7e-7.
 //
 // One persistent kernel runs all products of all steps and matrices.  Pairs of CTAs take tiles of 256 x N by a ticket, in an order
 // in which whatever a tile needs comes before it; a tile waits until its matrix's tiles of the earlier products are done
@@ -20,8 +21,9 @@
 // another's gaps.  A pair, because one SM's shared memory cannot feed its tensor core: of a product of 256 x 256 each CTA holds half of
 // either operand.  Roles: the first CTA's warp 2 takes tickets, waits and tells both; warp 0 of each copies its halves of the operands
 // (TMA, a copy of 16 KB for each operand and 64 of the summed dimension, warp 3 those of the second operand: a copy takes some 200
-// cycles to issue whatever its size, and copies of 8 KB took longer than the products, 0.45 against 0.31 us); the first CTA's warp 1 issues the products (two accumulators in tensor memory); eight warps of each read its half of
-// the result's rows, form the polynomial or the update and store them.
+// cycles to issue whatever its size, and copies of 8 KB took longer than the products, 0.45 against 0.31 us); the first CTA's warp 1
+// issues the products (two accumulators in tensor memory); eight warps of each read its half of the result's rows, form the
+// polynomial or the update and store them.  Matrices of few rows have a kernel of their own (orth_small_kernel).
 #include "attention.cuh"
 #include "tensor_core.cuh"
 
@@ -519,6 +521,7 @@ template <bool SEGMENTS> __global__ void __cluster_dims__(2, 1, 1) __launch_boun
     tmem_after_sync();
     const uint32_t tmem = bars.tmem;
     volatile uint32_t *const stop = &bars.abort;
+    next_may_start();
     wait_for_ahead();
 
     if (warp == 2 && rank == 0) {                                  // ---- tickets, one tile ahead of the copies
@@ -833,6 +836,167 @@ template <bool SEGMENTS> __global__ void __cluster_dims__(2, 1, 1) __launch_boun
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
+// --------------------------------------------------------------------------------------------- small matrices
+// A matrix of few rows (or columns: it is held turned, so that the shorter side m is the rows) in one CTA's shared memory, all
+// steps in one launch: a tensor core has nothing to do there, and what a step takes elsewhere is the way from SM to SM, 15 times
+// for five steps.  The smallest are held and computed in binary64: their roundings do not average out.
+// Gram matrix: a thread has 4 x 4 elements, of those that reach the diagonal or lie right of it, and every `parts`th column; the parts
+// are added up in order.  Update: a thread has four rows of a column.
+// One binary32 matrix here and by orthogonalize_kernel: 2 x 5 10 and 75 us, 512 x 16 35 and 113, 1 x 4096 41 and 231, 32 x 510 94 and
+// 124 (150 of these 184 and 312); errors 1.4e-7 and 8.7e-7, 6.3e-7 and 1.1e-6, 1.4e-7 and 4.8e-7, 9.0e-7 and 2.4e-6.  The Gram
+// matrix's parts, the polynomial, which rounds what five steps multiply by a hundred, and few rows' updates are summed in binary64
+// in any case (all in binary32: 2 x 5 2e-6, 1 x 4096 1.4e-6, and 4 us less for 32 x 510).
+constexpr uint32_t kSmallRows = 32, kSmallExact = 8;
+template <typename S> struct OrthSmall {
+    static constexpr bool kWide = sizeof(S) == 8;
+    static constexpr uint32_t kThreads = kWide ? 512 : 1024, kElems = kWide ? 4096 : 16384, kPartElems = kWide ? 8192 : 16384, kParts = 64;
+    S x[2][kElems + kSmallRows];                // rows of n | 1
+    S part[kPartElems];
+    double g[kSmallRows][kSmallRows + 1], sum[kThreads / 32];
+    alignas(16) double p[kSmallRows][kSmallRows + 4];
+    alignas(16) float p_float[kSmallRows][kSmallRows + 4];
+};
+struct OrthSmallArgs {
+    const void *in[kOrthMatrices];
+    void *out[kOrthMatrices];
+    uint32_t r[kOrthMatrices], c[kOrthMatrices], dtype[kOrthMatrices];
+    uint32_t steps;
+    float a, b, c_, eps;
+};
+
+template <typename T> __device__ __forceinline__ float small_load(const void *p, uint32_t i) { return (float)static_cast<const T *>(p)[i]; }
+__device__ __forceinline__ float fma_of(float a, float b, float c) { return __fmaf_rn(a, b, c); }
+__device__ __forceinline__ double fma_of(double a, double b, double c) { return __fma_rn(a, b, c); }
+
+// x' = by x + p x, summed as P.
+template <typename P, typename S> __device__ __forceinline__ void small_update(const P (&p)[kSmallRows][kSmallRows + 4], P by, const S *x, S *to, uint32_t pitch,
+                                                                              uint32_t rows, uint32_t n)
+{
+    struct alignas(16) Four { P v[4]; };
+    for (uint32_t unit = threadIdx.x; unit < rows / 4u * n; unit += OrthSmall<S>::kThreads) {
+        const uint32_t row = unit / n * 4u, col = unit % n;
+        P acc[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4u; e++) acc[e] = by * (P)x[(row + e) * pitch + col];
+#pragma unroll 2
+        for (uint32_t k = 0; k < rows; k += 4u) {
+            P v[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; e++) v[e] = (P)x[(k + e) * pitch + col];
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; e++) {
+                const Four w = *reinterpret_cast<const Four *>(&p[row + e][k]);
+#pragma unroll
+                for (int i = 0; i < 4; i++) acc[e] = fma_of(w.v[i], v[i], acc[e]);
+            }
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 4u; e++) to[(row + e) * pitch + col] = (S)acc[e];
+    }
+}
+
+template <typename S> __global__ void __launch_bounds__(OrthSmall<S>::kThreads, 1) orth_small_kernel(const __grid_constant__ OrthSmallArgs a)
+{
+    using Shared = OrthSmall<S>;
+    constexpr uint32_t kThreads = Shared::kThreads;
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    Shared &s = *reinterpret_cast<Shared *>(s_raw);
+    const uint32_t tid = threadIdx.x, r = a.r[blockIdx.x], c = a.c[blockIdx.x], dtype = a.dtype[blockIdx.x];
+    const bool tall = r > c;
+    const uint32_t m = tall ? c : r, n = tall ? r : c, pitch = n | 1u, blocks = (m + 3u) / 4u, rows = 4u * blocks;
+    const void *const in = a.in[blockIdx.x];
+    const auto place = [&](uint32_t i) {                            // of element i in x
+        const uint32_t row = i / c, col = i - row * c;
+        return tall ? col * pitch + row : row * pitch + col;
+    };
+    double sum = 0.0;
+    for (uint32_t i = tid; i < r * c; i += kThreads) {
+        const float v = dtype == DAF_F32 ? small_load<float>(in, i) : dtype == DAF_F16 ? small_load<__half>(in, i) : small_load<__nv_bfloat16>(in, i);
+        s.x[0][place(i)] = v;
+        sum = fma((double)v, (double)v, sum);
+    }
+    for (uint32_t i = m * pitch + tid; i < rows * pitch; i += kThreads) s.x[0][i] = S(0);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if ((tid & 31u) == 0) s.sum[tid >> 5] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (uint32_t w = 0; w < kThreads / 32u; w++) sum += s.sum[w];
+    const double norm = sqrt(sum) + (double)a.eps, factor = norm - norm == 0.0 ? 1.0 / norm : norm - norm;      // not finite: NaN
+    for (uint32_t i = tid; i < r * c; i += kThreads) s.x[0][place(i)] = (S)((double)s.x[0][place(i)] * factor);
+    // this thread's share of the Gram matrix
+    const uint32_t tiles = blocks * (blocks + 1u) / 2u, squares = rows * rows;
+    const uint32_t apart = tiles <= 1u ? 1u : 1u << (32 - __clz(tiles - 1u));
+    uint32_t parts = (n + 15u) / 16u < Shared::kParts ? (n + 15u) / 16u : Shared::kParts;       // 16 columns or more
+    if (parts > kThreads / apart) parts = kThreads / apart;
+    if (parts * squares > Shared::kPartElems) parts = Shared::kPartElems / squares;
+    uint32_t bi = 0, bj = tid & (apart - 1u);
+    const uint32_t part = bj < tiles ? tid / apart : parts;         // parts: none
+    while (bi < blocks && bj >= blocks - bi) {
+        bj -= blocks - bi;
+        bi++;
+    }
+    bj += bi;
+    for (uint32_t step = 0; step < a.steps; step++) {
+        const S *const x = s.x[step & 1u];
+        __syncthreads();
+        if (part < parts) {
+            S acc[4][4] = {};
+            const S *const xi = x + 4u * bi * pitch, *const xj = x + 4u * bj * pitch;
+#pragma unroll 2
+            for (uint32_t k = part; k < n; k += parts) {
+                S u[4], v[4];
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; i++) u[i] = xi[i * pitch + k], v[i] = xj[i * pitch + k];
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) acc[i][j] = fma_of(u[i], v[j], acc[i][j]);
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; i++)
+#pragma unroll
+                for (uint32_t j = 0; j < 4u; j++) s.part[part * squares + (4u * bi + i) * rows + 4u * bj + j] = acc[i][j];
+        }
+        __syncthreads();
+        for (uint32_t e = tid; e < squares; e += kThreads) {
+            const uint32_t i = e / rows, j = e - i * rows;
+            if (j < i) continue;
+            double v = 0.0;
+#pragma unroll 8
+            for (uint32_t q = 0; q < parts; q++) v += (double)s.part[q * squares + e];
+            s.g[i][j] = v;
+            s.g[j][i] = v;
+        }
+        __syncthreads();
+        for (uint32_t e = tid; e < squares; e += kThreads) {
+            const uint32_t i = e / rows, j = e - i * rows;
+            double v = 0.0;
+#pragma unroll 4
+            for (uint32_t k = 0; k < rows; k++) v = fma_of(s.g[i][k], s.g[j][k], v);
+            v = fma_of((double)a.c_, v, (double)a.b * s.g[i][j]);
+            s.p[i][j] = v;
+            s.p_float[i][j] = (float)v;
+        }
+        __syncthreads();
+        S *const to = s.x[(step + 1u) & 1u];
+        if (Shared::kWide || rows <= kSmallExact) small_update(s.p, (double)a.a, x, to, pitch, rows, n);
+        else small_update(s.p_float, a.a, x, to, pitch, rows, n);
+    }
+    __syncthreads();
+    const S *const x = s.x[a.steps & 1u];
+    void *const out = a.out[blockIdx.x];
+    for (uint32_t i = tid; i < r * c; i += kThreads) {
+        const S v = x[place(i)];
+        if (dtype == DAF_F32) static_cast<float *>(out)[i] = (float)v;
+        else if (dtype == DAF_F16) static_cast<__half *>(out)[i] = Shared::kWide ? __double2half((double)v) : __float2half_rn((float)v);
+        else static_cast<__nv_bfloat16 *>(out)[i] = Shared::kWide ? __double2bfloat16((double)v) : __float2bfloat16_rn((float)v);
+    }
+    // It may have run beside the products of larger matrices: whoever waits for this launch waits for those, too.
+    wait_for_ahead();
+}
+
 // --------------------------------------------------------------------------------------------- host
 static uint64_t up_to(uint64_t n, uint64_t by) { return (n + by - 1u) / by * by; }
 
@@ -860,8 +1024,14 @@ static uint32_t orth_sym_tiles(uint32_t m, uint32_t width)
     return tiles;
 }
 
-// Parts of a matrix's operands.  With few rows roundings do not average out: one row's polynomial is one number, and five steps with it in
-// one part are up to 4e-3 off; so small matrices take two, which costs them nothing to speak of.
+// Whether one CTA does it all, holding it as S.
+template <typename S> static bool orth_small(uint64_t rows, uint64_t cols)
+{
+    const uint64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    return m && m <= kSmallRows && (m + 3u) / 4u * 4u * (n | 1u) <= OrthSmall<S>::kElems + kSmallRows;
+}
+// Parts of a matrix's operands.  With few rows roundings do not average out: one row's polynomial is one number, and five steps with
+// it in one part are up to 4e-3 off; so these take two, which costs them nothing to speak of.
 static uint32_t orth_planes(uint32_t dtype, uint32_t rows, uint32_t cols) { return dtype == DAF_BF16 && rows > 32u && cols > 32u ? 1u : 2u; }
 // Whether sums are taken in segments.
 static bool orth_segments(uint32_t dtype, uint64_t rows, uint64_t cols) { return dtype == DAF_F32 || (dtype == DAF_F16 && (rows > 8192u || cols > 8192u)); }
@@ -880,7 +1050,7 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     a->groups = a->matrices = 0;
     for (; *next < n && a->matrices < kOrthMatrices; ++*next) {
         const uint32_t i = *next, r = (uint32_t)rows[i], c = (uint32_t)cols[i];
-        if (r == 0 || c == 0 || orth_segments(dtypes[i], r, c) != segments) continue;
+        if (r == 0 || c == 0 || orth_small<float>(r, c) || orth_segments(dtypes[i], r, c) != segments) continue;
         if (elems && elems + (uint64_t)r * c > kOrthBatch) break;
         uint32_t k = 0;
         while (k < a->groups && (shape[k].r != r || shape[k].c != c || shape[k].dtype != dtypes[i])) k++;
@@ -1012,6 +1182,35 @@ static bool orth_place(OrthArgs *a, char *at)
     return true;
 }
 
+template <typename S> static daf_status small_ones(const daf_orthogonalize_params *p, uint32_t n, const uint32_t *dtypes, const void *const *d_in,
+                                                  void *const *d_out, const uint64_t *rows, const uint64_t *cols, bool *behind, cudaStream_t s)
+{
+    OrthSmallArgs a;
+    a.steps = p->steps;
+    a.a = p->coefficients[0];
+    a.b = p->coefficients[1];
+    a.c_ = p->coefficients[2];
+    a.eps = p->eps;
+    for (uint32_t i = 0, count = 0; i < n; i++) {
+        if (orth_small<S>(rows[i], cols[i]) && (sizeof(S) == 8 || !orth_small<double>(rows[i], cols[i]))) {
+            a.in[count] = d_in[i];
+            a.out[count] = d_out[i];
+            a.r[count] = (uint32_t)rows[i];
+            a.c[count] = (uint32_t)cols[i];
+            a.dtype[count++] = dtypes[i];
+        }
+        if (count == 0 || (count < kOrthMatrices && i + 1u < n)) continue;
+        const auto kernel = &orth_small_kernel<S>;
+        int ctas = 0;                                               // also raises the kernel's limit of shared memory
+        if (persistent_ctas(reinterpret_cast<const void *>(kernel), (int)OrthSmall<S>::kThreads, (int)sizeof(OrthSmall<S>), &ctas) != cudaSuccess) return DAF_ERR_CUDA;
+        if (!*behind) kernel<<<count, OrthSmall<S>::kThreads, sizeof(OrthSmall<S>), s>>>(a);
+        else if (launch_behind(kernel, count, OrthSmall<S>::kThreads, sizeof(OrthSmall<S>), s, a) != cudaSuccess) return DAF_ERR_CUDA;
+        *behind = false;
+        count = 0;
+    }
+    return DAF_OK;
+}
+
 }  // namespace daf
 
 using namespace daf;
@@ -1069,6 +1268,12 @@ extern "C" daf_status daf_orthogonalize(const daf_orthogonalize_params *params, 
             const uint32_t most = a.sym_total > a.upd_total ? a.sym_total : a.upd_total, pairs = (uint32_t)ctas / 2u;
             if (launch_behind(kernel, 2u * (most < pairs ? most : pairs), kOrthThreads, kOrthSmem, s, a) != cudaSuccess) return DAF_ERR_CUDA;
         }
+    }
+    bool behind = any;                                              // the first runs beside the last batch, where SMs are free
+    for (const bool wide : {true, false}) {
+        const daf_status ran = wide ? small_ones<double>(params, n, dtypes, d_in, d_out, rows, cols, &behind, s)
+                                    : small_ones<float>(params, n, dtypes, d_in, d_out, rows, cols, &behind, s);
+        if (ran != DAF_OK) return ran;
     }
     if (!any && cudaMemsetAsync(d_workspace, 0, sizeof(uint32_t), s) != cudaSuccess) return DAF_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;

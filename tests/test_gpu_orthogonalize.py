@@ -81,6 +81,55 @@ def test_against_64_bits(shape, dtype, kind):
     assert apart(got, want) <= bound, (apart(got, want), of_model)
 
 
+# held in binary64: one rounding, to the result's type, and what 5 steps of sums of 1030 products in binary64 are off, times a hundred
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 1), (1, 2), (2, 5), (3, 1), (4, 1031), (1031, 3), (5, 515), (32, 32), (32, 128), (127, 32), (29, 129), (17, 200), (9, 3, 5)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_smallest_matrices(shape, dtype):
+    g = gradient(shape, dtype, 21)
+    got, = daf.orthogonalize([g], check=True)
+    want = exact(g)
+    slack = 100 * 5 * 1031 * 2.0 ** -53 * want.norm()
+    t = g.dtype
+    assert ((got.double() - want).abs() <= torch.finfo(t).eps / 2 * want.abs() + slack + (2.0 ** -25 if t == torch.float16 else 0.0)).all()
+
+
+# held in binary32: a sum of n products is at most n / 16 + 32 additions deep (parts of 16 columns or more, 64 parts at most, 16 or more of
+# a long sum), each off by 2^-24, in three products a step; the largest of these shapes and the next ones, which are not held by one CTA
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 1033), (4103, 1), (4, 4105), (5, 517), (32, 129), (32, 513), (513, 32), (512, 32), (32, 514), (33, 33), (1300, 12), (12, 1368)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_small_matrices(shape, dtype):
+    g = gradient(shape, dtype, 22)
+    got, = daf.orthogonalize([g], check=True)
+    want = exact(g)
+    of_model = apart(model(g, 1 if dtype == "bf16" and min(shape) > 32 else 2), want)
+    assert apart(got, want) <= torch.finfo(g.dtype).eps / 2 + 2 * of_model + 100 * 3 * (max(shape) / 16 + 32) * 2.0 ** -24
+
+
+def test_small_matrices_among_others():
+    """Those of one CTA run beside the products of the others, more of them than go together, in place, in a graph."""
+    shapes = [(2, 5), (300, 700), (32, 500)] * 3 + [(16, 40)] * 200 + [(30, 400)] * 195 + [(64, 9000), (0, 4), (4, 0)]
+    gs = [gradient(s, ("bf16", "f32", "f16")[i % 3], 30 + i) if 0 not in s else torch.zeros(s, device="cuda") for i, s in enumerate(shapes)]
+    want = [daf.orthogonalize([g], check=True)[0] for g in gs]
+    assert all(torch.equal(a, b) for a, b in zip(daf.orthogonalize(gs, check=True), want))
+    for order in (slice(None, None, -1), slice(None, None, 7)):
+        assert all(torch.equal(a, b) for a, b in zip(daf.orthogonalize(gs[order], check=True), want[order]))
+    held = [g.clone() for g in gs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        after = [2 * x for x in daf.orthogonalize(held, out=held)]
+    for _ in range(3):
+        for h, g in zip(held, gs):
+            h.copy_(g)
+        graph.replay()
+        assert all(torch.equal(a, 2 * b) for a, b in zip(after, want)) and all(torch.equal(a, b) for a, b in zip(held, want))
+    one = gradient((8, 20), "f32", 50)
+    one[3, 4] = math.inf
+    assert daf.orthogonalize([one])[0].isnan().all()
+    assert not daf.orthogonalize([torch.zeros((8, 20), device="cuda")])[0].any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shape", [(100, 333), (333, 100), (256, 256), (31, 2050)], ids=lambda s: "x".join(map(str, s)))
 def test_one_step_element_by_element(shape, dtype):
