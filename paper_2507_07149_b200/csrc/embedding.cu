@@ -565,13 +565,14 @@ template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) e
 }
 
 // --------------------------------------------------------------------------------------------- backward: few tokens
-// Few of them are looked through instead of sorted, in one launch: a CTA for every token and `across` slabs of the row ends if
-// the token came earlier, or finds its other places and sums their rows, in pieces of that list that its groups of lanes take;
-// clearing CTAs find which of their rows are named.  That grows with tokens times CTAs, so it is for up to kFewTokens of
-// up to kFewItems CTAs.  Against the sorted way: 47 tokens of 60000 x 344 from binary32 15 and 21 us, of 4000 x 2048 7.3 and 16.8,
-// 512 of those 13.4 and 18.0, 1024 20.9 and 18.3 (4096 CTAs), 1024 of 11327 x 135 9.8 and 19.9, 2048 17.6 and 20.2; the worst,
-// 256 times the same token of 1000 x 4048, 16.0 and 13.4.
-constexpr uint32_t kFewTokens = 1024, kFewItems = 2048;
+// Few of them are looked through instead of sorted, in one launch: an item, a token's place and `across` slabs of the row, ends if
+// the token came earlier; else its other places are found and their rows summed, in pieces of that list that a CTA's groups of
+// lanes take; clearing CTAs find which of their rows are named.  That grows with tokens times items and with the longest run, so it is
+// for up to kFewTokens of up to kFewItems, above half of them for vocabularies that are no smaller.  Against the sorted way: 47
+// tokens of 60000 x 344 from binary32 15 and 21 us, of 4000 x 2048 7.3 and 16.8, 512 of those 13 and 18, 1024 of 11327 x 135 9.4 and
+// 19.9, 2048 14.7 and 20.2, of 15 x 158 25.6 and 14.3; the worst, 256 times the same token of 1000 x 4048, 16.8 and 13.4.
+// kFewCtas, four an SM, take items in turn: 1024 of 60000 x 344 16.6 us, with two an SM 16.7, with a CTA for each 17.5.
+constexpr uint32_t kFewTokens = 2048, kFewItems = 2048, kFewCtas = 148u * 4u;
 
 template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads, 4) embedding_few_kernel(const __grid_constant__ EmbeddingArgs a)
 {
@@ -601,58 +602,64 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
         zero_rows<W>(a, r0, rows, absent);
         return;
     }
-    const uint32_t blocks = (a.slabs + a.across - 1u) / a.across, first = blockIdx.x / blocks, mine = key[first];
-    if (mine == a.vocabulary) return;
-    bool earlier = false;
-    for (uint32_t t = tid; t < first; t += kRowThreads) earlier |= key[t] == mine;
-    if (__syncthreads_or(earlier)) return;
-    uint32_t m = 0;                                                 // places of the token so far
-    for (uint32_t base = first; base < n; base += kRowThreads) {
-        const bool hit = base + tid < n && key[base + tid] == mine;
-        const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-        if ((tid & 31u) == 0) warp_count[tid >> 5] = __popc(hits);
-        __syncthreads();
-        uint32_t before = m;
-#pragma unroll
-        for (uint32_t w = 0; w < kRowThreads / 32u; w++) {
-            before += w < tid >> 5 ? warp_count[w] : 0u;
-            m += warp_count[w];
-        }
-        if (hit) list[before + __popc(hits & ((1u << (tid & 31u)) - 1u))] = base + tid;
-        __syncthreads();
-    }
+    const uint32_t blocks = (a.slabs + a.across - 1u) / a.across, items = n * blocks;
     const uint32_t lanes = 1u << a.lanes_log2, lane = tid & (lanes - 1u), group = tid >> a.lanes_log2, most = (kRowThreads >> a.lanes_log2) / a.across;
-    const uint32_t pieces = m < most ? m : most, piece = group % most, slab = (blockIdx.x - first * blocks) * a.across + group / most;
-    const uint32_t col = slab * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
-    const bool here = slab < a.slabs && col < a.width && piece < pieces;
-    float acc[8] = {};
-    if (here) {
-        const A *const grad = reinterpret_cast<const A *>(a.grad_out);
-        const uint32_t to = m * (piece + 1u) / pieces;
-        constexpr uint32_t kRows = 4;                               // together
-        for (uint32_t i = m * piece / pieces; i < to; i += kRows) {
-            float x[kRows][8];
+    const uint32_t piece = group % most;
+    for (uint32_t item = blockIdx.x; item < items; item += a.sum_ctas) {
+        const uint32_t first = item / blocks, mine = key[first];
+        if (mine == a.vocabulary) continue;
+        bool earlier = false;
+        for (uint32_t t = tid; t < first; t += kRowThreads) earlier |= key[t] == mine;
+        if (__syncthreads_or(earlier)) continue;                    // behind it nobody reads what the item before left
+        uint32_t m = 0;                                             // places of the token so far
+        for (uint32_t base = first; base < n; base += kRowThreads) {
+            const bool hit = base + tid < n && key[base + tid] == mine;
+            const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+            if ((tid & 31u) == 0) warp_count[tid >> 5] = __popc(hits);
+            __syncthreads();
+            uint32_t before = m;
 #pragma unroll
-            for (uint32_t j = 0; j < kRows; j++)
-                load_columns<A, VEC>(grad + (uint64_t)list[i + j < to ? i + j : i] * a.width, col, lanes, a.width, x[j]);
+            for (uint32_t w = 0; w < kRowThreads / 32u; w++) {
+                before += w < tid >> 5 ? warp_count[w] : 0u;
+                m += warp_count[w];
+            }
+            if (hit) list[before + __popc(hits & ((1u << (tid & 31u)) - 1u))] = base + tid;
+            __syncthreads();
+        }
+        const uint32_t pieces = m < most ? m : most, slab = (item - first * blocks) * a.across + group / most;
+        const uint32_t col = slab * lanes * kLaneCols + lane_column<VEC>(lane, lanes, 0);
+        const bool here = slab < a.slabs && col < a.width && piece < pieces;
+        float acc[8] = {};
+        if (here) {
+            constexpr uint32_t kRows = 4;                           // together
+            const A *const grad = reinterpret_cast<const A *>(a.grad_out);
+            const uint32_t to = m * (piece + 1u) / pieces;
+            for (uint32_t i = m * piece / pieces; i < to; i += kRows) {
+                float x[kRows][8];
 #pragma unroll
-            for (uint32_t j = 0; j < kRows; j++) {
-                if (i + j >= to) break;
+                for (uint32_t j = 0; j < kRows; j++)
+                    load_columns<A, VEC>(grad + (uint64_t)list[i + j < to ? i + j : i] * a.width, col, lanes, a.width, x[j]);
 #pragma unroll
-                for (int e = 0; e < 8; e++) acc[e] += x[j][e];
+                for (uint32_t j = 0; j < kRows; j++) {
+                    if (i + j >= to) break;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) acc[e] += x[j][e];
+                }
             }
         }
+        if (pieces > 1u) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) s_sum[e][tid] = acc[e];
+            __syncthreads();
+        }
+        if (!here || piece) continue;
+        for (uint32_t p = 1; p < pieces; p++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) acc[e] += s_sum[e][tid + p * lanes];
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[e] *= a.scale;
+        store_columns<W, VEC>(reinterpret_cast<W *>(a.grad_weight) + (uint64_t)mine * a.width, col, lanes, a.width, acc);
     }
-#pragma unroll
-    for (int e = 0; e < 8; e++) s_sum[e][tid] = acc[e];
-    __syncthreads();
-    if (!here || piece) return;
-    for (uint32_t p = 1; p < pieces; p++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) acc[e] += s_sum[e][tid + p * lanes];
-#pragma unroll
-    for (int e = 0; e < 8; e++) acc[e] *= a.scale;
-    store_columns<W, VEC>(reinterpret_cast<W *>(a.grad_weight) + (uint64_t)mine * a.width, col, lanes, a.width, acc);
 }
 
 // --------------------------------------------------------------------------------------------- host
@@ -815,9 +822,9 @@ extern "C" daf_status daf_embedding_grad(const daf_embedding_params *params, con
     const uint64_t row_bytes = (uint64_t)a.width * eb;
     const uint32_t across = a.slabs > 1u ? 2u : 1u;                 // so that a warp sums a quarter of a token's rows
     const uint64_t items = a.n * ((a.slabs + across - 1u) / across);
-    if (a.n <= kFewTokens && items <= kFewItems) {
+    if (items <= kFewItems && (a.n <= kFewTokens / 2u || (a.n <= kFewTokens && a.vocabulary >= a.n))) {
         a.across = across;
-        a.sum_ctas = (uint32_t)items;
+        a.sum_ctas = items < kFewCtas ? (uint32_t)items : kFewCtas;
         const uint64_t share = a.vocabulary * row_bytes / (148u * 8u), piece = share < 4096u ? 4096u : share < 65536u ? share : 65536u;
         a.fill_rows = row_bytes >= piece ? 1u : piece / row_bytes > kFillRows ? kFillRows : (uint32_t)(piece / row_bytes);
         a.fill_ctas = (a.vocabulary + a.fill_rows - 1u) / a.fill_rows;

@@ -79,11 +79,12 @@ def test_gradient(table, act, n, vocabulary, width, kind):
     assert torch.equal(got, again)                                 # the same bits
 
 
-# on both sides of where tokens are looked through (1024 of them, 2048 pairs of slabs of 256 columns) and sorted
+# on both sides of where tokens are looked through (1024 of them, 2048 of no smaller a vocabulary, 2048 pairs of slabs of 256 columns) and sorted
 @pytest.mark.parametrize("table,act", [("f32", "f32"), ("bf16", "bf16"), ("f32", "f16")])
 @pytest.mark.parametrize("n,vocabulary,width,kind", [
     (2, 70001, 3, "one"), (255, 31, 8, "few"), (256, 400, 264, "other"), (257, 9, 16, "one"), (1023, 2000, 135, "few"), (1024, 5, 256, "even"), (1024, 5000, 520, "few"),
-    (1025, 5000, 512, "few"), (1024, 300, 513, "one"), (409, 300, 2056, "few"), (410, 300, 2056, "few"), (600, 3, 1031, "even")])
+    (1025, 5000, 512, "few"), (1024, 300, 513, "one"), (409, 300, 2056, "few"), (410, 300, 2056, "few"), (600, 3, 1031, "even"),
+    (2048, 2048, 33, "few"), (2048, 2047, 40, "one"), (2047, 3000, 500, "one"), (2049, 5000, 24, "other")])
 def test_gradient_of_few_tokens(table, act, n, vocabulary, width, kind):
     test_gradient(table, act, n, vocabulary, width, kind)
 
