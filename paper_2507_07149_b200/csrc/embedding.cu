@@ -450,38 +450,45 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
     };
     Block block;
     block.place = (uint32_t)__cvta_generic_to_shared(raw) + threadIdx.x * 16u;
-    uint32_t key[kRows], next[kRows];
+    uint32_t key[kRows], next[kRows], behind_next[kRows], place[kRows];     // the list comes a block ahead of the rows
     const auto list = [](const uint32_t *from, uint32_t (&to)[kRows]) {
 #pragma unroll
         for (int h = 0; h < kRows; h += 4) *reinterpret_cast<uint4 *>(to + h) = __ldg(reinterpret_cast<const uint4 *>(from + h));
     };
-    const auto fetch = [&](uint32_t i, int half) {                  // the rows of next, from place i of the chunk on
-        uint32_t place[kRows];
-        list(places + i, place);
+    const auto fetch = [&](int half) {                              // the rows of next
 #pragma unroll
         for (int j = 0; j < kRows; j++)
             if (!VEC || (mine && next[j] != none)) block.fetch(half, j, grad + (uint64_t)place[j] * a.width, col, lanes, a.width);
     };
-    list(keys, next);
+    const auto look = [&](uint32_t i) {
+        if (i >= a.chunk) return;
+        list(keys + i, behind_next);
+        list(places + i, place);
+    };
+    look(0);
     if (VEC) {
-        fetch(0, 0);
+#pragma unroll
+        for (int j = 0; j < kRows; j++) next[j] = behind_next[j];
+        fetch(0);
         asm volatile("cp.async.commit_group;" ::: "memory");
+        look(kRows);
     }
     int half = 0;
     for (uint32_t i = 0; i < a.chunk; i += kRows) {
 #pragma unroll
-        for (int j = 0; j < kRows; j++) key[j] = next[j];
+        for (int j = 0; j < kRows; j++) {
+            key[j] = VEC ? next[j] : behind_next[j];
+            next[j] = behind_next[j];
+        }
         if (key[0] == none) break;
         if (VEC) {
-            if (i + kRows < a.chunk) {
-                list(keys + i + kRows, next);
-                fetch(i + kRows, half ^ 1);
-            }
+            if (i + kRows < a.chunk) fetch(half ^ 1);
             asm volatile("cp.async.commit_group;" ::: "memory");
+            look(i + 2u * kRows);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {
-            fetch(i, 0);
-            if (i + kRows < a.chunk) list(keys + i + kRows, next);
+            fetch(0);
+            look(i + kRows);
         }
 #pragma unroll
         for (int j = 0; j < kRows; j++) {

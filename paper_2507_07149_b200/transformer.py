@@ -1,8 +1,8 @@
 """The operators of a transformer's training step as differentiable functions and layers, and a small trainer.
 
 ``attention``, ``residual_norm``, ``embedding``, ``rotary_norm`` and ``clip_grad_norm_`` run the CUDA kernels behind the C ABI; they can
-be differentiated once.  ``Muon`` steps by orthogonalised updates.  Attention keeps q, k, v, its output and one float per row for the backward pass, the join keeps its two activations;
-what they keep goes through autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is held in compressed
+be differentiated once.  ``Muon`` steps by orthogonalised updates.  Attention keeps q, k, v, its output and one float per row for the
+backward pass, the join keeps its two activations, rotary norms keep q and k as they were, the embedding its tokens; what they keep goes through autograd's saved-tensor hooks, so inside ``saved_activation_compression`` it is held in compressed
 form like every other activation.  Attention's row statistics belong to the scores they were taken from: at 8 bits per value they are kept as they
 are, below that (or with a store, which may drop a tensor) the backward pass takes them, and the output, anew from the
 restored q, k and v, at the price of a second forward pass of attention and without keeping the output.
