@@ -14,6 +14,7 @@
 //                          chunks keep the SMs evenly busy however often one token occurs.  CTAs among these write zeros to the
 //                          other rows that no token names, so that reads and writes share the memory.
 //   embedding_join_kernel  the parts of a run that crosses borders are added up, in order.
+// Few tokens take one launch instead (embedding_few_kernel).
 // Bound: HBM, grad_out read once and the table's gradient written once (named rows among the first: twice).
 #include "common.cuh"
 
