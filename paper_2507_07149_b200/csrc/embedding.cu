@@ -351,13 +351,28 @@ template <typename A, bool VEC> struct RowBlock {
     }
 };
 
+// The sorted list, read behind wait_for_ahead(): the kernel that writes it may still run when these start, so the loads are neither the
+// read-only kind, which holds for memory that nobody writes while the kernel runs, nor ones that the compiler may move.
+__device__ __forceinline__ uint32_t listed(const uint32_t *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 listed4(const uint32_t *p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
 // The first place in keys[0, n) whose key is at least `key`, by a warp, thirty-two probes at a time.
 __device__ __forceinline__ uint64_t warp_lower_bound(const uint32_t *keys, uint64_t n, uint32_t key, uint32_t lane)
 {
     uint64_t lo = 0, hi = n;                                        // in [lo, hi]
     while (lo < hi) {
         const uint64_t step = (hi - lo + 31u) / 32u, at = lo + lane * step;
-        const uint32_t less = __ballot_sync(0xffffffffu, at < hi && __ldg(keys + at) < key);       // a run from lane 0 on
+        const uint32_t less = __ballot_sync(0xffffffffu, at < hi && listed(keys + at) < key);       // a run from lane 0 on
         if (!less) return lo;
         const uint32_t most = 31u - __clz(less);
         lo += most * step + 1u;
@@ -396,10 +411,10 @@ template <typename W> __device__ void clear_rows(const EmbeddingArgs &a, uint32_
         uint64_t lo = range[0], hi = range[1];
         while (lo < hi) {
             const uint64_t mid = (lo + hi) / 2u;
-            if (__ldg(keys + mid) < r0 + t) lo = mid + 1u;
+            if (listed(keys + mid) < r0 + t) lo = mid + 1u;
             else hi = mid;
         }
-        absent[t] = lo == range[1] || __ldg(keys + lo) != r0 + t;
+        absent[t] = lo == range[1] || listed(keys + lo) != r0 + t;
     }
     __syncthreads();
     zero_rows<W>(a, r0, rows, absent);
@@ -432,11 +447,11 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
     const uint32_t last = (a.passes + 1u) & 1u, none = a.vocabulary;
     const uint64_t first = (uint64_t)chunk * a.chunk;
     const uint32_t *keys = a.keys[last] + first, *places = a.places[last] + first;
-    const uint32_t ahead = chunk ? __ldg(keys - 1) : none, behind = chunk + 1u < a.n_chunks ? __ldg(keys + a.chunk) : none;
+    const uint32_t ahead = chunk ? listed(keys - 1) : none, behind = chunk + 1u < a.n_chunks ? listed(keys + a.chunk) : none;
     const A *grad = reinterpret_cast<const A *>(a.grad_out);
     const uint64_t part_col = (uint64_t)slab * lanes * kLaneCols + lane * kLaneCols;    // parts are always held in runs of eight
     float acc[8] = {};
-    uint32_t run = __ldg(keys);
+    uint32_t run = listed(keys);
     bool open = run == ahead;                                       // the run began in an earlier chunk
     const auto finish = [&](bool goes_on) {
         if (run == none || !mine) return;
@@ -454,7 +469,7 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
     uint32_t key[kRows], next[kRows], behind_next[kRows], place[kRows];     // the list comes a block ahead of the rows
     const auto list = [](const uint32_t *from, uint32_t (&to)[kRows]) {
 #pragma unroll
-        for (int h = 0; h < kRows; h += 4) *reinterpret_cast<uint4 *>(to + h) = __ldg(reinterpret_cast<const uint4 *>(from + h));
+        for (int h = 0; h < kRows; h += 4) *reinterpret_cast<uint4 *>(to + h) = listed4(from + h);
     };
     const auto fetch = [&](int half) {                              // the rows of next
 #pragma unroll
@@ -514,7 +529,7 @@ template <typename A, typename W, bool VEC> __global__ void __launch_bounds__(kR
     finish(goes_on);
     if (goes_on && !open && slab == 0 && lane == 0) {
         // most such runs end in the next chunk; the others' ends are looked for by those who join them (0)
-        const bool on = chunk + 2u < a.n_chunks && __ldg(keys + 2u * a.chunk) == run;
+        const bool on = chunk + 2u < a.n_chunks && listed(keys + 2u * a.chunk) == run;
         a.jobs[atomicAdd(a.n_jobs, 1u)] = make_uint4(chunk, on ? 0u : 2u, run, 0u);
     }
 }
@@ -538,7 +553,7 @@ template <typename W, bool VEC> __global__ void __launch_bounds__(kRowThreads) e
             while (hi - lo > 1u) {
                 const uint32_t step = (hi - lo + 31u) / 32u;
                 const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
-                const uint32_t yes = __ballot_sync(0xffffffffu, at < hi && __ldg(keys + at * a.chunk) == key);
+                const uint32_t yes = __ballot_sync(0xffffffffu, at < hi && listed(keys + at * a.chunk) == key);
                 const uint32_t next = lo + (31u - __clz(yes)) * step;       // lane 0 always says yes
                 hi = hi - next < step ? hi : next + step;
                 lo = next;
