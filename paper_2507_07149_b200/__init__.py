@@ -634,13 +634,17 @@ def daf_embedding_grad(params, d_tokens, d_grad_out, d_grad_weight, d_workspace,
     _check(status, "daf_embedding_grad")
 
 
-def _frequencies(frequencies):
-    return None if frequencies is None else (ctypes.c_double * len(frequencies))(*frequencies)
+def _frequencies(params, frequencies):
+    if frequencies is None:
+        return None
+    if len(frequencies) != params.rotary_dim // 2:                  # the library reads that many
+        raise ValueError(f"frequencies: {len(frequencies)} of them, expected rotary_dim / 2 = {params.rotary_dim // 2}")
+    return (ctypes.c_double * len(frequencies))(*frequencies)
 
 
 def daf_rotary_norm(params, frequencies, d_q, d_k, d_q_weight, d_k_weight, d_positions, d_q_out, d_k_out, stream=None):
-    """frequencies: rotary_dim / 2 numbers or None, as for ``rotary_norm``."""
-    status = _call(lib().daf_rotary_norm, d_q, stream, ctypes.byref(params), _frequencies(frequencies), _ptr(d_q), _ptr(d_k), _ptr(d_q_weight),
+    """frequencies: rotary_dim / 2 numbers (ValueError if it is another count) or None, as for ``rotary_norm``."""
+    status = _call(lib().daf_rotary_norm, d_q, stream, ctypes.byref(params), _frequencies(params, frequencies), _ptr(d_q), _ptr(d_k), _ptr(d_q_weight),
                    _ptr(d_k_weight), _ptr(d_positions), _ptr(d_q_out), _ptr(d_k_out))
     _check(status, "daf_rotary_norm")
 
@@ -651,7 +655,7 @@ def daf_rotary_norm_grad_workspace(params) -> int:
 
 def daf_rotary_norm_grad(params, frequencies, d_q, d_k, d_q_weight, d_k_weight, d_positions, d_grad_q_out, d_grad_k_out, d_grad_q, d_grad_k,
                          d_grad_q_weight, d_grad_k_weight, d_workspace, workspace_bytes, stream=None):
-    status = _call(lib().daf_rotary_norm_grad, d_q, stream, ctypes.byref(params), _frequencies(frequencies), _ptr(d_q), _ptr(d_k),
+    status = _call(lib().daf_rotary_norm_grad, d_q, stream, ctypes.byref(params), _frequencies(params, frequencies), _ptr(d_q), _ptr(d_k),
                    _ptr(d_q_weight), _ptr(d_k_weight), _ptr(d_positions), _ptr(d_grad_q_out), _ptr(d_grad_k_out), _ptr(d_grad_q),
                    _ptr(d_grad_k), _ptr(d_grad_q_weight), _ptr(d_grad_k_weight), _ptr(d_workspace), workspace_bytes)
     _check(status, "daf_rotary_norm_grad")

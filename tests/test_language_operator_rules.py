@@ -2,6 +2,8 @@
 import os
 import re
 
+import pytest
+
 import paper_2507_07149_b200 as daf
 
 CSRC = os.path.join(os.path.dirname(daf.__file__), "csrc")
@@ -12,3 +14,18 @@ def test_lists_that_another_launch_writes_are_not_read_as_constant():
     with open(os.path.join(CSRC, "embedding.cu")) as f:
         loads = re.findall(r"__ldg\(([^;]*?)\s*\+", f.read())
     assert loads and all("a.tokens" in what for what in loads), loads
+
+
+@pytest.mark.parametrize("count", [0, 1, 31, 33])
+def test_another_count_of_frequencies_is_refused_before_the_library_reads_them(count, monkeypatch):
+    called = []
+    monkeypatch.setattr(daf, "_call", lambda *a: called.append(a) or daf.OK)
+    p, f = daf.daf_rotary_params(rotary_dim=64), [1.0] * count
+    for call, more in ((daf.daf_rotary_norm, 7), (daf.daf_rotary_norm_grad, 14)):
+        with pytest.raises(ValueError):
+            call(p, f, *[None] * more)
+        assert not called
+        call(p, [1.0] * 32, *[None] * more)
+        call(p, None, *[None] * more)
+        assert len(called) == 2
+        called.clear()
