@@ -675,7 +675,9 @@ def daf_orthogonalize_workspace(params, d_in) -> int:
 
 
 def daf_orthogonalize(params, d_in, d_out, d_workspace, workspace_bytes, stream=None):
-    """d_in, d_out: lists of contiguous matrices."""
+    """d_in, d_out: lists of contiguous matrices, as many of one as of the other."""
+    if len(d_out) != len(d_in):                                     # the library reads as many addresses
+        raise ValueError(f"daf_orthogonalize: {len(d_out)} outputs for {len(d_in)} matrices")
     types, rows, cols = _matrices(d_in)
     status = _call(lib().daf_orthogonalize, d_workspace, stream, ctypes.byref(params), len(d_in), types, _ptr_array(d_in), _ptr_array(d_out), rows,
                    cols, _ptr(d_workspace), workspace_bytes)

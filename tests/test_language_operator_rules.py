@@ -29,3 +29,16 @@ def test_another_count_of_frequencies_is_refused_before_the_library_reads_them(c
         call(p, None, *[None] * more)
         assert len(called) == 2
         called.clear()
+
+
+def test_as_many_outputs_as_matrices(monkeypatch):
+    torch = pytest.importorskip("torch")
+    called = []
+    monkeypatch.setattr(daf, "_call", lambda *a: called.append(a) or daf.OK)
+    two = [torch.zeros(4, 8), torch.zeros(3, 5)]
+    for out in (two[:1], [], two + two):
+        with pytest.raises(ValueError):
+            daf.daf_orthogonalize(daf.daf_orthogonalize_params(), two, out, None, 0)
+    assert not called
+    daf.daf_orthogonalize(daf.daf_orthogonalize_params(), two, two, None, 0)
+    assert len(called) == 1
