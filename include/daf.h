@@ -460,8 +460,10 @@ daf_status daf_clip_norm_batch(uint32_t n, const uint32_t *dtypes, const void *c
  *   multiple of 8 and both matrices on the boundary of 8 elements).  table_dtype is dtype or DAF_F32.
  * padding: a token whose row takes no gradient (daf_embedding_grad; its row of the gradient is zero), negative: none.  A token
  * outside [0, vocabulary) gives a row of zeros and no gradient, and is recorded as DAF_ERR_INVALID_ARG in the word of
- * daf_device_status (and in the workspace of daf_embedding_grad).  d_workspace: daf_embedding_grad_workspace(params) bytes (0 for
- * bad params), 32-byte aligned, contents irrelevant.  No output may overlap an input.  tokens == 0 is valid.
+ * daf_device_status (and in the workspace of daf_embedding_grad).  daf_embedding_checked is daf_embedding with a status of its own:
+ * such a token is recorded in its workspace (daf_poll_status) and not in the device's word.  d_workspace:
+ * daf_embedding_workspace(params) or daf_embedding_grad_workspace(params) bytes (0 for bad params), 32-byte aligned, contents
+ * irrelevant.  No output may overlap an input.  tokens == 0 is valid.
  * vocabulary and width are positive (DAF_ERR_SHAPE); vocabulary < 2^31 - 1, tokens <= 2^31 - 256, width <= 2^24 (UNSUPPORTED).
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CAPACITY (workspace too small), CUDA.
  */
@@ -479,6 +481,9 @@ typedef struct daf_embedding_params {
 } daf_embedding_params;
 daf_status daf_embedding(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out,
                          daf_stream stream);
+uint64_t   daf_embedding_workspace(const daf_embedding_params *params);
+daf_status daf_embedding_checked(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out,
+                                 void *d_workspace, uint64_t workspace_bytes, daf_stream stream);
 uint64_t   daf_embedding_grad_workspace(const daf_embedding_params *params);
 daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_tokens, const void *d_grad_out,
                               void *d_grad_weight, void *d_workspace, uint64_t workspace_bytes, daf_stream stream);

@@ -150,6 +150,8 @@ SIGNATURES = {
     "daf_clip_norm_batch": (ctypes.c_int, [ctypes.c_uint32, _vp, _vp, _vp, _vp, ctypes.c_float, ctypes.c_float, _vp, _vp,
                                            ctypes.c_uint64, _vp]),
     "daf_embedding": (ctypes.c_int, [ctypes.POINTER(daf_embedding_params)] + [_vp] * 4),
+    "daf_embedding_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_embedding_params)]),
+    "daf_embedding_checked": (ctypes.c_int, [ctypes.POINTER(daf_embedding_params)] + [_vp] * 4 + [ctypes.c_uint64, _vp]),
     "daf_embedding_grad_workspace": (ctypes.c_uint64, [ctypes.POINTER(daf_embedding_params)]),
     "daf_embedding_grad": (ctypes.c_int, [ctypes.POINTER(daf_embedding_params)] + [_vp] * 4 + [ctypes.c_uint64, _vp]),
     "daf_rotary_norm": (ctypes.c_int, [ctypes.POINTER(daf_rotary_params)] + [_vp] * 9),
@@ -624,6 +626,16 @@ def daf_embedding(params, d_tokens, d_weight, d_out, stream=None):
     _check(_call(lib().daf_embedding, d_out, stream, ctypes.byref(params), _ptr(d_tokens), _ptr(d_weight), _ptr(d_out)), "daf_embedding")
 
 
+def daf_embedding_workspace(params) -> int:
+    return int(lib().daf_embedding_workspace(ctypes.byref(params)))
+
+
+def daf_embedding_checked(params, d_tokens, d_weight, d_out, d_workspace, workspace_bytes, stream=None):
+    status = _call(lib().daf_embedding_checked, d_out, stream, ctypes.byref(params), _ptr(d_tokens), _ptr(d_weight), _ptr(d_out), _ptr(d_workspace),
+                   workspace_bytes)
+    _check(status, "daf_embedding_checked")
+
+
 def daf_embedding_grad_workspace(params) -> int:
     return int(lib().daf_embedding_grad_workspace(ctypes.byref(params)))
 
@@ -794,14 +806,12 @@ def clip_grad_norm(grads, max_norm: float, *, eps: float = 1e-6, out=None, strea
 def embedding(tokens, weight, *, scale: float = 1.0, dtype=None, out=None, check: bool = False, stream=None):
     """scale * weight[tokens]: rows of weight [vocabulary, width] for int32 or int64 tokens of any shape (daf_embedding).  dtype:
     the output's type, the weight's by default, any of the three where the weight is float32.  A token outside the vocabulary
-    gives zeros and is recorded for ``check_device``; check asks at once (and waits for the device)."""
+    gives zeros and is recorded for ``check_device``; with check the call waits and raises for its own tokens, and records nothing there."""
     if stream is not None:
         with _torch().cuda.stream(stream):
             return embedding(tokens, weight, scale=scale, dtype=dtype, out=out, check=check)
-    made, status = _native().embedding(tokens, weight, scale, dtype, out)
+    made, status = _native().embedding(tokens, weight, scale, dtype, out, check)
     _check(status, "daf_embedding")
-    if check:
-        _check(daf_device_status(made.device), "daf_embedding (device status)")
     return made if out is None else out
 
 

@@ -39,7 +39,7 @@ struct EmbeddingArgs {
     uint32_t early_rows, fill_rows, fill_ctas, sum_ctas;   // rows cleared beside the sort; rows of a clearing CTA beside the sums, and how many of each
     uint32_t across;                            // few tokens: slabs of a CTA
     WorkspaceHeader *header;
-    unsigned int *device_status;
+    unsigned int *device_status;                // forward: or the caller's own
 };
 
 __device__ __forceinline__ long long token_at(const EmbeddingArgs &a, uint64_t i)
@@ -791,22 +791,50 @@ template <bool BACK, bool VEC> static daf_status by_type(uint32_t table, uint32_
 
 using namespace daf;
 
-extern "C" daf_status daf_embedding(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out, daf_stream stream)
+// Tokens that are none are recorded in *status; null: in the device's word.
+static daf_status embedding_rows(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out, unsigned int *status, cudaStream_t s)
 {
-    const daf_status st = check_embedding(params);
-    if (st != DAF_OK) return st;
-    if (params->tokens == 0) return DAF_OK;
-    if (!on_elements(d_tokens, params->token_bytes) || !on_elements(d_weight, elem_bytes(params->table_dtype)) || !on_elements(d_out, elem_bytes(params->dtype)))
-        return DAF_ERR_INVALID_ARG;
     EmbeddingArgs a = embedding_args(params, false);
     a.tokens = d_tokens;
     a.weight = d_weight;
     a.out = d_out;
-    if (!(a.device_status = device_status_word())) return DAF_ERR_CUDA;
-    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (!(a.device_status = status ? status : device_status_word())) return DAF_ERR_CUDA;
     const daf_status ran = wide(a, d_weight, params->table_dtype, d_out, params->dtype) ? by_type<false, true>(params->table_dtype, params->dtype, a, s)
                                                                                        : by_type<false, false>(params->table_dtype, params->dtype, a, s);
     return ran != DAF_OK ? ran : cudaGetLastError() == cudaSuccess ? DAF_OK : DAF_ERR_CUDA;
+}
+
+static daf_status check_embedding_rows(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, const void *d_out)
+{
+    const daf_status st = check_embedding(params);
+    if (st != DAF_OK || params->tokens == 0) return st;
+    return on_elements(d_tokens, params->token_bytes) && on_elements(d_weight, elem_bytes(params->table_dtype)) && on_elements(d_out, elem_bytes(params->dtype))
+               ? DAF_OK : DAF_ERR_INVALID_ARG;
+}
+
+extern "C" daf_status daf_embedding(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out, daf_stream stream)
+{
+    const daf_status st = check_embedding_rows(params, d_tokens, d_weight, d_out);
+    if (st != DAF_OK || params->tokens == 0) return st;
+    return embedding_rows(params, d_tokens, d_weight, d_out, nullptr, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" uint64_t daf_embedding_workspace(const daf_embedding_params *params)
+{
+    return check_embedding(params) == DAF_OK ? sizeof(WorkspaceHeader) : 0;
+}
+
+extern "C" daf_status daf_embedding_checked(const daf_embedding_params *params, const void *d_tokens, const void *d_weight, void *d_out, void *d_workspace,
+                                            uint64_t workspace_bytes, daf_stream stream)
+{
+    const daf_status st = check_embedding_rows(params, d_tokens, d_weight, d_out);
+    if (st != DAF_OK) return st;
+    if (!on_elements(d_workspace, 32u)) return DAF_ERR_INVALID_ARG;
+    if (workspace_bytes < daf_embedding_workspace(params)) return DAF_ERR_CAPACITY;
+    unsigned int *const status = &reinterpret_cast<WorkspaceHeader *>(d_workspace)->status;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (cudaMemsetAsync(status, 0, sizeof(*status), s) != cudaSuccess) return DAF_ERR_CUDA;
+    return params->tokens ? embedding_rows(params, d_tokens, d_weight, d_out, status, s) : DAF_OK;
 }
 
 extern "C" uint64_t daf_embedding_grad_workspace(const daf_embedding_params *params)

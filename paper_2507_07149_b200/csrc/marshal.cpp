@@ -445,10 +445,10 @@ struct Embedding {
     }
 };
 
-// (tokens, weight, scale, dtype, out) -> (out, status)
+// (tokens, weight, scale, dtype, out, check) -> (out, status)
 PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return guarded(n, 5, [&]() {
+    return guarded(n, 6, [&]() {
         const char *const where = "embedding";
         Embedding e(where, a[0], a[2]);
         at::Tensor weight = tensor(where, a[1]);
@@ -472,7 +472,13 @@ PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n)
                 refuse(where, "out is a contiguous tensor of the tokens' shape and the width, of the type that was asked for");
             modified(out);
         }
-        return answer({out}, daf_embedding(&e.p, ptr(e.tokens), ptr(weight), ptr(out), c10::cuda::getCurrentCUDAStream().stream()));
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+        if (!truth(a[5])) return answer({out}, daf_embedding(&e.p, ptr(e.tokens), ptr(weight), ptr(out), stream));
+        const uint64_t size = daf_embedding_workspace(&e.p);         // the call's own status: the device's word holds others' errors
+        const at::Tensor ws = bytes(size, weight);
+        daf_status st = daf_embedding_checked(&e.p, ptr(e.tokens), ptr(weight), ptr(out), ptr(ws), size, stream);
+        if (st == DAF_OK) st = daf_poll_status(ptr(ws), stream);
+        return answer({out}, st);
     });
 }
 

@@ -25,3 +25,28 @@ def test_a_workspace_that_one_call_after_another_uses(width):
     for t, out in zip(calls, made):
         assert torch.equal(out, torch.zeros((vocabulary, width), device="cuda").index_add_(0, t, grad))
     assert daf.daf_poll_status(ws) == daf.OK
+
+
+def test_a_checked_embedding_asks_for_its_own_tokens():
+    """The device's word holds what others have recorded: it neither fails a call of known tokens nor is it cleared by one."""
+    w = torch.randn((10, 24), device="cuda")
+    good, bad = torch.tensor([3, 9], device="cuda"), torch.tensor([3, 10], device="cuda")
+    daf.daf_device_status()
+    for t in (good, good[:0]):
+        daf.embedding(bad, w)                                       # somebody else's error, not asked for yet
+        assert torch.equal(daf.embedding(t, w, check=True), w[t])
+        with pytest.raises(daf.DafError):
+            daf.check_device()
+    for out in (None, torch.empty((2, 24), device="cuda")):
+        with pytest.raises(daf.DafError) as e:
+            daf.embedding(bad, w, out=out, check=True)
+        assert e.value.status == daf.ERR_INVALID_ARG
+    assert torch.equal(out, torch.stack((w[3], torch.zeros_like(w[3]))))
+    daf.check_device()                                              # who asked was told
+    p = daf.daf_embedding_params(ctypes.sizeof(daf.daf_embedding_params), daf.F32, daf.F32, 8, 2, 10, 24, 1.0, -1, 0)
+    size = daf.daf_embedding_workspace(p)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    for t, status in ((good, daf.OK), (bad, daf.ERR_INVALID_ARG), (good, daf.OK)):
+        daf.daf_embedding_checked(p, t, w, out, ws, size)
+        assert daf.daf_poll_status(ws) == status
+    daf.check_device()

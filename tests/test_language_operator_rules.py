@@ -1,10 +1,12 @@
 """Rules of the language operators that hold without a GPU: how memory is read, what host code refuses and asks for."""
+import ctypes
 import os
 import re
 
 import pytest
 
 import paper_2507_07149_b200 as daf
+from paper_2507_07149_b200 import build as daf_build
 
 CSRC = os.path.join(os.path.dirname(daf.__file__), "csrc")
 
@@ -42,3 +44,18 @@ def test_as_many_outputs_as_matrices(monkeypatch):
     assert not called
     daf.daf_orthogonalize(daf.daf_orthogonalize_params(), two, two, None, 0)
     assert len(called) == 1
+
+
+def test_checked_embedding_refuses_what_the_plain_one_does_and_its_workspace():
+    daf_build.build()
+    a, lib = 1 << 20, daf.lib()                  # an address that is never used: every call below is refused
+    p = daf.daf_embedding_params(ctypes.sizeof(daf.daf_embedding_params), daf.BF16, daf.F32, 8, 10, 100, 64, 1.0, -1, 0)
+    need = daf.daf_embedding_workspace(p)
+    ref = ctypes.byref(p)
+    assert need > 0
+    for bad in ((None, a, a, a), (a, None, a, a), (a, a, None, a), (a + 4, a, a, a), (a, a + 2, a, a), (a, a, a + 1, a), (a, a, a, None), (a, a, a, a + 16)):
+        assert lib.daf_embedding_checked(ref, *bad, need, None) == daf.ERR_INVALID_ARG
+    assert lib.daf_embedding_checked(ref, a, a, a, a, need - 1, None) == daf.ERR_CAPACITY
+    assert lib.daf_embedding_checked(None, a, a, a, a, need, None) == daf.ERR_INVALID_ARG
+    p.width = 0
+    assert lib.daf_embedding_checked(ref, a, a, a, a, need, None) == daf.ERR_SHAPE and daf.daf_embedding_workspace(p) == 0
