@@ -32,7 +32,7 @@ namespace daf {
 constexpr uint32_t kOrthThreads = 384, kOrthStages = 6, kOrthBox = 8192, kOrthStage = 4u * kOrthBox, kOrthOut = 2048, kOrthRows = 256;
 constexpr uint32_t kOrthGroups = 16, kOrthMatrices = 192, kOrthSlots = 2;
 constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
-constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch: bounds the workspace (8 bytes and more per element)
+constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch, rows taken up to their pitch: bounds the workspace (8 to 16 bytes each)
 // Binary32: sums of 128 of the summed dimension are taken in tensor memory and added up in registers.  A tensor memory sum loses about two
 // units of its 24th bit at every addition, always downwards: 4096 columns of one row 2e-5 without, 5e-7 so; segments of 64 cost a fifth
 // of the time (results cannot run as far ahead), of 256 are 2.5 times as far off.  float16 does without up to 8192 rows or columns, where
@@ -1051,7 +1051,8 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
     for (; *next < n && a->matrices < kOrthMatrices; ++*next) {
         const uint32_t i = *next, r = (uint32_t)rows[i], c = (uint32_t)cols[i];
         if (r == 0 || c == 0 || orth_small<float>(r, c) || orth_segments(dtypes[i], r, c) != segments) continue;
-        if (elems && elems + (uint64_t)r * c > kOrthBatch) break;
+        const uint64_t held = r * up_to(c, 64u);
+        if (elems && elems + held > kOrthBatch) break;
         uint32_t k = 0;
         while (k < a->groups && (shape[k].r != r || shape[k].c != c || shape[k].dtype != dtypes[i])) k++;
         if (k == kOrthGroups) break;
@@ -1059,7 +1060,7 @@ static void orth_batch(OrthArgs *a, const daf_orthogonalize_params *p, uint32_t 
         shape[k].count++;
         group_of[a->matrices] = k;
         taken[a->matrices++] = i;
-        elems += (uint64_t)r * c;
+        elems += held;
     }
     // Longest side first: the Gram matrix's tiles take as long as that is, and what waits for the last of them waits least so (two
     // blocks of width 2048: a tenth of the time).

@@ -50,3 +50,11 @@ def test_a_checked_embedding_asks_for_its_own_tokens():
         daf.daf_embedding_checked(p, t, w, out, ws, size)
         assert daf.daf_poll_status(ws) == status
     daf.check_device()
+
+
+def test_thin_matrices_of_several_batches_are_those_of_one():
+    g = torch.Generator(device="cuda").manual_seed(2)
+    gs = [torch.randn((60000, 1 + i % 3), generator=g, device="cuda").to((torch.float32, torch.bfloat16)[i % 2]) for i in range(90)]
+    made = daf.orthogonalize(gs, check=True)
+    for i in (0, 1, 33, 34, 35, 70, 89):
+        assert torch.equal(made[i], daf.orthogonalize([gs[i]])[0])

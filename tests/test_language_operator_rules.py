@@ -59,3 +59,14 @@ def test_checked_embedding_refuses_what_the_plain_one_does_and_its_workspace():
     assert lib.daf_embedding_checked(None, a, a, a, a, need, None) == daf.ERR_INVALID_ARG
     p.width = 0
     assert lib.daf_embedding_checked(ref, a, a, a, a, need, None) == daf.ERR_SHAPE and daf.daf_embedding_workspace(p) == 0
+
+
+@pytest.mark.parametrize("shape,count", [((65536, 1), 192), ((65536, 65), 192), ((1, 65536), 192), ((40000, 33), 500), ((2048, 8192), 64)])
+def test_a_batch_bounds_the_workspace_of_orthogonalised_updates(shape, count):
+    """16 bytes for each of 2^27 elements, or for one matrix if that is larger, whatever the rows are padded to; 64 KiB for the rest."""
+    daf_build.build()
+    p = daf.daf_orthogonalize_params(ctypes.sizeof(daf.daf_orthogonalize_params), 5, (3.4445, -4.7750, 2.0315), 1e-7)
+    for dtype in (daf.F32, daf.F16, daf.BF16):
+        sizes = ((ctypes.c_uint32 * count)(*[dtype] * count), (ctypes.c_uint64 * count)(*[shape[0]] * count), (ctypes.c_uint64 * count)(*[shape[1]] * count))
+        one = daf.lib().daf_orthogonalize_workspace(ctypes.byref(p), 1, *sizes)
+        assert one <= daf.lib().daf_orthogonalize_workspace(ctypes.byref(p), count, *sizes) <= 16 * 2 ** 27 + (1 << 16) + 192 * 512 * 8
