@@ -495,8 +495,10 @@ daf_status daf_embedding_grad(const daf_embedding_params *params, const void *d_
  *   the first rotary_dim elements of n in pairs (a, b): a' = a cos t - b sin t, b' = a sin t + b cos t with
  *   t = position * frequency[i] for pair i; the elements behind rotary_dim stay as they are.
  * Pair i is (i, i + rotary_dim / 2) for DAF_ROTARY_HALVES, (2 i, 2 i + 1) for DAF_ROTARY_PAIRS.  frequencies: HOST array of
- * rotary_dim / 2 finite numbers (radians per position), or NULL for base^(-2 i / rotary_dim).  Angles are exact products modulo a
- * turn, for positions of any size and sign.  A row with an element that is NaN or infinite may come out as NaN throughout.
+ * rotary_dim / 2 finite numbers (radians per position), or NULL for base^(-2 i / rotary_dim).  Angles are products in 64-bit
+ * integers modulo a turn, for positions of either sign: a frequency is held within 2^-64 turns per position (one above a turn, or
+ * made of a base below 100, within 2^-55 of itself), so an angle is off by |position| times that, and by what binary32 holds
+ * of it: 2^-31 turns at position 2^33, a quarter of a turn at 2^62.  A row with an element that is NaN or infinite may come out as NaN throughout.
  * d_positions: signed integers of position_bytes, [batch, tokens], or [tokens] with shared_positions; position_bytes == 0: token s
  * of every sequence is at first_position + s.  Arithmetic in binary32, one rounding.
  *   d_q, d_q_out, d_grad_q_out, d_grad_q : [batch, tokens, heads, head_dim];  d_k, ... : the same with kv_heads (0: no keys, NULL)

@@ -8,8 +8,9 @@
 // Bound: HBM (each element read once, or x and g, and written once) as far as the instructions per row allow, which is why all of
 // it is done on pairs of binary32.  A row is held by a group of lanes, 2 V elements each: both sides of its V pairs, so nothing but the
 // sums crosses lanes.  A group takes several heads of ONE token, because the angles are the token's: cosines and sines of a lane's V pairs
-// cost as much as a row.  Angles: a pair's frequency is held as turns per position, a 64-bit fraction of a turn; position * frequency modulo
-// 2^64 is then exact in integers, however far the position, and the top 32 bits give the angle within 2^-31 half turns.
+// cost as much as a row.  Angles: a pair's frequency is held as turns per position, a 64-bit fraction of a turn; its product with the position
+// modulo 2^64 is exact in integers, so that only the frequency's own rounding (2^-64 turns) grows with the position, and the top 32 bits give
+// the angle within 2^-31 half turns.
 //
 // The weights' gradients are summed in registers over the rows of a group, over the groups of a CTA in shared memory and over
 // the CTAs by a second launch, all in a fixed order.
@@ -567,12 +568,15 @@ static bool rotary_vector(const void *d, bool needed)
     return d ? (reinterpret_cast<uintptr_t>(d) & 15u) == 0 : !needed;
 }
 
-// Turns per position in 2^-64, from turns as products of 64-bit mantissas.
+// Turns per position in 2^-64, from turns as products of 64-bit mantissas.  Off by at most 2^-64 for frequencies of up to a turn: half of it
+// by this rounding or that of the product below, the rest by 1 / (2 pi).  Powers of a base of 100 or more, one product after another, stay
+// within that, too (computed for bases up to 10^8); a power function for each of 64 pairs would take 20 us of the host.
 static uint64_t fraction_of_turn(long double turns)
 {
     if (!(turns >= 0.0L && turns < 1.0L)) turns -= __builtin_floorl(turns);
     turns *= 18446744073709551616.0L;
-    return turns >= 18446744073709551615.0L ? 0u : (uint64_t)(turns + 0.5L);
+    if (turns >= 9223372036854775808.0L) return turns >= 18446744073709551616.0L ? 0u : (uint64_t)turns;      // whole, and a half more would be rounded
+    return (uint64_t)(turns + 0.5L);
 }
 constexpr long double kTurnsPerRadian = 0.159154943091895335768883763372514362L;
 

@@ -1,6 +1,8 @@
 """The language operators where calls meet: workspaces used again, errors of others, large offsets; and their results within bounds of
 their own arithmetic."""
 import ctypes
+import math
+from fractions import Fraction
 
 import pytest
 
@@ -58,3 +60,21 @@ def test_thin_matrices_of_several_batches_are_those_of_one():
     made = daf.orthogonalize(gs, check=True)
     for i in (0, 1, 33, 34, 35, 70, 89):
         assert torch.equal(made[i], daf.orthogonalize([gs[i]])[0])
+
+
+# Frequencies whose fraction of a turn lies above a half, the largest of what is held in 64 bits: they are held within 2^-64 turns, which
+# position 2^56 makes 2^-8 turns, far above what binary32 does to the angle.
+@pytest.mark.parametrize("sign", [1, -1])
+def test_frequencies_are_held_within_2_to_the_minus_64_turns(sign):
+    two_pi = Fraction("6.283185307179586476925286766559005768394338798750211641949889")
+    f = [6.220240124624253, 6.1985164879813235, 6.1188054798018, 6.262672126026183, 4.0, 3.25, 6.0, 1.0]
+    q = torch.zeros((1, 1, 1, 16), device="cuda")
+    q[..., :8] = 1.0
+    for frequencies in (f, [w - float(two_pi) for w in f]):          # and negative ones, up to a turn
+        out, _ = daf.rotary_norm(q, None, positions=sign << 56, frequencies=frequencies, eps=0.0)
+        for i, w in enumerate(frequencies):
+            turns = Fraction(w) * (sign << 56) / two_pi
+            a = float((turns - math.floor(turns)) * two_pi)
+            # n = sqrt(2); 2^-64 turns a position, the angle in 24 bits, its cut at 2^-32 turns, the accurate functions and four roundings
+            off = math.sqrt(2) * (2 * math.pi * 2.0 ** -8 + math.pi * 2.0 ** -24 + 2.0 ** -28 + 2.0 ** -22 + 4 * 2.0 ** -24)
+            assert abs(out[0, 0, 0, i].item() - math.sqrt(2) * math.cos(a)) <= off and abs(out[0, 0, 0, 8 + i].item() - math.sqrt(2) * math.sin(a)) <= off
