@@ -504,6 +504,8 @@ PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
             e.p.padding = whole(a[4]);
             if (e.p.padding < 0 || e.p.padding >= vocabulary) refuse(where, "padding is a token, or None");
         }
+        const uint64_t size = daf_embedding_grad_workspace(&e.p);    // 0: refused, ahead of room for a table that cannot be
+        if (size == 0) return answer({out}, daf_embedding_grad(&e.p, nullptr, nullptr, nullptr, nullptr, 0, nullptr));
         const c10::cuda::CUDAGuard on(grad.device());
         const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
         const int64_t shape[2] = {vocabulary, grad.size(-1)};
@@ -515,7 +517,6 @@ PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
                 refuse(where, "out is a contiguous tensor [vocabulary, width] of the type that was asked for");
             modified(out);
         }
-        const uint64_t size = daf_embedding_grad_workspace(&e.p);
         const at::Tensor ws = bytes(size, grad);
         daf_status st = daf_embedding_grad(&e.p, ptr(e.tokens), ptr(grad), ptr(out), ptr(ws), size, stream);
         if (st == DAF_OK && truth(a[7])) st = daf_poll_status(ptr(ws), stream);

@@ -78,3 +78,14 @@ def test_frequencies_are_held_within_2_to_the_minus_64_turns(sign):
             # n = sqrt(2); 2^-64 turns a position, the angle in 24 bits, its cut at 2^-32 turns, the accurate functions and four roundings
             off = math.sqrt(2) * (2 * math.pi * 2.0 ** -8 + math.pi * 2.0 ** -24 + 2.0 ** -28 + 2.0 ** -22 + 4 * 2.0 ** -24)
             assert abs(out[0, 0, 0, i].item() - math.sqrt(2) * math.cos(a)) <= off and abs(out[0, 0, 0, 8 + i].item() - math.sqrt(2) * math.sin(a)) <= off
+
+
+def test_a_vocabulary_beyond_the_limits_is_refused_as_such():
+    t, grad = torch.tensor([1, 2], device="cuda"), torch.ones((2, 8), device="cuda")
+    for vocabulary in (2 ** 31 - 1, 1 << 40, (1 << 63) - 1):         # not as a lack of memory for its table
+        with pytest.raises(daf.DafError) as e:
+            daf.embedding_grad(t, grad, vocabulary)
+        assert e.value.status == daf.ERR_UNSUPPORTED
+    with pytest.raises(daf.DafError) as e:
+        daf.embedding_grad(t, grad[:, :0], 10)
+    assert e.value.status == daf.ERR_SHAPE
