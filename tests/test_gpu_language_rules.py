@@ -89,3 +89,23 @@ def test_a_vocabulary_beyond_the_limits_is_refused_as_such():
     with pytest.raises(daf.DafError) as e:
         daf.embedding_grad(t, grad[:, :0], 10)
     assert e.value.status == daf.ERR_SHAPE
+
+
+@pytest.mark.parametrize("width", [8192, 8191])
+def test_a_sorted_gradient_of_a_table_beyond_32_bits(width):
+    """Rows of a table of more than 2^32 bytes and 2^31 elements, from the sums, the joined runs and both ways of clearing."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    vocabulary, n = 300000, 3000                                    # 4.9e9 bytes; more tokens than are looked through
+    t = torch.randint(vocabulary, (n,), generator=g, device="cuda")
+    t[::6] = vocabulary - 7                                         # runs across chunks, one beyond every border
+    t[1::12] = 3
+    t[2:2 + 9 * 13:9] = torch.tensor([0, vocabulary - 1, 262143, 262144, 262145, 131071, 131072, 2170, 2171, 2172, 2173, 2174, 290000], device="cuda")
+    grad = torch.randint(-1, 2, (n, width), generator=g, device="cuda").bfloat16()      # sums are exact, and rounded once
+    words, at = torch.unique(t, return_inverse=True)
+    want = torch.zeros((words.numel(), width), device="cuda").index_add_(0, at, grad.float()).bfloat16()
+    out = torch.full((vocabulary, width), 7.0, dtype=torch.bfloat16, device="cuda")
+    daf.embedding_grad(t, grad, vocabulary, out=out, check=True)
+    assert torch.equal(out[words], want)
+    out[words] = 0
+    for lo in range(0, vocabulary, 50000):
+        assert not out[lo:lo + 50000].any()
