@@ -109,3 +109,24 @@ def test_a_sorted_gradient_of_a_table_beyond_32_bits(width):
     out[words] = 0
     for lo in range(0, vocabulary, 50000):
         assert not out[lo:lo + 50000].any()
+
+
+# A weight's gradient is a sum over all rows in pieces: a group of lanes' own rows (of 296 CTAs of eight groups or more, eight heads at a time),
+# the groups of a CTA (256 at most), the CTAs (32 at a time), each piece in order.  Every addition of a chain of that length loses 2^-24 of
+# the magnitudes, and a term its own roundings.  The terms have one sign, so that a CTA's part that is lost is missed.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b,s,h,kv,d", [(64, 40, 12, 12, 64), (1, 2000, 24, 8, 32), (4, 1024, 16, 4, 128), (3, 700, 5, 3, 40)])
+def test_weight_gradients_are_sums_of_all_rows(dtype, b, s, h, kv, d):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k = (torch.randn((b, s, n, d), generator=g, device="cuda").to(dtype) for n in (h, kv))
+    gq, gk = ((x.sign() * torch.rand(x.shape, generator=g, device="cuda")).to(dtype) for x in (q, k))
+    w = torch.ones(d, device="cuda")
+    got = daf.rotary_norm_grad(q, k, w, w, gq, gk, rotary_dim=0)
+    for x, gx, made in ((q, gq, got[2]), (k, gk, got[3])):
+        x = x.double()
+        terms = gx.double() * x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)
+        want, rows = terms.sum((0, 1, 2)), b * s * x.shape[2]
+        chain = rows / (296 * 8) + 8 + min(256, rows) + 10 + 32
+        assert ((made.double() - want).abs() <= (chain + d / 2 + 12) * 2.0 ** -24 * terms.abs().sum((0, 1, 2))).all()
+        lost = terms.flatten(0, 2)[:max(1, rows // 296)].sum(0)       # what one CTA of them all adds
+        assert (lost > 4 * (chain + d / 2 + 12) * 2.0 ** -24 * want).all()
