@@ -12,8 +12,12 @@
 // by a hundred).  Relative error of the result in binary64 arithmetic with only these roundings (768 x 2304, spectra from flat to
 // strongly decaying): 1.3e-3 to 5.0e-3 with x rounded at the start, 0.9e-3 to 3.4e-3 so, and at most 1.4e-3 with the linear term
 // a x of the steps behind the first two taken from two float16 parts (the small singular values live there: what rounds the large
-// ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  float16 and binary32 matrices are held in
-// two parts throughout (three products instead of one): 7e-7.
+// ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  Where singular values are alike it is more,
+// because what rounds the diagonals of G and P then moves all of them the same way: bfloat16 results of 320 matrices of 33 to 1448 rows and
+// columns were 1.8e-3 to 2.9e-3 off in the middle of each of eight kinds of spectra and 4.6e-3 at worst (47 x 629, all equal).  Two parts of
+// G, P and x in the polynomial and the update would bring that below the rounding (computed: 1.5e-3 at most), at three products for one.
+// float16 and binary32 matrices are held in two parts throughout (three products instead of one): 7e-7, and with the sums 1e-6 (some
+// directions far stronger than others) to 4.2e-6 (all alike, 8192 x 48).
 //
 // One persistent kernel runs all products of all steps and matrices.  Pairs of CTAs take tiles of 256 x N by a ticket, in an order
 // in which whatever a tile needs comes before it; a tile waits until its matrix's tiles of the earlier products are done
@@ -34,9 +38,10 @@ constexpr uint32_t kOrthGroups = 16, kOrthMatrices = 192, kOrthSlots = 2;
 constexpr uint32_t kOrthBars = 1024, kOrthSmem = kOrthBars + kOrthStages * kOrthStage + 8u * kOrthOut;
 constexpr uint64_t kOrthBatch = 1ull << 27;     // elements of a batch, rows taken up to their pitch: bounds the workspace (8 to 16 bytes each)
 // Binary32: sums of 128 of the summed dimension are taken in tensor memory and added up in registers.  A tensor memory sum loses about two
-// units of its 24th bit at every addition, always downwards: 4096 columns of one row 2e-5 without, 5e-7 so; segments of 64 cost a fifth
-// of the time (results cannot run as far ahead), of 256 are 2.5 times as far off.  float16 does without up to 8192 rows or columns, where
-// the loss (4e-5) is far below the result's rounding: 403 us against 444 for the set of 768 and 2304.
+// units of its 24th bit at every addition of 16 products, always downwards (measured: all seventeen are cut two bits below the last of the
+// largest one's 24): 4096 columns of one row 2e-5 without, 5e-7 so; segments of 64 cost a fifth of the time (results cannot run as far
+// ahead), of 256 are 2.5 times as far off.  float16 does without up to 8192 rows or columns, where the loss (3e-5 to 6e-5) is far below the
+// result's rounding: 403 us against 444 for the set of 768 and 2304.
 constexpr uint32_t kOrthSegment = 2;            // copies of 64
 constexpr float kHeld = 4096.0f;                // G and P times this
 constexpr uint32_t kPrepUnits = 64;             // pieces of 256 columns of a row to a CTA of the preparing kernels
