@@ -550,13 +550,13 @@ daf_status daf_rotary_norm_grad(const daf_rotary_params *params, const double *f
  * elements; d_out[i] may be d_in[i], otherwise nothing overlaps.  Results have their input's type.
  * Arithmetic: products of 16-bit operands on the tensor cores, summed in binary32; the norm is summed in binary64.  DAF_BF16: x and
  * its Gram matrices are held in float16 between the products (x behind the first two steps with 22 bits where it is added).  Relative
- * to their norm results are then 1.8e-3 to 2.9e-3 off, 1.7e-3 of which is their own rounding, and up to 5e-3 where all singular values
- * are alike; for less, give binary32.  DAF_F16 and DAF_F32, and DAF_BF16 up to 32 rows or columns: in two float16 parts (22 bits)
- * throughout, 1e-6 to 5e-6 off before the result is rounded.  Matrices of up to 32 rows or columns and about 16000 elements are
- * computed in binary32, the smallest in binary64.  Entries below 2^-24 of a matrix's norm lose bits.  On the way x must stay below 7
- * in magnitude, x x^T and b (x x^T) + c (x x^T)^2 below 15 (the default coefficients keep them below 1.3, 1.6 and 2.9), otherwise the
- * result is not finite; neither is it for a matrix with an element that is not.  The same matrices give the same bits, alone or with
- * others.
+ * to their norm results are then 1.8e-3 to 3.2e-3 off (the least where a few directions stand out of noise, the most where a few are
+ * all there is), of which 1.7e-3 is their own rounding, and up to 5e-3 where all singular values are alike; for less, give binary32.
+ * DAF_F16 and DAF_F32, and DAF_BF16 up to 32 rows or columns: in two float16 parts (22 bits) throughout, 1e-6 to 5e-6 off before the
+ * result is rounded.  Matrices of up to 32 rows or columns and about 16000 elements are computed in binary32, the smallest in
+ * binary64.  Entries below 2^-24 of a matrix's norm lose bits.  On the way x must stay below 7 in magnitude, x x^T and
+ * b (x x^T) + c (x x^T)^2 below 15 (the default coefficients keep them below 1.3, 1.6 and 2.9), otherwise the result is not finite;
+ * neither is it for a matrix with an element that is not.  The same matrices give the same bits, alone or with others.
  * d_workspace: daf_orthogonalize_workspace(...) bytes (0 for bad arguments), 256-byte aligned, contents irrelevant; it holds the
  * device status word afterwards (daf_poll_status: DAF_OK, or DAF_ERR_TIMEOUT when a wait inside a kernel ran out).
  * rows, cols <= 65536, steps 1 to 64, coefficients and eps finite, eps > 0.

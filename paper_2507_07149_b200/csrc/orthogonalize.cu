@@ -12,10 +12,11 @@
 // by a hundred).  Relative error of the result in binary64 arithmetic with only these roundings (768 x 2304, spectra from flat to
 // strongly decaying): 1.3e-3 to 5.0e-3 with x rounded at the start, 0.9e-3 to 3.4e-3 so, and at most 1.4e-3 with the linear term
 // a x of the steps behind the first two taken from two float16 parts (the small singular values live there: what rounds the large
-// ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  Where singular values are alike it is more,
-// because what rounds the diagonals of G and P then moves all of them the same way: bfloat16 results of 320 matrices of 33 to 1448 rows and
-// columns were 1.8e-3 to 2.9e-3 off in the middle of each of eight kinds of spectra and 4.6e-3 at worst (47 x 629, all equal).  Two parts of
-// G, P and x in the polynomial and the update would bring that below the rounding (computed: 1.5e-3 at most), at three products for one.
+// ones away by 2^-12 is large next to them); rounding the result to bfloat16 is 1.7e-3.  Other spectra give more: an eighth of the directions
+// and next to nothing else, because the linear term of the last two steps is rounded; all alike, because what rounds the diagonals of G and P
+// moves all singular values the same way.  bfloat16 results of 650 matrices of 33 to 4000 rows and columns were 1.8e-3 to 3.2e-3 off in the
+// middle of each of eight kinds of spectra and 4.6e-3 at worst (47 x 629, all equal).  Two parts of G, P and x in the polynomial and the
+// update would bring that below the rounding (computed: 1.5e-3 at most), at three products for one.
 // float16 and binary32 matrices are held in two parts throughout (three products instead of one): 7e-7, and with the sums 1e-6 (some
 // directions far stronger than others) to 4.2e-6 (all alike, 8192 x 48).
 //
